@@ -463,6 +463,181 @@ TCL_API tcl_status tcl_trainer_timing_get(tcl_trainer* trainer, int32_t idx, con
                                           double* total_ms, int64_t* launches);
 TCL_API tcl_status tcl_trainer_timing_reset(tcl_trainer* trainer);
 
+/* ---------------------------------------------------------------------
+ * The sequence operators of the Mamba block (section 5.2) on their own, for
+ * models that carry their states: the causal convolution and the selective
+ * scan over prompts, over single tokens, and their gradients. The block's
+ * projections (x_proj, dt_proj) lie between the two and are the caller's.
+ *
+ * Conventions
+ *  - Activations are fp32 or bf16 (dtype), rows with a leading dimension ld >=
+ *    their columns; weights and the scan's states are fp32, the convolution's
+ *    states are of the activations' type. All arithmetic is fp32; results
+ *    are rounded to dtype once.
+ *  - Packed sequences: sequence i owns rows d_offs[i] .. d_offs[i+1]-1 (int32,
+ *    nondecreasing, in [0, rows]), any of them empty. Rows that no sequence
+ *    owns are neither read nor written. d_offs == NULL: every sequence is one
+ *    token, row i (rows == n_seq), the form for generating.
+ *  - States: sequence i starts from state d_slots[i] of a pool of n_slots
+ *    (d_slots == NULL: state i of n_seq), all zeros if the pool is NULL,
+ *    and its end state goes to the same place of the output pool, which may
+ *    be the same memory (and must not overlap otherwise). A slot outside
+ *    [0, n_slots) is a sequence without a state: it starts from zeros and
+ *    keeps nothing. The slots of one call that lie in the pool must be
+ *    distinct where an output pool is given. Other places of the output pool
+ *    are left as they are.
+ *  - Outputs must not overlap inputs (states aside) or each other.
+ *  - E in [1, 65536], d_state (N) 8 or 16, d_conv (K) in [1, 4]. Stream-ordered,
+ *    deterministic, no allocation; may be captured into a graph. Empty work
+ *    (n_seq == 0, or rows == 0 in the single-token form) is TCL_OK.
+ * ------------------------------------------------------------------- */
+
+/* u = SiLU(b + causal depthwise conv_K(x; w)): u_t = SiLU(b + sum_k w_k x_{t-K+1+k}),
+ * where the K-1 rows in front of a sequence are its state. The end state is the last
+ * K-1 rows of (state, sequence). */
+typedef struct tcl_ssm_conv_args {
+  int32_t dtype;         /* tcl_dtype                                        */
+  int32_t n_seq, rows;   /* sequences; rows of x                             */
+  int32_t E, K;          /* channels, taps                                   */
+  const int32_t* d_offs; /* [n_seq + 1] or NULL                              */
+  const void* d_x;       /* [rows, E], leading dimension ldx                 */
+  int64_t ldx;
+  const float* d_w;      /* [E, K], the last tap the token's own             */
+  const float* d_b;      /* [E] or NULL                                      */
+  const void* d_state;   /* [n_slots, K-1, E] states at the start, or NULL   */
+} tcl_ssm_conv_args;
+
+/* d_u [rows, E] with leading dimension ldu; d_state_out [n_slots, K-1, E] or NULL (not
+ * kept); d_slots [n_seq] int32 or NULL. */
+TCL_API tcl_status tcl_ssm_conv(const tcl_ssm_conv_args* args, const int32_t* d_slots, int32_t n_slots,
+                                void* d_state_out, void* d_u, int64_t ldu, void* stream);
+
+/* Gradients: d_du [rows, E] (lddu) and d_dstate_out [n_seq, K-1, E] (the gradient
+ * of the end states, NULL: zeros) to d_dx [rows, E] (lddx), d_dw [E, K] and d_db [E] (NULL:
+ * not wanted), both fp32 and overwritten, and d_dstate [n_seq, K-1, E] (the gradient of the
+ * states at the start, NULL: not wanted). State i belongs to sequence i (no slots).
+ * d_workspace: >= tcl_ssm_conv_workspace_bytes bytes, 256-byte aligned. */
+TCL_API size_t tcl_ssm_conv_workspace_bytes(int32_t n_seq, int32_t rows, int32_t E, int32_t K);
+TCL_API tcl_status tcl_ssm_conv_backward(const tcl_ssm_conv_args* args, const void* d_du, int64_t lddu,
+                                         const void* d_dstate_out, void* d_dx, int64_t lddx, float* d_dw,
+                                         float* d_db, void* d_dstate, void* d_workspace, size_t ws_bytes,
+                                         void* stream);
+
+/* The selective scan with its softplus in front and its gate behind:
+ *   d_t = softplus(dt_t + b_dt), A = -exp(A_log),
+ *   s_t = exp(d_t A) s_{t-1} + d_t u_t B_t,  y_t = (C_t . s_t + D u_t) SiLU(z_t).
+ * The states [E, N] of a sequence are fp32 throughout. */
+typedef struct tcl_ssm_scan_args {
+  int32_t dtype;         /* tcl_dtype                                        */
+  int32_t n_seq, rows;   /* sequences; rows of the activations               */
+  int32_t E, N;          /* channels, states per channel                     */
+  int32_t L;             /* no sequence is longer (with d_offs; it sizes the
+                            workspace, and decides how sequences are cut)    */
+  const int32_t* d_offs; /* [n_seq + 1] or NULL                              */
+  const void* d_u;       /* [rows, E], leading dimension ldu                 */
+  int64_t ldu;
+  const void* d_dt;      /* [rows, E], before bias and softplus              */
+  int64_t lddt;
+  const void* d_B;       /* [rows, N]                                        */
+  int64_t ldB;
+  const void* d_C;       /* [rows, N]                                        */
+  int64_t ldC;
+  const void* d_z;       /* [rows, E] or NULL (no gate)                      */
+  int64_t ldz;
+  const float* d_A_log;  /* [E, N], 16-byte aligned                          */
+  const float* d_D;      /* [E] or NULL (zeros)                              */
+  const float* d_b_dt;   /* [E] or NULL (zeros)                              */
+  const float* d_state;  /* [n_slots, E, N] states at the start, or NULL     */
+} tcl_ssm_scan_args;
+
+/* d_y [rows, E] with leading dimension ldy; d_state_out [n_slots, E, N] or NULL; both
+ * pools 16-byte aligned. d_workspace: >= tcl_ssm_scan_workspace_bytes bytes, 256-byte
+ * aligned; that is 0 (and d_workspace may be NULL) for batches of short or many sequences, and
+ * for single tokens (L = 1). Sequences longer than L give wrong results for
+ * themselves, and reach no memory that is not theirs. */
+TCL_API size_t tcl_ssm_scan_workspace_bytes(int32_t n_seq, int32_t rows, int32_t E, int32_t N, int32_t L);
+TCL_API tcl_status tcl_ssm_scan(const tcl_ssm_scan_args* args, const int32_t* d_slots, int32_t n_slots,
+                                float* d_state_out, void* d_y, int64_t ldy, void* d_workspace, size_t ws_bytes,
+                                void* stream);
+
+/* Where the gradients go. The activations' are of dtype, with leading
+ * dimensions; the parameters' are fp32, summed over all rows and overwritten. */
+typedef struct tcl_ssm_scan_grads {
+  void* d_du;       /* [rows, E] */
+  int64_t lddu;
+  void* d_ddt;      /* [rows, E] */
+  int64_t ldddt;
+  void* d_dB;       /* [rows, N] */
+  int64_t lddB;
+  void* d_dC;       /* [rows, N] */
+  int64_t lddC;
+  void* d_dz;       /* [rows, E]; NULL exactly when d_z is */
+  int64_t lddz;
+  float* d_dA_log;  /* [E, N] */
+  float* d_dD;      /* [E] or NULL (not wanted) */
+  float* d_db_dt;   /* [E] or NULL (not wanted) */
+  float* d_dstate;  /* [n_seq, E, N] gradient of the states at the start, or NULL */
+} tcl_ssm_scan_grads;
+
+/* Gradients of the scan from its inputs and d_dy [rows, E] (lddy); nothing is kept from
+ * the forward call. d_dstate_out [n_seq, E, N]: the gradient of the end states (NULL:
+ * zeros). State i belongs to sequence i (no slots). d_workspace: >=
+ * tcl_ssm_scan_backward_workspace_bytes bytes, 256-byte aligned. */
+TCL_API size_t tcl_ssm_scan_backward_workspace_bytes(int32_t n_seq, int32_t rows, int32_t E, int32_t N, int32_t L);
+TCL_API tcl_status tcl_ssm_scan_backward(const tcl_ssm_scan_args* args, const void* d_dy, int64_t lddy,
+                                         const float* d_dstate_out, const tcl_ssm_scan_grads* grads,
+                                         void* d_workspace, size_t ws_bytes, void* stream);
+
+/* ---------------------------------------------------------------------
+ * Operators on rows of logits: what a model answers with (log
+ * probabilities), and learning from a teacher's most likely answers. A row
+ * is V entries of an [n_rows, ld] array (d_seg_offsets NULL; entries are counted
+ * from the row's start), or a segment d_seg_offsets[g] .. d_seg_offsets[g+1]-1 of one
+ * array, V entries at most, as in tcl_topk (entries are counted from the
+ * array's start, ld is not used). Logits are fp32 or bf16 (dtype), of any
+ * alignment; arithmetic is fp32; temperature > 0 divides the logits. -inf is
+ * a masked entry, with no probability. V <= 2^30. Stream-ordered, deterministic, no
+ * allocation. d_workspace: >= tcl_logits_workspace_bytes(n_rows, V, K) bytes, 256-byte
+ * aligned; 0 bytes (d_workspace may be NULL) from 513 rows on. n_rows == 0 is TCL_OK.
+ * ------------------------------------------------------------------- */
+TCL_API size_t tcl_logits_workspace_bytes(int32_t n_rows, int32_t V, int32_t K);
+
+/* Log probabilities (natural logarithm) of p = softmax(logits / temperature):
+ *   d_logp [n_rows] fp32 (may be NULL): log p of entry d_tokens[r] (int32), NaN for an
+ *     entry outside the row;
+ *   d_entropy [n_rows] fp32 (may be NULL): -sum p log p;
+ *   d_top [n_rows, K] int32 and d_top_logp [n_rows, K] fp32 (may be NULL): the K most
+ *     likely entries and their log p, in tcl_topk's order: highest first, equal
+ *     logits by lower index, NaN after every number; -1 and -inf past the end of
+ *     a row with fewer than K entries. K in [0, 64]; 0: none (d_top may be NULL).
+ * NaN logits (unscored programs) are taken as masked. A row with nothing left
+ * (empty, or all masked) has entropy 0 and log p = -inf. A logit of +inf makes its
+ * row's values NaN. */
+TCL_API tcl_status tcl_logprobs(int32_t dtype, int32_t n_rows, int32_t V, const void* d_logits, int64_t ld,
+                                const int32_t* d_seg_offsets, float temperature, const int32_t* d_tokens, int32_t K,
+                                float* d_logp, float* d_entropy, int32_t* d_top, float* d_top_logp,
+                                void* d_workspace, size_t ws_bytes, void* stream);
+
+/* Distillation from a teacher's top logits: row r's teacher is known by K entries d_top
+ * [n_rows, K] int32 (tcl_topk's or tcl_logprobs' output, say) and its logits or log
+ * probabilities there, d_teacher [n_rows, K] fp32. With q = softmax of those / temperature and
+ * p = softmax(logits / temperature):
+ *   d_loss[r] = sum_k q_k (log q_k - log p_{top_k})        (fp32, [n_rows])
+ *   d_grad[r, v] = w_r / temperature (p_v - sum over k with top_k = v of q_k)
+ * d_weight [n_rows] fp32 (NULL: ones) is the gradient's factor w_r of each row (the loss is
+ * not weighted). d_grad (may be NULL) has the logits' type and layout with leading dimension
+ * ldg, and may be d_logits itself (ldg == ld). Entries of d_top outside the row (-1 past a short
+ * one) do not count; an entry listed twice counts with both probabilities. A row
+ * without any teacher's entry (none in the row, or all -inf), or with nothing left of its own (empty or
+ * all -inf), has loss 0 and gradient 0; the loss is +inf where the student masks an
+ * entry that the teacher does not. NaN in either's logits makes the row's
+ * results NaN. K in [1, 1024]. */
+TCL_API tcl_status tcl_distill_topk(int32_t dtype, int32_t n_rows, int32_t V, const void* d_logits, int64_t ld,
+                                    const int32_t* d_seg_offsets, float temperature, int32_t K,
+                                    const int32_t* d_top, const float* d_teacher, const float* d_weight,
+                                    float* d_loss, void* d_grad, int64_t ldg, void* d_workspace, size_t ws_bytes,
+                                    void* stream);
+
 /* Message describing the last failure on this thread ("" if none). */
 TCL_API const char* tcl_last_error(void);
 

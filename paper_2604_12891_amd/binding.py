@@ -45,7 +45,33 @@ class KDLoss(ctypes.Structure):
                 ("d_phi", ctypes.c_void_p)]
 
 
+class SsmConvArgs(ctypes.Structure):
+    """tcl_ssm_conv_args."""
+    _fields_ = [(n, ctypes.c_int32) for n in ("dtype", "n_seq", "rows", "E", "K")] + [
+        ("d_offs", ctypes.c_void_p), ("d_x", ctypes.c_void_p), ("ldx", ctypes.c_int64), ("d_w", ctypes.c_void_p),
+        ("d_b", ctypes.c_void_p), ("d_state", ctypes.c_void_p)]
+
+
+class SsmScanArgs(ctypes.Structure):
+    """tcl_ssm_scan_args."""
+    _fields_ = [(n, ctypes.c_int32) for n in ("dtype", "n_seq", "rows", "E", "N", "L")] + [
+        ("d_offs", ctypes.c_void_p), ("d_u", ctypes.c_void_p), ("ldu", ctypes.c_int64), ("d_dt", ctypes.c_void_p),
+        ("lddt", ctypes.c_int64), ("d_B", ctypes.c_void_p), ("ldB", ctypes.c_int64), ("d_C", ctypes.c_void_p),
+        ("ldC", ctypes.c_int64), ("d_z", ctypes.c_void_p), ("ldz", ctypes.c_int64), ("d_A_log", ctypes.c_void_p),
+        ("d_D", ctypes.c_void_p), ("d_b_dt", ctypes.c_void_p), ("d_state", ctypes.c_void_p)]
+
+
+class SsmScanGrads(ctypes.Structure):
+    """tcl_ssm_scan_grads."""
+    _fields_ = [("d_du", ctypes.c_void_p), ("lddu", ctypes.c_int64), ("d_ddt", ctypes.c_void_p),
+                ("ldddt", ctypes.c_int64), ("d_dB", ctypes.c_void_p), ("lddB", ctypes.c_int64),
+                ("d_dC", ctypes.c_void_p), ("lddC", ctypes.c_int64), ("d_dz", ctypes.c_void_p),
+                ("lddz", ctypes.c_int64), ("d_dA_log", ctypes.c_void_p), ("d_dD", ctypes.c_void_p),
+                ("d_db_dt", ctypes.c_void_p), ("d_dstate", ctypes.c_void_p)]
+
+
 _vp, _i32, _sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_size_t
+_i64, _f32 = ctypes.c_int64, ctypes.c_float
 _SIGS = {
     "tcl_param_count": (_sz, [ctypes.POINTER(Config)]),
     "tcl_cost_model_create": (_i32, [ctypes.POINTER(Config), _vp, _sz, ctypes.POINTER(_vp)]),
@@ -85,6 +111,19 @@ _SIGS = {
     "tcl_rdu_workspace_bytes": (_sz, [_i32, _i32]),
     "tcl_rdu_select": (_i32, [_i32, _vp, _vp, _i32, _vp, _i32, _i32, _vp, _vp, _vp, _sz, _vp]),
     "tcl_lambdarank": (_i32, [_i32, _vp, _vp, ctypes.c_float, _vp, _vp, _vp, _sz, _vp]),
+    "tcl_ssm_conv": (_i32, [ctypes.POINTER(SsmConvArgs), _vp, _i32, _vp, _vp, _i64, _vp]),
+    "tcl_ssm_conv_workspace_bytes": (_sz, [_i32] * 4),
+    "tcl_ssm_conv_backward": (_i32, [ctypes.POINTER(SsmConvArgs), _vp, _i64, _vp, _vp, _i64, _vp, _vp, _vp, _vp, _sz,
+                                     _vp]),
+    "tcl_ssm_scan_workspace_bytes": (_sz, [_i32] * 5),
+    "tcl_ssm_scan": (_i32, [ctypes.POINTER(SsmScanArgs), _vp, _i32, _vp, _vp, _i64, _vp, _sz, _vp]),
+    "tcl_ssm_scan_backward_workspace_bytes": (_sz, [_i32] * 5),
+    "tcl_ssm_scan_backward": (_i32, [ctypes.POINTER(SsmScanArgs), _vp, _i64, _vp, ctypes.POINTER(SsmScanGrads), _vp,
+                                     _sz, _vp]),
+    "tcl_logits_workspace_bytes": (_sz, [_i32] * 3),
+    "tcl_logprobs": (_i32, [_i32, _i32, _i32, _vp, _i64, _vp, _f32, _vp, _i32, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "tcl_distill_topk": (_i32, [_i32, _i32, _i32, _vp, _i64, _vp, _f32, _i32, _vp, _vp, _vp, _vp, _vp, _i64, _vp, _sz,
+                                _vp]),
     "tcl_trainer_timing_enable": (_i32, [_vp, _i32]),
     "tcl_trainer_timing_count": (_i32, [_vp]),
     "tcl_trainer_timing_get": (_i32, [_vp, _i32, ctypes.POINTER(ctypes.c_char_p), ctypes.POINTER(ctypes.c_double),
@@ -451,6 +490,298 @@ def lambdarank(scores, labels, sigma=1.0, grad=True, stream=None):
     check(lib().tcl_lambdarank(B, scores.data_ptr(), labels.data_ptr(), sigma, loss.data_ptr(), _ptr(g),
                                ws.data_ptr(), ws.numel(), _stream(stream)))
     return loss, g
+
+
+# ---------------------------------------------------------------------------
+# sequence and logit operators
+# ---------------------------------------------------------------------------
+
+def _dtype(t) -> int:
+    import torch
+    if t.dtype == torch.float32:
+        return TCL_F32
+    if t.dtype == torch.bfloat16:
+        return TCL_BF16
+    raise ValueError(f"fp32 or bf16 expected, not {t.dtype}")
+
+
+def _expect(name, t, dtype, shape, like, rows=False):
+    """t, when given, is a tensor of this type, shape and device; contiguous,
+    or (rows) with unit stride within its rows."""
+    if t is None:
+        return
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name}: {dtype} {tuple(shape)} expected, not {t.dtype} {tuple(t.shape)}")
+    if t.device != like.device:
+        raise ValueError(f"{name} is on {t.device}, not on {like.device}")
+    if rows:
+        ok = t.numel() == 0 or ((shape[1] == 1 or t.stride(1) == 1) and (shape[0] == 1 or t.stride(0) >= shape[1]))
+    else:
+        ok = t.is_contiguous()
+    if not ok:
+        raise ValueError(f"{name}: {'rows' if rows else 'tensor'} not contiguous (strides {t.stride()})")
+
+
+def _ld(t) -> int:
+    """Leading dimension of a matrix of rows (one row, or none, has any)."""
+    return max(t.stride(0), t.shape[1]) if t.shape[0] > 1 else t.shape[1]
+
+
+def _on_device(t):
+    import torch
+    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+        raise ValueError(f"tensors on {t.device}, which is not the current device")
+
+
+def _workspace(need, workspace, like):
+    """The caller's workspace, or one of `need` bytes."""
+    import torch
+    if workspace is not None:
+        if workspace.device != like.device or not workspace.is_contiguous():
+            raise ValueError(f"workspace: contiguous memory on {like.device} expected")
+        return workspace
+    return torch.empty(need, dtype=torch.uint8, device=like.device) if need else None
+
+
+def _ws_args(ws):
+    return (None, 0) if ws is None else (ws.data_ptr(), ws.numel() * ws.element_size())
+
+
+def _pools(state, state_out, slots, n_seq, shape, dtype, like):
+    """Checks a call's state pools; returns the number of places in them."""
+    import torch
+    for name, t in (("state", state), ("state_out", state_out)):
+        if t is not None:
+            if t.dim() != 1 + len(shape):
+                raise ValueError(f"{name}: {1 + len(shape)} dimensions expected, not {t.dim()}")
+            _expect(name, t, dtype, (t.shape[0], *shape), like)
+    if state is not None and state_out is not None and state.shape[0] != state_out.shape[0]:
+        raise ValueError(f"pools of {state.shape[0]} and {state_out.shape[0]} states")
+    _expect("slots", slots, torch.int32, (n_seq,), like)
+    pool = state if state is not None else state_out
+    return n_seq if pool is None else pool.shape[0]
+
+
+def _sequences(x, offs):
+    import torch
+    if x.dim() != 2:
+        raise ValueError(f"[rows, channels] expected, not {tuple(x.shape)}")
+    _on_device(x)
+    if offs is None:
+        return x.shape[0]
+    if offs.dim() != 1 or offs.numel() < 1:
+        raise ValueError("offs: [n_seq + 1] expected")
+    _expect("offs", offs, torch.int32, offs.shape, x)
+    return offs.numel() - 1
+
+
+def _conv_args(x, w, b, offs, n_seq, state):
+    import torch
+    rows, E = x.shape
+    if w.dim() != 2:
+        raise ValueError(f"w: [E, K] expected, not {tuple(w.shape)}")
+    _expect("x", x, x.dtype, (rows, E), x, rows=True)
+    _expect("w", w, torch.float32, (E, w.shape[1]), x)
+    _expect("b", b, torch.float32, (E,), x)
+    return SsmConvArgs(_dtype(x), n_seq, rows, E, w.shape[1], _ptr(offs), x.data_ptr(), _ld(x), w.data_ptr(), _ptr(b),
+                       _ptr(state))
+
+
+def ssm_conv(x, w, b=None, offs=None, state=None, state_out=None, slots=None, out=None, stream=None):
+    """u = SiLU(b + causal depthwise conv(x; w)) with carried states
+    (tcl_ssm_conv): x fp32 or bf16 [rows, E], w fp32 [E, K], b fp32 [E].
+    offs int32 [n_seq + 1]: packed sequences; None: each row is one token of its own
+    sequence. state / state_out [n, K-1, E] of x's type (may be the same tensor)
+    with slots int32 [n_seq] into them. Returns u [rows, E]."""
+    import torch
+    n_seq = _sequences(x, offs)
+    n_slots = _pools(state, state_out, slots, n_seq, (w.shape[1] - 1, x.shape[1]), x.dtype, x)
+    if out is None:
+        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    else:
+        _expect("out", out, x.dtype, x.shape, x, rows=True)
+    a = _conv_args(x, w, b, offs, n_seq, state)
+    check(lib().tcl_ssm_conv(ctypes.byref(a), _ptr(slots), n_slots, _ptr(state_out), out.data_ptr(), _ld(out),
+                             _stream(stream)))
+    return out
+
+
+def ssm_conv_workspace(n_seq, rows, E, K):
+    """A workspace for ssm_conv_backward, on the current device."""
+    import torch
+    return torch.empty(lib().tcl_ssm_conv_workspace_bytes(n_seq, rows, E, K), dtype=torch.uint8, device="cuda")
+
+
+def ssm_conv_backward(x, w, b, du, offs=None, state=None, state_grad=None, workspace=None, stream=None):
+    """Gradients of ssm_conv (tcl_ssm_conv_backward) from du [rows, E] and, for carried
+    states [n_seq, K-1, E], the gradient state_grad of the end states. Returns a
+    dict of dx, dw, db and dstate (None without a state)."""
+    import torch
+    n_seq = _sequences(x, offs)
+    K = w.shape[1]
+    for name, t in (("state", state), ("state_grad", state_grad)):
+        _expect(name, t, x.dtype, (n_seq, K - 1, x.shape[1]), x)
+    _expect("du", du, x.dtype, x.shape, x, rows=True)
+    a = _conv_args(x, w, b, offs, n_seq, state)
+    r = dict(dx=torch.empty(x.shape, dtype=x.dtype, device=x.device), dw=torch.empty_like(w),
+             db=torch.empty(x.shape[1], dtype=torch.float32, device=x.device),
+             dstate=None if state is None else torch.empty_like(state))
+    ws = _workspace(lib().tcl_ssm_conv_workspace_bytes(n_seq, x.shape[0], x.shape[1], K), workspace, x)
+    check(lib().tcl_ssm_conv_backward(ctypes.byref(a), du.data_ptr(), _ld(du), _ptr(state_grad), r["dx"].data_ptr(),
+                                      _ld(r["dx"]), r["dw"].data_ptr(), r["db"].data_ptr(), _ptr(r["dstate"]),
+                                      *_ws_args(ws), _stream(stream)))
+    return r
+
+
+def _scan_args(u, dt, A_log, B, C, D, z, b_dt, offs, n_seq, L, state):
+    import torch
+    rows, E = u.shape
+    if A_log.dim() != 2:
+        raise ValueError(f"A_log: [E, N] expected, not {tuple(A_log.shape)}")
+    N = A_log.shape[1]
+    for name, t, cols in (("u", u, E), ("dt", dt, E), ("B", B, N), ("C", C, N), ("z", z, E)):
+        _expect(name, t, u.dtype, (rows, cols), u, rows=True)
+    _expect("A_log", A_log, torch.float32, (E, N), u)
+    _expect("D", D, torch.float32, (E,), u)
+    _expect("b_dt", b_dt, torch.float32, (E,), u)
+    if L is None:
+        L = max(rows, 1) if offs is not None else 1
+    return SsmScanArgs(_dtype(u), n_seq, rows, E, N, L, _ptr(offs), u.data_ptr(), _ld(u), dt.data_ptr(), _ld(dt),
+                       B.data_ptr(), _ld(B), C.data_ptr(), _ld(C), _ptr(z), 0 if z is None else _ld(z),
+                       A_log.data_ptr(), _ptr(D), _ptr(b_dt), _ptr(state))
+
+
+def ssm_scan_workspace(n_seq, rows, E, N, L, backward=False):
+    """A workspace for ssm_scan (or ssm_scan_backward) with these sizes, on the
+    current device."""
+    import torch
+    f = lib().tcl_ssm_scan_backward_workspace_bytes if backward else lib().tcl_ssm_scan_workspace_bytes
+    return torch.empty(f(n_seq, rows, E, N, L), dtype=torch.uint8, device="cuda")
+
+
+def ssm_scan(u, dt, A_log, B, C, D=None, z=None, b_dt=None, offs=None, L=None, state=None, state_out=None, slots=None,
+             out=None, workspace=None, stream=None):
+    """The selective scan with carried states (tcl_ssm_scan): u, dt, z [rows, E]
+    and B, C [rows, N] fp32 or bf16, A_log [E, N], D, b_dt [E] and the states
+    [n, E, N] fp32. offs, slots as for ssm_conv; L bounds the sequences' lengths (None:
+    rows). Returns y [rows, E]."""
+    import torch
+    n_seq = _sequences(u, offs)
+    n_slots = _pools(state, state_out, slots, n_seq, A_log.shape, torch.float32, u)
+    a = _scan_args(u, dt, A_log, B, C, D, z, b_dt, offs, n_seq, L, state)
+    if out is None:
+        out = torch.empty(u.shape, dtype=u.dtype, device=u.device)
+    else:
+        _expect("out", out, u.dtype, u.shape, u, rows=True)
+    need = 0 if offs is None else lib().tcl_ssm_scan_workspace_bytes(n_seq, a.rows, a.E, a.N, a.L)
+    ws = _workspace(need, workspace, u)
+    check(lib().tcl_ssm_scan(ctypes.byref(a), _ptr(slots), n_slots, _ptr(state_out), out.data_ptr(), _ld(out),
+                             *_ws_args(ws), _stream(stream)))
+    return out
+
+
+def ssm_scan_backward(u, dt, A_log, B, C, dy, D=None, z=None, b_dt=None, offs=None, L=None, state=None,
+                      state_grad=None, workspace=None, stream=None):
+    """Gradients of ssm_scan (tcl_ssm_scan_backward) from dy [rows, E] and, for carried
+    states [n_seq, E, N], the gradient state_grad of the end states. Returns a dict of
+    du, ddt, dB, dC, dz (None without z), dA_log, dD, db_dt and dstate (None without a
+    state)."""
+    import torch
+    n_seq = _sequences(u, offs)
+    for name, t in (("state", state), ("state_grad", state_grad)):
+        _expect(name, t, torch.float32, (n_seq, *A_log.shape), u)
+    _expect("dy", dy, u.dtype, u.shape, u, rows=True)
+    a = _scan_args(u, dt, A_log, B, C, D, z, b_dt, offs, n_seq, L, state)
+
+    def new(*shape, dtype=u.dtype):
+        return torch.empty(shape, dtype=dtype, device=u.device)
+
+    rows, E, N, f32 = a.rows, a.E, a.N, torch.float32
+    r = dict(du=new(rows, E), ddt=new(rows, E), dz=None if z is None else new(rows, E), dB=new(rows, N),
+             dC=new(rows, N), dA_log=new(E, N, dtype=f32), dD=new(E, dtype=f32), db_dt=new(E, dtype=f32),
+             dstate=None if state is None else new(n_seq, E, N, dtype=f32))
+    g = SsmScanGrads(r["du"].data_ptr(), E, r["ddt"].data_ptr(), E, r["dB"].data_ptr(), N, r["dC"].data_ptr(), N,
+                     _ptr(r["dz"]), E, r["dA_log"].data_ptr(), r["dD"].data_ptr(), r["db_dt"].data_ptr(),
+                     _ptr(r["dstate"]))
+    ws = _workspace(lib().tcl_ssm_scan_backward_workspace_bytes(n_seq, rows, E, N, a.L), workspace, u)
+    check(lib().tcl_ssm_scan_backward(ctypes.byref(a), dy.data_ptr(), _ld(dy), _ptr(state_grad), ctypes.byref(g),
+                                      *_ws_args(ws), _stream(stream)))
+    return r
+
+
+def logits_workspace(n_rows, V, K):
+    """A workspace for logprobs and distill_topk with these sizes, on the
+    current device."""
+    import torch
+    return torch.empty(lib().tcl_logits_workspace_bytes(n_rows, V, K), dtype=torch.uint8, device="cuda")
+
+
+def _logit_rows(logits, seg_offsets, max_len):
+    """(rows, V, leading dimension) of rows [n, V], or of ragged segments of a
+    one-dimensional array."""
+    import torch
+    _on_device(logits)
+    if seg_offsets is None:
+        if logits.dim() != 2:
+            raise ValueError(f"[rows, V] logits expected, not {tuple(logits.shape)}")
+        _expect("logits", logits, logits.dtype, logits.shape, logits, rows=True)
+        return logits.shape[0], logits.shape[1], _ld(logits)
+    if logits.dim() != 1 or seg_offsets.dim() != 1 or seg_offsets.numel() < 1:
+        raise ValueError("segments: logits [n] and seg_offsets [n_seg + 1] expected")
+    _expect("logits", logits, logits.dtype, logits.shape, logits)
+    _expect("seg_offsets", seg_offsets, torch.int32, seg_offsets.shape, logits)
+    return seg_offsets.numel() - 1, max(logits.numel(), 1) if max_len is None else max_len, 0
+
+
+def logprobs(logits, tokens=None, K=0, temperature=1.0, seg_offsets=None, max_len=None, workspace=None, stream=None):
+    """Log probabilities of the given tokens, entropy and the K top alternatives
+    (tcl_logprobs): logits fp32 or bf16 [rows, V], or [n] with seg_offsets int32 [rows + 1]
+    (segments of max_len entries at most; indices then count from the array's start, as
+    topk's do); tokens int32 [rows]. Returns a dict of logp (None without tokens), entropy,
+    top [rows, K] int32 and top_logp [rows, K] (None for K = 0)."""
+    import torch
+    n, V, ld = _logit_rows(logits, seg_offsets, max_len)
+    _expect("tokens", tokens, torch.int32, (n,), logits)
+
+    def new(*shape, dtype=torch.float32):
+        return torch.empty(shape, dtype=dtype, device=logits.device)
+
+    r = dict(logp=None if tokens is None else new(n), entropy=new(n), top=new(n, K, dtype=torch.int32) if K else None,
+             top_logp=new(n, K) if K else None)
+    ws = _workspace(lib().tcl_logits_workspace_bytes(n, V, K), workspace, logits)
+    check(lib().tcl_logprobs(_dtype(logits), n, V, logits.data_ptr(), ld, _ptr(seg_offsets), temperature,
+                             _ptr(tokens), K, _ptr(r["logp"]), r["entropy"].data_ptr(), _ptr(r["top"]),
+                             _ptr(r["top_logp"]), *_ws_args(ws), _stream(stream)))
+    return r
+
+
+def distill_topk(logits, top, teacher, weight=None, temperature=1.0, seg_offsets=None, max_len=None, grad=True,
+                 workspace=None, stream=None):
+    """Distillation from a teacher's top logits (tcl_distill_topk): the student's
+    logits as for logprobs, top int32 and teacher fp32 [rows, K], weight fp32 [rows] (the
+    gradient's factor of each row). grad: True (a new tensor), False (the loss
+    alone), or the tensor that takes it, which may be logits itself. Returns a dict
+    of loss [rows] fp32 and grad (None if not wanted)."""
+    import torch
+    n, V, ld = _logit_rows(logits, seg_offsets, max_len)
+    if top.dim() != 2:
+        raise ValueError(f"top: [rows, K] expected, not {tuple(top.shape)}")
+    K = top.shape[1]
+    _expect("top", top, torch.int32, (n, K), logits)
+    _expect("teacher", teacher, torch.float32, (n, K), logits)
+    _expect("weight", weight, torch.float32, (n,), logits)
+    if grad is True:
+        grad = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+    elif grad is False:
+        grad = None
+    _expect("grad", grad, logits.dtype, logits.shape, logits, rows=seg_offsets is None)
+    ldg = _ld(grad) if grad is not None and seg_offsets is None else 0
+    loss = torch.empty(n, dtype=torch.float32, device=logits.device)
+    ws = _workspace(lib().tcl_logits_workspace_bytes(n, V, K), workspace, logits)
+    check(lib().tcl_distill_topk(_dtype(logits), n, V, logits.data_ptr(), ld, _ptr(seg_offsets), temperature, K,
+                                 top.data_ptr(), teacher.data_ptr(), _ptr(weight), loss.data_ptr(), _ptr(grad), ldg,
+                                 *_ws_args(ws), _stream(stream)))
+    return dict(loss=loss, grad=grad)
 
 
 def teacher_gate(e, out=None, stream=None):

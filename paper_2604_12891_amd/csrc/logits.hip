@@ -1,0 +1,716 @@
+// Operators on rows of logits: log probabilities of given entries with the
+// row's entropy and top alternatives, and distillation from a teacher's top
+// logits (loss and gradient).
+//
+// A row is read in aligned 16-byte vectors whatever its own alignment: vector v
+// covers entries v VE - h .. v VE - h + VE - 1, h the entries between the
+// aligned address and the row's start, and only the first and the last vector of a
+// row are read entry by entry.
+#include <algorithm>
+
+#include "common.h"
+#include "ops.h"
+
+namespace tcl {
+namespace {
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned long long u64;
+
+constexpr int kTB = 256;  // threads of the streaming kernels
+
+__device__ __forceinline__ float wave_max(float v) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
+  return v;
+}
+
+// A row's entries (or a part of it): VE to a vector.
+template <typename T>
+struct Row {
+  static constexpr int VE = 16 / sizeof(T);
+  const T* p;   // the first entry
+  int cnt;      // entries
+  int first;    // index of the first one as the caller counts
+  int h;        // entries in front of p in its aligned vector
+  int nvec;
+
+  __device__ __forceinline__ Row(const LogitRows& a, int r) {
+    const int64_t o = a.offs ? a.offs[r] : (int64_t)r * a.ld;
+    p = static_cast<const T*>(a.x) + o;
+    cnt = a.offs ? max(a.offs[r + 1] - a.offs[r], 0) : a.V;
+    first = a.offs ? a.offs[r] : 0;
+    h = (int)((reinterpret_cast<uintptr_t>(p) / sizeof(T)) % VE);
+    nvec = cnt > 0 ? (cnt + h + VE - 1) / VE : 0;
+  }
+  __device__ __forceinline__ bool whole(int v) const { return v * VE >= h && v * VE - h + VE <= cnt; }
+  // raw vector v; entries outside the row are -inf
+  __device__ __forceinline__ u32x4 load(int v) const {
+    if (whole(v)) return *reinterpret_cast<const u32x4*>(p + (v * VE - h));
+    u32x4 x;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if constexpr (sizeof(T) == 4) {
+        const int i = v * VE - h + k;
+        x[k] = i >= 0 && i < cnt ? __float_as_uint(p[i]) : 0xFF800000u;
+      } else {
+        const int i = v * VE - h + 2 * k;
+        const uint32_t lo = i >= 0 && i < cnt ? p[i] : 0xFF80u, hi = i + 1 >= 0 && i + 1 < cnt ? p[i + 1] : 0xFF80u;
+        x[k] = lo | hi << 16;
+      }
+    }
+    return x;
+  }
+  static __device__ __forceinline__ float get(u32x4 x, int i) {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(x[i]);
+    else return __uint_as_float(i & 1 ? x[i >> 1] & 0xFFFF0000u : x[i >> 1] << 16);
+  }
+  __device__ __forceinline__ float at(int i) const {
+    if constexpr (sizeof(T) == 4) return p[i];
+    else return bf16_to_f32(p[i]);
+  }
+};
+
+// ---------------------------------------------------------------- order of entries
+// One number per entry that orders as the top list does: by value, NaN after
+// every number, equal values by lower index. 0: no entry.
+__device__ __forceinline__ u64 key_of(float x, int i) {
+  uint32_t u = __float_as_uint(x + 0.0f);  // -0 as 0
+  u = u & 0x80000000u ? ~u : u | 0x80000000u;
+  if (!(x == x)) u = 0;
+  return (u64)u << 32 | (uint32_t)~i;
+}
+__device__ __forceinline__ int key_index(u64 k) { return (int)~(uint32_t)k; }
+__device__ __forceinline__ float key_value(u64 k) {  // NaN comes back as -inf
+  const uint32_t u = (uint32_t)(k >> 32);
+  if (u == 0) return -INFINITY;
+  return __uint_as_float(u & 0x80000000u ? u & 0x7FFFFFFFu : ~u);
+}
+
+// ---------------------------------------------------------------- sums of a softmax
+// m = max x, s = sum e, t = sum (x - m) e, e = exp((x - m) / temperature); zc = log2(e) / temperature.
+struct Stats {
+  float m, s, t;
+};
+__device__ __forceinline__ Stats merge(Stats a, Stats b, float zc) {
+  const float m = fmaxf(a.m, b.m);
+  Stats r = {m, 0.f, 0.f};
+  // (a part whose maximum is a type's lowest value may have d s beyond fp32, and f 0)
+  if (a.m > -INFINITY) {
+    const float d = a.m == m ? 0.f : a.m - m, f = __builtin_amdgcn_exp2f(d * zc);
+    r.s = f * a.s;
+    r.t = f > 0.f ? f * fmaf(d, a.s, a.t) : 0.f;
+  }
+  if (b.m > -INFINITY) {
+    const float d = b.m == m ? 0.f : b.m - m, f = __builtin_amdgcn_exp2f(d * zc);
+    r.s = fmaf(f, b.s, r.s);
+    if (f > 0.f) r.t = fmaf(f, fmaf(d, b.s, b.t), r.t);
+  }
+  return r;
+}
+__device__ __forceinline__ Stats wave_merge(Stats a, float zc) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) {
+    const Stats b = {__shfl_xor(a.m, o, 64), __shfl_xor(a.s, o, 64), __shfl_xor(a.t, o, 64)};
+    a = merge(a, b, zc);
+  }
+  return a;
+}
+
+// ---------------------------------------------------------------- the K highest
+// Finding the K highest costs one comparison per vector while the row streams by:
+// every thread keeps its own highest entry. Of those kTB keys the K-th highest is a bound
+// tau that at least K entries reach, and an entry that reaches it lies with one of the
+// K threads whose highest does; only their entries are read again (a share K / kTB of
+// the row, out of the caches), the ones >= tau go to a list in LDS, some K to
+// 8 K of them, and each entry of the list counts the ones above it for its rank. A list that
+// overflows (rows made of many near-copies of one stretch) takes the exact K-th
+// key by bisection over its 64 bits instead.
+constexpr int kCap = 1024;
+constexpr int kMaxTop = 64;
+
+struct TopShared {
+  u64 key[kTB];
+  u64 cand[kCap];
+  u64 best[kMaxTop];
+  int sel[kMaxTop];
+  int n, nsel;
+  u64 tau;
+};
+
+// From every thread's highest key (0: none): tau, the threads that reach it.
+__device__ __forceinline__ void top_threads(TopShared& sh, u64 key, int K) {
+  const int tid = threadIdx.x;
+  sh.key[tid] = key;
+  if (tid == 0) {
+    sh.n = 0;
+    sh.nsel = 0;
+    sh.tau = 1;  // fewer than K threads have an entry: all entries
+  }
+  if (tid < K) sh.best[tid] = 0;
+  __syncthreads();
+  int above = 0;
+#pragma unroll 8
+  for (int i = 0; i < kTB; i += 2) {
+    const ulonglong2 k2 = *reinterpret_cast<const ulonglong2*>(&sh.key[i]);
+    above += (k2.x > key) + (k2.y > key);
+  }
+  if (key && above < K) {
+    sh.sel[above] = tid;
+    atomicAdd(&sh.nsel, 1);
+    if (above == K - 1) sh.tau = key;
+  }
+  __syncthreads();
+}
+
+// The K highest of the keys that each(f) hands to f on all threads together, into
+// sh.best, highest first. All of them reach sh.tau's entries; sh.n starts at 0.
+template <typename Each>
+__device__ __forceinline__ void top_collect(TopShared& sh, int K, Each each) {
+  const int tid = threadIdx.x;
+  u64 tau = sh.tau;
+  each([&](u64 k) {
+    if (k >= tau) {
+      const int p = atomicAdd(&sh.n, 1);
+      if (p < kCap) sh.cand[p] = k;
+    }
+  });
+  __syncthreads();
+  int n = sh.n;
+  if (n > kCap) {
+    u64 lo = 0;  // at least K keys reach lo
+    for (int bit = 63; bit >= 0; --bit) {
+      const u64 trial = lo | 1ull << bit;
+      int c = 0;
+      each([&](u64 k) { c += k >= trial; });
+      __syncthreads();
+      if (tid == 0) sh.n = 0;
+      __syncthreads();
+      if (c) atomicAdd(&sh.n, c);
+      __syncthreads();
+      if (sh.n >= K) lo = trial;
+    }
+    __syncthreads();
+    if (tid == 0) sh.n = 0;
+    __syncthreads();
+    each([&](u64 k) {
+      if (k >= lo) {
+        const int p = atomicAdd(&sh.n, 1);
+        if (p < kCap) sh.cand[p] = k;
+      }
+    });
+    __syncthreads();
+    n = min(sh.n, kCap);
+  }
+  for (int i = tid; i < n; i += kTB) {
+    const u64 k = sh.cand[i];
+    int above = 0;
+    for (int j = 0; j < n; ++j) above += sh.cand[j] > k;
+    if (above < K) sh.best[above] = k;
+  }
+  __syncthreads();
+}
+
+// What leaves for one row.
+struct LogprobOut {
+  const int* tokens;
+  float *logp, *entropy;
+  int* top;
+  float* top_logp;
+};
+
+template <typename T>
+__device__ __forceinline__ void finish_row(const LogitRows& a, const Row<T>& row, int r, Stats st, const TopShared& sh,
+                                           int K, const LogprobOut& o) {
+  const float ls = logf(st.s);  // -inf for a row with nothing left
+  const bool none = !(st.m > -INFINITY);
+  auto logp = [&](float x) { return none || !(x > -INFINITY) ? -INFINITY : fmaf(x - st.m, a.inv_temp, -ls); };
+  if (threadIdx.x == 0) {
+    if (o.logp) {
+      const int64_t i = (int64_t)o.tokens[r] - row.first;
+      o.logp[r] = i >= 0 && i < row.cnt ? logp(row.at((int)i)) : NAN;
+    }
+    if (o.entropy) o.entropy[r] = none ? 0.f : fmaf(-a.inv_temp, st.t / st.s, ls);
+  }
+  if ((int)threadIdx.x < K) {
+    const u64 k = sh.best[threadIdx.x];
+    const int64_t j = (int64_t)r * K + threadIdx.x;
+    o.top[j] = k ? key_index(k) + row.first : -1;
+    if (o.top_logp) o.top_logp[j] = k ? logp(key_value(k)) : -INFINITY;
+  }
+}
+
+// A split's results in the workspace: the K highest keys, then the sums.
+__device__ __forceinline__ int64_t split_stride(int K) { return (int64_t)K * 8 + 16; }
+
+// One pass over a row (or the part of it that blockIdx.y names): running maximum with
+// the sums rescaled when it rises, once per vector at most. Bound by HBM from a
+// few thousand entries on. gridDim.y == 1: the row's results leave from here.
+template <typename T>
+__global__ __launch_bounds__(kTB) void logprobs_kernel(LogitRows a, int K, LogprobOut o, char* __restrict__ ws) {
+  constexpr int VE = Row<T>::VE;
+  __shared__ __attribute__((aligned(16))) TopShared sh;
+  __shared__ Stats part[kTB / 64];
+  const int r = blockIdx.x, tid = threadIdx.x;
+  const Row<T> row(a, r);
+  const int per = (row.nvec + gridDim.y - 1) / gridDim.y;
+  const int v0 = min((int)blockIdx.y * per, row.nvec), v1 = min(v0 + per, row.nvec);
+  const float zc = a.inv_temp * kLog2e;
+  Stats st = {-INFINITY, 0.f, 0.f};
+  float best = -INFINITY;
+  int bv = -1;
+  constexpr int U = 4;
+  for (int vb = v0 + tid; vb < v1; vb += U * kTB) {
+    u32x4 x[U];
+#pragma unroll
+    for (int k = 0; k < U; ++k)
+      if (vb + k * kTB < v1) x[k] = row.load(vb + k * kTB);
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+      if (vb + k * kTB >= v1) break;
+      float f[VE], vm = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < VE; ++i) {
+        f[i] = Row<T>::get(x[k], i);
+        vm = fmaxf(vm, f[i]);
+      }
+      if (vm > best) {
+        best = vm;
+        bv = vb + k * kTB;
+        // the sums move to the new maximum
+        if (st.m > -INFINITY) {
+          const float d = st.m - vm, g = __builtin_amdgcn_exp2f(d * zc);
+          st.t = g > 0.f ? g * fmaf(d, st.s, st.t) : 0.f;
+          st.s *= g;
+        }
+        st.m = vm;
+      }
+      if (st.m > -INFINITY) {
+#pragma unroll
+        for (int i = 0; i < VE; ++i) {
+          const float d = fmaxf(f[i] - st.m, -3.0e38f);  // -inf and NaN: no probability
+          const float e = __builtin_amdgcn_exp2f(d * zc);
+          st.s += e;
+          st.t = fmaf(d, e, st.t);
+        }
+      }
+    }
+  }
+  st = wave_merge(st, zc);
+  if ((tid & 63) == 0) part[tid >> 6] = st;
+  __syncthreads();
+  st = part[0];
+#pragma unroll
+  for (int k = 1; k < kTB / 64; ++k) st = merge(st, part[k], zc);
+
+  if (K > 0) {
+    auto vec_keys = [&](int v, auto f) {
+      const u32x4 x = row.load(v);
+#pragma unroll
+      for (int i = 0; i < VE; ++i) {
+        const int j = v * VE - row.h + i;
+        if (j >= 0 && j < row.cnt) f(key_of(Row<T>::get(x, i), j));
+      }
+    };
+    u64 key = 0;
+    if (bv >= 0) {
+      vec_keys(bv, [&](u64 k) { key = max(key, k); });
+    } else {  // nothing above -inf: the order among -inf and NaN
+      for (int v = v0 + tid; v < v1; v += kTB) vec_keys(v, [&](u64 k) { key = max(key, k); });
+    }
+    top_threads(sh, key, K);
+    // the vectors of the threads that reach tau, shared out over all threads
+    const int each_n = (v1 - v0 + kTB - 1) / kTB, units = sh.nsel * each_n;
+    top_collect(sh, K, [&](auto f) {
+      for (int q = tid; q < units; q += kTB) {
+        const int v = v0 + sh.sel[q / each_n] + q % each_n * kTB;
+        if (v < v1) vec_keys(v, f);
+      }
+    });
+  }
+  if (gridDim.y == 1) {
+    finish_row(a, row, r, st, sh, K, o);
+    return;
+  }
+  char* w = ws + ((int64_t)r * gridDim.y + blockIdx.y) * split_stride(K);
+  if (tid < K) reinterpret_cast<u64*>(w)[tid] = sh.best[tid];
+  if (tid == 0) *reinterpret_cast<Stats*>(w + (int64_t)K * 8) = st;
+}
+
+// The splits of a row joined: one workgroup per row.
+template <typename T>
+__global__ __launch_bounds__(kTB) void logprobs_join_kernel(LogitRows a, int K, int splits, LogprobOut o,
+                                                            const char* __restrict__ ws) {
+  __shared__ __attribute__((aligned(16))) TopShared sh;
+  __shared__ Stats part[kTB / 64];
+  const int r = blockIdx.x, tid = threadIdx.x;
+  const Row<T> row(a, r);
+  const float zc = a.inv_temp * kLog2e;
+  const char* w = ws + (int64_t)r * splits * split_stride(K);
+  Stats st = {-INFINITY, 0.f, 0.f};
+  for (int k = tid; k < splits; k += kTB)
+    st = merge(st, *reinterpret_cast<const Stats*>(w + k * split_stride(K) + (int64_t)K * 8), zc);
+  st = wave_merge(st, zc);
+  if ((tid & 63) == 0) part[tid >> 6] = st;
+  __syncthreads();
+  st = part[0];
+#pragma unroll
+  for (int k = 1; k < kTB / 64; ++k) st = merge(st, part[k], zc);
+  if (K > 0) {
+    auto each = [&](auto f) {
+      for (int q = tid; q < splits * K; q += kTB) {
+        const u64 k = reinterpret_cast<const u64*>(w + q / K * split_stride(K))[q % K];
+        if (k) f(k);
+      }
+    };
+    u64 key = 0;
+    each([&](u64 k) { key = max(key, k); });
+    top_threads(sh, key, K);
+    top_collect(sh, K, each);
+  }
+  finish_row(a, row, r, st, sh, K, o);
+}
+
+// ---------------------------------------------------------------- distillation from top logits
+// q = softmax of the teacher's K logits, p = softmax of the student's row, both at 1 / inv_temp:
+//   loss = sum_k q_k (log q_k - log p_(i_k)),  dloss/dx_v = inv_temp (p_v - sum_k [i_k = v] q_k).
+// Entries without a place in the row (index outside it) do not count. A row without any
+// teacher's entry, or whose own entries are all -inf, has loss 0 and gradient 0.
+struct TeacherArgs {
+  int K;
+  const int* top;
+  const float* val;
+  const float* weight;
+  float* loss;
+  void* grad;
+  int64_t ldg;
+};
+
+template <int NW>
+__device__ __forceinline__ float block_max(float v, float* red) {
+  v = wave_max(v);
+  if (NW > 1) {
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = red[0];
+#pragma unroll
+    for (int k = 1; k < NW; ++k) v = fmaxf(v, red[k]);
+  }
+  return v;
+}
+template <int NW>
+__device__ __forceinline__ float block_sum(float v, float* red) {
+  v = wave_sum(v);
+  if (NW > 1) {
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = red[0];
+#pragma unroll
+    for (int k = 1; k < NW; ++k) v += red[k];
+  }
+  return v;
+}
+
+constexpr int kMaxTeacher = 1024;
+struct TeacherShared {
+  float x[kMaxTeacher];   // the student's logit at the entry
+  float q[kMaxTeacher];   // the teacher's probability
+  int at[kMaxTeacher];    // its place in the row, -1: none
+  float red[16];
+};
+
+// The teacher's distribution of a row, and the student's logits at its entries
+// (read here, before a gradient may replace them). Returns whether there is one.
+template <typename T, int NW>
+__device__ __forceinline__ bool teacher_row(TeacherShared& sh, const Row<T>& row, const TeacherArgs& t, int r,
+                                            float inv_temp, const float* sx) {
+  float m = -INFINITY;
+  bool bad = false;
+  for (int k = threadIdx.x; k < t.K; k += 64 * NW) {
+    const int64_t j = (int64_t)t.top[(int64_t)r * t.K + k] - row.first;
+    const bool have = j >= 0 && j < row.cnt && t.top[(int64_t)r * t.K + k] >= 0;
+    const float v = t.val[(int64_t)r * t.K + k];
+    sh.at[k] = have ? (int)j : -1;
+    sh.q[k] = have ? v * inv_temp : -INFINITY;
+    if (have) bad |= !(v < INFINITY);  // NaN or +inf
+    sh.x[k] = sx ? sx[k] : have ? row.at((int)j) : -INFINITY;
+    m = fmaxf(m, sh.q[k]);
+  }
+  m = block_max<NW>(bad ? INFINITY : m, sh.red);
+  float s = 0.f;
+  for (int k = threadIdx.x; k < t.K; k += 64 * NW) s += m > -INFINITY ? expf(sh.q[k] - m) : 0.f;
+  s = block_sum<NW>(s, sh.red);
+  const float ls = m + logf(s);  // m = +inf: NaN, and so is everything that follows
+  for (int k = threadIdx.x; k < t.K; k += 64 * NW) sh.q[k] -= ls;  // log q until teacher_loss
+  return m > -INFINITY;
+}
+
+// The loss; sh.q becomes q. ms: the student's maximum, ls: log of its sum.
+template <int NW>
+__device__ __forceinline__ float teacher_loss(TeacherShared& sh, int K, float ms, float ls, float inv_temp) {
+  float loss = 0.f;
+  for (int k = threadIdx.x; k < K; k += 64 * NW) {
+    const float lq = sh.q[k], q = sh.at[k] >= 0 ? expf(lq) : 0.f;
+    sh.q[k] = q;
+    if (q != 0.f) loss += q * (lq - fmaf(sh.x[k] - ms, inv_temp, -ls));
+  }
+  return block_sum<NW>(loss, sh.red);
+}
+
+// Entry k of the list, if it is the first of its place: all the teacher's
+// probability there, by a loop over the list.
+__device__ __forceinline__ bool teacher_place(const TeacherShared& sh, int K, int k, float& q) {
+  const int at = sh.at[k];
+  if (at < 0) return false;
+  q = 0.f;
+  for (int j = 0; j < K; ++j)
+    if (sh.at[j] == at) {
+      if (j < k) return false;
+      q += sh.q[j];
+    }
+  return true;
+}
+
+__device__ __forceinline__ void st_grad(float* p, float v) { *p = v; }
+__device__ __forceinline__ void st_grad(uint16_t* p, float v) { *p = f32_to_bf16(v); }
+
+// Gradient vector v of a row out of its raw logits, f(x) each.
+template <typename T, typename F>
+__device__ __forceinline__ void grad_vec(const Row<T>& row, T* g, bool same, int v, u32x4 x, F f) {
+  constexpr int VE = Row<T>::VE;
+  if (same && row.whole(v)) {
+    u32x4 o;
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[i] = __float_as_uint(f(__uint_as_float(x[i])));
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[i] = f32x2_to_bf16x2(f(Row<T>::get(x, 2 * i)), f(Row<T>::get(x, 2 * i + 1)));
+    }
+    *reinterpret_cast<u32x4*>(g + (v * VE - row.h)) = o;
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < VE; ++i) {
+    const int j = v * VE - row.h + i;
+    if (j >= 0 && j < row.cnt) st_grad(g + j, f(Row<T>::get(x, i)));
+  }
+}
+
+template <typename T>
+__device__ __forceinline__ T* grad_row(const LogitRows& a, const TeacherArgs& t, int r) {
+  return static_cast<T*>(t.grad) + (a.offs ? (int64_t)a.offs[r] : (int64_t)r * t.ldg);
+}
+template <typename T>
+__device__ __forceinline__ bool same_phase(const Row<T>& row, const T* g) {
+  return (int)((reinterpret_cast<uintptr_t>(g) / sizeof(T)) % Row<T>::VE) == row.h;
+}
+
+// One workgroup per row, the row's NV x 64 NW vectors held in registers from the one
+// time they are read until the gradient leaves; of longer rows the rest is read
+// again for each of the three passes. Bound by HBM: each entry read and written once.
+template <typename T, int NW, int NV>
+__global__ __launch_bounds__(64 * NW) void distill_row_kernel(LogitRows a, TeacherArgs t) {
+  constexpr int VE = Row<T>::VE, TB = 64 * NW;
+  __shared__ TeacherShared sh;
+  const int r = blockIdx.x, tid = threadIdx.x;
+  const Row<T> row(a, r);
+  const float zc = a.inv_temp * kLog2e;
+  u32x4 x[NV];
+#pragma unroll
+  for (int k = 0; k < NV; ++k) x[k] = tid + k * TB < row.nvec ? row.load(tid + k * TB) : u32x4{0, 0, 0, 0};
+  const bool taught = teacher_row<T, NW>(sh, row, t, r, a.inv_temp, nullptr);
+  float m = -INFINITY;
+  auto vmax = [&](u32x4 v) {
+#pragma unroll
+    for (int i = 0; i < VE; ++i) m = fmaxf(m, Row<T>::get(v, i));
+  };
+#pragma unroll
+  for (int k = 0; k < NV; ++k)
+    if (tid + k * TB < row.nvec) vmax(x[k]);
+  for (int v = tid + NV * TB; v < row.nvec; v += TB) vmax(row.load(v));
+  m = block_max<NW>(m, sh.red);
+  if (!(m > -INFINITY)) m = 0.f;  // nothing but -inf (a sum of 0) or NaN (a sum of NaN)
+  float s = 0.f;
+  auto vsum = [&](u32x4 v) {
+#pragma unroll
+    for (int i = 0; i < VE; ++i) s += __builtin_amdgcn_exp2f((Row<T>::get(v, i) - m) * zc);
+  };
+#pragma unroll
+  for (int k = 0; k < NV; ++k)
+    if (tid + k * TB < row.nvec) vsum(x[k]);
+  for (int v = tid + NV * TB; v < row.nvec; v += TB) vsum(row.load(v));
+  s = block_sum<NW>(s, sh.red);
+  const bool live = taught && s != 0.f;
+  // (else the compiler holds all the differences and exponentials from here to the
+  // gradient, beside the logits: 1 KB of spills per lane in fp32)
+#pragma unroll
+  for (int k = 0; k < NV; ++k) asm volatile("" : "+v"(x[k]));
+  const float loss = teacher_loss<NW>(sh, t.K, m, logf(s), a.inv_temp);
+  if (tid == 0) t.loss[r] = live ? loss : 0.f;
+  if (!t.grad) return;
+  T* g = grad_row<T>(a, t, r);
+  const bool same = same_phase(row, g);
+  const float w = live ? (t.weight ? t.weight[r] : 1.f) * a.inv_temp : 0.f, ws = w / s;
+  auto f = [&](float v) { return live ? __builtin_amdgcn_exp2f((v - m) * zc) * ws : 0.f; };
+#pragma unroll
+  for (int k = 0; k < NV; ++k)
+    if (tid + k * TB < row.nvec) grad_vec(row, g, same, tid + k * TB, x[k], f);
+  for (int v = tid + NV * TB; v < row.nvec; v += TB) grad_vec(row, g, same, v, row.load(v), f);
+  __syncthreads();  // sh.q complete; the entries below are written after the ones above
+  if (!live) return;
+  for (int k = tid; k < t.K; k += TB) {
+    float q;
+    if (teacher_place(sh, t.K, k, q)) st_grad(g + sh.at[k], f(sh.x[k]) - w * q);
+  }
+}
+
+// Few long rows: each is split over gridDim.y workgroups, once for the sums, and
+// once more (out of the caches) for the gradient. The student's logits at the teacher's
+// entries wait in the workspace meanwhile, as the gradient may replace them.
+template <typename T>
+__global__ __launch_bounds__(kTB) void distill_sums_kernel(LogitRows a, TeacherArgs t, Stats* __restrict__ part,
+                                                           float* __restrict__ sx) {
+  constexpr int VE = Row<T>::VE;
+  __shared__ float red[16];
+  const int r = blockIdx.x, tid = threadIdx.x;
+  const Row<T> row(a, r);
+  const int per = (row.nvec + gridDim.y - 1) / gridDim.y;
+  const int v0 = min((int)blockIdx.y * per, row.nvec), v1 = min(v0 + per, row.nvec);
+  const float zc = a.inv_temp * kLog2e;
+  float m = -INFINITY, s = 0.f;
+  constexpr int U = 4;
+  for (int vb = v0 + tid; vb < v1; vb += U * kTB) {
+    u32x4 x[U];
+#pragma unroll
+    for (int k = 0; k < U; ++k)
+      if (vb + k * kTB < v1) x[k] = row.load(vb + k * kTB);
+    float nm = m;
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+      if (vb + k * kTB >= v1) break;
+#pragma unroll
+      for (int i = 0; i < VE; ++i) nm = fmaxf(nm, Row<T>::get(x[k], i));
+    }
+    if (nm > m) {
+      s = m > -INFINITY ? s * __builtin_amdgcn_exp2f((m - nm) * zc) : s;
+      m = nm;
+    }
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+      if (vb + k * kTB >= v1) break;
+#pragma unroll
+      for (int i = 0; i < VE; ++i) {
+        s += __builtin_amdgcn_exp2f((Row<T>::get(x[k], i) - (m > -INFINITY ? m : 0.f)) * zc);
+      }
+    }
+  }
+  const float bm = block_max<kTB / 64>(m, red);
+  s = block_sum<kTB / 64>(m > -INFINITY ? s * __builtin_amdgcn_exp2f((m - bm) * zc) : s, red);
+  if (tid == 0) part[(int64_t)r * gridDim.y + blockIdx.y] = Stats{bm, s, 0.f};
+  if (blockIdx.y == 0)
+    for (int k = tid; k < t.K; k += kTB) {
+      const int i = t.top[(int64_t)r * t.K + k];
+      const int64_t j = (int64_t)i - row.first;
+      sx[(int64_t)r * t.K + k] = i >= 0 && j >= 0 && j < row.cnt ? row.at((int)j) : -INFINITY;
+    }
+}
+
+template <typename T>
+__global__ __launch_bounds__(kTB) void distill_grad_kernel(LogitRows a, TeacherArgs t,
+                                                           const Stats* __restrict__ part,
+                                                           const float* __restrict__ sx) {
+  constexpr int VE = Row<T>::VE, NW = kTB / 64;
+  __shared__ TeacherShared sh;
+  const int r = blockIdx.x, tid = threadIdx.x, S = gridDim.y;
+  const Row<T> row(a, r);
+  const int per = (row.nvec + S - 1) / S;
+  const int v0 = min((int)blockIdx.y * per, row.nvec), v1 = min(v0 + per, row.nvec);
+  const float zc = a.inv_temp * kLog2e;
+  const bool taught = teacher_row<T, NW>(sh, row, t, r, a.inv_temp, sx + (int64_t)r * t.K);
+  float m = -INFINITY, s = 0.f;
+  for (int k = 0; k < S; ++k) m = fmaxf(m, part[(int64_t)r * S + k].m);
+  for (int k = 0; k < S; ++k) {
+    const Stats p = part[(int64_t)r * S + k];
+    s += p.m > -INFINITY ? p.s * __builtin_amdgcn_exp2f((p.m - m) * zc) : p.s;
+  }
+  if (!(m > -INFINITY)) m = 0.f;
+  const bool live = taught && s != 0.f;
+  const float loss = teacher_loss<NW>(sh, t.K, m, logf(s), a.inv_temp);
+  if (blockIdx.y == 0 && tid == 0) t.loss[r] = live ? loss : 0.f;
+  if (!t.grad) return;
+  T* g = grad_row<T>(a, t, r);
+  const bool same = same_phase(row, g);
+  const float w = live ? (t.weight ? t.weight[r] : 1.f) * a.inv_temp : 0.f, ws = w / s;
+  auto f = [&](float v) { return live ? __builtin_amdgcn_exp2f((v - m) * zc) * ws : 0.f; };
+  for (int v = v0 + tid; v < v1; v += kTB) grad_vec(row, g, same, v, row.load(v), f);
+  __syncthreads();
+  if (!live) return;
+  const int lo = v0 * VE - row.h, hi = v1 * VE - row.h;  // the entries of this part
+  for (int k = tid; k < t.K; k += kTB) {
+    float q;
+    if (sh.at[k] >= lo && sh.at[k] < hi && teacher_place(sh, t.K, k, q))
+      st_grad(g + sh.at[k], f(sh.x[k]) - w * q);
+  }
+}
+
+// Parts of a row: one while the rows alone give every CU four workgroups, else
+// enough for that, of 512 vectors (two per thread) at least.
+int row_splits(int n, int V) {
+  const int vecs = V / 4 + 1;
+  const int want = std::max(1, 1024 / std::max(n, 1));
+  return std::max(1, std::min({want, vecs / 512, 64}));
+}
+
+template <typename T>
+hipError_t logprobs(const LogitRows& a, int K, const LogprobOut& o, char* ws, hipStream_t s) {
+  const int S = row_splits(a.n, a.V);
+  logprobs_kernel<T><<<dim3(a.n, S), kTB, 0, s>>>(a, K, o, ws);
+  if (S > 1) logprobs_join_kernel<T><<<dim3(a.n), kTB, 0, s>>>(a, K, S, o, ws);
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t distill(const LogitRows& a, const TeacherArgs& t, char* ws, hipStream_t s) {
+  const int S = row_splits(a.n, a.V);
+  if (S > 1) {
+    Stats* part = reinterpret_cast<Stats*>(ws);
+    float* sx = reinterpret_cast<float*>(ws + (size_t)a.n * S * sizeof(Stats));
+    distill_sums_kernel<T><<<dim3(a.n, S), kTB, 0, s>>>(a, t, part, sx);
+    distill_grad_kernel<T><<<dim3(a.n, S), kTB, 0, s>>>(a, t, part, sx);
+    return hipGetLastError();
+  }
+  const int vecs = a.V / Row<T>::VE + (a.V % Row<T>::VE != 0);
+  if (vecs <= 64 * 4) distill_row_kernel<T, 1, 4><<<dim3(a.n), 64, 0, s>>>(a, t);
+  else if (vecs <= 256 * 4) distill_row_kernel<T, 4, 4><<<dim3(a.n), 256, 0, s>>>(a, t);
+  else if (vecs <= 512 * 8) distill_row_kernel<T, 8, 8><<<dim3(a.n), 512, 0, s>>>(a, t);
+  else if (vecs <= 1024 * 8) distill_row_kernel<T, 16, 8><<<dim3(a.n), 1024, 0, s>>>(a, t);
+  else distill_row_kernel<T, 16, 16><<<dim3(a.n), 1024, 0, s>>>(a, t);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+size_t logits_workspace_bytes(int n, int V, int K) {
+  const int S = row_splits(n, V);
+  if (S == 1) return 0;
+  const size_t lp = (size_t)n * S * (K * 8 + 16), di = (size_t)n * S * sizeof(Stats) + (size_t)n * K * sizeof(float);
+  return std::max(lp, di);
+}
+
+hipError_t launch_logprobs(const LogitRows& a, const int* tokens, int K, float* logp, float* entropy, int* top,
+                           float* top_logp, void* ws, hipStream_t s) {
+  const LogprobOut o = {tokens, logp, entropy, top, top_logp};
+  return a.bf16 ? logprobs<uint16_t>(a, K, o, static_cast<char*>(ws), s)
+                : logprobs<float>(a, K, o, static_cast<char*>(ws), s);
+}
+
+hipError_t launch_distill_topk(const LogitRows& a, int K, const int* top, const float* teacher, const float* weight,
+                               float* loss, void* grad, int64_t ldg, void* ws, hipStream_t s) {
+  const TeacherArgs t = {K, top, teacher, weight, loss, grad, ldg};
+  return a.bf16 ? distill<uint16_t>(a, t, static_cast<char*>(ws), s) : distill<float>(a, t, static_cast<char*>(ws), s);
+}
+
+}  // namespace tcl

@@ -1,0 +1,1223 @@
+// The causal convolution and the selective scan as operators of their own,
+// with states carried over: prompts (packed sequences), single tokens, and
+// their gradients.
+//
+// Sequence i owns rows offs[i] .. offs[i+1]-1 of every activation. Work along
+// the rows is cut into tiles of R rows that never straddle two sequences:
+// sequence i's tiles start at index key(i) = offs[i] / R + i, which leaves
+// room for ceil(len / R) of them (and at least one, so an empty sequence has
+// a tile that passes its state on), rises strictly with i, and is found from a
+// tile index by bisection, without a table. rows / R + n_seq bounds the
+// count on the host, which does not know the offsets.
+#include <algorithm>
+
+#include "common.h"
+#include "ops.h"
+
+namespace tcl {
+namespace {
+
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ float to_f32(float v) { return v; }
+__device__ __forceinline__ float to_f32(uint16_t v) { return bf16_to_f32(v); }
+__device__ __forceinline__ void st1(float* p, float v) { *p = v; }
+__device__ __forceinline__ void st1(uint16_t* p, float v) { *p = f32_to_bf16(v); }
+
+// CH adjacent channels of a row; the storage type's raw bits, widened at use.
+template <typename T, int CH> struct Pack { T v[CH]; };
+template <> struct Pack<float, 4> { floatx4 v; };
+template <> struct Pack<uint16_t, 8> { u32x4 v; };
+template <> struct Pack<uint16_t, 4> { u32x2 v; };
+
+template <typename T, int CH>
+__device__ __forceinline__ Pack<T, CH> pk_load(const T* p) {
+  return *reinterpret_cast<const Pack<T, CH>*>(p);
+}
+template <typename T, int CH>
+__device__ __forceinline__ float pk_get(const Pack<T, CH>& p, int i) {
+  if constexpr (CH == 1 || sizeof(T) == 4)
+    return to_f32(p.v[i]);
+  else
+    return __uint_as_float(i & 1 ? p.v[i >> 1] & 0xFFFF0000u : p.v[i >> 1] << 16);
+}
+template <typename T, int CH>
+__device__ __forceinline__ void pk_store(T* p, const float* v) {
+  if constexpr (CH == 1) {
+    st1(p, v[0]);
+  } else if constexpr (sizeof(T) == 4) {
+    *reinterpret_cast<floatx4*>(p) = floatx4{v[0], v[1], v[2], v[3]};
+  } else {
+    Pack<T, CH> o;
+#pragma unroll
+    for (int i = 0; i < CH / 2; ++i) o.v[i] = f32x2_to_bf16x2(v[2 * i], v[2 * i + 1]);
+    *reinterpret_cast<Pack<T, CH>*>(p) = o;
+  }
+}
+
+struct Tile {
+  int seq;   // -1: no sequence has this tile
+  int j;     // its index in the sequence
+  int base;  // the sequence's first row
+  int len;
+};
+
+// Tile w of R rows. Offsets are read as lying in [0, rows], so a wrong one
+// cannot lead outside the activations.
+__device__ __forceinline__ Tile find_tile(const int* __restrict__ offs, int n_seq, int rows, int R, int w) {
+  Tile t;
+  if (!offs) {
+    t.seq = w < n_seq ? w : -1;
+    t.j = 0;
+    t.base = w;
+    t.len = 1;
+    return t;
+  }
+  int lo = 0, hi = n_seq;  // key(lo) <= w < key(hi), once the ends are taken
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (offs[mid] / R + mid <= w) lo = mid;
+    else hi = mid;
+  }
+  const int o0 = min(max(offs[lo], 0), rows), o1 = min(max(offs[lo + 1], o0), rows);
+  t.j = w - (o0 / R + lo);
+  t.base = o0;
+  t.len = o1 - o0;
+  t.seq = t.j >= 0 && (t.j == 0 || (int64_t)t.j * R < t.len) ? lo : -1;
+  return t;
+}
+
+// The state of sequence `seq` in the pool, -1 for none.
+__device__ __forceinline__ int slot_of(const int* __restrict__ slots, int n_slots, int seq) {
+  const int j = slots ? slots[seq] : seq;
+  return j >= 0 && j < n_slots ? j : -1;
+}
+
+// ---------------------------------------------------------------- causal conv + SiLU
+// u_t = SiLU(b + sum_k w_k x_{t-K+1+k}). A thread takes CH adjacent channels
+// (16 bytes) of one tile and keeps the last K rows in registers; rows in front of
+// the tile are read again (K - 1 of R), those in front of the sequence come
+// from its state. The thread of the first tile is also the one that writes
+// the new state, after it has read the old one, so both may be the same
+// memory. Bound by HBM: each x read once, each u written once.
+template <typename T, int K, int CH>
+__global__ __launch_bounds__(256) void ssm_conv_kernel(const int* __restrict__ offs, int n_seq, int rows, int E,
+                                                       int R, int64_t n_work, const T* __restrict__ x, int64_t ldx,
+                                                       const float* __restrict__ w, const float* __restrict__ b,
+                                                       const T* state, const int* __restrict__ slots, int n_slots,
+                                                       T* state_out, T* __restrict__ u, int64_t ldu) {
+  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (id >= n_work) return;
+  const int CG = E / CH;
+  const int e = (int)(id % CG) * CH;
+  const Tile tl = find_tile(offs, n_seq, rows, R, (int)(id / CG));
+  if (tl.seq < 0) return;
+  const T* xs = x + (int64_t)tl.base * ldx + e;
+  const int t0 = tl.j * R, t1 = min(t0 + R, tl.len);
+
+  float wk[K][CH], bias[CH];
+#pragma unroll
+  for (int c = 0; c < CH; ++c) {
+    bias[c] = b ? b[e + c] : 0.f;
+#pragma unroll
+    for (int k = 0; k < K; ++k) wk[k][c] = w[(int64_t)(e + c) * K + k];
+  }
+  // win[k] = x_{t-K+1+k}; the slot K - 1 is the token's own
+  float win[K][CH];
+  if constexpr (K > 1) {
+    if (tl.j == 0) {
+      const int sl = slot_of(slots, n_slots, tl.seq);
+      const int64_t so = (int64_t)sl * (K - 1) * E + e;
+#pragma unroll
+      for (int k = 0; k < K - 1; ++k) {
+#pragma unroll
+        for (int c = 0; c < CH; ++c) win[k][c] = 0.f;
+        if (state && sl >= 0) {
+          const Pack<T, CH> p = pk_load<T, CH>(state + so + (int64_t)k * E);
+#pragma unroll
+          for (int c = 0; c < CH; ++c) win[k][c] = pk_get(p, c);
+        }
+      }
+      if (state_out && sl >= 0) {
+        // the last K - 1 rows of (old state, tokens)
+#pragma unroll
+        for (int k = 0; k < K - 1; ++k) {
+          const int t = tl.len - (K - 1) + k;
+          float v[CH];
+          if (t >= 0) {
+            const Pack<T, CH> p = pk_load<T, CH>(xs + (int64_t)t * ldx);
+#pragma unroll
+            for (int c = 0; c < CH; ++c) v[c] = pk_get(p, c);
+          } else {
+#pragma unroll
+            for (int c = 0; c < CH; ++c) v[c] = 0.f;
+#pragma unroll
+            for (int i = 0; i < K - 1; ++i)
+              if (i == K - 1 + t)
+#pragma unroll
+                for (int c = 0; c < CH; ++c) v[c] = win[i][c];
+          }
+          pk_store<T, CH>(state_out + so + (int64_t)k * E, v);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < K - 1; ++k) {  // R >= K - 1: these rows are the sequence's
+        const Pack<T, CH> p = pk_load<T, CH>(xs + (int64_t)(t0 - (K - 1) + k) * ldx);
+#pragma unroll
+        for (int c = 0; c < CH; ++c) win[k][c] = pk_get(p, c);
+      }
+    }
+  }
+  T* us = u + (int64_t)tl.base * ldu + e;
+  constexpr int U = 4;  // rows whose loads are in flight together
+  Pack<T, CH> nx[U];
+#pragma unroll
+  for (int i = 0; i < U; ++i)
+    if (t0 < t1) nx[i] = pk_load<T, CH>(xs + (int64_t)min(t0 + i, t1 - 1) * ldx);
+  for (int t = t0; t < t1; t += U) {
+    Pack<T, CH> cur[U];
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      cur[i] = nx[i];
+      if (t + U < t1) nx[i] = pk_load<T, CH>(xs + (int64_t)min(t + U + i, t1 - 1) * ldx);
+    }
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      if (t + i >= t1) break;
+      float o[CH];
+#pragma unroll
+      for (int c = 0; c < CH; ++c) {
+        win[K - 1][c] = pk_get(cur[i], c);
+        float v = bias[c];
+#pragma unroll
+        for (int k = 0; k < K; ++k) v = fmaf(wk[k][c], win[k][c], v);
+        o[c] = silu(v);
+#pragma unroll
+        for (int k = 0; k < K - 1; ++k) win[k][c] = win[k + 1][c];
+      }
+      pk_store<T, CH>(us + (int64_t)(t + i) * ldu, o);
+    }
+  }
+}
+
+// SiLU'(x) = sg (1 + x (1 - sg)), sg = sigmoid(x).
+__device__ __forceinline__ float silu_grad(float x) {
+  const float sg = rcp_fast(1.0f + exp_fast(-x));
+  return sg * fmaf(x, 1.0f - sg, 1.0f);
+}
+
+// Gradients of the convolution. With g_t = du_t SiLU'(pre_t):
+//   dx_t = sum_k w_k g_{t+K-1-k},  dw_k = sum_t g_t x_{t-K+1+k},  db = sum_t g_t
+// and the state's rows are the x_t of t < 0. A thread takes CH channels of
+// `per` tiles in a row; in each it walks forward over the tile's rows and the
+// K - 1 behind it, forming pre and g again there, so that dx leaves complete and
+// nothing passes between threads. dw and db stay in registers over its tiles
+// and go out once, as part `p` of the partial sums.
+template <typename T, int K, int CH>
+__global__ __launch_bounds__(256) void ssm_conv_bwd_kernel(
+    const int* __restrict__ offs, int n_seq, int rows, int E, int R, int per, int parts, const T* __restrict__ x,
+    int64_t ldx, const float* __restrict__ w, const float* __restrict__ b, const T* __restrict__ state,
+    const T* __restrict__ du, int64_t lddu, const T* __restrict__ dstate_out, T* __restrict__ dx, int64_t lddx,
+    T* __restrict__ dstate, float* __restrict__ part) {
+  const int CG = E / CH;
+  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (id >= (int64_t)parts * CG) return;
+  const int p = (int)(id / CG), e = (int)(id % CG) * CH;
+  float wk[K][CH], bias[CH], dw[K][CH], db[CH];
+#pragma unroll
+  for (int c = 0; c < CH; ++c) {
+    bias[c] = b ? b[e + c] : 0.f;
+    db[c] = 0.f;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      wk[k][c] = w[(int64_t)(e + c) * K + k];
+      dw[k][c] = 0.f;
+    }
+  }
+  for (int q = 0; q < per; ++q) {
+    const Tile tl = find_tile(offs, n_seq, rows, R, p * per + q);
+    if (tl.seq < 0) continue;
+    const int t0 = tl.j * R, t1 = min(t0 + R, tl.len);
+    const T* xs = x + (int64_t)tl.base * ldx + e;
+    const T* dus = du + (int64_t)tl.base * lddu + e;
+    T* dxs = dx + (int64_t)tl.base * lddx + e;
+    const int64_t so = (int64_t)tl.seq * (K - 1) * E + e;
+    float win[K][CH], g[K][CH];  // x_{t-K+1+k}; g[k] = g_{t-K+1+k}
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+#pragma unroll
+      for (int c = 0; c < CH; ++c) {
+        win[k][c] = 0.f;
+        g[k][c] = 0.f;
+      }
+      if (k < K - 1) {
+        const T* src = nullptr;
+        if (tl.j > 0) src = xs + (int64_t)(t0 - (K - 1) + k) * ldx;
+        else if (state) src = state + so + (int64_t)k * E;
+        if (src) {
+          const Pack<T, CH> v = pk_load<T, CH>(src);
+#pragma unroll
+          for (int c = 0; c < CH; ++c) win[k][c] = pk_get(v, c);
+        }
+      }
+    }
+    // rows t0 .. t1 + K - 2; those past the sequence have g = 0
+    const int tend = t1 + K - 1;
+    constexpr int U = 4;
+    Pack<T, CH> nx[U], nd[U];
+    auto load = [&](int t) {
+      if (tl.len == 0) return;
+#pragma unroll
+      for (int i = 0; i < U; ++i) {
+        const int r = min(t + i, tl.len - 1);
+        nx[i] = pk_load<T, CH>(xs + (int64_t)r * ldx);
+        nd[i] = pk_load<T, CH>(dus + (int64_t)r * lddu);
+      }
+    };
+    load(t0);
+    for (int tb = t0; tb < tend; tb += U) {
+      Pack<T, CH> cx[U], cd[U];
+#pragma unroll
+      for (int i = 0; i < U; ++i) {
+        cx[i] = nx[i];
+        cd[i] = nd[i];
+      }
+      if (tb + U < tend) load(tb + U);
+#pragma unroll
+      for (int i = 0; i < U; ++i) {
+        const int t = tb + i;
+        if (t >= tend) break;
+        const bool in = t < tl.len, mine = t < t1;
+        const int td = t - (K - 1);  // the row whose dx is complete with this one
+        const bool out = td >= t0 || (tl.j == 0 && td < 0);
+        float o[CH];
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+          win[K - 1][c] = in ? pk_get(cx[i], c) : 0.f;
+          float v = bias[c];
+#pragma unroll
+          for (int k = 0; k < K; ++k) v = fmaf(wk[k][c], win[k][c], v);
+          const float gt = in ? pk_get(cd[i], c) * silu_grad(v) : 0.f;
+          g[K - 1][c] = gt;
+          if (mine) {
+            db[c] += gt;
+#pragma unroll
+            for (int k = 0; k < K; ++k) dw[k][c] = fmaf(gt, win[k][c], dw[k][c]);
+          }
+          float d = 0.f;
+#pragma unroll
+          for (int k = 0; k < K; ++k) d = fmaf(wk[k][c], g[K - 1 - k][c], d);
+          o[c] = d;
+#pragma unroll
+          for (int k = 0; k < K - 1; ++k) {
+            win[k][c] = win[k + 1][c];
+            g[k][c] = g[k + 1][c];
+          }
+        }
+        if (!out) continue;
+        const int k = td - (tl.len - (K - 1));  // the row of the new state that td is
+        if (dstate_out && k >= 0) {
+          const Pack<T, CH> v = pk_load<T, CH>(dstate_out + so + (int64_t)k * E);
+#pragma unroll
+          for (int c = 0; c < CH; ++c) o[c] += pk_get(v, c);
+        }
+        if (td >= 0) pk_store<T, CH>(dxs + (int64_t)td * lddx, o);
+        else if (dstate) pk_store<T, CH>(dstate + so + (int64_t)(K - 1 + td) * E, o);
+      }
+    }
+  }
+  float* o = part + (int64_t)p * (K + 1) * E + e;
+#pragma unroll
+  for (int c = 0; c < CH; ++c) {
+#pragma unroll
+    for (int k = 0; k < K; ++k) o[(int64_t)k * E + c] = dw[k][c];
+    o[(int64_t)K * E + c] = db[c];
+  }
+}
+
+// Sums of `parts` partial vectors part[p][M + extra][E] in a fixed order, laid out as
+// the parameters are: o0[e, m] for m < M, then o1[e], o2[e] (null: not wanted).
+constexpr int kSumLanes = 16;
+__global__ __launch_bounds__(64 * kSumLanes) void sum_parts_kernel(const float* __restrict__ part, int parts, int M,
+                                                                   int total, int E, float* __restrict__ o0,
+                                                                   float* __restrict__ o1, float* __restrict__ o2) {
+  __shared__ float red[kSumLanes][64];
+  const int lane = threadIdx.x & 63, g = threadIdx.x >> 6;
+  const int64_t i = (int64_t)blockIdx.x * 64 + lane, stride = (int64_t)total * E;
+  float acc = 0.f;
+  if (i < stride) {
+    const float* src = part + i;
+    int p = g;
+    for (; p + 3 * kSumLanes < parts; p += 4 * kSumLanes) {
+      const float a = src[p * stride], b = src[(p + kSumLanes) * stride], c = src[(p + 2 * kSumLanes) * stride],
+                  d = src[(p + 3 * kSumLanes) * stride];
+      acc += (a + b) + (c + d);
+    }
+    for (; p < parts; p += kSumLanes) acc += src[p * stride];
+  }
+  red[g][lane] = acc;
+  __syncthreads();
+  if (g || i >= stride) return;
+  acc = 0.f;
+#pragma unroll
+  for (int k = 0; k < kSumLanes; ++k) acc += red[k][lane];
+  const int m = (int)(i / E), e = (int)(i % E);
+  if (m < M) o0[(int64_t)e * M + m] = acc;
+  else if (m == M) { if (o1) o1[e] = acc; }
+  else if (o2) o2[e] = acc;
+}
+
+// ---------------------------------------------------------------- selective scan, prompts
+// s_t = exp(d_t A) s_{t-1} + d_t u_t B_t,  y_t = (C_t . s_t + D u_t) SiLU(z_t),
+// d = softplus(dt + b_dt), A = -exp(A_log).
+// One lane per channel holds its N states and decay rates (in base-2 units);
+// a workgroup is one wavefront, so nothing waits for another. B and C rows
+// go through LDS kTC tokens at a time (widened once, read as broadcasts), the
+// next kTC rows on their way in registers meanwhile; u, dt and z come four
+// tokens ahead. Per token and wavefront 6 N issue slots for the states and
+// some 25 for softplus, gate and output, against 4 x 64 elements of traffic: the
+// vector unit is what bounds it (see launch_ssm_scan for figures).
+//
+// A sequence is cut into chunks of CL tokens when there are too few of them to
+// fill the GPU. s -> P s + s_loc with P = exp(A sum d) is what a chunk does to a
+// state, so LOCAL runs every chunk but a sequence's last from zero for (s_loc,
+// sum d), ssm_combine_kernel composes them into every chunk's start state,
+// and the plain form runs the chunks from there. Twice the exponentials.
+constexpr int kTC = 32;
+
+struct ScanIn {
+  const int* offs;
+  int n_seq, rows, E, CL, ntile;
+  int64_t ldu, lddt, ldB, ldC, ldz;
+  const float *A_log, *D, *b_dt, *state;
+  const int* slots;
+  int n_slots;
+};
+
+// blockIdx.x -> (tile, channel group): the channel groups of a tile follow each
+// other on one XCD (workgroups go to the 8 XCDs in turn), whose L2 then holds
+// the tile's B and C rows.
+__device__ __forceinline__ bool tile_of_block(int ntile, int CG, int& w, int& cg) {
+  const int xcd = blockIdx.x & 7, j = blockIdx.x >> 3;
+  w = (j / CG) * 8 + xcd;
+  cg = j % CG;
+  return w < ntile;
+}
+inline unsigned tile_blocks(int ntile, int CG) { return (unsigned)((ntile + 7) / 8 * 8) * CG; }
+
+__device__ __forceinline__ float decay_rate(float a_log) {  // A log2(e)
+  return -__builtin_amdgcn_exp2f(a_log * kLog2e) * kLog2e;
+}
+
+template <typename T, int N, bool LOCAL>
+__global__ __launch_bounds__(64, 4) void ssm_scan_kernel(ScanIn a, const T* __restrict__ u, const T* __restrict__ dt,
+                                                         const T* __restrict__ B, const T* __restrict__ C,
+                                                         const T* __restrict__ z, float* state_out,
+                                                         T* __restrict__ y, int64_t ldy, float* cst, float* csum) {
+  __shared__ __attribute__((aligned(16))) float sBC[kTC * 2 * N];
+  int w, cg;
+  if (!tile_of_block(a.ntile, (a.E + 63) / 64, w, cg)) return;
+  const Tile tl = find_tile(a.offs, a.n_seq, a.rows, a.CL, w);
+  if (tl.seq < 0) return;
+  const int t0 = tl.j * a.CL, t1 = min(tl.len, t0 + a.CL);
+  if (LOCAL && t1 == tl.len) return;  // nobody follows
+  const int lane = threadIdx.x, E = a.E;
+  const int e = cg * 64 + lane;
+  const bool active = e < E;
+  const int ec = active ? e : E - 1;
+
+  float a2[N], s[N];
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    a2[n] = decay_rate(a.A_log[(int64_t)ec * N + n]);
+    s[n] = 0.f;
+  }
+  const int sl = slot_of(a.slots, a.n_slots, tl.seq);
+  if (!LOCAL) {
+    if (cst) {
+#pragma unroll
+      for (int n = 0; n < N; ++n) s[n] = cst[((int64_t)w * N + n) * E + ec];
+    } else if (a.state && sl >= 0) {
+#pragma unroll
+      for (int n = 0; n < N; ++n) s[n] = a.state[((int64_t)sl * E + ec) * N + n];
+    }
+  }
+  const float bias = a.b_dt ? a.b_dt[ec] : 0.f, Dv = !LOCAL && a.D ? a.D[ec] : 0.f;
+
+  if (t0 < t1) {
+    const int64_t r0 = tl.base;
+    const T *us = u + r0 * a.ldu, *ds = dt + r0 * a.lddt, *zs = z ? z + r0 * a.ldz : nullptr;
+    const T *Bs = B + r0 * a.ldB, *Cs = LOCAL ? nullptr : C + r0 * a.ldC;
+    T* ys = LOCAL ? nullptr : y + r0 * ldy;
+    // value i of a stage: token i / (2N), B's or C's column (LOCAL: B's only)
+    constexpr int W = LOCAL ? N : 2 * N, PER = kTC * W / 64;
+    T st[PER];
+    auto stage = [&](int t) {
+#pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        const int k = i * 64 + lane, col = k % W, row = min(t + k / W, t1 - 1);
+        st[i] = col < N ? Bs[(int64_t)row * a.ldB + col] : Cs[(int64_t)row * a.ldC + col - N];
+      }
+    };
+    constexpr int U = 4;
+    T nu[U], nd[U], nz[U];
+    auto load = [&](int t) {
+#pragma unroll
+      for (int i = 0; i < U; ++i) {
+        const int r = min(t + i, t1 - 1);
+        nu[i] = (us + (int64_t)r * a.ldu)[ec];
+        nd[i] = (ds + (int64_t)r * a.lddt)[ec];
+        if (!LOCAL && z) nz[i] = (zs + (int64_t)r * a.ldz)[ec];
+      }
+    };
+    float sum = 0.f;
+    stage(t0);
+    load(t0);
+    for (int tc = t0; tc < t1; tc += kTC) {
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < PER; ++i) sBC[i * 64 + lane] = to_f32(st[i]);
+      __syncthreads();
+      if (tc + kTC < t1) stage(tc + kTC);
+      const int te = min(t1, tc + kTC);
+      for (int tg = tc; tg < te; tg += U) {
+        T cu[U], cd[U], cz[U];
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+          cu[i] = nu[i];
+          cd[i] = nd[i];
+          if (!LOCAL && z) cz[i] = nz[i];
+        }
+        if (tg + U < t1) load(tg + U);
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+          const int t = tg + i;
+          if (t >= te) break;
+          const float* x = &sBC[(t - tc) * W];
+          const float uv = to_f32(cu[i]), d = softplus(to_f32(cd[i]) + bias), du = d * uv;
+          if (LOCAL) sum += d;
+          float acc = 0.f;
+#pragma unroll
+          for (int n = 0; n < N; ++n) {
+            s[n] = fmaf(__builtin_amdgcn_exp2f(d * a2[n]), s[n], du * x[n]);
+            if (!LOCAL) acc = fmaf(s[n], x[N + n], acc);
+          }
+          if (!LOCAL) {
+            acc = fmaf(Dv, uv, acc);
+            if (z) acc *= silu(to_f32(cz[i]));
+            if (active) st1((ys + (int64_t)t * ldy) + e, acc);
+          }
+        }
+      }
+    }
+    if (LOCAL && active) csum[(int64_t)w * E + e] = sum;
+  }
+  if (!active) return;
+  if (LOCAL) {
+#pragma unroll
+    for (int n = 0; n < N; ++n) cst[((int64_t)w * N + n) * E + e] = s[n];
+  } else if (state_out && sl >= 0 && t1 == tl.len) {
+#pragma unroll
+    for (int n = 0; n < N; ++n) state_out[((int64_t)sl * E + e) * N + n] = s[n];
+  }
+}
+
+// Every chunk's start state out of the chunks' (s_loc, sum d), in place of
+// s_loc; with G, also the adjoint that reaches every chunk's end out of the
+// chunks' own adjoints of their start, in place of those. One thread per
+// (channel, state, sequence), the chunks in sequence, eight of them loaded together.
+template <int N>
+__global__ __launch_bounds__(256) void ssm_combine_kernel(ScanIn a, float* __restrict__ cst,
+                                                          const float* __restrict__ csum, float* __restrict__ G,
+                                                          const float* __restrict__ dstate_out) {
+  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int E = a.E;
+  const int e = (int)(id % E), n = (int)(id / E % N);
+  const int64_t seq = id / E / N;
+  if (seq >= a.n_seq) return;
+  const int o0 = min(max(a.offs[seq], 0), a.rows), o1 = min(max(a.offs[seq + 1], o0), a.rows);
+  const int nch = max(1, (o1 - o0 + a.CL - 1) / a.CL);
+  const int64_t w0 = o0 / a.CL + seq;
+  const float a2 = decay_rate(a.A_log[(int64_t)e * N + n]);
+  const int sl = slot_of(a.slots, a.n_slots, (int)seq);
+  float s = a.state && sl >= 0 ? a.state[((int64_t)sl * E + e) * N + n] : 0.f;
+  float* st = cst + (w0 * N + n) * E + e;
+  const float* sm = csum + w0 * E + e;
+  const int64_t step = (int64_t)N * E;
+  constexpr int U = 8;
+  for (int c = 0; c < nch - 1; c += U) {
+    float v[U], d[U];
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const int k = min(c + i, nch - 2);
+      v[i] = st[k * step];
+      d[i] = sm[(int64_t)k * E];
+    }
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      if (c + i >= nch - 1) break;
+      st[(c + i) * step] = s;
+      s = fmaf(__builtin_amdgcn_exp2f(a2 * d[i]), s, v[i]);
+    }
+  }
+  st[(nch - 1) * step] = s;
+  if (!G) return;
+  float h = dstate_out ? dstate_out[(seq * E + e) * N + n] : 0.f;
+  float* g = G + (w0 * N + n) * E + e;
+  for (int c = nch - 1; c >= 0; c -= U) {
+    float v[U], d[U];
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const int k = max(c - i, 0);
+      v[i] = g[k * step];
+      d[i] = sm[(int64_t)k * E];
+    }
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      if (c - i < 0) break;
+      g[(c - i) * step] = h;
+      h = fmaf(__builtin_amdgcn_exp2f(a2 * d[i]), h, v[i]);
+    }
+  }
+}
+
+// ---------------------------------------------------------------- selective scan, single tokens
+// N / 4 lanes per channel hold four states each: a wavefront reads and writes
+// 1 KB of states in one access, and y is summed over the lanes of a channel
+// by DPP. A workgroup takes 1,024 / N channels of SB sequences, whose loads are all in
+// flight together and share the decay rates. Bound by the states' bytes.
+template <typename T, int N, int SB>
+__global__ __launch_bounds__(256) void ssm_scan_token_kernel(ScanIn a, const T* __restrict__ u,
+                                                             const T* __restrict__ dt, const T* __restrict__ B,
+                                                             const T* __restrict__ C, const T* __restrict__ z,
+                                                             float* state_out, T* __restrict__ y, int64_t ldy) {
+  constexpr int Q = N / 4;
+  const int E = a.E;
+  const int e = blockIdx.x * (256 / Q) + threadIdx.x / Q, n0 = (threadIdx.x % Q) * 4;
+  const bool active = e < E;
+  const int ec = active ? e : E - 1;
+  const floatx4 al = *reinterpret_cast<const floatx4*>(a.A_log + (int64_t)ec * N + n0);
+  const float bias = a.b_dt ? a.b_dt[ec] : 0.f, Dv = a.D ? a.D[ec] : 0.f;
+  floatx4 s[SB];
+  T ur[SB], dr[SB], zr[SB], br[SB][4], cr[SB][4];
+  int sl[SB];
+#pragma unroll
+  for (int i = 0; i < SB; ++i) {
+    const int q = min((int)blockIdx.y * SB + i, a.n_seq - 1);
+    sl[i] = slot_of(a.slots, a.n_slots, q);
+    s[i] = floatx4{0.f, 0.f, 0.f, 0.f};
+    if (a.state && sl[i] >= 0)
+      s[i] = *reinterpret_cast<const floatx4*>(a.state + ((int64_t)sl[i] * E + ec) * N + n0);
+    ur[i] = u[q * a.ldu + ec];
+    dr[i] = dt[q * a.lddt + ec];
+    if (z) zr[i] = z[q * a.ldz + ec];
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+      br[i][n] = B[q * a.ldB + n0 + n];
+      cr[i][n] = C[q * a.ldC + n0 + n];
+    }
+  }
+  float a2[4];
+#pragma unroll
+  for (int n = 0; n < 4; ++n) a2[n] = decay_rate(al[n]);
+#pragma unroll
+  for (int i = 0; i < SB; ++i) {
+    const int q = blockIdx.y * SB + i;
+    const float uv = to_f32(ur[i]), d = softplus(to_f32(dr[i]) + bias), du = d * uv;
+    float acc = 0.f;
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+      s[i][n] = fmaf(__builtin_amdgcn_exp2f(d * a2[n]), s[i][n], du * to_f32(br[i][n]));
+      acc = fmaf(s[i][n], to_f32(cr[i][n]), acc);
+    }
+    acc += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(acc), 0xB1, 0xF, 0xF, false));  // xor 1
+    if (Q == 4)
+      acc += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(acc), 0x4E, 0xF, 0xF, false));  // xor 2
+    acc = fmaf(Dv, uv, acc);
+    if (z) acc *= silu(to_f32(zr[i]));
+    if (!active || q >= a.n_seq) continue;
+    if (state_out && sl[i] >= 0)
+      *reinterpret_cast<floatx4*>(state_out + ((int64_t)sl[i] * E + e) * N + n0) = s[i];
+    if (n0 == 0) st1(y + q * ldy + e, acc);
+  }
+}
+
+// ---------------------------------------------------------------- selective scan, gradients
+// Adjoints run backwards: g_t = q_t C_t + h_t, h_{t-1} = exp(d_t A) g_t, with q = dy SiLU(z)
+// and h after the last token the gradient of the end state. Then
+//   dB_t = sum_e g d u,  dC_t = sum_e q s_t,  dd = sum_n g (A a s_{t-1} + u B),
+//   du = D q + d sum_n g B,  dz = dy (C . s_t + D u) SiLU'(z),  ddt = dd sigmoid(dt + b_dt),
+//   dA_log = A sum_t g d a s_{t-1},  dD = sum_t q u,  db_dt = sum_t ddt.
+// Sequences are cut into chunks of kBCL tokens, which the adjoints need as the
+// states do: ssm_bwd_local_kernel forms a chunk's (s_loc, sum d) and, in the same
+// forward walk, its adjoint of the start state, sum_t (prod a) C_t q_t;
+// ssm_combine_kernel joins them. Sequences of one chunk skip both.
+constexpr int kBCL = 32;  // tokens per chunk
+constexpr int kSub = 8;   // tokens whose states are held in registers together
+
+template <typename T, int N>
+__global__ __launch_bounds__(64, 4) void ssm_bwd_local_kernel(ScanIn a, const T* __restrict__ u,
+                                                              const T* __restrict__ dt, const T* __restrict__ B,
+                                                              const T* __restrict__ C, const T* __restrict__ z,
+                                                              const T* __restrict__ dy, int64_t lddy,
+                                                              float* __restrict__ cst, float* __restrict__ csum,
+                                                              float* __restrict__ G) {
+  __shared__ __attribute__((aligned(16))) float sBC[kBCL * 2 * N];
+  int w, cg;
+  if (!tile_of_block(a.ntile, (a.E + 63) / 64, w, cg)) return;
+  const Tile tl = find_tile(a.offs, a.n_seq, a.rows, kBCL, w);
+  if (tl.seq < 0) return;
+  const int t0 = tl.j * kBCL, t1 = min(tl.len, t0 + kBCL);
+  const int lane = threadIdx.x, E = a.E;
+  const int e = cg * 64 + lane;
+  const bool active = e < E;
+  const int ec = active ? e : E - 1;
+  const int64_t r0 = tl.base;
+  float a2[N], s[N], p[N], g[N];
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    a2[n] = decay_rate(a.A_log[(int64_t)ec * N + n]);
+    s[n] = 0.f;
+    p[n] = 1.f;
+    g[n] = 0.f;
+  }
+  const float bias = a.b_dt ? a.b_dt[ec] : 0.f;
+  float sum = 0.f;
+  for (int i = lane; i < (t1 - t0) * 2 * N; i += 64) {
+    const int col = i % (2 * N);
+    const int64_t row = r0 + t0 + i / (2 * N);
+    sBC[i] = to_f32(col < N ? B[row * a.ldB + col] : C[row * a.ldC + col - N]);
+  }
+  __syncthreads();
+  if (t0 < t1) {
+    constexpr int U = 4;
+    T nu[U], nd[U], nz[U], ng[U];
+    auto load = [&](int t) {
+#pragma unroll
+      for (int i = 0; i < U; ++i) {
+        const int64_t r = r0 + min(t + i, t1 - 1);
+        nu[i] = (u + r * a.ldu)[ec];
+        nd[i] = (dt + r * a.lddt)[ec];
+        ng[i] = (dy + r * lddy)[ec];
+        if (z) nz[i] = (z + r * a.ldz)[ec];
+      }
+    };
+    load(t0);
+    for (int tg = t0; tg < t1; tg += U) {
+      T cu[U], cd[U], cz[U], cg_[U];
+#pragma unroll
+      for (int i = 0; i < U; ++i) {
+        cu[i] = nu[i];
+        cd[i] = nd[i];
+        cg_[i] = ng[i];
+        if (z) cz[i] = nz[i];
+      }
+      if (tg + U < t1) load(tg + U);
+#pragma unroll
+      for (int i = 0; i < U; ++i) {
+        const int t = tg + i;
+        if (t >= t1) break;
+        const float* x = &sBC[(t - t0) * 2 * N];
+        const float d = softplus(to_f32(cd[i]) + bias), du = d * to_f32(cu[i]);
+        const float q = z ? to_f32(cg_[i]) * silu(to_f32(cz[i])) : to_f32(cg_[i]);
+        sum += d;
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+          const float an = __builtin_amdgcn_exp2f(d * a2[n]);
+          s[n] = fmaf(an, s[n], du * x[n]);
+          p[n] *= an;
+          g[n] = fmaf(p[n], q * x[N + n], g[n]);
+        }
+      }
+    }
+  }
+  if (!active) return;
+  csum[(int64_t)w * E + e] = sum;
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    cst[((int64_t)w * N + n) * E + e] = s[n];
+    G[((int64_t)w * N + n) * E + e] = g[n];
+  }
+}
+
+template <int CTRL>
+__device__ __forceinline__ float dpp(float v) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xF, 0xF, false));
+}
+
+// Sums of M = 32 or 16 values over the 64 lanes, scattered: lane l ends with the
+// total of value l / (64 / M). Halves of the values go to halves of the lanes step by
+// step (half-wave and row swaps route a pair at once; within rows of 16 by
+// DPP: rotation by 8, mirrors of 8, quad permutations), M - 1 additions and as many
+// moves instead of 6 M of each.
+template <int M>
+__device__ __forceinline__ float reduce_scatter(float* v, int lane) {
+#pragma unroll
+  for (int i = 0; i < M / 2; ++i) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v[i]), __float_as_uint(v[M / 2 + i]), false, false);
+    v[i] = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  }
+#pragma unroll
+  for (int i = 0; i < M / 4; ++i) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v[i]), __float_as_uint(v[M / 4 + i]), false, false);
+    v[i] = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  }
+  const bool b3 = (lane & 8) != 0, b2 = (lane & 4) != 0, b1 = (lane & 2) != 0;
+#pragma unroll
+  for (int i = 0; i < M / 8; ++i) {  // row_ror:8
+    const float mine = b3 ? v[M / 8 + i] : v[i], other = b3 ? v[i] : v[M / 8 + i];
+    v[i] = mine + dpp<0x128>(other);
+  }
+#pragma unroll
+  for (int i = 0; i < M / 16; ++i) {  // row_half_mirror: lane ^ 7
+    const float mine = b2 ? v[M / 16 + i] : v[i], other = b2 ? v[i] : v[M / 16 + i];
+    v[i] = mine + dpp<0x141>(other);
+  }
+  float z;
+  if constexpr (M == 32) {
+    const float mine = b1 ? v[1] : v[0], other = b1 ? v[0] : v[1];
+    z = mine + dpp<0x4E>(other);  // quad_perm: lane ^ 2
+  } else {
+    z = v[0] + dpp<0x4E>(v[0]);
+  }
+  return z + dpp<0xB1>(z);  // lane ^ 1
+}
+
+// A workgroup takes one chunk of 64 nw channels, a lane per channel. The chunk's
+// start state is walked forward once to leave the state in front of every
+// kSub tokens in LDS; then, from the last kSub tokens to the first, the states
+// in front of each token are formed again into registers and the tokens walked
+// backwards. dB and dC of a token are sums over channels: over a wavefront by
+// reduce_scatter, over the workgroup's wavefronts through LDS at the chunk's end, over
+// workgroups (more than 64 nw channels) by ssm_sum_bc_kernel, all in a fixed order.
+// dA_log, dD and db_dt leave as partial sums per chunk. 22 N slots per token and
+// wavefront for the states, 70 for the two sums over channels, as many for the rest.
+template <typename T, int N>
+__global__ __launch_bounds__(256, 2) void ssm_bwd_kernel(
+    ScanIn a, const T* __restrict__ u, const T* __restrict__ dt, const T* __restrict__ B, const T* __restrict__ C,
+    const T* __restrict__ z, const T* __restrict__ dy, int64_t lddy, const float* __restrict__ cst,
+    const float* __restrict__ H, const float* __restrict__ dstate_out, T* __restrict__ du_o, int64_t lddu,
+    T* __restrict__ ddt_o, int64_t ldddt, T* __restrict__ dz_o, int64_t lddz, T* __restrict__ dB_o, int64_t lddB,
+    T* __restrict__ dC_o, int64_t lddC, float* __restrict__ dstate, float* __restrict__ part,
+    float* __restrict__ bc_part) {
+  constexpr int W = 2 * N, NSUB = kBCL / kSub;
+  extern __shared__ __attribute__((aligned(16))) float smem[];
+  const int nw = blockDim.x >> 6, wave = threadIdx.x >> 6, lane = threadIdx.x & 63, E = a.E;
+  float* sBC = smem;                                       // [kBCL][2N]
+  float* sRed = smem + kBCL * W;                           // [kBCL][nw][2N]
+  float* sCk = sRed + kBCL * nw * W + wave * (NSUB - 1) * N * 64 + lane;  // [NSUB - 1][N][64] per wavefront
+  int w, cg;
+  const int CG = (E + blockDim.x - 1) / blockDim.x;
+  if (!tile_of_block(a.ntile, CG, w, cg)) return;
+  const int e = cg * blockDim.x + threadIdx.x;
+  const bool active = e < E;
+  const int ec = active ? e : E - 1;
+  const Tile tl = find_tile(a.offs, a.n_seq, a.rows, kBCL, w);
+  float* po = part + (int64_t)w * (N + 2) * E + e;
+  if (tl.seq < 0) {  // the partial sums have a place for it
+    if (active)
+      for (int n = 0; n < N + 2; ++n) po[(int64_t)n * E] = 0.f;
+    return;
+  }
+  const int t0 = tl.j * kBCL, nt = max(0, min(tl.len - t0, kBCL));
+  const int64_t r0 = (int64_t)tl.base + t0;
+  for (int i = threadIdx.x; i < nt * W; i += blockDim.x) {
+    const int col = i % W;
+    const int64_t row = r0 + i / W;
+    sBC[i] = to_f32(col < N ? B[row * a.ldB + col] : C[row * a.ldC + col - N]);
+  }
+  float a2[N], s[N], h[N], dA[N];
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    a2[n] = decay_rate(a.A_log[(int64_t)ec * N + n]);
+    dA[n] = 0.f;
+    const int64_t c = ((int64_t)w * N + n) * E + ec, q = ((int64_t)tl.seq * E + ec) * N + n;
+    s[n] = cst ? cst[c] : a.state ? a.state[q] : 0.f;
+    h[n] = cst ? H[c] : dstate_out ? dstate_out[q] : 0.f;
+  }
+  const float bias = a.b_dt ? a.b_dt[ec] : 0.f, Dv = a.D ? a.D[ec] : 0.f;
+  float dD = 0.f, dbias = 0.f;
+  __syncthreads();
+  const int nsub = (nt + kSub - 1) / kSub;
+  const T *us = u + r0 * a.ldu, *ds = dt + r0 * a.lddt, *zs = z ? z + r0 * a.ldz : nullptr, *gs = dy + r0 * lddy;
+  for (int b = 0; b < nsub - 1; ++b) {
+    T ru[kSub], rd[kSub];
+#pragma unroll
+    for (int i = 0; i < kSub; ++i) {  // all of these tokens exist
+      ru[i] = (us + (int64_t)(b * kSub + i) * a.ldu)[ec];
+      rd[i] = (ds + (int64_t)(b * kSub + i) * a.lddt)[ec];
+    }
+    if (b > 0) {
+#pragma unroll
+      for (int n = 0; n < N; ++n) sCk[((b - 1) * N + n) * 64] = s[n];
+    }
+#pragma unroll
+    for (int i = 0; i < kSub; ++i) {
+      const float d = softplus(to_f32(rd[i]) + bias), du = d * to_f32(ru[i]);
+      const float* x = &sBC[(b * kSub + i) * W];
+#pragma unroll
+      for (int n = 0; n < N; ++n) s[n] = fmaf(__builtin_amdgcn_exp2f(d * a2[n]), s[n], du * x[n]);
+    }
+  }
+  // s is now the state in front of the last kSub tokens
+  for (int b = nsub - 1; b >= 0; --b) {
+    T ru[kSub], rd[kSub], rz[kSub], rg[kSub];
+#pragma unroll
+    for (int i = 0; i < kSub; ++i) {
+      const int64_t t = min(b * kSub + i, nt - 1);
+      ru[i] = (us + t * a.ldu)[ec];
+      rd[i] = (ds + t * a.lddt)[ec];
+      rg[i] = (gs + t * lddy)[ec];
+      if (z) rz[i] = (zs + t * a.ldz)[ec];
+    }
+    float hist[kSub][N];  // the state in front of each token
+    if (b < nsub - 1) {
+      if (b > 0) {
+#pragma unroll
+        for (int n = 0; n < N; ++n) hist[0][n] = sCk[((b - 1) * N + n) * 64];
+      } else {
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+          const int64_t c = ((int64_t)w * N + n) * E + ec, q = ((int64_t)tl.seq * E + ec) * N + n;
+          hist[0][n] = cst ? cst[c] : a.state ? a.state[q] : 0.f;
+        }
+      }
+    } else {
+#pragma unroll
+      for (int n = 0; n < N; ++n) hist[0][n] = s[n];
+    }
+#pragma unroll
+    for (int i = 0; i + 1 < kSub; ++i) {
+      if (b * kSub + i + 1 < nt) {
+        const float d = softplus(to_f32(rd[i]) + bias), du = d * to_f32(ru[i]);
+        const float* x = &sBC[(b * kSub + i) * W];
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+          hist[i + 1][n] = fmaf(__builtin_amdgcn_exp2f(d * a2[n]), hist[i][n], du * x[n]);
+      }
+    }
+#pragma unroll
+    for (int i = kSub - 1; i >= 0; --i) {
+      const int t = b * kSub + i;
+      if (t >= nt) continue;  // the same for the whole workgroup
+      const float* x = &sBC[t * W];
+      const float uv = active ? to_f32(ru[i]) : 0.f, v = to_f32(rd[i]) + bias, gy = active ? to_f32(rg[i]) : 0.f;
+      const float d = softplus(v), du = d * uv;
+      float gate = 1.f, dgate = 0.f;
+      if (z) {
+        const float zv = to_f32(rz[i]), sg = rcp_fast(1.f + exp_fast(-zv));
+        gate = zv * sg;
+        dgate = sg * fmaf(zv, 1.f - sg, 1.f);
+      }
+      const float q = gy * gate;
+      float yv = 0.f, gB = 0.f, dd = 0.f, red[W];
+#pragma unroll
+      for (int n = 0; n < N; ++n) {
+        const float an = __builtin_amdgcn_exp2f(d * a2[n]);
+        const float as = an * hist[i][n], st = fmaf(du, x[n], as);
+        const float g = fmaf(q, x[N + n], h[n]);
+        yv = fmaf(st, x[N + n], yv);
+        gB = fmaf(g, x[n], gB);
+        const float ga = g * as;
+        dd = fmaf(ga, a2[n], dd);  // in units of 1 / ln 2
+        dA[n] = fmaf(ga, d, dA[n]);
+        h[n] = an * g;
+        red[n] = g * du;
+        red[N + n] = q * st;
+      }
+      yv = fmaf(Dv, uv, yv);
+      const float ddt = fmaf(dd, kLn2, uv * gB) * rcp_fast(1.f + exp_fast(-v));
+      dD = fmaf(q, uv, dD);
+      dbias += ddt;
+      if (active) {
+        const int64_t r = r0 + t;
+        st1(du_o + r * lddu + e, fmaf(Dv, q, d * gB));
+        st1(ddt_o + r * ldddt + e, ddt);
+        if (z) st1(dz_o + r * lddz + e, gy * yv * dgate);
+      }
+      const float tot = reduce_scatter<W>(red, lane);
+      if (lane % (64 / W) == 0) sRed[(t * nw + wave) * W + lane / (64 / W)] = tot;
+    }
+  }
+  if (active) {
+#pragma unroll
+    for (int n = 0; n < N; ++n) po[(int64_t)n * E] = dA[n] * (a2[n] * kLn2);
+    po[(int64_t)N * E] = dD;
+    po[(int64_t)(N + 1) * E] = dbias;
+    if (dstate && tl.j == 0) {
+#pragma unroll
+      for (int n = 0; n < N; ++n) dstate[((int64_t)tl.seq * E + e) * N + n] = h[n];
+    }
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < nt * W; i += blockDim.x) {
+    const int t = i / W, col = i % W;
+    float acc = 0.f;
+    for (int k = 0; k < nw; ++k) acc += sRed[(t * nw + k) * W + col];
+    const int64_t r = r0 + t;
+    if (bc_part) bc_part[((int64_t)cg * a.rows + r) * W + col] = acc;
+    else if (col < N) st1(dB_o + r * lddB + col, acc);
+    else st1(dC_o + r * lddC + col - N, acc);
+  }
+}
+
+// dB and dC over the channel groups. Rows that no sequence owns have no
+// partial sums and are left as they are.
+template <typename T, int N>
+__global__ __launch_bounds__(256) void ssm_sum_bc_kernel(const int* __restrict__ offs, int n_seq, int rows, int CG,
+                                                         const float* __restrict__ bc_part, T* __restrict__ dB,
+                                                         int64_t lddB, T* __restrict__ dC, int64_t lddC) {
+  constexpr int W = 2 * N;
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t row = i / W;
+  const int r0 = offs ? offs[0] : 0, r1 = offs ? min(offs[n_seq], rows) : n_seq;
+  if (row < r0 || row >= r1) return;
+  const int col = (int)(i % W);
+  float acc = 0.f;
+  for (int c = 0; c < CG; ++c) acc += bc_part[((int64_t)c * rows + row) * W + col];
+  if (col < N) st1(dB + row * lddB + col, acc);
+  else st1(dC + row * lddC + col - N, acc);
+}
+
+bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+
+constexpr int kCUs = 256;
+
+// ---- convolution plans
+// Forward tiles: 32 rows reread 3 of 32 rows; with few rows, shorter tiles
+// give the GPU more wavefronts to have in flight.
+int conv_rows(int rows, int CG) {
+  for (int R = 32; R > 8; R /= 2)
+    if ((int64_t)rows / R * CG >= (int64_t)kCUs * 8 * 64) return R;
+  return 8;
+}
+constexpr int kConvBwdRows = 32;
+// Partial sums of dw and db: as many threads as fill the GPU, at most 1,024 parts.
+void conv_parts(int n_seq, int rows, int CG, int& parts, int& per) {
+  const int tiles = rows / kConvBwdRows + n_seq;
+  int want = std::max(1, std::min(1024, kCUs * 16 * 64 / CG));
+  per = (tiles + want - 1) / want;
+  parts = (tiles + per - 1) / per;
+}
+
+template <typename T, int K, int CH>
+hipError_t conv_fwd(const ConvOp& a, void* state_out, void* u, int64_t ldu, hipStream_t s) {
+  const int CG = a.E / CH, R = a.offs ? conv_rows(a.rows, CG) : 8;
+  const int64_t tiles = a.offs ? (int64_t)a.rows / R + a.n_seq : a.n_seq, work = tiles * CG;
+  ssm_conv_kernel<T, K, CH><<<dim3((unsigned)((work + 255) / 256)), 256, 0, s>>>(
+      a.offs, a.n_seq, a.rows, a.E, R, work, static_cast<const T*>(a.x), a.ldx, a.w, a.b,
+      static_cast<const T*>(a.state), a.slots, a.n_slots, static_cast<T*>(state_out), static_cast<T*>(u), ldu);
+  return hipGetLastError();
+}
+
+template <typename T, int K, int CH>
+hipError_t conv_bwd(const ConvOp& a, const void* du, int64_t lddu, const void* dstate_out, void* dx, int64_t lddx,
+                    float* dw, float* db, void* dstate, float* ws, hipStream_t s) {
+  const int CG = a.E / CH;
+  int parts, per;
+  conv_parts(a.n_seq, a.rows, (a.E + 3) / 4, parts, per);
+  const int64_t work = (int64_t)parts * CG;
+  ssm_conv_bwd_kernel<T, K, CH><<<dim3((unsigned)((work + 255) / 256)), 256, 0, s>>>(
+      a.offs, a.n_seq, a.rows, a.E, kConvBwdRows, per, parts, static_cast<const T*>(a.x), a.ldx, a.w, a.b,
+      static_cast<const T*>(a.state), static_cast<const T*>(du), lddu, static_cast<const T*>(dstate_out),
+      static_cast<T*>(dx), lddx, static_cast<T*>(dstate), ws);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const int64_t n = (int64_t)(K + 1) * a.E;
+  sum_parts_kernel<<<dim3((unsigned)((n + 63) / 64)), 64 * kSumLanes, 0, s>>>(ws, parts, K, K + 1, a.E, dw, db,
+                                                                             nullptr);
+  return hipGetLastError();
+}
+
+// ---- scan plans
+// Chunk length of the forward scan: sequences run whole (0) while they give
+// every SIMD four wavefronts, or are too short to cut.
+int scan_chunk(int n_seq, int rows, int E, int L) {
+  const int64_t waves = (int64_t)n_seq * ((E + 63) / 64), fill = (int64_t)kCUs * 4 * 4;
+  if (L <= 2 * kTC || waves * 2 > fill) return 0;
+  const int64_t chunks = fill / waves;  // per sequence, were all of them L long
+  int64_t CL = (L + chunks - 1) / chunks;
+  CL = (CL + kTC - 1) / kTC * kTC;
+  CL = std::max<int64_t>(CL, kTC);
+  return CL < L ? (int)CL : 0;
+}
+
+ScanIn scan_in(const ScanOp& a, int CL) {
+  ScanIn in;
+  in.offs = a.offs; in.n_seq = a.n_seq; in.rows = a.rows; in.E = a.E; in.CL = CL;
+  in.ntile = a.offs ? a.rows / CL + a.n_seq : a.n_seq;
+  in.ldu = a.ldu; in.lddt = a.lddt; in.ldB = a.ldB; in.ldC = a.ldC; in.ldz = a.ldz;
+  in.A_log = a.A_log; in.D = a.D; in.b_dt = a.b_dt; in.state = a.state;
+  in.slots = a.slots; in.n_slots = a.n_slots;
+  return in;
+}
+
+template <typename T, int N>
+hipError_t scan_fwd(const ScanOp& a, float* state_out, void* y_, int64_t ldy, float* ws, hipStream_t s) {
+  const T *u = static_cast<const T*>(a.u), *dt = static_cast<const T*>(a.dt), *B = static_cast<const T*>(a.B),
+          *C = static_cast<const T*>(a.C), *z = static_cast<const T*>(a.z);
+  T* y = static_cast<T*>(y_);
+  if (!a.offs) {
+    const ScanIn in = scan_in(a, 1);
+    const unsigned gx = (a.E + 1024 / N - 1) / (1024 / N);
+    constexpr int SB = 4;
+    if ((int64_t)gx * a.n_seq >= (int64_t)kCUs * 4 * SB)
+      ssm_scan_token_kernel<T, N, SB><<<dim3(gx, (a.n_seq + SB - 1) / SB), 256, 0, s>>>(in, u, dt, B, C, z, state_out,
+                                                                                       y, ldy);
+    else
+      ssm_scan_token_kernel<T, N, 1><<<dim3(gx, a.n_seq), 256, 0, s>>>(in, u, dt, B, C, z, state_out, y, ldy);
+    return hipGetLastError();
+  }
+  const int CG = (a.E + 63) / 64, CL = scan_chunk(a.n_seq, a.rows, a.E, a.L);
+  if (!CL) {
+    const ScanIn in = scan_in(a, a.rows + 1);  // one tile per sequence
+    ssm_scan_kernel<T, N, false><<<dim3(tile_blocks(in.ntile, CG)), 64, 0, s>>>(in, u, dt, B, C, z, state_out, y, ldy,
+                                                                               nullptr, nullptr);
+    return hipGetLastError();
+  }
+  const ScanIn in = scan_in(a, CL);
+  float *cst = ws, *csum = ws + (int64_t)in.ntile * N * a.E;
+  ssm_scan_kernel<T, N, true><<<dim3(tile_blocks(in.ntile, CG)), 64, 0, s>>>(in, u, dt, B, nullptr, nullptr, nullptr,
+                                                                            nullptr, 0, cst, csum);
+  const int64_t n = (int64_t)a.n_seq * N * a.E;
+  ssm_combine_kernel<N><<<dim3((unsigned)((n + 255) / 256)), 256, 0, s>>>(in, cst, csum, nullptr, nullptr);
+  ssm_scan_kernel<T, N, false><<<dim3(tile_blocks(in.ntile, CG)), 64, 0, s>>>(in, u, dt, B, C, z, state_out, y, ldy,
+                                                                             cst, nullptr);
+  return hipGetLastError();
+}
+
+struct BwdPlan {
+  int nw, CG, ntile;
+  bool chunks;
+  size_t cst, csum, G, part, bc, total;  // in floats
+};
+BwdPlan bwd_plan(bool packed, int n_seq, int rows, int E, int N, int L) {
+  BwdPlan p;
+  p.nw = std::min(4, (E + 63) / 64);
+  p.CG = (E + 64 * p.nw - 1) / (64 * p.nw);
+  p.ntile = packed ? rows / kBCL + n_seq : n_seq;
+  p.chunks = packed && L > kBCL;
+  size_t o = 0;
+  const size_t st = p.chunks ? (size_t)p.ntile * N * E : 0;
+  p.cst = o; o += st;
+  p.G = o; o += st;
+  p.csum = o; o += p.chunks ? (size_t)p.ntile * E : 0;
+  p.part = o; o += (size_t)p.ntile * (N + 2) * E;
+  p.bc = o; o += p.CG > 1 ? (size_t)p.CG * rows * 2 * N : 0;
+  p.total = o;
+  return p;
+}
+
+template <typename T, int N>
+hipError_t scan_bwd(const ScanOp& a, const void* dy_, int64_t lddy, const float* dstate_out, const ScanGrads& g,
+                    float* ws, hipStream_t s) {
+  const T *u = static_cast<const T*>(a.u), *dt = static_cast<const T*>(a.dt), *B = static_cast<const T*>(a.B),
+          *C = static_cast<const T*>(a.C), *z = static_cast<const T*>(a.z), *dy = static_cast<const T*>(dy_);
+  const BwdPlan p = bwd_plan(a.offs != nullptr, a.n_seq, a.rows, a.E, N, a.L);
+  const ScanIn in = scan_in(a, kBCL);
+  float *cst = p.chunks ? ws + p.cst : nullptr, *G = p.chunks ? ws + p.G : nullptr, *part = ws + p.part,
+        *bc = p.CG > 1 ? ws + p.bc : nullptr;
+  if (p.chunks) {
+    ssm_bwd_local_kernel<T, N><<<dim3(tile_blocks(in.ntile, (a.E + 63) / 64)), 64, 0, s>>>(
+        in, u, dt, B, C, z, dy, lddy, cst, ws + p.csum, G);
+    const int64_t n = (int64_t)a.n_seq * N * a.E;
+    ssm_combine_kernel<N><<<dim3((unsigned)((n + 255) / 256)), 256, 0, s>>>(in, cst, ws + p.csum, G, dstate_out);
+  }
+  const size_t lds = sizeof(float) * (kBCL * 2 * N * (1 + p.nw) + (size_t)p.nw * (kBCL / kSub - 1) * N * 64);
+  hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&ssm_bwd_kernel<T, N>),
+                                     hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+  if (e != hipSuccess) return e;
+  ssm_bwd_kernel<T, N><<<dim3(tile_blocks(in.ntile, p.CG)), 64 * p.nw, lds, s>>>(
+      in, u, dt, B, C, z, dy, lddy, cst, G, dstate_out, static_cast<T*>(g.du), g.lddu, static_cast<T*>(g.ddt),
+      g.ldddt, static_cast<T*>(g.dz), g.lddz, static_cast<T*>(g.dB), g.lddB, static_cast<T*>(g.dC), g.lddC, g.dstate,
+      part, bc);
+  e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  if (bc) {
+    const int64_t n = (int64_t)a.rows * 2 * N;
+    ssm_sum_bc_kernel<T, N><<<dim3((unsigned)((n + 255) / 256)), 256, 0, s>>>(
+        a.offs, a.n_seq, a.rows, p.CG, bc, static_cast<T*>(g.dB), g.lddB, static_cast<T*>(g.dC), g.lddC);
+  }
+  const int64_t n = (int64_t)(N + 2) * a.E;
+  sum_parts_kernel<<<dim3((unsigned)((n + 63) / 64)), 64 * kSumLanes, 0, s>>>(part, in.ntile, N, N + 2, a.E, g.dA_log,
+                                                                             g.dD, g.db_dt);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_ssm_conv(const ConvOp& a, void* state_out, void* u, int64_t ldu, hipStream_t s) {
+  const int ch = a.bf16 ? 8 : 4;
+  const bool vec = a.E % ch == 0 && a.ldx % ch == 0 && ldu % ch == 0 && aligned16(a.x) && aligned16(u) &&
+                   aligned16(a.state) && aligned16(state_out);
+#define TCL_CONV(KK)                                                                                       \
+  case KK:                                                                                                 \
+    if (a.bf16) return vec ? conv_fwd<uint16_t, KK, 8>(a, state_out, u, ldu, s)                            \
+                           : conv_fwd<uint16_t, KK, 1>(a, state_out, u, ldu, s);                           \
+    return vec ? conv_fwd<float, KK, 4>(a, state_out, u, ldu, s) : conv_fwd<float, KK, 1>(a, state_out, u, ldu, s);
+  switch (a.K) {
+    TCL_CONV(1)
+    TCL_CONV(2)
+    TCL_CONV(3)
+    TCL_CONV(4)
+  }
+#undef TCL_CONV
+  return hipErrorInvalidValue;
+}
+
+size_t ssm_conv_workspace_bytes(int n_seq, int rows, int E, int K) {
+  int parts, per;
+  conv_parts(n_seq, rows, (E + 3) / 4, parts, per);
+  return (size_t)parts * (K + 1) * E * sizeof(float);
+}
+
+hipError_t launch_ssm_conv_bwd(const ConvOp& a, const void* du, int64_t lddu, const void* dstate_out, void* dx,
+                               int64_t lddx, float* dw, float* db, void* dstate, float* ws, hipStream_t s) {
+  const bool vec = a.E % 4 == 0 && a.ldx % 4 == 0 && lddu % 4 == 0 && lddx % 4 == 0 && aligned16(a.x) &&
+                   aligned16(du) && aligned16(dx) && aligned16(a.state) && aligned16(dstate_out) && aligned16(dstate);
+#define TCL_CONV(KK)                                                                                          \
+  case KK:                                                                                                    \
+    if (a.bf16)                                                                                               \
+      return vec ? conv_bwd<uint16_t, KK, 4>(a, du, lddu, dstate_out, dx, lddx, dw, db, dstate, ws, s)        \
+                 : conv_bwd<uint16_t, KK, 1>(a, du, lddu, dstate_out, dx, lddx, dw, db, dstate, ws, s);       \
+    return vec ? conv_bwd<float, KK, 4>(a, du, lddu, dstate_out, dx, lddx, dw, db, dstate, ws, s)             \
+               : conv_bwd<float, KK, 1>(a, du, lddu, dstate_out, dx, lddx, dw, db, dstate, ws, s);
+  switch (a.K) {
+    TCL_CONV(1)
+    TCL_CONV(2)
+    TCL_CONV(3)
+    TCL_CONV(4)
+  }
+#undef TCL_CONV
+  return hipErrorInvalidValue;
+}
+
+size_t ssm_scan_workspace_bytes(int n_seq, int rows, int E, int N, int L) {
+  const int CL = scan_chunk(n_seq, rows, E, L);
+  return CL ? ((size_t)rows / CL + n_seq) * (N + 1) * E * sizeof(float) : 0;
+}
+
+hipError_t launch_ssm_scan(const ScanOp& a, float* state_out, void* y, int64_t ldy, float* ws, hipStream_t s) {
+  if (a.bf16)
+    return a.N == 16 ? scan_fwd<uint16_t, 16>(a, state_out, y, ldy, ws, s)
+                     : scan_fwd<uint16_t, 8>(a, state_out, y, ldy, ws, s);
+  return a.N == 16 ? scan_fwd<float, 16>(a, state_out, y, ldy, ws, s) : scan_fwd<float, 8>(a, state_out, y, ldy, ws, s);
+}
+
+size_t ssm_scan_bwd_workspace_bytes(int n_seq, int rows, int E, int N, int L) {
+  // (a call without offsets needs no more than one with them)
+  return bwd_plan(true, n_seq, rows, E, N, L).total * sizeof(float);
+}
+
+hipError_t launch_ssm_scan_bwd(const ScanOp& a, const void* dy, int64_t lddy, const float* dstate_out,
+                               const ScanGrads& g, float* ws, hipStream_t s) {
+  if (a.bf16)
+    return a.N == 16 ? scan_bwd<uint16_t, 16>(a, dy, lddy, dstate_out, g, ws, s)
+                     : scan_bwd<uint16_t, 8>(a, dy, lddy, dstate_out, g, ws, s);
+  return a.N == 16 ? scan_bwd<float, 16>(a, dy, lddy, dstate_out, g, ws, s)
+                   : scan_bwd<float, 8>(a, dy, lddy, dstate_out, g, ws, s);
+}
+
+}  // namespace tcl
