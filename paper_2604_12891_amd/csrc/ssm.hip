@@ -25,6 +25,49 @@ __device__ __forceinline__ float to_f32(uint16_t v) { return bf16_to_f32(v); }
 __device__ __forceinline__ void st1(float* p, float v) { *p = v; }
 __device__ __forceinline__ void st1(uint16_t* p, float v) { *p = f32_to_bf16(v); }
 
+// Element of a wave-uniform row at a lane's byte offset, addressed as scalar base
+// plus 32-bit lane offset. Left to itself the compiler adds the lane's part to the matrix's
+// base once and the row's part per access, which costs a 64-bit vector sum and a
+// register pair each (100 registers of the gradient kernel); the empty asm keeps the row's
+// address a scalar value of its own.
+typedef __attribute__((address_space(1))) char gchar;
+template <typename T>
+__device__ __forceinline__ gchar* scalar_row(const T* row) {
+  gchar* p = (gchar*)(row);
+  asm("" : "+s"(p));
+  return p;
+}
+// (and the lane's part a 32-bit value at each access)
+__device__ __forceinline__ uint32_t lane_part(uint32_t bytes) {
+  asm("" : "+v"(bytes));
+  return bytes;
+}
+template <typename T>
+__device__ __forceinline__ T ld_at(const T* row, uint32_t bytes) {
+  return *(const __attribute__((address_space(1))) T*)(scalar_row(row) + lane_part(bytes));
+}
+__device__ __forceinline__ void st_at(float* row, uint32_t bytes, float v) {
+  *(__attribute__((address_space(1))) float*)(scalar_row(row) + lane_part(bytes)) = v;
+}
+__device__ __forceinline__ void st_at(uint16_t* row, uint32_t bytes, float v) {
+  *(__attribute__((address_space(1))) uint16_t*)(scalar_row(row) + lane_part(bytes)) = f32_to_bf16(v);
+}
+// N consecutive floats there, N a multiple of 4.
+template <int N>
+__device__ __forceinline__ void ld_vec(const float* row, uint32_t bytes, float* v) {
+#pragma unroll
+  for (int n = 0; n < N; n += 4) {
+    const floatx4 x = *reinterpret_cast<const floatx4*>(reinterpret_cast<const char*>(row) + bytes + 4 * n);
+    v[n] = x.x; v[n + 1] = x.y; v[n + 2] = x.z; v[n + 3] = x.w;
+  }
+}
+template <int N>
+__device__ __forceinline__ void st_vec(float* row, uint32_t bytes, const float* v) {
+#pragma unroll
+  for (int n = 0; n < N; n += 4)
+    *reinterpret_cast<floatx4*>(reinterpret_cast<char*>(row) + bytes + 4 * n) = floatx4{v[n], v[n + 1], v[n + 2], v[n + 3]};
+}
+
 // CH adjacent channels of a row; the storage type's raw bits, widened at use.
 template <typename T, int CH> struct Pack { T v[CH]; };
 template <> struct Pack<float, 4> { floatx4 v; };
@@ -66,15 +109,17 @@ struct Tile {
 // Tile w of R rows. Offsets are read as lying in [0, rows], so a wrong one
 // cannot lead outside the activations.
 __device__ __forceinline__ Tile find_tile(const int* __restrict__ offs, int n_seq, int rows, int R, int w) {
-  Tile t;
+  Tile t = {-1, 0, 0, 0};
   if (!offs) {
-    t.seq = w < n_seq ? w : -1;
-    t.j = 0;
-    t.base = w;
-    t.len = 1;
+    if (w < n_seq) t = {w, 0, w, 1};
     return t;
   }
   int lo = 0, hi = n_seq;  // key(lo) <= w < key(hi), once the ends are taken
+  if (R > rows) {          // one tile per sequence
+    if (w >= n_seq) return t;
+    lo = w;
+    hi = w + 1;
+  }
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;
     if (offs[mid] / R + mid <= w) lo = mid;
@@ -428,20 +473,21 @@ __global__ __launch_bounds__(64, 4) void ssm_scan_kernel(ScanIn a, const T* __re
   const bool active = e < E;
   const int ec = active ? e : E - 1;
 
+  const uint32_t le = ec * sizeof(T), lf = ec * 4, ln = ec * N * 4;  // a lane's place in a row
   float a2[N], s[N];
+  ld_vec<N>(a.A_log, ln, a2);
 #pragma unroll
   for (int n = 0; n < N; ++n) {
-    a2[n] = decay_rate(a.A_log[(int64_t)ec * N + n]);
+    a2[n] = decay_rate(a2[n]);
     s[n] = 0.f;
   }
   const int sl = slot_of(a.slots, a.n_slots, tl.seq);
   if (!LOCAL) {
     if (cst) {
 #pragma unroll
-      for (int n = 0; n < N; ++n) s[n] = cst[((int64_t)w * N + n) * E + ec];
+      for (int n = 0; n < N; ++n) s[n] = ld_at(cst + ((int64_t)w * N + n) * E, lf);
     } else if (a.state && sl >= 0) {
-#pragma unroll
-      for (int n = 0; n < N; ++n) s[n] = a.state[((int64_t)sl * E + ec) * N + n];
+      ld_vec<N>(a.state + (int64_t)sl * E * N, ln, s);
     }
   }
   const float bias = a.b_dt ? a.b_dt[ec] : 0.f, Dv = !LOCAL && a.D ? a.D[ec] : 0.f;
@@ -451,36 +497,41 @@ __global__ __launch_bounds__(64, 4) void ssm_scan_kernel(ScanIn a, const T* __re
     const T *us = u + r0 * a.ldu, *ds = dt + r0 * a.lddt, *zs = z ? z + r0 * a.ldz : nullptr;
     const T *Bs = B + r0 * a.ldB, *Cs = LOCAL ? nullptr : C + r0 * a.ldC;
     T* ys = LOCAL ? nullptr : y + r0 * ldy;
-    // value i of a stage: token i / (2N), B's or C's column (LOCAL: B's only)
-    constexpr int W = LOCAL ? N : 2 * N, PER = kTC * W / 64;
-    T st[PER];
-    auto stage = [&](int t) {
-#pragma unroll
-      for (int i = 0; i < PER; ++i) {
-        const int k = i * 64 + lane, col = k % W, row = min(t + k / W, t1 - 1);
-        st[i] = col < N ? Bs[(int64_t)row * a.ldB + col] : Cs[(int64_t)row * a.ldC + col - N];
-      }
-    };
-    constexpr int U = 4;
+    // A stage: lane l takes column l % W (B's, then C's; LOCAL: B's only) of every
+    // RW-th row from l / W on. Rows past the end read the last one again.
+    constexpr int W = LOCAL ? N : 2 * N, RW = 64 / W, PER = kTC / RW;
+    const int col = lane % W;
+    const bool isB = LOCAL || col < N;
+    const int64_t ldS = isB ? a.ldB : a.ldC;
+    const T* src = isB ? Bs + col : Cs + (col - N);
+    const T* last = src + (int64_t)(t1 - 1) * ldS;
+    constexpr int U = 2;
     T nu[U], nd[U], nz[U];
     auto load = [&](int t) {
 #pragma unroll
       for (int i = 0; i < U; ++i) {
         const int r = min(t + i, t1 - 1);
-        nu[i] = (us + (int64_t)r * a.ldu)[ec];
-        nd[i] = (ds + (int64_t)r * a.lddt)[ec];
-        if (!LOCAL && z) nz[i] = (zs + (int64_t)r * a.ldz)[ec];
+        nu[i] = ld_at(us + r * a.ldu, le);
+        nd[i] = ld_at(ds + r * a.lddt, le);
+        if (!LOCAL && z) nz[i] = ld_at(zs + r * a.ldz, le);
       }
     };
     float sum = 0.f;
-    stage(t0);
     load(t0);
     for (int tc = t0; tc < t1; tc += kTC) {
+      T st[PER];
+      const T* q = src + (tc + lane / W) * ldS;
+      if (tc + kTC <= t1) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i, q += RW * ldS) st[i] = *q;
+      } else {
+#pragma unroll
+        for (int i = 0; i < PER; ++i, q += RW * ldS) st[i] = tc + lane / W + i * RW < t1 ? *q : *last;
+      }
       __syncthreads();
 #pragma unroll
       for (int i = 0; i < PER; ++i) sBC[i * 64 + lane] = to_f32(st[i]);
       __syncthreads();
-      if (tc + kTC < t1) stage(tc + kTC);
       const int te = min(t1, tc + kTC);
       for (int tg = tc; tg < te; tg += U) {
         T cu[U], cd[U], cz[U];
@@ -507,20 +558,19 @@ __global__ __launch_bounds__(64, 4) void ssm_scan_kernel(ScanIn a, const T* __re
           if (!LOCAL) {
             acc = fmaf(Dv, uv, acc);
             if (z) acc *= silu(to_f32(cz[i]));
-            if (active) st1((ys + (int64_t)t * ldy) + e, acc);
+            if (active) st_at(ys + t * ldy, le, acc);
           }
         }
       }
     }
-    if (LOCAL && active) csum[(int64_t)w * E + e] = sum;
+    if (LOCAL && active) st_at(csum + (int64_t)w * E, lf, sum);
   }
   if (!active) return;
   if (LOCAL) {
 #pragma unroll
-    for (int n = 0; n < N; ++n) cst[((int64_t)w * N + n) * E + e] = s[n];
+    for (int n = 0; n < N; ++n) st_at(cst + ((int64_t)w * N + n) * E, lf, s[n]);
   } else if (state_out && sl >= 0 && t1 == tl.len) {
-#pragma unroll
-    for (int n = 0; n < N; ++n) state_out[((int64_t)sl * E + e) * N + n] = s[n];
+    st_vec<N>(state_out + (int64_t)sl * E * N, ln, s);
   }
 }
 
@@ -657,6 +707,17 @@ __global__ __launch_bounds__(256) void ssm_scan_token_kernel(ScanIn a, const T* 
 constexpr int kBCL = 32;  // tokens per chunk
 constexpr int kSub = 8;   // tokens whose states are held in registers together
 
+// nt rows of B | C, widened, into LDS by n threads (a multiple of 2N).
+template <typename T, int N>
+__device__ __forceinline__ void stage_bc(float* s, const T* B, int64_t ldB, const T* C, int64_t ldC, int nt, int tid,
+                                         int n) {
+  const int col = tid % (2 * N), step = n / (2 * N);
+  const int64_t ld = col < N ? ldB : ldC;
+  int row = tid / (2 * N);
+  const T* q = (col < N ? B + col : C + (col - N)) + row * ld;
+  for (; row < nt; row += step, q += step * ld) s[row * 2 * N + col] = to_f32(*q);
+}
+
 template <typename T, int N>
 __global__ __launch_bounds__(64, 4) void ssm_bwd_local_kernel(ScanIn a, const T* __restrict__ u,
                                                               const T* __restrict__ dt, const T* __restrict__ B,
@@ -675,33 +736,31 @@ __global__ __launch_bounds__(64, 4) void ssm_bwd_local_kernel(ScanIn a, const T*
   const bool active = e < E;
   const int ec = active ? e : E - 1;
   const int64_t r0 = tl.base;
+  const uint32_t le = ec * sizeof(T), lf = ec * 4;
   float a2[N], s[N], p[N], g[N];
+  ld_vec<N>(a.A_log, ec * N * 4, a2);
 #pragma unroll
   for (int n = 0; n < N; ++n) {
-    a2[n] = decay_rate(a.A_log[(int64_t)ec * N + n]);
+    a2[n] = decay_rate(a2[n]);
     s[n] = 0.f;
     p[n] = 1.f;
     g[n] = 0.f;
   }
   const float bias = a.b_dt ? a.b_dt[ec] : 0.f;
   float sum = 0.f;
-  for (int i = lane; i < (t1 - t0) * 2 * N; i += 64) {
-    const int col = i % (2 * N);
-    const int64_t row = r0 + t0 + i / (2 * N);
-    sBC[i] = to_f32(col < N ? B[row * a.ldB + col] : C[row * a.ldC + col - N]);
-  }
+  stage_bc<T, N>(sBC, B + (r0 + t0) * a.ldB, a.ldB, C + (r0 + t0) * a.ldC, a.ldC, t1 - t0, lane, 64);
   __syncthreads();
   if (t0 < t1) {
-    constexpr int U = 4;
+    constexpr int U = 2;
     T nu[U], nd[U], nz[U], ng[U];
     auto load = [&](int t) {
 #pragma unroll
       for (int i = 0; i < U; ++i) {
         const int64_t r = r0 + min(t + i, t1 - 1);
-        nu[i] = (u + r * a.ldu)[ec];
-        nd[i] = (dt + r * a.lddt)[ec];
-        ng[i] = (dy + r * lddy)[ec];
-        if (z) nz[i] = (z + r * a.ldz)[ec];
+        nu[i] = ld_at(u + r * a.ldu, le);
+        nd[i] = ld_at(dt + r * a.lddt, le);
+        ng[i] = ld_at(dy + r * lddy, le);
+        if (z) nz[i] = ld_at(z + r * a.ldz, le);
       }
     };
     load(t0);
@@ -734,11 +793,11 @@ __global__ __launch_bounds__(64, 4) void ssm_bwd_local_kernel(ScanIn a, const T*
     }
   }
   if (!active) return;
-  csum[(int64_t)w * E + e] = sum;
+  st_at(csum + (int64_t)w * E, lf, sum);
 #pragma unroll
   for (int n = 0; n < N; ++n) {
-    cst[((int64_t)w * N + n) * E + e] = s[n];
-    G[((int64_t)w * N + n) * E + e] = g[n];
+    st_at(cst + ((int64_t)w * N + n) * E, lf, s[n]);
+    st_at(G + ((int64_t)w * N + n) * E, lf, g[n]);
   }
 }
 
@@ -747,42 +806,41 @@ __device__ __forceinline__ float dpp(float v) {
   return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xF, 0xF, false));
 }
 
-// Sums of M = 32 or 16 values over the 64 lanes, scattered: lane l ends with the
-// total of value l / (64 / M). Halves of the values go to halves of the lanes step by
-// step (half-wave and row swaps route a pair at once; within rows of 16 by
-// DPP: rotation by 8, mirrors of 8, quad permutations), M - 1 additions and as many
-// moves instead of 6 M of each.
+// Sums of many values over the 64 lanes, scattered over the lanes: halves of the
+// values go to halves of the lanes step by step, half-wave and row swaps routing a pair at
+// once, then within rows of 16 by DPP (rotation by 8, mirrors of 8, quad
+// permutations). Some 2 M operations for M values instead of 12 M.
+__device__ __forceinline__ float swap_add32(float a, float b) {  // lanes 0-31: a's sums, 32-63: b's
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(a), __float_as_uint(b), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+__device__ __forceinline__ float swap_add16(float a, float b) {  // rows 0, 2 of 16: a's sums, 1, 3: b's
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(a), __float_as_uint(b), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+// M = 8 or 4 values over rows of 16 lanes: lane l of a row ends with value l M / 16's total.
 template <int M>
-__device__ __forceinline__ float reduce_scatter(float* v, int lane) {
-#pragma unroll
-  for (int i = 0; i < M / 2; ++i) {
-    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v[i]), __float_as_uint(v[M / 2 + i]), false, false);
-    v[i] = __uint_as_float(r[0]) + __uint_as_float(r[1]);
-  }
-#pragma unroll
-  for (int i = 0; i < M / 4; ++i) {
-    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v[i]), __float_as_uint(v[M / 4 + i]), false, false);
-    v[i] = __uint_as_float(r[0]) + __uint_as_float(r[1]);
-  }
+__device__ __forceinline__ float reduce_rows(const float* v, int lane) {
   const bool b3 = (lane & 8) != 0, b2 = (lane & 4) != 0, b1 = (lane & 2) != 0;
+  float x[M / 2], y[M / 4];
 #pragma unroll
-  for (int i = 0; i < M / 8; ++i) {  // row_ror:8
-    const float mine = b3 ? v[M / 8 + i] : v[i], other = b3 ? v[i] : v[M / 8 + i];
-    v[i] = mine + dpp<0x128>(other);
+  for (int i = 0; i < M / 2; ++i) {  // row_ror:8
+    const float mine = b3 ? v[M / 2 + i] : v[i], other = b3 ? v[i] : v[M / 2 + i];
+    x[i] = mine + dpp<0x128>(other);
   }
 #pragma unroll
-  for (int i = 0; i < M / 16; ++i) {  // row_half_mirror: lane ^ 7
-    const float mine = b2 ? v[M / 16 + i] : v[i], other = b2 ? v[i] : v[M / 16 + i];
-    v[i] = mine + dpp<0x141>(other);
+  for (int i = 0; i < M / 4; ++i) {  // row_half_mirror: lane ^ 7
+    const float mine = b2 ? x[M / 4 + i] : x[i], other = b2 ? x[i] : x[M / 4 + i];
+    y[i] = mine + dpp<0x141>(other);
   }
-  float z;
-  if constexpr (M == 32) {
-    const float mine = b1 ? v[1] : v[0], other = b1 ? v[0] : v[1];
-    z = mine + dpp<0x4E>(other);  // quad_perm: lane ^ 2
+  float s;
+  if constexpr (M == 8) {
+    const float mine = b1 ? y[1] : y[0], other = b1 ? y[0] : y[1];
+    s = mine + dpp<0x4E>(other);  // quad_perm: lane ^ 2
   } else {
-    z = v[0] + dpp<0x4E>(v[0]);
+    s = y[0] + dpp<0x4E>(y[0]);
   }
-  return z + dpp<0xB1>(z);  // lane ^ 1
+  return s + dpp<0xB1>(s);  // lane ^ 1
 }
 
 // A workgroup takes one chunk of 64 nw channels, a lane per channel. The chunk's
@@ -790,7 +848,7 @@ __device__ __forceinline__ float reduce_scatter(float* v, int lane) {
 // kSub tokens in LDS; then, from the last kSub tokens to the first, the states
 // in front of each token are formed again into registers and the tokens walked
 // backwards. dB and dC of a token are sums over channels: over a wavefront by
-// reduce_scatter, over the workgroup's wavefronts through LDS at the chunk's end, over
+// swaps and DPP, over the workgroup's wavefronts through LDS, over
 // workgroups (more than 64 nw channels) by ssm_sum_bc_kernel, all in a fixed order.
 // dA_log, dD and db_dt leave as partial sums per chunk. 22 N slots per token and
 // wavefront for the states, 70 for the two sums over channels, as many for the rest.
@@ -806,8 +864,8 @@ __global__ __launch_bounds__(256, 2) void ssm_bwd_kernel(
   extern __shared__ __attribute__((aligned(16))) float smem[];
   const int nw = blockDim.x >> 6, wave = threadIdx.x >> 6, lane = threadIdx.x & 63, E = a.E;
   float* sBC = smem;                                       // [kBCL][2N]
-  float* sRed = smem + kBCL * W;                           // [kBCL][nw][2N]
-  float* sCk = sRed + kBCL * nw * W + wave * (NSUB - 1) * N * 64 + lane;  // [NSUB - 1][N][64] per wavefront
+  float* sRed = smem + kBCL * W;                           // [kSub][nw][2N]
+  float* sCk = sRed + kSub * nw * W + wave * NSUB * N * 64 + lane;  // [NSUB][N][64] per wavefront
   int w, cg;
   const int CG = (E + blockDim.x - 1) / blockDim.x;
   if (!tile_of_block(a.ntile, CG, w, cg)) return;
@@ -815,43 +873,49 @@ __global__ __launch_bounds__(256, 2) void ssm_bwd_kernel(
   const bool active = e < E;
   const int ec = active ? e : E - 1;
   const Tile tl = find_tile(a.offs, a.n_seq, a.rows, kBCL, w);
-  float* po = part + (int64_t)w * (N + 2) * E + e;
+  float* po = part + (int64_t)w * (N + 2) * E;
   if (tl.seq < 0) {  // the partial sums have a place for it
     if (active)
-      for (int n = 0; n < N + 2; ++n) po[(int64_t)n * E] = 0.f;
+      for (int n = 0; n < N + 2; ++n) po[(int64_t)n * E + e] = 0.f;
     return;
   }
   const int t0 = tl.j * kBCL, nt = max(0, min(tl.len - t0, kBCL));
   const int64_t r0 = (int64_t)tl.base + t0;
-  for (int i = threadIdx.x; i < nt * W; i += blockDim.x) {
-    const int col = i % W;
-    const int64_t row = r0 + i / W;
-    sBC[i] = to_f32(col < N ? B[row * a.ldB + col] : C[row * a.ldC + col - N]);
-  }
+  stage_bc<T, N>(sBC, B + r0 * a.ldB, a.ldB, C + r0 * a.ldC, a.ldC, nt, threadIdx.x, blockDim.x);
+  const uint32_t le = ec * sizeof(T), lf = ec * 4, ln = ec * N * 4;
   float a2[N], s[N], h[N], dA[N];
+  ld_vec<N>(a.A_log, ln, a2);
 #pragma unroll
   for (int n = 0; n < N; ++n) {
-    a2[n] = decay_rate(a.A_log[(int64_t)ec * N + n]);
-    dA[n] = 0.f;
-    const int64_t c = ((int64_t)w * N + n) * E + ec, q = ((int64_t)tl.seq * E + ec) * N + n;
-    s[n] = cst ? cst[c] : a.state ? a.state[q] : 0.f;
-    h[n] = cst ? H[c] : dstate_out ? dstate_out[q] : 0.f;
+    a2[n] = decay_rate(a2[n]);
+    s[n] = h[n] = dA[n] = 0.f;
+  }
+  if (cst) {  // the state in front of the chunk
+#pragma unroll
+    for (int n = 0; n < N; ++n) s[n] = ld_at(cst + ((int64_t)w * N + n) * E, lf);
+  } else if (a.state) {
+    ld_vec<N>(a.state + (int64_t)tl.seq * E * N, ln, s);
+  }
+  if (cst) {
+#pragma unroll
+    for (int n = 0; n < N; ++n) h[n] = ld_at(H + ((int64_t)w * N + n) * E, lf);
+  } else if (dstate_out) {
+    ld_vec<N>(dstate_out + (int64_t)tl.seq * E * N, ln, h);
   }
   const float bias = a.b_dt ? a.b_dt[ec] : 0.f, Dv = a.D ? a.D[ec] : 0.f;
   float dD = 0.f, dbias = 0.f;
   __syncthreads();
   const int nsub = (nt + kSub - 1) / kSub;
   const T *us = u + r0 * a.ldu, *ds = dt + r0 * a.lddt, *zs = z ? z + r0 * a.ldz : nullptr, *gs = dy + r0 * lddy;
-  for (int b = 0; b < nsub - 1; ++b) {
+  for (int b = 0; b < nsub; ++b) {  // the states in front of every kSub tokens
+#pragma unroll
+    for (int n = 0; n < N; ++n) sCk[(b * N + n) * 64] = s[n];
+    if (b == nsub - 1) break;
     T ru[kSub], rd[kSub];
 #pragma unroll
     for (int i = 0; i < kSub; ++i) {  // all of these tokens exist
-      ru[i] = (us + (int64_t)(b * kSub + i) * a.ldu)[ec];
-      rd[i] = (ds + (int64_t)(b * kSub + i) * a.lddt)[ec];
-    }
-    if (b > 0) {
-#pragma unroll
-      for (int n = 0; n < N; ++n) sCk[((b - 1) * N + n) * 64] = s[n];
+      ru[i] = ld_at(us + (b * kSub + i) * a.ldu, le);
+      rd[i] = ld_at(ds + (b * kSub + i) * a.lddt, le);
     }
 #pragma unroll
     for (int i = 0; i < kSub; ++i) {
@@ -859,43 +923,42 @@ __global__ __launch_bounds__(256, 2) void ssm_bwd_kernel(
       const float* x = &sBC[(b * kSub + i) * W];
 #pragma unroll
       for (int n = 0; n < N; ++n) s[n] = fmaf(__builtin_amdgcn_exp2f(d * a2[n]), s[n], du * x[n]);
+      __builtin_amdgcn_sched_barrier(0);
     }
   }
-  // s is now the state in front of the last kSub tokens
+  // what the lane holds of a token's 2N sums: dB or dC by its half, the state's parity by its
+  // row, the pair of states within the row
+  const int place = lane / 32 * N + lane % 16 / (32 / N) * 2 + lane / 16 % 2;
+  T cu, cd, cz, cg_;  // the token's inputs, one token ahead
+  auto load = [&](int t) {
+    const int64_t r = max(t, 0);
+    cu = ld_at(us + r * a.ldu, le);
+    cd = ld_at(ds + r * a.lddt, le);
+    cg_ = ld_at(gs + r * lddy, le);
+    if (z) cz = ld_at(zs + r * a.ldz, le);
+  };
+  if (nt > 0) load(nt - 1);
   for (int b = nsub - 1; b >= 0; --b) {
-    T ru[kSub], rd[kSub], rz[kSub], rg[kSub];
+    const float* ck = sCk + b * N * 64;
+    float hist[kSub - 1][N];  // the state in front of each token but the first
+    {
+      T ru[kSub - 1], rd[kSub - 1];
 #pragma unroll
-    for (int i = 0; i < kSub; ++i) {
-      const int64_t t = min(b * kSub + i, nt - 1);
-      ru[i] = (us + t * a.ldu)[ec];
-      rd[i] = (ds + t * a.lddt)[ec];
-      rg[i] = (gs + t * lddy)[ec];
-      if (z) rz[i] = (zs + t * a.ldz)[ec];
-    }
-    float hist[kSub][N];  // the state in front of each token
-    if (b < nsub - 1) {
-      if (b > 0) {
-#pragma unroll
-        for (int n = 0; n < N; ++n) hist[0][n] = sCk[((b - 1) * N + n) * 64];
-      } else {
-#pragma unroll
-        for (int n = 0; n < N; ++n) {
-          const int64_t c = ((int64_t)w * N + n) * E + ec, q = ((int64_t)tl.seq * E + ec) * N + n;
-          hist[0][n] = cst ? cst[c] : a.state ? a.state[q] : 0.f;
-        }
+      for (int i = 0; i + 1 < kSub; ++i) {
+        const int64_t t = min(b * kSub + i, nt - 1);
+        ru[i] = ld_at(us + t * a.ldu, le);
+        rd[i] = ld_at(ds + t * a.lddt, le);
       }
-    } else {
 #pragma unroll
-      for (int n = 0; n < N; ++n) hist[0][n] = s[n];
-    }
+      for (int i = 0; i + 1 < kSub; ++i) {
+        if (b * kSub + i + 1 < nt) {
+          const float d = softplus(to_f32(rd[i]) + bias), du = d * to_f32(ru[i]);
+          const float* x = &sBC[(b * kSub + i) * W];
 #pragma unroll
-    for (int i = 0; i + 1 < kSub; ++i) {
-      if (b * kSub + i + 1 < nt) {
-        const float d = softplus(to_f32(rd[i]) + bias), du = d * to_f32(ru[i]);
-        const float* x = &sBC[(b * kSub + i) * W];
-#pragma unroll
-        for (int n = 0; n < N; ++n)
-          hist[i + 1][n] = fmaf(__builtin_amdgcn_exp2f(d * a2[n]), hist[i][n], du * x[n]);
+          for (int n = 0; n < N; ++n)
+            hist[i][n] = fmaf(__builtin_amdgcn_exp2f(d * a2[n]), i ? hist[i - 1][n] : ck[n * 64], du * x[n]);
+        }
+        __builtin_amdgcn_sched_barrier(0);
       }
     }
 #pragma unroll
@@ -903,20 +966,25 @@ __global__ __launch_bounds__(256, 2) void ssm_bwd_kernel(
       const int t = b * kSub + i;
       if (t >= nt) continue;  // the same for the whole workgroup
       const float* x = &sBC[t * W];
-      const float uv = active ? to_f32(ru[i]) : 0.f, v = to_f32(rd[i]) + bias, gy = active ? to_f32(rg[i]) : 0.f;
+      const float uv = active ? to_f32(cu) : 0.f, v = to_f32(cd) + bias, gy = active ? to_f32(cg_) : 0.f;
+      const float zv = z ? to_f32(cz) : 0.f;
+      load(t - 1);
       const float d = softplus(v), du = d * uv;
       float gate = 1.f, dgate = 0.f;
       if (z) {
-        const float zv = to_f32(rz[i]), sg = rcp_fast(1.f + exp_fast(-zv));
+        const float sg = rcp_fast(1.f + exp_fast(-zv));
         gate = zv * sg;
         dgate = sg * fmaf(zv, 1.f - sg, 1.f);
       }
       const float q = gy * gate;
-      float yv = 0.f, gB = 0.f, dd = 0.f, red[W];
+      float yv = 0.f, gB = 0.f, dd = 0.f, red[N / 2], half[2];
+      // A state's terms of dB and dC go through the first step of their sums at once, a pair
+      // of states' through the second: N / 2 values stay of the 2 N. Four states at a time
+      // (the barriers keep the scheduler from holding all of a token's B, C and terms).
 #pragma unroll
       for (int n = 0; n < N; ++n) {
         const float an = __builtin_amdgcn_exp2f(d * a2[n]);
-        const float as = an * hist[i][n], st = fmaf(du, x[n], as);
+        const float as = an * (i ? hist[i - 1][n] : ck[n * 64]), st = fmaf(du, x[n], as);
         const float g = fmaf(q, x[N + n], h[n]);
         yv = fmaf(st, x[N + n], yv);
         gB = fmaf(g, x[n], gB);
@@ -924,8 +992,9 @@ __global__ __launch_bounds__(256, 2) void ssm_bwd_kernel(
         dd = fmaf(ga, a2[n], dd);  // in units of 1 / ln 2
         dA[n] = fmaf(ga, d, dA[n]);
         h[n] = an * g;
-        red[n] = g * du;
-        red[N + n] = q * st;
+        half[n % 2] = swap_add32(g * du, q * st);  // lanes 0-31: dB, 32-63: dC
+        if (n % 2) red[n / 2] = swap_add16(half[0], half[1]);
+        if (n % 4 == 3) __builtin_amdgcn_sched_barrier(0);
       }
       yv = fmaf(Dv, uv, yv);
       const float ddt = fmaf(dd, kLn2, uv * gB) * rcp_fast(1.f + exp_fast(-v));
@@ -933,33 +1002,32 @@ __global__ __launch_bounds__(256, 2) void ssm_bwd_kernel(
       dbias += ddt;
       if (active) {
         const int64_t r = r0 + t;
-        st1(du_o + r * lddu + e, fmaf(Dv, q, d * gB));
-        st1(ddt_o + r * ldddt + e, ddt);
-        if (z) st1(dz_o + r * lddz + e, gy * yv * dgate);
+        st_at(du_o + r * lddu, le, fmaf(Dv, q, d * gB));
+        st_at(ddt_o + r * ldddt, le, ddt);
+        if (z) st_at(dz_o + r * lddz, le, gy * yv * dgate);
       }
-      const float tot = reduce_scatter<W>(red, lane);
-      if (lane % (64 / W) == 0) sRed[(t * nw + wave) * W + lane / (64 / W)] = tot;
+      const float tot = reduce_rows<N / 2>(red, lane);
+      if (lane % (64 / W) == 0) sRed[(i * nw + wave) * W + place] = tot;
+      __builtin_amdgcn_sched_barrier(0);
     }
+    __syncthreads();
+    for (int i = threadIdx.x; i < min(kSub, nt - b * kSub) * W; i += blockDim.x) {
+      const int k = i / W, col = i % W;
+      float acc = 0.f;
+      for (int j = 0; j < nw; ++j) acc += sRed[(k * nw + j) * W + col];
+      const int64_t r = r0 + b * kSub + k;
+      if (bc_part) bc_part[((int64_t)cg * a.rows + r) * W + col] = acc;
+      else if (col < N) st1(dB_o + r * lddB + col, acc);
+      else st1(dC_o + r * lddC + col - N, acc);
+    }
+    __syncthreads();
   }
   if (active) {
 #pragma unroll
-    for (int n = 0; n < N; ++n) po[(int64_t)n * E] = dA[n] * (a2[n] * kLn2);
-    po[(int64_t)N * E] = dD;
-    po[(int64_t)(N + 1) * E] = dbias;
-    if (dstate && tl.j == 0) {
-#pragma unroll
-      for (int n = 0; n < N; ++n) dstate[((int64_t)tl.seq * E + e) * N + n] = h[n];
-    }
-  }
-  __syncthreads();
-  for (int i = threadIdx.x; i < nt * W; i += blockDim.x) {
-    const int t = i / W, col = i % W;
-    float acc = 0.f;
-    for (int k = 0; k < nw; ++k) acc += sRed[(t * nw + k) * W + col];
-    const int64_t r = r0 + t;
-    if (bc_part) bc_part[((int64_t)cg * a.rows + r) * W + col] = acc;
-    else if (col < N) st1(dB_o + r * lddB + col, acc);
-    else st1(dC_o + r * lddC + col - N, acc);
+    for (int n = 0; n < N; ++n) st_at(po + (int64_t)n * E, lf, dA[n] * (a2[n] * kLn2));
+    st_at(po + (int64_t)N * E, lf, dD);
+    st_at(po + (int64_t)(N + 1) * E, lf, dbias);
+    if (dstate && tl.j == 0) st_vec<N>(dstate + (int64_t)tl.seq * E * N, ln, h);
   }
 }
 
@@ -1125,7 +1193,7 @@ hipError_t scan_bwd(const ScanOp& a, const void* dy_, int64_t lddy, const float*
     const int64_t n = (int64_t)a.n_seq * N * a.E;
     ssm_combine_kernel<N><<<dim3((unsigned)((n + 255) / 256)), 256, 0, s>>>(in, cst, ws + p.csum, G, dstate_out);
   }
-  const size_t lds = sizeof(float) * (kBCL * 2 * N * (1 + p.nw) + (size_t)p.nw * (kBCL / kSub - 1) * N * 64);
+  const size_t lds = sizeof(float) * (2 * N * (kBCL + kSub * p.nw) + (size_t)p.nw * (kBCL / kSub) * N * 64);
   hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&ssm_bwd_kernel<T, N>),
                                      hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
   if (e != hipSuccess) return e;
