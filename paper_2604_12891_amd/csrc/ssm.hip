@@ -28,14 +28,14 @@ __device__ __forceinline__ void st1(uint16_t* p, float v) { *p = f32_to_bf16(v);
 // Element of a wave-uniform row at a lane's byte offset, addressed as scalar base
 // plus 32-bit lane offset. Left to itself the compiler adds the lane's part to the matrix's
 // base once and the row's part per access, which costs a 64-bit vector sum and a
-// register pair each (100 registers of the gradient kernel); the empty asm keeps the row's
+// register pair each (100 registers of the gradient kernel); readfirstlane keeps the row's
 // address a scalar value of its own.
 typedef __attribute__((address_space(1))) char gchar;
 template <typename T>
 __device__ __forceinline__ gchar* scalar_row(const T* row) {
-  gchar* p = (gchar*)(row);
-  asm("" : "+s"(p));
-  return p;
+  const uint64_t p = reinterpret_cast<uint64_t>(row);
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)p), hi = __builtin_amdgcn_readfirstlane((uint32_t)(p >> 32));
+  return (gchar*)((uint64_t)hi << 32 | lo);
 }
 // (and the lane's part a 32-bit value at each access)
 __device__ __forceinline__ uint32_t lane_part(uint32_t bytes) {
@@ -704,8 +704,8 @@ __global__ __launch_bounds__(256) void ssm_scan_token_kernel(ScanIn a, const T* 
 // states do: ssm_bwd_local_kernel forms a chunk's (s_loc, sum d) and, in the same
 // forward walk, its adjoint of the start state, sum_t (prod a) C_t q_t;
 // ssm_combine_kernel joins them. Sequences of one chunk skip both.
-constexpr int kBCL = 32;  // tokens per chunk
-constexpr int kSub = 8;   // tokens whose states are held in registers together
+constexpr int kBCL = 30;  // tokens per chunk
+constexpr int kSub = 6;   // tokens whose states are held in registers together
 
 // nt rows of B | C, widened, into LDS by n threads (a multiple of 2N).
 template <typename T, int N>
@@ -845,7 +845,7 @@ __device__ __forceinline__ float reduce_rows(const float* v, int lane) {
 
 // A workgroup takes one chunk of 64 nw channels, a lane per channel. The chunk's
 // start state is walked forward once to leave the state in front of every
-// kSub tokens in LDS; then, from the last kSub tokens to the first, the states
+// kSub tokens (but the first) in LDS; then, from the last kSub tokens to the first, the states
 // in front of each token are formed again into registers and the tokens walked
 // backwards. dB and dC of a token are sums over channels: over a wavefront by
 // swaps and DPP, over the workgroup's wavefronts through LDS, over
@@ -865,7 +865,7 @@ __global__ __launch_bounds__(256, 2) void ssm_bwd_kernel(
   const int nw = blockDim.x >> 6, wave = threadIdx.x >> 6, lane = threadIdx.x & 63, E = a.E;
   float* sBC = smem;                                       // [kBCL][2N]
   float* sRed = smem + kBCL * W;                           // [kSub][nw][2N]
-  float* sCk = sRed + kSub * nw * W + wave * NSUB * N * 64 + lane;  // [NSUB][N][64] per wavefront
+  float* sCk = sRed + kSub * nw * W + wave * (NSUB - 1) * N * 64 + lane;  // [NSUB - 1][N][64] per wavefront
   int w, cg;
   const int CG = (E + blockDim.x - 1) / blockDim.x;
   if (!tile_of_block(a.ntile, CG, w, cg)) return;
@@ -888,14 +888,20 @@ __global__ __launch_bounds__(256, 2) void ssm_bwd_kernel(
 #pragma unroll
   for (int n = 0; n < N; ++n) {
     a2[n] = decay_rate(a2[n]);
-    s[n] = h[n] = dA[n] = 0.f;
+    h[n] = dA[n] = 0.f;
   }
-  if (cst) {  // the state in front of the chunk
+  auto start = [&]() {  // the state in front of the chunk
+    if (cst) {
 #pragma unroll
-    for (int n = 0; n < N; ++n) s[n] = ld_at(cst + ((int64_t)w * N + n) * E, lf);
-  } else if (a.state) {
-    ld_vec<N>(a.state + (int64_t)tl.seq * E * N, ln, s);
-  }
+      for (int n = 0; n < N; ++n) s[n] = ld_at(cst + ((int64_t)w * N + n) * E, lf);
+    } else if (a.state) {
+      ld_vec<N>(a.state + (int64_t)tl.seq * E * N, ln, s);
+    } else {
+#pragma unroll
+      for (int n = 0; n < N; ++n) s[n] = 0.f;
+    }
+  };
+  start();
   if (cst) {
 #pragma unroll
     for (int n = 0; n < N; ++n) h[n] = ld_at(H + ((int64_t)w * N + n) * E, lf);
@@ -907,10 +913,13 @@ __global__ __launch_bounds__(256, 2) void ssm_bwd_kernel(
   __syncthreads();
   const int nsub = (nt + kSub - 1) / kSub;
   const T *us = u + r0 * a.ldu, *ds = dt + r0 * a.lddt, *zs = z ? z + r0 * a.ldz : nullptr, *gs = dy + r0 * lddy;
-  for (int b = 0; b < nsub; ++b) {  // the states in front of every kSub tokens
+  auto park = [&](int b) {  // s in front of the kSub tokens b; the first ones' place is the second ones'
+    float* ck = sCk + max(b - 1, 0) * N * 64;
 #pragma unroll
-    for (int n = 0; n < N; ++n) sCk[(b * N + n) * 64] = s[n];
-    if (b == nsub - 1) break;
+    for (int n = 0; n < N; ++n) ck[n * 64] = s[n];
+  };
+  for (int b = 0; b < nsub - 1; ++b) {
+    if (b > 0) park(b);
     T ru[kSub], rd[kSub];
 #pragma unroll
     for (int i = 0; i < kSub; ++i) {  // all of these tokens exist
@@ -926,6 +935,7 @@ __global__ __launch_bounds__(256, 2) void ssm_bwd_kernel(
       __builtin_amdgcn_sched_barrier(0);
     }
   }
+  if (nsub > 0) park(nsub - 1);
   // what the lane holds of a token's 2N sums: dB or dC by its half, the state's parity by its
   // row, the pair of states within the row
   const int place = lane / 32 * N + lane % 16 / (32 / N) * 2 + lane / 16 % 2;
@@ -939,7 +949,11 @@ __global__ __launch_bounds__(256, 2) void ssm_bwd_kernel(
   };
   if (nt > 0) load(nt - 1);
   for (int b = nsub - 1; b >= 0; --b) {
-    const float* ck = sCk + b * N * 64;
+    if (b == 0 && nsub > 1) {
+      start();
+      park(0);
+    }
+    const float* ck = sCk + max(b - 1, 0) * N * 64;
     float hist[kSub - 1][N];  // the state in front of each token but the first
     {
       T ru[kSub - 1], rd[kSub - 1];
@@ -1193,7 +1207,7 @@ hipError_t scan_bwd(const ScanOp& a, const void* dy_, int64_t lddy, const float*
     const int64_t n = (int64_t)a.n_seq * N * a.E;
     ssm_combine_kernel<N><<<dim3((unsigned)((n + 255) / 256)), 256, 0, s>>>(in, cst, ws + p.csum, G, dstate_out);
   }
-  const size_t lds = sizeof(float) * (2 * N * (kBCL + kSub * p.nw) + (size_t)p.nw * (kBCL / kSub) * N * 64);
+  const size_t lds = sizeof(float) * (2 * N * (kBCL + kSub * p.nw) + (size_t)p.nw * (kBCL / kSub - 1) * N * 64);
   hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&ssm_bwd_kernel<T, N>),
                                      hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
   if (e != hipSuccess) return e;
