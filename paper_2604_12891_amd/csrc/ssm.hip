@@ -575,9 +575,11 @@ __global__ __launch_bounds__(64, 4) void ssm_scan_kernel(ScanIn a, const T* __re
 }
 
 // Every chunk's start state out of the chunks' (s_loc, sum d), in place of
-// s_loc; with G, also the adjoint that reaches every chunk's end out of the
+// s_loc; and (blockIdx.y = 1) the adjoint that reaches every chunk's end out of the
 // chunks' own adjoints of their start, in place of those. One thread per
-// (channel, state, sequence), the chunks in sequence, eight of them loaded together.
+// (channel, state, sequence), the chunks one after the other, kCombine of them loaded together
+// (a trip also waits for the stores of the one before: few long trips).
+constexpr int kCombine = 32;
 template <int N>
 __global__ __launch_bounds__(256) void ssm_combine_kernel(ScanIn a, float* __restrict__ cst,
                                                           const float* __restrict__ csum, float* __restrict__ G,
@@ -591,47 +593,43 @@ __global__ __launch_bounds__(256) void ssm_combine_kernel(ScanIn a, float* __res
   const int nch = max(1, (o1 - o0 + a.CL - 1) / a.CL);
   const int64_t w0 = o0 / a.CL + seq;
   const float a2 = decay_rate(a.A_log[(int64_t)e * N + n]);
-  const int sl = slot_of(a.slots, a.n_slots, (int)seq);
-  float s = a.state && sl >= 0 ? a.state[((int64_t)sl * E + e) * N + n] : 0.f;
-  float* st = cst + (w0 * N + n) * E + e;
+  const bool back = blockIdx.y != 0;
+  float* st = (back ? G : cst) + (w0 * N + n) * E + e;
   const float* sm = csum + w0 * E + e;
   const int64_t step = (int64_t)N * E;
-  constexpr int U = 8;
-  for (int c = 0; c < nch - 1; c += U) {
-    float v[U], d[U];
+  float s = 0.f;
+  if (back) {
+    if (dstate_out) s = dstate_out[(seq * E + e) * N + n];
+  } else {
+    const int sl = slot_of(a.slots, a.n_slots, (int)seq);
+    if (a.state && sl >= 0) s = a.state[((int64_t)sl * E + e) * N + n];
+  }
+  // the chunk that comes last gives its place and takes part in nothing
+  const int dir = back ? -1 : 1;
+  if (back) {
+    st += (nch - 1) * step;
+    sm += (int64_t)(nch - 1) * E;
+  }
+  const int last = nch - 2;  // the last one to take part
+  for (int c = 0; c <= last; c += kCombine) {
+    float v[kCombine], d[kCombine];
 #pragma unroll
-    for (int i = 0; i < U; ++i) {
-      const int k = min(c + i, nch - 2);
+    for (int i = 0; i < kCombine; ++i) {
+      const int k = min(c + i, last) * dir;
       v[i] = st[k * step];
       d[i] = sm[(int64_t)k * E];
     }
 #pragma unroll
-    for (int i = 0; i < U; ++i) {
-      if (c + i >= nch - 1) break;
-      st[(c + i) * step] = s;
-      s = fmaf(__builtin_amdgcn_exp2f(a2 * d[i]), s, v[i]);
+    for (int i = 0; i < kCombine; ++i) {
+      const bool in = c + i <= last;
+      if (in) st[(c + i) * dir * step] = s;
+      const float f = __builtin_amdgcn_exp2f(a2 * d[i]);
+      s = in ? fmaf(f, s, v[i]) : s;
     }
   }
-  st[(nch - 1) * step] = s;
-  if (!G) return;
-  float h = dstate_out ? dstate_out[(seq * E + e) * N + n] : 0.f;
-  float* g = G + (w0 * N + n) * E + e;
-  for (int c = nch - 1; c >= 0; c -= U) {
-    float v[U], d[U];
-#pragma unroll
-    for (int i = 0; i < U; ++i) {
-      const int k = max(c - i, 0);
-      v[i] = g[k * step];
-      d[i] = sm[(int64_t)k * E];
-    }
-#pragma unroll
-    for (int i = 0; i < U; ++i) {
-      if (c - i < 0) break;
-      g[(c - i) * step] = h;
-      h = fmaf(__builtin_amdgcn_exp2f(a2 * d[i]), h, v[i]);
-    }
-  }
+  st[(nch - 1) * dir * step] = s;
 }
+
 
 // ---------------------------------------------------------------- selective scan, single tokens
 // N / 4 lanes per channel hold four states each: a wavefront reads and writes
@@ -1205,7 +1203,7 @@ hipError_t scan_bwd(const ScanOp& a, const void* dy_, int64_t lddy, const float*
     ssm_bwd_local_kernel<T, N><<<dim3(tile_blocks(in.ntile, (a.E + 63) / 64)), 64, 0, s>>>(
         in, u, dt, B, C, z, dy, lddy, cst, ws + p.csum, G);
     const int64_t n = (int64_t)a.n_seq * N * a.E;
-    ssm_combine_kernel<N><<<dim3((unsigned)((n + 255) / 256)), 256, 0, s>>>(in, cst, ws + p.csum, G, dstate_out);
+    ssm_combine_kernel<N><<<dim3((unsigned)((n + 255) / 256), 2), 256, 0, s>>>(in, cst, ws + p.csum, G, dstate_out);
   }
   const size_t lds = sizeof(float) * (2 * N * (kBCL + kSub * p.nw) + (size_t)p.nw * (kBCL / kSub - 1) * N * 64);
   hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&ssm_bwd_kernel<T, N>),
