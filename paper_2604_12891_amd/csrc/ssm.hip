@@ -310,7 +310,7 @@ __global__ __launch_bounds__(256) void ssm_conv_bwd_kernel(
     }
     // rows t0 .. t1 + K - 2; those past the sequence have g = 0
     const int tend = t1 + K - 1;
-    constexpr int U = 4;
+    constexpr int U = 2;
     Pack<T, CH> nx[U], nd[U];
     auto load = [&](int t) {
       if (tl.len == 0) return;
@@ -1073,13 +1073,22 @@ int conv_rows(int rows, int CG) {
     if ((int64_t)rows / R * CG >= (int64_t)kCUs * 8 * 64) return R;
   return 8;
 }
+// Gradients: as many threads as the GPU holds at once (four wavefronts to a SIMD), at most 1,024
+// parts; a thread takes one tile, of as many rows as that leaves it, or several of
+// kConvBwdRows where the sequences alone are more than that.
 constexpr int kConvBwdRows = 32;
-// Partial sums of dw and db: as many threads as fill the GPU, at most 1,024 parts.
-void conv_parts(int n_seq, int rows, int CG, int& parts, int& per) {
-  const int tiles = rows / kConvBwdRows + n_seq;
-  int want = std::max(1, std::min(1024, kCUs * 16 * 64 / CG));
-  per = (tiles + want - 1) / want;
-  parts = (tiles + per - 1) / per;
+struct ConvParts {
+  int R, per, parts;
+};
+ConvParts conv_parts(int n_seq, int rows, int E) {
+  const int CG = (E + 3) / 4, want = std::max(1, std::min(1024, kCUs * 16 * 64 / CG));
+  ConvParts p;
+  p.R = kConvBwdRows;
+  if (want > n_seq) p.R = std::max(p.R, (int)(((int64_t)rows + want - n_seq - 1) / (want - n_seq)));
+  const int tiles = rows / p.R + n_seq;
+  p.per = (tiles + want - 1) / want;
+  p.parts = (tiles + p.per - 1) / p.per;
+  return p;
 }
 
 template <typename T, int K, int CH>
@@ -1096,17 +1105,16 @@ template <typename T, int K, int CH>
 hipError_t conv_bwd(const ConvOp& a, const void* du, int64_t lddu, const void* dstate_out, void* dx, int64_t lddx,
                     float* dw, float* db, void* dstate, float* ws, hipStream_t s) {
   const int CG = a.E / CH;
-  int parts, per;
-  conv_parts(a.n_seq, a.rows, (a.E + 3) / 4, parts, per);
-  const int64_t work = (int64_t)parts * CG;
+  const ConvParts p = conv_parts(a.n_seq, a.rows, a.E);
+  const int64_t work = (int64_t)p.parts * CG;
   ssm_conv_bwd_kernel<T, K, CH><<<dim3((unsigned)((work + 255) / 256)), 256, 0, s>>>(
-      a.offs, a.n_seq, a.rows, a.E, kConvBwdRows, per, parts, static_cast<const T*>(a.x), a.ldx, a.w, a.b,
+      a.offs, a.n_seq, a.rows, a.E, p.R, p.per, p.parts, static_cast<const T*>(a.x), a.ldx, a.w, a.b,
       static_cast<const T*>(a.state), static_cast<const T*>(du), lddu, static_cast<const T*>(dstate_out),
       static_cast<T*>(dx), lddx, static_cast<T*>(dstate), ws);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const int64_t n = (int64_t)(K + 1) * a.E;
-  sum_parts_kernel<<<dim3((unsigned)((n + 63) / 64)), 64 * kSumLanes, 0, s>>>(ws, parts, K, K + 1, a.E, dw, db,
+  sum_parts_kernel<<<dim3((unsigned)((n + 63) / 64)), 64 * kSumLanes, 0, s>>>(ws, p.parts, K, K + 1, a.E, dw, db,
                                                                              nullptr);
   return hipGetLastError();
 }
@@ -1234,7 +1242,7 @@ hipError_t launch_ssm_conv(const ConvOp& a, void* state_out, void* u, int64_t ld
                    aligned16(a.state) && aligned16(state_out);
 #define TCL_CONV(KK)                                                                                       \
   case KK:                                                                                                 \
-    if (a.bf16) return vec ? conv_fwd<uint16_t, KK, 8>(a, state_out, u, ldu, s)                            \
+    if (a.bf16) return vec ? conv_fwd<uint16_t, KK, 4>(a, state_out, u, ldu, s)                            \
                            : conv_fwd<uint16_t, KK, 1>(a, state_out, u, ldu, s);                           \
     return vec ? conv_fwd<float, KK, 4>(a, state_out, u, ldu, s) : conv_fwd<float, KK, 1>(a, state_out, u, ldu, s);
   switch (a.K) {
@@ -1248,9 +1256,7 @@ hipError_t launch_ssm_conv(const ConvOp& a, void* state_out, void* u, int64_t ld
 }
 
 size_t ssm_conv_workspace_bytes(int n_seq, int rows, int E, int K) {
-  int parts, per;
-  conv_parts(n_seq, rows, (E + 3) / 4, parts, per);
-  return (size_t)parts * (K + 1) * E * sizeof(float);
+  return (size_t)conv_parts(n_seq, rows, E).parts * (K + 1) * E * sizeof(float);
 }
 
 hipError_t launch_ssm_conv_bwd(const ConvOp& a, const void* du, int64_t lddu, const void* dstate_out, void* dx,
