@@ -73,19 +73,23 @@ struct Row {
 
 // ---------------------------------------------------------------- order of entries
 // One number per entry that orders as the top list does: by value, NaN after
-// every number, equal values by lower index. 0: no entry.
-__device__ __forceinline__ u64 key_of(float x, int i) {
+// every number, equal values by lower index. The value's bits as an unsigned number that
+// rises with it (16 of them for bf16), from bit 32 up; below 2^b - index, 2^b > the row's
+// entries. 0: no entry.
+template <typename T>
+__device__ __forceinline__ uint32_t ord_of(float x) {
   uint32_t u = __float_as_uint(x + 0.0f);  // -0 as 0
   u = u & 0x80000000u ? ~u : u | 0x80000000u;
   if (!(x == x)) u = 0;
-  return (u64)u << 32 | (uint32_t)~i;
+  return sizeof(T) == 2 ? u >> 16 : u;
 }
-__device__ __forceinline__ int key_index(u64 k) { return (int)~(uint32_t)k; }
-__device__ __forceinline__ float key_value(u64 k) {  // NaN comes back as -inf
-  const uint32_t u = (uint32_t)(k >> 32);
-  if (u == 0) return -INFINITY;
+template <typename T>
+__device__ __forceinline__ float ord_value(uint32_t u) {  // -inf for NaN
+  if (sizeof(T) == 2) u = u << 16 | (u & 0x8000u ? 0 : 0xFFFFu);
+  if (u <= 0x007FFFFFu) return -INFINITY;
   return __uint_as_float(u & 0x80000000u ? u & 0x7FFFFFFFu : ~u);
 }
+__device__ __forceinline__ int index_bits(int cnt) { return 32 - __clz(cnt); }
 
 // ---------------------------------------------------------------- sums of a softmax
 // m = max x, s = sum e, t = sum (x - m) e, e = exp((x - m) / temperature); zc = log2(e) / temperature.
@@ -119,56 +123,75 @@ __device__ __forceinline__ Stats wave_merge(Stats a, float zc) {
 
 // ---------------------------------------------------------------- the K highest
 // Finding the K highest costs one comparison per vector while the row streams by:
-// every thread keeps its own highest entry. Of those kTB keys the K-th highest is a bound
-// tau that at least K entries reach, and an entry that reaches it lies with one of the
-// K threads whose highest does; only their entries are read again (a share K / kTB of
-// the row, out of the caches), the ones >= tau go to a list in LDS, some K to
-// 8 K of them, and each entry of the list counts the ones above it for its rank. A list that
-// overflows (rows made of many near-copies of one stretch) takes the exact K-th
-// key by bisection over its 64 bits instead.
+// every thread keeps its own highest entry, and in LDS the highest value of each of up
+// to kGroups stretches of its entries. Of the kTB keys the K-th highest is a bound tau that
+// at least K entries reach, and an entry that reaches it lies in a stretch, of one of the K threads
+// whose highest does, whose highest value does: some K stretches, read again out of the caches. What
+// is >= tau there goes to a list in LDS, K to some 2 K entries, and each entry of the list
+// counts the ones above it for its rank. A list that overflows (rows made of many
+// near-copies of one stretch) takes the exact K-th key by bisection over its bits instead.
 constexpr int kCap = 1024;
 constexpr int kMaxTop = 64;
+constexpr int kGroups = 16;
 
 struct TopShared {
+  union {
+    u64 cand[kCap];
+    uint16_t high[kGroups][kTB];  // bits 16..31 (of bf16 all) of a stretch's ord_of
+  };
   u64 key[kTB];
-  u64 cand[kCap];
   u64 best[kMaxTop];
-  int sel[kMaxTop];
-  int n, nsel;
+  uint16_t list[kMaxTop * kGroups];  // stretches to read again: group * kTB + thread
+  int n, nlist;
   u64 tau;
 };
 
-// From every thread's highest key (0: none): tau, the threads that reach it.
-__device__ __forceinline__ void top_threads(TopShared& sh, u64 key, int K) {
+// From every thread's highest key (0: none) the bound tau. The first wavefront finds the K-th highest
+// key bit by bit, four keys to a lane, counting by ballot, until exactly K reach the bits so
+// far (comparing every key with every other takes 30 times the instructions). `top` value bits
+// from bit 32 up, and b + 1 bits of the index.
+__device__ __forceinline__ void top_bound(TopShared& sh, u64 key, int K, int top, int b) {
   const int tid = threadIdx.x;
   sh.key[tid] = key;
-  if (tid == 0) {
-    sh.n = 0;
-    sh.nsel = 0;
-    sh.tau = 1;  // fewer than K threads have an entry: all entries
-  }
   if (tid < K) sh.best[tid] = 0;
   __syncthreads();
-  int above = 0;
-#pragma unroll 8
-  for (int i = 0; i < kTB; i += 2) {
-    const ulonglong2 k2 = *reinterpret_cast<const ulonglong2*>(&sh.key[i]);
-    above += (k2.x > key) + (k2.y > key);
-  }
-  if (key && above < K) {
-    sh.sel[above] = tid;
-    atomicAdd(&sh.nsel, 1);
-    if (above == K - 1) sh.tau = key;
+  if (tid < 64) {
+    constexpr int Q = kTB / 64;
+    u64 k[Q];
+    int have = 0;
+#pragma unroll
+    for (int j = 0; j < Q; ++j) {
+      k[j] = sh.key[j * 64 + tid];
+      have += __popcll(__ballot(k[j] != 0));
+    }
+    u64 lo = 1;  // fewer than K threads have an entry: all entries
+    if (have > K) {
+      lo = 0;
+      for (int bit = 31 + top; bit >= 0; --bit) {
+        if (bit == 31) bit = b;
+        const u64 trial = lo | 1ull << bit;
+        int c = 0;
+#pragma unroll
+        for (int j = 0; j < Q; ++j) c += __popcll(__ballot(k[j] >= trial));
+        if (c >= K) lo = trial;
+        if (c == K) break;
+      }
+    }
+    if (tid == 0) {
+      sh.n = 0;
+      sh.nlist = 0;
+      sh.tau = lo;
+    }
   }
   __syncthreads();
 }
 
 // The K highest of the keys that each(f) hands to f on all threads together, into
-// sh.best, highest first. All of them reach sh.tau's entries; sh.n starts at 0.
+// sh.best, highest first; at least K reach sh.tau (or all that there are). sh.n starts at 0.
 template <typename Each>
 __device__ __forceinline__ void top_collect(TopShared& sh, int K, Each each) {
   const int tid = threadIdx.x;
-  u64 tau = sh.tau;
+  const u64 tau = sh.tau;
   each([&](u64 k) {
     if (k >= tau) {
       const int p = atomicAdd(&sh.n, 1);
@@ -235,8 +258,8 @@ __device__ __forceinline__ void finish_row(const LogitRows& a, const Row<T>& row
   if ((int)threadIdx.x < K) {
     const u64 k = sh.best[threadIdx.x];
     const int64_t j = (int64_t)r * K + threadIdx.x;
-    o.top[j] = k ? key_index(k) + row.first : -1;
-    if (o.top_logp) o.top_logp[j] = k ? logp(key_value(k)) : -INFINITY;
+    o.top[j] = k ? (int)((1u << index_bits(row.cnt)) - (uint32_t)k) + row.first : -1;
+    if (o.top_logp) o.top_logp[j] = k ? logp(ord_value<T>((uint32_t)(k >> 32))) : -INFINITY;
   }
 }
 
@@ -259,12 +282,18 @@ __global__ __launch_bounds__(kTB) void logprobs_kernel(LogitRows a, int K, Logpr
   Stats st = {-INFINITY, 0.f, 0.f};
   float best = -INFINITY;
   int bv = -1;
+  u32x4 bx = {0, 0, 0, 0};  // the vector that holds it
   constexpr int U = 4;
-  for (int vb = v0 + tid; vb < v1; vb += U * kTB) {
+  // trips of U vectors to a stretch
+  const int trips = (v1 - v0 + U * kTB - 1) / (U * kTB), span = (trips + kGroups - 1) / kGroups;
+  float high = -INFINITY;
+  int trip = 0;
+  for (int vb = v0 + tid; vb < v1; vb += U * kTB, ++trip) {
     u32x4 x[U];
 #pragma unroll
     for (int k = 0; k < U; ++k)
       if (vb + k * kTB < v1) x[k] = row.load(vb + k * kTB);
+    if (trip % span == 0) high = -INFINITY;
 #pragma unroll
     for (int k = 0; k < U; ++k) {
       if (vb + k * kTB >= v1) break;
@@ -274,9 +303,11 @@ __global__ __launch_bounds__(kTB) void logprobs_kernel(LogitRows a, int K, Logpr
         f[i] = Row<T>::get(x[k], i);
         vm = fmaxf(vm, f[i]);
       }
+      high = fmaxf(high, vm);
       if (vm > best) {
         best = vm;
         bv = vb + k * kTB;
+        bx = x[k];
         // the sums move to the new maximum
         if (st.m > -INFINITY) {
           const float d = st.m - vm, g = __builtin_amdgcn_exp2f(d * zc);
@@ -295,6 +326,7 @@ __global__ __launch_bounds__(kTB) void logprobs_kernel(LogitRows a, int K, Logpr
         }
       }
     }
+    if (K > 0) sh.high[trip / span][tid] = (uint16_t)(ord_of<T>(high) >> (8 * sizeof(T) - 16));
   }
   st = wave_merge(st, zc);
   if ((tid & 63) == 0) part[tid >> 6] = st;
@@ -304,27 +336,40 @@ __global__ __launch_bounds__(kTB) void logprobs_kernel(LogitRows a, int K, Logpr
   for (int k = 1; k < kTB / 64; ++k) st = merge(st, part[k], zc);
 
   if (K > 0) {
-    auto vec_keys = [&](int v, auto f) {
-      const u32x4 x = row.load(v);
+    const int b = index_bits(row.cnt);
+    auto vec_keys = [&](int v, u32x4 y, auto f) {
 #pragma unroll
       for (int i = 0; i < VE; ++i) {
         const int j = v * VE - row.h + i;
-        if (j >= 0 && j < row.cnt) f(key_of(Row<T>::get(x, i), j));
+        if (j >= 0 && j < row.cnt) f((u64)ord_of<T>(Row<T>::get(y, i)) << 32 | ((1u << b) - (uint32_t)j));
       }
     };
     u64 key = 0;
     if (bv >= 0) {
-      vec_keys(bv, [&](u64 k) { key = max(key, k); });
+      vec_keys(bv, bx, [&](u64 k) { key = max(key, k); });
     } else {  // nothing above -inf: the order among -inf and NaN
-      for (int v = v0 + tid; v < v1; v += kTB) vec_keys(v, [&](u64 k) { key = max(key, k); });
+      for (int v = v0 + tid; v < v1; v += kTB) vec_keys(v, row.load(v), [&](u64 k) { key = max(key, k); });
     }
-    top_threads(sh, key, K);
-    // the vectors of the threads that reach tau, shared out over all threads
-    const int each_n = (v1 - v0 + kTB - 1) / kTB, units = sh.nsel * each_n;
+    top_bound(sh, key, K, 8 * sizeof(T), b);
+    const uint32_t need = (uint32_t)(sh.tau >> 32);
+    if (key && key >= sh.tau) {
+      const int mine = v0 + tid < v1 ? ((v1 - v0 - tid - 1) / (U * kTB)) / span + 1 : 0;
+      for (int g = 0; g < mine; ++g)
+        if (sh.high[g][tid] >= need >> (8 * sizeof(T) - 16)) sh.list[atomicAdd(&sh.nlist, 1)] = (uint16_t)(g * kTB + tid);
+    }
+    __syncthreads();
+    // the vectors of those stretches, shared out over all threads
+    const int each_n = U * span, units = sh.nlist * each_n;
+    const float floor = ord_value<T>(need);
     top_collect(sh, K, [&](auto f) {
       for (int q = tid; q < units; q += kTB) {
-        const int v = v0 + sh.sel[q / each_n] + q % each_n * kTB;
-        if (v < v1) vec_keys(v, f);
+        const int l = sh.list[q / each_n], v = v0 + l % kTB + (l / kTB * each_n + q % each_n) * kTB;
+        if (v >= v1) continue;
+        const u32x4 y = row.load(v);
+        float vm = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < VE; ++i) vm = fmaxf(vm, Row<T>::get(y, i));
+        if (vm >= floor) vec_keys(v, y, f);
       }
     });
   }
@@ -365,7 +410,7 @@ __global__ __launch_bounds__(kTB) void logprobs_join_kernel(LogitRows a, int K, 
     };
     u64 key = 0;
     each([&](u64 k) { key = max(key, k); });
-    top_threads(sh, key, K);
+    top_bound(sh, key, K, 8 * sizeof(T), index_bits(row.cnt));
     top_collect(sh, K, each);
   }
   finish_row(a, row, r, st, sh, K, o);
