@@ -124,39 +124,56 @@ __device__ __forceinline__ Stats wave_merge(Stats a, float zc) {
 // ---------------------------------------------------------------- the K highest
 // Finding the K highest costs one comparison per vector while the row streams by:
 // every thread keeps its own highest entry, and in LDS the highest value of each of up
-// to kGroups stretches of its entries. Of the kTB keys the K-th highest is a bound tau that
+// to kGroups stretches of its entries. Of the threads' keys the K-th highest is a bound tau that
 // at least K entries reach, and an entry that reaches it lies in a stretch, of one of the K threads
 // whose highest does, whose highest value does: some K stretches, read again out of the caches. What
 // is >= tau there goes to a list in LDS, K to some 2 K entries, and each entry of the list
 // counts the ones above it for its rank. A list that overflows (rows made of many
 // near-copies of one stretch) takes the exact K-th key by bisection over its bits instead.
-constexpr int kCap = 1024;
 constexpr int kMaxTop = 64;
 constexpr int kGroups = 16;
 
+template <int TB>
 struct TopShared {
+  static constexpr int kCap = 4 * TB;
   union {
     u64 cand[kCap];
-    uint16_t high[kGroups][kTB];  // bits 16..31 (of bf16 all) of a stretch's ord_of
+    uint16_t high[kGroups][TB];  // bits 16..31 (of bf16 all) of a stretch's ord_of
   };
-  u64 key[kTB];
+  u64 key[TB];
   u64 best[kMaxTop];
-  uint16_t list[kMaxTop * kGroups];  // stretches to read again: group * kTB + thread
+  uint16_t list[kMaxTop * kGroups];  // stretches to read again: group * TB + thread
   int n, nlist;
   u64 tau;
 };
 
-// From every thread's highest key (0: none) the bound tau. The first wavefront finds the K-th highest
-// key bit by bit, four keys to a lane, counting by ballot, until exactly K reach the bits so
-// far (comparing every key with every other takes 30 times the instructions). `top` value bits
-// from bit 32 up, and b + 1 bits of the index.
-__device__ __forceinline__ void top_bound(TopShared& sh, u64 key, int K, int top, int b) {
+// On one wavefront: the K-th highest of n > K distinct keys (Q to a lane, 0: none), or a bound that exactly K
+// reach, bit by bit, counting by ballot (comparing every key with every other takes 30 times the
+// instructions at 256 keys). Value bits 32 .. top + 31, index bits 0 .. b.
+template <int Q>
+__device__ __forceinline__ u64 kth_key(const u64* k, int K, int top, int b) {
+  u64 lo = 0;
+  for (int bit = 31 + top; bit >= 0; --bit) {
+    if (bit == 31) bit = b;
+    const u64 trial = lo | 1ull << bit;
+    int c = 0;
+#pragma unroll
+    for (int j = 0; j < Q; ++j) c += __popcll(__ballot(k[j] >= trial));
+    if (c >= K) lo = trial;
+    if (c == K) break;
+  }
+  return lo;
+}
+
+// From every thread's highest key (0: none) the bound tau.
+template <int TB>
+__device__ __forceinline__ void top_bound(TopShared<TB>& sh, u64 key, int K, int top, int b) {
   const int tid = threadIdx.x;
   sh.key[tid] = key;
-  if (tid < K) sh.best[tid] = 0;
+  for (int i = tid; i < K; i += TB) sh.best[i] = 0;
   __syncthreads();
   if (tid < 64) {
-    constexpr int Q = kTB / 64;
+    constexpr int Q = TB / 64;
     u64 k[Q];
     int have = 0;
 #pragma unroll
@@ -164,23 +181,11 @@ __device__ __forceinline__ void top_bound(TopShared& sh, u64 key, int K, int top
       k[j] = sh.key[j * 64 + tid];
       have += __popcll(__ballot(k[j] != 0));
     }
-    u64 lo = 1;  // fewer than K threads have an entry: all entries
-    if (have > K) {
-      lo = 0;
-      for (int bit = 31 + top; bit >= 0; --bit) {
-        if (bit == 31) bit = b;
-        const u64 trial = lo | 1ull << bit;
-        int c = 0;
-#pragma unroll
-        for (int j = 0; j < Q; ++j) c += __popcll(__ballot(k[j] >= trial));
-        if (c >= K) lo = trial;
-        if (c == K) break;
-      }
-    }
+    const u64 tau = have > K ? kth_key<Q>(k, K, top, b) : 1;  // too few: all entries
     if (tid == 0) {
       sh.n = 0;
       sh.nlist = 0;
-      sh.tau = lo;
+      sh.tau = tau;
     }
   }
   __syncthreads();
@@ -188,21 +193,25 @@ __device__ __forceinline__ void top_bound(TopShared& sh, u64 key, int K, int top
 
 // The K highest of the keys that each(f) hands to f on all threads together, into
 // sh.best, highest first; at least K reach sh.tau (or all that there are). sh.n starts at 0.
-template <typename Each>
-__device__ __forceinline__ void top_collect(TopShared& sh, int K, Each each) {
+template <int TB, typename Each>
+__device__ __forceinline__ void top_collect(TopShared<TB>& sh, int K, int top, int b, Each each) {
+  constexpr int kCap = TopShared<TB>::kCap;
   const int tid = threadIdx.x;
-  const u64 tau = sh.tau;
-  each([&](u64 k) {
-    if (k >= tau) {
-      const int p = atomicAdd(&sh.n, 1);
-      if (p < kCap) sh.cand[p] = k;
-    }
-  });
-  __syncthreads();
+  auto gather = [&](u64 tau) {
+    each([&](u64 k) {
+      if (k >= tau) {
+        const int p = atomicAdd(&sh.n, 1);
+        if (p < kCap) sh.cand[p] = k;
+      }
+    });
+    __syncthreads();
+  };
+  gather(sh.tau);
   int n = sh.n;
   if (n > kCap) {
     u64 lo = 0;  // at least K keys reach lo
-    for (int bit = 63; bit >= 0; --bit) {
+    for (int bit = 31 + top; bit >= 0; --bit) {
+      if (bit == 31) bit = b;
       const u64 trial = lo | 1ull << bit;
       int c = 0;
       each([&](u64 k) { c += k >= trial; });
@@ -216,16 +225,30 @@ __device__ __forceinline__ void top_collect(TopShared& sh, int K, Each each) {
     __syncthreads();
     if (tid == 0) sh.n = 0;
     __syncthreads();
-    each([&](u64 k) {
-      if (k >= lo) {
-        const int p = atomicAdd(&sh.n, 1);
-        if (p < kCap) sh.cand[p] = k;
-      }
-    });
-    __syncthreads();
+    gather(lo);
     n = min(sh.n, kCap);
   }
-  for (int i = tid; i < n; i += kTB) {
+  if (n > K + K / 2 + 8) {
+    // only the K highest of the list are ranked
+    if (tid < 64) {
+      constexpr int Q = kCap / 64;
+      u64 k[Q];
+#pragma unroll
+      for (int j = 0; j < Q; ++j) k[j] = j * 64 + tid < n ? sh.cand[j * 64 + tid] : 0;
+      const u64 lo = kth_key<Q>(k, K, top, b);
+      int at = 0;
+#pragma unroll
+      for (int j = 0; j < Q; ++j) {
+        const bool in = k[j] >= lo && k[j] != 0;
+        const u64 m = __ballot(in);
+        if (in) sh.cand[at + __popcll(m & ((1ull << tid) - 1))] = k[j];
+        at += __popcll(m);
+      }
+    }
+    n = K;
+    __syncthreads();
+  }
+  for (int i = tid; i < n; i += TB) {
     const u64 k = sh.cand[i];
     int above = 0;
     for (int j = 0; j < n; ++j) above += sh.cand[j] > k;
@@ -242,9 +265,9 @@ struct LogprobOut {
   float* top_logp;
 };
 
-template <typename T>
-__device__ __forceinline__ void finish_row(const LogitRows& a, const Row<T>& row, int r, Stats st, const TopShared& sh,
-                                           int K, const LogprobOut& o) {
+template <typename T, int TB>
+__device__ __forceinline__ void finish_row(const LogitRows& a, const Row<T>& row, int r, Stats st,
+                                           const TopShared<TB>& sh, int K, const LogprobOut& o) {
   const float ls = logf(st.s);  // -inf for a row with nothing left
   const bool none = !(st.m > -INFINITY);
   auto logp = [&](float x) { return none || !(x > -INFINITY) ? -INFINITY : fmaf(x - st.m, a.inv_temp, -ls); };
@@ -255,9 +278,9 @@ __device__ __forceinline__ void finish_row(const LogitRows& a, const Row<T>& row
     }
     if (o.entropy) o.entropy[r] = none ? 0.f : fmaf(-a.inv_temp, st.t / st.s, ls);
   }
-  if ((int)threadIdx.x < K) {
-    const u64 k = sh.best[threadIdx.x];
-    const int64_t j = (int64_t)r * K + threadIdx.x;
+  for (int i = threadIdx.x; i < K; i += TB) {
+    const u64 k = sh.best[i];
+    const int64_t j = (int64_t)r * K + i;
     o.top[j] = k ? (int)((1u << index_bits(row.cnt)) - (uint32_t)k) + row.first : -1;
     if (o.top_logp) o.top_logp[j] = k ? logp(ord_value<T>((uint32_t)(k >> 32))) : -INFINITY;
   }
@@ -269,11 +292,11 @@ __device__ __forceinline__ int64_t split_stride(int K) { return (int64_t)K * 8 +
 // One pass over a row (or the part of it that blockIdx.y names): running maximum with
 // the sums rescaled when it rises, once per vector at most. Bound by HBM from a
 // few thousand entries on. gridDim.y == 1: the row's results leave from here.
-template <typename T>
-__global__ __launch_bounds__(kTB) void logprobs_kernel(LogitRows a, int K, LogprobOut o, char* __restrict__ ws) {
+template <typename T, int TB>
+__global__ __launch_bounds__(TB) void logprobs_kernel(LogitRows a, int K, LogprobOut o, char* __restrict__ ws) {
   constexpr int VE = Row<T>::VE;
-  __shared__ __attribute__((aligned(16))) TopShared sh;
-  __shared__ Stats part[kTB / 64];
+  __shared__ __attribute__((aligned(16))) TopShared<TB> sh;
+  __shared__ Stats part[TB / 64];
   const int r = blockIdx.x, tid = threadIdx.x;
   const Row<T> row(a, r);
   const int per = (row.nvec + gridDim.y - 1) / gridDim.y;
@@ -285,18 +308,18 @@ __global__ __launch_bounds__(kTB) void logprobs_kernel(LogitRows a, int K, Logpr
   u32x4 bx = {0, 0, 0, 0};  // the vector that holds it
   constexpr int U = 4;
   // trips of U vectors to a stretch
-  const int trips = (v1 - v0 + U * kTB - 1) / (U * kTB), span = (trips + kGroups - 1) / kGroups;
+  const int trips = (v1 - v0 + U * TB - 1) / (U * TB), span = (trips + kGroups - 1) / kGroups;
   float high = -INFINITY;
   int trip = 0;
-  for (int vb = v0 + tid; vb < v1; vb += U * kTB, ++trip) {
+  for (int vb = v0 + tid; vb < v1; vb += U * TB, ++trip) {
     u32x4 x[U];
 #pragma unroll
     for (int k = 0; k < U; ++k)
-      if (vb + k * kTB < v1) x[k] = row.load(vb + k * kTB);
+      if (vb + k * TB < v1) x[k] = row.load(vb + k * TB);
     if (trip % span == 0) high = -INFINITY;
 #pragma unroll
     for (int k = 0; k < U; ++k) {
-      if (vb + k * kTB >= v1) break;
+      if (vb + k * TB >= v1) break;
       float f[VE], vm = -INFINITY;
 #pragma unroll
       for (int i = 0; i < VE; ++i) {
@@ -306,7 +329,7 @@ __global__ __launch_bounds__(kTB) void logprobs_kernel(LogitRows a, int K, Logpr
       high = fmaxf(high, vm);
       if (vm > best) {
         best = vm;
-        bv = vb + k * kTB;
+        bv = vb + k * TB;
         bx = x[k];
         // the sums move to the new maximum
         if (st.m > -INFINITY) {
@@ -333,7 +356,7 @@ __global__ __launch_bounds__(kTB) void logprobs_kernel(LogitRows a, int K, Logpr
   __syncthreads();
   st = part[0];
 #pragma unroll
-  for (int k = 1; k < kTB / 64; ++k) st = merge(st, part[k], zc);
+  for (int k = 1; k < TB / 64; ++k) st = merge(st, part[k], zc);
 
   if (K > 0) {
     const int b = index_bits(row.cnt);
@@ -348,22 +371,22 @@ __global__ __launch_bounds__(kTB) void logprobs_kernel(LogitRows a, int K, Logpr
     if (bv >= 0) {
       vec_keys(bv, bx, [&](u64 k) { key = max(key, k); });
     } else {  // nothing above -inf: the order among -inf and NaN
-      for (int v = v0 + tid; v < v1; v += kTB) vec_keys(v, row.load(v), [&](u64 k) { key = max(key, k); });
+      for (int v = v0 + tid; v < v1; v += TB) vec_keys(v, row.load(v), [&](u64 k) { key = max(key, k); });
     }
     top_bound(sh, key, K, 8 * sizeof(T), b);
     const uint32_t need = (uint32_t)(sh.tau >> 32);
     if (key && key >= sh.tau) {
-      const int mine = v0 + tid < v1 ? ((v1 - v0 - tid - 1) / (U * kTB)) / span + 1 : 0;
+      const int mine = v0 + tid < v1 ? ((v1 - v0 - tid - 1) / (U * TB)) / span + 1 : 0;
       for (int g = 0; g < mine; ++g)
-        if (sh.high[g][tid] >= need >> (8 * sizeof(T) - 16)) sh.list[atomicAdd(&sh.nlist, 1)] = (uint16_t)(g * kTB + tid);
+        if (sh.high[g][tid] >= need >> (8 * sizeof(T) - 16)) sh.list[atomicAdd(&sh.nlist, 1)] = (uint16_t)(g * TB + tid);
     }
     __syncthreads();
     // the vectors of those stretches, shared out over all threads
     const int each_n = U * span, units = sh.nlist * each_n;
     const float floor = ord_value<T>(need);
-    top_collect(sh, K, [&](auto f) {
-      for (int q = tid; q < units; q += kTB) {
-        const int l = sh.list[q / each_n], v = v0 + l % kTB + (l / kTB * each_n + q % each_n) * kTB;
+    top_collect(sh, K, 8 * sizeof(T), b, [&](auto f) {
+      for (int q = tid; q < units; q += TB) {
+        const int l = sh.list[q / each_n], v = v0 + l % TB + (l / TB * each_n + q % each_n) * TB;
         if (v >= v1) continue;
         const u32x4 y = row.load(v);
         float vm = -INFINITY;
@@ -378,7 +401,7 @@ __global__ __launch_bounds__(kTB) void logprobs_kernel(LogitRows a, int K, Logpr
     return;
   }
   char* w = ws + ((int64_t)r * gridDim.y + blockIdx.y) * split_stride(K);
-  if (tid < K) reinterpret_cast<u64*>(w)[tid] = sh.best[tid];
+  for (int i = tid; i < K; i += TB) reinterpret_cast<u64*>(w)[i] = sh.best[i];
   if (tid == 0) *reinterpret_cast<Stats*>(w + (int64_t)K * 8) = st;
 }
 
@@ -386,7 +409,7 @@ __global__ __launch_bounds__(kTB) void logprobs_kernel(LogitRows a, int K, Logpr
 template <typename T>
 __global__ __launch_bounds__(kTB) void logprobs_join_kernel(LogitRows a, int K, int splits, LogprobOut o,
                                                             const char* __restrict__ ws) {
-  __shared__ __attribute__((aligned(16))) TopShared sh;
+  __shared__ __attribute__((aligned(16))) TopShared<kTB> sh;
   __shared__ Stats part[kTB / 64];
   const int r = blockIdx.x, tid = threadIdx.x;
   const Row<T> row(a, r);
@@ -410,8 +433,9 @@ __global__ __launch_bounds__(kTB) void logprobs_join_kernel(LogitRows a, int K, 
     };
     u64 key = 0;
     each([&](u64 k) { key = max(key, k); });
-    top_bound(sh, key, K, 8 * sizeof(T), index_bits(row.cnt));
-    top_collect(sh, K, each);
+    const int b = index_bits(row.cnt);
+    top_bound(sh, key, K, 8 * sizeof(T), b);
+    top_collect(sh, K, 8 * sizeof(T), b, each);
   }
   finish_row(a, row, r, st, sh, K, o);
 }
@@ -712,7 +736,11 @@ int row_splits(int n, int V) {
 template <typename T>
 hipError_t logprobs(const LogitRows& a, int K, const LogprobOut& o, char* ws, hipStream_t s) {
   const int S = row_splits(a.n, a.V);
-  logprobs_kernel<T><<<dim3(a.n, S), kTB, 0, s>>>(a, K, o, ws);
+  // Many short rows: one wavefront each, or two for more top entries than half its lanes. 65,536 bf16 rows of
+  // 2,048, K 20: 137 us, with kTB threads 308; 8,192 of 16,384 72 with one wavefront, 76 with kTB.
+  if (S == 1 && a.n >= 256 && a.V <= 8192 && K <= 32) logprobs_kernel<T, 64><<<dim3(a.n), 64, 0, s>>>(a, K, o, ws);
+  else if (S == 1 && a.n >= 256 && a.V <= 8192) logprobs_kernel<T, 128><<<dim3(a.n), 128, 0, s>>>(a, K, o, ws);
+  else logprobs_kernel<T, kTB><<<dim3(a.n, S), kTB, 0, s>>>(a, K, o, ws);
   if (S > 1) logprobs_join_kernel<T><<<dim3(a.n), kTB, 0, s>>>(a, K, S, o, ws);
   return hipGetLastError();
 }
