@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import Optional
 
 import numpy as np
@@ -70,6 +71,12 @@ class SsmScanGrads(ctypes.Structure):
                 ("d_db_dt", ctypes.c_void_p), ("d_dstate", ctypes.c_void_p)]
 
 
+# The same layouts as bytes: packing them takes a fraction of a ctypes structure's time, which
+# a single token's call would notice.
+_PACK_CONV = struct.Struct("@5iPPqPPP")
+_PACK_SCAN = struct.Struct("@6iPPqPqPqPqPqPPPP")
+_PACK_GRADS = struct.Struct("@PqPqPqPqPqPPPP")
+
 _vp, _i32, _sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_size_t
 _i64, _f32 = ctypes.c_int64, ctypes.c_float
 _SIGS = {
@@ -111,14 +118,14 @@ _SIGS = {
     "tcl_rdu_workspace_bytes": (_sz, [_i32, _i32]),
     "tcl_rdu_select": (_i32, [_i32, _vp, _vp, _i32, _vp, _i32, _i32, _vp, _vp, _vp, _sz, _vp]),
     "tcl_lambdarank": (_i32, [_i32, _vp, _vp, ctypes.c_float, _vp, _vp, _vp, _sz, _vp]),
-    "tcl_ssm_conv": (_i32, [ctypes.POINTER(SsmConvArgs), _vp, _i32, _vp, _vp, _i64, _vp]),
+    "tcl_ssm_conv": (_i32, [_vp, _vp, _i32, _vp, _vp, _i64, _vp]),
     "tcl_ssm_conv_workspace_bytes": (_sz, [_i32] * 4),
-    "tcl_ssm_conv_backward": (_i32, [ctypes.POINTER(SsmConvArgs), _vp, _i64, _vp, _vp, _i64, _vp, _vp, _vp, _vp, _sz,
+    "tcl_ssm_conv_backward": (_i32, [_vp, _vp, _i64, _vp, _vp, _i64, _vp, _vp, _vp, _vp, _sz,
                                      _vp]),
     "tcl_ssm_scan_workspace_bytes": (_sz, [_i32] * 5),
-    "tcl_ssm_scan": (_i32, [ctypes.POINTER(SsmScanArgs), _vp, _i32, _vp, _vp, _i64, _vp, _sz, _vp]),
+    "tcl_ssm_scan": (_i32, [_vp, _vp, _i32, _vp, _vp, _i64, _vp, _sz, _vp]),
     "tcl_ssm_scan_backward_workspace_bytes": (_sz, [_i32] * 5),
-    "tcl_ssm_scan_backward": (_i32, [ctypes.POINTER(SsmScanArgs), _vp, _i64, _vp, ctypes.POINTER(SsmScanGrads), _vp,
+    "tcl_ssm_scan_backward": (_i32, [_vp, _vp, _i64, _vp, _vp, _vp,
                                      _sz, _vp]),
     "tcl_logits_workspace_bytes": (_sz, [_i32] * 3),
     "tcl_logprobs": (_i32, [_i32, _i32, _i32, _vp, _i64, _vp, _f32, _vp, _i32, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
@@ -510,26 +517,34 @@ def _expect(name, t, dtype, shape, like, rows=False):
     or (rows) with unit stride within its rows."""
     if t is None:
         return
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape):
+    if t.dtype is not dtype or t.shape != shape:
         raise ValueError(f"{name}: {dtype} {tuple(shape)} expected, not {t.dtype} {tuple(t.shape)}")
-    if t.device != like.device:
+    if t.get_device() != like.get_device():
         raise ValueError(f"{name} is on {t.device}, not on {like.device}")
-    if rows:
-        ok = t.numel() == 0 or ((shape[1] == 1 or t.stride(1) == 1) and (shape[0] == 1 or t.stride(0) >= shape[1]))
-    else:
-        ok = t.is_contiguous()
-    if not ok:
+    if t.is_contiguous():
+        return
+    if not rows or (shape[1] != 1 and t.stride(1) != 1) or (shape[0] != 1 and t.stride(0) < shape[1]):
         raise ValueError(f"{name}: {'rows' if rows else 'tensor'} not contiguous (strides {t.stride()})")
 
 
 def _ld(t) -> int:
     """Leading dimension of a matrix of rows (one row, or none, has any)."""
-    return max(t.stride(0), t.shape[1]) if t.shape[0] > 1 else t.shape[1]
+    return t.shape[1] if t.is_contiguous() else t.stride(0)
+
+
+def _adr(t) -> int:
+    return 0 if t is None else t.data_ptr()
+
+
+def _stream_of(stream, t) -> int:
+    """The caller's stream, or the current one of t's device (the current device)."""
+    import torch
+    return (torch.cuda.current_stream(t.get_device()) if stream is None else stream).cuda_stream
 
 
 def _on_device(t):
     import torch
-    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
         raise ValueError(f"tensors on {t.device}, which is not the current device")
 
 
@@ -583,8 +598,8 @@ def _conv_args(x, w, b, offs, n_seq, state):
     _expect("x", x, x.dtype, (rows, E), x, rows=True)
     _expect("w", w, torch.float32, (E, w.shape[1]), x)
     _expect("b", b, torch.float32, (E,), x)
-    return SsmConvArgs(_dtype(x), n_seq, rows, E, w.shape[1], _ptr(offs), x.data_ptr(), _ld(x), w.data_ptr(), _ptr(b),
-                       _ptr(state))
+    return _PACK_CONV.pack(_dtype(x), n_seq, rows, E, w.shape[1], _adr(offs), x.data_ptr(), _ld(x), w.data_ptr(),
+                           _adr(b), _adr(state))
 
 
 def ssm_conv(x, w, b=None, offs=None, state=None, state_out=None, slots=None, out=None, stream=None):
@@ -601,8 +616,8 @@ def ssm_conv(x, w, b=None, offs=None, state=None, state_out=None, slots=None, ou
     else:
         _expect("out", out, x.dtype, x.shape, x, rows=True)
     a = _conv_args(x, w, b, offs, n_seq, state)
-    check(lib().tcl_ssm_conv(ctypes.byref(a), _ptr(slots), n_slots, _ptr(state_out), out.data_ptr(), _ld(out),
-                             _stream(stream)))
+    check(lib().tcl_ssm_conv(a, _ptr(slots), n_slots, _ptr(state_out), out.data_ptr(), _ld(out),
+                             _stream_of(stream, x)))
     return out
 
 
@@ -627,13 +642,14 @@ def ssm_conv_backward(x, w, b, du, offs=None, state=None, state_grad=None, works
              db=torch.empty(x.shape[1], dtype=torch.float32, device=x.device),
              dstate=None if state is None else torch.empty_like(state))
     ws = _workspace(lib().tcl_ssm_conv_workspace_bytes(n_seq, x.shape[0], x.shape[1], K), workspace, x)
-    check(lib().tcl_ssm_conv_backward(ctypes.byref(a), du.data_ptr(), _ld(du), _ptr(state_grad), r["dx"].data_ptr(),
+    check(lib().tcl_ssm_conv_backward(a, du.data_ptr(), _ld(du), _ptr(state_grad), r["dx"].data_ptr(),
                                       _ld(r["dx"]), r["dw"].data_ptr(), r["db"].data_ptr(), _ptr(r["dstate"]),
-                                      *_ws_args(ws), _stream(stream)))
+                                      *_ws_args(ws), _stream_of(stream, x)))
     return r
 
 
 def _scan_args(u, dt, A_log, B, C, D, z, b_dt, offs, n_seq, L, state):
+    """(L, the packed tcl_ssm_scan_args)"""
     import torch
     rows, E = u.shape
     if A_log.dim() != 2:
@@ -646,9 +662,9 @@ def _scan_args(u, dt, A_log, B, C, D, z, b_dt, offs, n_seq, L, state):
     _expect("b_dt", b_dt, torch.float32, (E,), u)
     if L is None:
         L = max(rows, 1) if offs is not None else 1
-    return SsmScanArgs(_dtype(u), n_seq, rows, E, N, L, _ptr(offs), u.data_ptr(), _ld(u), dt.data_ptr(), _ld(dt),
-                       B.data_ptr(), _ld(B), C.data_ptr(), _ld(C), _ptr(z), 0 if z is None else _ld(z),
-                       A_log.data_ptr(), _ptr(D), _ptr(b_dt), _ptr(state))
+    return L, _PACK_SCAN.pack(_dtype(u), n_seq, rows, E, N, L, _adr(offs), u.data_ptr(), _ld(u), dt.data_ptr(), _ld(dt),
+                              B.data_ptr(), _ld(B), C.data_ptr(), _ld(C), _adr(z), 0 if z is None else _ld(z),
+                              A_log.data_ptr(), _adr(D), _adr(b_dt), _adr(state))
 
 
 def ssm_scan_workspace(n_seq, rows, E, N, L, backward=False):
@@ -668,15 +684,15 @@ def ssm_scan(u, dt, A_log, B, C, D=None, z=None, b_dt=None, offs=None, L=None, s
     import torch
     n_seq = _sequences(u, offs)
     n_slots = _pools(state, state_out, slots, n_seq, A_log.shape, torch.float32, u)
-    a = _scan_args(u, dt, A_log, B, C, D, z, b_dt, offs, n_seq, L, state)
+    L, a = _scan_args(u, dt, A_log, B, C, D, z, b_dt, offs, n_seq, L, state)
     if out is None:
         out = torch.empty(u.shape, dtype=u.dtype, device=u.device)
     else:
         _expect("out", out, u.dtype, u.shape, u, rows=True)
-    need = 0 if offs is None else lib().tcl_ssm_scan_workspace_bytes(n_seq, a.rows, a.E, a.N, a.L)
+    need = 0 if offs is None else lib().tcl_ssm_scan_workspace_bytes(n_seq, *u.shape, A_log.shape[1], L)
     ws = _workspace(need, workspace, u)
-    check(lib().tcl_ssm_scan(ctypes.byref(a), _ptr(slots), n_slots, _ptr(state_out), out.data_ptr(), _ld(out),
-                             *_ws_args(ws), _stream(stream)))
+    check(lib().tcl_ssm_scan(a, _ptr(slots), n_slots, _ptr(state_out), out.data_ptr(), _ld(out),
+                             *_ws_args(ws), _stream_of(stream, u)))
     return out
 
 
@@ -691,21 +707,21 @@ def ssm_scan_backward(u, dt, A_log, B, C, dy, D=None, z=None, b_dt=None, offs=No
     for name, t in (("state", state), ("state_grad", state_grad)):
         _expect(name, t, torch.float32, (n_seq, *A_log.shape), u)
     _expect("dy", dy, u.dtype, u.shape, u, rows=True)
-    a = _scan_args(u, dt, A_log, B, C, D, z, b_dt, offs, n_seq, L, state)
+    L, a = _scan_args(u, dt, A_log, B, C, D, z, b_dt, offs, n_seq, L, state)
 
     def new(*shape, dtype=u.dtype):
         return torch.empty(shape, dtype=dtype, device=u.device)
 
-    rows, E, N, f32 = a.rows, a.E, a.N, torch.float32
+    (rows, E), N, f32 = u.shape, A_log.shape[1], torch.float32
     r = dict(du=new(rows, E), ddt=new(rows, E), dz=None if z is None else new(rows, E), dB=new(rows, N),
              dC=new(rows, N), dA_log=new(E, N, dtype=f32), dD=new(E, dtype=f32), db_dt=new(E, dtype=f32),
              dstate=None if state is None else new(n_seq, E, N, dtype=f32))
-    g = SsmScanGrads(r["du"].data_ptr(), E, r["ddt"].data_ptr(), E, r["dB"].data_ptr(), N, r["dC"].data_ptr(), N,
-                     _ptr(r["dz"]), E, r["dA_log"].data_ptr(), r["dD"].data_ptr(), r["db_dt"].data_ptr(),
-                     _ptr(r["dstate"]))
-    ws = _workspace(lib().tcl_ssm_scan_backward_workspace_bytes(n_seq, rows, E, N, a.L), workspace, u)
-    check(lib().tcl_ssm_scan_backward(ctypes.byref(a), dy.data_ptr(), _ld(dy), _ptr(state_grad), ctypes.byref(g),
-                                      *_ws_args(ws), _stream(stream)))
+    g = _PACK_GRADS.pack(r["du"].data_ptr(), E, r["ddt"].data_ptr(), E, r["dB"].data_ptr(), N, r["dC"].data_ptr(), N,
+                         _adr(r["dz"]), E, r["dA_log"].data_ptr(), r["dD"].data_ptr(), r["db_dt"].data_ptr(),
+                         _adr(r["dstate"]))
+    ws = _workspace(lib().tcl_ssm_scan_backward_workspace_bytes(n_seq, rows, E, N, L), workspace, u)
+    check(lib().tcl_ssm_scan_backward(a, dy.data_ptr(), _ld(dy), _ptr(state_grad), g,
+                                      *_ws_args(ws), _stream_of(stream, u)))
     return r
 
 
@@ -751,7 +767,7 @@ def logprobs(logits, tokens=None, K=0, temperature=1.0, seg_offsets=None, max_le
     ws = _workspace(lib().tcl_logits_workspace_bytes(n, V, K), workspace, logits)
     check(lib().tcl_logprobs(_dtype(logits), n, V, logits.data_ptr(), ld, _ptr(seg_offsets), temperature,
                              _ptr(tokens), K, _ptr(r["logp"]), r["entropy"].data_ptr(), _ptr(r["top"]),
-                             _ptr(r["top_logp"]), *_ws_args(ws), _stream(stream)))
+                             _ptr(r["top_logp"]), *_ws_args(ws), _stream_of(stream, logits)))
     return r
 
 
@@ -780,7 +796,7 @@ def distill_topk(logits, top, teacher, weight=None, temperature=1.0, seg_offsets
     ws = _workspace(lib().tcl_logits_workspace_bytes(n, V, K), workspace, logits)
     check(lib().tcl_distill_topk(_dtype(logits), n, V, logits.data_ptr(), ld, _ptr(seg_offsets), temperature, K,
                                  top.data_ptr(), teacher.data_ptr(), _ptr(weight), loss.data_ptr(), _ptr(grad), ldg,
-                                 *_ws_args(ws), _stream(stream)))
+                                 *_ws_args(ws), _stream_of(stream, logits)))
     return dict(loss=loss, grad=grad)
 
 

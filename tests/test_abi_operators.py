@@ -198,3 +198,12 @@ def test_binding_checks_tensors():
         tb._pools(pool, None, torch.zeros(4, dtype=torch.int32), 5, (3, 8), torch.float32, x)
     with pytest.raises(ValueError, match="state"):
         tb._pools(pool[0], None, None, 5, (3, 8), torch.float32, x)
+
+
+def test_packed_arguments_have_the_structures_layout():
+    for pack, struct in ((tb._PACK_CONV, tb.SsmConvArgs), (tb._PACK_SCAN, tb.SsmScanArgs),
+                         (tb._PACK_GRADS, tb.SsmScanGrads)):
+        assert pack.size == ctypes.sizeof(struct)
+        values = list(range(1, len(struct._fields_) + 1))
+        back = struct.from_buffer_copy(pack.pack(*values))
+        assert [getattr(back, n) for n, _ in struct._fields_] == values
