@@ -455,91 +455,87 @@ struct TeacherArgs {
   int64_t ldg;
 };
 
-template <int NW>
-__device__ __forceinline__ float block_max(float v, float* red) {
-  v = wave_max(v);
-  if (NW > 1) {
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
-    __syncthreads();
-    v = red[0];
-#pragma unroll
-    for (int k = 1; k < NW; ++k) v = fmaxf(v, red[k]);
+// Two values over a workgroup's wavefronts at once, the larger or the sum of each. `red` is
+// used once, so one barrier is enough.
+template <int NW, bool MAX>
+__device__ __forceinline__ void block_reduce(float& a, float& b, float* red) {
+  a = MAX ? wave_max(a) : wave_sum(a);
+  b = MAX ? wave_max(b) : wave_sum(b);
+  if ((threadIdx.x & 63) == 0) {
+    red[threadIdx.x >> 6] = a;
+    red[16 + (threadIdx.x >> 6)] = b;
   }
-  return v;
-}
-template <int NW>
-__device__ __forceinline__ float block_sum(float v, float* red) {
-  v = wave_sum(v);
-  if (NW > 1) {
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
-    __syncthreads();
-    v = red[0];
+  __syncthreads();
+  a = red[0];
+  b = red[16];
 #pragma unroll
-    for (int k = 1; k < NW; ++k) v += red[k];
+  for (int k = 1; k < NW; ++k) {
+    a = MAX ? fmaxf(a, red[k]) : a + red[k];
+    b = MAX ? fmaxf(b, red[16 + k]) : b + red[16 + k];
   }
-  return v;
 }
 
-constexpr int kMaxTeacher = 1024;
-struct TeacherShared {
-  float x[kMaxTeacher];   // the student's logit at the entry
-  float q[kMaxTeacher];   // the teacher's probability
-  int at[kMaxTeacher];    // its place in the row, -1: none
-  float red[16];
+struct TeacherShared {  // three arrays of K in dynamic LDS
+  float* x;              // the student's logit at the entry
+  float* q;              // the teacher's logit at 1 / temperature, then its probability
+  int* at;               // its place in the row, -1: none
+  __device__ __forceinline__ TeacherShared(float* mem, int K)
+      : x(mem), q(mem + K), at(reinterpret_cast<int*>(mem + 2 * K)) {}
 };
 
-// The teacher's distribution of a row, and the student's logits at its entries
-// (read here, before a gradient may replace them). Returns whether there is one.
+// The teacher's entries of a row, and the student's logits there (read here, before
+// a gradient may replace them). The thread's part of the maximum; +inf where one is NaN or +inf.
 template <typename T, int NW>
-__device__ __forceinline__ bool teacher_row(TeacherShared& sh, const Row<T>& row, const TeacherArgs& t, int r,
-                                            float inv_temp, const float* sx) {
+__device__ __forceinline__ float teacher_entries(const TeacherShared& sh, const Row<T>& row, const TeacherArgs& t, int r,
+                                                 float inv_temp, const float* sx) {
   float m = -INFINITY;
-  bool bad = false;
   for (int k = threadIdx.x; k < t.K; k += 64 * NW) {
-    const int64_t j = (int64_t)t.top[(int64_t)r * t.K + k] - row.first;
-    const bool have = j >= 0 && j < row.cnt && t.top[(int64_t)r * t.K + k] >= 0;
+    const int i = t.top[(int64_t)r * t.K + k];
     const float v = t.val[(int64_t)r * t.K + k];
+    const int64_t j = (int64_t)i - row.first;
+    const bool have = i >= 0 && j >= 0 && j < row.cnt;
     sh.at[k] = have ? (int)j : -1;
     sh.q[k] = have ? v * inv_temp : -INFINITY;
-    if (have) bad |= !(v < INFINITY);  // NaN or +inf
     sh.x[k] = sx ? sx[k] : have ? row.at((int)j) : -INFINITY;
     m = fmaxf(m, sh.q[k]);
+    if (have && !(v < INFINITY)) m = INFINITY;
   }
-  m = block_max<NW>(bad ? INFINITY : m, sh.red);
-  float s = 0.f;
-  for (int k = threadIdx.x; k < t.K; k += 64 * NW) s += m > -INFINITY ? expf(sh.q[k] - m) : 0.f;
-  s = block_sum<NW>(s, sh.red);
-  const float ls = m + logf(s);  // m = +inf: NaN, and so is everything that follows
-  for (int k = threadIdx.x; k < t.K; k += 64 * NW) sh.q[k] -= ls;  // log q until teacher_loss
-  return m > -INFINITY;
+  return m;
 }
-
-// The loss; sh.q becomes q. ms: the student's maximum, ls: log of its sum.
+// The thread's part of the teacher's sum of exponentials, m its maximum.
 template <int NW>
-__device__ __forceinline__ float teacher_loss(TeacherShared& sh, int K, float ms, float ls, float inv_temp) {
+__device__ __forceinline__ float teacher_sum(const TeacherShared& sh, int K, float m) {
+  float s = 0.f;
+  for (int k = threadIdx.x; k < K; k += 64 * NW) s += m > -INFINITY ? expf(sh.q[k] - m) : 0.f;
+  return s;
+}
+// The thread's part of the loss; sh.q becomes q. lt: log of the teacher's sum of exponentials (m + log
+// sum; NaN for m = +inf, and so is all that follows), ms the student's maximum, ls the log of its sum.
+template <int NW>
+__device__ __forceinline__ float teacher_loss(const TeacherShared& sh, int K, float lt, float ms, float ls,
+                                              float inv_temp) {
   float loss = 0.f;
   for (int k = threadIdx.x; k < K; k += 64 * NW) {
-    const float lq = sh.q[k], q = sh.at[k] >= 0 ? expf(lq) : 0.f;
+    const float lq = sh.q[k] - lt, q = sh.at[k] >= 0 ? expf(lq) : 0.f;
     sh.q[k] = q;
     if (q != 0.f) loss += q * (lq - fmaf(sh.x[k] - ms, inv_temp, -ls));
   }
-  return block_sum<NW>(loss, sh.red);
+  return loss;
 }
 
 // Entry k of the list, if it is the first of its place: all the teacher's
 // probability there, by a loop over the list.
 __device__ __forceinline__ bool teacher_place(const TeacherShared& sh, int K, int k, float& q) {
   const int at = sh.at[k];
-  if (at < 0) return false;
+  bool first = at >= 0;
   q = 0.f;
-  for (int j = 0; j < K; ++j)
-    if (sh.at[j] == at) {
-      if (j < k) return false;
-      q += sh.q[j];
-    }
-  return true;
+#pragma unroll 8
+  for (int j = 0; j < K; ++j) {
+    const bool same = sh.at[j] == at;
+    if (same) q += sh.q[j];
+    first = first && !(same && j < k);
+  }
+  return first;
 }
 
 __device__ __forceinline__ void st_grad(float* p, float v) { *p = v; }
@@ -583,14 +579,16 @@ __device__ __forceinline__ bool same_phase(const Row<T>& row, const T* g) {
 template <typename T, int NW, int NV>
 __global__ __launch_bounds__(64 * NW) void distill_row_kernel(LogitRows a, TeacherArgs t) {
   constexpr int VE = Row<T>::VE, TB = 64 * NW;
-  __shared__ TeacherShared sh;
+  extern __shared__ __attribute__((aligned(16))) float teacher_mem[];
+  __shared__ float red[3][32];
+  TeacherShared sh(teacher_mem, t.K);
   const int r = blockIdx.x, tid = threadIdx.x;
   const Row<T> row(a, r);
   const float zc = a.inv_temp * kLog2e;
   u32x4 x[NV];
 #pragma unroll
   for (int k = 0; k < NV; ++k) x[k] = tid + k * TB < row.nvec ? row.load(tid + k * TB) : u32x4{0, 0, 0, 0};
-  const bool taught = teacher_row<T, NW>(sh, row, t, r, a.inv_temp, nullptr);
+  float mt = teacher_entries<T, NW>(sh, row, t, r, a.inv_temp, nullptr);
   float m = -INFINITY;
   auto vmax = [&](u32x4 v) {
 #pragma unroll
@@ -600,9 +598,9 @@ __global__ __launch_bounds__(64 * NW) void distill_row_kernel(LogitRows a, Teach
   for (int k = 0; k < NV; ++k)
     if (tid + k * TB < row.nvec) vmax(x[k]);
   for (int v = tid + NV * TB; v < row.nvec; v += TB) vmax(row.load(v));
-  m = block_max<NW>(m, sh.red);
+  block_reduce<NW, true>(m, mt, red[0]);
   if (!(m > -INFINITY)) m = 0.f;  // nothing but -inf (a sum of 0) or NaN (a sum of NaN)
-  float s = 0.f;
+  float s = 0.f, qs = teacher_sum<NW>(sh, t.K, mt);
   auto vsum = [&](u32x4 v) {
 #pragma unroll
     for (int i = 0; i < VE; ++i) s += __builtin_amdgcn_exp2f((Row<T>::get(v, i) - m) * zc);
@@ -611,13 +609,14 @@ __global__ __launch_bounds__(64 * NW) void distill_row_kernel(LogitRows a, Teach
   for (int k = 0; k < NV; ++k)
     if (tid + k * TB < row.nvec) vsum(x[k]);
   for (int v = tid + NV * TB; v < row.nvec; v += TB) vsum(row.load(v));
-  s = block_sum<NW>(s, sh.red);
-  const bool live = taught && s != 0.f;
+  block_reduce<NW, false>(s, qs, red[1]);
+  const bool live = mt > -INFINITY && s != 0.f;
   // (else the compiler holds all the differences and exponentials from here to the
   // gradient, beside the logits: 1 KB of spills per lane in fp32)
 #pragma unroll
   for (int k = 0; k < NV; ++k) asm volatile("" : "+v"(x[k]));
-  const float loss = teacher_loss<NW>(sh, t.K, m, logf(s), a.inv_temp);
+  float loss = teacher_loss<NW>(sh, t.K, mt + logf(qs), m, logf(s), a.inv_temp), none = 0.f;
+  block_reduce<NW, false>(loss, none, red[2]);
   if (tid == 0) t.loss[r] = live ? loss : 0.f;
   if (!t.grad) return;
   T* g = grad_row<T>(a, t, r);
@@ -628,8 +627,8 @@ __global__ __launch_bounds__(64 * NW) void distill_row_kernel(LogitRows a, Teach
   for (int k = 0; k < NV; ++k)
     if (tid + k * TB < row.nvec) grad_vec(row, g, same, tid + k * TB, x[k], f);
   for (int v = tid + NV * TB; v < row.nvec; v += TB) grad_vec(row, g, same, v, row.load(v), f);
-  __syncthreads();  // sh.q complete; the entries below are written after the ones above
   if (!live) return;
+  __syncthreads();  // the entries below are written after the ones above
   for (int k = tid; k < t.K; k += TB) {
     float q;
     if (teacher_place(sh, t.K, k, q)) st_grad(g + sh.at[k], f(sh.x[k]) - w * q);
@@ -643,7 +642,7 @@ template <typename T>
 __global__ __launch_bounds__(kTB) void distill_sums_kernel(LogitRows a, TeacherArgs t, Stats* __restrict__ part,
                                                            float* __restrict__ sx) {
   constexpr int VE = Row<T>::VE;
-  __shared__ float red[16];
+  __shared__ float red[2][32];
   const int r = blockIdx.x, tid = threadIdx.x;
   const Row<T> row(a, r);
   const int per = (row.nvec + gridDim.y - 1) / gridDim.y;
@@ -676,8 +675,10 @@ __global__ __launch_bounds__(kTB) void distill_sums_kernel(LogitRows a, TeacherA
       }
     }
   }
-  const float bm = block_max<kTB / 64>(m, red);
-  s = block_sum<kTB / 64>(m > -INFINITY ? s * __builtin_amdgcn_exp2f((m - bm) * zc) : s, red);
+  float bm = m, none = 0.f;
+  block_reduce<kTB / 64, true>(bm, none, red[0]);
+  s = m > -INFINITY ? s * __builtin_amdgcn_exp2f((m - bm) * zc) : s;
+  block_reduce<kTB / 64, false>(s, none, red[1]);
   if (tid == 0) part[(int64_t)r * gridDim.y + blockIdx.y] = Stats{bm, s, 0.f};
   if (blockIdx.y == 0)
     for (int k = tid; k < t.K; k += kTB) {
@@ -692,22 +693,28 @@ __global__ __launch_bounds__(kTB) void distill_grad_kernel(LogitRows a, TeacherA
                                                            const Stats* __restrict__ part,
                                                            const float* __restrict__ sx) {
   constexpr int VE = Row<T>::VE, NW = kTB / 64;
-  __shared__ TeacherShared sh;
+  extern __shared__ __attribute__((aligned(16))) float teacher_mem[];
+  __shared__ float red[3][32];
+  TeacherShared sh(teacher_mem, t.K);
   const int r = blockIdx.x, tid = threadIdx.x, S = gridDim.y;
   const Row<T> row(a, r);
   const int per = (row.nvec + S - 1) / S;
   const int v0 = min((int)blockIdx.y * per, row.nvec), v1 = min(v0 + per, row.nvec);
   const float zc = a.inv_temp * kLog2e;
-  const bool taught = teacher_row<T, NW>(sh, row, t, r, a.inv_temp, sx + (int64_t)r * t.K);
-  float m = -INFINITY, s = 0.f;
+  float mt = teacher_entries<T, NW>(sh, row, t, r, a.inv_temp, sx + (int64_t)r * t.K);
+  float m = -INFINITY, s = 0.f, none = 0.f;
   for (int k = 0; k < S; ++k) m = fmaxf(m, part[(int64_t)r * S + k].m);
   for (int k = 0; k < S; ++k) {
     const Stats p = part[(int64_t)r * S + k];
     s += p.m > -INFINITY ? p.s * __builtin_amdgcn_exp2f((p.m - m) * zc) : p.s;
   }
   if (!(m > -INFINITY)) m = 0.f;
-  const bool live = taught && s != 0.f;
-  const float loss = teacher_loss<NW>(sh, t.K, m, logf(s), a.inv_temp);
+  block_reduce<NW, true>(mt, none, red[0]);
+  const bool live = mt > -INFINITY && s != 0.f;
+  float qs = teacher_sum<NW>(sh, t.K, mt);
+  block_reduce<NW, false>(qs, none, red[1]);
+  float loss = teacher_loss<NW>(sh, t.K, mt + logf(qs), m, logf(s), a.inv_temp);
+  block_reduce<NW, false>(loss, none, red[2]);
   if (blockIdx.y == 0 && tid == 0) t.loss[r] = live ? loss : 0.f;
   if (!t.grad) return;
   T* g = grad_row<T>(a, t, r);
@@ -715,8 +722,8 @@ __global__ __launch_bounds__(kTB) void distill_grad_kernel(LogitRows a, TeacherA
   const float w = live ? (t.weight ? t.weight[r] : 1.f) * a.inv_temp : 0.f, ws = w / s;
   auto f = [&](float v) { return live ? __builtin_amdgcn_exp2f((v - m) * zc) * ws : 0.f; };
   for (int v = v0 + tid; v < v1; v += kTB) grad_vec(row, g, same, v, row.load(v), f);
-  __syncthreads();
   if (!live) return;
+  __syncthreads();
   const int lo = v0 * VE - row.h, hi = v1 * VE - row.h;  // the entries of this part
   for (int k = tid; k < t.K; k += kTB) {
     float q;
@@ -726,12 +733,17 @@ __global__ __launch_bounds__(kTB) void distill_grad_kernel(LogitRows a, TeacherA
 }
 
 // Parts of a row: one while the rows alone give every CU four workgroups, else
-// enough for that, of 512 vectors (two per thread) at least.
+// enough for that, of 512 vectors (two per thread) at least. 4 rows of 50,001 fp32 logits:
+// 24 parts and their join 14 us, one workgroup of 1,024 threads a row 18.
 int row_splits(int n, int V) {
   const int vecs = V / 4 + 1;
   const int want = std::max(1, 1024 / std::max(n, 1));
   return std::max(1, std::min({want, vecs / 512, 64}));
 }
+// Distillation takes two passes over a split row instead of one in registers, so a row
+// is split from where the registers of a workgroup do not hold it. 16 rows of 4,096 fp32
+// logits: 11 us whole, 18 in two parts.
+int distill_splits(int n, int V) { return V / 4 + 1 <= 16 * 1024 ? 1 : row_splits(n, V); }
 
 template <typename T>
 hipError_t logprobs(const LogitRows& a, int K, const LogprobOut& o, char* ws, hipStream_t s) {
@@ -747,29 +759,29 @@ hipError_t logprobs(const LogitRows& a, int K, const LogprobOut& o, char* ws, hi
 
 template <typename T>
 hipError_t distill(const LogitRows& a, const TeacherArgs& t, char* ws, hipStream_t s) {
-  const int S = row_splits(a.n, a.V);
+  const int S = distill_splits(a.n, a.V);
   if (S > 1) {
     Stats* part = reinterpret_cast<Stats*>(ws);
     float* sx = reinterpret_cast<float*>(ws + (size_t)a.n * S * sizeof(Stats));
     distill_sums_kernel<T><<<dim3(a.n, S), kTB, 0, s>>>(a, t, part, sx);
-    distill_grad_kernel<T><<<dim3(a.n, S), kTB, 0, s>>>(a, t, part, sx);
+    distill_grad_kernel<T><<<dim3(a.n, S), kTB, 12 * t.K, s>>>(a, t, part, sx);
     return hipGetLastError();
   }
   const int vecs = a.V / Row<T>::VE + (a.V % Row<T>::VE != 0);
-  if (vecs <= 64 * 4) distill_row_kernel<T, 1, 4><<<dim3(a.n), 64, 0, s>>>(a, t);
-  else if (vecs <= 256 * 4) distill_row_kernel<T, 4, 4><<<dim3(a.n), 256, 0, s>>>(a, t);
-  else if (vecs <= 512 * 8) distill_row_kernel<T, 8, 8><<<dim3(a.n), 512, 0, s>>>(a, t);
-  else if (vecs <= 1024 * 8) distill_row_kernel<T, 16, 8><<<dim3(a.n), 1024, 0, s>>>(a, t);
-  else distill_row_kernel<T, 16, 16><<<dim3(a.n), 1024, 0, s>>>(a, t);
+  if (vecs <= 64 * 4) distill_row_kernel<T, 1, 4><<<dim3(a.n), 64, 12 * t.K, s>>>(a, t);
+  else if (vecs <= 256 * 4) distill_row_kernel<T, 4, 4><<<dim3(a.n), 256, 12 * t.K, s>>>(a, t);
+  else if (vecs <= 512 * 8) distill_row_kernel<T, 8, 8><<<dim3(a.n), 512, 12 * t.K, s>>>(a, t);
+  else if (vecs <= 1024 * 8) distill_row_kernel<T, 16, 8><<<dim3(a.n), 1024, 12 * t.K, s>>>(a, t);
+  else distill_row_kernel<T, 16, 16><<<dim3(a.n), 1024, 12 * t.K, s>>>(a, t);
   return hipGetLastError();
 }
 
 }  // namespace
 
 size_t logits_workspace_bytes(int n, int V, int K) {
-  const int S = row_splits(n, V);
-  if (S == 1) return 0;
-  const size_t lp = (size_t)n * S * (K * 8 + 16), di = (size_t)n * S * sizeof(Stats) + (size_t)n * K * sizeof(float);
+  const int S = row_splits(n, V), D = distill_splits(n, V);
+  const size_t lp = S > 1 ? (size_t)n * S * (K * 8 + 16) : 0;
+  const size_t di = D > 1 ? (size_t)n * D * sizeof(Stats) + (size_t)n * K * sizeof(float) : 0;
   return std::max(lp, di);
 }
 

@@ -229,9 +229,10 @@ def test_distill(n, V, ld, K, kind, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("n,V", [(515, 17000), (514, 70001), (513, 140003)])
+@pytest.mark.parametrize("n,V", [(515, 17000), (514, 70001), (513, 140003), (259, 70001), (258, 150001)])
 def test_distill_rows_of_every_length(n, V, dtype):
-    """Rows that the registers hold, and longer ones whose rest is read again."""
+    """Rows that the registers hold, longer ones whose rest is read again, and few long ones, which are
+    split over workgroups."""
     print(f"distill rows n={n} V={V} {dtype}", flush=True)
     g = torch.Generator(device="cuda").manual_seed(V)
     x = (2 * torch.randn(n, V, generator=g, device="cuda")).to(DT[dtype])
