@@ -414,6 +414,11 @@ __global__ __launch_bounds__(64 * kSumLanes) void sum_parts_kernel(const float* 
   else if (o2) o2[e] = acc;
 }
 
+template <int CTRL>
+__device__ __forceinline__ float dpp(float v) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xF, 0xF, false));
+}
+
 // ---------------------------------------------------------------- selective scan, prompts
 // s_t = exp(d_t A) s_{t-1} + d_t u_t B_t,  y_t = (C_t . s_t + D u_t) SiLU(z_t),
 // d = softplus(dt + b_dt), A = -exp(A_log).
@@ -423,10 +428,12 @@ __global__ __launch_bounds__(64 * kSumLanes) void sum_parts_kernel(const float* 
 // next kTC rows on their way in registers meanwhile; u, dt and z come four
 // tokens ahead. Per token and wavefront 6 N issue slots for the states and
 // some 25 for softplus, gate and output, against 4 x 64 elements of traffic: the
-// vector unit is what bounds it (see launch_ssm_scan for figures).
+// vector unit is what bounds it: 4,096 programs of up to 25 tokens, E 512, fp32, in 139 us, where their
+// traffic takes 108 and their issue slots 112; a prompt of 8,192 tokens, E 4,096, bf16 in chunks
+// 113 + 12 + 150.
 //
-// A sequence is cut into chunks of CL tokens when there are too few of them to
-// fill the GPU. s -> P s + s_loc with P = exp(A sum d) is what a chunk does to a
+// A sequence is cut into chunks of CL tokens when there are far too few of them to
+// fill the GPU (scan_chunk). s -> P s + s_loc with P = exp(A sum d) is what a chunk does to a
 // state, so LOCAL runs every chunk but a sequence's last from zero for (s_loc,
 // sum d), ssm_combine_kernel composes them into every chunk's start state,
 // and the plain form runs the chunks from there. Twice the exponentials.
@@ -572,6 +579,100 @@ __global__ __launch_bounds__(64, 4) void ssm_scan_kernel(ScanIn a, const T* __re
   } else if (state_out && sl >= 0 && t1 == tl.len) {
     st_vec<N>(state_out + (int64_t)sl * E * N, ln, s);
   }
+}
+
+// The same, for batches too small to give a SIMD two wavefronts of one lane per channel but large
+// enough that cutting the sequences (twice the exponentials) would not pay: Q = N / 4 lanes per channel
+// hold four states each, and a token costs a wavefront a quarter. What a token needs once
+// per channel (softplus, gate, output) is done by one lane for each of Q tokens and passed round by
+// DPP, so it is not done Q times: 150 issue slots per token and 64 channels against 140. Tokens past the
+// end have d = 0, which leaves the states as they are.
+constexpr int kQuadThreads = 256;
+template <typename T, int N>
+__global__ __launch_bounds__(kQuadThreads) void ssm_scan_quad_kernel(
+    ScanIn a, const T* __restrict__ u, const T* __restrict__ dt, const T* __restrict__ B, const T* __restrict__ C,
+    const T* __restrict__ z, float* state_out, T* __restrict__ y, int64_t ldy) {
+  constexpr int Q = N / 4, W = 2 * N, CH = kQuadThreads / Q, PER = kTC * W / kQuadThreads;
+  __shared__ __attribute__((aligned(16))) float sBC[kTC * W];
+  int w, cg;
+  if (!tile_of_block(a.ntile, (a.E + CH - 1) / CH, w, cg)) return;
+  const Tile tl = find_tile(a.offs, a.n_seq, a.rows, a.CL, w);
+  if (tl.seq < 0) return;
+  const int E = a.E, q = threadIdx.x % Q, n0 = 4 * q;
+  const int e = cg * CH + threadIdx.x / Q;
+  const bool active = e < E;
+  const int ec = active ? e : E - 1;
+  float a2[4], s[4] = {0.f, 0.f, 0.f, 0.f};
+  ld_vec<4>(a.A_log, (uint32_t)(ec * N + n0) * 4, a2);
+#pragma unroll
+  for (int n = 0; n < 4; ++n) a2[n] = decay_rate(a2[n]);
+  const int sl = slot_of(a.slots, a.n_slots, tl.seq);
+  if (a.state && sl >= 0) ld_vec<4>(a.state + (int64_t)sl * E * N, (uint32_t)(ec * N + n0) * 4, s);
+  const float bias = a.b_dt ? a.b_dt[ec] : 0.f, Dv = a.D ? a.D[ec] : 0.f;
+  const int len = tl.len;
+  const int64_t r0 = tl.base;
+  const T *us = u + r0 * a.ldu + ec, *ds = dt + r0 * a.lddt + ec, *zs = z ? z + r0 * a.ldz + ec : nullptr;
+  T* ys = y + r0 * ldy + ec;
+  // staging: a thread takes one column of every RW-th row
+  constexpr int RW = kQuadThreads / W;
+  const int col = threadIdx.x % W, row0 = threadIdx.x / W;
+  const int64_t ldS = col < N ? a.ldB : a.ldC;
+  const T* src = col < N ? B + r0 * a.ldB + col : C + r0 * a.ldC + (col - N);
+  T st[PER], nu, nd, nz;
+  auto stage = [&](int t) {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) st[i] = src[min(t + row0 + i * RW, len - 1) * ldS];
+  };
+  auto load = [&](int t) {  // the lane's token of the next Q
+    const int64_t r = min(t + q, len - 1);
+    nu = us[r * a.ldu];
+    nd = ds[r * a.lddt];
+    if (z) nz = zs[r * a.ldz];
+  };
+  if (len > 0) {
+    stage(0);
+    load(0);
+  }
+  for (int tc = 0; tc < len; tc += kTC) {
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < PER; ++i) sBC[i * kQuadThreads + threadIdx.x] = to_f32(st[i]);
+    __syncthreads();
+    if (tc + kTC < len) stage(tc + kTC);
+    const int te = min(len, tc + kTC);
+    for (int tg = tc; tg < te; tg += Q) {
+      const int t = tg + q;
+      const float uv = to_f32(nu), d = t < len ? softplus(to_f32(nd) + bias) : 0.f, du = d * uv;
+      const float gate = z ? silu(to_f32(nz)) : 1.f;
+      if (tg + Q < len) load(tg + Q);
+      float mine = 0.f;
+      auto token = [&](int i, float di, float dui) {
+        const float* x = &sBC[(tg - tc + i) * W + n0];
+        float xb[4], xc[4], acc = 0.f;
+        ld_vec<4>(x, 0, xb);
+        ld_vec<4>(x + N, 0, xc);
+#pragma unroll
+        for (int n = 0; n < 4; ++n) {
+          s[n] = fmaf(__builtin_amdgcn_exp2f(di * a2[n]), s[n], dui * xb[n]);
+          acc = fmaf(s[n], xc[n], acc);
+        }
+        acc += dpp<0xB1>(acc);                 // quad_perm: lane ^ 1
+        if (Q == 4) acc += dpp<0x4E>(acc);     // lane ^ 2
+        if (q == i) mine = acc;
+      };
+      if constexpr (Q == 4) {  // quad_perm: lane i's value to all four
+        token(0, dpp<0x00>(d), dpp<0x00>(du));
+        token(1, dpp<0x55>(d), dpp<0x55>(du));
+        token(2, dpp<0xAA>(d), dpp<0xAA>(du));
+        token(3, dpp<0xFF>(d), dpp<0xFF>(du));
+      } else {  // the even (odd) lane's value to its pair
+        token(0, dpp<0xA0>(d), dpp<0xA0>(du));
+        token(1, dpp<0xF5>(d), dpp<0xF5>(du));
+      }
+      if (active && t < len) st1(ys + t * ldy, fmaf(Dv, uv, mine) * gate);
+    }
+  }
+  if (active && state_out && sl >= 0) st_vec<4>(state_out + (int64_t)sl * E * N, (uint32_t)(ec * N + n0) * 4, s);
 }
 
 // Every chunk's start state out of the chunks' (s_loc, sum d), in place of
@@ -799,11 +900,6 @@ __global__ __launch_bounds__(64, 4) void ssm_bwd_local_kernel(ScanIn a, const T*
   }
 }
 
-template <int CTRL>
-__device__ __forceinline__ float dpp(float v) {
-  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xF, 0xF, false));
-}
-
 // Sums of many values over the 64 lanes, scattered over the lanes: halves of the
 // values go to halves of the lanes step by step, half-wave and row swaps routing a pair at
 // once, then within rows of 16 by DPP (rotation by 8, mirrors of 8, quad
@@ -952,23 +1048,27 @@ __global__ __launch_bounds__(256, 2) void ssm_bwd_kernel(
       park(0);
     }
     const float* ck = sCk + max(b - 1, 0) * N * 64;
-    float hist[kSub - 1][N];  // the state in front of each token but the first
+    // the states behind each of the tokens but the last, and the tokens' steps
+    float hist[kSub - 1][N], step[kSub];
     {
-      T ru[kSub - 1], rd[kSub - 1];
+      T ru[kSub - 1], rd[kSub];
 #pragma unroll
-      for (int i = 0; i + 1 < kSub; ++i) {
+      for (int i = 0; i < kSub; ++i) {
         const int64_t t = min(b * kSub + i, nt - 1);
-        ru[i] = ld_at(us + t * a.ldu, le);
+        if (i + 1 < kSub) ru[i] = ld_at(us + t * a.ldu, le);
         rd[i] = ld_at(ds + t * a.lddt, le);
       }
 #pragma unroll
-      for (int i = 0; i + 1 < kSub; ++i) {
-        if (b * kSub + i + 1 < nt) {
-          const float d = softplus(to_f32(rd[i]) + bias), du = d * to_f32(ru[i]);
-          const float* x = &sBC[(b * kSub + i) * W];
+      for (int i = 0; i < kSub; ++i) {
+        if (b * kSub + i < nt) {
+          step[i] = softplus(to_f32(rd[i]) + bias);
+          if (i + 1 < kSub) {
+            const float du = step[i] * to_f32(ru[i]);
+            const float* x = &sBC[(b * kSub + i) * W];
 #pragma unroll
-          for (int n = 0; n < N; ++n)
-            hist[i][n] = fmaf(__builtin_amdgcn_exp2f(d * a2[n]), i ? hist[i - 1][n] : ck[n * 64], du * x[n]);
+            for (int n = 0; n < N; ++n)
+              hist[i][n] = fmaf(__builtin_amdgcn_exp2f(step[i] * a2[n]), i ? hist[i - 1][n] : ck[n * 64], du * x[n]);
+          }
         }
         __builtin_amdgcn_sched_barrier(0);
       }
@@ -981,7 +1081,7 @@ __global__ __launch_bounds__(256, 2) void ssm_bwd_kernel(
       const float uv = active ? to_f32(cu) : 0.f, v = to_f32(cd) + bias, gy = active ? to_f32(cg_) : 0.f;
       const float zv = z ? to_f32(cz) : 0.f;
       load(t - 1);
-      const float d = softplus(v), du = d * uv;
+      const float d = step[i], du = d * uv;
       float gate = 1.f, dgate = 0.f;
       if (z) {
         const float sg = rcp_fast(1.f + exp_fast(-zv));
@@ -996,7 +1096,8 @@ __global__ __launch_bounds__(256, 2) void ssm_bwd_kernel(
 #pragma unroll
       for (int n = 0; n < N; ++n) {
         const float an = __builtin_amdgcn_exp2f(d * a2[n]);
-        const float as = an * (i ? hist[i - 1][n] : ck[n * 64]), st = fmaf(du, x[n], as);
+        const float as = an * (i ? hist[i - 1][n] : ck[n * 64]);
+        const float st = i + 1 < kSub ? hist[i][n] : fmaf(du, x[n], as);
         const float g = fmaf(q, x[N + n], h[n]);
         yv = fmaf(st, x[N + n], yv);
         gB = fmaf(g, x[n], gB);
@@ -1120,15 +1221,22 @@ hipError_t conv_bwd(const ConvOp& a, const void* du, int64_t lddu, const void* d
 }
 
 // ---- scan plans
-// Chunk length of the forward scan: sequences run whole (0) while they give
-// every SIMD four wavefronts, or are too short to cut.
-int scan_chunk(int n_seq, int rows, int E, int L) {
-  const int64_t waves = (int64_t)n_seq * ((E + 63) / 64), fill = (int64_t)kCUs * 4 * 4;
-  if (L <= 2 * kTC || waves * 2 > fill) return 0;
-  const int64_t chunks = fill / waves;  // per sequence, were all of them L long
+// How the forward scan runs, by the wavefronts that one lane per channel would give it. From 2,048 on
+// (two to a SIMD) sequences run whole, a lane per channel; below, whole with N / 4 lanes per channel;
+// below 256, longer than two stages, in chunks. E 4,096, bf16 (us: chunks / lane per channel / N / 4 lanes):
+// 32 sequences of 1,024 tokens (2,048 wavefronts) 971 / 665 / 648, 16 544 / 547 / 395, 8 294 / 462 / 243;
+// 4 of 256 (256) 60 / 121 / 61, one (64) 39 / 111 / 57; E 512: 16 of 512 (128) 57 / 220 / 83, 512 of 100
+// at E 256 (2,048) 180 / 70 / 68, 64 of 128 at E 4,096 (4,096) - / 131 / 151.
+int64_t scan_waves(int n_seq, int E) { return (int64_t)n_seq * ((E + 63) / 64); }
+bool scan_quad(int n_seq, int E) { return scan_waves(n_seq, E) < 2048; }
+// Tokens per chunk, 0 for whole sequences: enough chunks for four wavefronts to every SIMD, were all
+// sequences L long.
+int scan_chunk(int n_seq, int E, int L) {
+  const int64_t waves = scan_waves(n_seq, E), fill = (int64_t)kCUs * 4 * 4;
+  if (L <= 2 * kTC || waves >= 256) return 0;
+  const int64_t chunks = fill / std::max<int64_t>(waves, 1);
   int64_t CL = (L + chunks - 1) / chunks;
-  CL = (CL + kTC - 1) / kTC * kTC;
-  CL = std::max<int64_t>(CL, kTC);
+  CL = std::max<int64_t>((CL + kTC - 1) / kTC * kTC, kTC);
   return CL < L ? (int)CL : 0;
 }
 
@@ -1158,9 +1266,15 @@ hipError_t scan_fwd(const ScanOp& a, float* state_out, void* y_, int64_t ldy, fl
       ssm_scan_token_kernel<T, N, 1><<<dim3(gx, a.n_seq), 256, 0, s>>>(in, u, dt, B, C, z, state_out, y, ldy);
     return hipGetLastError();
   }
-  const int CG = (a.E + 63) / 64, CL = scan_chunk(a.n_seq, a.rows, a.E, a.L);
+  const int CG = (a.E + 63) / 64, CL = scan_chunk(a.n_seq, a.E, a.L);
   if (!CL) {
     const ScanIn in = scan_in(a, a.rows + 1);  // one tile per sequence
+    if (scan_quad(a.n_seq, a.E)) {
+      constexpr int CH = kQuadThreads / (N / 4);
+      ssm_scan_quad_kernel<T, N><<<dim3(tile_blocks(in.ntile, (a.E + CH - 1) / CH)), kQuadThreads, 0, s>>>(
+          in, u, dt, B, C, z, state_out, y, ldy);
+      return hipGetLastError();
+    }
     ssm_scan_kernel<T, N, false><<<dim3(tile_blocks(in.ntile, CG)), 64, 0, s>>>(in, u, dt, B, C, z, state_out, y, ldy,
                                                                                nullptr, nullptr);
     return hipGetLastError();
@@ -1281,7 +1395,7 @@ hipError_t launch_ssm_conv_bwd(const ConvOp& a, const void* du, int64_t lddu, co
 }
 
 size_t ssm_scan_workspace_bytes(int n_seq, int rows, int E, int N, int L) {
-  const int CL = scan_chunk(n_seq, rows, E, L);
+  const int CL = scan_chunk(n_seq, E, L);
   return CL ? ((size_t)rows / CL + n_seq) * (N + 1) * E * sizeof(float) : 0;
 }
 

@@ -180,6 +180,34 @@ def test_scan(lens, E, ld, full, N, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,E,N", [(300, 450, 16), (1100, 70, 8)])
+def test_scan_of_many_sequences(n, E, N, dtype):
+    """Batches large enough for one lane per channel, with slots, some sequences empty or
+    without a state."""
+    print(f"scan many n={n} E={E} N={N} {dtype}", flush=True)
+    rng = np.random.default_rng(n)
+    lens = rng.integers(0, 12, n).tolist()
+    lens[3] = 70
+    a = _scan_case(lens, E, N, dtype, n)
+    offs, T, pool = _offs(lens), sum(lens), n + 3
+    slots = rng.permutation(pool)[:n].astype(np.int32)
+    slots[5], slots[6] = -1, pool
+    live = (slots >= 0) & (slots < pool)
+    a["state"][~live] = 0.0
+    k = _scan_tensors(a, dtype, T)
+    S = torch.zeros(pool, E, N, device="cuda")
+    at = torch.from_numpy(slots[live].astype(np.int64)).cuda()
+    S[at] = _cuda(a["state"][live])
+    y = _tb().ssm_scan(offs=_cuda(offs, torch.int32), L=70, state_out=S, slots=_cuda(slots, torch.int32),
+                       **dict(k, state=S))
+    ref = osq.scan(offs=offs, **a)
+    _near("y", y, ref["y"], ref["bound"]["y"], HALF[dtype])
+    _near("end", S[at], ref["end"][live], ref["bound"]["end"][live], HALF["f32"])
+    S[at] = 0.0
+    assert not S.any()  # the other places of the pool are as they were
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("lens,E,N", [([70, 3, 40], 64, 16), ([300], 65, 8)])
 def test_scan_of_steep_steps(lens, E, N, dtype):
     """Steps of 1e-26 to 40: states that stay, states that are forgotten."""
