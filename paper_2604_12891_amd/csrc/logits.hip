@@ -445,6 +445,23 @@ __global__ __launch_bounds__(kTB) void logprobs_join_kernel(LogitRows a, int K, 
 //   loss = sum_k q_k (log q_k - log p_(i_k)),  dloss/dx_v = inv_temp (p_v - sum_k [i_k = v] q_k).
 // Entries without a place in the row (index outside it) do not count. A row without any
 // teacher's entry, or whose own entries are all -inf, has loss 0 and gradient 0.
+// exp(d / temperature) for a difference d of logits. One product with log2(e) / temperature and the
+// hardware's exp2 are off by |d / temperature| units of rounding, which a bf16 gradient does not show;
+// for fp32 logits what the product and the constant round away is put back.
+template <typename T>
+struct ScaledExp {
+  float hi, lo;
+  __device__ __forceinline__ explicit ScaledExp(float inv_temp) {
+    hi = inv_temp * kLog2e;
+    lo = fmaf(inv_temp, 1.925963e-8f, fmaf(inv_temp, kLog2e, -hi));  // log2(e) is kLog2e + 1.925963e-8
+  }
+  __device__ __forceinline__ float operator()(float d) const {
+    if constexpr (sizeof(T) == 2) return __builtin_amdgcn_exp2f(d * hi);
+    d = d < -1e30f ? -1e30f : d;  // (a NaN stays one)
+    const float t = d * hi, e = __builtin_amdgcn_exp2f(t);
+    return fmaf(e, fmaf(d, lo, fmaf(d, hi, -t)) * kLn2, e);
+  }
+};
 struct TeacherArgs {
   int K;
   const int* top;
@@ -509,14 +526,14 @@ __device__ __forceinline__ float teacher_sum(const TeacherShared& sh, int K, flo
   for (int k = threadIdx.x; k < K; k += 64 * NW) s += m > -INFINITY ? expf(sh.q[k] - m) : 0.f;
   return s;
 }
-// The thread's part of the loss; sh.q becomes q. lt: log of the teacher's sum of exponentials (m + log
-// sum; NaN for m = +inf, and so is all that follows), ms the student's maximum, ls the log of its sum.
+// The thread's part of the loss; sh.q becomes q. mt, lt: the teacher's maximum and the log of its sum
+// of exponentials (mt = +inf makes all that follows NaN); ms, ls: the student's.
 template <int NW>
-__device__ __forceinline__ float teacher_loss(const TeacherShared& sh, int K, float lt, float ms, float ls,
+__device__ __forceinline__ float teacher_loss(const TeacherShared& sh, int K, float mt, float lt, float ms, float ls,
                                               float inv_temp) {
   float loss = 0.f;
   for (int k = threadIdx.x; k < K; k += 64 * NW) {
-    const float lq = sh.q[k] - lt, q = sh.at[k] >= 0 ? expf(lq) : 0.f;
+    const float lq = sh.q[k] - mt - lt, q = sh.at[k] >= 0 ? expf(lq) : 0.f;
     sh.q[k] = q;
     if (q != 0.f) loss += q * (lq - fmaf(sh.x[k] - ms, inv_temp, -ls));
   }
@@ -584,7 +601,7 @@ __global__ __launch_bounds__(64 * NW) void distill_row_kernel(LogitRows a, Teach
   TeacherShared sh(teacher_mem, t.K);
   const int r = blockIdx.x, tid = threadIdx.x;
   const Row<T> row(a, r);
-  const float zc = a.inv_temp * kLog2e;
+  const ScaledExp<T> ex(a.inv_temp);
   u32x4 x[NV];
 #pragma unroll
   for (int k = 0; k < NV; ++k) x[k] = tid + k * TB < row.nvec ? row.load(tid + k * TB) : u32x4{0, 0, 0, 0};
@@ -603,7 +620,7 @@ __global__ __launch_bounds__(64 * NW) void distill_row_kernel(LogitRows a, Teach
   float s = 0.f, qs = teacher_sum<NW>(sh, t.K, mt);
   auto vsum = [&](u32x4 v) {
 #pragma unroll
-    for (int i = 0; i < VE; ++i) s += __builtin_amdgcn_exp2f((Row<T>::get(v, i) - m) * zc);
+    for (int i = 0; i < VE; ++i) s += ex(Row<T>::get(v, i) - m);
   };
 #pragma unroll
   for (int k = 0; k < NV; ++k)
@@ -615,14 +632,14 @@ __global__ __launch_bounds__(64 * NW) void distill_row_kernel(LogitRows a, Teach
   // gradient, beside the logits: 1 KB of spills per lane in fp32)
 #pragma unroll
   for (int k = 0; k < NV; ++k) asm volatile("" : "+v"(x[k]));
-  float loss = teacher_loss<NW>(sh, t.K, mt + logf(qs), m, logf(s), a.inv_temp), none = 0.f;
+  float loss = teacher_loss<NW>(sh, t.K, mt, logf(qs), m, logf(s), a.inv_temp), none = 0.f;
   block_reduce<NW, false>(loss, none, red[2]);
   if (tid == 0) t.loss[r] = live ? loss : 0.f;
   if (!t.grad) return;
   T* g = grad_row<T>(a, t, r);
   const bool same = same_phase(row, g);
   const float w = live ? (t.weight ? t.weight[r] : 1.f) * a.inv_temp : 0.f, ws = w / s;
-  auto f = [&](float v) { return live ? __builtin_amdgcn_exp2f((v - m) * zc) * ws : 0.f; };
+  auto f = [&](float v) { return live ? ex(v - m) * ws : 0.f; };
 #pragma unroll
   for (int k = 0; k < NV; ++k)
     if (tid + k * TB < row.nvec) grad_vec(row, g, same, tid + k * TB, x[k], f);
@@ -647,7 +664,7 @@ __global__ __launch_bounds__(kTB) void distill_sums_kernel(LogitRows a, TeacherA
   const Row<T> row(a, r);
   const int per = (row.nvec + gridDim.y - 1) / gridDim.y;
   const int v0 = min((int)blockIdx.y * per, row.nvec), v1 = min(v0 + per, row.nvec);
-  const float zc = a.inv_temp * kLog2e;
+  const ScaledExp<T> ex(a.inv_temp);
   float m = -INFINITY, s = 0.f;
   constexpr int U = 4;
   for (int vb = v0 + tid; vb < v1; vb += U * kTB) {
@@ -663,7 +680,7 @@ __global__ __launch_bounds__(kTB) void distill_sums_kernel(LogitRows a, TeacherA
       for (int i = 0; i < VE; ++i) nm = fmaxf(nm, Row<T>::get(x[k], i));
     }
     if (nm > m) {
-      s = m > -INFINITY ? s * __builtin_amdgcn_exp2f((m - nm) * zc) : s;
+      s = m > -INFINITY ? s * ex(m - nm) : s;
       m = nm;
     }
 #pragma unroll
@@ -671,13 +688,13 @@ __global__ __launch_bounds__(kTB) void distill_sums_kernel(LogitRows a, TeacherA
       if (vb + k * kTB >= v1) break;
 #pragma unroll
       for (int i = 0; i < VE; ++i) {
-        s += __builtin_amdgcn_exp2f((Row<T>::get(x[k], i) - (m > -INFINITY ? m : 0.f)) * zc);
+        s += ex(Row<T>::get(x[k], i) - (m > -INFINITY ? m : 0.f));
       }
     }
   }
   float bm = m, none = 0.f;
   block_reduce<kTB / 64, true>(bm, none, red[0]);
-  s = m > -INFINITY ? s * __builtin_amdgcn_exp2f((m - bm) * zc) : s;
+  s = m > -INFINITY ? s * ex(m - bm) : s;
   block_reduce<kTB / 64, false>(s, none, red[1]);
   if (tid == 0) part[(int64_t)r * gridDim.y + blockIdx.y] = Stats{bm, s, 0.f};
   if (blockIdx.y == 0)
@@ -700,27 +717,27 @@ __global__ __launch_bounds__(kTB) void distill_grad_kernel(LogitRows a, TeacherA
   const Row<T> row(a, r);
   const int per = (row.nvec + S - 1) / S;
   const int v0 = min((int)blockIdx.y * per, row.nvec), v1 = min(v0 + per, row.nvec);
-  const float zc = a.inv_temp * kLog2e;
+  const ScaledExp<T> ex(a.inv_temp);
   float mt = teacher_entries<T, NW>(sh, row, t, r, a.inv_temp, sx + (int64_t)r * t.K);
   float m = -INFINITY, s = 0.f, none = 0.f;
   for (int k = 0; k < S; ++k) m = fmaxf(m, part[(int64_t)r * S + k].m);
   for (int k = 0; k < S; ++k) {
     const Stats p = part[(int64_t)r * S + k];
-    s += p.m > -INFINITY ? p.s * __builtin_amdgcn_exp2f((p.m - m) * zc) : p.s;
+    s += p.m > -INFINITY ? p.s * ex(p.m - m) : p.s;
   }
   if (!(m > -INFINITY)) m = 0.f;
   block_reduce<NW, true>(mt, none, red[0]);
   const bool live = mt > -INFINITY && s != 0.f;
   float qs = teacher_sum<NW>(sh, t.K, mt);
   block_reduce<NW, false>(qs, none, red[1]);
-  float loss = teacher_loss<NW>(sh, t.K, mt + logf(qs), m, logf(s), a.inv_temp);
+  float loss = teacher_loss<NW>(sh, t.K, mt, logf(qs), m, logf(s), a.inv_temp);
   block_reduce<NW, false>(loss, none, red[2]);
   if (blockIdx.y == 0 && tid == 0) t.loss[r] = live ? loss : 0.f;
   if (!t.grad) return;
   T* g = grad_row<T>(a, t, r);
   const bool same = same_phase(row, g);
   const float w = live ? (t.weight ? t.weight[r] : 1.f) * a.inv_temp : 0.f, ws = w / s;
-  auto f = [&](float v) { return live ? __builtin_amdgcn_exp2f((v - m) * zc) * ws : 0.f; };
+  auto f = [&](float v) { return live ? ex(v - m) * ws : 0.f; };
   for (int v = v0 + tid; v < v1; v += kTB) grad_vec(row, g, same, v, row.load(v), f);
   if (!live) return;
   __syncthreads();
