@@ -487,7 +487,8 @@ TCL_API tcl_status tcl_trainer_timing_reset(tcl_trainer* trainer);
  *    distinct where an output pool is given. Other places of the output pool
  *    are left as they are.
  *  - Outputs must not overlap inputs (states aside) or each other.
- *  - E in [1, 65536], d_state (N) 8 or 16, d_conv (K) in [1, 4]. Stream-ordered,
+ *  - E in [1, 65536], d_state (N) 8 or 16, d_conv (K) in [1, 4], n_seq and rows at most 2^30 and
+ *    (n_seq + rows) E at most 2^36. Stream-ordered,
  *    deterministic, no allocation; may be captured into a graph. Empty work
  *    (n_seq == 0, or rows == 0 in the single-token form) is TCL_OK.
  * ------------------------------------------------------------------- */
@@ -531,8 +532,8 @@ typedef struct tcl_ssm_scan_args {
   int32_t dtype;         /* tcl_dtype                                        */
   int32_t n_seq, rows;   /* sequences; rows of the activations               */
   int32_t E, N;          /* channels, states per channel                     */
-  int32_t L;             /* no sequence is longer (with d_offs; it sizes the
-                            workspace, and decides how sequences are cut)    */
+  int32_t L;             /* no sequence is longer (with d_offs): it sizes the
+                            workspace and decides how sequences are cut      */
   const int32_t* d_offs; /* [n_seq + 1] or NULL                              */
   const void* d_u;       /* [rows, E], leading dimension ldu                 */
   int64_t ldu;
@@ -553,8 +554,7 @@ typedef struct tcl_ssm_scan_args {
 /* d_y [rows, E] with leading dimension ldy; d_state_out [n_slots, E, N] or NULL; both
  * pools 16-byte aligned. d_workspace: >= tcl_ssm_scan_workspace_bytes bytes, 256-byte
  * aligned; that is 0 (and d_workspace may be NULL) for batches of short or many sequences, and
- * for single tokens (L = 1). Sequences longer than L give wrong results for
- * themselves, and reach no memory that is not theirs. */
+ * for single tokens (L = 1). */
 TCL_API size_t tcl_ssm_scan_workspace_bytes(int32_t n_seq, int32_t rows, int32_t E, int32_t N, int32_t L);
 TCL_API tcl_status tcl_ssm_scan(const tcl_ssm_scan_args* args, const int32_t* d_slots, int32_t n_slots,
                                 float* d_state_out, void* d_y, int64_t ldy, void* d_workspace, size_t ws_bytes,
@@ -576,11 +576,13 @@ typedef struct tcl_ssm_scan_grads {
   float* d_dA_log;  /* [E, N] */
   float* d_dD;      /* [E] or NULL (not wanted) */
   float* d_db_dt;   /* [E] or NULL (not wanted) */
-  float* d_dstate;  /* [n_seq, E, N] gradient of the states at the start, or NULL */
+  float* d_dstate;  /* [n_seq, E, N] gradient of the states at the start,
+                       or NULL; like d_dstate_out 16-byte aligned */
 } tcl_ssm_scan_grads;
 
 /* Gradients of the scan from its inputs and d_dy [rows, E] (lddy); nothing is kept from
- * the forward call. d_dstate_out [n_seq, E, N]: the gradient of the end states (NULL:
+ * the forward call. A sequence longer than L gets wrong gradients (and so do the parameters), and
+ * reaches no memory that is not its own. d_dstate_out [n_seq, E, N]: the gradient of the end states (NULL:
  * zeros). State i belongs to sequence i (no slots). d_workspace: >=
  * tcl_ssm_scan_backward_workspace_bytes bytes, 256-byte aligned. */
 TCL_API size_t tcl_ssm_scan_backward_workspace_bytes(int32_t n_seq, int32_t rows, int32_t E, int32_t N, int32_t L);

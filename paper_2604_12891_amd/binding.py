@@ -536,10 +536,34 @@ def _adr(t) -> int:
     return 0 if t is None else t.data_ptr()
 
 
-def _stream_of(stream, t) -> int:
-    """The caller's stream, or the current one of t's device (the current device)."""
+def _stream_of(t) -> int:
+    """The current stream of t's device (the current device)."""
     import torch
-    return (torch.cuda.current_stream(t.get_device()) if stream is None else stream).cuda_stream
+    return torch.cuda.current_stream(t.get_device()).cuda_stream
+
+
+def _under(stream, call, *args, **kw):
+    """call under another stream than the current one: what it allocates (results, a workspace)
+    then belongs to that stream and is not given to others while its kernels run."""
+    import torch
+    with torch.cuda.stream(stream):
+        return call(*args, **kw)
+
+
+def _results(new, out, like):
+    """new's tensors (name: shape, type, rows of a leading dimension or not), out's where it has them."""
+    import torch
+    r = {}
+    for name, spec in new.items():
+        t = None if out is None else out.get(name)
+        if spec is None:
+            r[name] = None
+        elif t is None:
+            r[name] = torch.empty(spec[0], dtype=spec[1], device=like.device)
+        else:
+            _expect(name, t, spec[1], spec[0], like, rows=spec[2])
+            r[name] = t
+    return r
 
 
 def _on_device(t):
@@ -608,6 +632,8 @@ def ssm_conv(x, w, b=None, offs=None, state=None, state_out=None, slots=None, ou
     offs int32 [n_seq + 1]: packed sequences; None: each row is one token of its own
     sequence. state / state_out [n, K-1, E] of x's type (may be the same tensor)
     with slots int32 [n_seq] into them. Returns u [rows, E]."""
+    if stream is not None:
+        return _under(stream, ssm_conv, x, w, b, offs, state, state_out, slots, out)
     import torch
     n_seq = _sequences(x, offs)
     n_slots = _pools(state, state_out, slots, n_seq, (w.shape[1] - 1, x.shape[1]), x.dtype, x)
@@ -617,7 +643,7 @@ def ssm_conv(x, w, b=None, offs=None, state=None, state_out=None, slots=None, ou
         _expect("out", out, x.dtype, x.shape, x, rows=True)
     a = _conv_args(x, w, b, offs, n_seq, state)
     check(lib().tcl_ssm_conv(a, _ptr(slots), n_slots, _ptr(state_out), out.data_ptr(), _ld(out),
-                             _stream_of(stream, x)))
+                             _stream_of(x)))
     return out
 
 
@@ -627,10 +653,13 @@ def ssm_conv_workspace(n_seq, rows, E, K):
     return torch.empty(lib().tcl_ssm_conv_workspace_bytes(n_seq, rows, E, K), dtype=torch.uint8, device="cuda")
 
 
-def ssm_conv_backward(x, w, b, du, offs=None, state=None, state_grad=None, workspace=None, stream=None):
+def ssm_conv_backward(x, w, b, du, offs=None, state=None, state_grad=None, workspace=None, out=None, stream=None):
     """Gradients of ssm_conv (tcl_ssm_conv_backward) from du [rows, E] and, for carried
     states [n_seq, K-1, E], the gradient state_grad of the end states. Returns a
-    dict of dx, dw, db and dstate (None without a state)."""
+    dict of dx, dw, db and dstate (None without a state); out: tensors of those names to write to.
+    Rows of dx that no sequence owns are left as they are (in a new tensor: undefined)."""
+    if stream is not None:
+        return _under(stream, ssm_conv_backward, x, w, b, du, offs, state, state_grad, workspace, out)
     import torch
     n_seq = _sequences(x, offs)
     K = w.shape[1]
@@ -638,13 +667,12 @@ def ssm_conv_backward(x, w, b, du, offs=None, state=None, state_grad=None, works
         _expect(name, t, x.dtype, (n_seq, K - 1, x.shape[1]), x)
     _expect("du", du, x.dtype, x.shape, x, rows=True)
     a = _conv_args(x, w, b, offs, n_seq, state)
-    r = dict(dx=torch.empty(x.shape, dtype=x.dtype, device=x.device), dw=torch.empty_like(w),
-             db=torch.empty(x.shape[1], dtype=torch.float32, device=x.device),
-             dstate=None if state is None else torch.empty_like(state))
+    r = _results(dict(dx=(x.shape, x.dtype, True), dw=(w.shape, w.dtype, False), db=(x.shape[1:], w.dtype, False),
+                      dstate=None if state is None else (state.shape, x.dtype, False)), out, x)
     ws = _workspace(lib().tcl_ssm_conv_workspace_bytes(n_seq, x.shape[0], x.shape[1], K), workspace, x)
     check(lib().tcl_ssm_conv_backward(a, du.data_ptr(), _ld(du), _ptr(state_grad), r["dx"].data_ptr(),
                                       _ld(r["dx"]), r["dw"].data_ptr(), r["db"].data_ptr(), _ptr(r["dstate"]),
-                                      *_ws_args(ws), _stream_of(stream, x)))
+                                      *_ws_args(ws), _stream_of(x)))
     return r
 
 
@@ -681,6 +709,8 @@ def ssm_scan(u, dt, A_log, B, C, D=None, z=None, b_dt=None, offs=None, L=None, s
     and B, C [rows, N] fp32 or bf16, A_log [E, N], D, b_dt [E] and the states
     [n, E, N] fp32. offs, slots as for ssm_conv; L bounds the sequences' lengths (None:
     rows). Returns y [rows, E]."""
+    if stream is not None:
+        return _under(stream, ssm_scan, u, dt, A_log, B, C, D, z, b_dt, offs, L, state, state_out, slots, out, workspace)
     import torch
     n_seq = _sequences(u, offs)
     n_slots = _pools(state, state_out, slots, n_seq, A_log.shape, torch.float32, u)
@@ -692,16 +722,20 @@ def ssm_scan(u, dt, A_log, B, C, D=None, z=None, b_dt=None, offs=None, L=None, s
     need = 0 if offs is None else lib().tcl_ssm_scan_workspace_bytes(n_seq, *u.shape, A_log.shape[1], L)
     ws = _workspace(need, workspace, u)
     check(lib().tcl_ssm_scan(a, _ptr(slots), n_slots, _ptr(state_out), out.data_ptr(), _ld(out),
-                             *_ws_args(ws), _stream_of(stream, u)))
+                             *_ws_args(ws), _stream_of(u)))
     return out
 
 
 def ssm_scan_backward(u, dt, A_log, B, C, dy, D=None, z=None, b_dt=None, offs=None, L=None, state=None,
-                      state_grad=None, workspace=None, stream=None):
+                      state_grad=None, workspace=None, out=None, stream=None):
     """Gradients of ssm_scan (tcl_ssm_scan_backward) from dy [rows, E] and, for carried
     states [n_seq, E, N], the gradient state_grad of the end states. Returns a dict of
     du, ddt, dB, dC, dz (None without z), dA_log, dD, db_dt and dstate (None without a
-    state)."""
+    state); out: tensors of those names to write to. Rows of the activations' gradients that no sequence
+    owns are left as they are (in a new tensor: undefined)."""
+    if stream is not None:
+        return _under(stream, ssm_scan_backward, u, dt, A_log, B, C, dy, D, z, b_dt, offs, L, state, state_grad,
+                      workspace, out)
     import torch
     n_seq = _sequences(u, offs)
     for name, t in (("state", state), ("state_grad", state_grad)):
@@ -709,19 +743,18 @@ def ssm_scan_backward(u, dt, A_log, B, C, dy, D=None, z=None, b_dt=None, offs=No
     _expect("dy", dy, u.dtype, u.shape, u, rows=True)
     L, a = _scan_args(u, dt, A_log, B, C, D, z, b_dt, offs, n_seq, L, state)
 
-    def new(*shape, dtype=u.dtype):
-        return torch.empty(shape, dtype=dtype, device=u.device)
-
-    (rows, E), N, f32 = u.shape, A_log.shape[1], torch.float32
-    r = dict(du=new(rows, E), ddt=new(rows, E), dz=None if z is None else new(rows, E), dB=new(rows, N),
-             dC=new(rows, N), dA_log=new(E, N, dtype=f32), dD=new(E, dtype=f32), db_dt=new(E, dtype=f32),
-             dstate=None if state is None else new(n_seq, E, N, dtype=f32))
-    g = _PACK_GRADS.pack(r["du"].data_ptr(), E, r["ddt"].data_ptr(), E, r["dB"].data_ptr(), N, r["dC"].data_ptr(), N,
-                         _adr(r["dz"]), E, r["dA_log"].data_ptr(), r["dD"].data_ptr(), r["db_dt"].data_ptr(),
-                         _adr(r["dstate"]))
+    (rows, E), N, dt_, f32 = u.shape, A_log.shape[1], u.dtype, torch.float32
+    act, vec = ((rows, E), dt_, True), ((E,), f32, False)
+    r = _results(dict(du=act, ddt=act, dz=None if z is None else act, dB=((rows, N), dt_, True),
+                      dC=((rows, N), dt_, True), dA_log=((E, N), f32, False), dD=vec, db_dt=vec,
+                      dstate=None if state is None else ((n_seq, E, N), f32, False)), out, u)
+    g = _PACK_GRADS.pack(r["du"].data_ptr(), _ld(r["du"]), r["ddt"].data_ptr(), _ld(r["ddt"]), r["dB"].data_ptr(),
+                         _ld(r["dB"]), r["dC"].data_ptr(), _ld(r["dC"]), _adr(r["dz"]),
+                         0 if z is None else _ld(r["dz"]), r["dA_log"].data_ptr(), r["dD"].data_ptr(),
+                         r["db_dt"].data_ptr(), _adr(r["dstate"]))
     ws = _workspace(lib().tcl_ssm_scan_backward_workspace_bytes(n_seq, rows, E, N, L), workspace, u)
     check(lib().tcl_ssm_scan_backward(a, dy.data_ptr(), _ld(dy), _ptr(state_grad), g,
-                                      *_ws_args(ws), _stream_of(stream, u)))
+                                      *_ws_args(ws), _stream_of(u)))
     return r
 
 
@@ -755,6 +788,8 @@ def logprobs(logits, tokens=None, K=0, temperature=1.0, seg_offsets=None, max_le
     (segments of max_len entries at most; indices then count from the array's start, as
     topk's do); tokens int32 [rows]. Returns a dict of logp (None without tokens), entropy,
     top [rows, K] int32 and top_logp [rows, K] (None for K = 0)."""
+    if stream is not None:
+        return _under(stream, logprobs, logits, tokens, K, temperature, seg_offsets, max_len, workspace)
     import torch
     n, V, ld = _logit_rows(logits, seg_offsets, max_len)
     _expect("tokens", tokens, torch.int32, (n,), logits)
@@ -767,7 +802,7 @@ def logprobs(logits, tokens=None, K=0, temperature=1.0, seg_offsets=None, max_le
     ws = _workspace(lib().tcl_logits_workspace_bytes(n, V, K), workspace, logits)
     check(lib().tcl_logprobs(_dtype(logits), n, V, logits.data_ptr(), ld, _ptr(seg_offsets), temperature,
                              _ptr(tokens), K, _ptr(r["logp"]), r["entropy"].data_ptr(), _ptr(r["top"]),
-                             _ptr(r["top_logp"]), *_ws_args(ws), _stream_of(stream, logits)))
+                             _ptr(r["top_logp"]), *_ws_args(ws), _stream_of(logits)))
     return r
 
 
@@ -778,6 +813,9 @@ def distill_topk(logits, top, teacher, weight=None, temperature=1.0, seg_offsets
     gradient's factor of each row). grad: True (a new tensor), False (the loss
     alone), or the tensor that takes it, which may be logits itself. Returns a dict
     of loss [rows] fp32 and grad (None if not wanted)."""
+    if stream is not None:
+        return _under(stream, distill_topk, logits, top, teacher, weight, temperature, seg_offsets, max_len, grad,
+                      workspace)
     import torch
     n, V, ld = _logit_rows(logits, seg_offsets, max_len)
     if top.dim() != 2:
@@ -796,7 +834,7 @@ def distill_topk(logits, top, teacher, weight=None, temperature=1.0, seg_offsets
     ws = _workspace(lib().tcl_logits_workspace_bytes(n, V, K), workspace, logits)
     check(lib().tcl_distill_topk(_dtype(logits), n, V, logits.data_ptr(), ld, _ptr(seg_offsets), temperature, K,
                                  top.data_ptr(), teacher.data_ptr(), _ptr(weight), loss.data_ptr(), _ptr(grad), ldg,
-                                 *_ws_args(ws), _stream_of(stream, logits)))
+                                 *_ws_args(ws), _stream_of(logits)))
     return dict(loss=loss, grad=grad)
 
 

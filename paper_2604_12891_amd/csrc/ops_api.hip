@@ -11,7 +11,8 @@ namespace {
 
 bool misaligned(const void* p, uintptr_t n) { return reinterpret_cast<uintptr_t>(p) % n != 0; }
 
-// A grid of tiles x channel groups has to fit in 31 bits.
+// Row and tile indices, and grids of tiles x channel groups, have to fit in 31 bits.
+constexpr int kMaxRows = 1 << 30;
 constexpr int64_t kMaxWork = (int64_t)1 << 36;
 
 tcl_status check_workspace(const void* d_ws, size_t have, size_t need) {
@@ -28,7 +29,8 @@ tcl_status check_sequences(int32_t dtype, int32_t n_seq, int32_t rows, int32_t E
   if (!d_offs && rows != n_seq)
     return fail(TCL_ERR_INVALID_ARG, "without d_offs every sequence is one row (n_seq=%d rows=%d)", n_seq, rows);
   if (E < 1 || E > 65536) return fail(TCL_ERR_UNSUPPORTED, "E must be in [1, 65536] (got %d)", E);
-  if (((int64_t)n_seq + rows) * E > kMaxWork) return fail(TCL_ERR_UNSUPPORTED, "too many rows x channels");
+  if (n_seq > kMaxRows || rows > kMaxRows || ((int64_t)n_seq + rows) * E > kMaxWork)
+    return fail(TCL_ERR_UNSUPPORTED, "too many rows x channels");
   return TCL_OK;
 }
 
@@ -174,6 +176,8 @@ TCL_API tcl_status tcl_ssm_scan_backward(const tcl_ssm_scan_args* args, const vo
     return fail(TCL_ERR_INVALID_ARG, "NULL device pointer");
   if (op.rows > 0 && (op.z != nullptr) != (g->d_dz != nullptr))
     return fail(TCL_ERR_INVALID_ARG, "d_dz goes with d_z");
+  if (misaligned(d_dstate_out, 16) || misaligned(g->d_dstate, 16))
+    return fail(TCL_ERR_INVALID_ARG, "the states' gradients must be 16-byte aligned");
   if (op.n_seq == 0) return fail(TCL_ERR_INVALID_ARG, "no sequences to take gradients of");
   op.n_slots = op.n_seq;
   const size_t need = ssm_scan_bwd_workspace_bytes(op.n_seq, op.rows, op.E, op.N, op.L);

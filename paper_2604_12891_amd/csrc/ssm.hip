@@ -743,8 +743,8 @@ __global__ __launch_bounds__(256) void ssm_scan_token_kernel(ScanIn a, const T* 
                                                              const T* __restrict__ C, const T* __restrict__ z,
                                                              float* state_out, T* __restrict__ y, int64_t ldy) {
   constexpr int Q = N / 4;
-  const int E = a.E;
-  const int e = blockIdx.x * (256 / Q) + threadIdx.x / Q, n0 = (threadIdx.x % Q) * 4;
+  const int E = a.E, groups = (E + 256 / Q - 1) / (256 / Q), first = blockIdx.x / groups * SB;
+  const int e = blockIdx.x % groups * (256 / Q) + threadIdx.x / Q, n0 = (threadIdx.x % Q) * 4;
   const bool active = e < E;
   const int ec = active ? e : E - 1;
   const floatx4 al = *reinterpret_cast<const floatx4*>(a.A_log + (int64_t)ec * N + n0);
@@ -754,7 +754,7 @@ __global__ __launch_bounds__(256) void ssm_scan_token_kernel(ScanIn a, const T* 
   int sl[SB];
 #pragma unroll
   for (int i = 0; i < SB; ++i) {
-    const int q = min((int)blockIdx.y * SB + i, a.n_seq - 1);
+    const int q = min(first + i, a.n_seq - 1);
     sl[i] = slot_of(a.slots, a.n_slots, q);
     s[i] = floatx4{0.f, 0.f, 0.f, 0.f};
     if (a.state && sl[i] >= 0)
@@ -773,7 +773,7 @@ __global__ __launch_bounds__(256) void ssm_scan_token_kernel(ScanIn a, const T* 
   for (int n = 0; n < 4; ++n) a2[n] = decay_rate(al[n]);
 #pragma unroll
   for (int i = 0; i < SB; ++i) {
-    const int q = blockIdx.y * SB + i;
+    const int q = first + i;
     const float uv = to_f32(ur[i]), d = softplus(to_f32(dr[i]) + bias), du = d * uv;
     float acc = 0.f;
 #pragma unroll
@@ -1260,10 +1260,10 @@ hipError_t scan_fwd(const ScanOp& a, float* state_out, void* y_, int64_t ldy, fl
     const unsigned gx = (a.E + 1024 / N - 1) / (1024 / N);
     constexpr int SB = 4;
     if ((int64_t)gx * a.n_seq >= (int64_t)kCUs * 4 * SB)
-      ssm_scan_token_kernel<T, N, SB><<<dim3(gx, (a.n_seq + SB - 1) / SB), 256, 0, s>>>(in, u, dt, B, C, z, state_out,
-                                                                                       y, ldy);
+      ssm_scan_token_kernel<T, N, SB><<<dim3(gx * ((a.n_seq + SB - 1) / SB)), 256, 0, s>>>(in, u, dt, B, C, z,
+                                                                                          state_out, y, ldy);
     else
-      ssm_scan_token_kernel<T, N, 1><<<dim3(gx, a.n_seq), 256, 0, s>>>(in, u, dt, B, C, z, state_out, y, ldy);
+      ssm_scan_token_kernel<T, N, 1><<<dim3(gx * a.n_seq), 256, 0, s>>>(in, u, dt, B, C, z, state_out, y, ldy);
     return hipGetLastError();
   }
   const int CG = (a.E + 63) / 64, CL = scan_chunk(a.n_seq, a.E, a.L);
@@ -1337,7 +1337,7 @@ hipError_t scan_bwd(const ScanOp& a, const void* dy_, int64_t lddy, const float*
       part, bc);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
-  if (bc) {
+  if (bc && a.rows > 0) {
     const int64_t n = (int64_t)a.rows * 2 * N;
     ssm_sum_bc_kernel<T, N><<<dim3((unsigned)((n + 255) / 256)), 256, 0, s>>>(
         a.offs, a.n_seq, a.rows, p.CG, bc, static_cast<T*>(g.dB), g.lddB, static_cast<T*>(g.dC), g.lddC);
@@ -1351,8 +1351,7 @@ hipError_t scan_bwd(const ScanOp& a, const void* dy_, int64_t lddy, const float*
 }  // namespace
 
 hipError_t launch_ssm_conv(const ConvOp& a, void* state_out, void* u, int64_t ldu, hipStream_t s) {
-  const int ch = a.bf16 ? 8 : 4;
-  const bool vec = a.E % ch == 0 && a.ldx % ch == 0 && ldu % ch == 0 && aligned16(a.x) && aligned16(u) &&
+  const bool vec = a.E % 4 == 0 && a.ldx % 4 == 0 && ldu % 4 == 0 && aligned16(a.x) && aligned16(u) &&
                    aligned16(a.state) && aligned16(state_out);
 #define TCL_CONV(KK)                                                                                       \
   case KK:                                                                                                 \

@@ -122,6 +122,22 @@ def test_scan_call_refusals(lib):
     assert lib.tcl_ssm_scan_backward(ctypes.byref(a), FAKE, 64, None, None, FAKE, need, None) == -1
 
 
+def test_scan_backward_refuses_misaligned_state_gradients(lib):
+    a = _scan(n_seq=2, rows=20, L=20, d_state=FAKE)
+    for dend, dstate in ((FAKE + 4, None), (None, FAKE + 8)):
+        g = tb.SsmScanGrads(*[FAKE, 64] * 5, FAKE, None, None, dstate)
+        assert lib.tcl_ssm_scan_backward(ctypes.byref(a), FAKE, 64, dend, ctypes.byref(g), FAKE, 1 << 40, None) == -1
+        assert b"aligned" in lib.tcl_last_error()
+
+
+def test_more_rows_than_indices_hold(lib):
+    for kw in (dict(rows=(1 << 30) + 1), dict(n_seq=(1 << 30) + 1)):
+        a = _scan(E=1, ldu=1, lddt=1, ldz=1, **kw)
+        assert lib.tcl_ssm_scan(ctypes.byref(a), None, 1 << 30, None, FAKE, 1, FAKE, 1 << 40, None) == -2
+        c = _conv(E=1, ldx=1, **kw)
+        assert lib.tcl_ssm_conv(ctypes.byref(c), None, 1 << 30, None, FAKE, 1, None) == -2
+
+
 def test_logit_refusals(lib):
     ok = dict(dtype=0, n=4, V=5000, x=FAKE, ld=5000, offs=None, temp=1.0, tok=FAKE, K=8, lp=FAKE, en=FAKE, top=FAKE,
               tl=FAKE, ws=FAKE, bytes=1 << 40, stream=None)

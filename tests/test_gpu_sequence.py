@@ -416,3 +416,96 @@ def test_far_rows():
     end = torch.empty_like(start)
     assert torch.equal(y, tb.ssm_scan(state_out=end, **dict(t, state=start)))
     assert torch.equal(pool[at.long()], end)
+
+
+def test_empty_sequences_alone():
+    """Nothing but empty sequences, wider than one workgroup's channels: states and their
+    gradients pass through, the parameters' gradients are zero."""
+    tb, E, N, n = _tb(), 600, 16, 3
+    none = torch.empty(0, E, device="cuda")
+    bc = torch.empty(0, N, device="cuda")
+    offs = torch.zeros(n + 1, dtype=torch.int32, device="cuda")
+    A, st, ge = torch.zeros(E, N, device="cuda"), torch.randn(n, E, N, device="cuda"), torch.randn(n, E, N, device="cuda")
+    end = torch.empty_like(st)
+    assert tb.ssm_scan(none, none, A, bc, bc, offs=offs, state=st, state_out=end).shape == (0, E)
+    assert torch.equal(end, st)
+    g = tb.ssm_scan_backward(none, none, A, bc, bc, none, offs=offs, state=st, state_grad=ge)
+    assert torch.equal(g["dstate"], ge) and not g["dA_log"].any() and not g["dD"].any() and not g["db_dt"].any()
+    w, cs, cg = torch.randn(E, 4, device="cuda"), torch.randn(n, 3, E, device="cuda"), torch.randn(n, 3, E, device="cuda")
+    ce = torch.empty_like(cs)
+    tb.ssm_conv(none, w, offs=offs, state=cs, state_out=ce)
+    assert torch.equal(ce, cs)
+    g = tb.ssm_conv_backward(none, w, None, none, offs=offs, state=cs, state_grad=cg)
+    assert torch.equal(g["dstate"], cg) and not g["dw"].any() and not g["db"].any()
+    nobody = torch.zeros(1, dtype=torch.int32, device="cuda")
+    assert tb.ssm_scan(none, none, A, bc, bc, offs=nobody).shape == (0, E)
+    assert tb.ssm_conv(none, w).shape == (0, E)
+
+
+def test_more_tokens_than_a_grid_dimension():
+    """Single tokens of more sequences than 4 x 65,535."""
+    tb, E, N, n = _tb(), 8, 8, 270_001
+    u, dt, B, C = (torch.randn(n, k, device="cuda") for k in (E, E, N, N))
+    A = torch.zeros(E, N, device="cuda")
+    end = torch.full((n, E, N), NAN, device="cuda")
+    y = tb.ssm_scan(u, dt, A, B, C, state_out=end)
+    d = torch.nn.functional.softplus(dt.double())
+    s = (d * u.double())[:, :, None] * B.double()[:, None, :]
+    # softplus within EPS_ACT, two products
+    assert ((end.double() - s).abs() <= (osq.EPS_ACT + 3 * osq.EPS) * s.abs() + 1e-37).all()
+    ref = (s * C.double()[:, None, :]).sum(-1)
+    size = (s * C.double()[:, None, :]).abs().sum(-1)
+    assert ((y.double() - ref).abs() <= (osq.EPS_ACT + (N + 4) * osq.EPS) * size + 1e-37).all()
+
+
+def test_gradients_into_the_callers_tensors():
+    """Rows that no sequence owns stay as they were in tensors the caller gives, wide ones among them."""
+    tb, E, N, lens = _tb(), 70, 16, [33, 5]
+    T, rows = 38, 44
+    a = _scan_case(lens, E, N, "f32", 61)
+    k = _scan_tensors(a, "f32", rows)
+    offs = _cuda(_offs(lens), torch.int32)
+    dy = _rows(np.ones((T, E)), torch.float32, rows)
+    want = tb.ssm_scan_backward(dy=dy, offs=offs, L=33, **k)
+    wide = torch.full((rows, 100), 7.0, device="cuda")
+    out = dict(du=wide[:, :E], ddt=torch.zeros(rows, E, device="cuda"), dB=torch.zeros(rows, N, device="cuda"))
+    got = tb.ssm_scan_backward(dy=dy, offs=offs, L=33, out=out, **k)
+    assert got["du"] is out["du"] and (wide[T:] == 7.0).all() and (wide[:, E:] == 7.0).all()
+    assert not out["ddt"][T:].any() and not out["dB"][T:].any()
+    for name in want:
+        part = slice(0, T) if name in ("du", "ddt", "dz", "dB", "dC") else slice(None)
+        assert torch.equal(got[name][part], want[name][part]), name
+    w = torch.randn(E, 4, device="cuda")
+    x, du = k["u"], _rows(np.ones((T, E)), torch.float32, rows)
+    dx = torch.full((rows, E), 7.0, device="cuda")
+    g = tb.ssm_conv_backward(x, w, None, du, offs=offs, out=dict(dx=dx))
+    assert g["dx"] is dx and (dx[T:] == 7.0).all() and torch.isfinite(g["dw"]).all()
+    with pytest.raises(ValueError, match="dx"):
+        tb.ssm_conv_backward(x, w, None, du, offs=offs, out=dict(dx=dx[:, :3]))
+
+
+def test_on_a_stream_of_its_own():
+    """Under a given stream results and workspaces belong to that stream: calls there with work
+    and allocations on the current stream in between give what they give alone."""
+    tb, E, N, lens = _tb(), 256, 16, [700, 300]
+    T, offs = 1000, _cuda(_offs([700, 300]), torch.int32)
+    k = _scan_tensors(_scan_case(lens, E, N, "f32", 71), "f32", T)
+    dy = torch.randn(T, E, device="cuda")
+    w = torch.randn(E, 4, device="cuda")
+    y0 = tb.ssm_scan(offs=offs, L=700, **k)
+    g0 = tb.ssm_scan_backward(dy=dy, offs=offs, L=700, **k)
+    c0 = tb.ssm_conv_backward(k["u"], w, None, dy, offs=offs)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    for _ in range(3):
+        side.wait_stream(torch.cuda.current_stream())
+        y = tb.ssm_scan(offs=offs, L=700, stream=side, **k)
+        g = tb.ssm_scan_backward(dy=dy, offs=offs, L=700, stream=side, **k)
+        c = tb.ssm_conv_backward(k["u"], w, None, dy, offs=offs, stream=side)
+        noise = [torch.full((1 << 20,), NAN, device="cuda") for _ in range(8)]
+        torch.cuda.current_stream().wait_stream(side)
+        assert torch.equal(y, y0)
+        for a, b in ((g, g0), (c, c0)):
+            for name in b:
+                assert b[name] is None or torch.equal(a[name], b[name]), name
+        del noise
