@@ -540,13 +540,27 @@ __device__ __forceinline__ float teacher_loss(const TeacherShared& sh, int K, fl
   return loss;
 }
 
+// Whether an entry of the list stands at another one's place, as far as this thread looks: the pairs
+// are shared out over the workgroup.
+template <int TB>
+__device__ __forceinline__ bool teacher_twice(const TeacherShared& sh, int K) {
+  const int slices = max(TB / K, 1), s = (int)threadIdx.x / K;
+  bool twice = false;
+  if (s < slices)
+    for (int k = threadIdx.x - s * K; k < K; k += TB) {
+      const int at = sh.at[k];
+      for (int j = s; j < k; j += slices) twice |= at >= 0 && sh.at[j] == at;
+    }
+  return twice;
+}
 // Entry k of the list, if it is the first of its place: all the teacher's
-// probability there, by a loop over the list.
-__device__ __forceinline__ bool teacher_place(const TeacherShared& sh, int K, int k, float& q) {
+// probability there. `twice`: there are entries at the place of others.
+__device__ __forceinline__ bool teacher_place(const TeacherShared& sh, int K, int k, bool twice, float& q) {
   const int at = sh.at[k];
   bool first = at >= 0;
+  q = sh.q[k];
+  if (!twice) return first;
   q = 0.f;
-#pragma unroll 8
   for (int j = 0; j < K; ++j) {
     const bool same = sh.at[j] == at;
     if (same) q += sh.q[j];
@@ -598,7 +612,9 @@ __global__ __launch_bounds__(64 * NW) void distill_row_kernel(LogitRows a, Teach
   constexpr int VE = Row<T>::VE, TB = 64 * NW;
   extern __shared__ __attribute__((aligned(16))) float teacher_mem[];
   __shared__ float red[3][32];
+  __shared__ int twice;
   TeacherShared sh(teacher_mem, t.K);
+  if (threadIdx.x == 0) twice = 0;
   const int r = blockIdx.x, tid = threadIdx.x;
   const Row<T> row(a, r);
   const ScaledExp<T> ex(a.inv_temp);
@@ -615,7 +631,15 @@ __global__ __launch_bounds__(64 * NW) void distill_row_kernel(LogitRows a, Teach
   for (int k = 0; k < NV; ++k)
     if (tid + k * TB < row.nvec) vmax(x[k]);
   for (int v = tid + NV * TB; v < row.nvec; v += TB) vmax(row.load(v));
+  // Between the passes the logits are opaque: else the compiler holds what one pass made of them (widened
+  // values, differences, exponentials) for the next, beside them, up to 1 KB of spills per lane.
+  auto hold = [&]() {
+#pragma unroll
+    for (int k = 0; k < NV; ++k) asm volatile("" : "+v"(x[k]));
+  };
   block_reduce<NW, true>(m, mt, red[0]);
+  if (NW < 16) hold();  // (at 1,024 threads the 128 registers do without it, and spill with it)
+  if (t.grad && teacher_twice<TB>(sh, t.K)) twice = 1;
   if (!(m > -INFINITY)) m = 0.f;  // nothing but -inf (a sum of 0) or NaN (a sum of NaN)
   float s = 0.f, qs = teacher_sum<NW>(sh, t.K, mt);
   auto vsum = [&](u32x4 v) {
@@ -628,10 +652,7 @@ __global__ __launch_bounds__(64 * NW) void distill_row_kernel(LogitRows a, Teach
   for (int v = tid + NV * TB; v < row.nvec; v += TB) vsum(row.load(v));
   block_reduce<NW, false>(s, qs, red[1]);
   const bool live = mt > -INFINITY && s != 0.f;
-  // (else the compiler holds all the differences and exponentials from here to the
-  // gradient, beside the logits: 1 KB of spills per lane in fp32)
-#pragma unroll
-  for (int k = 0; k < NV; ++k) asm volatile("" : "+v"(x[k]));
+  hold();
   float loss = teacher_loss<NW>(sh, t.K, mt, logf(qs), m, logf(s), a.inv_temp), none = 0.f;
   block_reduce<NW, false>(loss, none, red[2]);
   if (tid == 0) t.loss[r] = live ? loss : 0.f;
@@ -648,7 +669,7 @@ __global__ __launch_bounds__(64 * NW) void distill_row_kernel(LogitRows a, Teach
   __syncthreads();  // the entries below are written after the ones above
   for (int k = tid; k < t.K; k += TB) {
     float q;
-    if (teacher_place(sh, t.K, k, q)) st_grad(g + sh.at[k], f(sh.x[k]) - w * q);
+    if (teacher_place(sh, t.K, k, twice != 0, q)) st_grad(g + sh.at[k], f(sh.x[k]) - w * q);
   }
 }
 
@@ -712,7 +733,9 @@ __global__ __launch_bounds__(kTB) void distill_grad_kernel(LogitRows a, TeacherA
   constexpr int VE = Row<T>::VE, NW = kTB / 64;
   extern __shared__ __attribute__((aligned(16))) float teacher_mem[];
   __shared__ float red[3][32];
+  __shared__ int twice;
   TeacherShared sh(teacher_mem, t.K);
+  if (threadIdx.x == 0) twice = 0;
   const int r = blockIdx.x, tid = threadIdx.x, S = gridDim.y;
   const Row<T> row(a, r);
   const int per = (row.nvec + S - 1) / S;
@@ -727,6 +750,7 @@ __global__ __launch_bounds__(kTB) void distill_grad_kernel(LogitRows a, TeacherA
   }
   if (!(m > -INFINITY)) m = 0.f;
   block_reduce<NW, true>(mt, none, red[0]);
+  if (t.grad && teacher_twice<kTB>(sh, t.K)) twice = 1;
   const bool live = mt > -INFINITY && s != 0.f;
   float qs = teacher_sum<NW>(sh, t.K, mt);
   block_reduce<NW, false>(qs, none, red[1]);
@@ -744,7 +768,7 @@ __global__ __launch_bounds__(kTB) void distill_grad_kernel(LogitRows a, TeacherA
   const int lo = v0 * VE - row.h, hi = v1 * VE - row.h;  // the entries of this part
   for (int k = tid; k < t.K; k += kTB) {
     float q;
-    if (sh.at[k] >= lo && sh.at[k] < hi && teacher_place(sh, t.K, k, q))
+    if (sh.at[k] >= lo && sh.at[k] < hi && teacher_place(sh, t.K, k, twice != 0, q))
       st_grad(g + sh.at[k], f(sh.x[k]) - w * q);
   }
 }
@@ -788,7 +812,7 @@ hipError_t distill(const LogitRows& a, const TeacherArgs& t, char* ws, hipStream
   if (vecs <= 64 * 4) distill_row_kernel<T, 1, 4><<<dim3(a.n), 64, 12 * t.K, s>>>(a, t);
   else if (vecs <= 256 * 4) distill_row_kernel<T, 4, 4><<<dim3(a.n), 256, 12 * t.K, s>>>(a, t);
   else if (vecs <= 512 * 8) distill_row_kernel<T, 8, 8><<<dim3(a.n), 512, 12 * t.K, s>>>(a, t);
-  else if (vecs <= 1024 * 8) distill_row_kernel<T, 16, 8><<<dim3(a.n), 1024, 12 * t.K, s>>>(a, t);
+  else if (vecs <= 512 * 16) distill_row_kernel<T, 8, 16><<<dim3(a.n), 512, 12 * t.K, s>>>(a, t);
   else distill_row_kernel<T, 16, 16><<<dim3(a.n), 1024, 12 * t.K, s>>>(a, t);
   return hipGetLastError();
 }

@@ -394,13 +394,14 @@ __global__ __launch_bounds__(64 * kSumLanes) void sum_parts_kernel(const float* 
   float acc = 0.f;
   if (i < stride) {
     const float* src = part + i;
-    int p = g;
-    for (; p + 3 * kSumLanes < parts; p += 4 * kSumLanes) {
-      const float a = src[p * stride], b = src[(p + kSumLanes) * stride], c = src[(p + 2 * kSumLanes) * stride],
-                  d = src[(p + 3 * kSumLanes) * stride];
-      acc += (a + b) + (c + d);
+    constexpr int U = 16;  // loads in flight: a trip is one latency
+    for (int p = g; p < parts; p += U * kSumLanes) {
+      float v[U];
+#pragma unroll
+      for (int k = 0; k < U; ++k) v[k] = src[min(p + k * kSumLanes, parts - 1) * stride];
+#pragma unroll
+      for (int k = 0; k < U; ++k) acc += p + k * kSumLanes < parts ? v[k] : 0.f;
     }
-    for (; p < parts; p += kSumLanes) acc += src[p * stride];
   }
   red[g][lane] = acc;
   __syncthreads();
