@@ -938,22 +938,22 @@ __device__ __forceinline__ float reduce_rows(const float* v, int lane) {
   return s + dpp<0xB1>(s);  // lane ^ 1
 }
 
-// A workgroup takes one chunk of 64 nw channels, a lane per channel. The chunk's
+// A workgroup takes `per` chunks of 64 nw channels one after the other, a lane per channel. The chunk's
 // start state is walked forward once to leave the state in front of every
 // kSub tokens (but the first) in LDS; then, from the last kSub tokens to the first, the states
 // in front of each token are formed again into registers and the tokens walked
 // backwards. dB and dC of a token are sums over channels: over a wavefront by
 // swaps and DPP, over the workgroup's wavefronts through LDS, over
 // workgroups (more than 64 nw channels) by ssm_sum_bc_kernel, all in a fixed order.
-// dA_log, dD and db_dt leave as partial sums per chunk. 22 N slots per token and
+// dA_log, dD and db_dt leave as partial sums, one set per workgroup. 22 N slots per token and
 // wavefront for the states, 70 for the two sums over channels, as many for the rest.
-template <typename T, int N>
+template <typename T, int N, bool MULTI>
 __global__ __launch_bounds__(256, 2) void ssm_bwd_kernel(
     ScanIn a, const T* __restrict__ u, const T* __restrict__ dt, const T* __restrict__ B, const T* __restrict__ C,
     const T* __restrict__ z, const T* __restrict__ dy, int64_t lddy, const float* __restrict__ cst,
     const float* __restrict__ H, const float* __restrict__ dstate_out, T* __restrict__ du_o, int64_t lddu,
     T* __restrict__ ddt_o, int64_t ldddt, T* __restrict__ dz_o, int64_t lddz, T* __restrict__ dB_o, int64_t lddB,
-    T* __restrict__ dC_o, int64_t lddC, float* __restrict__ dstate, float* __restrict__ part,
+    T* __restrict__ dC_o, int64_t lddC, float* __restrict__ dstate, float* __restrict__ part, int parts, int per,
     float* __restrict__ bc_part) {
   constexpr int W = 2 * N, NSUB = kBCL / kSub;
   extern __shared__ __attribute__((aligned(16))) float smem[];
@@ -961,188 +961,194 @@ __global__ __launch_bounds__(256, 2) void ssm_bwd_kernel(
   float* sBC = smem;                                       // [kBCL][2N]
   float* sRed = smem + kBCL * W;                           // [kSub][nw][2N]
   float* sCk = sRed + kSub * nw * W + wave * (NSUB - 1) * N * 64 + lane;  // [NSUB - 1][N][64] per wavefront
-  int w, cg;
+  int p, cg;
   const int CG = (E + blockDim.x - 1) / blockDim.x;
-  if (!tile_of_block(a.ntile, CG, w, cg)) return;
+  if (!tile_of_block(parts, CG, p, cg)) return;
   const int e = cg * blockDim.x + threadIdx.x;
   const bool active = e < E;
   const int ec = active ? e : E - 1;
-  const Tile tl = find_tile(a.offs, a.n_seq, a.rows, kBCL, w);
-  float* po = part + (int64_t)w * (N + 2) * E;
-  if (tl.seq < 0) {  // the partial sums have a place for it
-    if (active)
-      for (int n = 0; n < N + 2; ++n) po[(int64_t)n * E + e] = 0.f;
-    return;
-  }
-  const int t0 = tl.j * kBCL, nt = max(0, min(tl.len - t0, kBCL));
-  const int64_t r0 = (int64_t)tl.base + t0;
-  stage_bc<T, N>(sBC, B + r0 * a.ldB, a.ldB, C + r0 * a.ldC, a.ldC, nt, threadIdx.x, blockDim.x);
   const uint32_t le = ec * sizeof(T), lf = ec * 4, ln = ec * N * 4;
   float a2[N], s[N], h[N], dA[N];
   ld_vec<N>(a.A_log, ln, a2);
 #pragma unroll
   for (int n = 0; n < N; ++n) {
     a2[n] = decay_rate(a2[n]);
-    h[n] = dA[n] = 0.f;
-  }
-  auto start = [&]() {  // the state in front of the chunk
-    if (cst) {
-#pragma unroll
-      for (int n = 0; n < N; ++n) s[n] = ld_at(cst + ((int64_t)w * N + n) * E, lf);
-    } else if (a.state) {
-      ld_vec<N>(a.state + (int64_t)tl.seq * E * N, ln, s);
-    } else {
-#pragma unroll
-      for (int n = 0; n < N; ++n) s[n] = 0.f;
-    }
-  };
-  start();
-  if (cst) {
-#pragma unroll
-    for (int n = 0; n < N; ++n) h[n] = ld_at(H + ((int64_t)w * N + n) * E, lf);
-  } else if (dstate_out) {
-    ld_vec<N>(dstate_out + (int64_t)tl.seq * E * N, ln, h);
+    dA[n] = 0.f;
   }
   const float bias = a.b_dt ? a.b_dt[ec] : 0.f, Dv = a.D ? a.D[ec] : 0.f;
   float dD = 0.f, dbias = 0.f;
-  __syncthreads();
-  const int nsub = (nt + kSub - 1) / kSub;
-  const T *us = u + r0 * a.ldu, *ds = dt + r0 * a.lddt, *zs = z ? z + r0 * a.ldz : nullptr, *gs = dy + r0 * lddy;
-  auto park = [&](int b) {  // s in front of the kSub tokens b; the first ones' place is the second ones'
-    float* ck = sCk + max(b - 1, 0) * N * 64;
-#pragma unroll
-    for (int n = 0; n < N; ++n) ck[n * 64] = s[n];
-  };
-  for (int b = 0; b < nsub - 1; ++b) {
-    if (b > 0) park(b);
-    T ru[kSub], rd[kSub];
-#pragma unroll
-    for (int i = 0; i < kSub; ++i) {  // all of these tokens exist
-      ru[i] = ld_at(us + (b * kSub + i) * a.ldu, le);
-      rd[i] = ld_at(ds + (b * kSub + i) * a.lddt, le);
-    }
-#pragma unroll
-    for (int i = 0; i < kSub; ++i) {
-      const float d = softplus(to_f32(rd[i]) + bias), du = d * to_f32(ru[i]);
-      const float* x = &sBC[(b * kSub + i) * W];
-#pragma unroll
-      for (int n = 0; n < N; ++n) s[n] = fmaf(__builtin_amdgcn_exp2f(d * a2[n]), s[n], du * x[n]);
-      __builtin_amdgcn_sched_barrier(0);
-    }
-  }
-  if (nsub > 0) park(nsub - 1);
   // what the lane holds of a token's 2N sums: dB or dC by its half, the state's parity by its
   // row, the pair of states within the row
   const int place = lane / 32 * N + lane % 16 / (32 / N) * 2 + lane / 16 % 2;
-  T cu, cd, cz, cg_;  // the token's inputs, one token ahead
-  auto load = [&](int t) {
-    const int64_t r = max(t, 0);
-    cu = ld_at(us + r * a.ldu, le);
-    cd = ld_at(ds + r * a.lddt, le);
-    cg_ = ld_at(gs + r * lddy, le);
-    if (z) cz = ld_at(zs + r * a.ldz, le);
-  };
-  if (nt > 0) load(nt - 1);
-  for (int b = nsub - 1; b >= 0; --b) {
-    if (b == 0 && nsub > 1) {
-      start();
-      park(0);
-    }
-    const float* ck = sCk + max(b - 1, 0) * N * 64;
-    // the states behind each of the tokens but the last, and the tokens' steps
-    float hist[kSub - 1][N], step[kSub];
-    {
-      T ru[kSub - 1], rd[kSub];
+  auto chunk = [&](int w) {
+    const Tile tl = find_tile(a.offs, a.n_seq, a.rows, kBCL, w);
+    if (tl.seq < 0) return;
+    const int t0 = tl.j * kBCL, nt = max(0, min(tl.len - t0, kBCL));
+    const int64_t r0 = (int64_t)tl.base + t0;
+    // (the chunk before has left the shared memory behind a barrier)
+    stage_bc<T, N>(sBC, B + r0 * a.ldB, a.ldB, C + r0 * a.ldC, a.ldC, nt, threadIdx.x, blockDim.x);
+    auto start = [&]() {  // the state in front of the chunk
+      if (cst) {
 #pragma unroll
-      for (int i = 0; i < kSub; ++i) {
-        const int64_t t = min(b * kSub + i, nt - 1);
-        if (i + 1 < kSub) ru[i] = ld_at(us + t * a.ldu, le);
-        rd[i] = ld_at(ds + t * a.lddt, le);
+        for (int n = 0; n < N; ++n) s[n] = ld_at(cst + ((int64_t)w * N + n) * E, lf);
+      } else if (a.state) {
+        ld_vec<N>(a.state + (int64_t)tl.seq * E * N, ln, s);
+      } else {
+#pragma unroll
+        for (int n = 0; n < N; ++n) s[n] = 0.f;
+      }
+    };
+    start();
+    if (cst) {
+#pragma unroll
+      for (int n = 0; n < N; ++n) h[n] = ld_at(H + ((int64_t)w * N + n) * E, lf);
+    } else if (dstate_out) {
+      ld_vec<N>(dstate_out + (int64_t)tl.seq * E * N, ln, h);
+    } else {
+#pragma unroll
+      for (int n = 0; n < N; ++n) h[n] = 0.f;
+    }
+    __syncthreads();
+    const int nsub = (nt + kSub - 1) / kSub;
+    const T *us = u + r0 * a.ldu, *ds = dt + r0 * a.lddt, *zs = z ? z + r0 * a.ldz : nullptr, *gs = dy + r0 * lddy;
+    auto park = [&](int b) {  // s in front of the kSub tokens b; the first ones' place is the second ones'
+      float* ck = sCk + max(b - 1, 0) * N * 64;
+#pragma unroll
+      for (int n = 0; n < N; ++n) ck[n * 64] = s[n];
+    };
+    for (int b = 0; b < nsub - 1; ++b) {
+      if (b > 0) park(b);
+      T ru[kSub], rd[kSub];
+#pragma unroll
+      for (int i = 0; i < kSub; ++i) {  // all of these tokens exist
+        ru[i] = ld_at(us + (b * kSub + i) * a.ldu, le);
+        rd[i] = ld_at(ds + (b * kSub + i) * a.lddt, le);
       }
 #pragma unroll
       for (int i = 0; i < kSub; ++i) {
-        if (b * kSub + i < nt) {
-          step[i] = softplus(to_f32(rd[i]) + bias);
-          if (i + 1 < kSub) {
-            const float du = step[i] * to_f32(ru[i]);
-            const float* x = &sBC[(b * kSub + i) * W];
+        const float d = softplus(to_f32(rd[i]) + bias), du = d * to_f32(ru[i]);
+        const float* x = &sBC[(b * kSub + i) * W];
 #pragma unroll
-            for (int n = 0; n < N; ++n)
-              hist[i][n] = fmaf(__builtin_amdgcn_exp2f(step[i] * a2[n]), i ? hist[i - 1][n] : ck[n * 64], du * x[n]);
-          }
-        }
+        for (int n = 0; n < N; ++n) s[n] = fmaf(__builtin_amdgcn_exp2f(d * a2[n]), s[n], du * x[n]);
         __builtin_amdgcn_sched_barrier(0);
       }
     }
+    if (nsub > 0) park(nsub - 1);
+    T cu, cd, cz, cg_;  // the token's inputs, one token ahead
+    auto load = [&](int t) {
+      const int64_t r = max(t, 0);
+      cu = ld_at(us + r * a.ldu, le);
+      cd = ld_at(ds + r * a.lddt, le);
+      cg_ = ld_at(gs + r * lddy, le);
+      if (z) cz = ld_at(zs + r * a.ldz, le);
+    };
+    if (nt > 0) load(nt - 1);
+    for (int b = nsub - 1; b >= 0; --b) {
+      if (b == 0 && nsub > 1) {
+        start();
+        park(0);
+      }
+      const float* ck = sCk + max(b - 1, 0) * N * 64;
+      // the states behind each of the tokens but the last, and the tokens' steps
+      float hist[kSub - 1][N], step[kSub];
+      {
+        T ru[kSub - 1], rd[kSub];
 #pragma unroll
-    for (int i = kSub - 1; i >= 0; --i) {
-      const int t = b * kSub + i;
-      if (t >= nt) continue;  // the same for the whole workgroup
-      const float* x = &sBC[t * W];
-      const float uv = active ? to_f32(cu) : 0.f, v = to_f32(cd) + bias, gy = active ? to_f32(cg_) : 0.f;
-      const float zv = z ? to_f32(cz) : 0.f;
-      load(t - 1);
-      const float d = step[i], du = d * uv;
-      float gate = 1.f, dgate = 0.f;
-      if (z) {
-        const float sg = rcp_fast(1.f + exp_fast(-zv));
-        gate = zv * sg;
-        dgate = sg * fmaf(zv, 1.f - sg, 1.f);
-      }
-      const float q = gy * gate;
-      float yv = 0.f, gB = 0.f, dd = 0.f, red[N / 2], half[2];
-      // A state's terms of dB and dC go through the first step of their sums at once, a pair
-      // of states' through the second: N / 2 values stay of the 2 N. Four states at a time
-      // (the barriers keep the scheduler from holding all of a token's B, C and terms).
+        for (int i = 0; i < kSub; ++i) {
+          const int64_t t = min(b * kSub + i, nt - 1);
+          if (i + 1 < kSub) ru[i] = ld_at(us + t * a.ldu, le);
+          rd[i] = ld_at(ds + t * a.lddt, le);
+        }
 #pragma unroll
-      for (int n = 0; n < N; ++n) {
-        const float an = __builtin_amdgcn_exp2f(d * a2[n]);
-        const float as = an * (i ? hist[i - 1][n] : ck[n * 64]);
-        const float st = i + 1 < kSub ? hist[i][n] : fmaf(du, x[n], as);
-        const float g = fmaf(q, x[N + n], h[n]);
-        yv = fmaf(st, x[N + n], yv);
-        gB = fmaf(g, x[n], gB);
-        const float ga = g * as;
-        dd = fmaf(ga, a2[n], dd);  // in units of 1 / ln 2
-        dA[n] = fmaf(ga, d, dA[n]);
-        h[n] = an * g;
-        half[n % 2] = swap_add32(g * du, q * st);  // lanes 0-31: dB, 32-63: dC
-        if (n % 2) red[n / 2] = swap_add16(half[0], half[1]);
-        if (n % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+        for (int i = 0; i < kSub; ++i) {
+          if (b * kSub + i < nt) {
+            step[i] = softplus(to_f32(rd[i]) + bias);
+            if (i + 1 < kSub) {
+              const float du = step[i] * to_f32(ru[i]);
+              const float* x = &sBC[(b * kSub + i) * W];
+#pragma unroll
+              for (int n = 0; n < N; ++n)
+                hist[i][n] = fmaf(__builtin_amdgcn_exp2f(step[i] * a2[n]), i ? hist[i - 1][n] : ck[n * 64], du * x[n]);
+            }
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
       }
-      yv = fmaf(Dv, uv, yv);
-      const float ddt = fmaf(dd, kLn2, uv * gB) * rcp_fast(1.f + exp_fast(-v));
-      dD = fmaf(q, uv, dD);
-      dbias += ddt;
-      if (active) {
-        const int64_t r = r0 + t;
-        st_at(du_o + r * lddu, le, fmaf(Dv, q, d * gB));
-        st_at(ddt_o + r * ldddt, le, ddt);
-        if (z) st_at(dz_o + r * lddz, le, gy * yv * dgate);
+#pragma unroll
+      for (int i = kSub - 1; i >= 0; --i) {
+        const int t = b * kSub + i;
+        if (t >= nt) continue;  // the same for the whole workgroup
+        const float* x = &sBC[t * W];
+        const float uv = active ? to_f32(cu) : 0.f, v = to_f32(cd) + bias, gy = active ? to_f32(cg_) : 0.f;
+        const float zv = z ? to_f32(cz) : 0.f;
+        load(t - 1);
+        const float d = step[i], du = d * uv;
+        float gate = 1.f, dgate = 0.f;
+        if (z) {
+          const float sg = rcp_fast(1.f + exp_fast(-zv));
+          gate = zv * sg;
+          dgate = sg * fmaf(zv, 1.f - sg, 1.f);
+        }
+        const float q = gy * gate;
+        float yv = 0.f, gB = 0.f, dd = 0.f, red[N / 2], half[2];
+        // A state's terms of dB and dC go through the first step of their sums at once, a pair
+        // of states' through the second: N / 2 values stay of the 2 N. Four states at a time
+        // (the barriers keep the scheduler from holding all of a token's B, C and terms).
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+          const float an = __builtin_amdgcn_exp2f(d * a2[n]);
+          const float as = an * (i ? hist[i - 1][n] : ck[n * 64]);
+          const float st = i + 1 < kSub ? hist[i][n] : fmaf(du, x[n], as);
+          const float g = fmaf(q, x[N + n], h[n]);
+          yv = fmaf(st, x[N + n], yv);
+          gB = fmaf(g, x[n], gB);
+          const float ga = g * as;
+          dd = fmaf(ga, a2[n], dd);  // in units of 1 / ln 2
+          dA[n] = fmaf(ga, d, dA[n]);
+          h[n] = an * g;
+          half[n % 2] = swap_add32(g * du, q * st);  // lanes 0-31: dB, 32-63: dC
+          if (n % 2) red[n / 2] = swap_add16(half[0], half[1]);
+          if (n % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+        }
+        yv = fmaf(Dv, uv, yv);
+        const float ddt = fmaf(dd, kLn2, uv * gB) * rcp_fast(1.f + exp_fast(-v));
+        dD = fmaf(q, uv, dD);
+        dbias += ddt;
+        if (active) {
+          const int64_t r = r0 + t;
+          st_at(du_o + r * lddu, le, fmaf(Dv, q, d * gB));
+          st_at(ddt_o + r * ldddt, le, ddt);
+          if (z) st_at(dz_o + r * lddz, le, gy * yv * dgate);
+        }
+        const float tot = reduce_rows<N / 2>(red, lane);
+        if (lane % (64 / W) == 0) sRed[(i * nw + wave) * W + place] = tot;
+        __builtin_amdgcn_sched_barrier(0);
       }
-      const float tot = reduce_rows<N / 2>(red, lane);
-      if (lane % (64 / W) == 0) sRed[(i * nw + wave) * W + place] = tot;
-      __builtin_amdgcn_sched_barrier(0);
+      __syncthreads();
+      for (int i = threadIdx.x; i < min(kSub, nt - b * kSub) * W; i += blockDim.x) {
+        const int k = i / W, col = i % W;
+        float acc = 0.f;
+        for (int j = 0; j < nw; ++j) acc += sRed[(k * nw + j) * W + col];
+        const int64_t r = r0 + b * kSub + k;
+        if (bc_part) bc_part[((int64_t)cg * a.rows + r) * W + col] = acc;
+        else if (col < N) st1(dB_o + r * lddB + col, acc);
+        else st1(dC_o + r * lddC + col - N, acc);
+      }
+      __syncthreads();
     }
-    __syncthreads();
-    for (int i = threadIdx.x; i < min(kSub, nt - b * kSub) * W; i += blockDim.x) {
-      const int k = i / W, col = i % W;
-      float acc = 0.f;
-      for (int j = 0; j < nw; ++j) acc += sRed[(k * nw + j) * W + col];
-      const int64_t r = r0 + b * kSub + k;
-      if (bc_part) bc_part[((int64_t)cg * a.rows + r) * W + col] = acc;
-      else if (col < N) st1(dB_o + r * lddB + col, acc);
-      else st1(dC_o + r * lddC + col - N, acc);
-    }
-    __syncthreads();
+    if (active && dstate && tl.j == 0) st_vec<N>(dstate + (int64_t)tl.seq * E * N, ln, h);
+  };
+  if constexpr (MULTI) {
+    for (int w = p * per; w < min((p + 1) * per, a.ntile); ++w) chunk(w);
+  } else {
+    chunk(p);
   }
-  if (active) {
+  if (!active) return;
+  float* po = part + (int64_t)p * (N + 2) * E;
 #pragma unroll
-    for (int n = 0; n < N; ++n) st_at(po + (int64_t)n * E, lf, dA[n] * (a2[n] * kLn2));
-    st_at(po + (int64_t)N * E, lf, dD);
-    st_at(po + (int64_t)(N + 1) * E, lf, dbias);
-    if (dstate && tl.j == 0) st_vec<N>(dstate + (int64_t)tl.seq * E * N, ln, h);
-  }
+  for (int n = 0; n < N; ++n) st_at(po + (int64_t)n * E, lf, dA[n] * (a2[n] * kLn2));
+  st_at(po + (int64_t)N * E, lf, dD);
+  st_at(po + (int64_t)(N + 1) * E, lf, dbias);
 }
 
 // dB and dC over the channel groups. Rows that no sequence owns have no
@@ -1292,7 +1298,7 @@ hipError_t scan_fwd(const ScanOp& a, float* state_out, void* y_, int64_t ldy, fl
 }
 
 struct BwdPlan {
-  int nw, CG, ntile;
+  int nw, CG, ntile, per, parts;
   bool chunks;
   size_t cst, csum, G, part, bc, total;  // in floats
 };
@@ -1302,12 +1308,18 @@ BwdPlan bwd_plan(bool packed, int n_seq, int rows, int E, int N, int L) {
   p.CG = (E + 64 * p.nw - 1) / (64 * p.nw);
   p.ntile = packed ? rows / kBCL + n_seq : n_seq;
   p.chunks = packed && L > kBCL;
+  // Short sequences, a chunk each, go several to a workgroup once there are eight rounds of them: the partial
+  // sums of the parameters' gradients are as large as a chunk of two tokens. 4,096 of 25 tokens, E 512: 1,241
+  // to 1,105 us (bf16), 1,222 to 1,063 (fp32). Not chunks of long ones, which lose 5% to the registers
+  // that the loop takes.
+  p.per = p.chunks ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(16, (int64_t)p.ntile * p.CG / (kCUs * 16)));
+  p.parts = (p.ntile + p.per - 1) / p.per;
   size_t o = 0;
   const size_t st = p.chunks ? (size_t)p.ntile * N * E : 0;
   p.cst = o; o += st;
   p.G = o; o += st;
   p.csum = o; o += p.chunks ? (size_t)p.ntile * E : 0;
-  p.part = o; o += (size_t)p.ntile * (N + 2) * E;
+  p.part = o; o += (size_t)p.parts * (N + 2) * E;
   p.bc = o; o += p.CG > 1 ? (size_t)p.CG * rows * 2 * N : 0;
   p.total = o;
   return p;
@@ -1329,13 +1341,14 @@ hipError_t scan_bwd(const ScanOp& a, const void* dy_, int64_t lddy, const float*
     ssm_combine_kernel<N><<<dim3((unsigned)((n + 255) / 256), 2), 256, 0, s>>>(in, cst, ws + p.csum, G, dstate_out);
   }
   const size_t lds = sizeof(float) * (2 * N * (kBCL + kSub * p.nw) + (size_t)p.nw * (kBCL / kSub - 1) * N * 64);
-  hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&ssm_bwd_kernel<T, N>),
+  auto kernel = p.per > 1 ? &ssm_bwd_kernel<T, N, true> : &ssm_bwd_kernel<T, N, false>;
+  hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
                                      hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
   if (e != hipSuccess) return e;
-  ssm_bwd_kernel<T, N><<<dim3(tile_blocks(in.ntile, p.CG)), 64 * p.nw, lds, s>>>(
+  kernel<<<dim3(tile_blocks(p.parts, p.CG)), 64 * p.nw, lds, s>>>(
       in, u, dt, B, C, z, dy, lddy, cst, G, dstate_out, static_cast<T*>(g.du), g.lddu, static_cast<T*>(g.ddt),
       g.ldddt, static_cast<T*>(g.dz), g.lddz, static_cast<T*>(g.dB), g.lddB, static_cast<T*>(g.dC), g.lddC, g.dstate,
-      part, bc);
+      part, p.parts, p.per, bc);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
   if (bc && a.rows > 0) {
@@ -1344,7 +1357,7 @@ hipError_t scan_bwd(const ScanOp& a, const void* dy_, int64_t lddy, const float*
         a.offs, a.n_seq, a.rows, p.CG, bc, static_cast<T*>(g.dB), g.lddB, static_cast<T*>(g.dC), g.lddC);
   }
   const int64_t n = (int64_t)(N + 2) * a.E;
-  sum_parts_kernel<<<dim3((unsigned)((n + 63) / 64)), 64 * kSumLanes, 0, s>>>(part, in.ntile, N, N + 2, a.E, g.dA_log,
+  sum_parts_kernel<<<dim3((unsigned)((n + 63) / 64)), 64 * kSumLanes, 0, s>>>(part, p.parts, N, N + 2, a.E, g.dA_log,
                                                                              g.dD, g.db_dt);
   return hipGetLastError();
 }
@@ -1407,8 +1420,9 @@ hipError_t launch_ssm_scan(const ScanOp& a, float* state_out, void* y, int64_t l
 }
 
 size_t ssm_scan_bwd_workspace_bytes(int n_seq, int rows, int E, int N, int L) {
-  // (a call without offsets needs no more than one with them)
-  return bwd_plan(true, n_seq, rows, E, N, L).total * sizeof(float);
+  // (as many rows as sequences may also be single tokens without offsets, with a plan of their own)
+  const size_t packed = bwd_plan(true, n_seq, rows, E, N, L).total;
+  return (rows == n_seq ? std::max(packed, bwd_plan(false, n_seq, rows, E, N, 1).total) : packed) * sizeof(float);
 }
 
 hipError_t launch_ssm_scan_bwd(const ScanOp& a, const void* dy, int64_t lddy, const float* dstate_out,

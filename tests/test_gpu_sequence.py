@@ -308,6 +308,37 @@ def test_scan_gradients_of_single_tokens(dtype):
     _check_scan_grads(g, r, dtype, n, ["du", "ddt", "dz", "dB", "dC", "dA_log", "dD", "db_dt", "dstate"])
 
 
+@pytest.mark.parametrize("packed", [True, False])
+def test_scan_gradients_of_many_short_sequences(packed):
+    """Several sequences to a workgroup, some of them empty."""
+    n, E, N = 1400, 1500, 16
+    rng = np.random.default_rng(8)
+    lens = rng.integers(0, 4, n).tolist() if packed else [1] * n
+    a = _scan_case(lens, E, N, "f32", 9)
+    T, offs = sum(lens), _offs(lens)
+    dy, dend = rng.standard_normal((T, E)).astype(np.float32), rng.standard_normal((n, E, N)).astype(np.float32)
+    k = _scan_tensors(a, "f32", T)
+    if packed:
+        k.update(offs=_cuda(offs, torch.int32), L=3)
+    g = _tb().ssm_scan_backward(dy=_cuda(dy), state_grad=_cuda(dend), **k)
+    r = osq.scan_backward(dy=dy, offs=offs, dend=dend, **a)
+    _check_scan_grads(g, r, "f32", T, ["du", "ddt", "dz", "dB", "dC", "dA_log", "dD", "db_dt", "dstate"])
+
+
+def test_workspace_covers_single_tokens():
+    """As many rows as sequences: the workspace serves the call with offsets and the one without."""
+    tb = _tb()
+    for n, E in ((3990, 256), (4097, 256), (1400, 1500), (8130, 300), (100, 64)):
+        u, bc = torch.zeros(n, E, device="cuda"), torch.zeros(n, 8, device="cuda")
+        A = torch.zeros(E, 8, device="cuda")
+        ws = tb.ssm_scan_workspace(n, n, E, 8, 1, backward=True)
+        guard = torch.full((ws.numel() + 4096,), 255, dtype=torch.uint8, device="cuda")
+        for offs in (None, torch.arange(n + 1, dtype=torch.int32, device="cuda")):
+            tb.ssm_scan_backward(u, u, A, bc, bc, u, offs=offs, L=1, workspace=guard[:ws.numel()])
+        torch.cuda.synchronize()
+        assert (guard[ws.numel():] == 255).all(), (n, E)
+
+
 def test_scan_gradient_is_a_difference():
     """The gradient along one direction of all inputs together against the
     forward operator's own central difference. The loss sums T E = 1,376 terms of size 1 to 10, off by
