@@ -537,9 +537,11 @@ def _adr(t) -> int:
 
 
 def _stream_of(t) -> int:
-    """The current stream of t's device (the current device)."""
+    """The current stream of t's device (the current device); by torch's way to the bare handle where
+    it has one, as a Stream object takes 1 us, a tenth of a token's call."""
     import torch
-    return torch.cuda.current_stream(t.get_device()).cuda_stream
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return raw(t.get_device()) if raw else torch.cuda.current_stream(t.get_device()).cuda_stream
 
 
 def _under(stream, call, *args, **kw):
@@ -572,13 +574,14 @@ def _on_device(t):
         raise ValueError(f"tensors on {t.device}, which is not the current device")
 
 
-def _workspace(need, workspace, like):
-    """The caller's workspace, or one of `need` bytes."""
+def _workspace(workspace, like, size, *args):
+    """The caller's workspace, or one of size(*args) bytes."""
     import torch
     if workspace is not None:
-        if workspace.device != like.device or not workspace.is_contiguous():
+        if workspace.get_device() != like.get_device() or not workspace.is_contiguous():
             raise ValueError(f"workspace: contiguous memory on {like.device} expected")
         return workspace
+    need = size(*args)
     return torch.empty(need, dtype=torch.uint8, device=like.device) if need else None
 
 
@@ -669,7 +672,7 @@ def ssm_conv_backward(x, w, b, du, offs=None, state=None, state_grad=None, works
     a = _conv_args(x, w, b, offs, n_seq, state)
     r = _results(dict(dx=(x.shape, x.dtype, True), dw=(w.shape, w.dtype, False), db=(x.shape[1:], w.dtype, False),
                       dstate=None if state is None else (state.shape, x.dtype, False)), out, x)
-    ws = _workspace(lib().tcl_ssm_conv_workspace_bytes(n_seq, x.shape[0], x.shape[1], K), workspace, x)
+    ws = _workspace(workspace, x, lib().tcl_ssm_conv_workspace_bytes, n_seq, *x.shape, K)
     check(lib().tcl_ssm_conv_backward(a, du.data_ptr(), _ld(du), _ptr(state_grad), r["dx"].data_ptr(),
                                       _ld(r["dx"]), r["dw"].data_ptr(), r["db"].data_ptr(), _ptr(r["dstate"]),
                                       *_ws_args(ws), _stream_of(x)))
@@ -719,8 +722,8 @@ def ssm_scan(u, dt, A_log, B, C, D=None, z=None, b_dt=None, offs=None, L=None, s
         out = torch.empty(u.shape, dtype=u.dtype, device=u.device)
     else:
         _expect("out", out, u.dtype, u.shape, u, rows=True)
-    need = 0 if offs is None else lib().tcl_ssm_scan_workspace_bytes(n_seq, *u.shape, A_log.shape[1], L)
-    ws = _workspace(need, workspace, u)
+    ws = None if offs is None else _workspace(workspace, u, lib().tcl_ssm_scan_workspace_bytes, n_seq, *u.shape,
+                                              A_log.shape[1], L)
     check(lib().tcl_ssm_scan(a, _ptr(slots), n_slots, _ptr(state_out), out.data_ptr(), _ld(out),
                              *_ws_args(ws), _stream_of(u)))
     return out
@@ -752,7 +755,7 @@ def ssm_scan_backward(u, dt, A_log, B, C, dy, D=None, z=None, b_dt=None, offs=No
                          _ld(r["dB"]), r["dC"].data_ptr(), _ld(r["dC"]), _adr(r["dz"]),
                          0 if z is None else _ld(r["dz"]), r["dA_log"].data_ptr(), r["dD"].data_ptr(),
                          r["db_dt"].data_ptr(), _adr(r["dstate"]))
-    ws = _workspace(lib().tcl_ssm_scan_backward_workspace_bytes(n_seq, rows, E, N, L), workspace, u)
+    ws = _workspace(workspace, u, lib().tcl_ssm_scan_backward_workspace_bytes, n_seq, rows, E, N, L)
     check(lib().tcl_ssm_scan_backward(a, dy.data_ptr(), _ld(dy), _ptr(state_grad), g,
                                       *_ws_args(ws), _stream_of(u)))
     return r
@@ -799,7 +802,7 @@ def logprobs(logits, tokens=None, K=0, temperature=1.0, seg_offsets=None, max_le
 
     r = dict(logp=None if tokens is None else new(n), entropy=new(n), top=new(n, K, dtype=torch.int32) if K else None,
              top_logp=new(n, K) if K else None)
-    ws = _workspace(lib().tcl_logits_workspace_bytes(n, V, K), workspace, logits)
+    ws = _workspace(workspace, logits, lib().tcl_logits_workspace_bytes, n, V, K)
     check(lib().tcl_logprobs(_dtype(logits), n, V, logits.data_ptr(), ld, _ptr(seg_offsets), temperature,
                              _ptr(tokens), K, _ptr(r["logp"]), r["entropy"].data_ptr(), _ptr(r["top"]),
                              _ptr(r["top_logp"]), *_ws_args(ws), _stream_of(logits)))
@@ -831,7 +834,7 @@ def distill_topk(logits, top, teacher, weight=None, temperature=1.0, seg_offsets
     _expect("grad", grad, logits.dtype, logits.shape, logits, rows=seg_offsets is None)
     ldg = _ld(grad) if grad is not None and seg_offsets is None else 0
     loss = torch.empty(n, dtype=torch.float32, device=logits.device)
-    ws = _workspace(lib().tcl_logits_workspace_bytes(n, V, K), workspace, logits)
+    ws = _workspace(workspace, logits, lib().tcl_logits_workspace_bytes, n, V, K)
     check(lib().tcl_distill_topk(_dtype(logits), n, V, logits.data_ptr(), ld, _ptr(seg_offsets), temperature, K,
                                  top.data_ptr(), teacher.data_ptr(), _ptr(weight), loss.data_ptr(), _ptr(grad), ldg,
                                  *_ws_args(ws), _stream_of(logits)))

@@ -788,7 +788,9 @@ int distill_splits(int n, int V) { return V / 4 + 1 <= 16 * 1024 ? 1 : row_split
 
 template <typename T>
 hipError_t logprobs(const LogitRows& a, int K, const LogprobOut& o, char* ws, hipStream_t s) {
-  const int S = row_splits(a.n, a.V);
+  // Up to 16 vectors per thread a row is not worth the second launch: 64 of 12,000 fp32 logits, K 20,
+  // 12 us whole, 16 split; 8 of 30,000 in bf16, K 5, 13 and 15, in fp32 (30 vectors) 14 and 14.
+  const int S = a.V / Row<T>::VE < 16 * kTB ? 1 : row_splits(a.n, a.V);
   // Many short rows: one wavefront each, or two for more top entries than half its lanes. 65,536 bf16 rows of
   // 2,048, K 20: 137 us, with kTB threads 308; 8,192 of 16,384 72 with one wavefront, 76 with kTB.
   if (S == 1 && a.n >= 256 && a.V <= 8192 && K <= 32) logprobs_kernel<T, 64><<<dim3(a.n), 64, 0, s>>>(a, K, o, ws);
