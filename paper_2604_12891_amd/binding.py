@@ -532,6 +532,14 @@ def _ld(t) -> int:
     return t.shape[1] if t.is_contiguous() else t.stride(0)
 
 
+def _row_ld(name, t, dtype, shape, like) -> int:
+    """_expect's check of a matrix of rows, and its leading dimension."""
+    if t.dtype is dtype and t.shape == shape and t.is_contiguous() and t.get_device() == like.get_device():
+        return shape[1]
+    _expect(name, t, dtype, shape, like, rows=True)
+    return _ld(t)
+
+
 def _adr(t) -> int:
     return 0 if t is None else t.data_ptr()
 
@@ -622,10 +630,10 @@ def _conv_args(x, w, b, offs, n_seq, state):
     rows, E = x.shape
     if w.dim() != 2:
         raise ValueError(f"w: [E, K] expected, not {tuple(w.shape)}")
-    _expect("x", x, x.dtype, (rows, E), x, rows=True)
+    ldx = _row_ld("x", x, x.dtype, x.shape, x)
     _expect("w", w, torch.float32, (E, w.shape[1]), x)
     _expect("b", b, torch.float32, (E,), x)
-    return _PACK_CONV.pack(_dtype(x), n_seq, rows, E, w.shape[1], _adr(offs), x.data_ptr(), _ld(x), w.data_ptr(),
+    return _PACK_CONV.pack(_dtype(x), n_seq, rows, E, w.shape[1], _adr(offs), x.data_ptr(), ldx, w.data_ptr(),
                            _adr(b), _adr(state))
 
 
@@ -686,16 +694,18 @@ def _scan_args(u, dt, A_log, B, C, D, z, b_dt, offs, n_seq, L, state):
     if A_log.dim() != 2:
         raise ValueError(f"A_log: [E, N] expected, not {tuple(A_log.shape)}")
     N = A_log.shape[1]
-    for name, t, cols in (("u", u, E), ("dt", dt, E), ("B", B, N), ("C", C, N), ("z", z, E)):
-        _expect(name, t, u.dtype, (rows, cols), u, rows=True)
+    act, bc = u.shape, (rows, N)
+    ldu, lddt = _row_ld("u", u, u.dtype, act, u), _row_ld("dt", dt, u.dtype, act, u)
+    ldB, ldC = _row_ld("B", B, u.dtype, bc, u), _row_ld("C", C, u.dtype, bc, u)
+    ldz = 0 if z is None else _row_ld("z", z, u.dtype, act, u)
     _expect("A_log", A_log, torch.float32, (E, N), u)
     _expect("D", D, torch.float32, (E,), u)
     _expect("b_dt", b_dt, torch.float32, (E,), u)
     if L is None:
         L = max(rows, 1) if offs is not None else 1
-    return L, _PACK_SCAN.pack(_dtype(u), n_seq, rows, E, N, L, _adr(offs), u.data_ptr(), _ld(u), dt.data_ptr(), _ld(dt),
-                              B.data_ptr(), _ld(B), C.data_ptr(), _ld(C), _adr(z), 0 if z is None else _ld(z),
-                              A_log.data_ptr(), _adr(D), _adr(b_dt), _adr(state))
+    return L, _PACK_SCAN.pack(_dtype(u), n_seq, rows, E, N, L, _adr(offs), u.data_ptr(), ldu, dt.data_ptr(), lddt,
+                              B.data_ptr(), ldB, C.data_ptr(), ldC, _adr(z), ldz, A_log.data_ptr(), _adr(D),
+                              _adr(b_dt), _adr(state))
 
 
 def ssm_scan_workspace(n_seq, rows, E, N, L, backward=False):
@@ -776,8 +786,7 @@ def _logit_rows(logits, seg_offsets, max_len):
     if seg_offsets is None:
         if logits.dim() != 2:
             raise ValueError(f"[rows, V] logits expected, not {tuple(logits.shape)}")
-        _expect("logits", logits, logits.dtype, logits.shape, logits, rows=True)
-        return logits.shape[0], logits.shape[1], _ld(logits)
+        return *logits.shape, _row_ld("logits", logits, logits.dtype, logits.shape, logits)
     if logits.dim() != 1 or seg_offsets.dim() != 1 or seg_offsets.numel() < 1:
         raise ValueError("segments: logits [n] and seg_offsets [n_seg + 1] expected")
     _expect("logits", logits, logits.dtype, logits.shape, logits)
