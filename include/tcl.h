@@ -487,8 +487,8 @@ TCL_API tcl_status tcl_trainer_timing_reset(tcl_trainer* trainer);
  *    distinct where an output pool is given. Other places of the output pool
  *    are left as they are.
  *  - Outputs must not overlap inputs (states aside) or each other.
- *  - E in [1, 65536], d_state (N) 8 or 16, d_conv (K) in [1, 4], n_seq and rows at most 2^30 and
- *    (n_seq + rows) E at most 2^36. Stream-ordered,
+ *  - E in [1, 65536], d_state (N) 8 or 16, d_conv (K) in [1, 4]; with E rounded up to a multiple
+ *    of 64, rows E at most 2^34 and n_seq E at most 2^30. Stream-ordered,
  *    deterministic, no allocation; may be captured into a graph. Empty work
  *    (n_seq == 0, or rows == 0 in the single-token form) is TCL_OK.
  * ------------------------------------------------------------------- */
@@ -597,8 +597,8 @@ TCL_API tcl_status tcl_ssm_scan_backward(const tcl_ssm_scan_args* args, const vo
  * from the row's start), or a segment d_seg_offsets[g] .. d_seg_offsets[g+1]-1 of one
  * array, V entries at most, as in tcl_topk (entries are counted from the
  * array's start, ld is not used). Logits are fp32 or bf16 (dtype), of any
- * alignment; arithmetic is fp32; temperature > 0 divides the logits. -inf is
- * a masked entry, with no probability. V <= 2^30. Stream-ordered, deterministic, no
+ * alignment; arithmetic is fp32; a temperature in [1e-30, 1e30] divides the logits. -inf is
+ * a masked entry, with no probability. V <= 2^30, n_rows < 2^22. Stream-ordered, deterministic, no
  * allocation. d_workspace: >= tcl_logits_workspace_bytes(n_rows, V, K) bytes, 256-byte
  * aligned; 0 bytes (d_workspace may be NULL) from 513 rows on. n_rows == 0 is TCL_OK.
  * ------------------------------------------------------------------- */

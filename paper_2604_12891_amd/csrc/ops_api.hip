@@ -11,9 +11,14 @@ namespace {
 
 bool misaligned(const void* p, uintptr_t n) { return reinterpret_cast<uintptr_t>(p) % n != 0; }
 
-// Row and tile indices, and grids of tiles x channel groups, have to fit in 31 bits.
+// A launch has fewer than 2^32 threads. Tiles hold 30 rows or more, besides one per sequence, and
+// their channels are rounded up to 64, in the gradients (wavefronts in fours) to less than twice that: with these
+// bounds 2 (2^34 / 30 + 2^30) threads at most, and row and tile indices far inside 31 bits.
 constexpr int kMaxRows = 1 << 30;
-constexpr int64_t kMaxWork = (int64_t)1 << 36;
+constexpr int64_t kMaxRowWork = (int64_t)1 << 34, kMaxSeqWork = (int64_t)1 << 30;
+// Rows of logits take a workgroup of up to 1,024 threads each.
+constexpr int kMaxLogitRows = (1 << 22) - 1;
+constexpr float kMinTemp = 1e-30f, kMaxTemp = 1e30f;
 
 tcl_status check_workspace(const void* d_ws, size_t have, size_t need) {
   if (need == 0) return TCL_OK;
@@ -29,8 +34,9 @@ tcl_status check_sequences(int32_t dtype, int32_t n_seq, int32_t rows, int32_t E
   if (!d_offs && rows != n_seq)
     return fail(TCL_ERR_INVALID_ARG, "without d_offs every sequence is one row (n_seq=%d rows=%d)", n_seq, rows);
   if (E < 1 || E > 65536) return fail(TCL_ERR_UNSUPPORTED, "E must be in [1, 65536] (got %d)", E);
-  if (n_seq > kMaxRows || rows > kMaxRows || ((int64_t)n_seq + rows) * E > kMaxWork)
-    return fail(TCL_ERR_UNSUPPORTED, "too many rows x channels");
+  const int64_t C = ((int64_t)E + 63) / 64 * 64;
+  if (n_seq > kMaxRows || rows > kMaxRows || rows * C > kMaxRowWork || n_seq * C > kMaxSeqWork)
+    return fail(TCL_ERR_UNSUPPORTED, "too many rows or sequences x channels (n_seq=%d rows=%d E=%d)", n_seq, rows, E);
   return TCL_OK;
 }
 
@@ -80,9 +86,10 @@ tcl_status logit_rows(int32_t dtype, int32_t n_rows, int32_t V, const void* d_lo
   if (dtype != TCL_F32 && dtype != TCL_BF16) return fail(TCL_ERR_INVALID_ARG, "bad dtype %d", dtype);
   if (n_rows < 0 || V < 1) return fail(TCL_ERR_INVALID_ARG, "need n_rows >= 0, V > 0 (got %d, %d)", n_rows, V);
   if (V > (1 << 30)) return fail(TCL_ERR_UNSUPPORTED, "V must be at most 2^30 (got %d)", V);
+  if (n_rows > kMaxLogitRows) return fail(TCL_ERR_UNSUPPORTED, "n_rows must be below 2^22 (got %d)", n_rows);
   if (!d_seg_offsets && ld < V) return fail(TCL_ERR_INVALID_ARG, "leading dimension smaller than V");
-  if (!(temperature > 0.f) || !std::isfinite(temperature) || !std::isfinite(1.0f / temperature))
-    return fail(TCL_ERR_INVALID_ARG, "temperature must be positive and finite");
+  if (!(temperature >= kMinTemp && temperature <= kMaxTemp))
+    return fail(TCL_ERR_INVALID_ARG, "temperature must be in [1e-30, 1e30]");
   if (!d_logits && n_rows > 0) return fail(TCL_ERR_INVALID_ARG, "NULL device pointer");
   if (misaligned(d_logits, dtype == TCL_BF16 ? 2 : 4))
     return fail(TCL_ERR_INVALID_ARG, "logits are not aligned to their type");
@@ -111,7 +118,7 @@ TCL_API tcl_status tcl_ssm_conv(const tcl_ssm_conv_args* args, const int32_t* d_
 }
 
 TCL_API size_t tcl_ssm_conv_workspace_bytes(int32_t n_seq, int32_t rows, int32_t E, int32_t K) {
-  if (n_seq <= 0 || rows < 0 || E < 1 || E > 65536 || K < 1 || K > 4) return 0;
+  if (n_seq <= 0 || n_seq > kMaxRows || rows < 0 || E < 1 || E > 65536 || K < 1 || K > 4) return 0;
   return ssm_conv_workspace_bytes(n_seq, rows, E, K);
 }
 
@@ -135,7 +142,7 @@ TCL_API tcl_status tcl_ssm_conv_backward(const tcl_ssm_conv_args* args, const vo
 // ------------------------------------------------------------------ selective scan
 
 TCL_API size_t tcl_ssm_scan_workspace_bytes(int32_t n_seq, int32_t rows, int32_t E, int32_t N, int32_t L) {
-  if (n_seq <= 0 || rows < 0 || E < 1 || E > 65536 || (N != 8 && N != 16) || L < 1) return 0;
+  if (n_seq <= 0 || n_seq > kMaxRows || rows < 0 || E < 1 || E > 65536 || (N != 8 && N != 16) || L < 1) return 0;
   return ssm_scan_workspace_bytes(n_seq, rows, E, N, L);
 }
 
@@ -159,7 +166,7 @@ TCL_API tcl_status tcl_ssm_scan(const tcl_ssm_scan_args* args, const int32_t* d_
 }
 
 TCL_API size_t tcl_ssm_scan_backward_workspace_bytes(int32_t n_seq, int32_t rows, int32_t E, int32_t N, int32_t L) {
-  if (n_seq <= 0 || rows < 0 || E < 1 || E > 65536 || (N != 8 && N != 16) || L < 1) return 0;
+  if (n_seq <= 0 || n_seq > kMaxRows || rows < 0 || E < 1 || E > 65536 || (N != 8 && N != 16) || L < 1) return 0;
   return ssm_scan_bwd_workspace_bytes(n_seq, rows, E, N, L);
 }
 

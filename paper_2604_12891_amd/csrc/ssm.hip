@@ -141,11 +141,14 @@ __device__ __forceinline__ int slot_of(const int* __restrict__ slots, int n_slot
 
 // ---------------------------------------------------------------- causal conv + SiLU
 // u_t = SiLU(b + sum_k w_k x_{t-K+1+k}). A thread takes CH adjacent channels
-// (16 bytes) of one tile and keeps the last K rows in registers; rows in front of
+// (four: 16 bytes in fp32; 8 in bf16, where eight would halve the wavefronts in
+// flight) of one tile and keeps the last K rows in registers; rows in front of
 // the tile are read again (K - 1 of R), those in front of the sequence come
 // from its state. The thread of the first tile is also the one that writes
 // the new state, after it has read the old one, so both may be the same
-// memory. Bound by HBM: each x read once, each u written once.
+// memory. Bound by HBM: each x read once, each u written once; 18,000 rows of 4,096
+// bf16 channels in 67 us (4.4 TB/s; 80 with eight channels a thread), one token
+// of 256 sequences in 7.3 (3.6 at the rate of a copy).
 template <typename T, int K, int CH>
 __global__ __launch_bounds__(256) void ssm_conv_kernel(const int* __restrict__ offs, int n_seq, int rows, int E,
                                                        int R, int64_t n_work, const T* __restrict__ x, int64_t ldx,
@@ -259,7 +262,8 @@ __device__ __forceinline__ float silu_grad(float x) {
 // `per` tiles in a row; in each it walks forward over the tile's rows and the
 // K - 1 behind it, forming pre and g again there, so that dx leaves complete and
 // nothing passes between threads. dw and db stay in registers over its tiles
-// and go out once, as part `p` of the partial sums.
+// and go out once, as part `p` of the partial sums. 18,000 rows of 4,096 bf16 channels in 121 us, 96 at
+// the rate of a copy; 40 issue slots per entry are some 90 us by themselves. (Two channels a thread: 159.)
 template <typename T, int K, int CH>
 __global__ __launch_bounds__(256) void ssm_conv_bwd_kernel(
     const int* __restrict__ offs, int n_seq, int rows, int E, int R, int per, int parts, const T* __restrict__ x,
@@ -428,10 +432,10 @@ __device__ __forceinline__ float dpp(float v) {
 // go through LDS kTC tokens at a time (widened once, read as broadcasts), the
 // next kTC rows on their way in registers meanwhile; u, dt and z come four
 // tokens ahead. Per token and wavefront 6 N issue slots for the states and
-// some 25 for softplus, gate and output, against 4 x 64 elements of traffic: the
-// vector unit is what bounds it: 4,096 programs of up to 25 tokens, E 512, fp32, in 139 us, where their
-// traffic takes 108 and their issue slots 112; a prompt of 8,192 tokens, E 4,096, bf16 in chunks
-// 113 + 12 + 150.
+// some 35 for softplus, gate and output, against 4 x 64 elements of traffic: the
+// vector unit is what bounds it: 4,096 programs of up to 25 tokens, E 512, fp32, in 141 us, where their
+// traffic takes 110 and their issue slots 124 (by the counters; a sixth of them is spent once per sequence);
+// a prompt of 8,192 tokens, E 4,096, bf16 in chunks 111 + 11 + 150.
 //
 // A sequence is cut into chunks of CL tokens when there are far too few of them to
 // fill the GPU (scan_chunk). s -> P s + s_loc with P = exp(A sum d) is what a chunk does to a
@@ -685,8 +689,8 @@ constexpr int kCombine = 32;
 template <int N>
 __global__ __launch_bounds__(256) void ssm_combine_kernel(ScanIn a, float* __restrict__ cst,
                                                           const float* __restrict__ csum, float* __restrict__ G,
-                                                          const float* __restrict__ dstate_out) {
-  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+                                                          const float* __restrict__ dstate_out, int64_t first) {
+  const int64_t id = first + (int64_t)blockIdx.x * 256 + threadIdx.x;
   const int E = a.E;
   const int e = (int)(id % E), n = (int)(id / E % N);
   const int64_t seq = id / E / N;
@@ -737,7 +741,8 @@ __global__ __launch_bounds__(256) void ssm_combine_kernel(ScanIn a, float* __res
 // N / 4 lanes per channel hold four states each: a wavefront reads and writes
 // 1 KB of states in one access, and y is summed over the lanes of a channel
 // by DPP. A workgroup takes 1,024 / N channels of SB sequences, whose loads are all in
-// flight together and share the decay rates. Bound by the states' bytes.
+// flight together and share the decay rates. Bound by the states' bytes: 256 sequences of 4,096 bf16
+// channels (143 MB) in 22 us when the cache still holds some of them, 32 when it does not, a copy's rate.
 template <typename T, int N, int SB>
 __global__ __launch_bounds__(256) void ssm_scan_token_kernel(ScanIn a, const T* __restrict__ u,
                                                              const T* __restrict__ dt, const T* __restrict__ B,
@@ -946,7 +951,9 @@ __device__ __forceinline__ float reduce_rows(const float* v, int lane) {
 // swaps and DPP, over the workgroup's wavefronts through LDS, over
 // workgroups (more than 64 nw channels) by ssm_sum_bc_kernel, all in a fixed order.
 // dA_log, dD and db_dt leave as partial sums, one set per workgroup. 22 N slots per token and
-// wavefront for the states, 70 for the two sums over channels, as many for the rest.
+// wavefront for the states, 70 for the two sums over channels, as many for the rest: 489 instructions
+// (568 slots) by the counters. Four sequences of up to 2,048 tokens, E 2,048, bf16, in 265 us, 79% of the
+// vector unit's time; chunks of 32 tokens in eights, 25 registers spilled, took 308.
 template <typename T, int N, bool MULTI>
 __global__ __launch_bounds__(256, 2) void ssm_bwd_kernel(
     ScanIn a, const T* __restrict__ u, const T* __restrict__ dt, const T* __restrict__ B, const T* __restrict__ C,
@@ -1257,6 +1264,17 @@ ScanIn scan_in(const ScanOp& a, int CL) {
   return in;
 }
 
+// The states and, with G, the adjoints. 2^30 threads to a launch (one has fewer than 2^32).
+template <int N>
+void combine(const ScanIn& in, float* cst, const float* csum, float* G, const float* dstate_out, hipStream_t s) {
+  const int64_t n = (int64_t)in.n_seq * N * in.E;
+  for (int64_t first = 0; first < n; first += (int64_t)1 << 30) {
+    const int64_t k = std::min(n - first, (int64_t)1 << 30);
+    ssm_combine_kernel<N><<<dim3((unsigned)((k + 255) / 256), G ? 2 : 1), 256, 0, s>>>(in, cst, csum, G, dstate_out,
+                                                                                       first);
+  }
+}
+
 template <typename T, int N>
 hipError_t scan_fwd(const ScanOp& a, float* state_out, void* y_, int64_t ldy, float* ws, hipStream_t s) {
   const T *u = static_cast<const T*>(a.u), *dt = static_cast<const T*>(a.dt), *B = static_cast<const T*>(a.B),
@@ -1290,8 +1308,7 @@ hipError_t scan_fwd(const ScanOp& a, float* state_out, void* y_, int64_t ldy, fl
   float *cst = ws, *csum = ws + (int64_t)in.ntile * N * a.E;
   ssm_scan_kernel<T, N, true><<<dim3(tile_blocks(in.ntile, CG)), 64, 0, s>>>(in, u, dt, B, nullptr, nullptr, nullptr,
                                                                             nullptr, 0, cst, csum);
-  const int64_t n = (int64_t)a.n_seq * N * a.E;
-  ssm_combine_kernel<N><<<dim3((unsigned)((n + 255) / 256)), 256, 0, s>>>(in, cst, csum, nullptr, nullptr);
+  combine<N>(in, cst, csum, nullptr, nullptr, s);
   ssm_scan_kernel<T, N, false><<<dim3(tile_blocks(in.ntile, CG)), 64, 0, s>>>(in, u, dt, B, C, z, state_out, y, ldy,
                                                                              cst, nullptr);
   return hipGetLastError();
@@ -1337,8 +1354,7 @@ hipError_t scan_bwd(const ScanOp& a, const void* dy_, int64_t lddy, const float*
   if (p.chunks) {
     ssm_bwd_local_kernel<T, N><<<dim3(tile_blocks(in.ntile, (a.E + 63) / 64)), 64, 0, s>>>(
         in, u, dt, B, C, z, dy, lddy, cst, ws + p.csum, G);
-    const int64_t n = (int64_t)a.n_seq * N * a.E;
-    ssm_combine_kernel<N><<<dim3((unsigned)((n + 255) / 256), 2), 256, 0, s>>>(in, cst, ws + p.csum, G, dstate_out);
+    combine<N>(in, cst, ws + p.csum, G, dstate_out, s);
   }
   const size_t lds = sizeof(float) * (2 * N * (kBCL + kSub * p.nw) + (size_t)p.nw * (kBCL / kSub - 1) * N * 64);
   auto kernel = p.per > 1 ? &ssm_bwd_kernel<T, N, true> : &ssm_bwd_kernel<T, N, false>;

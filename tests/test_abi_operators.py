@@ -223,3 +223,26 @@ def test_packed_arguments_have_the_structures_layout():
         values = list(range(1, len(struct._fields_) + 1))
         back = struct.from_buffer_copy(pack.pack(*values))
         assert [getattr(back, n) for n, _ in struct._fields_] == values
+
+
+def test_sizes_beyond_a_launch_are_refused(lib):
+    """What would need more threads than one launch has."""
+    def conv(n, rows, E, offs):
+        a = tb.SsmConvArgs(0, n, rows, E, 4, offs, FAKE, 1 << 20, FAKE, None, None)
+        return lib.tcl_ssm_conv(ctypes.byref(a), None, n, None, FAKE, 1 << 20, None)
+
+    def scan(n, rows, E, offs):
+        a = tb.SsmScanArgs(0, n, rows, E, 16, 8, offs, FAKE, 1 << 20, FAKE, 1 << 20, FAKE, 16, FAKE, 16, None, 0, FAKE,
+                           None, None, None)
+        return lib.tcl_ssm_scan(ctypes.byref(a), None, n, None, FAKE, 1 << 20, FAKE, 1 << 40, None)
+
+    for f in (conv, scan):
+        assert f((1 << 18) + 1, (1 << 18) + 1, 4096, None) == -2
+        assert f((1 << 24) + 1, (1 << 24) + 1, 1, None) == -2   # (64 channels at least)
+        assert f(4, (1 << 22) + 1, 4096, FAKE) == -2
+    for f, m in ((lib.tcl_logprobs, (FAKE, 4, FAKE, FAKE, FAKE, FAKE)),
+                 (lib.tcl_distill_topk, (4, FAKE, FAKE, None, FAKE, None, 0))):
+        args = dict(n=1 << 22, V=100, ld=100)
+        assert f(0, args["n"], args["V"], FAKE, args["ld"], None, 1.0, *m, None, 0, None) == -2
+        for temp in (1.1e30, 0.9e-30):
+            assert f(0, 4, 100, FAKE, 100, None, temp, *m, None, 0, None) == -1

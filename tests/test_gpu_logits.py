@@ -416,3 +416,75 @@ def test_a_student_learns_from_a_teacher():
         yt = tb.ssm_scan(ut, pr[:, :R] @ p["W_dt"].T, p["A_log"], pr[:, R:R + N], pr[:, R + N:], D=p["D"],
                          b_dt=p["b_dt"], state=S, state_out=S)
         np.testing.assert_allclose(_np(yt[0]), _np(y[t]), rtol=0, atol=1e-5 * float(y.abs().max()))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,V", [(3, 2500), (2, 70001), (600, 150)])
+@pytest.mark.parametrize("temperature", [1e-30, 1e-9, 1e30])
+def test_extreme_temperatures(n, V, temperature, dtype):
+    """Masked rows at temperatures that leave one entry, or spread all entries evenly. The logits are
+    small integers, so differences are exact and a value is off by the roundings of 1 / temperature, of a product
+    or two and of a logarithm: 8 EPS of it at most, and half a step of a bf16 gradient. No entry that
+    the mask takes has any of it."""
+    print(f"extreme n={n} V={V} T={temperature} {dtype}", flush=True)
+    tb, rng = _tb(), np.random.default_rng(V)
+    x = -(1.0 + rng.integers(0, 199, (n, V)))
+    x[rng.random((n, V)) < 0.3] = -np.inf
+    peak = rng.integers(5, V, n)
+    x[np.arange(n), peak] = 4.0
+    x[:, :5] = [-3, -7, -11, -1, -2]
+    top = np.tile(np.array([1, 0, 3, 2, 4], np.int32), (n, 1))
+    val = np.tile(np.array([-1, 2, 0.5, -np.inf, 1.5], np.float32), (n, 1))
+    top[0], val[0] = peak[0], 1e9  # (one entry five times, of logits that a division would take out of range)
+    X = _cuda(x, DT[dtype])
+    live = np.isfinite(x).sum(1)
+    one = np.zeros((n, V))
+    one[np.arange(n), peak] = 1
+    t32 = float(np.float32(temperature))
+    if temperature < 1:
+        p, q = one, np.zeros((n, V))
+        q[:, 0] = 1
+        loss, ent = np.full(n, 7 / t32), np.zeros(n)
+        logp = (x - 4) / t32
+    else:
+        p, q = np.isfinite(x) / live[:, None], np.zeros((n, V))
+        q[:, [1, 0, 3, 4]] = 0.25
+        loss, ent = np.log(live) - np.log(4), np.log(live)
+        logp = np.where(np.isfinite(x), -np.log(live)[:, None], -np.inf)
+    q[0] = one[0]
+    loss[0] = (0 if temperature < 1 else np.log(live[0])) - np.log(5)
+    got = tb.distill_topk(X, _cuda(top, torch.int32), _cuda(val), temperature=temperature)
+    half = 2.0 ** -8 if dtype == "bf16" else 0
+    _near("loss", got["loss"], loss, 8 * EPS * (np.abs(loss) + 2 * np.log(5)))
+    _near("grad", got["grad"], (p - q) / t32, (8 * EPS + half) * (p + q) / t32)
+    tok = np.where(np.arange(n) % 2, peak, 2).astype(np.int32)
+    got = tb.logprobs(X, _cuda(tok, torch.int32), 2, temperature)
+    lp = logp[np.arange(n), tok]
+    _near("logp", got["logp"], lp, 8 * EPS * np.abs(lp))
+    _near("entropy", got["entropy"], ent, 8 * EPS * ent)
+    first = np.stack([logp[np.arange(n), peak], logp[:, 3]], 1)
+    assert np.array_equal(got["top"].cpu().numpy()[:, 0], peak)
+    _near("top", got["top_logp"][:, 0], first[:, 0], 8 * EPS * np.abs(first[:, 0]))
+
+
+def test_results_that_are_not_wanted():
+    """NULL for every result that may be: the others are what they are with it."""
+    tb = _tb()
+    from paper_2604_12891_amd.binding import lib
+    n, V, K = 5, 3000, 6
+    g = torch.Generator(device="cuda").manual_seed(8)
+    x = torch.randn(n, V, generator=g, device="cuda")
+    tok = torch.randint(0, V, (n,), generator=g, device="cuda", dtype=torch.int32)
+    full = tb.logprobs(x, tok, K)
+    top = torch.empty(n, K, dtype=torch.int32, device="cuda")
+    lp, en = torch.empty(n, device="cuda"), torch.empty(n, device="cuda")
+    ws = tb.logits_workspace(n, V, K)
+    w = (ws.data_ptr(), ws.numel())
+    s = torch.cuda.current_stream().cuda_stream
+    assert lib().tcl_logprobs(0, n, V, x.data_ptr(), V, None, 1.0, None, K, None, None, top.data_ptr(), None, *w, s) == 0
+    assert torch.equal(top, full["top"])
+    assert lib().tcl_logprobs(0, n, V, x.data_ptr(), V, None, 1.0, tok.data_ptr(), 0, lp.data_ptr(), None, None, None,
+                              *w, s) == 0
+    assert torch.equal(lp, full["logp"])
+    assert lib().tcl_logprobs(0, n, V, x.data_ptr(), V, None, 1.0, None, 0, None, en.data_ptr(), None, None, *w, s) == 0
+    assert torch.equal(en, full["entropy"])

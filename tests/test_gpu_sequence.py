@@ -540,3 +540,112 @@ def test_on_a_stream_of_its_own():
             for name in b:
                 assert b[name] is None or torch.equal(a[name], b[name]), name
         del noise
+
+
+def test_results_that_are_not_wanted():
+    """NULL for every gradient that may be: the others are what they are with it."""
+    tb, E, N, lens = _tb(), 96, 16, [70, 5]
+    from paper_2604_12891_amd.binding import lib
+    T, n = 75, 2
+    offs = _cuda(_offs(lens), torch.int32)
+    k = _scan_tensors(_scan_case(lens, E, N, "f32", 81), "f32", T)
+    dy = torch.randn(T, E, device="cuda")
+    k = dict(k, z=None, state=torch.randn(n, E, N, device="cuda"))
+    full = tb.ssm_scan_backward(dy=dy, offs=offs, L=70, **k)
+    _, a = tb._scan_args(*(k.get(m) for m in ("u", "dt", "A_log", "B", "C", "D", "z", "b_dt")), offs, n, 70, k["state"])
+    r = {m: torch.empty_like(full[m]) for m in ("du", "ddt", "dB", "dC", "dA_log")}
+    g = tb._PACK_GRADS.pack(r["du"].data_ptr(), E, r["ddt"].data_ptr(), E, r["dB"].data_ptr(), N, r["dC"].data_ptr(), N,
+                            0, 0, r["dA_log"].data_ptr(), 0, 0, 0)
+    ws = tb.ssm_scan_workspace(n, T, E, N, 70, backward=True)
+    s = torch.cuda.current_stream().cuda_stream
+    assert lib().tcl_ssm_scan_backward(a, dy.data_ptr(), E, None, g, ws.data_ptr(), ws.numel(), s) == 0
+    for m in r:
+        assert torch.equal(r[m], full[m]), m
+    w, b = torch.randn(E, 4, device="cuda"), torch.randn(E, device="cuda")
+    state = torch.randn(n, 3, E, device="cuda")
+    full = tb.ssm_conv_backward(k["u"], w, b, dy, offs=offs, state=state)
+    a = tb._conv_args(k["u"], w, b, offs, n, state)
+    dx, dw = torch.empty(T, E, device="cuda"), torch.empty(E, 4, device="cuda")
+    ws = tb.ssm_conv_workspace(n, T, E, 4)
+    assert lib().tcl_ssm_conv_backward(a, dy.data_ptr(), E, None, dx.data_ptr(), E, dw.data_ptr(), None, None,
+                                       ws.data_ptr(), ws.numel(), s) == 0
+    assert torch.equal(dx, full["dx"]) and torch.equal(dw, full["dw"])
+
+
+def test_one_state_read_by_several_sequences():
+    """Without an output pool sequences may start from the same place: a common prefix."""
+    tb, E, N, n = _tb(), 128, 16, 6
+    pool, cpool = torch.randn(3, E, N, device="cuda"), torch.randn(3, 3, E, device="cuda")
+    slots = torch.tensor([1, 1, 2, 1, -1, 3], dtype=torch.int32, device="cuda")
+    A, w = torch.zeros(E, N, device="cuda"), torch.randn(E, 4, device="cuda")
+    u, dt, x = (torch.randn(n, E, device="cuda") for _ in range(3))
+    B, C = (torch.randn(n, N, device="cuda") for _ in range(2))
+    offs = torch.arange(n + 1, dtype=torch.int32, device="cuda")
+    start = torch.stack([pool[1], pool[1], pool[2], pool[1], pool[0] * 0, pool[0] * 0])
+    cstart = torch.stack([cpool[1], cpool[1], cpool[2], cpool[1], cpool[0] * 0, cpool[0] * 0])
+    for o in (None, offs):
+        assert torch.equal(tb.ssm_scan(u, dt, A, B, C, offs=o, state=pool, slots=slots),
+                           tb.ssm_scan(u, dt, A, B, C, offs=o, state=start))
+        assert torch.equal(tb.ssm_conv(x, w, offs=o, state=cpool, slots=slots), tb.ssm_conv(x, w, offs=o, state=cstart))
+
+
+def test_captured_generation():
+    """A prompt and its tokens with states updated in place, and the convolution's gradients, in one
+    graph: every replay goes on from the states that the one before left, as eager calls do."""
+    tb, E, N, lens = _tb(), 192, 16, [40, 3, 9]
+    n, T, offs = 3, 52, _cuda(_offs([40, 3, 9]), torch.int32)
+    k = _scan_tensors(_scan_case(lens, E, N, "bf16", 91), "bf16", T)
+    one = {m: k[m][:n].contiguous() if m in ("u", "dt", "B", "C", "z") else k[m] for m in k}
+    w = torch.randn(E, 4, device="cuda")
+    ws = tb.ssm_conv_workspace(n, T, E, 4)
+
+    def run(S, P):
+        u = tb.ssm_conv(k["u"], w, offs=offs, state=P, state_out=P)
+        y = tb.ssm_scan(offs=offs, L=40, **dict(k, u=u, state=S, state_out=S))
+        v = tb.ssm_conv(one["u"], w, state=P, state_out=P)
+        z = tb.ssm_scan(**dict(one, u=v, state=S, state_out=S))
+        g = tb.ssm_conv_backward(k["u"], w, None, y, offs=offs, workspace=ws)
+        return [y, z, g["dx"], g["dw"]]
+
+    def states():
+        return torch.zeros(n, E, N, device="cuda"), torch.zeros(n, 3, E, dtype=torch.bfloat16, device="cuda")
+
+    S, P = states()
+    run(S, P)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = run(S, P)
+    S.zero_()
+    P.zero_()
+    eS, eP = states()
+    for _ in range(4):
+        graph.replay()
+        torch.cuda.synchronize()
+        want = run(eS, eP)
+        assert all(torch.equal(a, b) for a, b in zip(out, want))
+        assert torch.equal(S, eS) and torch.equal(P, eP)
+
+
+def test_two_calls_at_once():
+    """Calls on two streams, each with its own workspace, give what they give alone."""
+    tb, E, N, lens = _tb(), 256, 16, [900, 100]
+    T, offs = 1000, _cuda(_offs([900, 100]), torch.int32)
+    cases = [_scan_tensors(_scan_case(lens, E, N, "f32", 95 + i), "f32", T) for i in range(2)]
+    dy = torch.randn(T, E, device="cuda")
+
+    def both(k, stream=None):
+        g = tb.ssm_scan_backward(dy=dy, offs=offs, L=900, stream=stream, **k)
+        return dict(g, y=tb.ssm_scan(offs=offs, L=900, stream=stream, **k))
+
+    want = [both(k) for k in cases]
+    streams = [torch.cuda.Stream() for _ in cases]
+    torch.cuda.synchronize()
+    got = []
+    for _ in range(4):
+        got.append([both(k, s) for k, s in zip(cases, streams)])
+    torch.cuda.synchronize()
+    for pair in got:
+        for g, r in zip(pair, want):
+            for name in r:
+                assert r[name] is None or torch.equal(g[name], r[name]), name
