@@ -943,6 +943,29 @@ __device__ __forceinline__ float reduce_rows(const float* v, int lane) {
   return s + dpp<0xB1>(s);  // lane ^ 1
 }
 
+// Sequences by falling length, lengths past kBCL as equals, by a count per length; equals in
+// no fixed order, which nothing depends on (results lie where the sequence's do). One workgroup.
+__global__ __launch_bounds__(1024) void ssm_order_kernel(const int* __restrict__ offs, int n_seq, int rows,
+                                                         int* __restrict__ ord) {
+  __shared__ int count[kBCL + 2];
+  const int tid = threadIdx.x;
+  auto bin = [&](int i) {  // 0: the longest
+    const int o0 = min(max(offs[i], 0), rows), o1 = min(max(offs[i + 1], o0), rows);
+    return kBCL + 1 - min(o1 - o0, kBCL + 1);
+  };
+  if (tid < kBCL + 2) count[tid] = 0;
+  __syncthreads();
+  for (int i = tid; i < n_seq; i += 1024) atomicAdd(&count[bin(i)], 1);
+  __syncthreads();
+  int before = 0;
+  if (tid < kBCL + 2)
+    for (int j = 0; j < tid; ++j) before += count[j];
+  __syncthreads();
+  if (tid < kBCL + 2) count[tid] = before;
+  __syncthreads();
+  for (int i = tid; i < n_seq; i += 1024) ord[atomicAdd(&count[bin(i)], 1)] = i;
+}
+
 // A workgroup takes `per` chunks of 64 nw channels one after the other, a lane per channel. The chunk's
 // start state is walked forward once to leave the state in front of every
 // kSub tokens (but the first) in LDS; then, from the last kSub tokens to the first, the states
@@ -961,7 +984,7 @@ __global__ __launch_bounds__(256, 2) void ssm_bwd_kernel(
     const float* __restrict__ H, const float* __restrict__ dstate_out, T* __restrict__ du_o, int64_t lddu,
     T* __restrict__ ddt_o, int64_t ldddt, T* __restrict__ dz_o, int64_t lddz, T* __restrict__ dB_o, int64_t lddB,
     T* __restrict__ dC_o, int64_t lddC, float* __restrict__ dstate, float* __restrict__ part, int parts, int per,
-    float* __restrict__ bc_part) {
+    const int* __restrict__ ord, float* __restrict__ bc_part) {
   constexpr int W = 2 * N, NSUB = kBCL / kSub;
   extern __shared__ __attribute__((aligned(16))) float smem[];
   const int nw = blockDim.x >> 6, wave = threadIdx.x >> 6, lane = threadIdx.x & 63, E = a.E;
@@ -971,6 +994,7 @@ __global__ __launch_bounds__(256, 2) void ssm_bwd_kernel(
   int p, cg;
   const int CG = (E + blockDim.x - 1) / blockDim.x;
   if (!tile_of_block(parts, CG, p, cg)) return;
+  if (!MULTI && ord) p = __builtin_amdgcn_readfirstlane(ord[p]);
   const int e = cg * blockDim.x + threadIdx.x;
   const bool active = e < E;
   const int ec = active ? e : E - 1;
@@ -988,7 +1012,7 @@ __global__ __launch_bounds__(256, 2) void ssm_bwd_kernel(
   // row, the pair of states within the row
   const int place = lane / 32 * N + lane % 16 / (32 / N) * 2 + lane / 16 % 2;
   auto chunk = [&](int w) {
-    const Tile tl = find_tile(a.offs, a.n_seq, a.rows, kBCL, w);
+    const Tile tl = find_tile(a.offs, a.n_seq, a.rows, a.CL, w);
     if (tl.seq < 0) return;
     const int t0 = tl.j * kBCL, nt = max(0, min(tl.len - t0, kBCL));
     const int64_t r0 = (int64_t)tl.base + t0;
@@ -1317,19 +1341,25 @@ hipError_t scan_fwd(const ScanOp& a, float* state_out, void* y_, int64_t ldy, fl
 struct BwdPlan {
   int nw, CG, ntile, per, parts;
   bool chunks;
-  size_t cst, csum, G, part, bc, total;  // in floats
+  bool order;
+  size_t cst, csum, G, part, bc, ord, total;  // in floats
 };
 BwdPlan bwd_plan(bool packed, int n_seq, int rows, int E, int N, int L) {
   BwdPlan p;
   p.nw = std::min(4, (E + 63) / 64);
   p.CG = (E + 64 * p.nw - 1) / (64 * p.nw);
-  p.ntile = packed ? rows / kBCL + n_seq : n_seq;
   p.chunks = packed && L > kBCL;
-  // Short sequences, a chunk each, go several to a workgroup once there are eight rounds of them: the partial
-  // sums of the parameters' gradients are as large as a chunk of two tokens. 4,096 of 25 tokens, E 512: 1,241
-  // to 1,105 us (bf16), 1,222 to 1,063 (fp32). Not chunks of long ones, which lose 5% to the registers
-  // that the loop takes.
-  p.per = p.chunks ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(16, (int64_t)p.ntile * p.CG / (kCUs * 16)));
+  p.ntile = p.chunks ? rows / kBCL + n_seq : n_seq;
+  // Short sequences, a chunk each, are handed out longest first, so that the workgroups (two on a CU at a time)
+  // end together: 1,024 of 1 to 25 tokens, E 256, fp32, 118 to 83 us, 4,096 of them 387 to 288. With more
+  // than 32 rounds of workgroups, or 16 of sequences with too few tokens to pay for partial sums as large
+  // as two tokens, they go several to a workgroup in their order: 30,000 of 1 to 15, E 256, fp32, 1,326 us
+  // against 1,459, 9,000 of 1 to 7 267 against 286 (of 1 to 15 459 against 437). Not chunks of long ones, which lose
+  // 5% to the registers that the loop takes.
+  const int64_t groups = (int64_t)p.ntile * p.CG, round = kCUs * 2;
+  p.order = packed && !p.chunks && groups > round && groups <= 32 * round &&
+            (groups < 16 * round || rows >= 6 * (int64_t)n_seq);
+  p.per = p.chunks || p.order ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(16, groups / (8 * round)));
   p.parts = (p.ntile + p.per - 1) / p.per;
   size_t o = 0;
   const size_t st = p.chunks ? (size_t)p.ntile * N * E : 0;
@@ -1338,6 +1368,7 @@ BwdPlan bwd_plan(bool packed, int n_seq, int rows, int E, int N, int L) {
   p.csum = o; o += p.chunks ? (size_t)p.ntile * E : 0;
   p.part = o; o += (size_t)p.parts * (N + 2) * E;
   p.bc = o; o += p.CG > 1 ? (size_t)p.CG * rows * 2 * N : 0;
+  p.ord = o; o += p.order ? n_seq : 0;
   p.total = o;
   return p;
 }
@@ -1348,7 +1379,7 @@ hipError_t scan_bwd(const ScanOp& a, const void* dy_, int64_t lddy, const float*
   const T *u = static_cast<const T*>(a.u), *dt = static_cast<const T*>(a.dt), *B = static_cast<const T*>(a.B),
           *C = static_cast<const T*>(a.C), *z = static_cast<const T*>(a.z), *dy = static_cast<const T*>(dy_);
   const BwdPlan p = bwd_plan(a.offs != nullptr, a.n_seq, a.rows, a.E, N, a.L);
-  const ScanIn in = scan_in(a, kBCL);
+  const ScanIn in = scan_in(a, p.chunks || !a.offs ? kBCL : a.rows + 1);  // (+ 1: a tile per sequence)
   float *cst = p.chunks ? ws + p.cst : nullptr, *G = p.chunks ? ws + p.G : nullptr, *part = ws + p.part,
         *bc = p.CG > 1 ? ws + p.bc : nullptr;
   if (p.chunks) {
@@ -1356,6 +1387,8 @@ hipError_t scan_bwd(const ScanOp& a, const void* dy_, int64_t lddy, const float*
         in, u, dt, B, C, z, dy, lddy, cst, ws + p.csum, G);
     combine<N>(in, cst, ws + p.csum, G, dstate_out, s);
   }
+  int* ord = p.order ? reinterpret_cast<int*>(ws + p.ord) : nullptr;
+  if (ord) ssm_order_kernel<<<dim3(1), 1024, 0, s>>>(a.offs, a.n_seq, a.rows, ord);
   const size_t lds = sizeof(float) * (2 * N * (kBCL + kSub * p.nw) + (size_t)p.nw * (kBCL / kSub - 1) * N * 64);
   auto kernel = p.per > 1 ? &ssm_bwd_kernel<T, N, true> : &ssm_bwd_kernel<T, N, false>;
   hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
@@ -1364,7 +1397,7 @@ hipError_t scan_bwd(const ScanOp& a, const void* dy_, int64_t lddy, const float*
   kernel<<<dim3(tile_blocks(p.parts, p.CG)), 64 * p.nw, lds, s>>>(
       in, u, dt, B, C, z, dy, lddy, cst, G, dstate_out, static_cast<T*>(g.du), g.lddu, static_cast<T*>(g.ddt),
       g.ldddt, static_cast<T*>(g.dz), g.lddz, static_cast<T*>(g.dB), g.lddB, static_cast<T*>(g.dC), g.lddC, g.dstate,
-      part, p.parts, p.per, bc);
+      part, p.parts, p.per, ord, bc);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
   if (bc && a.rows > 0) {

@@ -649,3 +649,30 @@ def test_two_calls_at_once():
         for g, r in zip(pair, want):
             for name in r:
                 assert r[name] is None or torch.equal(g[name], r[name]), name
+
+
+@pytest.mark.parametrize("N", [8, 16])
+def test_scan_gradients_of_short_sequences_by_length(N):
+    """More short sequences, some of them empty, than the GPU takes at once: the longest go first,
+    with the same bits every time. The first row that a sequence owns is row 2."""
+    n, E = 700, 70
+    print(f"scan gradients by length n={n} E={E} N={N}", flush=True)
+    rng = np.random.default_rng(18)
+    lens = rng.integers(0, 31, n).tolist()
+    a = _scan_case(lens, E, N, "f32", 19)
+    a["state"] = rng.standard_normal((n, E, N)).astype(np.float32)
+    T, offs = sum(lens), _offs(lens)
+    dy, dend = rng.standard_normal((T, E)).astype(np.float32), rng.standard_normal((n, E, N)).astype(np.float32)
+    k = _scan_tensors(a, "f32", T)
+    for name in ("u", "dt", "z", "B", "C"):
+        k[name] = torch.cat([torch.full_like(k[name][:2], NAN), k[name]])
+    args = dict(k, dy=torch.cat([torch.full((2, E), NAN, device="cuda"), _cuda(dy)]), state_grad=_cuda(dend),
+                offs=_cuda(offs + 2, torch.int32), L=30)
+    out = {m: torch.full((T + 2, w), 7.0, device="cuda") for m, w in dict(du=E, ddt=E, dz=E, dB=N, dC=N).items()}
+    g = _tb().ssm_scan_backward(out=out, **args)
+    assert all((g[m][:2] == 7.0).all() for m in out)
+    again = _tb().ssm_scan_backward(**args)
+    assert all(torch.equal(g[m][2:] if m in out else g[m], again[m][2:] if m in out else again[m]) for m in g)
+    r = osq.scan_backward(dy=dy, offs=offs, dend=dend, **a)
+    _check_scan_grads({m: v[2:] if m in out else v for m, v in g.items()}, r, "f32", T,
+                      ["du", "ddt", "dz", "dB", "dC", "dA_log", "dD", "db_dt", "dstate"])
