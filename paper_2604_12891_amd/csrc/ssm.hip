@@ -389,6 +389,7 @@ __global__ __launch_bounds__(256) void ssm_conv_bwd_kernel(
 // Sums of `parts` partial vectors part[p][M + extra][E] in a fixed order, laid out as
 // the parameters are: o0[e, m] for m < M, then o1[e], o2[e] (null: not wanted).
 constexpr int kSumLanes = 16;
+template <int U>  // loads in flight: a trip is one latency
 __global__ __launch_bounds__(64 * kSumLanes) void sum_parts_kernel(const float* __restrict__ part, int parts, int M,
                                                                    int total, int E, float* __restrict__ o0,
                                                                    float* __restrict__ o1, float* __restrict__ o2) {
@@ -398,7 +399,6 @@ __global__ __launch_bounds__(64 * kSumLanes) void sum_parts_kernel(const float* 
   float acc = 0.f;
   if (i < stride) {
     const float* src = part + i;
-    constexpr int U = 16;  // loads in flight: a trip is one latency
     for (int p = g; p < parts; p += U * kSumLanes) {
       float v[U];
 #pragma unroll
@@ -1230,6 +1230,13 @@ ConvParts conv_parts(int n_seq, int rows, int E) {
   return p;
 }
 
+// One trip up to 512 parts, by halves.
+void sum_parts(const float* part, int parts, int M, int total, int E, float* o0, float* o1, float* o2, hipStream_t s) {
+  const dim3 grid((unsigned)(((int64_t)total * E + 63) / 64));
+  if (parts > 16 * kSumLanes) sum_parts_kernel<32><<<grid, 64 * kSumLanes, 0, s>>>(part, parts, M, total, E, o0, o1, o2);
+  else sum_parts_kernel<16><<<grid, 64 * kSumLanes, 0, s>>>(part, parts, M, total, E, o0, o1, o2);
+}
+
 template <typename T, int K, int CH>
 hipError_t conv_fwd(const ConvOp& a, void* state_out, void* u, int64_t ldu, hipStream_t s) {
   const int CG = a.E / CH, R = a.offs ? conv_rows(a.rows, CG) : 8;
@@ -1252,9 +1259,7 @@ hipError_t conv_bwd(const ConvOp& a, const void* du, int64_t lddu, const void* d
       static_cast<T*>(dx), lddx, static_cast<T*>(dstate), ws);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const int64_t n = (int64_t)(K + 1) * a.E;
-  sum_parts_kernel<<<dim3((unsigned)((n + 63) / 64)), 64 * kSumLanes, 0, s>>>(ws, p.parts, K, K + 1, a.E, dw, db,
-                                                                             nullptr);
+  sum_parts(ws, p.parts, K, K + 1, a.E, dw, db, nullptr, s);
   return hipGetLastError();
 }
 
@@ -1405,9 +1410,7 @@ hipError_t scan_bwd(const ScanOp& a, const void* dy_, int64_t lddy, const float*
     ssm_sum_bc_kernel<T, N><<<dim3((unsigned)((n + 255) / 256)), 256, 0, s>>>(
         a.offs, a.n_seq, a.rows, p.CG, bc, static_cast<T*>(g.dB), g.lddB, static_cast<T*>(g.dC), g.lddC);
   }
-  const int64_t n = (int64_t)(N + 2) * a.E;
-  sum_parts_kernel<<<dim3((unsigned)((n + 63) / 64)), 64 * kSumLanes, 0, s>>>(part, p.parts, N, N + 2, a.E, g.dA_log,
-                                                                             g.dD, g.db_dt);
+  sum_parts(part, p.parts, N, N + 2, a.E, g.dA_log, g.dD, g.db_dt, s);
   return hipGetLastError();
 }
 
