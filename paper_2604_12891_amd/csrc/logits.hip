@@ -527,17 +527,20 @@ __device__ __forceinline__ float teacher_entries(const TeacherShared& sh, const 
 template <int NW>
 __device__ __forceinline__ float teacher_sum(const TeacherShared& sh, int K, float m, float inv_temp) {
   float s = 0.f;
-  for (int k = threadIdx.x; k < K; k += 64 * NW) s += m > -INFINITY ? expf((sh.q[k] - m) * inv_temp) : 0.f;
+  const ScaledExp<float> ex(inv_temp);
+  for (int k = threadIdx.x; k < K; k += 64 * NW) s += m > -INFINITY ? ex(sh.q[k] - m) : 0.f;
   return s;
 }
-// The thread's part of the loss; sh.q becomes q. mt, lt: the teacher's maximum and the log of its sum
-// of exponentials (mt = +inf makes all that follows NaN); ms, ls: the student's.
+// The thread's part of the loss; sh.q becomes q. mt, qs: the teacher's maximum and its sum of
+// exponentials (mt = +inf makes all that follows NaN); ms, ls: the student's maximum and its sum's log.
 template <int NW>
-__device__ __forceinline__ float teacher_loss(const TeacherShared& sh, int K, float mt, float lt, float ms, float ls,
+__device__ __forceinline__ float teacher_loss(const TeacherShared& sh, int K, float mt, float qs, float ms, float ls,
                                               float inv_temp) {
   float loss = 0.f;
+  const ScaledExp<float> ex(inv_temp);
+  const float lt = logf(qs);
   for (int k = threadIdx.x; k < K; k += 64 * NW) {
-    const float lq = fmaf(sh.q[k] - mt, inv_temp, -lt), q = sh.at[k] >= 0 ? expf(lq) : 0.f;
+    const float d = sh.q[k] - mt, lq = fmaf(d, inv_temp, -lt), q = sh.at[k] >= 0 ? ex(d) / qs : 0.f;
     sh.q[k] = q;
     if (q != 0.f) loss += q * (lq - fmaf(sh.x[k] - ms, inv_temp, -ls));
   }
@@ -658,7 +661,7 @@ __global__ __launch_bounds__(64 * NW) void distill_row_kernel(LogitRows a, Teach
   block_reduce<NW, false>(s, qs, red[1]);
   const bool live = mt > -INFINITY && s != 0.f;
   hold();
-  float loss = teacher_loss<NW>(sh, t.K, mt, logf(qs), m, logf(s), a.inv_temp), none = 0.f;
+  float loss = teacher_loss<NW>(sh, t.K, mt, qs, m, logf(s), a.inv_temp), none = 0.f;
   block_reduce<NW, false>(loss, none, red[2]);
   if (tid == 0) t.loss[r] = live ? loss : 0.f;
   if (!t.grad) return;
@@ -759,7 +762,7 @@ __global__ __launch_bounds__(kTB) void distill_grad_kernel(LogitRows a, TeacherA
   const bool live = mt > -INFINITY && s != 0.f;
   float qs = teacher_sum<NW>(sh, t.K, mt, a.inv_temp);
   block_reduce<NW, false>(qs, none, red[1]);
-  float loss = teacher_loss<NW>(sh, t.K, mt, logf(qs), m, logf(s), a.inv_temp);
+  float loss = teacher_loss<NW>(sh, t.K, mt, qs, m, logf(s), a.inv_temp);
   block_reduce<NW, false>(loss, none, red[2]);
   if (blockIdx.y == 0 && tid == 0) t.loss[r] = live ? loss : 0.f;
   if (!t.grad) return;
