@@ -542,7 +542,8 @@ __device__ __forceinline__ float teacher_loss(const TeacherShared& sh, int K, fl
   for (int k = threadIdx.x; k < K; k += 64 * NW) {
     const float d = sh.q[k] - mt, lq = fmaf(d, inv_temp, -lt), q = sh.at[k] >= 0 ? ex(d) / qs : 0.f;
     sh.q[k] = q;
-    if (q != 0.f) loss += q * (lq - fmaf(sh.x[k] - ms, inv_temp, -ls));
+    // (q first: log p of a mask of the type's lowest value may be beyond fp32 where q log p is not)
+    if (q != 0.f) loss += fmaf(q * (sh.x[k] - ms), -inv_temp, q * (lq + ls));
   }
   return loss;
 }

@@ -488,3 +488,17 @@ def test_results_that_are_not_wanted():
     assert torch.equal(lp, full["logp"])
     assert lib().tcl_logprobs(0, n, V, x.data_ptr(), V, None, 1.0, None, 0, None, en.data_ptr(), None, None, *w, s) == 0
     assert torch.equal(en, full["entropy"])
+
+
+@pytest.mark.parametrize("n,V,K", [(5, 255, 257), (244, 1000, 20), (3, 70001, 64)])
+def test_distill_of_masks_beyond_fp32(n, V, K):
+    """Where the mask is the type's lowest value and the temperature below 1, log p is beyond fp32 (-6.8e38),
+    and the loss, with the teacher's small probability there, is often not."""
+    print(f"distill beyond n={n} V={V} K={K}", flush=True)
+    rng = np.random.default_rng(n + V)
+    x = _logits(rng, n, V, "f32", "lowest")
+    top, val = _teacher(rng, x, K)
+    val *= 2  # (probabilities down to e^-40)
+    got = _tb().distill_topk(_cuda(x), _cuda(top, torch.int32), _cuda(val), temperature=0.5)
+    _check_distill(got, list(x), top, val, None, 0.5, "f32")
+    assert torch.isfinite(got["loss"]).any()
