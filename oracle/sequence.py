@@ -6,9 +6,8 @@ Sequences are packed: sequence i is rows offs[i] .. offs[i+1]-1. `state` holds o
 start state per sequence (None: zeros); end states are returned per sequence.
 
 Every function also returns, under "bound", how far fp32 arithmetic of the
-same formulas may be off, element by element: the sums of the absolute values
-of everything that enters a result, times the relative error of one path
-through the formula (see EPS_*).
+same formulas may be off, element by element: every term's absolute value times
+the relative error with which it is formed (see EPS_*), to first order.
 """
 from __future__ import annotations
 
@@ -88,104 +87,133 @@ def conv_backward(x, w, b, du, offs, state=None, dend=None):
     return dict(dx=dx, dw=dw, db=db, dstate=ds, bound=dict(dx=bx, dw=bw, db=bb, dstate=bs))
 
 
+def _steps(dt, b_dt):
+    """v = dt + b_dt, d = softplus(v), sigmoid(v), and the relative error of d in fp32: v rounds
+    once, which moves d by softplus'(v) = sigmoid(v) as much, and softplus is off by EPS_ACT."""
+    v = dt if b_dt is None else dt + b_dt
+    d, sv = softplus(v), sigmoid(v)
+    return v, d, sv, EPS_ACT + EPS * np.abs(v) * sv / d
+
+
+def _decay(d, rel, A, A_log, length):
+    """One token's decays exp(d A) [E, N] and their relative error: the exponent's own (d; A, whose
+    exponent A_log rounds twice, and three roundings more; the product; where decays are multiplied by
+    adding up their steps, a rounding per token of the sequence) times the exponent, and six
+    roundings: exp2 (one unit, two roundings), the product with a state, the sum that it enters, and as
+    many again where a sequence's parts are joined."""
+    x = d[:, None] * A
+    return np.exp(x), np.abs(x) * (rel[:, None] + (2 * np.abs(A_log) + 5 + length) * EPS) + 6 * EPS
+
+
 def scan(u, dt, A_log, B, C, offs, D=None, z=None, b_dt=None, state=None):
-    """-> dict(y, end, bound: dict(y, end))"""
+    """-> dict(y, end, bound: dict(y, end))
+
+    The states' bound runs along with them: a step passes on the error that is there and adds
+    the decay's and the input's relative errors, times what these multiply with every term's
+    absolute value (as parts of a sequence may be summed apart)."""
     u, dt, A_log, B, C, D, z, b_dt, state = _f64(u, dt, A_log, B, C, D, z, b_dt, state)
     T, E = u.shape
     N = A_log.shape[1]
     A = -np.exp(A_log)
     D = np.zeros(E) if D is None else D
-    v = dt if b_dt is None else dt + b_dt
-    d = softplus(v)
+    _, d, _, rel = _steps(dt, b_dt)
     n = len(offs) - 1
     y, end = np.zeros_like(u), np.zeros((n, E, N))
     by, be = np.zeros_like(u), np.zeros((n, E, N))
     gate = np.ones_like(u) if z is None else z * sigmoid(z)
     for i in range(n):
         s = np.zeros((E, N)) if state is None else state[i].copy()
-        err = np.zeros((E, N))
+        size, err = np.abs(s), np.zeros((E, N))
         for t in range(offs[i], offs[i + 1]):
-            dA = d[t][:, None] * A
-            a = np.exp(dA)
-            new = a * s + (d[t] * u[t])[:, None] * B[t]
-            # dt + b_dt rounds once (|softplus'| <= 1), softplus is off by EPS_ACT; the exponent
-            # by that and three roundings (A, its product, log2 e), exp by one
-            rel = EPS_ACT + (EPS * np.abs(v[t]) / d[t])
-            err = a * err + np.abs(a * s) * (np.abs(dA) * (rel[:, None] + 4 * EPS) + 3 * EPS)
-            err += np.abs((d[t] * u[t])[:, None] * B[t]) * (rel[:, None] + 3 * EPS) + np.abs(new) * EPS
-            s = new
+            a, ea = _decay(d[t], rel[t], A, A_log, offs[i + 1] - offs[i])
+            x = (d[t] * u[t])[:, None] * B[t]
+            err = a * (err + ea * size) + np.abs(x) * (rel[t][:, None] + 4 * EPS)
+            s, size = a * s + x, a * size + np.abs(x)
+            err += 2 * EPS * size
             full = (s * C[t]).sum(1) + D * u[t]
-            size = (np.abs(s * C[t])).sum(1) + np.abs(D * u[t])
+            terms = (np.abs(s * C[t])).sum(1) + np.abs(D * u[t])
             y[t] = full * gate[t]
-            by[t] = ((np.abs(C[t]) * err).sum(1) + (N + 2) * EPS * size) * np.abs(gate[t]) + EPS_ACT * np.abs(y[t])
+            by[t] = ((np.abs(C[t]) * err).sum(1) + (N + 2) * EPS * terms) * np.abs(gate[t]) + EPS_ACT * np.abs(y[t])
         end[i], be[i] = s, err
     return dict(y=y, end=end, bound=dict(y=by, end=be))
 
 
 def scan_backward(u, dt, A_log, B, C, dy, offs, D=None, z=None, b_dt=None, state=None, dend=None):
-    """-> dict(du, ddt, dz, dB, dC, dA_log, dD, db_dt, dstate, bound: dict of the same)"""
+    """-> dict(du, ddt, dz, dB, dC, dA_log, dD, db_dt, dstate, bound: dict of the same)
+
+    The bound of every element is a sum over what enters it: states S and adjoints g each with an
+    error of their own (eS, eg, propagated as in scan), and every product with the relative errors of
+    its factors, on sums of absolute values (M for S, ga for g)."""
     u, dt, A_log, B, C, dy, D, z, b_dt, state, dend = _f64(u, dt, A_log, B, C, dy, D, z, b_dt, state, dend)
     T, E = u.shape
     N = A_log.shape[1]
     A = -np.exp(A_log)
+    absA, eA = -A, (2 * np.abs(A_log) + 4) * EPS
     D = np.zeros(E) if D is None else D
-    v = dt if b_dt is None else dt + b_dt
-    d, sv = softplus(v), sigmoid(v)
+    v, d, sv, rel = _steps(dt, b_dt)
+    e_sv = EPS_ACT + EPS * np.abs(v) * (1 - sv)  # sigmoid' / sigmoid = 1 - sigmoid
     sz = None if z is None else sigmoid(z)
     gate = np.ones_like(u) if z is None else z * sz
     dgate = None if z is None else sz * (1 + z * (1 - sz))
+    e_gate = (0.0 if z is None else EPS_ACT) + 2 * EPS
     n = len(offs) - 1
-    o = dict(du=np.zeros((T, E)), ddt=np.zeros((T, E)), dz=np.zeros((T, E)), dB=np.zeros((T, N)), dC=np.zeros((T, N)),
-             dA_log=np.zeros((E, N)), dD=np.zeros(E), db_dt=np.zeros(E), dstate=np.zeros((n, E, N)))
-    m = {k: np.zeros_like(a) for k, a in o.items()}  # the same with every term's absolute value
-    longest = 0.0
+    names = dict(du=(T, E), ddt=(T, E), dz=(T, E), dB=(T, N), dC=(T, N), dA_log=(E, N), dD=(E,), db_dt=(E,),
+                 dstate=(n, E, N))
+    o = {k: np.zeros(s) for k, s in names.items()}
+    b = {k: np.zeros(s) for k, s in names.items()}
+
+    def add(k, t, terms, errors, axis=None):
+        """Terms of a sum over all channels (axis 0 of them) or all tokens, with their errors, and
+        a rounding for each of the sum's additions."""
+        more = errors + ((E if axis == 0 else T) + 2) * EPS * np.abs(terms)
+        o[k][t] += terms if axis is None else terms.sum(axis)
+        b[k][t] += more if axis is None else more.sum(axis)
+
     for i in range(n):
         lo, hi = offs[i], offs[i + 1]
         S = [np.zeros((E, N)) if state is None else state[i]]
-        M = [np.abs(S[0])]
-        total = np.zeros((E, N))
+        M, eS = [np.abs(S[0])], [np.zeros((E, N))]
+        decays = []
         for t in range(lo, hi):
-            a = np.exp(d[t][:, None] * A)
-            S.append(a * S[-1] + (d[t] * u[t])[:, None] * B[t])
-            M.append(a * M[-1] + np.abs((d[t] * u[t])[:, None] * B[t]))
-            total += np.abs(d[t][:, None] * A)
-        longest = max(longest, total.max() if hi > lo else 0.0)
+            a, ea = _decay(d[t], rel[t], A, A_log, hi - lo)
+            x = (d[t] * u[t])[:, None] * B[t]
+            S.append(a * S[-1] + x)
+            M.append(a * M[-1] + np.abs(x))
+            eS.append(a * (eS[-1] + ea * M[-2]) + np.abs(x) * (rel[t][:, None] + 4 * EPS) + 2 * EPS * M[-1])
+            decays.append((a, ea))
         g = np.zeros((E, N)) if dend is None else dend[i].copy()
-        ga = np.abs(g)
+        ga, eg = np.abs(g), np.zeros((E, N))
         for t in reversed(range(lo, hi)):
             k = t - lo
-            a = np.exp(d[t][:, None] * A)
+            a, ea = decays[k]
             q = dy[t] * gate[t]
-            full, size = (S[k + 1] * C[t]).sum(1) + D * u[t], (M[k + 1] * np.abs(C[t])).sum(1) + np.abs(D * u[t])
+            aq, aC, aB, au = np.abs(q), np.abs(C[t]), np.abs(B[t]), np.abs(u[t])
             if z is not None:
+                full, terms = (S[k + 1] * C[t]).sum(1) + D * u[t], (M[k + 1] * aC).sum(1) + np.abs(D * u[t])
                 o["dz"][t] = dy[t] * full * dgate[t]
-                m["dz"][t] = np.abs(dy[t]) * size * sz[t] * (1 + np.abs(z[t]))
-            g = g + q[:, None] * C[t]
-            ga = ga + np.abs(q[:, None] * C[t])
-            o["dC"][t] = (q[:, None] * S[k + 1]).sum(0)
-            m["dC"][t] = (np.abs(q)[:, None] * M[k + 1]).sum(0)
-            o["dB"][t] = (g * (d[t] * u[t])[:, None]).sum(0)
-            m["dB"][t] = (ga * np.abs(d[t] * u[t])[:, None]).sum(0)
-            gB, gBa = (g * B[t]).sum(1), (ga * np.abs(B[t])).sum(1)
+                # SiLU' = sg (1 + z (1 - sg)): sg's relative error on both
+                b["dz"][t] = np.abs(dy[t]) * (((eS[k + 1] * aC).sum(1) + (N + 4) * EPS * terms) * np.abs(dgate[t]) +
+                                              terms * (EPS_ACT * sz[t] * (1 + np.abs(z[t])) + 4 * EPS))
+            x = q[:, None] * C[t]
+            g, ga, eg = g + x, ga + np.abs(x), eg + np.abs(x) * (e_gate + EPS)
+            eg = eg + EPS * ga
+            step = (d[t] * u[t])[:, None]
+            add("dC", t, q[:, None] * S[k + 1], aq[:, None] * (eS[k + 1] + M[k + 1] * (e_gate + EPS)), 0)
+            add("dB", t, g * step, (eg + ga * (rel[t][:, None] + 3 * EPS)) * np.abs(step), 0)
+            gB, gBa = (g * B[t]).sum(1), (ga * aB).sum(1)
+            egB = (eg * aB).sum(1) + (N + 1) * EPS * gBa
             gs, gsa = g * a * S[k], ga * a * M[k]
+            egs = a * (eg * M[k] + ga * eS[k]) + gsa * (ea + 2 * EPS)
             o["du"][t] = D * q + d[t] * gB
-            m["du"][t] = np.abs(D * q) + d[t] * gBa
-            o["ddt"][t] = ((gs * A).sum(1) + u[t] * gB) * sv[t]
-            m["ddt"][t] = ((gsa * -A).sum(1) + np.abs(u[t]) * gBa) * sv[t]
-            o["dA_log"] += gs * d[t][:, None] * A
-            m["dA_log"] += gsa * d[t][:, None] * -A
-            o["dD"] += q * u[t]
-            m["dD"] += np.abs(q * u[t])
-            o["db_dt"] += o["ddt"][t]
-            m["db_dt"] += m["ddt"][t]
-            g, ga = g * a, ga * a
-        o["dstate"][i], m["dstate"][i] = g, ga
-    # One path: a product of decays, whose exponents sum to `longest` at most and are off by d's
-    # error and four roundings each (|x e^-x| and the decays' own factor aside, an overestimate),
-    # its L factors' roundings forwards and back, the activations, and sums of N or, for dB,
-    # dC and the parameters, of E or T terms.
-    L = int(max(np.diff(offs), default=0))
-    rel_v = (EPS * np.abs(v) / d).max() if T else 0.0
-    path = (longest + 4) * (EPS_ACT + rel_v + 4 * EPS) + (4 * L + N + 16) * EPS
-    long_sum = dict(dB=E, dC=E, dA_log=T, dD=T, db_dt=T)
-    return dict(o, bound={k: a * (path + long_sum.get(k, 0) * EPS) for k, a in m.items()})
+            b["du"][t] = np.abs(D * q) * (e_gate + 2 * EPS) + d[t] * (egB + gBa * (rel[t] + 3 * EPS))
+            dd, dda = (gs * A).sum(1) + u[t] * gB, (gsa * absA).sum(1) + au * gBa
+            edd = ((egs + gsa * (eA + (N + 2) * EPS)) * absA).sum(1) + au * egB + 3 * EPS * dda
+            ddt, eddt = dd * sv[t], edd * sv[t] + dda * sv[t] * (e_sv[t] + 2 * EPS)
+            o["ddt"][t], b["ddt"][t] = ddt, eddt
+            add("dA_log", slice(None), gs * d[t][:, None] * A,
+                (egs + gsa * (rel[t][:, None] + eA + 3 * EPS)) * d[t][:, None] * absA)
+            add("dD", slice(None), q * u[t], aq * au * (e_gate + EPS))
+            add("db_dt", slice(None), ddt, eddt)
+            g, ga, eg = g * a, ga * a, a * (eg + ga * ea)
+        o["dstate"][i], b["dstate"][i] = g, eg
+    return dict(o, bound=b)
