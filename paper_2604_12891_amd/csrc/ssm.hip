@@ -1212,10 +1212,13 @@ int conv_rows(int rows, int CG) {
     if ((int64_t)rows / R * CG >= (int64_t)kCUs * 8 * 64) return R;
   return 8;
 }
-// Gradients: as many threads as the GPU holds at once (four wavefronts to a SIMD), at most 1,024
-// parts; a thread takes one tile, of as many rows as that leaves it, or several of
-// kConvBwdRows where the sequences alone are more than that.
-constexpr int kConvBwdRows = 32;
+// Gradients: as many threads as four wavefronts to a SIMD are, at most 1,024 parts; a thread takes one
+// tile, of as many rows as that leaves it, or several of kConvBwdRows where the sequences alone are more than
+// that. Where they are nearly as many, what that leaves is far more than an even share, and a long sequence
+// among short ones would be one thread's (20,000 tokens and 254 of one, 4,096 bf16 channels: 11.1 ms, now 0.49): a
+// tile has at most kConvBwdShares times the even share, or kConvBwdMost rows, for an eighth more parts.
+// (Twice the share: 0.24 ms there, but 255 sequences of 1,000 tokens 1.32 to 1.72.)
+constexpr int kConvBwdRows = 32, kConvBwdMost = 256, kConvBwdShares = 8;
 struct ConvParts {
   int R, per, parts;
 };
@@ -1223,9 +1226,13 @@ ConvParts conv_parts(int n_seq, int rows, int E) {
   const int CG = (E + 3) / 4, want = std::max(1, std::min(1024, kCUs * 16 * 64 / CG));
   ConvParts p;
   p.R = kConvBwdRows;
-  if (want > n_seq) p.R = std::max(p.R, (int)(((int64_t)rows + want - n_seq - 1) / (want - n_seq)));
+  p.per = 1;
+  if (want > n_seq) {
+    const int64_t left = ((int64_t)rows + want - n_seq - 1) / (want - n_seq);
+    p.R = std::max(p.R, (int)std::min(left, std::max<int64_t>(kConvBwdMost, kConvBwdShares * ((int64_t)rows / want + 1))));
+  }
   const int tiles = rows / p.R + n_seq;
-  p.per = (tiles + want - 1) / want;
+  if (want <= n_seq) p.per = (tiles + want - 1) / want;
   p.parts = (tiles + p.per - 1) / p.per;
   return p;
 }
