@@ -50,11 +50,13 @@ def conv(x, w, b, offs, state=None):
     return dict(u=u, end=end, bound=bound)
 
 
-def conv_backward(x, w, b, du, offs, state=None, dend=None):
-    """-> dict(dx, dw, db, dstate, bound: dict of the same)"""
+def conv_backward(x, w, b, du, offs, state=None, dend=None, chain=None):
+    """-> dict(dx, dw, db, dstate, bound: dict of the same); chain: the most additions that a
+    term of dw or db passes through (None: one for every token)"""
     x, w, b, du, state, dend = _f64(x, w, b, du, state, dend)
     E, K = w.shape
     b = np.zeros(E) if b is None else b
+    chain = len(x) if chain is None else chain
     dx, dw, db = np.zeros_like(x), np.zeros_like(w), np.zeros(E)
     bx, bw, bb = np.zeros_like(x), np.zeros_like(w), np.zeros(E)
     n = len(offs) - 1
@@ -79,9 +81,9 @@ def conv_backward(x, w, b, du, offs, state=None, dend=None):
             g_ext[t:t + K] += w.T * g
             g_abs[t:t + K] += np.abs(w.T) * (e + (K + 1) * EPS * np.abs(g))
             dw += (g * win).T
-            bw += (np.abs(win) * (e + (len(x) + 2) * EPS * np.abs(g))).T
+            bw += (np.abs(win) * (e + (chain + 2) * EPS * np.abs(g))).T
             db += g
-            bb += e + (len(x) + 2) * EPS * np.abs(g)
+            bb += e + (chain + 2) * EPS * np.abs(g)
         dx[lo:hi], bx[lo:hi] = g_ext[K - 1:], g_abs[K - 1:]
         ds[i], bs[i] = g_ext[:K - 1], g_abs[:K - 1]
     return dict(dx=dx, dw=dw, db=db, dstate=ds, bound=dict(dx=bx, dw=bw, db=bb, dstate=bs))
