@@ -596,8 +596,8 @@ TCL_API tcl_status tcl_ssm_scan_backward(const tcl_ssm_scan_args* args, const vo
  * is V entries of an [n_rows, ld] array (d_seg_offsets NULL; entries are counted
  * from the row's start), or a segment d_seg_offsets[g] .. d_seg_offsets[g+1]-1 of one
  * array, V entries at most, as in tcl_topk (entries are counted from the
- * array's start, ld is not used). Logits are fp32 or bf16 (dtype), of any
- * alignment; arithmetic is fp32; a temperature in [1e-30, 1e30] divides the logits. -inf is
+ * array's start, ld is not used; an array without entries may be NULL, and every
+ * segment of it is empty). Logits are fp32 or bf16 (dtype), of any alignment; arithmetic is fp32; a temperature in [1e-30, 1e30] divides the logits. -inf is
  * a masked entry, with no probability. V <= 2^30, n_rows < 2^22. Stream-ordered, deterministic, no
  * allocation. d_workspace: >= tcl_logits_workspace_bytes(n_rows, V, K) bytes, 256-byte
  * aligned; 0 bytes (d_workspace may be NULL) from 513 rows on. n_rows == 0 is TCL_OK.

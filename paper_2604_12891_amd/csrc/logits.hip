@@ -38,7 +38,7 @@ struct Row {
   __device__ __forceinline__ Row(const LogitRows& a, int r) {
     const int64_t o = a.offs ? a.offs[r] : (int64_t)r * a.ld;
     p = static_cast<const T*>(a.x) + o;
-    cnt = a.offs ? max(a.offs[r + 1] - a.offs[r], 0) : a.V;
+    cnt = !a.offs ? a.V : a.x ? max(a.offs[r + 1] - a.offs[r], 0) : 0;
     first = a.offs ? a.offs[r] : 0;
     h = (int)((reinterpret_cast<uintptr_t>(p) / sizeof(T)) % VE);
     nvec = cnt > 0 ? (cnt + h + VE - 1) / VE : 0;

@@ -90,7 +90,7 @@ tcl_status logit_rows(int32_t dtype, int32_t n_rows, int32_t V, const void* d_lo
   if (!d_seg_offsets && ld < V) return fail(TCL_ERR_INVALID_ARG, "leading dimension smaller than V");
   if (!(temperature >= kMinTemp && temperature <= kMaxTemp))
     return fail(TCL_ERR_INVALID_ARG, "temperature must be in [1e-30, 1e30]");
-  if (!d_logits && n_rows > 0) return fail(TCL_ERR_INVALID_ARG, "NULL device pointer");
+  if (!d_logits && !d_seg_offsets && n_rows > 0) return fail(TCL_ERR_INVALID_ARG, "NULL device pointer");
   if (misaligned(d_logits, dtype == TCL_BF16 ? 2 : 4))
     return fail(TCL_ERR_INVALID_ARG, "logits are not aligned to their type");
   a->bf16 = dtype == TCL_BF16;
