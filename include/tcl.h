@@ -490,7 +490,9 @@ TCL_API tcl_status tcl_trainer_timing_reset(tcl_trainer* trainer);
  *  - E in [1, 65536], d_state (N) 8 or 16, d_conv (K) in [1, 4]; with E rounded up to a multiple
  *    of 64, rows E at most 2^34 and n_seq E at most 2^30. Stream-ordered,
  *    deterministic, no allocation; may be captured into a graph. Empty work
- *    (n_seq == 0, or rows == 0 in the single-token form) is TCL_OK.
+ *    (n_seq == 0, or rows == 0 in the single-token form) is TCL_OK, except for the two
+ *    backward calls, which refuse n_seq == 0 (TCL_ERR_INVALID_ARG) and write nothing. Sequences
+ *    that are all empty are no exception: the parameters' gradients are then zeros.
  * ------------------------------------------------------------------- */
 
 /* u = SiLU(b + causal depthwise conv_K(x; w)): u_t = SiLU(b + sum_k w_k x_{t-K+1+k}),

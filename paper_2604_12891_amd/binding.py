@@ -668,7 +668,8 @@ def ssm_conv_backward(x, w, b, du, offs=None, state=None, state_grad=None, works
     """Gradients of ssm_conv (tcl_ssm_conv_backward) from du [rows, E] and, for carried
     states [n_seq, K-1, E], the gradient state_grad of the end states. Returns a
     dict of dx, dw, db and dstate (None without a state); out: tensors of those names to write to.
-    Rows of dx that no sequence owns are left as they are (in a new tensor: undefined)."""
+    Rows of dx that no sequence owns are left as they are (in a new tensor: undefined). A batch
+    of no sequences at all is refused."""
     if stream is not None:
         return _under(stream, ssm_conv_backward, x, w, b, du, offs, state, state_grad, workspace, out)
     import torch
@@ -745,7 +746,7 @@ def ssm_scan_backward(u, dt, A_log, B, C, dy, D=None, z=None, b_dt=None, offs=No
     states [n_seq, E, N], the gradient state_grad of the end states. Returns a dict of
     du, ddt, dB, dC, dz (None without z), dA_log, dD, db_dt and dstate (None without a
     state); out: tensors of those names to write to. Rows of the activations' gradients that no sequence
-    owns are left as they are (in a new tensor: undefined)."""
+    owns are left as they are (in a new tensor: undefined). A batch of no sequences at all is refused."""
     if stream is not None:
         return _under(stream, ssm_scan_backward, u, dt, A_log, B, C, dy, D, z, b_dt, offs, L, state, state_grad,
                       workspace, out)
