@@ -599,8 +599,9 @@ TCL_API tcl_status tcl_ssm_scan_backward(const tcl_ssm_scan_args* args, const vo
  * from the row's start), or a segment d_seg_offsets[g] .. d_seg_offsets[g+1]-1 of one
  * array, V entries at most, as in tcl_topk (entries are counted from the
  * array's start, ld is not used; an array without entries may be NULL, and every
- * segment of it is empty). Logits are fp32 or bf16 (dtype), of any alignment; arithmetic is fp32; a temperature in [1e-30, 1e30] divides the logits. -inf is
- * a masked entry, with no probability. V <= 2^30, n_rows < 2^22. Stream-ordered, deterministic, no
+ * segment of it is empty). Logits are fp32 or bf16 (dtype), of any alignment; arithmetic
+ * is fp32; a temperature in [1e-30, 1e30] divides the logits. -inf is a masked entry, with no
+ * probability. V <= 2^30, n_rows < 2^22. Stream-ordered, deterministic, no
  * allocation. d_workspace: >= tcl_logits_workspace_bytes(n_rows, V, K) bytes, 256-byte
  * aligned; 0 bytes (d_workspace may be NULL) from 513 rows on. n_rows == 0 is TCL_OK.
  * ------------------------------------------------------------------- */
@@ -616,7 +617,7 @@ TCL_API size_t tcl_logits_workspace_bytes(int32_t n_rows, int32_t V, int32_t K);
  *     a row with fewer than K entries. K in [0, 64]; 0: none (d_top may be NULL).
  * NaN logits (unscored programs) are taken as masked. A row with nothing left
  * (empty, or all masked) has entropy 0 and log p = -inf. A logit of +inf makes its
- * row's values NaN. */
+ * row's values NaN, but for log p of masked entries. */
 TCL_API tcl_status tcl_logprobs(int32_t dtype, int32_t n_rows, int32_t V, const void* d_logits, int64_t ld,
                                 const int32_t* d_seg_offsets, float temperature, const int32_t* d_tokens, int32_t K,
                                 float* d_logp, float* d_entropy, int32_t* d_top, float* d_top_logp,
@@ -633,9 +634,10 @@ TCL_API tcl_status tcl_logprobs(int32_t dtype, int32_t n_rows, int32_t V, const 
  * ldg, and may be d_logits itself (ldg == ld). Entries of d_top outside the row (-1 past a short
  * one) do not count; an entry listed twice counts with both probabilities. A row
  * without any teacher's entry (none in the row, or all -inf), or with nothing left of its own (empty or
- * all -inf), has loss 0 and gradient 0; the loss is +inf where the student masks an
- * entry that the teacher does not. NaN in either's logits makes the row's
- * results NaN. K in [1, 1024]. */
+ * all -inf), has loss 0 and gradient 0. In every other row NaN or +inf in either's logits makes
+ * the results NaN, and the loss is +inf where the student masks an entry that has a probability q_k
+ * with the teacher (one below 2^-126, fp32's smallest normal number, counts as 0). K in
+ * [1, 1024]. */
 TCL_API tcl_status tcl_distill_topk(int32_t dtype, int32_t n_rows, int32_t V, const void* d_logits, int64_t ld,
                                     const int32_t* d_seg_offsets, float temperature, int32_t K,
                                     const int32_t* d_top, const float* d_teacher, const float* d_weight,

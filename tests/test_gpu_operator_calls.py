@@ -32,3 +32,35 @@ def test_segments_of_an_empty_array(n, dtype):
     d = tb.distill_topk(x, top, val, seg_offsets=offs + 4, max_len=1, grad=False)
     assert not d["loss"].any()
     assert torch.equal(tb.logprobs(x, K=K, seg_offsets=offs + 4, max_len=1)["top"], r["top"])
+
+
+@pytest.mark.parametrize("n,V", [(3, 900), (2, 70001), (600, 150)])
+def test_what_the_student_masks(n, V):
+    """A student's mask where the teacher has a probability: an infinite loss, unless that is below
+    fp32's smallest normal number; finite gradients either way. Rows without a teacher are zeros whatever the
+    student's logits are; NaN and +inf show in all others."""
+    tb, inf, nan = _tb(), float("inf"), float("nan")
+    for dtype in (torch.float32, torch.bfloat16):
+        x = torch.zeros(n, V, device="cuda", dtype=dtype)
+        x[:, 7] = -inf
+        top = torch.tensor([[3, 7]], dtype=torch.int32, device="cuda").repeat(n, 1)
+
+        def loss(*teacher, x=x, top=top):
+            r = tb.distill_topk(x, top, torch.tensor([teacher], device="cuda").repeat(n, 1))
+            return r["loss"].double().cpu().numpy(), r["grad"]
+
+        for low, want in ((-80.0, inf), (-100.0, np.log(V - 1)), (-inf, np.log(V - 1))):
+            got, grad = loss(0.0, low)
+            # log of a sum of ones: a few roundings of log V < 16
+            assert (got == want).all() if want == inf else (np.abs(got - want) < 16 * 8 * 2.0 ** -24).all(), (low, got)
+            assert torch.isfinite(grad).all()
+        for v in (nan, inf):
+            bad = x.clone()
+            bad[0, 1] = v
+            got, grad = loss(0.0, -1.0, x=bad)
+            assert np.isnan(got[0]) and (got[1:] == inf).all()
+            assert torch.isnan(grad[0]).any() and torch.isfinite(grad[1:]).all()
+            got, grad = loss(0.0, v)
+            assert np.isnan(got).all()
+            got, grad = loss(0.0, -1.0, x=bad, top=torch.full_like(top, -1))  # no teacher
+            assert not got.any() and not grad.any()
