@@ -64,3 +64,25 @@ def test_what_the_student_masks(n, V):
             assert np.isnan(got).all()
             got, grad = loss(0.0, -1.0, x=bad, top=torch.full_like(top, -1))  # no teacher
             assert not got.any() and not grad.any()
+
+
+def test_the_readme_example():
+    """What README.md shows, on small tensors."""
+    tcl = _tb()
+    T, n, E, N, V, K = 12, 3, 16, 16, 40, 5
+    r = lambda *s: torch.randn(*s, device="cuda")
+    x, x1, w, b, dt, dt1, z, z1 = r(T, E), r(n, E), r(E, 4), r(E), r(T, E), r(n, E), r(T, E), r(n, E)
+    A_log, B, C, B1, C1, D, b_dt, dy = r(E, N), r(T, N), r(T, N), r(n, N), r(n, N), r(E), r(E), r(T, E)
+    offs, longest = torch.tensor([0, 5, 5, 12], dtype=torch.int32, device="cuda"), 7
+    conv_state, state = torch.empty(n, 3, E, device="cuda"), torch.empty(n, E, N, device="cuda")
+    teacher_logits, logits, tokens = r(T, V), r(T, V), torch.zeros(T, dtype=torch.int32, device="cuda")
+    u = tcl.ssm_conv(x, w, b, offs=offs, state_out=conv_state)
+    y = tcl.ssm_scan(u, dt, A_log, B, C, D=D, z=z, b_dt=b_dt, offs=offs, L=longest, state_out=state)
+    u1 = tcl.ssm_conv(x1, w, b, state=conv_state, state_out=conv_state)
+    y1 = tcl.ssm_scan(u1, dt1, A_log, B1, C1, D=D, z=z1, b_dt=b_dt, state=state, state_out=state)
+    t = tcl.logprobs(teacher_logits, tokens, K=K)
+    d = tcl.distill_topk(logits, t["top"], t["top_logp"])
+    g = tcl.ssm_scan_backward(u, dt, A_log, B, C, dy, D=D, z=z, b_dt=b_dt, offs=offs, L=longest)
+    assert y.shape == (T, E) and y1.shape == (n, E) and d["grad"].shape == (T, V) and g["du"].shape == (T, E)
+    for v in (u, y, u1, y1, conv_state, state, d["loss"], d["grad"], g["du"], g["dA_log"]):
+        assert torch.isfinite(v).all()
