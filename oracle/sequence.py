@@ -15,6 +15,7 @@ import numpy as np
 
 EPS = 2.0 ** -24        # one fp32 rounding
 EPS_ACT = 4e-6          # SiLU, sigmoid and softplus in fp32, relative
+TINY = 2.0 ** -126      # a decay below it, or a product of decays, may be zero in fp32
 
 
 def sigmoid(x):
@@ -98,20 +99,21 @@ def _steps(dt, b_dt):
 
 
 def _decay(d, rel, A, A_log, length):
-    """One token's decays exp(d A) [E, N] and their relative error: the exponent's own (d; A, whose
-    exponent A_log rounds twice, and three roundings more; the product; where decays are multiplied by
-    adding up their steps, a rounding per token of the sequence) times the exponent, and six
+    """One token's decays exp(d A) [E, N] and their error: TINY and, relative, the exponent's own (d; A,
+    whose exponent A_log rounds twice, and three roundings more; the product; where decays are multiplied
+    by adding up their steps, a rounding per token of the sequence) times the exponent, and six
     roundings: exp2 (one unit, two roundings), the product with a state, the sum that it enters, and as
     many again where a sequence's parts are joined."""
     x = d[:, None] * A
-    return np.exp(x), np.abs(x) * (rel[:, None] + (2 * np.abs(A_log) + 5 + length) * EPS) + 6 * EPS
+    a = np.exp(x)
+    return a, a * (np.abs(x) * (rel[:, None] + (2 * np.abs(A_log) + 5 + length) * EPS) + 6 * EPS) + TINY
 
 
 def scan(u, dt, A_log, B, C, offs, D=None, z=None, b_dt=None, state=None):
     """-> dict(y, end, bound: dict(y, end))
 
     The states' bound runs along with them: a step passes on the error that is there and adds
-    the decay's and the input's relative errors, times what these multiply with every term's
+    the decay's and the input's errors, times what these multiply with every term's
     absolute value (as parts of a sequence may be summed apart)."""
     u, dt, A_log, B, C, D, z, b_dt, state = _f64(u, dt, A_log, B, C, D, z, b_dt, state)
     T, E = u.shape
@@ -129,7 +131,7 @@ def scan(u, dt, A_log, B, C, offs, D=None, z=None, b_dt=None, state=None):
         for t in range(offs[i], offs[i + 1]):
             a, ea = _decay(d[t], rel[t], A, A_log, offs[i + 1] - offs[i])
             x = (d[t] * u[t])[:, None] * B[t]
-            err = a * (err + ea * size) + np.abs(x) * (rel[t][:, None] + 4 * EPS)
+            err = a * err + ea * size + np.abs(x) * (rel[t][:, None] + 4 * EPS)
             s, size = a * s + x, a * size + np.abs(x)
             err += 2 * EPS * size
             full = (s * C[t]).sum(1) + D * u[t]
@@ -181,7 +183,7 @@ def scan_backward(u, dt, A_log, B, C, dy, offs, D=None, z=None, b_dt=None, state
             x = (d[t] * u[t])[:, None] * B[t]
             S.append(a * S[-1] + x)
             M.append(a * M[-1] + np.abs(x))
-            eS.append(a * (eS[-1] + ea * M[-2]) + np.abs(x) * (rel[t][:, None] + 4 * EPS) + 2 * EPS * M[-1])
+            eS.append(a * eS[-1] + ea * M[-2] + np.abs(x) * (rel[t][:, None] + 4 * EPS) + 2 * EPS * M[-1])
             decays.append((a, ea))
         g = np.zeros((E, N)) if dend is None else dend[i].copy()
         ga, eg = np.abs(g), np.zeros((E, N))
@@ -205,7 +207,7 @@ def scan_backward(u, dt, A_log, B, C, dy, offs, D=None, z=None, b_dt=None, state
             gB, gBa = (g * B[t]).sum(1), (ga * aB).sum(1)
             egB = (eg * aB).sum(1) + (N + 1) * EPS * gBa
             gs, gsa = g * a * S[k], ga * a * M[k]
-            egs = a * (eg * M[k] + ga * eS[k]) + gsa * (ea + 2 * EPS)
+            egs = a * (eg * M[k] + ga * eS[k]) + ga * M[k] * ea + 2 * EPS * gsa
             o["du"][t] = D * q + d[t] * gB
             b["du"][t] = np.abs(D * q) * (e_gate + 2 * EPS) + d[t] * (egB + gBa * (rel[t] + 3 * EPS))
             dd, dda = (gs * A).sum(1) + u[t] * gB, (gsa * absA).sum(1) + au * gBa
@@ -216,6 +218,6 @@ def scan_backward(u, dt, A_log, B, C, dy, offs, D=None, z=None, b_dt=None, state
                 (egs + gsa * (rel[t][:, None] + eA + 3 * EPS)) * d[t][:, None] * absA)
             add("dD", slice(None), q * u[t], aq * au * (e_gate + EPS))
             add("db_dt", slice(None), ddt, eddt)
-            g, ga, eg = g * a, ga * a, a * (eg + ga * ea)
+            g, ga, eg = g * a, ga * a, a * eg + ga * ea
         o["dstate"][i], b["dstate"][i] = g, eg
     return dict(o, bound=b)

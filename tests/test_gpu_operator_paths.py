@@ -157,3 +157,19 @@ def test_logprobs_where_the_list_overflows(K, threads, dtype):
     got = _tb().logprobs(_cuda(x, DT[dtype]), None, K)
     ref = ol.logprobs(list(x), None, K)
     assert np.array_equal(got["top"].cpu().numpy(), ref["top"])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("lens,E,N", [([70, 3, 40], 64, 16), ([300], 65, 8), ([9, 1, 30] * 200, 60, 8)])
+def test_scan_gradients_of_steep_steps(lens, E, N, dtype):
+    """Steps of 1e-26 to 40: decays of one, of nothing, and, with the last ones' products, between fp32's
+    smallest numbers and zero."""
+    print(f"scan gradients steep lens={lens[:3]} E={E} N={N} {dtype}", flush=True)
+    a = _scan_case(lens, E, N, dtype, 111, steep=True)
+    T, n, offs = sum(lens), len(lens), _offs(lens)
+    rng = np.random.default_rng(112)
+    dy, dend = _round(rng.standard_normal((T, E)), dtype), rng.standard_normal((n, E, N)).astype(np.float32)
+    g = _tb().ssm_scan_backward(dy=_cuda(dy, DT[dtype]), offs=_cuda(offs, torch.int32), L=max(lens),
+                                state_grad=_cuda(dend), **_scan_tensors(a, dtype, T))
+    r = osq.scan_backward(dy=dy, offs=offs, dend=dend, **a)
+    _check_scan_grads(g, r, dtype, T, ["du", "ddt", "dz", "dB", "dC", "dA_log", "dD", "db_dt", "dstate"])
