@@ -18,7 +18,6 @@ namespace tcl {
 namespace {
 
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 __device__ __forceinline__ float to_f32(float v) { return v; }
 __device__ __forceinline__ float to_f32(uint16_t v) { return bf16_to_f32(v); }
@@ -71,7 +70,6 @@ __device__ __forceinline__ void st_vec(float* row, uint32_t bytes, const float* 
 // CH adjacent channels of a row; the storage type's raw bits, widened at use.
 template <typename T, int CH> struct Pack { T v[CH]; };
 template <> struct Pack<float, 4> { floatx4 v; };
-template <> struct Pack<uint16_t, 8> { u32x4 v; };
 template <> struct Pack<uint16_t, 4> { u32x2 v; };
 
 template <typename T, int CH>
