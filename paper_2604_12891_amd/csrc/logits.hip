@@ -615,7 +615,8 @@ __device__ __forceinline__ bool same_phase(const Row<T>& row, const T* g) {
 // One workgroup per row, the row's NV x 64 NW vectors held in registers from the one
 // time they are read until the gradient leaves; of longer rows the rest is read
 // again for each of the three passes. Bound by HBM: each entry read and written once; 2,048 rows of
-// 131,072 bf16 entries in 251 us, 230 at the rate of a copy.
+// 131,072 bf16 entries in 251 us, 230 at the rate of a copy; 1,024 of 131,072 fp32 ones, half of which the
+// registers hold, in 338.
 template <typename T, int NW, int NV>
 __global__ __launch_bounds__(64 * NW) void distill_row_kernel(LogitRows a, TeacherArgs t) {
   constexpr int VE = Row<T>::VE, TB = 64 * NW;
@@ -647,7 +648,7 @@ __global__ __launch_bounds__(64 * NW) void distill_row_kernel(LogitRows a, Teach
     for (int k = 0; k < NV; ++k) asm volatile("" : "+v"(x[k]));
   };
   block_reduce<NW, true>(m, mt, red[0]);
-  if (NW < 16) hold();  // (at 1,024 threads the 128 registers do without it, and spill with it)
+  if (NW < 16) hold();  // (at 1,024 threads, 128 registers, one (bf16) and four (fp32) are spilled so, six and three with it)
   if (t.grad && teacher_twice<TB>(sh, t.K)) twice = 1;
   if (!(m > -INFINITY)) m = 0.f;  // nothing but -inf (a sum of 0) or NaN (a sum of NaN)
   float s = 0.f, qs = teacher_sum<NW>(sh, t.K, mt, a.inv_temp);

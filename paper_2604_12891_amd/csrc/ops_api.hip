@@ -11,9 +11,11 @@ namespace {
 
 bool misaligned(const void* p, uintptr_t n) { return reinterpret_cast<uintptr_t>(p) % n != 0; }
 
-// A launch has fewer than 2^32 threads. Tiles hold 30 rows or more, besides one per sequence, and
+// A launch has fewer than 2^32 threads. A scan's tiles hold 30 rows or more, besides one per sequence, and
 // their channels are rounded up to 64, in the gradients (wavefronts in fours) to less than twice that: with these
-// bounds 2 (2^34 / 30 + 2^30) threads at most, and row and tile indices far inside 31 bits.
+// bounds 2 (2^34 / 30 + 2^30) threads at most, and row and tile indices far inside 31 bits. The convolution's
+// tiles hold 8 to 16 rows only where 32 would give fewer than 2^17 threads, 32 or more else, and a thread takes
+// one channel or more of a tile: 2^34 / 32 + 2^30 threads at most.
 constexpr int kMaxRows = 1 << 30;
 constexpr int64_t kMaxRowWork = (int64_t)1 << 34, kMaxSeqWork = (int64_t)1 << 30;
 // Rows of logits take a workgroup of up to 1,024 threads each.

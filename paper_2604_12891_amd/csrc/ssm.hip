@@ -144,9 +144,10 @@ __device__ __forceinline__ int slot_of(const int* __restrict__ slots, int n_slot
 // the tile are read again (K - 1 of R), those in front of the sequence come
 // from its state. The thread of the first tile is also the one that writes
 // the new state, after it has read the old one, so both may be the same
-// memory. Bound by HBM: each x read once, each u written once; 18,000 rows of 4,096
-// bf16 channels in 67 us (4.4 TB/s; 80 with eight channels a thread), one token
-// of 256 sequences in 7.3 (3.6 at the rate of a copy).
+// memory. Bound by HBM: each x read once, each u written once; 20,415 rows of 4,096
+// bf16 channels in 68 us (4.9 TB/s, a part out of the cache; 72 at the rate of a copy; a fifth more with
+// eight channels a thread), one token of 256 sequences in 7.2 (3.6 at the rate of a copy: a thread's weights
+// are as many bytes as its rows and states).
 template <typename T, int K, int CH>
 __global__ __launch_bounds__(256) void ssm_conv_kernel(const int* __restrict__ offs, int n_seq, int rows, int E,
                                                        int R, int64_t n_work, const T* __restrict__ x, int64_t ldx,
@@ -260,8 +261,9 @@ __device__ __forceinline__ float silu_grad(float x) {
 // `per` tiles in a row; in each it walks forward over the tile's rows and the
 // K - 1 behind it, forming pre and g again there, so that dx leaves complete and
 // nothing passes between threads. dw and db stay in registers over its tiles
-// and go out once, as part `p` of the partial sums. 18,000 rows of 4,096 bf16 channels in 121 us, 96 at
-// the rate of a copy; 40 issue slots per entry are some 90 us by themselves. (Two channels a thread: 159.)
+// and go out once, as part `p` of the partial sums. 20,415 rows of 4,096 bf16 channels in 120 us, 108 at
+// the rate of a copy; 44 issue slots per 64 entries (by the counters) are 94 us by themselves. (Two channels a
+// thread: 13% longer.) With K = 4 an fp32 thread holds 134 registers, three wavefronts to a SIMD, a bf16 one 122, four.
 template <typename T, int K, int CH>
 __global__ __launch_bounds__(256) void ssm_conv_bwd_kernel(
     const int* __restrict__ offs, int n_seq, int rows, int E, int R, int per, int parts, const T* __restrict__ x,
@@ -427,13 +429,13 @@ __device__ __forceinline__ float dpp(float v) {
 // d = softplus(dt + b_dt), A = -exp(A_log).
 // One lane per channel holds its N states and decay rates (in base-2 units);
 // a workgroup is one wavefront, so nothing waits for another. B and C rows
-// go through LDS kTC tokens at a time (widened once, read as broadcasts), the
-// next kTC rows on their way in registers meanwhile; u, dt and z come four
-// tokens ahead. Per token and wavefront 6 N issue slots for the states and
-// some 35 for softplus, gate and output, against 4 x 64 elements of traffic: the
-// vector unit is what bounds it: 4,096 programs of up to 25 tokens, E 512, fp32, in 141 us, where their
-// traffic takes 110 and their issue slots 124 (by the counters; a sixth of them is spent once per sequence);
-// a prompt of 8,192 tokens, E 4,096, bf16 in chunks 111 + 11 + 150.
+// go through LDS kTC tokens at a time (widened once, read as broadcasts), loaded and
+// waited for in front of each kTC tokens; u, dt and z come two tokens at a time, the next two
+// on their way meanwhile. Per token and wavefront 6 N issue slots for the states and
+// some 35 for softplus, gate and output (146 in all by the counters, on a prompt), against 4 x 64
+// elements of traffic: the vector unit is what bounds it: 4,096 programs of up to 25 tokens, E 512, fp32, in 142
+// us, where their traffic takes 110 and their issue slots 124 (by the counters; a sixth of them is spent once per
+// sequence); a prompt of 8,032 tokens, E 4,096, bf16 in chunks 113 + 12 + 150, the last of them 122 of issue.
 //
 // A sequence is cut into chunks of CL tokens when there are far too few of them to
 // fill the GPU (scan_chunk). s -> P s + s_loc with P = exp(A sum d) is what a chunk does to a
@@ -972,9 +974,10 @@ __global__ __launch_bounds__(1024) void ssm_order_kernel(const int* __restrict__
 // swaps and DPP, over the workgroup's wavefronts through LDS, over
 // workgroups (more than 64 nw channels) by ssm_sum_bc_kernel, all in a fixed order.
 // dA_log, dD and db_dt leave as partial sums, one set per workgroup. 22 N slots per token and
-// wavefront for the states, 70 for the two sums over channels, as many for the rest: 489 instructions
-// (568 slots) by the counters. Four sequences of up to 2,048 tokens, E 2,048, bf16, in 265 us, 79% of the
-// vector unit's time; chunks of 32 tokens in eights, 25 registers spilled, took 308.
+// wavefront for the states, 70 for the two sums over channels, the rest for what is per channel: 462 instructions
+// (515 slots) by the counters. Four sequences of 7,127 tokens together, E 2,048, bf16, in 276 us at best, of which issue
+// takes 192 (the vector unit 75% busy, two wavefronts to a SIMD by 249 registers); chunks of 32 tokens in eights, 25
+// registers spilled, took 16% longer. With N = 16 the loop of several chunks (MULTI) spills 9 to 10 registers.
 template <typename T, int N, bool MULTI>
 __global__ __launch_bounds__(256, 2) void ssm_bwd_kernel(
     ScanIn a, const T* __restrict__ u, const T* __restrict__ dt, const T* __restrict__ B, const T* __restrict__ C,
@@ -1365,7 +1368,7 @@ BwdPlan bwd_plan(bool packed, int n_seq, int rows, int E, int N, int L) {
   // than 32 rounds of workgroups, or 16 of sequences with too few tokens to pay for partial sums as large
   // as two tokens, they go several to a workgroup in their order: 30,000 of 1 to 15, E 256, fp32, 1,326 us
   // against 1,459, 9,000 of 1 to 7 267 against 286 (of 1 to 15 459 against 437). Not chunks of long ones, which lose
-  // 5% to the registers that the loop takes.
+  // 5% to the registers that the loop takes (with N = 16 it spills 9 to 10).
   const int64_t groups = (int64_t)p.ntile * p.CG, round = kCUs * 2;
   p.order = packed && !p.chunks && groups > round && groups <= 32 * round &&
             (groups < 16 * round || rows >= 6 * (int64_t)n_seq);
