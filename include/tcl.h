@@ -556,7 +556,8 @@ typedef struct tcl_ssm_scan_args {
 /* d_y [rows, E] with leading dimension ldy; d_state_out [n_slots, E, N] or NULL; both
  * pools 16-byte aligned. d_workspace: >= tcl_ssm_scan_workspace_bytes bytes, 256-byte
  * aligned; that is 0 (and d_workspace may be NULL) for batches of short or many sequences, and
- * for single tokens (L = 1). */
+ * for single tokens (L = 1). In a batch of many sequences each is walked whole, so one that is
+ * far longer than the others sets the time and is better given a call of its own. */
 TCL_API size_t tcl_ssm_scan_workspace_bytes(int32_t n_seq, int32_t rows, int32_t E, int32_t N, int32_t L);
 TCL_API tcl_status tcl_ssm_scan(const tcl_ssm_scan_args* args, const int32_t* d_slots, int32_t n_slots,
                                 float* d_state_out, void* d_y, int64_t ldy, void* d_workspace, size_t ws_bytes,
