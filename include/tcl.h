@@ -594,6 +594,95 @@ TCL_API tcl_status tcl_ssm_scan_backward(const tcl_ssm_scan_args* args, const vo
                                          void* d_workspace, size_t ws_bytes, void* stream);
 
 /* ---------------------------------------------------------------------
+ * The gated delta rule: a layer whose heads carry a matrix, with the sequences, states and slots of
+ * the sequence operators above (their conventions hold here too). Per value head, with
+ * a state S [Dk, Dv], each token does
+ *   S <- e^g S,   u = beta (v - S^T k),   S <- S + k u^T,   o = scale S^T q.
+ * H value heads share Hk key heads, H / Hk neighbours each (value head h reads q and k of
+ * key head h / (H / Hk)). q and k are taken as they are: layers that want unit length norm
+ * them first. g is any decay that is not NaN, -inf (forget all) among them; with beta |k|^2 above 2 the rule itself
+ * grows without bound.
+ *
+ * Dk in [8, 128], Dv in [8, 256], multiples of 8; H at most 1024; rows H at most 2^28, n_seq H below
+ * 2^20. Activations fp32 or bf16 of any alignment, g, beta and the states fp32; all sums are fp32 (fp32-level
+ * products on the matrix cores), results rounded to dtype once. Stream-ordered, deterministic, no allocation; may be
+ * captured into a graph.
+ * ------------------------------------------------------------------- */
+typedef struct tcl_delta_rule_args {
+  int32_t dtype;         /* tcl_dtype                                        */
+  int32_t n_seq, rows;   /* sequences; rows of the activations               */
+  int32_t Hk, H;         /* key heads, value heads                           */
+  int32_t Dk, Dv;        /* a head's state                                   */
+  float scale;           /* of the answers o                                 */
+  const int32_t* d_offs; /* [n_seq + 1] or NULL: a token of each sequence    */
+  const void* d_q;       /* [rows, Hk, Dk], a row's heads beside each other  */
+  int64_t ldq;
+  const void* d_k;       /* [rows, Hk, Dk]                                   */
+  int64_t ldk;
+  const void* d_v;       /* [rows, H, Dv]                                    */
+  int64_t ldv;
+  const float* d_g;      /* [rows, H] logarithms of the decays               */
+  int64_t ldg;
+  const float* d_beta;   /* [rows, H]                                        */
+  int64_t ldbeta;
+  const float* d_state;  /* [n_slots, H, Dk, Dv] states at the start, or NULL; 16-byte aligned */
+} tcl_delta_rule_args;
+
+/* d_o [rows, H, Dv] with leading dimension ldo; d_state_out [n_slots, H, Dk, Dv] or NULL, 16-byte aligned, may be
+ * d_state. d_workspace: >= tcl_delta_rule_workspace_bytes bytes, 256-byte aligned (0, and NULL, for
+ * single tokens, where d_offs is NULL). */
+TCL_API size_t tcl_delta_rule_workspace_bytes(int32_t dtype, int32_t n_seq, int32_t rows, int32_t Hk, int32_t H,
+                                              int32_t Dk, int32_t Dv);
+TCL_API tcl_status tcl_delta_rule(const tcl_delta_rule_args* args, const int32_t* d_slots, int32_t n_slots,
+                                  float* d_state_out, void* d_o, int64_t ldo, void* d_workspace, size_t ws_bytes,
+                                  void* stream);
+
+/* Where the gradients go: of the activations' type, g's and beta's fp32. */
+typedef struct tcl_delta_rule_grads {
+  void* d_dq;       /* [rows, Hk, Dk], summed over the value heads that share it */
+  int64_t lddq;
+  void* d_dk;       /* [rows, Hk, Dk] */
+  int64_t lddk;
+  void* d_dv;       /* [rows, H, Dv]  */
+  int64_t lddv;
+  float* d_dg;      /* [rows, H]      */
+  int64_t lddg;
+  float* d_dbeta;   /* [rows, H]      */
+  int64_t lddbeta;
+  float* d_dstate;  /* [n_seq, H, Dk, Dv] gradient of the states at the start, or NULL; 16-byte aligned */
+} tcl_delta_rule_grads;
+
+/* Gradients from the inputs and d_do [rows, H, Dv] (lddo); nothing is kept from the forward
+ * call. d_dstate_out [n_seq, H, Dk, Dv]: the gradient of the end states (NULL: zeros). State i belongs to
+ * sequence i (no slots). No sequences at all are refused (TCL_ERR_INVALID_ARG). */
+TCL_API size_t tcl_delta_rule_backward_workspace_bytes(int32_t dtype, int32_t n_seq, int32_t rows, int32_t Hk,
+                                                       int32_t H, int32_t Dk, int32_t Dv);
+TCL_API tcl_status tcl_delta_rule_backward(const tcl_delta_rule_args* args, const void* d_do, int64_t lddo,
+                                           const float* d_dstate_out, const tcl_delta_rule_grads* grads,
+                                           void* d_workspace, size_t ws_bytes, void* stream);
+
+/* ---------------------------------------------------------------------
+ * Layer norm over the C columns of each row, in front of a block:
+ *   h = (x - mean x) / sqrt(mean (x - mean x)^2 + eps),   y = h w + b.
+ * x and y are fp32 or bf16 (dtype) of any alignment, rows with a leading dimension >= C; w and b [C] fp32, NULL: ones,
+ * zeros. Statistics are fp32, the variance from deviations; y is rounded to dtype once and must not
+ * overlap x. eps finite, not negative (0: a row of equal values gives NaN); C in [1, 16384], rows <= 2^30; rows == 0
+ * is TCL_OK. Stream-ordered, deterministic, no allocation.
+ * ------------------------------------------------------------------- */
+TCL_API tcl_status tcl_layer_norm(int32_t dtype, int32_t rows, int32_t C, const void* d_x, int64_t ldx,
+                                  const float* d_w, const float* d_b, float eps, void* d_y, int64_t ldy,
+                                  void* stream);
+
+/* Gradients from x, w and d_dy [rows, C] (lddy); nothing is kept from the forward call. d_dx [rows, C] (lddx)
+ * has x's type and must not overlap the inputs; d_dw and d_db (NULL: not wanted) [C] are fp32, summed over all rows
+ * and overwritten (zeros for no rows). d_workspace: >= tcl_layer_norm_workspace_bytes bytes, 256-byte aligned. */
+TCL_API size_t tcl_layer_norm_workspace_bytes(int32_t dtype, int32_t rows, int32_t C);
+TCL_API tcl_status tcl_layer_norm_backward(int32_t dtype, int32_t rows, int32_t C, const void* d_x, int64_t ldx,
+                                           const float* d_w, float eps, const void* d_dy, int64_t lddy, void* d_dx,
+                                           int64_t lddx, float* d_dw, float* d_db, void* d_workspace,
+                                           size_t ws_bytes, void* stream);
+
+/* ---------------------------------------------------------------------
  * Operators on rows of logits: what a model answers with (log
  * probabilities), and learning from a teacher's most likely answers. A row
  * is V entries of an [n_rows, ld] array (d_seg_offsets NULL; entries are counted
@@ -644,6 +733,42 @@ TCL_API tcl_status tcl_distill_topk(int32_t dtype, int32_t n_rows, int32_t V, co
                                     const int32_t* d_top, const float* d_teacher, const float* d_weight,
                                     float* d_loss, void* d_grad, int64_t ldg, void* d_workspace, size_t ws_bytes,
                                     void* stream);
+
+/* Beam search. n_groups requests have W beams each; row g W + b belongs to beam b of group g.
+ *
+ * The selection: candidate (b, v) is beam b followed by token v, with the score
+ *   d_score[g, b] + log p_b(v),   p = softmax(logits / temperature),
+ * d_score [n_groups, W] fp32 the beams' own. A group's K best go to d_parent (the row g W + b), d_token
+ * (v) and d_out_score, all [n_groups, K]: highest first, equal scores by lower row, then by lower token
+ * (compared in 64 bits, rounded to fp32 at the end). d_ended [n_groups, W] int32 or NULL: a beam with an entry
+ * >= 0 has ended, and is one candidate itself, with that entry as its token and its own score. A beam
+ * whose score is -inf or NaN is dead. Neither's logits are read. Masked (-inf) and NaN logits, and rows with a logit of
+ * +inf, are no candidates; past the end of a group with fewer than K: -1, -1 and -inf. logits
+ * as for tcl_logprobs (rows); W and K in [1, 64], n_groups W < 2^22. d_workspace: >=
+ * tcl_beam_select_workspace_bytes bytes, 256-byte aligned. n_groups == 0 is TCL_OK. */
+TCL_API size_t tcl_beam_select_workspace_bytes(int32_t n_groups, int32_t W, int32_t V, int32_t K);
+TCL_API tcl_status tcl_beam_select(int32_t dtype, int32_t n_groups, int32_t W, int32_t V, const void* d_logits,
+                                   int64_t ld, float temperature, const float* d_score, const int32_t* d_ended,
+                                   int32_t K, int32_t* d_parent, int32_t* d_token, float* d_out_score,
+                                   void* d_workspace, size_t ws_bytes, void* stream);
+
+/* A pool of states, [n_slots] of `bytes` bytes each (1 to 2^31), contiguous, of any alignment. */
+typedef struct tcl_beam_pool {
+  void* d_states;
+  int64_t bytes;
+} tcl_beam_pool;
+
+/* The reordering that follows: d_parent [n_groups, W] int32 holds, for each new beam, the row of the beam
+ * it continues (of its own group; any other value: none). d_slots [n_groups, W]: where the old beams' states are in
+ * the pools (distinct; outside [0, n_slots): nowhere). d_slots_out [n_groups, W] receives the new beams' places: the
+ * first child of a parent keeps the parent's, the others and beams without a parent take, in their order, those
+ * of the parents without a child, in theirs. The states of the other children are copied there, in every
+ * pool; all other places are left as they are. So a group's set of places stays the same, and
+ * a search in which every beam goes on copies nothing. d_slots_out must not overlap the inputs. pools: an array in
+ * host memory, read before the call returns. Stream-ordered, no allocation. */
+TCL_API tcl_status tcl_beam_reorder(int32_t n_groups, int32_t W, const int32_t* d_parent, const int32_t* d_slots,
+                                    int32_t n_slots, int32_t* d_slots_out, int32_t n_pools,
+                                    const tcl_beam_pool* pools, void* stream);
 
 /* Message describing the last failure on this thread ("" if none). */
 TCL_API const char* tcl_last_error(void);

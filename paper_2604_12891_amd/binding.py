@@ -71,11 +71,35 @@ class SsmScanGrads(ctypes.Structure):
                 ("d_db_dt", ctypes.c_void_p), ("d_dstate", ctypes.c_void_p)]
 
 
+class DeltaRuleArgs(ctypes.Structure):
+    """tcl_delta_rule_args."""
+    _fields_ = [(n, ctypes.c_int32) for n in ("dtype", "n_seq", "rows", "Hk", "H", "Dk", "Dv")] + [
+        ("scale", ctypes.c_float), ("d_offs", ctypes.c_void_p), ("d_q", ctypes.c_void_p), ("ldq", ctypes.c_int64),
+        ("d_k", ctypes.c_void_p), ("ldk", ctypes.c_int64), ("d_v", ctypes.c_void_p), ("ldv", ctypes.c_int64),
+        ("d_g", ctypes.c_void_p), ("ldg", ctypes.c_int64), ("d_beta", ctypes.c_void_p), ("ldbeta", ctypes.c_int64),
+        ("d_state", ctypes.c_void_p)]
+
+
+class DeltaRuleGrads(ctypes.Structure):
+    """tcl_delta_rule_grads."""
+    _fields_ = [("d_dq", ctypes.c_void_p), ("lddq", ctypes.c_int64), ("d_dk", ctypes.c_void_p),
+                ("lddk", ctypes.c_int64), ("d_dv", ctypes.c_void_p), ("lddv", ctypes.c_int64),
+                ("d_dg", ctypes.c_void_p), ("lddg", ctypes.c_int64), ("d_dbeta", ctypes.c_void_p),
+                ("lddbeta", ctypes.c_int64), ("d_dstate", ctypes.c_void_p)]
+
+
+class BeamPool(ctypes.Structure):
+    """tcl_beam_pool."""
+    _fields_ = [("d_states", ctypes.c_void_p), ("bytes", ctypes.c_int64)]
+
+
 # The same layouts as bytes: packing them takes a fraction of a ctypes structure's time, which
 # a single token's call would notice.
 _PACK_CONV = struct.Struct("@5iPPqPPP")
 _PACK_SCAN = struct.Struct("@6iPPqPqPqPqPqPPPP")
 _PACK_GRADS = struct.Struct("@PqPqPqPqPqPPPP")
+_PACK_DELTA = struct.Struct("@7ifPPqPqPqPqPqP")
+_PACK_DELTA_GRADS = struct.Struct("@PqPqPqPqPqP")
 
 _vp, _i32, _sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_size_t
 _i64, _f32 = ctypes.c_int64, ctypes.c_float
@@ -131,6 +155,17 @@ _SIGS = {
     "tcl_logprobs": (_i32, [_i32, _i32, _i32, _vp, _i64, _vp, _f32, _vp, _i32, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
     "tcl_distill_topk": (_i32, [_i32, _i32, _i32, _vp, _i64, _vp, _f32, _i32, _vp, _vp, _vp, _vp, _vp, _i64, _vp, _sz,
                                 _vp]),
+    "tcl_delta_rule_workspace_bytes": (_sz, [_i32] * 7),
+    "tcl_delta_rule": (_i32, [_vp, _vp, _i32, _vp, _vp, _i64, _vp, _sz, _vp]),
+    "tcl_delta_rule_backward_workspace_bytes": (_sz, [_i32] * 7),
+    "tcl_delta_rule_backward": (_i32, [_vp, _vp, _i64, _vp, _vp, _vp, _sz, _vp]),
+    "tcl_layer_norm": (_i32, [_i32, _i32, _i32, _vp, _i64, _vp, _vp, _f32, _vp, _i64, _vp]),
+    "tcl_layer_norm_workspace_bytes": (_sz, [_i32] * 3),
+    "tcl_layer_norm_backward": (_i32, [_i32, _i32, _i32, _vp, _i64, _vp, _f32, _vp, _i64, _vp, _i64, _vp, _vp, _vp,
+                                       _sz, _vp]),
+    "tcl_beam_select_workspace_bytes": (_sz, [_i32] * 4),
+    "tcl_beam_select": (_i32, [_i32, _i32, _i32, _i32, _vp, _i64, _f32, _vp, _vp, _i32, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "tcl_beam_reorder": (_i32, [_i32, _i32, _vp, _vp, _i32, _vp, _i32, _vp, _vp]),
     "tcl_trainer_timing_enable": (_i32, [_vp, _i32]),
     "tcl_trainer_timing_count": (_i32, [_vp]),
     "tcl_trainer_timing_get": (_i32, [_vp, _i32, ctypes.POINTER(ctypes.c_char_p), ctypes.POINTER(ctypes.c_double),
@@ -772,6 +807,154 @@ def ssm_scan_backward(u, dt, A_log, B, C, dy, D=None, z=None, b_dt=None, offs=No
     return r
 
 
+def _heads_ld(name, t, dtype, shape, like) -> int:
+    """Checks a tensor [rows, heads, width] whose rows are contiguous; its leading dimension."""
+    if t.dtype is not dtype or t.shape != shape:
+        raise ValueError(f"{name}: {dtype} {tuple(shape)} expected, not {t.dtype} {tuple(t.shape)}")
+    if t.get_device() != like.get_device():
+        raise ValueError(f"{name} is on {t.device}, not on {like.device}")
+    width = shape[1] * shape[2]
+    if t.is_contiguous():
+        return width
+    if (shape[2] != 1 and t.stride(2) != 1) or (shape[1] != 1 and t.stride(1) != shape[2]) or (
+            shape[0] != 1 and t.stride(0) < width):
+        raise ValueError(f"{name}: rows not contiguous (strides {t.stride()})")
+    return max(t.stride(0), width)
+
+
+def _delta_args(q, k, v, g, beta, scale, offs, state):
+    """(number of sequences, the packed tcl_delta_rule_args)"""
+    import torch
+    for name, t in (("q", q), ("v", v)):
+        if t.dim() != 3:
+            raise ValueError(f"{name}: [rows, heads, width] expected, not {tuple(t.shape)}")
+    _on_device(q)
+    n_seq = q.shape[0]
+    if offs is not None:
+        if offs.dim() != 1 or offs.numel() < 1:
+            raise ValueError("offs: [n_seq + 1] expected")
+        _expect("offs", offs, torch.int32, offs.shape, q)
+        n_seq = offs.numel() - 1
+    (rows, Hk, Dk), (_, H, Dv) = q.shape, v.shape
+    ldq, ldk = _heads_ld("q", q, q.dtype, q.shape, q), _heads_ld("k", k, q.dtype, q.shape, q)
+    ldv = _heads_ld("v", v, q.dtype, (rows, H, Dv), q)
+    ldg, ldb = _row_ld("g", g, torch.float32, (rows, H), q), _row_ld("beta", beta, torch.float32, (rows, H), q)
+    return n_seq, _PACK_DELTA.pack(_dtype(q), n_seq, rows, Hk, H, Dk, Dv, Dk ** -0.5 if scale is None else scale,
+                                   _adr(offs), q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(), ldv, g.data_ptr(),
+                                   ldg, beta.data_ptr(), ldb, _adr(state))
+
+
+def delta_rule_workspace(dtype, n_seq, rows, Hk, H, Dk, Dv, backward=False):
+    """A workspace for delta_rule (or delta_rule_backward) with these sizes and torch type, on the
+    current device."""
+    import torch
+    f = lib().tcl_delta_rule_backward_workspace_bytes if backward else lib().tcl_delta_rule_workspace_bytes
+    size = f(TCL_BF16 if dtype is torch.bfloat16 else TCL_F32, n_seq, rows, Hk, H, Dk, Dv)
+    return torch.empty(size, dtype=torch.uint8, device="cuda")
+
+
+def delta_rule(q, k, v, g, beta, scale=None, offs=None, state=None, state_out=None, slots=None, out=None,
+               workspace=None, stream=None):
+    """The gated delta rule with carried states (tcl_delta_rule): q, k [rows, Hk, Dk] and v [rows, H, Dv]
+    fp32 or bf16, g (logarithms of the decays) and beta [rows, H] and the states [n, H, Dk, Dv]
+    fp32; scale None: Dk ** -0.5. offs int32 [n_seq + 1]: packed sequences; None: each row is one token of its own
+    sequence. state / state_out (may be the same tensor) with slots int32 [n_seq] into them. Returns o
+    [rows, H, Dv]."""
+    if stream is not None:
+        return _under(stream, delta_rule, q, k, v, g, beta, scale, offs, state, state_out, slots, out, workspace)
+    import torch
+    n_seq, a = _delta_args(q, k, v, g, beta, scale, offs, state)
+    shape = (v.shape[1], q.shape[2], v.shape[2])
+    n_slots = _pools(state, state_out, slots, n_seq, shape, torch.float32, q)
+    if out is None:
+        out = torch.empty(v.shape, dtype=v.dtype, device=v.device)
+        ldo = v.shape[1] * v.shape[2]
+    else:
+        ldo = _heads_ld("out", out, q.dtype, v.shape, q)
+    ws = None if offs is None else _workspace(workspace, q, lib().tcl_delta_rule_workspace_bytes, _dtype(q), n_seq,
+                                              q.shape[0], q.shape[1], *shape)
+    check(lib().tcl_delta_rule(a, _ptr(slots), n_slots, _ptr(state_out), out.data_ptr(), ldo, *_ws_args(ws),
+                               _stream_of(q)))
+    return out
+
+
+def delta_rule_backward(q, k, v, g, beta, do, scale=None, offs=None, state=None, state_grad=None, workspace=None,
+                        out=None, stream=None):
+    """Gradients of delta_rule (tcl_delta_rule_backward) from do [rows, H, Dv] and, for carried states
+    [n_seq, H, Dk, Dv], the gradient state_grad of the end states. Returns a dict of dq, dk, dv, dg, dbeta and
+    dstate (None without a state); out: contiguous tensors of those names to write to. Rows that no sequence owns
+    are left as they are (in a new tensor: undefined). A batch of no sequences at all is refused."""
+    if stream is not None:
+        return _under(stream, delta_rule_backward, q, k, v, g, beta, do, scale, offs, state, state_grad, workspace, out)
+    import torch
+    n_seq, a = _delta_args(q, k, v, g, beta, scale, offs, state)
+    lddo = _heads_ld("do", do, q.dtype, v.shape, q)
+    f32, full = torch.float32, (n_seq, v.shape[1], q.shape[2], v.shape[2])
+    for name, t in (("state", state), ("state_grad", state_grad)):
+        _expect(name, t, f32, full, q)
+    r = _results(dict(dq=(q.shape, q.dtype, False), dk=(q.shape, q.dtype, False), dv=(v.shape, q.dtype, False),
+                      dg=(v.shape[:2], f32, False), dbeta=(v.shape[:2], f32, False),
+                      dstate=None if state is None else (full, f32, False)), out, q)
+    qk, H = q.shape[1] * q.shape[2], v.shape[1]
+    gr = _PACK_DELTA_GRADS.pack(r["dq"].data_ptr(), qk, r["dk"].data_ptr(), qk, r["dv"].data_ptr(), H * v.shape[2],
+                                r["dg"].data_ptr(), H, r["dbeta"].data_ptr(), H, _adr(r["dstate"]))
+    ws = _workspace(workspace, q, lib().tcl_delta_rule_backward_workspace_bytes, _dtype(q), n_seq, q.shape[0],
+                    q.shape[1], H, q.shape[2], v.shape[2])
+    check(lib().tcl_delta_rule_backward(a, do.data_ptr(), lddo, _ptr(state_grad), gr, *_ws_args(ws), _stream_of(q)))
+    return r
+
+
+def _row_matrix(x):
+    if x.dim() != 2:
+        raise ValueError(f"[rows, channels] expected, not {tuple(x.shape)}")
+    _on_device(x)
+    return x.shape
+
+
+def layer_norm(x, w=None, b=None, eps=1e-5, out=None, stream=None):
+    """Layer norm over the columns of x [rows, C] fp32 or bf16 (tcl_layer_norm); w, b [C] fp32
+    (None: ones, zeros). Returns y [rows, C]."""
+    if stream is not None:
+        return _under(stream, layer_norm, x, w, b, eps, out)
+    import torch
+    rows, C = _row_matrix(x)
+    ldx = _row_ld("x", x, x.dtype, x.shape, x)
+    _expect("w", w, torch.float32, (C,), x)
+    _expect("b", b, torch.float32, (C,), x)
+    if out is None:
+        out, ldy = torch.empty(x.shape, dtype=x.dtype, device=x.device), C
+    else:
+        ldy = _row_ld("out", out, x.dtype, x.shape, x)
+    check(lib().tcl_layer_norm(_dtype(x), rows, C, x.data_ptr(), ldx, _ptr(w), _ptr(b), eps, out.data_ptr(), ldy,
+                               _stream_of(x)))
+    return out
+
+
+def layer_norm_workspace(dtype, rows, C):
+    """A workspace for layer_norm_backward of this torch type, on the current device."""
+    import torch
+    size = lib().tcl_layer_norm_workspace_bytes(TCL_BF16 if dtype is torch.bfloat16 else TCL_F32, rows, C)
+    return torch.empty(size, dtype=torch.uint8, device="cuda")
+
+
+def layer_norm_backward(x, w, dy, eps=1e-5, workspace=None, out=None, stream=None):
+    """Gradients of layer_norm (tcl_layer_norm_backward) from dy [rows, C]; w as there. Returns a dict of
+    dx, dw and db; out: tensors of those names to write to."""
+    if stream is not None:
+        return _under(stream, layer_norm_backward, x, w, dy, eps, workspace, out)
+    import torch
+    rows, C = _row_matrix(x)
+    ldx, lddy = _row_ld("x", x, x.dtype, x.shape, x), _row_ld("dy", dy, x.dtype, x.shape, x)
+    _expect("w", w, torch.float32, (C,), x)
+    vec = ((C,), torch.float32, False)
+    r = _results(dict(dx=(x.shape, x.dtype, True), dw=vec, db=vec), out, x)
+    ws = _workspace(workspace, x, lib().tcl_layer_norm_workspace_bytes, _dtype(x), rows, C)
+    check(lib().tcl_layer_norm_backward(_dtype(x), rows, C, x.data_ptr(), ldx, _ptr(w), eps, dy.data_ptr(), lddy,
+                                        r["dx"].data_ptr(), _ld(r["dx"]), r["dw"].data_ptr(), r["db"].data_ptr(),
+                                        *_ws_args(ws), _stream_of(x)))
+    return r
+
+
 def logits_workspace(n_rows, V, K):
     """A workspace for logprobs and distill_topk with these sizes, on the
     current device."""
@@ -849,6 +1032,66 @@ def distill_topk(logits, top, teacher, weight=None, temperature=1.0, seg_offsets
                                  top.data_ptr(), teacher.data_ptr(), _ptr(weight), loss.data_ptr(), _ptr(grad), ldg,
                                  *_ws_args(ws), _stream_of(logits)))
     return dict(loss=loss, grad=grad)
+
+
+def beam_select_workspace(groups, W, V, K):
+    """A workspace for beam_select with these sizes, on the current device."""
+    import torch
+    return torch.empty(lib().tcl_beam_select_workspace_bytes(groups, W, V, K), dtype=torch.uint8, device="cuda")
+
+
+def beam_select(logits, score, K=None, ended=None, temperature=1.0, workspace=None, stream=None):
+    """The K (None: W) best continuations of each group's W beams (tcl_beam_select): logits fp32 or bf16
+    [groups * W, V], score fp32 [groups, W] (-inf: a dead beam), ended int32 [groups, W] (>= 0: the beam has ended,
+    with that token). Returns a dict of parent (rows of logits), token int32 and score fp32, all [groups, K]."""
+    if stream is not None:
+        return _under(stream, beam_select, logits, score, K, ended, temperature, workspace)
+    import torch
+    n, V, ld = _logit_rows(logits, None, None)
+    if score.dim() != 2 or score.numel() != n:
+        raise ValueError(f"score: [groups, W] with {n} beams expected, not {tuple(score.shape)}")
+    G, W = score.shape
+    _expect("score", score, torch.float32, (G, W), logits)
+    _expect("ended", ended, torch.int32, (G, W), logits)
+    K = W if K is None else K
+    r = dict(parent=torch.empty(G, max(K, 0), dtype=torch.int32, device=logits.device),
+             token=torch.empty(G, max(K, 0), dtype=torch.int32, device=logits.device),
+             score=torch.empty(G, max(K, 0), dtype=torch.float32, device=logits.device))
+    ws = _workspace(workspace, logits, lib().tcl_beam_select_workspace_bytes, G, W, V, K)
+    check(lib().tcl_beam_select(_dtype(logits), G, W, V, logits.data_ptr(), ld, temperature, score.data_ptr(),
+                                _ptr(ended), K, r["parent"].data_ptr(), r["token"].data_ptr(), r["score"].data_ptr(),
+                                *_ws_args(ws), _stream_of(logits)))
+    return r
+
+
+def beam_reorder(parent, slots, pools, out=None, stream=None):
+    """The beams' states after a selection (tcl_beam_reorder): parent int32 [groups, W], the rows that the new
+    beams continue; slots int32 [groups, W], the old beams' places in every one of pools (contiguous tensors
+    [n_slots, ...] of any type, changed in place). Returns the new beams' places [groups, W]."""
+    if stream is not None:
+        return _under(stream, beam_reorder, parent, slots, pools, out)
+    import torch
+    if parent.dim() != 2:
+        raise ValueError(f"parent: [groups, W] expected, not {tuple(parent.shape)}")
+    _on_device(parent)
+    G, W = parent.shape
+    for name, t in (("parent", parent), ("slots", slots), ("out", out)):
+        _expect(name, t, torch.int32, (G, W), parent)
+    n_slots = 0
+    array = (BeamPool * max(len(pools), 1))()
+    for i, t in enumerate(pools):
+        if t.dim() < 1 or not t.is_contiguous() or t.get_device() != parent.get_device():
+            raise ValueError(f"pools[{i}]: contiguous states on {parent.device} expected")
+        if i and t.shape[0] != n_slots:
+            raise ValueError(f"pools of {n_slots} and {t.shape[0]} states")
+        n_slots = t.shape[0]
+        array[i].d_states = t.data_ptr()
+        array[i].bytes = t.numel() // max(n_slots, 1) * t.element_size() if n_slots else 1
+    if out is None:
+        out = torch.empty(G, W, dtype=torch.int32, device=parent.device)
+    check(lib().tcl_beam_reorder(G, W, parent.data_ptr(), slots.data_ptr(), n_slots, out.data_ptr(), len(pools), array,
+                                 _stream_of(parent)))
+    return out
 
 
 def teacher_gate(e, out=None, stream=None):

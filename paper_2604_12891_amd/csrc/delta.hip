@@ -1,0 +1,988 @@
+// The gated delta rule with carried states: prompts, single tokens, gradients.
+//
+// Per value head, with a state S [Dk, Dv], each token does
+//   S <- e^g S,  u = beta (v - S^T k),  S <- S + k u^T,  o = scale S^T q.
+// A chunk of kC tokens with the state S0 in front of it, G_i = g_1 + .. + g_i, D_ij = e^(G_i - G_j) and
+//   A_ij = beta_i D_ij k_i.k_j (j < i),  T = (I + A)^-1,  P_ij = scale D_ij q_i.k_j (j <= i)
+// does the same as
+//   R = beta (V - e^G K S0),  U = T R,  O = scale e^G Q S0 + P U,  S1 = e^G_C S0 + K^T (w U),  w_j = e^(G_C - G_j).
+// T, P and the factors need no state: delta_prep_kernel forms them for all chunks at once, and what walks
+// the chunks in order is left with matrix products. States do not mix their columns (Dv), so the walk is also
+// spread over slices of them.
+//
+// G is summed and subtracted in 64 bits and its exponentials are taken of the differences: with g down to
+// -inf, e^G_i / e^G_j would be 0 / 0 where D_ij is 1. A decay below e^-10000 counts as that.
+#include <algorithm>
+
+#include "common.h"
+#include "ops.h"
+#include "packing.h"
+
+namespace tcl {
+namespace {
+
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kC = 64;        // tokens of a chunk
+constexpr int kMat = kC * kC;  // entries of T or P
+
+__device__ __forceinline__ float to_f32(float v) { return v; }
+__device__ __forceinline__ float to_f32(uint16_t v) { return bf16_to_f32(v); }
+__device__ __forceinline__ void st1(float* p, float v) { *p = v; }
+__device__ __forceinline__ void st1(uint16_t* p, float v) { *p = f32_to_bf16(v); }
+
+// Four neighbours of a row, widened, and back; rows start at any element.
+typedef floatx4 floatx4_any __attribute__((aligned(4)));
+typedef u32x2 u32x2_any __attribute__((aligned(2)));
+__device__ __forceinline__ floatx4 ld4(const float* p) { return *reinterpret_cast<const floatx4_any*>(p); }
+__device__ __forceinline__ floatx4 ld4(const uint16_t* p) {
+  const u32x2 x = *reinterpret_cast<const u32x2_any*>(p);
+  return floatx4{__uint_as_float(x[0] << 16), __uint_as_float(x[0] & 0xFFFF0000u), __uint_as_float(x[1] << 16),
+                 __uint_as_float(x[1] & 0xFFFF0000u)};
+}
+__device__ __forceinline__ void st4(float* p, floatx4 v) { *reinterpret_cast<floatx4_any*>(p) = v; }
+__device__ __forceinline__ void st4(uint16_t* p, floatx4 v) {
+  *reinterpret_cast<u32x2_any*>(p) = u32x2{f32x2_to_bf16x2(v[0], v[1]), f32x2_to_bf16x2(v[2], v[3])};
+}
+
+// e^x of a sum of logarithms in 64 bits, to an fp32 rounding or two.
+__device__ __forceinline__ float exp_of(double x) {
+  const double t = x * 1.4426950408889634;
+  const double n = __builtin_rint(t);
+  return ldexpf(__builtin_amdgcn_exp2f((float)(t - n)), n < -1000.0 ? -1000 : n > 1000.0 ? 1000 : (int)n);
+}
+__device__ __forceinline__ double log_decay(float g) { return g < -1e4f ? -1e4 : (double)g; }
+
+struct DeltaIn {
+  const int* offs;
+  int n_seq, rows, Hk, H, Dk, Dv;
+  int64_t ldq, ldk, ldv, ldg, ldb;
+  const float *g, *beta;
+  float scale;
+  const float* state;
+  const int* slots;
+  int n_slots;
+};
+
+// ---------------------------------------------------------------- token by token
+// A wavefront holds 32 columns of a head's state: lane l columns 4 (l / 8) .. + 3 of rows RK (l % 8) .. + RK - 1, so
+// that sums over the rows are lanes' neighbours (DPP) and a state's lines are read whole. With
+// p = S^T k and r = S^T q of the state before the token,
+//   u = beta (v - a p),  o = scale (a r + (k.q) u),  S <- a S + k u^T:
+// one reduction per token. Single tokens are bound by the states' bytes; sequences by the chain of a token's
+// products, reduction and update.
+template <int CTRL>
+__device__ __forceinline__ float dpp(float v) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xF, 0xF, false));
+}
+__device__ __forceinline__ float sum8(float v) {
+  v += dpp<0xB1>(v);   // xor 1
+  v += dpp<0x4E>(v);   // xor 2
+  return v + dpp<0x141>(v);  // the other four of eight
+}
+
+template <typename T, int RK>
+__global__ __launch_bounds__(64) void delta_walk_kernel(DeltaIn a, const T* __restrict__ q, const T* __restrict__ k,
+                                                        const T* __restrict__ v, float* state_out, T* __restrict__ o,
+                                                        int64_t ldo) {
+  const int lane = threadIdx.x, kg = lane & 7, parts = (a.Dv + 31) / 32;
+  const int h = (int)(blockIdx.x / parts % a.H), seq = (int)(blockIdx.x / parts / a.H);
+  const int c = (int)(blockIdx.x % parts) * 32 + (lane >> 3) * 4, r0 = kg * RK;
+  const bool live = c < a.Dv;
+  int base = seq, len = 1;
+  if (a.offs) {
+    base = min(max(a.offs[seq], 0), a.rows);
+    len = min(max(a.offs[seq + 1], base), a.rows) - base;
+  }
+  const int slot = slot_of(a.slots, a.n_slots, seq);
+  const int64_t at = (((int64_t)slot * a.H + h) * a.Dk + r0) * a.Dv + c;
+  floatx4 s[RK];
+#pragma unroll
+  for (int i = 0; i < RK; ++i) {
+    s[i] = floatx4{0.f, 0.f, 0.f, 0.f};
+    if (a.state && slot >= 0 && live && r0 + i < a.Dk)
+      s[i] = *reinterpret_cast<const floatx4*>(a.state + at + (int64_t)i * a.Dv);
+  }
+  const int hk = h / (a.H / a.Hk);
+  const T* kp = k + base * a.ldk + (int64_t)hk * a.Dk + r0;
+  const T* qp = q + base * a.ldq + (int64_t)hk * a.Dk + r0;
+  const T* vp = v + base * a.ldv + (int64_t)h * a.Dv + c;
+  const float* gp = a.g + base * a.ldg + h;
+  const float* bp = a.beta + base * a.ldb + h;
+  T* op = o + base * ldo + (int64_t)h * a.Dv + c;
+  floatx4 kn[RK / 4], qn[RK / 4], vn = {0.f, 0.f, 0.f, 0.f};
+  float gn = 0.f, bn = 0.f;
+  auto fetch = [&](int t) {
+#pragma unroll
+    for (int i = 0; i < RK / 4; ++i) {
+      kn[i] = qn[i] = floatx4{0.f, 0.f, 0.f, 0.f};
+      if (r0 + 4 * i < a.Dk) {
+        kn[i] = ld4(kp + t * a.ldk + 4 * i);
+        qn[i] = ld4(qp + t * a.ldq + 4 * i);
+      }
+    }
+    if (live) vn = ld4(vp + t * a.ldv);
+    gn = gp[t * a.ldg];
+    bn = bp[t * a.ldb];
+  };
+  if (len > 0) fetch(0);
+  for (int t = 0; t < len; ++t) {
+    floatx4 kv[RK / 4], qv[RK / 4];
+    const floatx4 vv = vn;
+    const float dec = exp_of(log_decay(gn)), beta = bn;
+#pragma unroll
+    for (int i = 0; i < RK / 4; ++i) {
+      kv[i] = kn[i];
+      qv[i] = qn[i];
+    }
+    if (t + 1 < len) fetch(t + 1);
+    floatx4 p = {0.f, 0.f, 0.f, 0.f}, r = p;
+    float kq = 0.f;
+#pragma unroll
+    for (int i = 0; i < RK; ++i) {
+      const float ki = kv[i / 4][i % 4], qi = qv[i / 4][i % 4];
+      kq = fmaf(ki, qi, kq);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        p[j] = fmaf(s[i][j], ki, p[j]);
+        r[j] = fmaf(s[i][j], qi, r[j]);
+      }
+    }
+    kq = sum8(kq);
+    floatx4 u, out;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      u[j] = beta * fmaf(-dec, sum8(p[j]), vv[j]);
+      out[j] = a.scale * fmaf(kq, u[j], dec * sum8(r[j]));
+    }
+#pragma unroll
+    for (int i = 0; i < RK; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) s[i][j] = fmaf(kv[i / 4][i % 4], u[j], dec * s[i][j]);
+    if (kg == 0 && live) st4(op + t * ldo, out);
+  }
+  if (state_out && slot >= 0 && live)
+#pragma unroll
+    for (int i = 0; i < RK; ++i)
+      if (r0 + i < a.Dk) *reinterpret_cast<floatx4*>(state_out + at + (int64_t)i * a.Dv) = s[i];
+}
+
+// ---------------------------------------------------------------- matrix products
+// v_mfma_f32_16x16x4_f32: lane l holds A[l % 16][l / 16], B[l / 16][l % 16] and D[4 (l / 16) + r][l % 16]. The
+// order of the k's is free, so four steps share one 16-byte read where k runs along memory: a
+// fragment of 16 k's is, in lane l, the four entries k = 4 (l / 16) .. + 3 of its row.
+__device__ __forceinline__ floatx4 mma16(floatx4 a, floatx4 b, floatx4 c) {
+#pragma unroll
+  for (int m = 0; m < 4; ++m) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[m], b[m], c, 0, 0, 0);
+  return c;
+}
+// Fragment s of the 16 rows at p (leading dimension ld, in LDS): k along memory, or (frag_t) along the rows.
+__device__ __forceinline__ floatx4 frag(const float* p, int ld, int s) {
+  const int l = threadIdx.x & 63;
+  return *reinterpret_cast<const floatx4*>(p + (l & 15) * ld + 16 * s + 4 * (l >> 4));
+}
+__device__ __forceinline__ floatx4 frag_t(const float* p, int ld, int s) {
+  const int l = threadIdx.x & 63;
+  const float* q = p + (16 * s + 4 * (l >> 4)) * ld + (l & 15);
+  return floatx4{q[0], q[ld], q[2 * ld], q[3 * ld]};
+}
+// A matrix [kC, kC] as fragments: of the 16 rows 16 w .. fragment s.
+__device__ __forceinline__ floatx4 mat_frag(const float* m, int w, int s) {
+  return *reinterpret_cast<const floatx4*>(m + ((w * 4 + s) * 64 + (threadIdx.x & 63)) * 4);
+}
+
+// A chunk of a sequence: its first row and how many tokens it has.
+struct Chunk {
+  int row, n;
+};
+
+// Of a head's rows in a chunk the fragments of the 16 tokens 16 w .., D wide (a multiple of 8), zeros
+// elsewhere.
+template <typename T, int NF>
+__device__ __forceinline__ void row_frags(const T* p, int64_t ld, Chunk c, int w, int D, floatx4* f) {
+  const int l = threadIdx.x & 63, t = 16 * w + (l & 15), k0 = 4 * (l >> 4);
+  const T* q = p + (c.row + min(t, c.n - 1)) * ld + k0;
+#pragma unroll
+  for (int s = 0; s < NF; ++s) {
+    f[s] = floatx4{0.f, 0.f, 0.f, 0.f};
+    if (t < c.n && 16 * s + k0 < D) f[s] = ld4(q + 16 * s);
+  }
+}
+
+// ---------------------------------------------------------------- what needs no state
+// T and P (or, for the gradients, T, T^T and P^T) as fragments and beta, e^G and w of every chunk, a
+// workgroup per chunk and key head, which goes through the value heads that share it. Each of four
+// wavefronts has 16 rows. T: the diagonal blocks of 16 by substitution, a column per lane, then blocks of
+// 32 and 64 by products, T21 = -T22 A21 T11.
+constexpr int kLdM = kC + 4;
+
+template <typename T, int DKP, bool GRADS>
+__global__ __launch_bounds__(256) void delta_prep_kernel(DeltaIn a, const T* __restrict__ q, const T* __restrict__ k,
+                                                         float* __restrict__ mats, float* __restrict__ coef) {
+  __shared__ __attribute__((aligned(16))) float sA[kC * kLdM], sT[kC * kLdM], sX[32 * 36];
+  __shared__ double sG[kC];
+  __shared__ float sB[kC];
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, li = lane & 15, lk = lane >> 4;
+  const int tile = blockIdx.x / a.Hk, hk = blockIdx.x % a.Hk;
+  const Tile tl = find_tile(a.offs, a.n_seq, a.rows, kC, tile);
+  if (tl.seq < 0 || tl.len == 0) return;
+  const Chunk c = {tl.base + tl.j * kC, min(kC, tl.len - tl.j * kC)};
+  constexpr int NF = DKP / 16;
+  // products of rows: lane's entries [16 w + 4 lk + r][16 t + li]
+  floatx4 kk[4], qk[4];
+  {
+    floatx4 kf[NF], qf[NF];
+    const T* kp = k + (int64_t)hk * a.Dk;
+    row_frags<T, NF>(kp, a.ldk, c, w, a.Dk, kf);
+    row_frags<T, NF>(q + (int64_t)hk * a.Dk, a.ldq, c, w, a.Dk, qf);
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      kk[t] = qk[t] = floatx4{0.f, 0.f, 0.f, 0.f};
+      if (t > w || 16 * t >= c.n) continue;
+      floatx4 bf[NF];
+      row_frags<T, NF>(kp, a.ldk, c, t, a.Dk, bf);
+#pragma unroll
+      for (int s = 0; s < NF; ++s) {
+        kk[t] = mma16(kf[s], bf[s], kk[t]);
+        qk[t] = mma16(qf[s], bf[s], qk[t]);
+      }
+    }
+  }
+  const int share = a.H / a.Hk;
+  for (int hv = 0; hv < share; ++hv) {
+    const int h = hk * share + hv;
+    float* out = mats + ((int64_t)tile * a.H + h) * (GRADS ? 3 : 2) * kMat;
+    float* co = coef + ((int64_t)tile * a.H + h) * 3 * kC;
+    __syncthreads();
+    if (tid < kC) {
+      // past the chunk's end nothing decays and nothing is written
+      double G = tid < c.n ? log_decay(a.g[(c.row + tid) * a.ldg + h]) : 0.0;
+      const float beta = tid < c.n ? a.beta[(c.row + tid) * a.ldb + h] : 0.f;
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const double up = __shfl_up(G, o, 64);
+        if (tid >= o) G += up;
+      }
+      sG[tid] = G;
+      sB[tid] = beta;
+      const double end = __shfl(G, kC - 1, 64);
+      co[tid] = beta;
+      co[kC + tid] = exp_of(G);
+      co[2 * kC + tid] = exp_of(end - G);
+    }
+    for (int i = tid; i < kC * kLdM; i += 256) sT[i] = 0.f;
+    __syncthreads();
+    floatx4 pm[4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int i = 16 * w + 4 * lk + r, j = 16 * t + li;
+        const float d = j <= i ? exp_of(sG[i] - sG[j]) : 0.f;
+        sA[i * kLdM + j] = j < i ? sB[i] * d * kk[t][r] : 0.f;
+        pm[t][r] = j <= i ? a.scale * d * qk[t][r] : 0.f;
+      }
+    __syncthreads();
+    {  // diagonal block w, column li (four lanes do the same)
+      const float* A = sA + 16 * w * kLdM + 16 * w;
+      float x[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        float v = i == li ? 1.f : 0.f;
+#pragma unroll
+        for (int j = 0; j < i; ++j) v = fmaf(-A[i * kLdM + j], x[j], v);
+        x[i] = v;
+      }
+      if (lk == 0)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sT[(16 * w + i) * kLdM + 16 * w + li] = x[i];
+    }
+    __syncthreads();
+    const floatx4 zero = {0.f, 0.f, 0.f, 0.f};
+    if (w < 2) {  // blocks of 32, a wavefront each
+      const int b = 32 * w;
+      const floatx4 x = mma16(frag(sA + (b + 16) * kLdM + b, kLdM, 0), frag_t(sT + b * kLdM + b, kLdM, 0), zero);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) sX[(16 * w + 4 * lk + r) * 36 + li] = x[r];
+    }
+    __syncthreads();
+    if (w < 2) {
+      const int b = 32 * w;
+      const floatx4 x = mma16(frag(sT + (b + 16) * kLdM + b + 16, kLdM, 0), frag_t(sX + 16 * w * 36, 36, 0), zero);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) sT[(b + 16 + 4 * lk + r) * kLdM + b + li] = -x[r];
+    }
+    __syncthreads();
+    const int bi = 16 * (w >> 1), bj = 16 * (w & 1);  // the block of 32, a tile per wavefront
+    {
+      floatx4 x = zero;
+#pragma unroll
+      for (int s = 0; s < 2; ++s)
+        x = mma16(frag(sA + (32 + bi) * kLdM, kLdM, s), frag_t(sT + bj, kLdM, s), x);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) sX[(bi + 4 * lk + r) * 36 + bj + li] = x[r];
+    }
+    __syncthreads();
+    {
+      floatx4 x = zero;
+#pragma unroll
+      for (int s = 0; s < 2; ++s)
+        x = mma16(frag(sT + (32 + bi) * kLdM + 32, kLdM, s), frag_t(sX + bj, 36, s), x);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) sT[(32 + bi + 4 * lk + r) * kLdM + bj + li] = -x[r];
+    }
+    __syncthreads();  // P to where A was
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) sA[(16 * w + 4 * lk + r) * kLdM + 16 * t + li] = pm[t][r];
+    __syncthreads();
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      float* p = out + ((w * 4 + s) * 64 + lane) * 4;
+      *reinterpret_cast<floatx4*>(p) = frag(sT + 16 * w * kLdM, kLdM, s);
+      if constexpr (GRADS) {
+        *reinterpret_cast<floatx4*>(p + kMat) = frag_t(sT + 16 * w, kLdM, s);
+        *reinterpret_cast<floatx4*>(p + 2 * kMat) = frag_t(sA + 16 * w, kLdM, s);
+      } else {
+        *reinterpret_cast<floatx4*>(p + kMat) = frag(sA + 16 * w * kLdM, kLdM, s);
+      }
+    }
+  }
+}
+
+// ---------------------------------------------------------------- the walk over chunks
+// A workgroup per sequence, value head and slice of DVS columns, all matrices transposed: columns are
+// rows, so that a lane's four results are neighbours in memory. Each of four wavefronts has 16 tokens, and
+// DKP / 4 rows of the state, which it keeps in registers; a copy in LDS feeds the products. Three barriers
+// a chunk. SAVE (for the gradients): the states in front of the chunks and U are kept, O is not formed.
+template <typename T, int DKP, int DVS, bool SAVE>
+__global__ __launch_bounds__(256) void delta_chunk_kernel(DeltaIn a, const T* __restrict__ q, const T* __restrict__ k,
+                                                          const T* __restrict__ v, const float* __restrict__ mats,
+                                                          const float* __restrict__ coef, float* state_out,
+                                                          T* __restrict__ o, int64_t ldo, float* __restrict__ s0,
+                                                          float* __restrict__ us) {
+  constexpr int NF = DKP / 16, NT = DKP / 64, MB = DVS / 16, LDS = DKP + 4;
+  __shared__ __attribute__((aligned(16))) float sS[DVS * LDS], sK[kC * LDS], sR[DVS * kLdM], sU[DVS * kLdM];
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, li = lane & 15, lk = lane >> 4;
+  const int parts = (a.Dv + DVS - 1) / DVS;
+  const int c0 = (int)(blockIdx.x % parts) * DVS, h = (int)(blockIdx.x / parts % a.H),
+            seq = (int)(blockIdx.x / parts / a.H), hk = h / (a.H / a.Hk);
+  const int base = min(max(a.offs ? a.offs[seq] : seq, 0), a.rows),
+            len = a.offs ? min(max(a.offs[seq + 1], base), a.rows) - base : 1;
+  const int key = !a.offs || kC > a.rows ? seq : base / kC + seq;
+  const int slot = slot_of(a.slots, a.n_slots, seq);
+  const T* kp = k + (int64_t)hk * a.Dk;
+  const T* qp = q + (int64_t)hk * a.Dk;
+  const int t = 16 * w + li;  // the lane's token
+  // state entries [c0 + 16 m + 4 lk + r][NT 16 w + 16 n + li]
+  floatx4 st[MB][NT];
+  auto at = [&](int m, int n) { return (int64_t)(16 * (NT * w + n) + li) * a.Dv + c0 + 16 * m + 4 * lk; };
+  auto in = [&](int m, int n) { return 16 * (NT * w + n) + li < a.Dk && c0 + 16 * m + 4 * lk < a.Dv; };
+  const int64_t head = (int64_t)a.Dk * a.Dv;
+#pragma unroll
+  for (int m = 0; m < MB; ++m)
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      st[m][n] = floatx4{0.f, 0.f, 0.f, 0.f};
+      if (a.state && slot >= 0 && in(m, n))
+        st[m][n] = *reinterpret_cast<const floatx4*>(a.state + ((int64_t)slot * a.H + h) * head + at(m, n));
+    }
+  const int chunks = (len + kC - 1) / kC;
+  for (int ch = 0; ch < chunks; ++ch) {
+    const Chunk c = {base + ch * kC, min(kC, len - ch * kC)};
+    const int64_t th = (int64_t)(key + ch) * a.H + h;
+    const float* mat = mats + th * (SAVE ? 3 : 2) * kMat;
+    const float* co = coef + th * 3 * kC;
+#pragma unroll
+    for (int m = 0; m < MB; ++m)
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) sS[(16 * m + 4 * lk + r) * LDS + 16 * (NT * w + n) + li] = st[m][n][r];
+        if (SAVE && in(m, n)) *reinterpret_cast<floatx4*>(s0 + th * head + at(m, n)) = st[m][n];
+      }
+    floatx4 kf[NF], qf[NF];
+    row_frags<T, NF>(kp, a.ldk, c, w, a.Dk, kf);
+    if (!SAVE) row_frags<T, NF>(qp, a.ldq, c, w, a.Dk, qf);
+    floatx4 vv[MB];
+    const bool live = t < c.n;
+#pragma unroll
+    for (int m = 0; m < MB; ++m) {
+      vv[m] = floatx4{0.f, 0.f, 0.f, 0.f};
+      if (live && c0 + 16 * m + 4 * lk < a.Dv)
+        vv[m] = ld4(v + (c.row + t) * a.ldv + (int64_t)h * a.Dv + c0 + 16 * m + 4 * lk);
+    }
+    const float beta = co[t], e = co[kC + t], wj = co[2 * kC + t], eC = co[2 * kC - 1];
+#pragma unroll
+    for (int s = 0; s < NF; ++s) *reinterpret_cast<floatx4*>(sK + t * LDS + 16 * s + 4 * lk) = kf[s];
+    __syncthreads();
+    floatx4 ks[MB], qs[MB];
+#pragma unroll
+    for (int m = 0; m < MB; ++m) {
+      ks[m] = qs[m] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int s = 0; s < NF; ++s) {
+        const floatx4 sf = frag(sS + 16 * m * LDS, LDS, s);
+        ks[m] = mma16(sf, kf[s], ks[m]);
+        if (!SAVE) qs[m] = mma16(sf, qf[s], qs[m]);
+      }
+#pragma unroll
+      for (int r = 0; r < 4; ++r) sR[(16 * m + 4 * lk + r) * kLdM + t] = beta * fmaf(-e, ks[m][r], vv[m][r]);
+    }
+    __syncthreads();
+    floatx4 u[MB];
+#pragma unroll
+    for (int m = 0; m < MB; ++m) u[m] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      const floatx4 tf = mat_frag(mat, w, s);
+#pragma unroll
+      for (int m = 0; m < MB; ++m) u[m] = mma16(frag(sR + 16 * m * kLdM, kLdM, s), tf, u[m]);
+    }
+    if (SAVE && live)
+#pragma unroll
+      for (int m = 0; m < MB; ++m)
+        if (c0 + 16 * m + 4 * lk < a.Dv)
+          *reinterpret_cast<floatx4*>(us + ((int64_t)(c.row + t) * a.H + h) * a.Dv + c0 + 16 * m + 4 * lk) = u[m];
+#pragma unroll
+    for (int m = 0; m < MB; ++m)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) sU[(16 * m + 4 * lk + r) * kLdM + t] = u[m][r];
+    __syncthreads();
+    // w U where R was, by the wavefront that wrote R there: what others read of it is behind the barrier
+#pragma unroll
+    for (int m = 0; m < MB; ++m)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) sR[(16 * m + 4 * lk + r) * kLdM + t] = wj * u[m][r];
+    if (!SAVE) {
+      floatx4 out[MB];
+#pragma unroll
+      for (int m = 0; m < MB; ++m)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) out[m][r] = a.scale * e * qs[m][r];
+#pragma unroll
+      for (int s = 0; s < 4; ++s) {
+        if (s > w) break;  // (P is zero there)
+        const floatx4 pf = mat_frag(mat + kMat, w, s);
+#pragma unroll
+        for (int m = 0; m < MB; ++m) out[m] = mma16(frag(sU + 16 * m * kLdM, kLdM, s), pf, out[m]);
+      }
+      if (live)
+#pragma unroll
+        for (int m = 0; m < MB; ++m)
+          if (c0 + 16 * m + 4 * lk < a.Dv)
+            st4(o + (c.row + t) * ldo + (int64_t)h * a.Dv + c0 + 16 * m + 4 * lk, out[m]);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+#pragma unroll
+      for (int m = 0; m < MB; ++m) st[m][n] *= eC;
+#pragma unroll
+      for (int s = 0; s < 4; ++s) {
+        const floatx4 kt = frag_t(sK + 16 * (NT * w + n), LDS, s);
+#pragma unroll
+        for (int m = 0; m < MB; ++m) st[m][n] = mma16(frag(sR + 16 * m * kLdM, kLdM, s), kt, st[m][n]);
+      }
+    }
+    __syncthreads();
+  }
+  if (!SAVE && state_out && slot >= 0)
+#pragma unroll
+    for (int m = 0; m < MB; ++m)
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+        if (in(m, n))
+          *reinterpret_cast<floatx4*>(state_out + ((int64_t)slot * a.H + h) * head + at(m, n)) = st[m][n];
+}
+
+// ---------------------------------------------------------------- gradients
+// From dO and the adjoint dS1 of a chunk's end state:
+//   dU = P^T dO + w K dS1,  dR = T^T dU,  dV = beta dR,
+//   dS0 = e^G_C dS1 + scale Q^T (e^G dO) - K^T (beta e^G dR),
+// which walks the chunks backwards as the forward pass walks them, keeping dS1 and dR; then, with
+//   dA = -dR U^T (j < i),  dP = dO U^T (j <= i),  M1 = scale D dP,  M2 = beta D dA,
+//   dQ = scale e^G dO S0^T + M1 K,
+//   dK = -(beta e^G dR) S0^T + w U dS1^T + M1^T Q + (M2 + M2^T) K,
+//   dbeta_i = dR_i . V_i - e^G_i k_i . (dR S0^T)_i + sum_j dA_ij D_ij k_i.k_j,
+//   dg_t = sum_(i >= t > j) (dP_ij P_ij + dA_ij A_ij) + sum_(i >= t) (scale e^G q.(dO S0^T) - beta e^G k.(dR S0^T))_i
+//          + sum_(j < t) (w k.(U dS1^T))_j + e^G_C <S0, dS1>
+// all chunks at once. (dg_t is what passes over token t; as sums of such terms alone, without differences of
+// the chunk's totals, it keeps its digits where a token forgets nearly all.)
+template <typename T, int DKP, int DVS>
+__global__ __launch_bounds__(256) void delta_back_kernel(DeltaIn a, const T* __restrict__ q, const T* __restrict__ k,
+                                                         const T* __restrict__ d_o, int64_t lddo,
+                                                         const float* __restrict__ mats,
+                                                         const float* __restrict__ coef,
+                                                         const float* __restrict__ dstate_out, float* __restrict__ dstate,
+                                                         T* __restrict__ dv, int64_t lddv, float* __restrict__ ds1,
+                                                         float* __restrict__ drs) {
+  constexpr int NF = DKP / 16, NT = DKP / 64, MB = DVS / 16, LDS = DKP + 4;
+  __shared__ __attribute__((aligned(16))) float sS[DVS * LDS], sK[kC * LDS], sQ[kC * LDS], sO[DVS * kLdM],
+      sU[DVS * kLdM];
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, li = lane & 15, lk = lane >> 4;
+  const int parts = (a.Dv + DVS - 1) / DVS;
+  const int c0 = (int)(blockIdx.x % parts) * DVS, h = (int)(blockIdx.x / parts % a.H),
+            seq = (int)(blockIdx.x / parts / a.H), hk = h / (a.H / a.Hk);
+  const int base = min(max(a.offs ? a.offs[seq] : seq, 0), a.rows),
+            len = a.offs ? min(max(a.offs[seq + 1], base), a.rows) - base : 1;
+  const int key = !a.offs || kC > a.rows ? seq : base / kC + seq;
+  const T* kp = k + (int64_t)hk * a.Dk;
+  const T* qp = q + (int64_t)hk * a.Dk;
+  const int t = 16 * w + li;
+  floatx4 st[MB][NT];
+  auto at = [&](int m, int n) { return (int64_t)(16 * (NT * w + n) + li) * a.Dv + c0 + 16 * m + 4 * lk; };
+  auto in = [&](int m, int n) { return 16 * (NT * w + n) + li < a.Dk && c0 + 16 * m + 4 * lk < a.Dv; };
+  const int64_t head = (int64_t)a.Dk * a.Dv;
+#pragma unroll
+  for (int m = 0; m < MB; ++m)
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      st[m][n] = floatx4{0.f, 0.f, 0.f, 0.f};
+      if (dstate_out && in(m, n))
+        st[m][n] = *reinterpret_cast<const floatx4*>(dstate_out + ((int64_t)seq * a.H + h) * head + at(m, n));
+    }
+  for (int ch = (len + kC - 1) / kC - 1; ch >= 0; --ch) {
+    const Chunk c = {base + ch * kC, min(kC, len - ch * kC)};
+    const int64_t th = (int64_t)(key + ch) * a.H + h;
+    const float* mat = mats + th * 3 * kMat;
+    const float* co = coef + th * 3 * kC;
+#pragma unroll
+    for (int m = 0; m < MB; ++m)
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) sS[(16 * m + 4 * lk + r) * LDS + 16 * (NT * w + n) + li] = st[m][n][r];
+        if (in(m, n)) *reinterpret_cast<floatx4*>(ds1 + th * head + at(m, n)) = st[m][n];
+      }
+    floatx4 kf[NF], qf[NF], dov[MB];
+    row_frags<T, NF>(kp, a.ldk, c, w, a.Dk, kf);
+    row_frags<T, NF>(qp, a.ldq, c, w, a.Dk, qf);
+    const bool live = t < c.n;
+#pragma unroll
+    for (int m = 0; m < MB; ++m) {
+      dov[m] = floatx4{0.f, 0.f, 0.f, 0.f};
+      if (live && c0 + 16 * m + 4 * lk < a.Dv)
+        dov[m] = ld4(d_o + (c.row + t) * lddo + (int64_t)h * a.Dv + c0 + 16 * m + 4 * lk);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) sO[(16 * m + 4 * lk + r) * kLdM + t] = dov[m][r];
+    }
+    const float beta = co[t], e = co[kC + t], wj = co[2 * kC + t], eC = co[2 * kC - 1];
+#pragma unroll
+    for (int s = 0; s < NF; ++s) {
+      *reinterpret_cast<floatx4*>(sK + t * LDS + 16 * s + 4 * lk) = kf[s];
+      *reinterpret_cast<floatx4*>(sQ + t * LDS + 16 * s + 4 * lk) = qf[s];
+    }
+    __syncthreads();
+    floatx4 du[MB];
+#pragma unroll
+    for (int m = 0; m < MB; ++m) {
+      du[m] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int s = 0; s < NF; ++s) du[m] = mma16(frag(sS + 16 * m * LDS, LDS, s), kf[s], du[m]);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) du[m][r] *= wj;
+    }
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      const floatx4 pf = mat_frag(mat + 2 * kMat, w, s);
+#pragma unroll
+      for (int m = 0; m < MB; ++m) du[m] = mma16(frag(sO + 16 * m * kLdM, kLdM, s), pf, du[m]);
+    }
+#pragma unroll
+    for (int m = 0; m < MB; ++m)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) sU[(16 * m + 4 * lk + r) * kLdM + t] = du[m][r];
+    __syncthreads();
+    floatx4 dr[MB];
+#pragma unroll
+    for (int m = 0; m < MB; ++m) dr[m] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      const floatx4 tf = mat_frag(mat + kMat, w, s);
+#pragma unroll
+      for (int m = 0; m < MB; ++m) dr[m] = mma16(frag(sU + 16 * m * kLdM, kLdM, s), tf, dr[m]);
+    }
+    if (live)
+#pragma unroll
+      for (int m = 0; m < MB; ++m)
+        if (c0 + 16 * m + 4 * lk < a.Dv) {
+          *reinterpret_cast<floatx4*>(drs + ((int64_t)(c.row + t) * a.H + h) * a.Dv + c0 + 16 * m + 4 * lk) = dr[m];
+          st4(dv + (c.row + t) * lddv + (int64_t)h * a.Dv + c0 + 16 * m + 4 * lk, dr[m] * beta);
+        }
+    __syncthreads();  // sO and sU are read
+#pragma unroll
+    for (int m = 0; m < MB; ++m)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        sO[(16 * m + 4 * lk + r) * kLdM + t] = a.scale * e * dov[m][r];
+        sU[(16 * m + 4 * lk + r) * kLdM + t] = -beta * e * dr[m][r];
+      }
+    __syncthreads();
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+#pragma unroll
+      for (int m = 0; m < MB; ++m) st[m][n] *= eC;
+#pragma unroll
+      for (int s = 0; s < 4; ++s) {
+        const floatx4 kt = frag_t(sK + 16 * (NT * w + n), LDS, s), qt = frag_t(sQ + 16 * (NT * w + n), LDS, s);
+#pragma unroll
+        for (int m = 0; m < MB; ++m) {
+          st[m][n] = mma16(frag(sO + 16 * m * kLdM, kLdM, s), qt, st[m][n]);
+          st[m][n] = mma16(frag(sU + 16 * m * kLdM, kLdM, s), kt, st[m][n]);
+        }
+      }
+    }
+    __syncthreads();
+  }
+  if (dstate)
+#pragma unroll
+    for (int m = 0; m < MB; ++m)
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+        if (in(m, n)) *reinterpret_cast<floatx4*>(dstate + ((int64_t)seq * a.H + h) * head + at(m, n)) = st[m][n];
+}
+
+// Sum over the 16 lanes that share l / 16; every lane receives it.
+__device__ __forceinline__ float sum16(float v) {
+  v += dpp<0xB1>(v);
+  v += dpp<0x4E>(v);
+  v += dpp<0x141>(v);  // half mirror: the other four of eight
+  return v + dpp<0x140>(v);  // mirror: the other eight
+}
+
+// What the chunks give once their states and adjoints are known, a workgroup per chunk and key head, which
+// sums dQ and dK over the value heads that share it. Each wavefront has 16 tokens; U and slices of the states
+// go through LDS, 32 columns at a time.
+constexpr int kSl = 32, kLdSl = kSl + 4;
+
+template <typename T, int DKP>
+__global__ __launch_bounds__(256) void delta_grads_kernel(DeltaIn a, const T* __restrict__ q, const T* __restrict__ k,
+                                                          const T* __restrict__ v, const T* __restrict__ d_o,
+                                                          int64_t lddo, const float* __restrict__ coef,
+                                                          const float* __restrict__ s0, const float* __restrict__ ds1,
+                                                          const float* __restrict__ us, const float* __restrict__ drs,
+                                                          T* __restrict__ dq, int64_t lddq, T* __restrict__ dk,
+                                                          int64_t lddk, float* __restrict__ dg, int64_t lddg,
+                                                          float* __restrict__ dbeta, int64_t lddb) {
+  constexpr int NF = DKP / 16, LDS = DKP + 4;
+  constexpr int kSlices = 2 * DKP * kLdSl + kC * kLdSl;  // S0, dS1, U
+  constexpr int kPool = kSlices > 2 * kC * kLdM ? kSlices : 2 * kC * kLdM;  // then M1, M2 + M2^T
+  __shared__ __attribute__((aligned(16))) float sK[kC * LDS], sQ[kC * LDS], pool[kPool];
+  __shared__ double sG[kC];
+  __shared__ float sB[kC], sRow[kC], sCol[kC], sSeg[4][kC], sDot[4];
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, li = lane & 15, lk = lane >> 4;
+  const int tile = blockIdx.x / a.Hk, hk = blockIdx.x % a.Hk;
+  const Tile tl = find_tile(a.offs, a.n_seq, a.rows, kC, tile);
+  if (tl.seq < 0 || tl.len == 0) return;
+  const Chunk c = {tl.base + tl.j * kC, min(kC, tl.len - tl.j * kC)};
+  const int t = 16 * w + li;
+  const bool live = t < c.n;
+  const floatx4 zero = {0.f, 0.f, 0.f, 0.f};
+  floatx4 kk[4], qk[4];  // [16 w + 4 lk + r][16 j + li]
+  {
+    floatx4 kf[NF], qf[NF];
+    row_frags<T, NF>(k + (int64_t)hk * a.Dk, a.ldk, c, w, a.Dk, kf);
+    row_frags<T, NF>(q + (int64_t)hk * a.Dk, a.ldq, c, w, a.Dk, qf);
+#pragma unroll
+    for (int s = 0; s < NF; ++s) {
+      *reinterpret_cast<floatx4*>(sK + t * LDS + 16 * s + 4 * lk) = kf[s];
+      *reinterpret_cast<floatx4*>(sQ + t * LDS + 16 * s + 4 * lk) = qf[s];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      kk[j] = qk[j] = zero;
+      if (j > w) continue;
+#pragma unroll
+      for (int s = 0; s < NF; ++s) {
+        const floatx4 bf = frag(sK + 16 * j * LDS, LDS, s);
+        kk[j] = mma16(kf[s], bf, kk[j]);
+        qk[j] = mma16(qf[s], bf, qk[j]);
+      }
+    }
+  }
+  floatx4 dqa[NF], dka[NF];  // [16 n + 4 lk + r][16 w + li]
+#pragma unroll
+  for (int n = 0; n < NF; ++n) dqa[n] = dka[n] = zero;
+  const int share = a.H / a.Hk;
+  const int64_t head = (int64_t)a.Dk * a.Dv;
+  for (int hv = 0; hv < share; ++hv) {
+    const int h = hk * share + hv;
+    const int64_t th = (int64_t)tile * a.H + h;
+    const float* co = coef + th * 3 * kC;
+    __syncthreads();
+    if (tid < kC) {
+      double G = tid < c.n ? log_decay(a.g[(c.row + tid) * a.ldg + h]) : 0.0;
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const double up = __shfl_up(G, o, 64);
+        if (tid >= o) G += up;
+      }
+      sG[tid] = G;
+      sB[tid] = co[tid];
+    }
+    floatx4 dp[4], da[4], x1[NF], x2[NF], x3[NF];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) dp[j] = da[j] = zero;
+#pragma unroll
+    for (int n = 0; n < NF; ++n) x1[n] = x2[n] = x3[n] = zero;
+    float rv = 0.f, dot = 0.f;
+    for (int c0 = 0; c0 < a.Dv; c0 += kSl) {
+      float* sS0 = pool;
+      float* sD1 = pool + DKP * kLdSl;
+      float* sUs = pool + 2 * DKP * kLdSl;
+      __syncthreads();
+      for (int i = tid; i < DKP * (kSl / 4); i += 256) {
+        const int r = i / (kSl / 4), cc = 4 * (i % (kSl / 4));
+        floatx4 x = zero, y = zero;
+        if (r < a.Dk && c0 + cc < a.Dv) {
+          x = *reinterpret_cast<const floatx4*>(s0 + th * head + (int64_t)r * a.Dv + c0 + cc);
+          y = *reinterpret_cast<const floatx4*>(ds1 + th * head + (int64_t)r * a.Dv + c0 + cc);
+        }
+        *reinterpret_cast<floatx4*>(sS0 + r * kLdSl + cc) = x;
+        *reinterpret_cast<floatx4*>(sD1 + r * kLdSl + cc) = y;
+#pragma unroll
+        for (int m = 0; m < 4; ++m) dot = fmaf(x[m], y[m], dot);
+      }
+      floatx4 of[2], uf[2], rf[2];
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        const int cc = c0 + 16 * s + 4 * lk;
+        of[s] = uf[s] = rf[s] = zero;
+        if (live && cc < a.Dv) {
+          const int64_t row = c.row + t;
+          of[s] = ld4(d_o + row * lddo + (int64_t)h * a.Dv + cc);
+          uf[s] = *reinterpret_cast<const floatx4*>(us + (row * a.H + h) * a.Dv + cc);
+          rf[s] = *reinterpret_cast<const floatx4*>(drs + (row * a.H + h) * a.Dv + cc);
+          const floatx4 vv = ld4(v + row * a.ldv + (int64_t)h * a.Dv + cc);
+#pragma unroll
+          for (int m = 0; m < 4; ++m) rv = fmaf(rf[s][m], vv[m], rv);
+        }
+        *reinterpret_cast<floatx4*>(sUs + t * kLdSl + 16 * s + 4 * lk) = uf[s];
+      }
+      __syncthreads();
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          if (j > w) continue;
+          const floatx4 uj = frag(sUs + 16 * j * kLdSl, kLdSl, s);
+          dp[j] = mma16(of[s], uj, dp[j]);
+          da[j] = mma16(rf[s], uj, da[j]);
+        }
+#pragma unroll
+        for (int n = 0; n < NF; ++n) {
+          const floatx4 x = frag(sS0 + 16 * n * kLdSl, kLdSl, s), y = frag(sD1 + 16 * n * kLdSl, kLdSl, s);
+          x1[n] = mma16(x, of[s], x1[n]);
+          x2[n] = mma16(x, rf[s], x2[n]);
+          x3[n] = mma16(y, uf[s], x3[n]);
+        }
+      }
+    }
+    const float beta = co[t], e = co[kC + t], wj = co[2 * kC + t], eC = co[2 * kC - 1];
+    // q.(dO S0^T), k.(dR S0^T), k.(U dS1^T) of the lane's token, and dQ, dK's terms
+    float q1 = 0.f, k2 = 0.f, k3 = 0.f;
+#pragma unroll
+    for (int n = 0; n < NF; ++n) {
+      const floatx4 qv = *reinterpret_cast<const floatx4*>(sQ + t * LDS + 16 * n + 4 * lk),
+                    kv = *reinterpret_cast<const floatx4*>(sK + t * LDS + 16 * n + 4 * lk);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        q1 = fmaf(qv[r], x1[n][r], q1);
+        k2 = fmaf(kv[r], x2[n][r], k2);
+        k3 = fmaf(kv[r], x3[n][r], k3);
+        dqa[n][r] = fmaf(a.scale * e, x1[n][r], dqa[n][r]);
+        dka[n][r] = fmaf(wj, x3[n][r], fmaf(-beta * e, x2[n][r], dka[n][r]));
+      }
+    }
+    auto sum4 = [](float x) {
+      x += __shfl_xor(x, 16, 64);
+      return x + __shfl_xor(x, 32, 64);
+    };
+    q1 = sum4(q1); k2 = sum4(k2); k3 = sum4(k3); rv = sum4(rv);
+    dot = wave_sum(dot);
+    if (lk == 0) {
+      sRow[t] = a.scale * e * q1 - beta * e * k2;
+      sCol[t] = wj * k3;
+    }
+    if (lane == 0) sDot[w] = dot;
+    float db = rv - e * k2;  // of the lane's token; the products with kk follow by rows
+    __syncthreads();         // the slices are read, sG is written
+    float* m1 = pool;
+    float* m2 = pool + kC * kLdM;
+    floatx4 mm[4];   // dP P + dA A
+    floatx4 rowsum = zero;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int row = 16 * w + 4 * lk + r, col = 16 * j + li;
+        const float d = col <= row ? exp_of(sG[row] - sG[col]) : 0.f;
+        const float ga = col < row ? -da[j][r] * d : 0.f, gp = a.scale * d * dp[j][r];
+        m1[row * kLdM + col] = col <= row ? gp : 0.f;
+        const float y = sB[row] * ga;
+        if (col < row) {
+          m2[row * kLdM + col] = y;
+          m2[col * kLdM + row] = y;
+        } else if (col == row) {
+          m2[row * kLdM + col] = 0.f;
+        }
+        mm[j][r] = col < row ? fmaf(gp, qk[j][r], y * kk[j][r]) : 0.f;
+        rowsum[r] = fmaf(ga, kk[j][r], rowsum[r]);
+      }
+    __syncthreads();
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      const floatx4 b1 = frag(m1 + 16 * w * kLdM, kLdM, s), b2 = frag_t(m1 + 16 * w, kLdM, s),
+                    b3 = frag(m2 + 16 * w * kLdM, kLdM, s);
+#pragma unroll
+      for (int n = 0; n < NF; ++n) {
+        const floatx4 kt = frag_t(sK + 16 * n, LDS, s), qt = frag_t(sQ + 16 * n, LDS, s);
+        if (s <= w) dqa[n] = mma16(kt, b1, dqa[n]);
+        if (s >= w) dka[n] = mma16(qt, b2, dka[n]);
+        dka[n] = mma16(kt, b3, dka[n]);
+      }
+    }
+    // sums of rows of dA D kk to their tokens' lanes
+#pragma unroll
+    for (int r = 0; r < 4; ++r) rowsum[r] = sum16(rowsum[r]);
+    __syncthreads();  // m1, m2 are read
+    if (li == 0)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) sSeg[0][16 * w + 4 * lk + r] = rowsum[r];
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) m1[(16 * w + 4 * lk + r) * kLdM + 16 * j + li] = mm[j][r];
+    __syncthreads();
+    if (lk == 0 && live) dbeta[(c.row + t) * lddb + h] = db + sSeg[0][t];
+    __syncthreads();
+    // column `lane`, rows 16 w .. + 15: sums from each row to the last
+    float z[16], z_all = 0.f;
+#pragma unroll
+    for (int i = 15; i >= 0; --i) {
+      z_all += m1[(16 * w + i) * kLdM + lane];
+      z[i] = z_all;
+    }
+    sSeg[w][lane] = z_all;
+    __syncthreads();
+    float below = 0.f;
+    for (int x = w + 1; x < 4; ++x) below += sSeg[x][lane];
+    const float rt = sRow[lane], ct = sCol[lane], all = eC * (sDot[0] + sDot[1] + sDot[2] + sDot[3]);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int row = 16 * w + i;
+      // lane j: what it adds to token `row`'s sum
+      const float x = (lane >= row ? rt : ct + z[i] + below);
+      const float sum = wave_sum(x);
+      if (lane == 0 && row < c.n) dg[(c.row + row) * lddg + h] = sum + all;
+    }
+  }
+  if (live)
+#pragma unroll
+    for (int n = 0; n < NF; ++n)
+      if (16 * n + 4 * lk < a.Dk) {
+        st4(dq + (c.row + t) * lddq + (int64_t)hk * a.Dk + 16 * n + 4 * lk, dqa[n]);
+        st4(dk + (c.row + t) * lddk + (int64_t)hk * a.Dk + 16 * n + 4 * lk, dka[n]);
+      }
+}
+
+// ---------------------------------------------------------------- launches
+
+// Chunks of kC tokens pay from 32 tokens a sequence on average.
+bool chunked(int n_seq, int rows) { return rows / 32 >= n_seq; }
+int64_t tiles_of(int n_seq, int rows) { return (int64_t)rows / kC + n_seq; }
+
+DeltaIn in_of(const DeltaOp& a) {
+  return {a.offs, a.n_seq, a.rows, a.Hk, a.H, a.Dk, a.Dv, a.ldq, a.ldk, a.ldv, a.ldg, a.ldb, a.g, a.beta, a.scale,
+          a.state, a.slots, a.n_slots};
+}
+
+template <typename T>
+hipError_t walk(const DeltaOp& a, float* state_out, void* o, int64_t ldo, hipStream_t s) {
+  const dim3 grid((unsigned)((int64_t)a.n_seq * a.H * ((a.Dv + 31) / 32)));
+  const T *q = static_cast<const T*>(a.q), *k = static_cast<const T*>(a.k), *v = static_cast<const T*>(a.v);
+  if (a.Dk <= 64) delta_walk_kernel<T, 8><<<grid, 64, 0, s>>>(in_of(a), q, k, v, state_out, static_cast<T*>(o), ldo);
+  else delta_walk_kernel<T, 16><<<grid, 64, 0, s>>>(in_of(a), q, k, v, state_out, static_cast<T*>(o), ldo);
+  return hipGetLastError();
+}
+
+template <typename T, int DKP>
+hipError_t chunks(const DeltaOp& a, float* state_out, void* o, int64_t ldo, float* ws, hipStream_t s) {
+  const int64_t tiles = tiles_of(a.n_seq, a.rows);
+  float* coef = ws;
+  float* mats = ws + tiles * a.H * 3 * kC;
+  const T *q = static_cast<const T*>(a.q), *k = static_cast<const T*>(a.k), *v = static_cast<const T*>(a.v);
+  delta_prep_kernel<T, DKP, false><<<dim3((unsigned)(tiles * a.Hk)), 256, 0, s>>>(in_of(a), q, k, mats, coef);
+  delta_chunk_kernel<T, DKP, 16, false><<<dim3((unsigned)((int64_t)a.n_seq * a.H * ((a.Dv + 15) / 16))), 256, 0, s>>>(
+      in_of(a), q, k, v, mats, coef, state_out, static_cast<T*>(o), ldo, nullptr, nullptr);
+  return hipGetLastError();
+}
+
+// The parts of the gradients' workspace, in floats.
+struct BackSpace {
+  int64_t coef, mats, s0, ds1, us, drs, end;
+  BackSpace(int n_seq, int rows, int H, int Dk, int Dv) {
+    const int64_t th = tiles_of(n_seq, rows) * H, head = (int64_t)Dk * Dv, act = (int64_t)rows * H * Dv;
+    coef = 0;
+    mats = coef + th * 3 * kC;
+    s0 = mats + th * 3 * kMat;
+    ds1 = s0 + th * head;
+    us = ds1 + th * head;
+    drs = us + act;
+    end = drs + act;
+  }
+};
+
+template <typename T, int DKP>
+hipError_t grads(const DeltaOp& a, const void* d_o_, int64_t lddo, const float* dstate_out, const DeltaGrads& g,
+                 float* ws, hipStream_t s) {
+  const int64_t tiles = tiles_of(a.n_seq, a.rows);
+  const BackSpace b(a.n_seq, a.rows, a.H, a.Dk, a.Dv);
+  const T *q = static_cast<const T*>(a.q), *k = static_cast<const T*>(a.k), *v = static_cast<const T*>(a.v);
+  const T* d_o = static_cast<const T*>(d_o_);
+  const DeltaIn in = in_of(a);
+  const dim3 flat((unsigned)(tiles * a.Hk)), slices((unsigned)((int64_t)a.n_seq * a.H * ((a.Dv + 15) / 16)));
+  delta_prep_kernel<T, DKP, true><<<flat, 256, 0, s>>>(in, q, k, ws + b.mats, ws + b.coef);
+  delta_chunk_kernel<T, DKP, 16, true><<<slices, 256, 0, s>>>(in, q, k, v, ws + b.mats, ws + b.coef, nullptr, nullptr,
+                                                              0, ws + b.s0, ws + b.us);
+  delta_back_kernel<T, DKP, 16><<<slices, 256, 0, s>>>(in, q, k, d_o, lddo, ws + b.mats, ws + b.coef, dstate_out,
+                                                       g.dstate, static_cast<T*>(g.dv), g.lddv, ws + b.ds1, ws + b.drs);
+  delta_grads_kernel<T, DKP><<<flat, 256, 0, s>>>(in, q, k, v, d_o, lddo, ws + b.coef, ws + b.s0, ws + b.ds1, ws + b.us,
+                                                  ws + b.drs, static_cast<T*>(g.dq), g.lddq, static_cast<T*>(g.dk),
+                                                  g.lddk, g.dg, g.lddg, g.dbeta, g.lddb);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+size_t delta_rule_workspace_bytes(bool bf16, int n_seq, int rows, int Hk, int H, int Dk, int Dv) {
+  (void)bf16; (void)Hk; (void)Dk; (void)Dv;
+  if (!chunked(n_seq, rows)) return 0;
+  return (size_t)(tiles_of(n_seq, rows) * H * (3 * kC + 2 * kMat)) * sizeof(float);
+}
+
+hipError_t launch_delta_rule(const DeltaOp& a, float* state_out, void* o, int64_t ldo, float* ws, hipStream_t s) {
+  if (!a.offs || !chunked(a.n_seq, a.rows))
+    return a.bf16 ? walk<uint16_t>(a, state_out, o, ldo, s) : walk<float>(a, state_out, o, ldo, s);
+  if (a.Dk <= 64)
+    return a.bf16 ? chunks<uint16_t, 64>(a, state_out, o, ldo, ws, s) : chunks<float, 64>(a, state_out, o, ldo, ws, s);
+  return a.bf16 ? chunks<uint16_t, 128>(a, state_out, o, ldo, ws, s) : chunks<float, 128>(a, state_out, o, ldo, ws, s);
+}
+
+size_t delta_rule_bwd_workspace_bytes(bool bf16, int n_seq, int rows, int Hk, int H, int Dk, int Dv) {
+  (void)bf16; (void)Hk;
+  return (size_t)BackSpace(n_seq, rows, H, Dk, Dv).end * sizeof(float);
+}
+
+hipError_t launch_delta_rule_bwd(const DeltaOp& a, const void* d_o, int64_t lddo, const float* dstate_out,
+                                 const DeltaGrads& g, float* ws, hipStream_t s) {
+  if (a.Dk <= 64)
+    return a.bf16 ? grads<uint16_t, 64>(a, d_o, lddo, dstate_out, g, ws, s) : grads<float, 64>(a, d_o, lddo, dstate_out, g, ws, s);
+  return a.bf16 ? grads<uint16_t, 128>(a, d_o, lddo, dstate_out, g, ws, s) : grads<float, 128>(a, d_o, lddo, dstate_out, g, ws, s);
+}
+
+}  // namespace tcl

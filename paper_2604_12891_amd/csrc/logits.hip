@@ -264,6 +264,12 @@ struct LogprobOut {
   int* top;
   float* top_logp;
 };
+// Rows that are a search's beams: whether beam r goes on (neither dead nor ended).
+struct Beams {
+  const float* score;
+  const int* ended;  // or null
+  __device__ __forceinline__ bool open(int r) const { return score[r] > -INFINITY && !(ended && ended[r] >= 0); }
+};
 
 template <typename T, int TB>
 __device__ __forceinline__ void finish_row(const LogitRows& a, const Row<T>& row, int r, Stats st,
@@ -293,9 +299,12 @@ __device__ __forceinline__ int64_t split_stride(int K) { return (int64_t)K * 8 +
 // the sums rescaled when it rises, once per vector at most. Bound by HBM from a
 // few thousand entries on: 4,096 rows of 32,768 bf16 entries in 66 us with 20 top entries, 53 without
 // (58 at the rate of a copy, which also writes). A workgroup that went on to a next row whose first vectors were
-// loaded ahead took 89. gridDim.y == 1: the row's results leave from here.
-template <typename T, int TB>
-__global__ __launch_bounds__(TB) void logprobs_kernel(LogitRows a, int K, LogprobOut o, char* __restrict__ ws) {
+// loaded ahead took 89. gridDim.y == 1: the row's results leave from here. BEAM: they go to the workspace, as
+// those of splits do, and rows of beams that do not go on are not read.
+template <typename T, int TB, bool BEAM = false>
+__global__ __launch_bounds__(TB) void logprobs_kernel(LogitRows a, int K, LogprobOut o, char* __restrict__ ws,
+                                                      Beams beams = {}) {
+  if (BEAM && !beams.open(blockIdx.x)) return;
   constexpr int VE = Row<T>::VE;
   __shared__ __attribute__((aligned(16))) TopShared<TB> sh;
   __shared__ Stats part[TB / 64];
@@ -398,7 +407,7 @@ __global__ __launch_bounds__(TB) void logprobs_kernel(LogitRows a, int K, Logpro
       }
     });
   }
-  if (gridDim.y == 1) {
+  if (!BEAM && gridDim.y == 1) {
     finish_row(a, row, r, st, sh, K, o);
     return;
   }
@@ -440,6 +449,102 @@ __global__ __launch_bounds__(kTB) void logprobs_join_kernel(LogitRows a, int K, 
     top_collect(sh, K, 8 * sizeof(T), b, each);
   }
   finish_row(a, row, r, st, sh, K, o);
+}
+
+// ---------------------------------------------------------------- beam search: selection
+// A group's K best candidates (b, v) by score_b + log p_b(v), out of its rows' lists of K: each list is
+// sorted, so every round takes the best of the lists' heads. Scores are compared in 64 bits: fp32 would make
+// neighbours equal that a long search's sum of log probabilities (-100: steps of 8e-6) cannot tell
+// apart. Equal scores: the lower row, then the lower token, which is the lower list, as splits are in their
+// rows' order. A wavefront runs the rounds, some 100 ns each, out of LDS where the lists fit.
+constexpr int kBeamLists = 1024;  // W x splits
+constexpr int kBeamKeys = 4096;   // keys held in LDS
+
+template <typename T>
+__global__ __launch_bounds__(kTB) void beam_join_kernel(LogitRows a, int W, int K, int splits, Beams beams,
+                                                        int* __restrict__ parent, int* __restrict__ token,
+                                                        float* __restrict__ out_score, const char* __restrict__ ws) {
+  __shared__ u64 keys[kBeamKeys];
+  __shared__ double head[kBeamLists];   // a list's best score that is left
+  __shared__ uint16_t at[kBeamLists];   // and its place
+  __shared__ double base[64], top[64];  // score - log of the sum; the maximum
+  const int g = blockIdx.x, tid = threadIdx.x, lane = tid & 63, lists = W * splits;
+  const float zc = a.inv_temp * kLog2e;
+  const double it = a.inv_temp;
+  const char* w = ws + (int64_t)g * lists * split_stride(K);
+  const bool held = lists * K <= kBeamKeys;
+  for (int b = tid >> 6; b < W; b += kTB / 64) {
+    const int r = g * W + b;
+    if (!beams.open(r)) continue;  // (uniform over the wavefront)
+    Stats st = {-INFINITY, 0.f, 0.f};
+    for (int k = lane; k < splits; k += 64)
+      st = merge(st, *reinterpret_cast<const Stats*>(w + (int64_t)(b * splits + k) * split_stride(K) + (int64_t)K * 8), zc);
+    st = wave_merge(st, zc);
+    if (lane == 0) {
+      base[b] = (double)beams.score[r] - log((double)st.s);
+      top[b] = st.m;
+    }
+  }
+  if (held)
+    for (int q = tid; q < lists * K; q += kTB)
+      if (beams.open(g * W + q / (K * splits)))
+        keys[q] = reinterpret_cast<const u64*>(w + (int64_t)(q / K) * split_stride(K))[q % K];
+  __syncthreads();
+  auto key_of = [&](int l, int i) {
+    return held ? keys[l * K + i] : reinterpret_cast<const u64*>(w + (int64_t)l * split_stride(K))[i];
+  };
+  // (NaN, of a row with a logit of +inf, is no score)
+  auto score_of = [&](int l, int i) {
+    const int b = l / splits, r = g * W + b;
+    if (!beams.open(r)) {  // an ended beam is its own one candidate
+      const bool one = i == 0 && l % splits == 0 && beams.score[r] > -INFINITY;
+      return one ? (double)beams.score[r] : -(double)INFINITY;
+    }
+    const u64 k = i < K ? key_of(l, i) : 0;
+    if (!k) return -(double)INFINITY;
+    const double s = base[b] + ((double)ord_value<T>((uint32_t)(k >> 32)) - top[b]) * it;
+    return s > -(double)INFINITY ? s : -(double)INFINITY;
+  };
+  for (int l = tid; l < lists; l += kTB) {
+    head[l] = score_of(l, 0);
+    at[l] = 0;
+  }
+  __syncthreads();
+  if (tid >= 64) return;
+  const int bits = index_bits(a.V);
+  for (int i = 0; i < K; ++i) {
+    double best = -(double)INFINITY;
+    int from = lists;
+    for (int l = lane; l < lists; l += 64)
+      if (head[l] > best) {
+        best = head[l];
+        from = l;
+      }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+      const double s = __shfl_xor(best, o, 64);
+      const int f = __shfl_xor(from, o, 64);
+      if (s > best || (s == best && f < from)) {
+        best = s;
+        from = f;
+      }
+    }
+    const bool some = from < lists;  // the same in every lane
+    if (lane == (some ? from & 63 : 0)) {
+      const int64_t j = (int64_t)g * K + i;
+      int r = -1, v = -1;
+      if (some) {
+        r = g * W + from / splits;
+        const int p = at[from];
+        v = beams.open(r) ? (int)((1u << bits) - (uint32_t)key_of(from, p)) : beams.ended[r];
+        head[from] = score_of(from, p + 1);
+        at[from] = (uint16_t)(p + 1);
+      }
+      parent[j] = r;
+      token[j] = v;
+      out_score[j] = (float)best;
+    }
+  }
 }
 
 // ---------------------------------------------------------------- distillation from top logits
@@ -811,6 +916,22 @@ hipError_t logprobs(const LogitRows& a, int K, const LogprobOut& o, char* ws, hi
   return hipGetLastError();
 }
 
+// The rows' lists as logprobs() has them, then one workgroup per group.
+int beam_splits(int n, int W, int V) { return std::min(V / 4 + 1 <= 16 * kTB ? 1 : row_splits(n, V), kBeamLists / W); }
+
+template <typename T>
+hipError_t beam_select(const LogitRows& a, int W, int K, const Beams& beams, int* parent, int* token, float* out_score,
+                       char* ws, hipStream_t s) {
+  const int S = beam_splits(a.n, W, a.V);
+  const LogprobOut o = {};
+  if (S == 1 && a.n >= 256 && a.V <= 8192 && K <= 32)
+    logprobs_kernel<T, 64, true><<<dim3(a.n), 64, 0, s>>>(a, K, o, ws, beams);
+  else
+    logprobs_kernel<T, kTB, true><<<dim3(a.n, S), kTB, 0, s>>>(a, K, o, ws, beams);
+  beam_join_kernel<T><<<dim3(a.n / W), kTB, 0, s>>>(a, W, K, S, beams, parent, token, out_score, ws);
+  return hipGetLastError();
+}
+
 template <typename T>
 hipError_t distill(const LogitRows& a, const TeacherArgs& t, char* ws, hipStream_t s) {
   const int S = distill_splits(a.n, a.V);
@@ -850,6 +971,18 @@ hipError_t launch_distill_topk(const LogitRows& a, int K, const int* top, const 
                                float* loss, void* grad, int64_t ldg, void* ws, hipStream_t s) {
   const TeacherArgs t = {K, top, teacher, weight, loss, grad, ldg};
   return a.bf16 ? distill<uint16_t>(a, t, static_cast<char*>(ws), s) : distill<float>(a, t, static_cast<char*>(ws), s);
+}
+
+size_t beam_select_workspace_bytes(int groups, int W, int V, int K) {
+  const int n = groups * W;
+  return (size_t)n * beam_splits(n, W, V) * (K * 8 + 16);
+}
+
+hipError_t launch_beam_select(const LogitRows& a, int W, int K, const float* score, const int* ended, int* parent,
+                              int* token, float* out_score, void* ws, hipStream_t s) {
+  const Beams b = {score, ended};
+  return a.bf16 ? beam_select<uint16_t>(a, W, K, b, parent, token, out_score, static_cast<char*>(ws), s)
+                : beam_select<float>(a, W, K, b, parent, token, out_score, static_cast<char*>(ws), s);
 }
 
 }  // namespace tcl

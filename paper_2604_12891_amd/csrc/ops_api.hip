@@ -1,5 +1,5 @@
 // C entry points of the sequence and logit operators (include/tcl.h): argument
-// checks, then the launchers of ssm.hip and logits.hip.
+// checks, then the launchers of ssm.hip, delta.hip, norm.hip, logits.hip and beam.hip.
 #include <cmath>
 
 #include "model.h"
@@ -240,5 +240,237 @@ TCL_API tcl_status tcl_distill_topk(int32_t dtype, int32_t n_rows, int32_t V, co
   if (tcl_status st = check_workspace(d_workspace, ws_bytes, logits_workspace_bytes(n_rows, V, K))) return st;
   TCL_HIP(launch_distill_topk(a, K, d_top, d_teacher, d_weight, d_loss, d_grad, ldg, d_workspace,
                               static_cast<hipStream_t>(stream)));
+  return TCL_OK;
+}
+
+// ------------------------------------------------------------------ layer norm
+
+namespace {
+
+tcl_status norm_op(int32_t dtype, int32_t rows, int32_t C, const void* d_x, int64_t ldx, const float* d_w,
+                   const float* d_b, float eps, NormOp* op) {
+  if (dtype != TCL_F32 && dtype != TCL_BF16) return fail(TCL_ERR_INVALID_ARG, "bad dtype %d", dtype);
+  if (rows < 0 || C < 1) return fail(TCL_ERR_INVALID_ARG, "need rows >= 0, C > 0 (got %d, %d)", rows, C);
+  if (C > kMaxNormC) return fail(TCL_ERR_UNSUPPORTED, "C must be at most %d (got %d)", kMaxNormC, C);
+  if (rows > kMaxRows) return fail(TCL_ERR_UNSUPPORTED, "rows must be at most 2^30 (got %d)", rows);
+  if (ldx < C) return fail(TCL_ERR_INVALID_ARG, "leading dimension smaller than C");
+  if (!(eps >= 0.f && eps < INFINITY)) return fail(TCL_ERR_INVALID_ARG, "eps must be finite and not negative");
+  if (!d_x && rows > 0) return fail(TCL_ERR_INVALID_ARG, "NULL device pointer");
+  if (misaligned(d_x, dtype == TCL_BF16 ? 2 : 4)) return fail(TCL_ERR_INVALID_ARG, "x is not aligned to its type");
+  op->bf16 = dtype == TCL_BF16;
+  op->rows = rows; op->C = C; op->x = d_x; op->ldx = ldx; op->w = d_w; op->b = d_b; op->eps = eps;
+  return TCL_OK;
+}
+
+}  // namespace
+
+TCL_API tcl_status tcl_layer_norm(int32_t dtype, int32_t rows, int32_t C, const void* d_x, int64_t ldx,
+                                  const float* d_w, const float* d_b, float eps, void* d_y, int64_t ldy,
+                                  void* stream) {
+  NormOp op;
+  if (tcl_status st = norm_op(dtype, rows, C, d_x, ldx, d_w, d_b, eps, &op)) return st;
+  if (ldy < C) return fail(TCL_ERR_INVALID_ARG, "leading dimension smaller than C");
+  if (rows == 0) return TCL_OK;
+  if (!d_y) return fail(TCL_ERR_INVALID_ARG, "NULL device pointer");
+  if (misaligned(d_y, op.bf16 ? 2 : 4)) return fail(TCL_ERR_INVALID_ARG, "y is not aligned to its type");
+  TCL_HIP(launch_layer_norm(op, d_y, ldy, static_cast<hipStream_t>(stream)));
+  return TCL_OK;
+}
+
+TCL_API size_t tcl_layer_norm_workspace_bytes(int32_t dtype, int32_t rows, int32_t C) {
+  if ((dtype != TCL_F32 && dtype != TCL_BF16) || rows <= 0 || rows > kMaxRows || C < 1 || C > kMaxNormC) return 0;
+  return layer_norm_workspace_bytes(dtype == TCL_BF16, rows, C);
+}
+
+TCL_API tcl_status tcl_layer_norm_backward(int32_t dtype, int32_t rows, int32_t C, const void* d_x, int64_t ldx,
+                                           const float* d_w, float eps, const void* d_dy, int64_t lddy, void* d_dx,
+                                           int64_t lddx, float* d_dw, float* d_db, void* d_workspace,
+                                           size_t ws_bytes, void* stream) {
+  NormOp op;
+  if (tcl_status st = norm_op(dtype, rows, C, d_x, ldx, d_w, nullptr, eps, &op)) return st;
+  if (lddy < C || lddx < C) return fail(TCL_ERR_INVALID_ARG, "leading dimension smaller than C");
+  if (!d_dw || (rows > 0 && (!d_dy || !d_dx))) return fail(TCL_ERR_INVALID_ARG, "NULL device pointer");
+  if (misaligned(d_dy, op.bf16 ? 2 : 4) || misaligned(d_dx, op.bf16 ? 2 : 4))
+    return fail(TCL_ERR_INVALID_ARG, "dy and dx have to be aligned to their type");
+  const size_t need = rows > 0 ? layer_norm_workspace_bytes(op.bf16, rows, C) : 0;
+  if (tcl_status st = check_workspace(d_workspace, ws_bytes, need)) return st;
+  TCL_HIP(launch_layer_norm_bwd(op, d_dy, lddy, d_dx, lddx, d_dw, d_db, static_cast<float*>(d_workspace),
+                                static_cast<hipStream_t>(stream)));
+  return TCL_OK;
+}
+
+// ------------------------------------------------------------------ gated delta rule
+
+namespace {
+
+// Fewer than 2^32 threads a launch: a sequence's head takes 16 workgroups of 256 at most, a chunk's (64 rows, or the rest
+// of a sequence) one.
+constexpr int kMaxHeads = 1024, kMaxDk = 128, kMaxDv = 256;
+
+bool delta_sizes(int32_t n_seq, int32_t rows, int32_t Hk, int32_t H, int32_t Dk, int32_t Dv) {
+  return n_seq >= 0 && rows >= 0 && n_seq <= kMaxRows && rows <= kMaxRows && Hk >= 1 && H >= Hk && H <= kMaxHeads &&
+         H % Hk == 0 && Dk >= 8 && Dk <= kMaxDk && Dk % 8 == 0 && Dv >= 8 && Dv <= kMaxDv && Dv % 8 == 0 &&
+         (int64_t)rows * H <= ((int64_t)1 << 28) && (int64_t)n_seq * H < ((int64_t)1 << 20);
+}
+
+tcl_status delta_op(const tcl_delta_rule_args* a, DeltaOp* op) {
+  if (!a) return fail(TCL_ERR_INVALID_ARG, "args is NULL");
+  if (a->dtype != TCL_F32 && a->dtype != TCL_BF16) return fail(TCL_ERR_INVALID_ARG, "bad dtype %d", a->dtype);
+  if (a->n_seq < 0 || a->rows < 0)
+    return fail(TCL_ERR_INVALID_ARG, "negative size (n_seq=%d rows=%d)", a->n_seq, a->rows);
+  if (!a->d_offs && a->rows != a->n_seq)
+    return fail(TCL_ERR_INVALID_ARG, "without d_offs every sequence is one row (n_seq=%d rows=%d)", a->n_seq, a->rows);
+  if (a->Hk < 1 || a->H < a->Hk || a->H > kMaxHeads || a->H % a->Hk)
+    return fail(TCL_ERR_UNSUPPORTED, "H must be a multiple of Hk, at most %d (got %d, %d)", kMaxHeads, a->H, a->Hk);
+  if (a->Dk < 8 || a->Dk > kMaxDk || a->Dk % 8 || a->Dv < 8 || a->Dv > kMaxDv || a->Dv % 8)
+    return fail(TCL_ERR_UNSUPPORTED, "Dk and Dv must be multiples of 8, at most %d and %d (got %d, %d)", kMaxDk, kMaxDv,
+                a->Dk, a->Dv);
+  if (!delta_sizes(a->n_seq, a->rows, a->Hk, a->H, a->Dk, a->Dv))
+    return fail(TCL_ERR_UNSUPPORTED, "too many rows or sequences x heads (n_seq=%d rows=%d H=%d)", a->n_seq, a->rows,
+                a->H);
+  const int64_t qk = (int64_t)a->Hk * a->Dk, v = (int64_t)a->H * a->Dv;
+  if (a->ldq < qk || a->ldk < qk || a->ldv < v || a->ldg < a->H || a->ldbeta < a->H)
+    return fail(TCL_ERR_INVALID_ARG, "leading dimension smaller than the row");
+  if (a->rows > 0 && (!a->d_q || !a->d_k || !a->d_v || !a->d_g || !a->d_beta))
+    return fail(TCL_ERR_INVALID_ARG, "NULL device pointer");
+  const uintptr_t el = a->dtype == TCL_BF16 ? 2 : 4;
+  if (misaligned(a->d_q, el) || misaligned(a->d_k, el) || misaligned(a->d_v, el))
+    return fail(TCL_ERR_INVALID_ARG, "activations are not aligned to their type");
+  if (misaligned(a->d_state, 16)) return fail(TCL_ERR_INVALID_ARG, "the states must be 16-byte aligned");
+  op->bf16 = a->dtype == TCL_BF16;
+  op->n_seq = a->n_seq; op->rows = a->rows; op->Hk = a->Hk; op->H = a->H; op->Dk = a->Dk; op->Dv = a->Dv;
+  op->offs = a->d_offs;
+  op->q = a->d_q; op->k = a->d_k; op->v = a->d_v; op->ldq = a->ldq; op->ldk = a->ldk; op->ldv = a->ldv;
+  op->g = a->d_g; op->beta = a->d_beta; op->ldg = a->ldg; op->ldb = a->ldbeta;
+  op->scale = a->scale; op->state = a->d_state;
+  return TCL_OK;
+}
+
+}  // namespace
+
+TCL_API size_t tcl_delta_rule_workspace_bytes(int32_t dtype, int32_t n_seq, int32_t rows, int32_t Hk, int32_t H,
+                                              int32_t Dk, int32_t Dv) {
+  if ((dtype != TCL_F32 && dtype != TCL_BF16) || n_seq == 0 || !delta_sizes(n_seq, rows, Hk, H, Dk, Dv)) return 0;
+  return delta_rule_workspace_bytes(dtype == TCL_BF16, n_seq, rows, Hk, H, Dk, Dv);
+}
+
+TCL_API tcl_status tcl_delta_rule(const tcl_delta_rule_args* args, const int32_t* d_slots, int32_t n_slots,
+                                  float* d_state_out, void* d_o, int64_t ldo, void* d_workspace, size_t ws_bytes,
+                                  void* stream) {
+  DeltaOp op;
+  if (tcl_status st = delta_op(args, &op)) return st;
+  if (tcl_status st = check_slots(d_slots, n_slots, op.n_seq, op.state || d_state_out)) return st;
+  if (ldo < (int64_t)op.H * op.Dv) return fail(TCL_ERR_INVALID_ARG, "leading dimension smaller than the row");
+  if (!d_o && op.rows > 0) return fail(TCL_ERR_INVALID_ARG, "NULL device pointer");
+  if (misaligned(d_o, op.bf16 ? 2 : 4)) return fail(TCL_ERR_INVALID_ARG, "o is not aligned to its type");
+  if (misaligned(d_state_out, 16)) return fail(TCL_ERR_INVALID_ARG, "the states must be 16-byte aligned");
+  if (op.n_seq == 0) return TCL_OK;
+  op.slots = d_slots;
+  op.n_slots = n_slots;
+  const size_t need =
+      op.offs ? delta_rule_workspace_bytes(op.bf16, op.n_seq, op.rows, op.Hk, op.H, op.Dk, op.Dv) : 0;
+  if (tcl_status st = check_workspace(d_workspace, ws_bytes, need)) return st;
+  TCL_HIP(launch_delta_rule(op, d_state_out, d_o, ldo, static_cast<float*>(d_workspace),
+                            static_cast<hipStream_t>(stream)));
+  return TCL_OK;
+}
+
+TCL_API size_t tcl_delta_rule_backward_workspace_bytes(int32_t dtype, int32_t n_seq, int32_t rows, int32_t Hk,
+                                                       int32_t H, int32_t Dk, int32_t Dv) {
+  if ((dtype != TCL_F32 && dtype != TCL_BF16) || n_seq == 0 || !delta_sizes(n_seq, rows, Hk, H, Dk, Dv)) return 0;
+  return delta_rule_bwd_workspace_bytes(dtype == TCL_BF16, n_seq, rows, Hk, H, Dk, Dv);
+}
+
+TCL_API tcl_status tcl_delta_rule_backward(const tcl_delta_rule_args* args, const void* d_do, int64_t lddo,
+                                           const float* d_dstate_out, const tcl_delta_rule_grads* g,
+                                           void* d_workspace, size_t ws_bytes, void* stream) {
+  DeltaOp op;
+  if (tcl_status st = delta_op(args, &op)) return st;
+  if (!g) return fail(TCL_ERR_INVALID_ARG, "grads is NULL");
+  const int64_t qk = (int64_t)op.Hk * op.Dk, v = (int64_t)op.H * op.Dv;
+  if (lddo < v || g->lddq < qk || g->lddk < qk || g->lddv < v || g->lddg < op.H || g->lddbeta < op.H)
+    return fail(TCL_ERR_INVALID_ARG, "leading dimension smaller than the row");
+  if (op.rows > 0 && (!d_do || !g->d_dq || !g->d_dk || !g->d_dv || !g->d_dg || !g->d_dbeta))
+    return fail(TCL_ERR_INVALID_ARG, "NULL device pointer");
+  const uintptr_t el = op.bf16 ? 2 : 4;
+  if (misaligned(d_do, el) || misaligned(g->d_dq, el) || misaligned(g->d_dk, el) || misaligned(g->d_dv, el))
+    return fail(TCL_ERR_INVALID_ARG, "activations are not aligned to their type");
+  if (misaligned(d_dstate_out, 16) || misaligned(g->d_dstate, 16))
+    return fail(TCL_ERR_INVALID_ARG, "the states' gradients must be 16-byte aligned");
+  if (op.n_seq == 0) return fail(TCL_ERR_INVALID_ARG, "no sequences to take gradients of");
+  op.n_slots = op.n_seq;
+  const size_t need = delta_rule_bwd_workspace_bytes(op.bf16, op.n_seq, op.rows, op.Hk, op.H, op.Dk, op.Dv);
+  if (tcl_status st = check_workspace(d_workspace, ws_bytes, need)) return st;
+  DeltaGrads o;
+  o.dq = g->d_dq; o.dk = g->d_dk; o.dv = g->d_dv; o.lddq = g->lddq; o.lddk = g->lddk; o.lddv = g->lddv;
+  o.dg = g->d_dg; o.dbeta = g->d_dbeta; o.lddg = g->lddg; o.lddb = g->lddbeta; o.dstate = g->d_dstate;
+  TCL_HIP(launch_delta_rule_bwd(op, d_do, lddo, d_dstate_out, o, static_cast<float*>(d_workspace),
+                                static_cast<hipStream_t>(stream)));
+  return TCL_OK;
+}
+
+// ------------------------------------------------------------------ beam search
+
+namespace {
+
+constexpr int kMaxBeams = 64, kMaxCandidates = 64;
+
+bool beam_sizes(int32_t groups, int32_t W, int32_t V, int32_t K) {
+  return groups >= 0 && W >= 1 && W <= kMaxBeams && (int64_t)groups * W <= kMaxLogitRows && V >= 1 && V <= (1 << 30) &&
+         K >= 1 && K <= kMaxCandidates;
+}
+
+}  // namespace
+
+TCL_API size_t tcl_beam_select_workspace_bytes(int32_t n_groups, int32_t W, int32_t V, int32_t K) {
+  if (n_groups == 0 || !beam_sizes(n_groups, W, V, K)) return 0;
+  return beam_select_workspace_bytes(n_groups, W, V, K);
+}
+
+TCL_API tcl_status tcl_beam_select(int32_t dtype, int32_t n_groups, int32_t W, int32_t V, const void* d_logits,
+                                   int64_t ld, float temperature, const float* d_score, const int32_t* d_ended,
+                                   int32_t K, int32_t* d_parent, int32_t* d_token, float* d_out_score,
+                                   void* d_workspace, size_t ws_bytes, void* stream) {
+  if (n_groups < 0 || W < 1) return fail(TCL_ERR_INVALID_ARG, "need n_groups >= 0, W > 0 (got %d, %d)", n_groups, W);
+  if (W > kMaxBeams || K < 1 || K > kMaxCandidates)
+    return fail(TCL_ERR_UNSUPPORTED, "W and K must be in [1, %d] and [1, %d] (got %d, %d)", kMaxBeams, kMaxCandidates, W,
+                K);
+  if ((int64_t)n_groups * W > kMaxLogitRows)
+    return fail(TCL_ERR_UNSUPPORTED, "there must be fewer than 2^22 beams (got %d x %d)", n_groups, W);
+  LogitRows a;
+  if (tcl_status st = logit_rows(dtype, n_groups * W, V, d_logits, ld, nullptr, temperature, &a)) return st;
+  if (n_groups == 0) return TCL_OK;
+  if (!d_score || !d_parent || !d_token || !d_out_score) return fail(TCL_ERR_INVALID_ARG, "NULL device pointer");
+  if (d_out_score == d_score) return fail(TCL_ERR_INVALID_ARG, "the candidates' scores in place of the beams'");
+  if (tcl_status st = check_workspace(d_workspace, ws_bytes, beam_select_workspace_bytes(n_groups, W, V, K))) return st;
+  TCL_HIP(launch_beam_select(a, W, K, d_score, d_ended, d_parent, d_token, d_out_score, d_workspace,
+                             static_cast<hipStream_t>(stream)));
+  return TCL_OK;
+}
+
+TCL_API tcl_status tcl_beam_reorder(int32_t n_groups, int32_t W, const int32_t* d_parent, const int32_t* d_slots,
+                                    int32_t n_slots, int32_t* d_slots_out, int32_t n_pools,
+                                    const tcl_beam_pool* pools, void* stream) {
+  if (n_groups < 0 || W < 1 || n_slots < 0 || n_pools < 0)
+    return fail(TCL_ERR_INVALID_ARG, "negative size (n_groups=%d W=%d n_slots=%d n_pools=%d)", n_groups, W, n_slots,
+                n_pools);
+  if (W > kMaxBeams) return fail(TCL_ERR_UNSUPPORTED, "W must be in [1, %d] (got %d)", kMaxBeams, W);
+  if ((int64_t)n_groups * W > kMaxLogitRows)
+    return fail(TCL_ERR_UNSUPPORTED, "there must be fewer than 2^22 beams (got %d x %d)", n_groups, W);
+  if (n_pools > 0 && !pools) return fail(TCL_ERR_INVALID_ARG, "pools is NULL");
+  for (int i = 0; i < n_pools; ++i) {
+    if (pools[i].bytes < 1 || pools[i].bytes > ((int64_t)1 << 31))
+      return fail(TCL_ERR_UNSUPPORTED, "pool %d: a state has 1 to 2^31 bytes (got %lld)", i, (long long)pools[i].bytes);
+    if (!pools[i].d_states && n_slots > 0) return fail(TCL_ERR_INVALID_ARG, "NULL device pointer");
+  }
+  if (n_groups == 0) return TCL_OK;
+  if (!d_parent || !d_slots || !d_slots_out) return fail(TCL_ERR_INVALID_ARG, "NULL device pointer");
+  const uintptr_t in = reinterpret_cast<uintptr_t>(d_slots), par = reinterpret_cast<uintptr_t>(d_parent),
+                  out = reinterpret_cast<uintptr_t>(d_slots_out), len = (uintptr_t)n_groups * W * sizeof(int32_t);
+  if ((out < in + len && in < out + len) || (out < par + len && par < out + len))
+    return fail(TCL_ERR_INVALID_ARG, "d_slots_out overlaps an input");
+  static_assert(sizeof(tcl_beam_pool) == sizeof(BeamPool), "one layout");
+  TCL_HIP(launch_beam_reorder(n_groups, W, d_parent, d_slots, n_slots, d_slots_out, n_pools,
+                              reinterpret_cast<const BeamPool*>(pools), static_cast<hipStream_t>(stream)));
   return TCL_OK;
 }

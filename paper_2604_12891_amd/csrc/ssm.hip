@@ -1,18 +1,12 @@
 // The causal convolution and the selective scan as operators of their own,
 // with states carried over: prompts (packed sequences), single tokens, and
 // their gradients.
-//
-// Sequence i owns rows offs[i] .. offs[i+1]-1 of every activation. Work along
-// the rows is cut into tiles of R rows that never straddle two sequences:
-// sequence i's tiles start at index key(i) = offs[i] / R + i, which leaves
-// room for ceil(len / R) of them (and at least one, so an empty sequence has
-// a tile that passes its state on), rises strictly with i, and is found from a
-// tile index by bisection, without a table. rows / R + n_seq bounds the
-// count on the host, which does not know the offsets.
+// Work along the rows is cut into tiles of R rows (packing.h).
 #include <algorithm>
 
 #include "common.h"
 #include "ops.h"
+#include "packing.h"
 
 namespace tcl {
 namespace {
@@ -95,46 +89,6 @@ __device__ __forceinline__ void pk_store(T* p, const float* v) {
     for (int i = 0; i < CH / 2; ++i) o.v[i] = f32x2_to_bf16x2(v[2 * i], v[2 * i + 1]);
     *reinterpret_cast<Pack<T, CH>*>(p) = o;
   }
-}
-
-struct Tile {
-  int seq;   // -1: no sequence has this tile
-  int j;     // its index in the sequence
-  int base;  // the sequence's first row
-  int len;
-};
-
-// Tile w of R rows. Offsets are read as lying in [0, rows], so a wrong one
-// cannot lead outside the activations.
-__device__ __forceinline__ Tile find_tile(const int* __restrict__ offs, int n_seq, int rows, int R, int w) {
-  Tile t = {-1, 0, 0, 0};
-  if (!offs) {
-    if (w < n_seq) t = {w, 0, w, 1};
-    return t;
-  }
-  int lo = 0, hi = n_seq;  // key(lo) <= w < key(hi), once the ends are taken
-  if (R > rows) {          // one tile per sequence
-    if (w >= n_seq) return t;
-    lo = w;
-    hi = w + 1;
-  }
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (offs[mid] / R + mid <= w) lo = mid;
-    else hi = mid;
-  }
-  const int o0 = min(max(offs[lo], 0), rows), o1 = min(max(offs[lo + 1], o0), rows);
-  t.j = w - (o0 / R + lo);
-  t.base = o0;
-  t.len = o1 - o0;
-  t.seq = t.j >= 0 && (t.j == 0 || (int64_t)t.j * R < t.len) ? lo : -1;
-  return t;
-}
-
-// The state of sequence `seq` in the pool, -1 for none.
-__device__ __forceinline__ int slot_of(const int* __restrict__ slots, int n_slots, int seq) {
-  const int j = slots ? slots[seq] : seq;
-  return j >= 0 && j < n_slots ? j : -1;
 }
 
 // ---------------------------------------------------------------- causal conv + SiLU
@@ -1238,12 +1192,16 @@ ConvParts conv_parts(int n_seq, int rows, int E) {
   return p;
 }
 
+}  // namespace
+
 // One trip up to 512 parts, by halves.
 void sum_parts(const float* part, int parts, int M, int total, int E, float* o0, float* o1, float* o2, hipStream_t s) {
   const dim3 grid((unsigned)(((int64_t)total * E + 63) / 64));
   if (parts > 16 * kSumLanes) sum_parts_kernel<32><<<grid, 64 * kSumLanes, 0, s>>>(part, parts, M, total, E, o0, o1, o2);
   else sum_parts_kernel<16><<<grid, 64 * kSumLanes, 0, s>>>(part, parts, M, total, E, o0, o1, o2);
 }
+
+namespace {
 
 template <typename T, int K, int CH>
 hipError_t conv_fwd(const ConvOp& a, void* state_out, void* u, int64_t ldu, hipStream_t s) {

@@ -1,0 +1,175 @@
+"""Beam search (tcl_beam_select, tcl_beam_reorder) against the fp64 oracle (oracle/search.py).
+
+Parents and tokens are equal; scores are sums of numbers of order 30, whose softmax sums carry some sixteen fp32
+roundings each way of the hardware's exponential: 2^-24 (32 + 2 |score|) at most."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import search as osr
+
+pytestmark = pytest.mark.gpu
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+INF, NAN = float("inf"), float("nan")
+
+
+def _tb():
+    from paper_2604_12891_amd import binding as tb
+    return tb
+
+
+def _same(r, ref):
+    assert np.array_equal(r["parent"].cpu().numpy(), ref["parent"]), np.argwhere(r["parent"].cpu().numpy() != ref["parent"])[:4]
+    assert np.array_equal(r["token"].cpu().numpy(), ref["token"])
+    got, want = r["score"].double().cpu().numpy(), ref["score"]
+    live = np.isfinite(want)
+    assert np.array_equal(got[~live], want[~live])
+    got, want = got[live], want[live]
+    assert (np.abs(got - want) <= 2.0 ** -24 * (32 + 2 * np.abs(want))).all()
+
+
+# rows whole, in wavefronts and in parts; lists in LDS and not; fewer candidates than places
+SIZES = [(1, 1, 1, 1), (1, 4, 50001, 4), (3, 5, 7, 64), (2, 64, 40, 64), (70, 4, 1000, 8), (1, 64, 70001, 64),
+         (9, 8, 20000, 16), (300, 3, 90, 3), (2, 1, 131072, 2), (33, 16, 5000, 33), (1, 16, 40000, 64)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("G,W,V,K", SIZES)
+def test_select(G, W, V, K, dtype):
+    print(f"select G={G} W={W} V={V} K={K} {dtype}", flush=True)
+    rng = np.random.default_rng(V)
+    x = torch.from_numpy(2.5 * rng.standard_normal((G * W, V)) + rng.standard_normal((G * W, 1))).to(DT[dtype])
+    x[torch.from_numpy(rng.random((G * W, V)) < 0.2)] = -INF
+    score = (-10 * rng.random((G, 1)) - 3 * rng.random((G, W))).astype(np.float32)
+    ended = np.full((G, W), -1, np.int32)
+    if W > 2:
+        ended[::2, W - 1] = 5
+        score[::3, 0] = -INF
+        score[1::3, 1] = NAN
+    buf = torch.full((G * W, V + 3), NAN, dtype=DT[dtype], device="cuda")
+    X = buf[:, 1:V + 1]
+    X.copy_(x)
+    closed = torch.from_numpy(~(score > -INF) | (ended >= 0)).reshape(-1)
+    X[closed.cuda()] = NAN  # beams that are dead or ended are not read
+    r = _tb().beam_select(X, torch.from_numpy(score).cuda(), K, torch.from_numpy(ended).cuda())
+    _same(r, osr.beam_select(x.double().numpy(), score, K, ended))
+    r = _tb().beam_select(X, torch.from_numpy(score).cuda(), K, torch.from_numpy(ended).cuda(), temperature=0.5)
+    _same(r, osr.beam_select(x.double().numpy(), score, K, ended, 0.5))
+
+
+def test_ties():
+    """Equal scores: the lower row, then the lower token, also across the parts of a long row."""
+    for V in (70, 60000):
+        x = torch.zeros(6, V, device="cuda")
+        x[:, V // 2] = 1.0
+        x[:, V - 1] = 1.0
+        r = _tb().beam_select(x, torch.zeros(2, 3, device="cuda"), 8)
+        assert r["parent"].tolist() == [[0, 0, 1, 1, 2, 2, 0, 0], [3, 3, 4, 4, 5, 5, 3, 3]]
+        assert r["token"].tolist() == [[V // 2, V - 1] * 3 + [0, 1]] * 2
+        # a long search's score, to whose step in fp32 the logits' difference is nothing, still tells them apart
+        x = torch.zeros(2, V, device="cuda")
+        x[0, 3], x[1, 2] = 1e-4, 2e-4
+        r = _tb().beam_select(x, torch.full((1, 2), -20000.0, device="cuda"), 2)
+        assert r["parent"].tolist() == [[1, 0]] and r["token"].tolist() == [[2, 3]]
+
+
+def test_masks_and_infinities():
+    """All masked or dead: nothing; masks of the type's lowest value are candidates; NaN is masked; a row with
+    +inf is out."""
+    tb = _tb()
+    for t in (torch.float32, torch.bfloat16):
+        x = torch.full((4, 300), -INF, dtype=t, device="cuda")
+        z = torch.zeros(1, 4, device="cuda")
+        r = tb.beam_select(x, z, 3)
+        assert (r["parent"] == -1).all() and (r["token"] == -1).all() and (r["score"] == -INF).all()
+        r = tb.beam_select(x.zero_(), z - INF, 3)
+        assert (r["parent"] == -1).all() and (r["score"] == -INF).all()
+        x.fill_(torch.finfo(t).min)
+        x[0, 9] = 0.0
+        x[1] = NAN
+        x[2, 5] = INF
+        x[3] = -INF
+        x[3, 7] = 2.0
+        r = tb.beam_select(x, z, 4)
+        assert r["parent"].tolist() == [[0, 3, 0, 0]] and r["token"].tolist() == [[9, 7, 0, 1]]
+        # (the differences to a row's maximum are beyond fp32 once rounded there, not the order)
+        assert r["score"][0, :2].tolist() == [0.0, 0.0] and (r["score"][0, 2:] < -1e38).all()
+
+
+def _reorder_case(G, W, extra, seed, kind):
+    rng = np.random.default_rng(seed)
+    n = G * W
+    slots = rng.permutation(n + extra)[:n].reshape(G, W).astype(np.int32)
+    base = W * np.arange(G)[:, None]
+    parent = {"random": lambda: rng.integers(0, W, (G, W)) + base, "same": lambda: np.zeros((G, W), int) + base,
+              "stay": lambda: np.arange(W)[None] + base, "swap": lambda: np.arange(W)[None, ::-1] + base,
+              "none": lambda: np.full((G, W), -1), "wild": lambda: rng.integers(-2, n + 2, (G, W))}[kind]()
+    return parent.astype(np.int32), slots
+
+
+@pytest.mark.parametrize("kind", ["random", "same", "stay", "swap", "none", "wild"])
+@pytest.mark.parametrize("G,W", [(1, 1), (1, 4), (5, 3), (2, 64), (40, 8)])
+def test_reorder(G, W, kind):
+    """Pools of every alignment and size; places of other sequences are left as they are."""
+    print(f"reorder G={G} W={W} {kind}", flush=True)
+    rng = np.random.default_rng(W)
+    parent, slots = _reorder_case(G, W, 3, G, kind)
+    N = G * W + 3
+    if kind == "wild" and W > 1:
+        slots[0, 0], slots[-1, -1] = -1, N  # beams whose state is nowhere
+    shapes = [((3, 37), np.float32), ((5,), np.uint8), ((1,), np.float64), ((4099,), np.float32), ((33000,), np.uint8)]
+    host = [(rng.integers(0, 250, (N, *s)).astype(t)) for s, t in shapes]
+    pools = []
+    for h in host:  # from an odd element on
+        buf = torch.empty(h.size + 1, dtype=torch.from_numpy(h[:1]).dtype, device="cuda")
+        p = buf[1:].view(h.shape)
+        p.copy_(torch.from_numpy(h))
+        pools.append(p)
+    new = _tb().beam_reorder(torch.from_numpy(parent).cuda(), torch.from_numpy(slots).cuda(), pools)
+    want, after = osr.beam_reorder(parent, slots, N, host)
+    assert np.array_equal(new.cpu().numpy(), want)
+    for p, a in zip(pools, after):
+        assert np.array_equal(p.cpu().numpy(), a)
+
+
+def test_many_pools():
+    """More pools than one launch takes, as layers have them."""
+    parent, slots = _reorder_case(3, 4, 2, 0, "random")
+    host = [np.random.default_rng(i).standard_normal((14, 3 + i)).astype(np.float32) for i in range(150)]
+    pools = [torch.from_numpy(h).cuda() for h in host]
+    new = _tb().beam_reorder(torch.from_numpy(parent).cuda(), torch.from_numpy(slots).cuda(), pools)
+    want, after = osr.beam_reorder(parent, slots, 14, host)
+    assert np.array_equal(new.cpu().numpy(), want)
+    assert all(np.array_equal(p.cpu().numpy(), a) for p, a in zip(pools, after))
+    new = _tb().beam_reorder(torch.from_numpy(parent).cuda(), torch.from_numpy(slots).cuda(), [])
+    assert np.array_equal(new.cpu().numpy(), want)
+
+
+def test_streams_and_graph():
+    """A step of a search captured with its workspace: selection, then reordering; replays give the eager bits."""
+    tb = _tb()
+    torch.manual_seed(0)
+    G, W, V = 3, 4, 9000
+    x, score = torch.randn(G * W, V, device="cuda"), -torch.rand(G, W, device="cuda")
+    slots = torch.randperm(G * W, device="cuda").int().view(G, W)
+    start = torch.randn(G * W, 500, device="cuda")
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    r = tb.beam_select(x, score, stream=s)
+    torch.cuda.current_stream().wait_stream(s)
+    e = tb.beam_select(x, score)
+    assert all(torch.equal(r[k], e[k]) for k in r)
+    pool, new = start.clone(), torch.empty_like(slots)
+    ws = tb.beam_select_workspace(G, W, V, W)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        r = tb.beam_select(x, score, workspace=ws)
+        tb.beam_reorder(r["parent"], slots, [pool], out=new)
+    for _ in range(4):
+        x.copy_(torch.randn_like(x))
+        pool.copy_(start)
+        graph.replay()
+        torch.cuda.synchronize()
+        e, p = tb.beam_select(x, score), start.clone()
+        n = tb.beam_reorder(e["parent"], slots, [p])
+        assert all(torch.equal(r[k], e[k]) for k in e) and torch.equal(n, new) and torch.equal(p, pool)

@@ -1,0 +1,239 @@
+"""The gated delta rule with carried states (tcl_delta_rule and its gradients) against the fp64
+oracle (oracle/layer.py), token by token.
+
+Tolerance: per head, the 2-norm of the difference relative to that of the result. An entry of a
+chunk is a sum of up to Dk + 2 x 64 + 16 products, each with a rounding of 2^-24 of random sign, so its
+error grows as the root of their number; with |k| = 1 and beta <= 1 what a chunk passes on is contracted, so c chunks'
+errors add as independent ones, and gradients pass through both walks. That is
+tolerance(); what bf16 results round away (2^-8) is added."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import layer as ol
+
+pytestmark = pytest.mark.gpu
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+NAN = float("nan")
+GRADS = ("dq", "dk", "dv", "dg", "dbeta", "dstate")
+
+
+def tolerance(Dk, lens):
+    chunks = max([(x + 63) // 64 for x in lens] + [1])
+    return 2.0 ** -24 * 2 * (Dk + 2 * 64 + 16) ** 0.5 * (1 + chunks) ** 0.5
+
+
+def head_errors(got, ref):
+    """Relative 2-norms of the differences, per head: axis 1 of what has rows or sequences on axis 0."""
+    axes = tuple(i for i in range(ref.ndim) if i != 1)
+    norm = lambda a: np.sqrt((a ** 2).sum(axes))
+    return norm(got - ref) / np.maximum(norm(ref), 1e-30)
+
+
+def _tb():
+    from paper_2604_12891_amd import binding as tb
+    return tb
+
+
+def _near(name, got, ref, tol):
+    got = got.double().cpu().numpy()
+    assert got.shape == ref.shape and np.isfinite(got).all(), name
+    if ref.size:
+        e = head_errors(got, ref)
+        assert (e <= tol).all(), (name, e.max(), tol)
+
+
+def _case(lens, Hk, H, Dk, Dv, dtype, seed, full=True, steep=False):
+    """Inputs as the kernels get them (rounded), in float64."""
+    rng = np.random.default_rng(seed)
+    T, n = sum(lens), len(lens)
+    rnd = lambda a, t: torch.from_numpy(a).to(t).double().numpy()
+    unit = lambda a: a / np.linalg.norm(a, axis=-1, keepdims=True)
+    f32 = torch.float32
+    g = -rng.exponential(0.2, (T, H))
+    if steep and T:  # tokens that forget nearly all, or all
+        g[rng.random((T, H)) < 0.1] = -60.0
+        g[rng.random((T, H)) < 0.05] = -np.inf
+    return dict(q=rnd(unit(rng.standard_normal((T, Hk, Dk))), DT[dtype]), k=rnd(unit(rng.standard_normal((T, Hk, Dk))), DT[dtype]),
+                v=rnd(rng.standard_normal((T, H, Dv)), DT[dtype]), g=rnd(g, f32), beta=rnd(rng.uniform(0, 1, (T, H)), f32),
+                offs=np.concatenate([[0], np.cumsum(lens)]).astype(np.int32),
+                state=rnd(rng.standard_normal((n, H, Dk, Dv)), f32) if full else None)
+
+
+def _gpu(a, dtype, loose, spare=2, drop=("offs", "state")):
+    """The activations on the GPU; loose: with leading dimensions, from odd elements on, NaN beside them and in
+    `spare` rows that no sequence owns."""
+    out = {}
+    for name, x in a.items():
+        if name in drop or x is None:
+            continue
+        t = torch.float32 if name in ("g", "beta") else DT[dtype]
+        T, shape = x.shape[0], x.shape[1:]
+        width = int(np.prod(shape))
+        ld, first = (width + 5, 3) if loose else (width, 0)
+        buf = torch.full((first + (T + spare) * ld,), NAN, dtype=t, device="cuda")
+        v = buf[first:].view(T + spare, ld)[:, :width].unflatten(1, shape)
+        v[:T].copy_(torch.from_numpy(x))
+        out[name] = v
+    return out
+
+
+# lengths: empty sequences, one token, chunks that end before, at and after their last token
+CASES = [([1, 0, 25, 7, 2], 1, 2, 64, 64), ([64], 1, 1, 64, 64), ([65, 63, 0, 128], 2, 4, 128, 128),
+         ([200, 129, 1], 2, 2, 72, 40), ([33, 90], 1, 3, 8, 8), ([150], 1, 1, 128, 256), ([70, 40], 3, 3, 24, 136),
+         ([1] * 40, 2, 2, 16, 32), ([0, 0], 1, 1, 8, 16), ([2, 400], 1, 1, 120, 72)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("steep", [False, True])
+@pytest.mark.parametrize("lens,Hk,H,Dk,Dv", CASES)
+def test_rule_and_gradients(lens, Hk, H, Dk, Dv, steep, dtype):
+    print(f"delta lens={lens} Hk={Hk} H={H} Dk={Dk} Dv={Dv} steep={steep} {dtype}", flush=True)
+    tb, T, n = _tb(), sum(lens), len(lens)
+    rng = np.random.default_rng(7)
+    for full in (False, True):
+        a = _case(lens, Hk, H, Dk, Dv, dtype, Dk + Dv, full, steep)
+        x = _gpu(a, dtype, loose=full)
+        offs = torch.from_numpy(a["offs"]).cuda()
+        S = None if a["state"] is None else torch.from_numpy(a["state"]).float().cuda()
+        end = torch.full((n, H, Dk, Dv), NAN, device="cuda")
+        out = torch.full((T + 2, H, Dv), 7.0, dtype=DT[dtype], device="cuda")
+        tb.delta_rule(**x, offs=offs, state=S, state_out=end, out=out)
+        r = ol.delta_rule(**a)
+        tol, half = tolerance(Dk, lens), 2.0 ** -8 if dtype == "bf16" else 0.0
+        _near("o", out[:T], r["o"], tol + half)
+        _near("end", end, r["end"], tol)
+        assert (out[T:] == 7.0).all()
+        if S is not None:
+            tb.delta_rule(**x, offs=offs, state=S, state_out=S)  # in place
+            assert torch.equal(S, end)
+            S = torch.from_numpy(a["state"]).float().cuda()
+        do = torch.from_numpy(rng.standard_normal((T, H, Dv))).to(DT[dtype]).double().numpy()
+        dend = rng.standard_normal((n, H, Dk, Dv)).astype(np.float32) if full else None
+        r = ol.delta_rule_backward(do=do, dend=dend, **a)
+        DO = _gpu(dict(do=do), dtype, loose=full)["do"]
+        outs = dict(dq=(x["q"], DT[dtype]), dk=(x["k"], DT[dtype]), dv=(x["v"], DT[dtype]), dg=(x["g"], torch.float32),
+                    dbeta=(x["beta"], torch.float32))
+        outs = {k: torch.full(v.shape, 7.0, dtype=t, device="cuda") for k, (v, t) in outs.items()}
+        g = tb.delta_rule_backward(**x, do=DO, offs=offs, state=S,
+                                   state_grad=None if dend is None else torch.from_numpy(dend).cuda(), out=outs)
+        for name in GRADS:
+            if name == "dstate":
+                if full:
+                    _near(name, g[name], r[name], tol)
+                else:
+                    assert g[name] is None
+                continue
+            _near(name, g[name][:T], r[name], tol + (half if name in ("dq", "dk", "dv") else 0.0))
+            assert (g[name][T:] == 7.0).all(), name
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,Hk,H,Dk,Dv", [(1, 1, 1, 64, 64), (7, 2, 4, 24, 40), (40, 1, 2, 128, 256), (3, 1, 1, 8, 8)])
+def test_tokens_with_slots(n, Hk, H, Dk, Dv, dtype):
+    """One token per sequence, states in a pool larger than the batch, some sequences without one; a second
+    token continues the first; the gradients of single tokens."""
+    print(f"delta tokens n={n} Hk={Hk} H={H} Dk={Dk} Dv={Dv} {dtype}", flush=True)
+    tb, rng, pool = _tb(), np.random.default_rng(n), n + 5
+    slots = rng.permutation(pool)[:n].astype(np.int32)
+    slots[n // 2] = -1
+    if n > 3:
+        slots[0] = pool  # past the pool: none
+    live = (slots >= 0) & (slots < pool)
+    want = rng.standard_normal((pool, H, Dk, Dv)).astype(np.float32).astype(np.float64)
+    S = torch.from_numpy(want).float().cuda()
+    one, tol = np.arange(n + 1), tolerance(Dk, [1]) + (2.0 ** -8 if dtype == "bf16" else 0.0)
+    for t in range(2):
+        a = _case([1] * n, Hk, H, Dk, Dv, dtype, t + n, False)
+        x = _gpu(a, dtype, loose=t == 1, spare=0)
+        a["offs"], a["state"] = one, np.where(live[:, None, None, None], want[np.where(live, slots, 0)], 0.0)
+        o = tb.delta_rule(**x, state=S, state_out=S, slots=torch.from_numpy(slots).cuda())
+        r = ol.delta_rule(**a)
+        _near("o", o, r["o"], tol)
+        want[slots[live]] = r["end"][live]
+        _near("pool", S, want, tolerance(Dk, [1] * 2))
+    do = torch.from_numpy(rng.standard_normal((n, H, Dv))).to(DT[dtype])
+    st = torch.from_numpy(a["state"]).float()
+    a["state"] = st.double().numpy()
+    g, r = tb.delta_rule_backward(**x, do=do.cuda(), state=st.cuda()), ol.delta_rule_backward(do=do.double().numpy(), **a)
+    for name in GRADS:
+        _near(name, g[name], r[name], tol if name in ("dq", "dk", "dv") else tolerance(Dk, [1]))
+
+
+def test_a_prompt_then_tokens():
+    """A prompt in one call equals its tokens one by one, through the pool."""
+    tb, lens, H, D = _tb(), [130, 70], 2, 64
+    a = _case(lens, 1, H, D, D, "f32", 3, False)
+    x = _gpu(a, "f32", False, spare=0)
+    offs = torch.from_numpy(a["offs"]).cuda()
+    end, S = torch.empty(2, H, D, D, device="cuda"), torch.zeros(3, H, D, D, device="cuda")
+    o = tb.delta_rule(**x, offs=offs, state_out=end)
+    first = [int(v) for v in a["offs"][:2]]
+    slots = torch.tensor([2, 0], dtype=torch.int32, device="cuda")
+    for t in range(max(lens)):
+        rows = [first[i] + t for i in range(2) if t < lens[i]]
+        at = slots[:len(rows)] if len(rows) == 2 else slots[[i for i in range(2) if t < lens[i]]]
+        y = tb.delta_rule(**{k: v[rows] for k, v in x.items()}, state=S, state_out=S, slots=at)
+        # both are fp32 computations of the same: twice the tolerance
+        for i, row in enumerate(rows):
+            assert (y[i] - o[row]).norm() <= 2 * tolerance(D, lens) * o[row].norm() + 1e-6
+    _near("end", S[[2, 0]], end.double().cpu().numpy(), 2 * tolerance(D, lens))
+    assert not S[1].any()
+
+
+def test_gradients_are_differences():
+    """Of the kernel's own forward pass, along one direction of all inputs. Step 2^-7 of a unit direction: third
+    derivatives of order 100 give 100 step^2 / 6, the roundings (2^-24 x tolerance's factor) of some 4,000 results of order 1
+    divided by the step the rest."""
+    tb, H, D = _tb(), 2, 32
+    a = _case([100, 30], 1, H, D, D, "f32", 5)
+    x, offs = _gpu(a, "f32", False, spare=0), torch.from_numpy(a["offs"]).cuda()
+    x["state"] = torch.from_numpy(a["state"]).float().cuda()
+    torch.manual_seed(2)
+    do, dend = torch.randn(130, H, D, device="cuda"), torch.randn_like(x["state"])
+    g = tb.delta_rule_backward(**x, do=do, offs=offs, state_grad=dend)
+    for name in x:
+        d = torch.randn_like(x[name])
+        d /= d.norm()
+        step = 2.0 ** -7
+
+        def f(s):
+            y = dict(x, **{name: x[name] + s * step * d})
+            end = torch.empty_like(dend)
+            o = tb.delta_rule(**y, offs=offs, state_out=end)
+            return ((o.double() * do).sum() + (end.double() * dend).sum()).item()
+
+        want, got = (f(1.0) - f(-1.0)) / (2 * step), (g["d" + name].double() * d).sum().item()
+        assert abs(got - want) < 100 * step ** 2 / 6 + tolerance(D, [100]) * 4000 ** 0.5 / step, (name, got, want)
+
+
+def test_streams_and_graph():
+    """A prompt and its gradients on another stream, and captured with workspaces of their own: replays on
+    new inputs give the eager bits, with eager work between them."""
+    tb, lens, H, D = _tb(), [100, 61], 2, 64
+    a = _case(lens, 1, H, D, D, "bf16", 9)
+    x, offs = _gpu(a, "bf16", False, spare=0), torch.from_numpy(a["offs"]).cuda()
+    S = torch.from_numpy(a["state"]).float().cuda()
+    do = torch.randn(161, H, D, device="cuda").bfloat16()
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    o = tb.delta_rule(**x, offs=offs, state=S, stream=s)
+    g = tb.delta_rule_backward(**x, do=do, offs=offs, state=S, stream=s)
+    torch.cuda.current_stream().wait_stream(s)
+    assert torch.equal(o, tb.delta_rule(**x, offs=offs, state=S))
+    sizes = (torch.bfloat16, 2, 161, 1, H, D, D)
+    ws, wb = tb.delta_rule_workspace(*sizes), tb.delta_rule_workspace(*sizes, backward=True)
+    out, end, og = torch.empty_like(o), torch.empty_like(S), {k: torch.empty_like(v) for k, v in g.items()}
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        tb.delta_rule(**x, offs=offs, state=S, state_out=end, out=out, workspace=ws)
+        tb.delta_rule_backward(**x, do=do, offs=offs, state=S, state_grad=S, workspace=wb, out=og)
+    for _ in range(4):
+        x["v"].copy_(torch.randn_like(x["v"]))
+        S.copy_(torch.randn_like(S))
+        graph.replay()
+        torch.cuda.synchronize()
+        e = torch.empty_like(end)
+        assert torch.equal(out, tb.delta_rule(**x, offs=offs, state=S, state_out=e)) and torch.equal(end, e)
+        want = tb.delta_rule_backward(**x, do=do, offs=offs, state=S, state_grad=S)
+        assert all(torch.equal(og[k], want[k]) for k in want)
