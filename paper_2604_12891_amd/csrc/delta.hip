@@ -192,6 +192,89 @@ __device__ __forceinline__ floatx4 mat_frag(const float* m, int w, int s) {
   return *reinterpret_cast<const floatx4*>(m + ((w * 4 + s) * 64 + (threadIdx.x & 63)) * 4);
 }
 
+// fp32-level products on the bf16 matrix cores: a value is a sum of three bf16 parts, each 2^-8 of the one in
+// front (split3_pair), and of two values' nine products of parts the six down to 2^-16 count. What is bf16 in memory
+// is one part. v_mfma_f32_16x16x32_bf16: lane l holds A[l % 16] and B[..][l % 16] at eight k's (which eight of the
+// 32 is free, the same for both) and D[4 (l / 16) + r][l % 16]. Against v_mfma_f32_16x16x4_f32 a product takes an
+// eighth of the cycles with one exact operand (three products), a third to a half with six.
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+template <int N>
+struct Parts {
+  bf16x8 p[N];
+};
+__device__ __forceinline__ bf16x8 pack8(u32x4 v) { return __builtin_bit_cast(bf16x8, v); }
+template <int N>
+__device__ __forceinline__ Parts<N> split8(floatx4 a, floatx4 b) {
+  u32x4 h, m, l;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    uint32_t x, y, z;
+    split3_pair(a[2 * i], a[2 * i + 1], x, y, z);
+    h[i] = x; m[i] = y; l[i] = z;
+    split3_pair(b[2 * i], b[2 * i + 1], x, y, z);
+    h[2 + i] = x; m[2 + i] = y; l[2 + i] = z;
+  }
+  Parts<N> r;
+  r.p[0] = pack8(h);
+  if constexpr (N > 1) r.p[1] = pack8(m);
+  if constexpr (N > 2) r.p[2] = pack8(l);
+  return r;
+}
+// Four neighbours' parts into LDS, part p at base + p * stride (bf16 entries).
+template <int N>
+__device__ __forceinline__ void put_parts(uint16_t* base, int stride, floatx4 v) {
+  u32x2 w[3];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    uint32_t x, y, z;
+    split3_pair(v[2 * i], v[2 * i + 1], x, y, z);
+    w[0][i] = x; w[1][i] = y; w[2][i] = z;
+  }
+#pragma unroll
+  for (int p = 0; p < N; ++p) *reinterpret_cast<u32x2*>(base + p * stride) = w[p];
+}
+template <int N>
+__device__ __forceinline__ Parts<N> get_parts(const uint16_t* base, int stride) {
+  Parts<N> r;
+#pragma unroll
+  for (int p = 0; p < N; ++p) r.p[p] = pack8(*reinterpret_cast<const u32x4*>(base + p * stride));
+  return r;
+}
+// Sums by the products' order, the smaller ones apart (and three chains of dependent instructions, not one).
+struct Acc {
+  floatx4 v[3];
+  __device__ __forceinline__ void clear() { v[0] = v[1] = v[2] = floatx4{0.f, 0.f, 0.f, 0.f}; }
+  __device__ __forceinline__ floatx4 sum() const { return v[0] + (v[1] + v[2]); }
+};
+// Products of parts up to order O (2: all that count; 1: to 2^-16).
+template <int O, int NA, int NB>
+__device__ __forceinline__ void mma32(const Parts<NA>& a, const Parts<NB>& b, Acc& c) {
+#pragma unroll
+  for (int i = 0; i < NA; ++i)
+#pragma unroll
+    for (int j = 0; j < NB; ++j)
+      if (i + j <= O) c.v[i + j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.p[i], b.p[j], c.v[i + j], 0, 0, 0);
+}
+// Eight neighbours of a row as they are in memory.
+template <typename T> struct Raw8;
+template <> struct Raw8<uint16_t> {
+  u32x4 v;
+  typedef u32x4 any __attribute__((aligned(2)));
+  __device__ __forceinline__ void load(const uint16_t* p) { v = *reinterpret_cast<const any*>(p); }
+  __device__ __forceinline__ void clear() { v = u32x4{0, 0, 0, 0}; }
+  __device__ __forceinline__ Parts<1> parts() const { return {{pack8(v)}}; }
+};
+template <> struct Raw8<float> {
+  floatx4 a, b;
+  __device__ __forceinline__ void load(const float* p) { a = ld4(p); b = ld4(p + 4); }
+  __device__ __forceinline__ void clear() { a = b = floatx4{0.f, 0.f, 0.f, 0.f}; }
+  __device__ __forceinline__ Parts<3> parts() const { return split8<3>(a, b); }
+};
+// In products over tokens, the eight of lane group kq of the 32 from 32 s on: 32 s + 16 a + 4 kq + m at
+// place 4 a + m. So the four tokens of a lane's results are neighbours in LDS, and two fragments of a
+// matrix (mat_frag) are one operand. Where token t = 16 w + 4 lk stands:
+__device__ __forceinline__ int token_place(int w, int lk) { return 32 * (w >> 1) + 8 * lk + 4 * (w & 1); }
+
 // A chunk of a sequence: its first row and how many tokens it has.
 struct Chunk {
   int row, n;
@@ -210,6 +293,18 @@ __device__ __forceinline__ void row_frags(const T* p, int64_t ld, Chunk c, int w
   }
 }
 
+// The same as operands of 32 k's, as they are in memory.
+template <typename T, int NS>
+__device__ __forceinline__ void row_raw(const T* p, int64_t ld, Chunk c, int w, int D, Raw8<T>* f) {
+  const int l = threadIdx.x & 63, t = 16 * w + (l & 15), k0 = 8 * (l >> 4);
+  const T* q = p + (c.row + min(t, c.n - 1)) * ld + k0;
+#pragma unroll
+  for (int s = 0; s < NS; ++s) {
+    f[s].clear();
+    if (t < c.n && 32 * s + k0 < D) f[s].load(q + 32 * s);
+  }
+}
+
 // ---------------------------------------------------------------- what needs no state
 // T and P (or, for the gradients, T, T^T and P^T) as fragments and beta, e^G and w of every chunk, a
 // workgroup per chunk and key head, which goes through the value heads that share it. Each of four
@@ -219,7 +314,8 @@ constexpr int kLdM = kC + 4;
 
 template <typename T, int DKP, bool GRADS>
 __global__ __launch_bounds__(256) void delta_prep_kernel(DeltaIn a, const T* __restrict__ q, const T* __restrict__ k,
-                                                         float* __restrict__ mats, float* __restrict__ coef) {
+                                                         float* __restrict__ mats, float* __restrict__ coef,
+                                                         T* __restrict__ kt) {
   __shared__ __attribute__((aligned(16))) float sA[kC * kLdM], sT[kC * kLdM], sX[32 * 36];
   __shared__ double sG[kC];
   __shared__ float sB[kC];
@@ -228,25 +324,48 @@ __global__ __launch_bounds__(256) void delta_prep_kernel(DeltaIn a, const T* __r
   const Tile tl = find_tile(a.offs, a.n_seq, a.rows, kC, tile);
   if (tl.seq < 0 || tl.len == 0) return;
   const Chunk c = {tl.base + tl.j * kC, min(kC, tl.len - tl.j * kC)};
-  constexpr int NF = DKP / 16;
+  constexpr int NS = DKP / 32;
+  const T* kp = k + (int64_t)hk * a.Dk;
   // products of rows: lane's entries [16 w + 4 lk + r][16 t + li]
   floatx4 kk[4], qk[4];
   {
-    floatx4 kf[NF], qf[NF];
-    const T* kp = k + (int64_t)hk * a.Dk;
-    row_frags<T, NF>(kp, a.ldk, c, w, a.Dk, kf);
-    row_frags<T, NF>(q + (int64_t)hk * a.Dk, a.ldq, c, w, a.Dk, qf);
+    Raw8<T> kf[NS], qf[NS];
+    row_raw<T, NS>(kp, a.ldk, c, w, a.Dk, kf);
+    row_raw<T, NS>(q + (int64_t)hk * a.Dk, a.ldq, c, w, a.Dk, qf);
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
       kk[t] = qk[t] = floatx4{0.f, 0.f, 0.f, 0.f};
       if (t > w || 16 * t >= c.n) continue;
-      floatx4 bf[NF];
-      row_frags<T, NF>(kp, a.ldk, c, t, a.Dk, bf);
+      Raw8<T> bf[NS];
+      row_raw<T, NS>(kp, a.ldk, c, t, a.Dk, bf);
+      Acc x, y;
+      x.clear();
+      y.clear();
 #pragma unroll
-      for (int s = 0; s < NF; ++s) {
-        kk[t] = mma16(kf[s], bf[s], kk[t]);
-        qk[t] = mma16(qf[s], bf[s], qk[t]);
+      for (int s = 0; s < NS; ++s) {
+        const auto b = bf[s].parts();
+        mma32<2>(kf[s].parts(), b, x);
+        mma32<2>(qf[s].parts(), b, y);
       }
+      kk[t] = x.sum();
+      qk[t] = y.sum();
+    }
+  }
+  // K^T as operands over tokens
+  {
+    T* out = kt + ((int64_t)tile * a.Hk + hk) * DKP * kC;
+#pragma unroll
+    for (int f = w; f < DKP / 16 * 2; f += 4) {
+      const int col = 16 * (f >> 1) + li;
+      alignas(16) T v[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int t = 32 * (f & 1) + 16 * (i >> 2) + 4 * lk + (i & 3);
+        v[i] = t < c.n && col < a.Dk ? kp[(c.row + t) * a.ldk + col] : T(0);
+      }
+      Raw8<T> x;
+      x.load(v);
+      *reinterpret_cast<Raw8<T>*>(out + (f * 64 + lane) * 8) = x;
     }
   }
   const int share = a.H / a.Hk;
@@ -353,149 +472,186 @@ __global__ __launch_bounds__(256) void delta_prep_kernel(DeltaIn a, const T* __r
 }
 
 // ---------------------------------------------------------------- the walk over chunks
-// A workgroup per sequence, value head and slice of DVS columns, all matrices transposed: columns are
-// rows, so that a lane's four results are neighbours in memory. Each of four wavefronts has 16 tokens, and
-// DKP / 4 rows of the state, which it keeps in registers; a copy in LDS feeds the products. Three barriers
-// a chunk. SAVE (for the gradients): the states in front of the chunks and U are kept, O is not formed.
-template <typename T, int DKP, int DVS, bool SAVE>
-__global__ __launch_bounds__(256) void delta_chunk_kernel(DeltaIn a, const T* __restrict__ q, const T* __restrict__ k,
-                                                          const T* __restrict__ v, const float* __restrict__ mats,
-                                                          const float* __restrict__ coef, float* state_out,
-                                                          T* __restrict__ o, int64_t ldo, float* __restrict__ s0,
-                                                          float* __restrict__ us) {
-  constexpr int NF = DKP / 16, NT = DKP / 64, MB = DVS / 16, LDS = DKP + 4;
-  __shared__ __attribute__((aligned(16))) float sS[DVS * LDS], sK[kC * LDS], sR[DVS * kLdM], sU[DVS * kLdM];
+// Workgroup b of n heads (of sequences) x parts: neighbours in b go to the eight XCDs in turn, and the slices of a
+// head, which read the same keys and matrices, stay on one.
+__device__ __forceinline__ void head_and_part(int b, int heads, int parts, int& head, int& part) {
+  const int whole = heads / 8 * 8 * parts;
+  if (b < whole) {
+    head = b / (8 * parts) * 8 + b % 8;
+    part = b / 8 % parts;
+  } else {
+    head = (b - whole) / parts + heads / 8 * 8;
+    part = (b - whole) % parts;
+  }
+}
+
+// A workgroup per sequence, value head and slice of 16 columns. Each of four wavefronts has 16 tokens, and
+// DKP / 4 rows of the state, which it keeps in registers; its parts in LDS feed the products, [column][row].
+// Three barriers a chunk, and what the next one reads from memory is asked for as soon as its
+// registers are free. SAVE (for the gradients): the states in front of the chunks and U are kept, O is not formed.
+template <typename T, int DKP, bool SAVE>
+__global__ __launch_bounds__(256, 1) void delta_chunk_kernel(DeltaIn a, const T* __restrict__ q,
+                                                             const T* __restrict__ k, const T* __restrict__ v,
+                                                             const float* __restrict__ mats,
+                                                             const float* __restrict__ coef,
+                                                             const T* __restrict__ kt, float* state_out,
+                                                             T* __restrict__ o, int64_t ldo, float* __restrict__ s0,
+                                                             float* __restrict__ us) {
+  constexpr int NS = DKP / 32, NT = DKP / 64, LS = DKP + 8, LR = kC + 8;
+  constexpr int OP = sizeof(T) == 2 ? 2 : 3;  // parts behind an answer
+  __shared__ __attribute__((aligned(16))) uint16_t sS[3 * 16 * LS], sR[3 * 16 * LR], sW[3 * 16 * LR], sU[3 * 16 * LR];
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, li = lane & 15, lk = lane >> 4;
-  const int parts = (a.Dv + DVS - 1) / DVS;
-  const int c0 = (int)(blockIdx.x % parts) * DVS, h = (int)(blockIdx.x / parts % a.H),
-            seq = (int)(blockIdx.x / parts / a.H), hk = h / (a.H / a.Hk);
+  const int parts = (a.Dv + 15) / 16;
+  int head, part;
+  head_and_part(blockIdx.x, a.n_seq * a.H, parts, head, part);
+  const int c0 = part * 16, h = head % a.H, seq = head / a.H, hk = h / (a.H / a.Hk);
   const int base = min(max(a.offs ? a.offs[seq] : seq, 0), a.rows),
             len = a.offs ? min(max(a.offs[seq + 1], base), a.rows) - base : 1;
   const int key = !a.offs || kC > a.rows ? seq : base / kC + seq;
   const int slot = slot_of(a.slots, a.n_slots, seq);
   const T* kp = k + (int64_t)hk * a.Dk;
   const T* qp = q + (int64_t)hk * a.Dk;
-  const int t = 16 * w + li;  // the lane's token
-  // state entries [c0 + 16 m + 4 lk + r][NT 16 w + 16 n + li]
-  floatx4 st[MB][NT];
-  auto at = [&](int m, int n) { return (int64_t)(16 * (NT * w + n) + li) * a.Dv + c0 + 16 * m + 4 * lk; };
-  auto in = [&](int m, int n) { return 16 * (NT * w + n) + li < a.Dk && c0 + 16 * m + 4 * lk < a.Dv; };
-  const int64_t head = (int64_t)a.Dk * a.Dv;
+  const bool col = c0 + li < a.Dv;  // the lane's column
+  const int64_t size = (int64_t)a.Dk * a.Dv;
+  const int place = token_place(w, lk);
+  // state entries [16 (NT w + n) + 4 lk + r][c0 + li]
+  floatx4 st[NT];
+  auto at = [&](int n) { return (int64_t)(16 * (NT * w + n) + 4 * lk) * a.Dv + c0 + li; };
+  auto in = [&](int n) { return 16 * (NT * w + n) + 4 * lk < a.Dk && col; };
+  auto keep = [&](float* p, int n) {
+    if (in(n))
 #pragma unroll
-  for (int m = 0; m < MB; ++m)
+      for (int r = 0; r < 4; ++r) p[at(n) + (int64_t)r * a.Dv] = st[n][r];
+  };
+  auto share = [&]() {
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      st[m][n] = floatx4{0.f, 0.f, 0.f, 0.f};
-      if (a.state && slot >= 0 && in(m, n))
-        st[m][n] = *reinterpret_cast<const floatx4*>(a.state + ((int64_t)slot * a.H + h) * head + at(m, n));
-    }
+    for (int n = 0; n < NT; ++n) put_parts<3>(sS + li * LS + 16 * (NT * w + n) + 4 * lk, 16 * LS, st[n]);
+  };
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    st[n] = floatx4{0.f, 0.f, 0.f, 0.f};
+    if (a.state && slot >= 0 && in(n))
+#pragma unroll
+      for (int r = 0; r < 4; ++r) st[n][r] = a.state[((int64_t)slot * a.H + h) * size + at(n) + (int64_t)r * a.Dv];
+  }
+  share();
   const int chunks = (len + kC - 1) / kC;
+  auto chunk = [&](int ch) { return Chunk{base + ch * kC, min(kC, len - ch * kC)}; };
+  auto mat = [&](int ch) { return mats + ((int64_t)(key + ch) * a.H + h) * (SAVE ? 3 : 2) * kMat; };
+  Raw8<T> kf[NS], qf[NS], ktf[NT][2];
+  floatx4 tf[4], pf[4], beta, e, wj;
+  float eC;
+  T vv[4];
+  auto load_rows = [&](int ch) {
+    const Chunk c = chunk(ch);
+    row_raw<T, NS>(kp, a.ldk, c, w, a.Dk, kf);
+    if (!SAVE) row_raw<T, NS>(qp, a.ldq, c, w, a.Dk, qf);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      vv[r] = T(0);
+      const int t = 16 * w + 4 * lk + r;
+      if (t < c.n && col) vv[r] = v[(c.row + t) * a.ldv + (int64_t)h * a.Dv + c0 + li];
+    }
+    const float* co = coef + ((int64_t)(key + ch) * a.H + h) * 3 * kC + 16 * w + 4 * lk;
+    beta = *reinterpret_cast<const floatx4*>(co);
+    e = *reinterpret_cast<const floatx4*>(co + kC);
+    wj = *reinterpret_cast<const floatx4*>(co + 2 * kC);
+    eC = coef[((int64_t)(key + ch) * a.H + h) * 3 * kC + 2 * kC - 1];
+  };
+  auto load_mat = [&](const float* m, floatx4* f) {
+#pragma unroll
+    for (int s = 0; s < 4; ++s)
+      if (s <= w) f[s] = mat_frag(m, w, s);
+      else f[s] = floatx4{0.f, 0.f, 0.f, 0.f};
+  };
+  auto load_kt = [&](int ch) {
+    const T* p = kt + ((int64_t)(key + ch) * a.Hk + hk) * DKP * kC + (2 * NT * w * 64 + lane) * 8;
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int s = 0; s < 2; ++s) ktf[n][s] = *reinterpret_cast<const Raw8<T>*>(p + (2 * n + s) * 512);
+  };
+  if (chunks > 0) {
+    load_rows(0);
+    load_mat(mat(0), tf);
+    if (!SAVE) load_mat(mat(0) + kMat, pf);
+    load_kt(0);
+  }
+  __syncthreads();
   for (int ch = 0; ch < chunks; ++ch) {
-    const Chunk c = {base + ch * kC, min(kC, len - ch * kC)};
-    const int64_t th = (int64_t)(key + ch) * a.H + h;
-    const float* mat = mats + th * (SAVE ? 3 : 2) * kMat;
-    const float* co = coef + th * 3 * kC;
+    const Chunk c = chunk(ch);
+    const bool more = ch + 1 < chunks;
+    if (SAVE)
 #pragma unroll
-    for (int m = 0; m < MB; ++m)
+      for (int n = 0; n < NT; ++n) keep(s0 + ((int64_t)(key + ch) * a.H + h) * size, n);
+    Acc ks, qs;
+    ks.clear();
+    qs.clear();
 #pragma unroll
-      for (int n = 0; n < NT; ++n) {
-#pragma unroll
-        for (int r = 0; r < 4; ++r) sS[(16 * m + 4 * lk + r) * LDS + 16 * (NT * w + n) + li] = st[m][n][r];
-        if (SAVE && in(m, n)) *reinterpret_cast<floatx4*>(s0 + th * head + at(m, n)) = st[m][n];
-      }
-    floatx4 kf[NF], qf[NF];
-    row_frags<T, NF>(kp, a.ldk, c, w, a.Dk, kf);
-    if (!SAVE) row_frags<T, NF>(qp, a.ldq, c, w, a.Dk, qf);
-    floatx4 vv[MB];
-    const bool live = t < c.n;
-#pragma unroll
-    for (int m = 0; m < MB; ++m) {
-      vv[m] = floatx4{0.f, 0.f, 0.f, 0.f};
-      if (live && c0 + 16 * m + 4 * lk < a.Dv)
-        vv[m] = ld4(v + (c.row + t) * a.ldv + (int64_t)h * a.Dv + c0 + 16 * m + 4 * lk);
+    for (int s = 0; s < NS; ++s) {
+      const Parts<3> sf = get_parts<3>(sS + li * LS + 32 * s + 8 * lk, 16 * LS);
+      mma32<2>(kf[s].parts(), sf, ks);
+      if (!SAVE) mma32<OP - 1>(qf[s].parts(), sf, qs);
     }
-    const float beta = co[t], e = co[kC + t], wj = co[2 * kC + t], eC = co[2 * kC - 1];
+    const floatx4 ek = e, wk = wj;
+    const float eCk = eC;
+    {
+      const floatx4 x = ks.sum();
+      floatx4 rr;
 #pragma unroll
-    for (int s = 0; s < NF; ++s) *reinterpret_cast<floatx4*>(sK + t * LDS + 16 * s + 4 * lk) = kf[s];
+      for (int r = 0; r < 4; ++r) rr[r] = beta[r] * fmaf(-e[r], x[r], to_f32(vv[r]));
+      put_parts<3>(sR + li * LR + place, 16 * LR, rr);
+    }
+    if (more) load_rows(ch + 1);
     __syncthreads();
-    floatx4 ks[MB], qs[MB];
+    Acc acc;
+    acc.clear();
 #pragma unroll
-    for (int m = 0; m < MB; ++m) {
-      ks[m] = qs[m] = floatx4{0.f, 0.f, 0.f, 0.f};
+    for (int s = 0; s < 2; ++s)
+      if (2 * s <= w)
+        mma32<2>(split8<3>(tf[2 * s], tf[2 * s + 1]), get_parts<3>(sR + li * LR + 32 * s + 8 * lk, 16 * LR), acc);
+    const floatx4 u = acc.sum();
+    put_parts<3>(sW + li * LR + place, 16 * LR, u * wk);
+    if (!SAVE) put_parts<OP>(sU + li * LR + place, 16 * LR, u);
+    if (SAVE && col)
 #pragma unroll
-      for (int s = 0; s < NF; ++s) {
-        const floatx4 sf = frag(sS + 16 * m * LDS, LDS, s);
-        ks[m] = mma16(sf, kf[s], ks[m]);
-        if (!SAVE) qs[m] = mma16(sf, qf[s], qs[m]);
+      for (int r = 0; r < 4; ++r) {
+        const int t = 16 * w + 4 * lk + r;
+        if (t < c.n) us[((int64_t)(c.row + t) * a.H + h) * a.Dv + c0 + li] = u[r];
       }
-#pragma unroll
-      for (int r = 0; r < 4; ++r) sR[(16 * m + 4 * lk + r) * kLdM + t] = beta * fmaf(-e, ks[m][r], vv[m][r]);
-    }
-    __syncthreads();
-    floatx4 u[MB];
-#pragma unroll
-    for (int m = 0; m < MB; ++m) u[m] = floatx4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int s = 0; s < 4; ++s) {
-      const floatx4 tf = mat_frag(mat, w, s);
-#pragma unroll
-      for (int m = 0; m < MB; ++m) u[m] = mma16(frag(sR + 16 * m * kLdM, kLdM, s), tf, u[m]);
-    }
-    if (SAVE && live)
-#pragma unroll
-      for (int m = 0; m < MB; ++m)
-        if (c0 + 16 * m + 4 * lk < a.Dv)
-          *reinterpret_cast<floatx4*>(us + ((int64_t)(c.row + t) * a.H + h) * a.Dv + c0 + 16 * m + 4 * lk) = u[m];
-#pragma unroll
-    for (int m = 0; m < MB; ++m)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) sU[(16 * m + 4 * lk + r) * kLdM + t] = u[m][r];
-    __syncthreads();
-    // w U where R was, by the wavefront that wrote R there: what others read of it is behind the barrier
-#pragma unroll
-    for (int m = 0; m < MB; ++m)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) sR[(16 * m + 4 * lk + r) * kLdM + t] = wj * u[m][r];
-    if (!SAVE) {
-      floatx4 out[MB];
-#pragma unroll
-      for (int m = 0; m < MB; ++m)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) out[m][r] = a.scale * e * qs[m][r];
-#pragma unroll
-      for (int s = 0; s < 4; ++s) {
-        if (s > w) break;  // (P is zero there)
-        const floatx4 pf = mat_frag(mat + kMat, w, s);
-#pragma unroll
-        for (int m = 0; m < MB; ++m) out[m] = mma16(frag(sU + 16 * m * kLdM, kLdM, s), pf, out[m]);
-      }
-      if (live)
-#pragma unroll
-        for (int m = 0; m < MB; ++m)
-          if (c0 + 16 * m + 4 * lk < a.Dv)
-            st4(o + (c.row + t) * ldo + (int64_t)h * a.Dv + c0 + 16 * m + 4 * lk, out[m]);
-    }
+    if (more) load_mat(mat(ch + 1), tf);
     __syncthreads();
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
+      acc.clear();
 #pragma unroll
-      for (int m = 0; m < MB; ++m) st[m][n] *= eC;
+      for (int s = 0; s < 2; ++s)
+        mma32<2>(ktf[n][s].parts(), get_parts<3>(sW + li * LR + 32 * s + 8 * lk, 16 * LR), acc);
+      st[n] = st[n] * eCk + acc.sum();
+    }
+    share();
+    if (more) load_kt(ch + 1);
+    if (!SAVE) {
+      acc.clear();
 #pragma unroll
-      for (int s = 0; s < 4; ++s) {
-        const floatx4 kt = frag_t(sK + 16 * (NT * w + n), LDS, s);
+      for (int s = 0; s < 2; ++s)
+        if (2 * s <= w)
+          mma32<OP - 1>(split8<OP>(pf[2 * s], pf[2 * s + 1]),
+                        get_parts<OP>(sU + li * LR + 32 * s + 8 * lk, 16 * LR), acc);
+      if (more) load_mat(mat(ch + 1) + kMat, pf);
+      const floatx4 x = qs.sum(), y = acc.sum();
+      if (col)
 #pragma unroll
-        for (int m = 0; m < MB; ++m) st[m][n] = mma16(frag(sR + 16 * m * kLdM, kLdM, s), kt, st[m][n]);
-      }
+        for (int r = 0; r < 4; ++r) {
+          const int t = 16 * w + 4 * lk + r;
+          if (t < c.n) st1(o + (c.row + t) * ldo + (int64_t)h * a.Dv + c0 + li, fmaf(a.scale * ek[r], x[r], y[r]));
+        }
     }
     __syncthreads();
   }
   if (!SAVE && state_out && slot >= 0)
 #pragma unroll
-    for (int m = 0; m < MB; ++m)
-#pragma unroll
-      for (int n = 0; n < NT; ++n)
-        if (in(m, n))
-          *reinterpret_cast<floatx4*>(state_out + ((int64_t)slot * a.H + h) * head + at(m, n)) = st[m][n];
+    for (int n = 0; n < NT; ++n) keep(state_out + ((int64_t)slot * a.H + h) * size, n);
 }
 
 // ---------------------------------------------------------------- gradients
@@ -916,16 +1072,22 @@ hipError_t chunks(const DeltaOp& a, float* state_out, void* o, int64_t ldo, floa
   float* coef = ws;
   float* mats = ws + tiles * a.H * 3 * kC;
   const T *q = static_cast<const T*>(a.q), *k = static_cast<const T*>(a.k), *v = static_cast<const T*>(a.v);
-  delta_prep_kernel<T, DKP, false><<<dim3((unsigned)(tiles * a.Hk)), 256, 0, s>>>(in_of(a), q, k, mats, coef);
-  delta_chunk_kernel<T, DKP, 16, false><<<dim3((unsigned)((int64_t)a.n_seq * a.H * ((a.Dv + 15) / 16))), 256, 0, s>>>(
-      in_of(a), q, k, v, mats, coef, state_out, static_cast<T*>(o), ldo, nullptr, nullptr);
+  T* kt = reinterpret_cast<T*>(mats + tiles * a.H * 2 * kMat);
+  delta_prep_kernel<T, DKP, false><<<dim3((unsigned)(tiles * a.Hk)), 256, 0, s>>>(in_of(a), q, k, mats, coef, kt);
+  delta_chunk_kernel<T, DKP, false><<<dim3((unsigned)((int64_t)a.n_seq * a.H * ((a.Dv + 15) / 16))), 256, 0, s>>>(
+      in_of(a), q, k, v, mats, coef, kt, state_out, static_cast<T*>(o), ldo, nullptr, nullptr);
   return hipGetLastError();
+}
+
+// K^T of every chunk and key head, in floats.
+int64_t kt_floats(bool bf16, int n_seq, int rows, int Hk, int Dk) {
+  return tiles_of(n_seq, rows) * Hk * (Dk <= 64 ? 64 : 128) * kC / (bf16 ? 2 : 1);
 }
 
 // The parts of the gradients' workspace, in floats.
 struct BackSpace {
-  int64_t coef, mats, s0, ds1, us, drs, end;
-  BackSpace(int n_seq, int rows, int H, int Dk, int Dv) {
+  int64_t coef, mats, s0, ds1, us, drs, kt, end;
+  BackSpace(bool bf16, int n_seq, int rows, int Hk, int H, int Dk, int Dv) {
     const int64_t th = tiles_of(n_seq, rows) * H, head = (int64_t)Dk * Dv, act = (int64_t)rows * H * Dv;
     coef = 0;
     mats = coef + th * 3 * kC;
@@ -933,7 +1095,8 @@ struct BackSpace {
     ds1 = s0 + th * head;
     us = ds1 + th * head;
     drs = us + act;
-    end = drs + act;
+    kt = drs + act;
+    end = kt + kt_floats(bf16, n_seq, rows, Hk, Dk);
   }
 };
 
@@ -941,14 +1104,15 @@ template <typename T, int DKP>
 hipError_t grads(const DeltaOp& a, const void* d_o_, int64_t lddo, const float* dstate_out, const DeltaGrads& g,
                  float* ws, hipStream_t s) {
   const int64_t tiles = tiles_of(a.n_seq, a.rows);
-  const BackSpace b(a.n_seq, a.rows, a.H, a.Dk, a.Dv);
+  const BackSpace b(a.bf16, a.n_seq, a.rows, a.Hk, a.H, a.Dk, a.Dv);
+  T* kt = reinterpret_cast<T*>(ws + b.kt);
   const T *q = static_cast<const T*>(a.q), *k = static_cast<const T*>(a.k), *v = static_cast<const T*>(a.v);
   const T* d_o = static_cast<const T*>(d_o_);
   const DeltaIn in = in_of(a);
   const dim3 flat((unsigned)(tiles * a.Hk)), slices((unsigned)((int64_t)a.n_seq * a.H * ((a.Dv + 15) / 16)));
-  delta_prep_kernel<T, DKP, true><<<flat, 256, 0, s>>>(in, q, k, ws + b.mats, ws + b.coef);
-  delta_chunk_kernel<T, DKP, 16, true><<<slices, 256, 0, s>>>(in, q, k, v, ws + b.mats, ws + b.coef, nullptr, nullptr,
-                                                              0, ws + b.s0, ws + b.us);
+  delta_prep_kernel<T, DKP, true><<<flat, 256, 0, s>>>(in, q, k, ws + b.mats, ws + b.coef, kt);
+  delta_chunk_kernel<T, DKP, true><<<slices, 256, 0, s>>>(in, q, k, v, ws + b.mats, ws + b.coef, kt, nullptr, nullptr, 0,
+                                                          ws + b.s0, ws + b.us);
   delta_back_kernel<T, DKP, 16><<<slices, 256, 0, s>>>(in, q, k, d_o, lddo, ws + b.mats, ws + b.coef, dstate_out,
                                                        g.dstate, static_cast<T*>(g.dv), g.lddv, ws + b.ds1, ws + b.drs);
   delta_grads_kernel<T, DKP><<<flat, 256, 0, s>>>(in, q, k, v, d_o, lddo, ws + b.coef, ws + b.s0, ws + b.ds1, ws + b.us,
@@ -960,9 +1124,9 @@ hipError_t grads(const DeltaOp& a, const void* d_o_, int64_t lddo, const float* 
 }  // namespace
 
 size_t delta_rule_workspace_bytes(bool bf16, int n_seq, int rows, int Hk, int H, int Dk, int Dv) {
-  (void)bf16; (void)Hk; (void)Dk; (void)Dv;
+  (void)Dv;
   if (!chunked(n_seq, rows)) return 0;
-  return (size_t)(tiles_of(n_seq, rows) * H * (3 * kC + 2 * kMat)) * sizeof(float);
+  return (size_t)(tiles_of(n_seq, rows) * H * (3 * kC + 2 * kMat) + kt_floats(bf16, n_seq, rows, Hk, Dk)) * sizeof(float);
 }
 
 hipError_t launch_delta_rule(const DeltaOp& a, float* state_out, void* o, int64_t ldo, float* ws, hipStream_t s) {
@@ -974,8 +1138,7 @@ hipError_t launch_delta_rule(const DeltaOp& a, float* state_out, void* o, int64_
 }
 
 size_t delta_rule_bwd_workspace_bytes(bool bf16, int n_seq, int rows, int Hk, int H, int Dk, int Dv) {
-  (void)bf16; (void)Hk;
-  return (size_t)BackSpace(n_seq, rows, H, Dk, Dv).end * sizeof(float);
+  return (size_t)BackSpace(bf16, n_seq, rows, Hk, H, Dk, Dv).end * sizeof(float);
 }
 
 hipError_t launch_delta_rule_bwd(const DeltaOp& a, const void* d_o, int64_t lddo, const float* dstate_out,
