@@ -25,7 +25,14 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kC = 64;        // tokens of a chunk
-constexpr int kMat = kC * kC;  // entries of T or P
+constexpr int kMat = kC * kC;        // entries of T or P
+constexpr int kTParts = kMat / 2 * 3;  // floats that T's three bf16 parts take
+// Parts behind an answer: bf16 does not show what two leave out (2^-16).
+template <typename T>
+constexpr int kOutParts = sizeof(T) == 2 ? 2 : 3;
+// Floats of a chunk's matrices: T and P in parts, or for the gradients T in parts, T^T and P^T.
+template <typename T, bool GRADS>
+constexpr int kMats = GRADS ? kTParts + 2 * kMat : kTParts + kMat / 2 * kOutParts<T>;
 
 __device__ __forceinline__ float to_f32(float v) { return v; }
 __device__ __forceinline__ float to_f32(uint16_t v) { return bf16_to_f32(v); }
@@ -270,10 +277,43 @@ template <> struct Raw8<float> {
   __device__ __forceinline__ void clear() { a = b = floatx4{0.f, 0.f, 0.f, 0.f}; }
   __device__ __forceinline__ Parts<3> parts() const { return split8<3>(a, b); }
 };
+// One entry, a register of its own: two halves of one would make the second load wait for the first.
+template <typename T> struct Raw1;
+template <> struct Raw1<float> {
+  typedef float type;
+  static __device__ __forceinline__ float load(const float* p) { return *p; }
+  static __device__ __forceinline__ float value(float x) { return x; }
+};
+template <> struct Raw1<uint16_t> {
+  typedef uint32_t type;
+  static __device__ __forceinline__ uint32_t load(const uint16_t* p) {
+    return *p;
+  }
+  static __device__ __forceinline__ float value(uint32_t x) { return __uint_as_float(x << 16); }
+};
 // In products over tokens, the eight of lane group kq of the 32 from 32 s on: 32 s + 16 a + 4 kq + m at
-// place 4 a + m. So the four tokens of a lane's results are neighbours in LDS, and two fragments of a
-// matrix (mat_frag) are one operand. Where token t = 16 w + 4 lk stands:
+// place 4 a + m. So the four tokens of a lane's results are neighbours in LDS, and two fragments (frag) of a
+// matrix are one operand. Where token t = 16 w + 4 lk stands:
 __device__ __forceinline__ int token_place(int w, int lk) { return 32 * (w >> 1) + 8 * lk + 4 * (w & 1); }
+// A triangular matrix [kC, kC] as operands over tokens in N parts: of the 16 rows 16 w .., tokens 32 s ... (What is
+// zero is not read, but an address is given for it too: a branch would hide from the compiler how many loads are
+// under way, and it would wait for all.)
+template <int N>
+__device__ __forceinline__ Parts<N> mat_parts(const uint16_t* m, int w, int s) {
+  Parts<N> r;
+#pragma unroll
+  for (int p = 0; p < N; ++p)
+    r.p[p] = pack8(*reinterpret_cast<const u32x4*>(m + (((w * 2 + s) * N + p) * 64 + (threadIdx.x & 63)) * 8));
+  return r;
+}
+template <int N>
+__device__ __forceinline__ void put_mat(uint16_t* m, int w, int s, floatx4 a, floatx4 b) {
+  const Parts<N> v = split8<N>(a, b);
+#pragma unroll
+  for (int p = 0; p < N; ++p)
+    *reinterpret_cast<u32x4*>(m + (((w * 2 + s) * N + p) * 64 + (threadIdx.x & 63)) * 8) =
+        __builtin_bit_cast(u32x4, v.p[p]);
+}
 
 // A chunk of a sequence: its first row and how many tokens it has.
 struct Chunk {
@@ -371,7 +411,7 @@ __global__ __launch_bounds__(256) void delta_prep_kernel(DeltaIn a, const T* __r
   const int share = a.H / a.Hk;
   for (int hv = 0; hv < share; ++hv) {
     const int h = hk * share + hv;
-    float* out = mats + ((int64_t)tile * a.H + h) * (GRADS ? 3 : 2) * kMat;
+    float* out = mats + ((int64_t)tile * a.H + h) * kMats<T, GRADS>;
     float* co = coef + ((int64_t)tile * a.H + h) * 3 * kC;
     __syncthreads();
     if (tid < kC) {
@@ -457,16 +497,22 @@ __global__ __launch_bounds__(256) void delta_prep_kernel(DeltaIn a, const T* __r
 #pragma unroll
       for (int r = 0; r < 4; ++r) sA[(16 * w + 4 * lk + r) * kLdM + 16 * t + li] = pm[t][r];
     __syncthreads();
+    uint16_t* tp = reinterpret_cast<uint16_t*>(out);
+    if constexpr (GRADS) {
 #pragma unroll
-    for (int s = 0; s < 4; ++s) {
-      float* p = out + ((w * 4 + s) * 64 + lane) * 4;
-      *reinterpret_cast<floatx4*>(p) = frag(sT + 16 * w * kLdM, kLdM, s);
-      if constexpr (GRADS) {
-        *reinterpret_cast<floatx4*>(p + kMat) = frag_t(sT + 16 * w, kLdM, s);
-        *reinterpret_cast<floatx4*>(p + 2 * kMat) = frag_t(sA + 16 * w, kLdM, s);
-      } else {
-        *reinterpret_cast<floatx4*>(p + kMat) = frag(sA + 16 * w * kLdM, kLdM, s);
+      for (int s = 0; s < 4; ++s) {
+        float* p = out + kTParts + ((w * 4 + s) * 64 + lane) * 4;
+        *reinterpret_cast<floatx4*>(p) = frag_t(sT + 16 * w, kLdM, s);
+        *reinterpret_cast<floatx4*>(p + kMat) = frag_t(sA + 16 * w, kLdM, s);
       }
+    }
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      if (2 * s > w) continue;
+      put_mat<3>(tp, w, s, frag(sT + 16 * w * kLdM, kLdM, 2 * s), frag(sT + 16 * w * kLdM, kLdM, 2 * s + 1));
+      if constexpr (!GRADS)
+        put_mat<kOutParts<T>>(tp + 2 * kTParts, w, s, frag(sA + 16 * w * kLdM, kLdM, 2 * s),
+                              frag(sA + 16 * w * kLdM, kLdM, 2 * s + 1));
     }
   }
 }
@@ -490,7 +536,7 @@ __device__ __forceinline__ void head_and_part(int b, int heads, int parts, int& 
 // Three barriers a chunk, and what the next one reads from memory is asked for as soon as its
 // registers are free. SAVE (for the gradients): the states in front of the chunks and U are kept, O is not formed.
 template <typename T, int DKP, bool SAVE>
-__global__ __launch_bounds__(256, 1) void delta_chunk_kernel(DeltaIn a, const T* __restrict__ q,
+__global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void delta_chunk_kernel(DeltaIn a, const T* __restrict__ q,
                                                              const T* __restrict__ k, const T* __restrict__ v,
                                                              const float* __restrict__ mats,
                                                              const float* __restrict__ coef,
@@ -498,7 +544,7 @@ __global__ __launch_bounds__(256, 1) void delta_chunk_kernel(DeltaIn a, const T*
                                                              T* __restrict__ o, int64_t ldo, float* __restrict__ s0,
                                                              float* __restrict__ us) {
   constexpr int NS = DKP / 32, NT = DKP / 64, LS = DKP + 8, LR = kC + 8;
-  constexpr int OP = sizeof(T) == 2 ? 2 : 3;  // parts behind an answer
+  constexpr int OP = kOutParts<T>;
   __shared__ __attribute__((aligned(16))) uint16_t sS[3 * 16 * LS], sR[3 * 16 * LR], sW[3 * 16 * LR], sU[3 * 16 * LR];
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, li = lane & 15, lk = lane >> 4;
   const int parts = (a.Dv + 15) / 16;
@@ -537,50 +583,71 @@ __global__ __launch_bounds__(256, 1) void delta_chunk_kernel(DeltaIn a, const T*
   share();
   const int chunks = (len + kC - 1) / kC;
   auto chunk = [&](int ch) { return Chunk{base + ch * kC, min(kC, len - ch * kC)}; };
-  auto mat = [&](int ch) { return mats + ((int64_t)(key + ch) * a.H + h) * (SAVE ? 3 : 2) * kMat; };
+  auto mat = [&](int ch) {
+    return reinterpret_cast<const uint16_t*>(mats + ((int64_t)(key + ch) * a.H + h) * kMats<T, SAVE>);
+  };
   Raw8<T> kf[NS], qf[NS], ktf[NT][2];
-  floatx4 tf[4], pf[4], beta, e, wj;
+  Parts<3> tf[2];
+  Parts<OP> pf[2];
+  floatx4 beta, e, wj;
   float eC;
-  T vv[4];
+  typename Raw1<T>::type vv[4];
+  // Rows past a chunk's end are read as its last one, and columns past a row's end as its last ones: what
+  // they give meets zeros (beta, K^T, the states' rows).
+  const int ldk = (int)a.ldk, ldq = (int)a.ldq, ldv = (int)a.ldv, cv = min(c0 + li, a.Dv - 1);
+  int colk[NS];
+#pragma unroll
+  for (int s = 0; s < NS; ++s) colk[s] = min(32 * s + 8 * lk, a.Dk - 8);
   auto load_rows = [&](int ch) {
     const Chunk c = chunk(ch);
-    row_raw<T, NS>(kp, a.ldk, c, w, a.Dk, kf);
-    if (!SAVE) row_raw<T, NS>(qp, a.ldq, c, w, a.Dk, qf);
+    const T* kr = kp + c.row * a.ldk;
+    const T* qr = qp + c.row * a.ldq;
+    const int t = min(16 * w + li, c.n - 1);
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      vv[r] = T(0);
-      const int t = 16 * w + 4 * lk + r;
-      if (t < c.n && col) vv[r] = v[(c.row + t) * a.ldv + (int64_t)h * a.Dv + c0 + li];
-    }
-    const float* co = coef + ((int64_t)(key + ch) * a.H + h) * 3 * kC + 16 * w + 4 * lk;
-    beta = *reinterpret_cast<const floatx4*>(co);
-    e = *reinterpret_cast<const floatx4*>(co + kC);
-    wj = *reinterpret_cast<const floatx4*>(co + 2 * kC);
-    eC = coef[((int64_t)(key + ch) * a.H + h) * 3 * kC + 2 * kC - 1];
+    for (int s = 0; s < NS; ++s) kf[s].load(kr + (uint32_t)(t * ldk + colk[s]));
+    if (!SAVE)
+#pragma unroll
+      for (int s = 0; s < NS; ++s) qf[s].load(qr + (uint32_t)(t * ldq + colk[s]));
   };
-  auto load_mat = [&](const float* m, floatx4* f) {
+  auto load_v = [&](int ch) {
+    const Chunk c = chunk(ch);
+    const T* vr = v + c.row * a.ldv + (int64_t)h * a.Dv;
 #pragma unroll
-    for (int s = 0; s < 4; ++s)
-      if (s <= w) f[s] = mat_frag(m, w, s);
-      else f[s] = floatx4{0.f, 0.f, 0.f, 0.f};
+    for (int r = 0; r < 4; ++r) vv[r] = Raw1<T>::load(vr + (uint32_t)(min(16 * w + 4 * lk + r, c.n - 1) * ldv + cv));
+    const float* co = coef + ((int64_t)(key + ch) * a.H + h) * 3 * kC;
+    beta = *reinterpret_cast<const floatx4*>(co + 16 * w + 4 * lk);
+    e = *reinterpret_cast<const floatx4*>(co + kC + 16 * w + 4 * lk);
+    wj = *reinterpret_cast<const floatx4*>(co + 2 * kC + 16 * w + 4 * lk);
+    eC = co[2 * kC - 1];
+  };
+  const int s1 = w >> 1;  // the last 32 tokens that the wavefront's rows of T and P reach
+  auto load_t = [&](int ch) {
+    tf[0] = mat_parts<3>(mat(ch), w, 0);
+    tf[1] = mat_parts<3>(mat(ch), w, s1);
+  };
+  auto load_p = [&](int ch) {
+    pf[0] = mat_parts<OP>(mat(ch) + 2 * kTParts, w, 0);
+    pf[1] = mat_parts<OP>(mat(ch) + 2 * kTParts, w, s1);
   };
   auto load_kt = [&](int ch) {
-    const T* p = kt + ((int64_t)(key + ch) * a.Hk + hk) * DKP * kC + (2 * NT * w * 64 + lane) * 8;
+    const T* p = kt + ((int64_t)(key + ch) * a.Hk + hk) * DKP * kC;
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
-      for (int s = 0; s < 2; ++s) ktf[n][s] = *reinterpret_cast<const Raw8<T>*>(p + (2 * n + s) * 512);
+      for (int s = 0; s < 2; ++s)
+        ktf[n][s] = *reinterpret_cast<const Raw8<T>*>(p + (uint32_t)(((2 * NT * w + 2 * n + s) * 64 + lane) * 8));
   };
   if (chunks > 0) {
     load_rows(0);
-    load_mat(mat(0), tf);
-    if (!SAVE) load_mat(mat(0) + kMat, pf);
+    load_v(0);
+    load_t(0);
     load_kt(0);
+    if (!SAVE) load_p(0);
   }
   __syncthreads();
   for (int ch = 0; ch < chunks; ++ch) {
     const Chunk c = chunk(ch);
-    const bool more = ch + 1 < chunks;
+    const int next = min(ch + 1, chunks - 1);  // (the last chunk's are read again: see mat_parts)
     if (SAVE)
 #pragma unroll
       for (int n = 0; n < NT; ++n) keep(s0 + ((int64_t)(key + ch) * a.H + h) * size, n);
@@ -593,25 +660,23 @@ __global__ __launch_bounds__(256, 1) void delta_chunk_kernel(DeltaIn a, const T*
       mma32<2>(kf[s].parts(), sf, ks);
       if (!SAVE) mma32<OP - 1>(qf[s].parts(), sf, qs);
     }
-    const floatx4 ek = e, wk = wj;
-    const float eCk = eC;
     {
       const floatx4 x = ks.sum();
       floatx4 rr;
 #pragma unroll
-      for (int r = 0; r < 4; ++r) rr[r] = beta[r] * fmaf(-e[r], x[r], to_f32(vv[r]));
+      for (int r = 0; r < 4; ++r) rr[r] = beta[r] * fmaf(-e[r], x[r], Raw1<T>::value(vv[r]));
       put_parts<3>(sR + li * LR + place, 16 * LR, rr);
     }
-    if (more) load_rows(ch + 1);
+    load_rows(next);
     __syncthreads();
     Acc acc;
     acc.clear();
 #pragma unroll
     for (int s = 0; s < 2; ++s)
-      if (2 * s <= w)
-        mma32<2>(split8<3>(tf[2 * s], tf[2 * s + 1]), get_parts<3>(sR + li * LR + 32 * s + 8 * lk, 16 * LR), acc);
+      if (s <= s1) mma32<2>(tf[s], get_parts<3>(sR + li * LR + 32 * s + 8 * lk, 16 * LR), acc);
+    load_t(next);
     const floatx4 u = acc.sum();
-    put_parts<3>(sW + li * LR + place, 16 * LR, u * wk);
+    put_parts<3>(sW + li * LR + place, 16 * LR, u * wj);
     if (!SAVE) put_parts<OP>(sU + li * LR + place, 16 * LR, u);
     if (SAVE && col)
 #pragma unroll
@@ -619,7 +684,6 @@ __global__ __launch_bounds__(256, 1) void delta_chunk_kernel(DeltaIn a, const T*
         const int t = 16 * w + 4 * lk + r;
         if (t < c.n) us[((int64_t)(c.row + t) * a.H + h) * a.Dv + c0 + li] = u[r];
       }
-    if (more) load_mat(mat(ch + 1), tf);
     __syncthreads();
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
@@ -627,25 +691,29 @@ __global__ __launch_bounds__(256, 1) void delta_chunk_kernel(DeltaIn a, const T*
 #pragma unroll
       for (int s = 0; s < 2; ++s)
         mma32<2>(ktf[n][s].parts(), get_parts<3>(sW + li * LR + 32 * s + 8 * lk, 16 * LR), acc);
-      st[n] = st[n] * eCk + acc.sum();
+      st[n] = st[n] * eC + acc.sum();
     }
     share();
-    if (more) load_kt(ch + 1);
+    load_kt(next);
+    floatx4 out;
     if (!SAVE) {
       acc.clear();
 #pragma unroll
       for (int s = 0; s < 2; ++s)
-        if (2 * s <= w)
-          mma32<OP - 1>(split8<OP>(pf[2 * s], pf[2 * s + 1]),
-                        get_parts<OP>(sU + li * LR + 32 * s + 8 * lk, 16 * LR), acc);
-      if (more) load_mat(mat(ch + 1) + kMat, pf);
+        if (s <= s1) mma32<OP - 1>(pf[s], get_parts<OP>(sU + li * LR + 32 * s + 8 * lk, 16 * LR), acc);
+      load_p(next);
       const floatx4 x = qs.sum(), y = acc.sum();
-      if (col)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int t = 16 * w + 4 * lk + r;
-          if (t < c.n) st1(o + (c.row + t) * ldo + (int64_t)h * a.Dv + c0 + li, fmaf(a.scale * ek[r], x[r], y[r]));
-        }
+      for (int r = 0; r < 4; ++r) out[r] = fmaf(a.scale * e[r], x[r], y[r]);
+    }
+    load_v(next);
+    if (!SAVE && col) {
+      T* orow = o + c.row * ldo + (int64_t)h * a.Dv;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int t = 16 * w + 4 * lk + r;
+        if (t < c.n) st1(orow + (uint32_t)(t * (int)ldo + cv), out[r]);
+      }
     }
     __syncthreads();
   }
@@ -703,7 +771,7 @@ __global__ __launch_bounds__(256) void delta_back_kernel(DeltaIn a, const T* __r
   for (int ch = (len + kC - 1) / kC - 1; ch >= 0; --ch) {
     const Chunk c = {base + ch * kC, min(kC, len - ch * kC)};
     const int64_t th = (int64_t)(key + ch) * a.H + h;
-    const float* mat = mats + th * 3 * kMat;
+    const float* mat = mats + th * kMats<T, true> + kTParts;  // T^T, P^T
     const float* co = coef + th * 3 * kC;
 #pragma unroll
     for (int m = 0; m < MB; ++m)
@@ -743,7 +811,7 @@ __global__ __launch_bounds__(256) void delta_back_kernel(DeltaIn a, const T* __r
     }
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
-      const floatx4 pf = mat_frag(mat + 2 * kMat, w, s);
+      const floatx4 pf = mat_frag(mat + kMat, w, s);
 #pragma unroll
       for (int m = 0; m < MB; ++m) du[m] = mma16(frag(sO + 16 * m * kLdM, kLdM, s), pf, du[m]);
     }
@@ -757,7 +825,7 @@ __global__ __launch_bounds__(256) void delta_back_kernel(DeltaIn a, const T* __r
     for (int m = 0; m < MB; ++m) dr[m] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
-      const floatx4 tf = mat_frag(mat + kMat, w, s);
+      const floatx4 tf = mat_frag(mat, w, s);
 #pragma unroll
       for (int m = 0; m < MB; ++m) dr[m] = mma16(frag(sU + 16 * m * kLdM, kLdM, s), tf, dr[m]);
     }
@@ -1072,7 +1140,7 @@ hipError_t chunks(const DeltaOp& a, float* state_out, void* o, int64_t ldo, floa
   float* coef = ws;
   float* mats = ws + tiles * a.H * 3 * kC;
   const T *q = static_cast<const T*>(a.q), *k = static_cast<const T*>(a.k), *v = static_cast<const T*>(a.v);
-  T* kt = reinterpret_cast<T*>(mats + tiles * a.H * 2 * kMat);
+  T* kt = reinterpret_cast<T*>(mats + tiles * a.H * kMats<T, false>);
   delta_prep_kernel<T, DKP, false><<<dim3((unsigned)(tiles * a.Hk)), 256, 0, s>>>(in_of(a), q, k, mats, coef, kt);
   delta_chunk_kernel<T, DKP, false><<<dim3((unsigned)((int64_t)a.n_seq * a.H * ((a.Dv + 15) / 16))), 256, 0, s>>>(
       in_of(a), q, k, v, mats, coef, kt, state_out, static_cast<T*>(o), ldo, nullptr, nullptr);
@@ -1091,7 +1159,7 @@ struct BackSpace {
     const int64_t th = tiles_of(n_seq, rows) * H, head = (int64_t)Dk * Dv, act = (int64_t)rows * H * Dv;
     coef = 0;
     mats = coef + th * 3 * kC;
-    s0 = mats + th * 3 * kMat;
+    s0 = mats + th * kMats<float, true>;
     ds1 = s0 + th * head;
     us = ds1 + th * head;
     drs = us + act;
@@ -1126,7 +1194,8 @@ hipError_t grads(const DeltaOp& a, const void* d_o_, int64_t lddo, const float* 
 size_t delta_rule_workspace_bytes(bool bf16, int n_seq, int rows, int Hk, int H, int Dk, int Dv) {
   (void)Dv;
   if (!chunked(n_seq, rows)) return 0;
-  return (size_t)(tiles_of(n_seq, rows) * H * (3 * kC + 2 * kMat) + kt_floats(bf16, n_seq, rows, Hk, Dk)) * sizeof(float);
+  const int mats = bf16 ? kMats<uint16_t, false> : kMats<float, false>;
+  return (size_t)(tiles_of(n_seq, rows) * H * (3 * kC + mats) + kt_floats(bf16, n_seq, rows, Hk, Dk)) * sizeof(float);
 }
 
 hipError_t launch_delta_rule(const DeltaOp& a, float* state_out, void* o, int64_t ldo, float* ws, hipStream_t s) {

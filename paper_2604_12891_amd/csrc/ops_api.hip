@@ -306,6 +306,8 @@ namespace {
 // Fewer than 2^32 threads a launch: a sequence's head takes 16 workgroups of 256 at most, a chunk's (64 rows, or the rest
 // of a sequence) one.
 constexpr int kMaxHeads = 1024, kMaxDk = 128, kMaxDv = 256;
+// (a chunk's rows are addressed in 31 bits)
+constexpr int64_t kMaxLd = (int64_t)1 << 22;
 
 bool delta_sizes(int32_t n_seq, int32_t rows, int32_t Hk, int32_t H, int32_t Dk, int32_t Dv) {
   return n_seq >= 0 && rows >= 0 && n_seq <= kMaxRows && rows <= kMaxRows && Hk >= 1 && H >= Hk && H <= kMaxHeads &&
@@ -331,6 +333,8 @@ tcl_status delta_op(const tcl_delta_rule_args* a, DeltaOp* op) {
   const int64_t qk = (int64_t)a->Hk * a->Dk, v = (int64_t)a->H * a->Dv;
   if (a->ldq < qk || a->ldk < qk || a->ldv < v || a->ldg < a->H || a->ldbeta < a->H)
     return fail(TCL_ERR_INVALID_ARG, "leading dimension smaller than the row");
+  if (a->ldq > kMaxLd || a->ldk > kMaxLd || a->ldv > kMaxLd)
+    return fail(TCL_ERR_UNSUPPORTED, "leading dimensions must be at most %lld", (long long)kMaxLd);
   if (a->rows > 0 && (!a->d_q || !a->d_k || !a->d_v || !a->d_g || !a->d_beta))
     return fail(TCL_ERR_INVALID_ARG, "NULL device pointer");
   const uintptr_t el = a->dtype == TCL_BF16 ? 2 : 4;
@@ -361,6 +365,7 @@ TCL_API tcl_status tcl_delta_rule(const tcl_delta_rule_args* args, const int32_t
   if (tcl_status st = delta_op(args, &op)) return st;
   if (tcl_status st = check_slots(d_slots, n_slots, op.n_seq, op.state || d_state_out)) return st;
   if (ldo < (int64_t)op.H * op.Dv) return fail(TCL_ERR_INVALID_ARG, "leading dimension smaller than the row");
+  if (ldo > kMaxLd) return fail(TCL_ERR_UNSUPPORTED, "leading dimensions must be at most %lld", (long long)kMaxLd);
   if (!d_o && op.rows > 0) return fail(TCL_ERR_INVALID_ARG, "NULL device pointer");
   if (misaligned(d_o, op.bf16 ? 2 : 4)) return fail(TCL_ERR_INVALID_ARG, "o is not aligned to its type");
   if (misaligned(d_state_out, 16)) return fail(TCL_ERR_INVALID_ARG, "the states must be 16-byte aligned");
@@ -390,6 +395,8 @@ TCL_API tcl_status tcl_delta_rule_backward(const tcl_delta_rule_args* args, cons
   const int64_t qk = (int64_t)op.Hk * op.Dk, v = (int64_t)op.H * op.Dv;
   if (lddo < v || g->lddq < qk || g->lddk < qk || g->lddv < v || g->lddg < op.H || g->lddbeta < op.H)
     return fail(TCL_ERR_INVALID_ARG, "leading dimension smaller than the row");
+  if (lddo > kMaxLd || g->lddq > kMaxLd || g->lddk > kMaxLd || g->lddv > kMaxLd)
+    return fail(TCL_ERR_UNSUPPORTED, "leading dimensions must be at most %lld", (long long)kMaxLd);
   if (op.rows > 0 && (!d_do || !g->d_dq || !g->d_dk || !g->d_dv || !g->d_dg || !g->d_dbeta))
     return fail(TCL_ERR_INVALID_ARG, "NULL device pointer");
   const uintptr_t el = op.bf16 ? 2 : 4;
