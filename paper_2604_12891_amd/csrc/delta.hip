@@ -13,6 +13,7 @@
 // G is summed and subtracted in 64 bits and its exponentials are taken of the differences: with g down to
 // -inf, e^G_i / e^G_j would be 0 / 0 where D_ij is 1. A decay below e^-10000 counts as that.
 #include <algorithm>
+#include <type_traits>
 
 #include "common.h"
 #include "ops.h"
@@ -173,6 +174,13 @@ __global__ __launch_bounds__(64) void delta_walk_kernel(DeltaIn a, const T* __re
 #pragma unroll
     for (int i = 0; i < RK; ++i)
       if (r0 + i < a.Dk) *reinterpret_cast<floatx4*>(state_out + at + (int64_t)i * a.Dv) = s[i];
+}
+
+// A barrier behind which what the workgroup has written to LDS is seen; loads from memory stay under way.
+__device__ __forceinline__ void sync_lds() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
 // ---------------------------------------------------------------- matrix products
@@ -531,22 +539,23 @@ __device__ __forceinline__ void head_and_part(int b, int heads, int parts, int& 
   }
 }
 
-// A workgroup per sequence, value head and slice of 16 columns. Each of four wavefronts has 16 tokens, and
-// DKP / 4 rows of the state, which it keeps in registers; its parts in LDS feed the products, [column][row].
-// Three barriers a chunk, and what the next one reads from memory is asked for as soon as its
-// registers are free. SAVE (for the gradients): the states in front of the chunks and U are kept, O is not formed.
+// A workgroup per sequence, value head and slice of 16 columns. The parts of the state in LDS, [column][row],
+// feed the products; the state itself stays in registers, tiles of 16 rows to a wavefront. Four wavefronts of 16
+// tokens each form R, U and what goes into the state (K S0, T R), the chain that a chunk waits for; four more
+// the answers (Q S0, P U), so that each SIMD has two to issue from. Three barriers a chunk; what the
+// next one reads from memory is asked for as soon as its registers are free. SAVE (for the gradients): the states in
+// front of the chunks and U are kept, no answers are formed, by the first four alone.
 template <typename T, int DKP, bool SAVE>
-__global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void delta_chunk_kernel(DeltaIn a, const T* __restrict__ q,
-                                                             const T* __restrict__ k, const T* __restrict__ v,
-                                                             const float* __restrict__ mats,
-                                                             const float* __restrict__ coef,
-                                                             const T* __restrict__ kt, float* state_out,
-                                                             T* __restrict__ o, int64_t ldo, float* __restrict__ s0,
-                                                             float* __restrict__ us) {
-  constexpr int NS = DKP / 32, NT = DKP / 64, LS = DKP + 8, LR = kC + 8;
-  constexpr int OP = kOutParts<T>;
+__global__ __launch_bounds__(SAVE ? 256 : 512) void delta_chunk_kernel(
+    DeltaIn a, const T* __restrict__ q, const T* __restrict__ k, const T* __restrict__ v, const float* __restrict__ mats,
+    const float* __restrict__ coef, const T* __restrict__ kt, float* state_out, T* __restrict__ o, int64_t ldo,
+    float* __restrict__ s0, float* __restrict__ us) {
+  constexpr int NW = SAVE ? 4 : 8, TILES = DKP / 16, NT = TILES > NW ? TILES / NW : 1;
+  constexpr int NS = DKP / 32, LS = DKP + 8, LR = kC + 8, OP = kOutParts<T>;
   __shared__ __attribute__((aligned(16))) uint16_t sS[3 * 16 * LS], sR[3 * 16 * LR], sW[3 * 16 * LR], sU[3 * 16 * LR];
-  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, li = lane & 15, lk = lane >> 4;
+  const int tid = threadIdx.x, lane = tid & 63, li = lane & 15, lk = lane >> 4;
+  const int wv = __builtin_amdgcn_readfirstlane(tid >> 6), w = wv & 3;
+  const bool answers = wv >= 4, tiles = wv * NT < TILES;  // what the wavefront is for
   const int parts = (a.Dv + 15) / 16;
   int head, part;
   head_and_part(blockIdx.x, a.n_seq * a.H, parts, head, part);
@@ -555,15 +564,15 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void delta_chunk_kerne
             len = a.offs ? min(max(a.offs[seq + 1], base), a.rows) - base : 1;
   const int key = !a.offs || kC > a.rows ? seq : base / kC + seq;
   const int slot = slot_of(a.slots, a.n_slots, seq);
-  const T* kp = k + (int64_t)hk * a.Dk;
-  const T* qp = q + (int64_t)hk * a.Dk;
+  const T* rp = answers ? q + (int64_t)hk * a.Dk : k + (int64_t)hk * a.Dk;  // the rows that meet the state
+  const int64_t ldr = answers ? a.ldq : a.ldk;
   const bool col = c0 + li < a.Dv;  // the lane's column
   const int64_t size = (int64_t)a.Dk * a.Dv;
   const int place = token_place(w, lk);
-  // state entries [16 (NT w + n) + 4 lk + r][c0 + li]
+  // state entries [16 (NT wv + n) + 4 lk + r][c0 + li]
   floatx4 st[NT];
-  auto at = [&](int n) { return (int64_t)(16 * (NT * w + n) + 4 * lk) * a.Dv + c0 + li; };
-  auto in = [&](int n) { return 16 * (NT * w + n) + 4 * lk < a.Dk && col; };
+  auto at = [&](int n) { return (int64_t)(16 * (NT * wv + n) + 4 * lk) * a.Dv + c0 + li; };
+  auto in = [&](int n) { return tiles && 16 * (NT * wv + n) + 4 * lk < a.Dk && col; };
   auto keep = [&](float* p, int n) {
     if (in(n))
 #pragma unroll
@@ -571,7 +580,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void delta_chunk_kerne
   };
   auto share = [&]() {
 #pragma unroll
-    for (int n = 0; n < NT; ++n) put_parts<3>(sS + li * LS + 16 * (NT * w + n) + 4 * lk, 16 * LS, st[n]);
+    for (int n = 0; n < NT; ++n) put_parts<3>(sS + li * LS + 16 * (NT * wv + n) + 4 * lk, 16 * LS, st[n]);
   };
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
@@ -580,45 +589,38 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void delta_chunk_kerne
 #pragma unroll
       for (int r = 0; r < 4; ++r) st[n][r] = a.state[((int64_t)slot * a.H + h) * size + at(n) + (int64_t)r * a.Dv];
   }
-  share();
+  if (tiles) share();
   const int chunks = (len + kC - 1) / kC;
   auto chunk = [&](int ch) { return Chunk{base + ch * kC, min(kC, len - ch * kC)}; };
   auto mat = [&](int ch) {
     return reinterpret_cast<const uint16_t*>(mats + ((int64_t)(key + ch) * a.H + h) * kMats<T, SAVE>);
   };
-  Raw8<T> kf[NS], qf[NS], ktf[NT][2];
+  Raw8<T> rf[NS], ktf[NT][2];
   Parts<3> tf[2];
   Parts<OP> pf[2];
   floatx4 beta, e, wj;
-  float eC;
   typename Raw1<T>::type vv[4];
   // Rows past a chunk's end are read as its last one, and columns past a row's end as its last ones: what
   // they give meets zeros (beta, K^T, the states' rows).
-  const int ldk = (int)a.ldk, ldq = (int)a.ldq, ldv = (int)a.ldv, cv = min(c0 + li, a.Dv - 1);
+  const int ld = (int)ldr, ldv = (int)a.ldv, cv = min(c0 + li, a.Dv - 1);
   int colk[NS];
 #pragma unroll
   for (int s = 0; s < NS; ++s) colk[s] = min(32 * s + 8 * lk, a.Dk - 8);
   auto load_rows = [&](int ch) {
     const Chunk c = chunk(ch);
-    const T* kr = kp + c.row * a.ldk;
-    const T* qr = qp + c.row * a.ldq;
+    const T* r = rp + c.row * ldr;
     const int t = min(16 * w + li, c.n - 1);
 #pragma unroll
-    for (int s = 0; s < NS; ++s) kf[s].load(kr + (uint32_t)(t * ldk + colk[s]));
-    if (!SAVE)
-#pragma unroll
-      for (int s = 0; s < NS; ++s) qf[s].load(qr + (uint32_t)(t * ldq + colk[s]));
+    for (int s = 0; s < NS; ++s) rf[s].load(r + (uint32_t)(t * ld + colk[s]));
   };
   auto load_v = [&](int ch) {
     const Chunk c = chunk(ch);
     const T* vr = v + c.row * a.ldv + (int64_t)h * a.Dv;
 #pragma unroll
     for (int r = 0; r < 4; ++r) vv[r] = Raw1<T>::load(vr + (uint32_t)(min(16 * w + 4 * lk + r, c.n - 1) * ldv + cv));
-    const float* co = coef + ((int64_t)(key + ch) * a.H + h) * 3 * kC;
-    beta = *reinterpret_cast<const floatx4*>(co + 16 * w + 4 * lk);
-    e = *reinterpret_cast<const floatx4*>(co + kC + 16 * w + 4 * lk);
-    wj = *reinterpret_cast<const floatx4*>(co + 2 * kC + 16 * w + 4 * lk);
-    eC = co[2 * kC - 1];
+  };
+  auto factor = [&](int ch, int i) {
+    return *reinterpret_cast<const floatx4*>(coef + ((int64_t)(key + ch) * a.H + h) * 3 * kC + i * kC + 16 * w + 4 * lk);
   };
   const int s1 = w >> 1;  // the last 32 tokens that the wavefront's rows of T and P reach
   auto load_t = [&](int ch) {
@@ -635,87 +637,108 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void delta_chunk_kerne
     for (int n = 0; n < NT; ++n)
 #pragma unroll
       for (int s = 0; s < 2; ++s)
-        ktf[n][s] = *reinterpret_cast<const Raw8<T>*>(p + (uint32_t)(((2 * NT * w + 2 * n + s) * 64 + lane) * 8));
+        ktf[n][s] = *reinterpret_cast<const Raw8<T>*>(p + (uint32_t)(((2 * (NT * wv + n) + s) * 64 + lane) * 8));
+  };
+  // One loop for each kind of wavefront, with the same barriers: where both shared one, the compiler could not tell
+  // which loads are under way and waited for all of them (as many us again).
+  auto walk = [&](auto kind) {
+    constexpr bool A = decltype(kind)::value, TL = !A || TILES > 4;  // answers; has tiles of the state
+    // (in the order of their first use, here and below: loads come back in order)
+    load_rows(0);
+    if constexpr (!A) {
+      load_v(0);
+      beta = factor(0, 0);
+      e = factor(0, 1);
+      load_t(0);
+      wj = factor(0, 2);
+    }
+    if constexpr (TL) load_kt(0);
+    if constexpr (A) {
+      load_p(0);
+      e = factor(0, 1);
+    }
+    sync_lds();
+    for (int ch = 0; ch < chunks; ++ch) {
+      const Chunk c = chunk(ch);
+      const int next = min(ch + 1, chunks - 1);  // (the last chunk's are read again: see mat_parts)
+      if constexpr (SAVE)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) keep(s0 + ((int64_t)(key + ch) * a.H + h) * size, n);
+      Acc acc;
+      acc.clear();
+      floatx4 out;
+#pragma unroll
+      for (int s = 0; s < NS; ++s)
+        mma32<A ? OP - 1 : 2>(rf[s].parts(), get_parts<A ? OP : 3>(sS + li * LS + 32 * s + 8 * lk, 16 * LS), acc);
+      load_rows(next);
+      out = acc.sum();
+      if constexpr (!A) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) out[r] = beta[r] * fmaf(-e[r], out[r], Raw1<T>::value(vv[r]));
+        put_parts<3>(sR + li * LR + place, 16 * LR, out);
+        load_v(next);
+        beta = factor(next, 0);
+        e = factor(next, 1);
+      }
+      sync_lds();
+      if constexpr (!A) {
+        acc.clear();
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+          if (s <= s1) mma32<2>(tf[s], get_parts<3>(sR + li * LR + 32 * s + 8 * lk, 16 * LR), acc);
+        load_t(next);
+        const floatx4 u = acc.sum();
+        put_parts<3>(sW + li * LR + place, 16 * LR, u * wj);
+        wj = factor(next, 2);
+        if constexpr (!SAVE) put_parts<OP>(sU + li * LR + place, 16 * LR, u);
+        if (SAVE && col)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int t = 16 * w + 4 * lk + r;
+            if (t < c.n) us[((int64_t)(c.row + t) * a.H + h) * a.Dv + c0 + li] = u[r];
+          }
+      }
+      sync_lds();
+      if constexpr (TL) {
+        const float eC = coef[((int64_t)(key + ch) * a.H + h) * 3 * kC + 2 * kC - 1];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          acc.clear();
+#pragma unroll
+          for (int s = 0; s < 2; ++s)
+            mma32<2>(ktf[n][s].parts(), get_parts<3>(sW + li * LR + 32 * s + 8 * lk, 16 * LR), acc);
+          st[n] = st[n] * eC + acc.sum();
+        }
+        share();
+        load_kt(next);
+      }
+      if constexpr (A) {
+        acc.clear();
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+          if (s <= s1) mma32<OP - 1>(pf[s], get_parts<OP>(sU + li * LR + 32 * s + 8 * lk, 16 * LR), acc);
+        load_p(next);
+        const floatx4 x = acc.sum();
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          out[r] = fmaf(a.scale * e[r], out[r], x[r]);
+          asm("" : "+v"(out[r]));  // (formed before e's registers are loaded again, not where it is stored)
+        }
+        e = factor(next, 1);
+        T* orow = o + c.row * ldo + (int64_t)h * a.Dv;
+        if (col)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int t = 16 * w + 4 * lk + r;
+            if (t < c.n) st1(orow + (uint32_t)(t * (int)ldo + cv), out[r]);
+          }
+      }
+      sync_lds();
+    }
   };
   if (chunks > 0) {
-    load_rows(0);
-    load_v(0);
-    load_t(0);
-    load_kt(0);
-    if (!SAVE) load_p(0);
-  }
-  __syncthreads();
-  for (int ch = 0; ch < chunks; ++ch) {
-    const Chunk c = chunk(ch);
-    const int next = min(ch + 1, chunks - 1);  // (the last chunk's are read again: see mat_parts)
-    if (SAVE)
-#pragma unroll
-      for (int n = 0; n < NT; ++n) keep(s0 + ((int64_t)(key + ch) * a.H + h) * size, n);
-    Acc ks, qs;
-    ks.clear();
-    qs.clear();
-#pragma unroll
-    for (int s = 0; s < NS; ++s) {
-      const Parts<3> sf = get_parts<3>(sS + li * LS + 32 * s + 8 * lk, 16 * LS);
-      mma32<2>(kf[s].parts(), sf, ks);
-      if (!SAVE) mma32<OP - 1>(qf[s].parts(), sf, qs);
-    }
-    {
-      const floatx4 x = ks.sum();
-      floatx4 rr;
-#pragma unroll
-      for (int r = 0; r < 4; ++r) rr[r] = beta[r] * fmaf(-e[r], x[r], Raw1<T>::value(vv[r]));
-      put_parts<3>(sR + li * LR + place, 16 * LR, rr);
-    }
-    load_rows(next);
-    __syncthreads();
-    Acc acc;
-    acc.clear();
-#pragma unroll
-    for (int s = 0; s < 2; ++s)
-      if (s <= s1) mma32<2>(tf[s], get_parts<3>(sR + li * LR + 32 * s + 8 * lk, 16 * LR), acc);
-    load_t(next);
-    const floatx4 u = acc.sum();
-    put_parts<3>(sW + li * LR + place, 16 * LR, u * wj);
-    if (!SAVE) put_parts<OP>(sU + li * LR + place, 16 * LR, u);
-    if (SAVE && col)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int t = 16 * w + 4 * lk + r;
-        if (t < c.n) us[((int64_t)(c.row + t) * a.H + h) * a.Dv + c0 + li] = u[r];
-      }
-    __syncthreads();
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      acc.clear();
-#pragma unroll
-      for (int s = 0; s < 2; ++s)
-        mma32<2>(ktf[n][s].parts(), get_parts<3>(sW + li * LR + 32 * s + 8 * lk, 16 * LR), acc);
-      st[n] = st[n] * eC + acc.sum();
-    }
-    share();
-    load_kt(next);
-    floatx4 out;
-    if (!SAVE) {
-      acc.clear();
-#pragma unroll
-      for (int s = 0; s < 2; ++s)
-        if (s <= s1) mma32<OP - 1>(pf[s], get_parts<OP>(sU + li * LR + 32 * s + 8 * lk, 16 * LR), acc);
-      load_p(next);
-      const floatx4 x = qs.sum(), y = acc.sum();
-#pragma unroll
-      for (int r = 0; r < 4; ++r) out[r] = fmaf(a.scale * e[r], x[r], y[r]);
-    }
-    load_v(next);
-    if (!SAVE && col) {
-      T* orow = o + c.row * ldo + (int64_t)h * a.Dv;
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int t = 16 * w + 4 * lk + r;
-        if (t < c.n) st1(orow + (uint32_t)(t * (int)ldo + cv), out[r]);
-      }
-    }
-    __syncthreads();
+    if (answers) walk(std::true_type());
+    else walk(std::false_type());
   }
   if (!SAVE && state_out && slot >= 0)
 #pragma unroll
@@ -1142,7 +1165,7 @@ hipError_t chunks(const DeltaOp& a, float* state_out, void* o, int64_t ldo, floa
   const T *q = static_cast<const T*>(a.q), *k = static_cast<const T*>(a.k), *v = static_cast<const T*>(a.v);
   T* kt = reinterpret_cast<T*>(mats + tiles * a.H * kMats<T, false>);
   delta_prep_kernel<T, DKP, false><<<dim3((unsigned)(tiles * a.Hk)), 256, 0, s>>>(in_of(a), q, k, mats, coef, kt);
-  delta_chunk_kernel<T, DKP, false><<<dim3((unsigned)((int64_t)a.n_seq * a.H * ((a.Dv + 15) / 16))), 256, 0, s>>>(
+  delta_chunk_kernel<T, DKP, false><<<dim3((unsigned)((int64_t)a.n_seq * a.H * ((a.Dv + 15) / 16))), 512, 0, s>>>(
       in_of(a), q, k, v, mats, coef, kt, state_out, static_cast<T*>(o), ldo, nullptr, nullptr);
   return hipGetLastError();
 }
