@@ -183,6 +183,13 @@ __device__ __forceinline__ void sync_lds() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
+// The same for a wavefront with itself: its lanes' writes in front of its lanes' reads.
+__device__ __forceinline__ void sync_wave() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+}
+
 // ---------------------------------------------------------------- matrix products
 // v_mfma_f32_16x16x4_f32: lane l holds A[l % 16][l / 16], B[l / 16][l % 16] and D[4 (l / 16) + r][l % 16]. The
 // order of the k's is free, so four steps share one 16-byte read where k runs along memory: a
@@ -285,19 +292,17 @@ template <> struct Raw8<float> {
   __device__ __forceinline__ void clear() { a = b = floatx4{0.f, 0.f, 0.f, 0.f}; }
   __device__ __forceinline__ Parts<3> parts() const { return split8<3>(a, b); }
 };
-// One entry, a register of its own: two halves of one would make the second load wait for the first.
-template <typename T> struct Raw1;
-template <> struct Raw1<float> {
-  typedef float type;
-  static __device__ __forceinline__ float load(const float* p) { return *p; }
-  static __device__ __forceinline__ float value(float x) { return x; }
+// Four neighbours of a row as they are in memory.
+template <typename T> struct Raw4;
+template <> struct Raw4<uint16_t> {
+  u32x2 v;
+  __device__ __forceinline__ void load(const uint16_t* p) { v = *reinterpret_cast<const u32x2_any*>(p); }
+  __device__ __forceinline__ void store(uint16_t* p) const { *reinterpret_cast<u32x2_any*>(p) = v; }
 };
-template <> struct Raw1<uint16_t> {
-  typedef uint32_t type;
-  static __device__ __forceinline__ uint32_t load(const uint16_t* p) {
-    return *p;
-  }
-  static __device__ __forceinline__ float value(uint32_t x) { return __uint_as_float(x << 16); }
+template <> struct Raw4<float> {
+  floatx4 v;
+  __device__ __forceinline__ void load(const float* p) { v = ld4(p); }
+  __device__ __forceinline__ void store(float* p) const { st4(p, v); }
 };
 // In products over tokens, the eight of lane group kq of the 32 from 32 s on: 32 s + 16 a + 4 kq + m at
 // place 4 a + m. So the four tokens of a lane's results are neighbours in LDS, and two fragments (frag) of a
@@ -363,7 +368,7 @@ constexpr int kLdM = kC + 4;
 template <typename T, int DKP, bool GRADS>
 __global__ __launch_bounds__(256) void delta_prep_kernel(DeltaIn a, const T* __restrict__ q, const T* __restrict__ k,
                                                          float* __restrict__ mats, float* __restrict__ coef,
-                                                         T* __restrict__ kt) {
+                                                         T* __restrict__ ops) {
   __shared__ __attribute__((aligned(16))) float sA[kC * kLdM], sT[kC * kLdM], sX[32 * 36];
   __shared__ double sG[kC];
   __shared__ float sB[kC];
@@ -376,10 +381,10 @@ __global__ __launch_bounds__(256) void delta_prep_kernel(DeltaIn a, const T* __r
   const T* kp = k + (int64_t)hk * a.Dk;
   // products of rows: lane's entries [16 w + 4 lk + r][16 t + li]
   floatx4 kk[4], qk[4];
+  Raw8<T> kf[NS], qf[NS];
+  row_raw<T, NS>(kp, a.ldk, c, w, a.Dk, kf);
+  row_raw<T, NS>(q + (int64_t)hk * a.Dk, a.ldq, c, w, a.Dk, qf);
   {
-    Raw8<T> kf[NS], qf[NS];
-    row_raw<T, NS>(kp, a.ldk, c, w, a.Dk, kf);
-    row_raw<T, NS>(q + (int64_t)hk * a.Dk, a.ldq, c, w, a.Dk, qf);
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
       kk[t] = qk[t] = floatx4{0.f, 0.f, 0.f, 0.f};
@@ -399,9 +404,16 @@ __global__ __launch_bounds__(256) void delta_prep_kernel(DeltaIn a, const T* __r
       qk[t] = y.sum();
     }
   }
-  // K^T as operands over tokens
+  // K, Q and K^T as operands: a chunk's rows are a model's width apart, and every slice of every head that
+  // reads them so would ask one channel of the cache for all of them
   {
-    T* out = kt + ((int64_t)tile * a.Hk + hk) * DKP * kC;
+    T* out = ops + ((int64_t)tile * a.Hk + hk) * 3 * DKP * kC;
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+      *reinterpret_cast<Raw8<T>*>(out + ((w * NS + s) * 64 + lane) * 8) = kf[s];
+      *reinterpret_cast<Raw8<T>*>(out + DKP * kC + ((w * NS + s) * 64 + lane) * 8) = qf[s];
+    }
+    out += 2 * DKP * kC;
 #pragma unroll
     for (int f = w; f < DKP / 16 * 2; f += 4) {
       const int col = 16 * (f >> 1) + li;
@@ -547,12 +559,15 @@ __device__ __forceinline__ void head_and_part(int b, int heads, int parts, int& 
 // front of the chunks and U are kept, no answers are formed, by the first four alone.
 template <typename T, int DKP, bool SAVE>
 __global__ __launch_bounds__(SAVE ? 256 : 512) void delta_chunk_kernel(
-    DeltaIn a, const T* __restrict__ q, const T* __restrict__ k, const T* __restrict__ v, const float* __restrict__ mats,
-    const float* __restrict__ coef, const T* __restrict__ kt, float* state_out, T* __restrict__ o, int64_t ldo,
+    DeltaIn a, const T* __restrict__ v, const float* __restrict__ mats, const float* __restrict__ coef,
+    const T* __restrict__ ops, float* state_out, T* __restrict__ o, int64_t ldo,
     float* __restrict__ s0, float* __restrict__ us) {
   constexpr int NW = SAVE ? 4 : 8, TILES = DKP / 16, NT = TILES > NW ? TILES / NW : 1;
   constexpr int NS = DKP / 32, LS = DKP + 8, LR = kC + 8, OP = kOutParts<T>;
   __shared__ __attribute__((aligned(16))) uint16_t sS[3 * 16 * LS], sR[3 * 16 * LR], sW[3 * 16 * LR], sU[3 * 16 * LR];
+  // a wavefront's tokens' values and answers, on their way between rows in memory and columns in registers
+  constexpr int LV = 20;
+  __shared__ __attribute__((aligned(16))) T sV[NW][16 * LV];
   const int tid = threadIdx.x, lane = tid & 63, li = lane & 15, lk = lane >> 4;
   const int wv = __builtin_amdgcn_readfirstlane(tid >> 6), w = wv & 3;
   const bool answers = wv >= 4, tiles = wv * NT < TILES;  // what the wavefront is for
@@ -564,8 +579,6 @@ __global__ __launch_bounds__(SAVE ? 256 : 512) void delta_chunk_kernel(
             len = a.offs ? min(max(a.offs[seq + 1], base), a.rows) - base : 1;
   const int key = !a.offs || kC > a.rows ? seq : base / kC + seq;
   const int slot = slot_of(a.slots, a.n_slots, seq);
-  const T* rp = answers ? q + (int64_t)hk * a.Dk : k + (int64_t)hk * a.Dk;  // the rows that meet the state
-  const int64_t ldr = answers ? a.ldq : a.ldk;
   const bool col = c0 + li < a.Dv;  // the lane's column
   const int64_t size = (int64_t)a.Dk * a.Dv;
   const int place = token_place(w, lk);
@@ -599,25 +612,20 @@ __global__ __launch_bounds__(SAVE ? 256 : 512) void delta_chunk_kernel(
   Parts<3> tf[2];
   Parts<OP> pf[2];
   floatx4 beta, e, wj;
-  typename Raw1<T>::type vv[4];
-  // Rows past a chunk's end are read as its last one, and columns past a row's end as its last ones: what
-  // they give meets zeros (beta, K^T, the states' rows).
-  const int ld = (int)ldr, ldv = (int)a.ldv, cv = min(c0 + li, a.Dv - 1);
-  int colk[NS];
-#pragma unroll
-  for (int s = 0; s < NS; ++s) colk[s] = min(32 * s + 8 * lk, a.Dk - 8);
+  Raw4<T> vv;
+  const int ldv = (int)a.ldv, cv = c0 + 4 * (lane & 3), tv = 16 * w + lane / 4;
+  auto op = [&](int ch, int i) { return ops + (((int64_t)(key + ch) * a.Hk + hk) * 3 + i) * DKP * kC; };
   auto load_rows = [&](int ch) {
-    const Chunk c = chunk(ch);
-    const T* r = rp + c.row * ldr;
-    const int t = min(16 * w + li, c.n - 1);
+    const T* r = op(ch, answers ? 1 : 0);
 #pragma unroll
-    for (int s = 0; s < NS; ++s) rf[s].load(r + (uint32_t)(t * ld + colk[s]));
+    for (int s = 0; s < NS; ++s) rf[s] = *reinterpret_cast<const Raw8<T>*>(r + (uint32_t)(((w * NS + s) * 64 + lane) * 8));
   };
+  // (rows past a chunk's end, and columns past a row's, are read as the last ones: the first meet a beta of zero, the
+  // others' results are not kept)
   auto load_v = [&](int ch) {
     const Chunk c = chunk(ch);
     const T* vr = v + c.row * a.ldv + (int64_t)h * a.Dv;
-#pragma unroll
-    for (int r = 0; r < 4; ++r) vv[r] = Raw1<T>::load(vr + (uint32_t)(min(16 * w + 4 * lk + r, c.n - 1) * ldv + cv));
+    vv.load(vr + (uint32_t)(min(tv, c.n - 1) * ldv + min(cv, a.Dv - 4)));
   };
   auto factor = [&](int ch, int i) {
     return *reinterpret_cast<const floatx4*>(coef + ((int64_t)(key + ch) * a.H + h) * 3 * kC + i * kC + 16 * w + 4 * lk);
@@ -632,7 +640,7 @@ __global__ __launch_bounds__(SAVE ? 256 : 512) void delta_chunk_kernel(
     pf[1] = mat_parts<OP>(mat(ch) + 2 * kTParts, w, s1);
   };
   auto load_kt = [&](int ch) {
-    const T* p = kt + ((int64_t)(key + ch) * a.Hk + hk) * DKP * kC;
+    const T* p = op(ch, 2);
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -664,6 +672,11 @@ __global__ __launch_bounds__(SAVE ? 256 : 512) void delta_chunk_kernel(
       if constexpr (SAVE)
 #pragma unroll
         for (int n = 0; n < NT; ++n) keep(s0 + ((int64_t)(key + ch) * a.H + h) * size, n);
+      T* mine = sV[wv];
+      if constexpr (!A) {
+        *reinterpret_cast<Raw4<T>*>(mine + lane / 4 * LV + 4 * (lane & 3)) = vv;
+        sync_wave();
+      }
       Acc acc;
       acc.clear();
       floatx4 out;
@@ -674,8 +687,9 @@ __global__ __launch_bounds__(SAVE ? 256 : 512) void delta_chunk_kernel(
       out = acc.sum();
       if constexpr (!A) {
 #pragma unroll
-        for (int r = 0; r < 4; ++r) out[r] = beta[r] * fmaf(-e[r], out[r], Raw1<T>::value(vv[r]));
+        for (int r = 0; r < 4; ++r) out[r] = beta[r] * fmaf(-e[r], out[r], to_f32(mine[(4 * lk + r) * LV + li]));
         put_parts<3>(sR + li * LR + place, 16 * LR, out);
+        sync_wave();  // (the values are read)
         load_v(next);
         beta = factor(next, 0);
         e = factor(next, 1);
@@ -722,16 +736,13 @@ __global__ __launch_bounds__(SAVE ? 256 : 512) void delta_chunk_kernel(
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           out[r] = fmaf(a.scale * e[r], out[r], x[r]);
-          asm("" : "+v"(out[r]));  // (formed before e's registers are loaded again, not where it is stored)
+          st1(mine + (4 * lk + r) * LV + li, out[r]);
         }
+        sync_wave();
         e = factor(next, 1);
         T* orow = o + c.row * ldo + (int64_t)h * a.Dv;
-        if (col)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const int t = 16 * w + 4 * lk + r;
-            if (t < c.n) st1(orow + (uint32_t)(t * (int)ldo + cv), out[r]);
-          }
+        if (tv < c.n && cv < a.Dv)
+          reinterpret_cast<const Raw4<T>*>(mine + lane / 4 * LV + 4 * (lane & 3))->store(orow + (uint32_t)(tv * (int)ldo + cv));
       }
       sync_lds();
     }
@@ -1163,21 +1174,21 @@ hipError_t chunks(const DeltaOp& a, float* state_out, void* o, int64_t ldo, floa
   float* coef = ws;
   float* mats = ws + tiles * a.H * 3 * kC;
   const T *q = static_cast<const T*>(a.q), *k = static_cast<const T*>(a.k), *v = static_cast<const T*>(a.v);
-  T* kt = reinterpret_cast<T*>(mats + tiles * a.H * kMats<T, false>);
-  delta_prep_kernel<T, DKP, false><<<dim3((unsigned)(tiles * a.Hk)), 256, 0, s>>>(in_of(a), q, k, mats, coef, kt);
+  T* ops = reinterpret_cast<T*>(mats + tiles * a.H * kMats<T, false>);
+  delta_prep_kernel<T, DKP, false><<<dim3((unsigned)(tiles * a.Hk)), 256, 0, s>>>(in_of(a), q, k, mats, coef, ops);
   delta_chunk_kernel<T, DKP, false><<<dim3((unsigned)((int64_t)a.n_seq * a.H * ((a.Dv + 15) / 16))), 512, 0, s>>>(
-      in_of(a), q, k, v, mats, coef, kt, state_out, static_cast<T*>(o), ldo, nullptr, nullptr);
+      in_of(a), v, mats, coef, ops, state_out, static_cast<T*>(o), ldo, nullptr, nullptr);
   return hipGetLastError();
 }
 
-// K^T of every chunk and key head, in floats.
-int64_t kt_floats(bool bf16, int n_seq, int rows, int Hk, int Dk) {
-  return tiles_of(n_seq, rows) * Hk * (Dk <= 64 ? 64 : 128) * kC / (bf16 ? 2 : 1);
+// K, Q and K^T of every chunk and key head, in floats.
+int64_t op_floats(bool bf16, int n_seq, int rows, int Hk, int Dk) {
+  return tiles_of(n_seq, rows) * Hk * 3 * (Dk <= 64 ? 64 : 128) * kC / (bf16 ? 2 : 1);
 }
 
 // The parts of the gradients' workspace, in floats.
 struct BackSpace {
-  int64_t coef, mats, s0, ds1, us, drs, kt, end;
+  int64_t coef, mats, s0, ds1, us, drs, ops, end;
   BackSpace(bool bf16, int n_seq, int rows, int Hk, int H, int Dk, int Dv) {
     const int64_t th = tiles_of(n_seq, rows) * H, head = (int64_t)Dk * Dv, act = (int64_t)rows * H * Dv;
     coef = 0;
@@ -1186,8 +1197,8 @@ struct BackSpace {
     ds1 = s0 + th * head;
     us = ds1 + th * head;
     drs = us + act;
-    kt = drs + act;
-    end = kt + kt_floats(bf16, n_seq, rows, Hk, Dk);
+    ops = drs + act;
+    end = ops + op_floats(bf16, n_seq, rows, Hk, Dk);
   }
 };
 
@@ -1196,13 +1207,13 @@ hipError_t grads(const DeltaOp& a, const void* d_o_, int64_t lddo, const float* 
                  float* ws, hipStream_t s) {
   const int64_t tiles = tiles_of(a.n_seq, a.rows);
   const BackSpace b(a.bf16, a.n_seq, a.rows, a.Hk, a.H, a.Dk, a.Dv);
-  T* kt = reinterpret_cast<T*>(ws + b.kt);
+  T* ops = reinterpret_cast<T*>(ws + b.ops);
   const T *q = static_cast<const T*>(a.q), *k = static_cast<const T*>(a.k), *v = static_cast<const T*>(a.v);
   const T* d_o = static_cast<const T*>(d_o_);
   const DeltaIn in = in_of(a);
   const dim3 flat((unsigned)(tiles * a.Hk)), slices((unsigned)((int64_t)a.n_seq * a.H * ((a.Dv + 15) / 16)));
-  delta_prep_kernel<T, DKP, true><<<flat, 256, 0, s>>>(in, q, k, ws + b.mats, ws + b.coef, kt);
-  delta_chunk_kernel<T, DKP, true><<<slices, 256, 0, s>>>(in, q, k, v, ws + b.mats, ws + b.coef, kt, nullptr, nullptr, 0,
+  delta_prep_kernel<T, DKP, true><<<flat, 256, 0, s>>>(in, q, k, ws + b.mats, ws + b.coef, ops);
+  delta_chunk_kernel<T, DKP, true><<<slices, 256, 0, s>>>(in, v, ws + b.mats, ws + b.coef, ops, nullptr, nullptr, 0,
                                                           ws + b.s0, ws + b.us);
   delta_back_kernel<T, DKP, 16><<<slices, 256, 0, s>>>(in, q, k, d_o, lddo, ws + b.mats, ws + b.coef, dstate_out,
                                                        g.dstate, static_cast<T*>(g.dv), g.lddv, ws + b.ds1, ws + b.drs);
@@ -1218,7 +1229,7 @@ size_t delta_rule_workspace_bytes(bool bf16, int n_seq, int rows, int Hk, int H,
   (void)Dv;
   if (!chunked(n_seq, rows)) return 0;
   const int mats = bf16 ? kMats<uint16_t, false> : kMats<float, false>;
-  return (size_t)(tiles_of(n_seq, rows) * H * (3 * kC + mats) + kt_floats(bf16, n_seq, rows, Hk, Dk)) * sizeof(float);
+  return (size_t)(tiles_of(n_seq, rows) * H * (3 * kC + mats) + op_floats(bf16, n_seq, rows, Hk, Dk)) * sizeof(float);
 }
 
 hipError_t launch_delta_rule(const DeltaOp& a, float* state_out, void* o, int64_t ldo, float* ws, hipStream_t s) {
