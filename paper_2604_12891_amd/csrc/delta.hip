@@ -552,17 +552,18 @@ __device__ __forceinline__ void head_and_part(int b, int heads, int parts, int& 
 }
 
 // A workgroup per sequence, value head and slice of 16 columns. The parts of the state in LDS, [column][row],
-// feed the products; the state itself stays in registers, tiles of 16 rows to a wavefront. Four wavefronts of 16
-// tokens each form R, U and what goes into the state (K S0, T R), the chain that a chunk waits for; four more
-// the answers (Q S0, P U), so that each SIMD has two to issue from. Three barriers a chunk; what the
-// next one reads from memory is asked for as soon as its registers are free. SAVE (for the gradients): the states in
+// feed the products; the state itself stays in registers, tiles of 16 rows to a wavefront. Three barriers a chunk
+// make three phases. Four wavefronts of 16 tokens each form R (K S0), then U (T R); four more the answers of
+// the chunk before (P U), then Q S0, then the new state. So each SIMD has two to issue from, and LDS, whose 128
+// bytes a cycle every product's operands share, is asked evenly. What
+// the next chunk reads from memory is asked for as soon as its registers are free. SAVE (for the gradients): the states in
 // front of the chunks and U are kept, no answers are formed, by the first four alone.
 template <typename T, int DKP, bool SAVE>
 __global__ __launch_bounds__(SAVE ? 256 : 512) void delta_chunk_kernel(
     DeltaIn a, const T* __restrict__ v, const float* __restrict__ mats, const float* __restrict__ coef,
     const T* __restrict__ ops, float* state_out, T* __restrict__ o, int64_t ldo,
     float* __restrict__ s0, float* __restrict__ us) {
-  constexpr int NW = SAVE ? 4 : 8, TILES = DKP / 16, NT = TILES > NW ? TILES / NW : 1;
+  constexpr int NW = SAVE ? 4 : 8, NT = DKP / 64;
   constexpr int NS = DKP / 32, LS = DKP + 8, LR = kC + 8, OP = kOutParts<T>;
   __shared__ __attribute__((aligned(16))) uint16_t sS[3 * 16 * LS], sR[3 * 16 * LR], sW[3 * 16 * LR], sU[3 * 16 * LR];
   // a wavefront's tokens' values and answers, on their way between rows in memory and columns in registers
@@ -570,7 +571,7 @@ __global__ __launch_bounds__(SAVE ? 256 : 512) void delta_chunk_kernel(
   __shared__ __attribute__((aligned(16))) T sV[NW][16 * LV];
   const int tid = threadIdx.x, lane = tid & 63, li = lane & 15, lk = lane >> 4;
   const int wv = __builtin_amdgcn_readfirstlane(tid >> 6), w = wv & 3;
-  const bool answers = wv >= 4, tiles = wv * NT < TILES;  // what the wavefront is for
+  const bool answers = wv >= 4, tiles = SAVE || answers;  // what the wavefront is for
   const int parts = (a.Dv + 15) / 16;
   int head, part;
   head_and_part(blockIdx.x, a.n_seq * a.H, parts, head, part);
@@ -582,10 +583,10 @@ __global__ __launch_bounds__(SAVE ? 256 : 512) void delta_chunk_kernel(
   const bool col = c0 + li < a.Dv;  // the lane's column
   const int64_t size = (int64_t)a.Dk * a.Dv;
   const int place = token_place(w, lk);
-  // state entries [16 (NT wv + n) + 4 lk + r][c0 + li]
+  // state entries [16 (NT w + n) + 4 lk + r][c0 + li]
   floatx4 st[NT];
-  auto at = [&](int n) { return (int64_t)(16 * (NT * wv + n) + 4 * lk) * a.Dv + c0 + li; };
-  auto in = [&](int n) { return tiles && 16 * (NT * wv + n) + 4 * lk < a.Dk && col; };
+  auto at = [&](int n) { return (int64_t)(16 * (NT * w + n) + 4 * lk) * a.Dv + c0 + li; };
+  auto in = [&](int n) { return tiles && 16 * (NT * w + n) + 4 * lk < a.Dk && col; };
   auto keep = [&](float* p, int n) {
     if (in(n))
 #pragma unroll
@@ -593,7 +594,7 @@ __global__ __launch_bounds__(SAVE ? 256 : 512) void delta_chunk_kernel(
   };
   auto share = [&]() {
 #pragma unroll
-    for (int n = 0; n < NT; ++n) put_parts<3>(sS + li * LS + 16 * (NT * wv + n) + 4 * lk, 16 * LS, st[n]);
+    for (int n = 0; n < NT; ++n) put_parts<3>(sS + li * LS + 16 * (NT * w + n) + 4 * lk, 16 * LS, st[n]);
   };
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
@@ -645,47 +646,60 @@ __global__ __launch_bounds__(SAVE ? 256 : 512) void delta_chunk_kernel(
     for (int n = 0; n < NT; ++n)
 #pragma unroll
       for (int s = 0; s < 2; ++s)
-        ktf[n][s] = *reinterpret_cast<const Raw8<T>*>(p + (uint32_t)(((2 * (NT * wv + n) + s) * 64 + lane) * 8));
+        ktf[n][s] = *reinterpret_cast<const Raw8<T>*>(p + (uint32_t)(((2 * (NT * w + n) + s) * 64 + lane) * 8));
   };
   // One loop for each kind of wavefront, with the same barriers: where both shared one, the compiler could not tell
   // which loads are under way and waited for all of them (as many us again).
   auto walk = [&](auto kind) {
-    constexpr bool A = decltype(kind)::value, TL = !A || TILES > 4;  // answers; has tiles of the state
+    constexpr bool A = decltype(kind)::value;  // answers and (always where there are no others) the state
+    constexpr bool B = !A;
     // (in the order of their first use, here and below: loads come back in order)
     load_rows(0);
-    if constexpr (!A) {
+    if constexpr (B) {
       load_v(0);
       beta = factor(0, 0);
       e = factor(0, 1);
       load_t(0);
       wj = factor(0, 2);
     }
-    if constexpr (TL) load_kt(0);
+    if constexpr (A || SAVE) load_kt(0);
     if constexpr (A) {
       load_p(0);
       e = factor(0, 1);
     }
     sync_lds();
+    T* mine = sV[wv];
+    Acc acc;
+    floatx4 out;
+    // the answers of chunk ch, from Q S0 (out) and U; asks for P and e of chunk `next`
+    auto answer = [&](int ch, int next) {
+      const Chunk c = chunk(ch);
+      acc.clear();
+#pragma unroll
+      for (int s = 0; s < 2; ++s)
+        if (s <= s1) mma32<OP - 1>(pf[s], get_parts<OP>(sU + li * LR + 32 * s + 8 * lk, 16 * LR), acc);
+      load_p(next);
+      const floatx4 x = acc.sum();
+#pragma unroll
+      for (int r = 0; r < 4; ++r) st1(mine + (4 * lk + r) * LV + li, fmaf(a.scale * e[r], out[r], x[r]));
+      sync_wave();
+      e = factor(next, 1);
+      T* orow = o + c.row * ldo + (int64_t)h * a.Dv;
+      if (tv < c.n && cv < a.Dv)
+        reinterpret_cast<const Raw4<T>*>(mine + lane / 4 * LV + 4 * (lane & 3))->store(orow + (uint32_t)(tv * (int)ldo + cv));
+    };
     for (int ch = 0; ch < chunks; ++ch) {
       const Chunk c = chunk(ch);
       const int next = min(ch + 1, chunks - 1);  // (the last chunk's are read again: see mat_parts)
-      if constexpr (SAVE)
-#pragma unroll
-        for (int n = 0; n < NT; ++n) keep(s0 + ((int64_t)(key + ch) * a.H + h) * size, n);
-      T* mine = sV[wv];
-      if constexpr (!A) {
+      if constexpr (B) {
         *reinterpret_cast<Raw4<T>*>(mine + lane / 4 * LV + 4 * (lane & 3)) = vv;
         sync_wave();
-      }
-      Acc acc;
-      acc.clear();
-      floatx4 out;
+        acc.clear();
 #pragma unroll
-      for (int s = 0; s < NS; ++s)
-        mma32<A ? OP - 1 : 2>(rf[s].parts(), get_parts<A ? OP : 3>(sS + li * LS + 32 * s + 8 * lk, 16 * LS), acc);
-      load_rows(next);
-      out = acc.sum();
-      if constexpr (!A) {
+        for (int s = 0; s < NS; ++s)
+          mma32<2>(rf[s].parts(), get_parts<3>(sS + li * LS + 32 * s + 8 * lk, 16 * LS), acc);
+        load_rows(next);
+        out = acc.sum();
 #pragma unroll
         for (int r = 0; r < 4; ++r) out[r] = beta[r] * fmaf(-e[r], out[r], to_f32(mine[(4 * lk + r) * LV + li]));
         put_parts<3>(sR + li * LR + place, 16 * LR, out);
@@ -693,9 +707,14 @@ __global__ __launch_bounds__(SAVE ? 256 : 512) void delta_chunk_kernel(
         load_v(next);
         beta = factor(next, 0);
         e = factor(next, 1);
+      } else if (ch > 0) {
+        answer(ch - 1, ch);
       }
+      if constexpr (SAVE)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) keep(s0 + ((int64_t)(key + ch) * a.H + h) * size, n);
       sync_lds();
-      if constexpr (!A) {
+      if constexpr (B) {
         acc.clear();
 #pragma unroll
         for (int s = 0; s < 2; ++s)
@@ -711,41 +730,33 @@ __global__ __launch_bounds__(SAVE ? 256 : 512) void delta_chunk_kernel(
             const int t = 16 * w + 4 * lk + r;
             if (t < c.n) us[((int64_t)(c.row + t) * a.H + h) * a.Dv + c0 + li] = u[r];
           }
+      } else {
+        acc.clear();
+#pragma unroll
+        for (int s = 0; s < NS; ++s)
+          mma32<OP - 1>(rf[s].parts(), get_parts<OP>(sS + li * LS + 32 * s + 8 * lk, 16 * LS), acc);
+        load_rows(next);
+        out = acc.sum();
       }
       sync_lds();
-      if constexpr (TL) {
+      if constexpr (A || SAVE) {
         const float eC = coef[((int64_t)(key + ch) * a.H + h) * 3 * kC + 2 * kC - 1];
+        Parts<3> wf[2];
+#pragma unroll
+        for (int s = 0; s < 2; ++s) wf[s] = get_parts<3>(sW + li * LR + 32 * s + 8 * lk, 16 * LR);
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
           acc.clear();
 #pragma unroll
-          for (int s = 0; s < 2; ++s)
-            mma32<2>(ktf[n][s].parts(), get_parts<3>(sW + li * LR + 32 * s + 8 * lk, 16 * LR), acc);
+          for (int s = 0; s < 2; ++s) mma32<2>(ktf[n][s].parts(), wf[s], acc);
           st[n] = st[n] * eC + acc.sum();
         }
         share();
         load_kt(next);
       }
-      if constexpr (A) {
-        acc.clear();
-#pragma unroll
-        for (int s = 0; s < 2; ++s)
-          if (s <= s1) mma32<OP - 1>(pf[s], get_parts<OP>(sU + li * LR + 32 * s + 8 * lk, 16 * LR), acc);
-        load_p(next);
-        const floatx4 x = acc.sum();
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          out[r] = fmaf(a.scale * e[r], out[r], x[r]);
-          st1(mine + (4 * lk + r) * LV + li, out[r]);
-        }
-        sync_wave();
-        e = factor(next, 1);
-        T* orow = o + c.row * ldo + (int64_t)h * a.Dv;
-        if (tv < c.n && cv < a.Dv)
-          reinterpret_cast<const Raw4<T>*>(mine + lane / 4 * LV + 4 * (lane & 3))->store(orow + (uint32_t)(tv * (int)ldo + cv));
-      }
       sync_lds();
     }
+    if constexpr (A) answer(chunks - 1, chunks - 1);
   };
   if (chunks > 0) {
     if (answers) walk(std::true_type());
