@@ -456,9 +456,24 @@ __global__ __launch_bounds__(kTB) void logprobs_join_kernel(LogitRows a, int K, 
 // sorted, so every round takes the best of the lists' heads. Scores are compared in 64 bits: fp32 would make
 // neighbours equal that a long search's sum of log probabilities (-100: steps of 8e-6) cannot tell
 // apart. Equal scores: the lower row, then the lower token, which is the lower list, as splits are in their
-// rows' order. A wavefront runs the rounds, some 100 ns each, out of LDS where the lists fit.
+// rows' order. A wavefront runs the rounds, out of LDS where the lists fit; a lane has its lists' best head
+// in registers, so that a round is the reduction over lanes and one lane's step on.
 constexpr int kBeamLists = 1024;  // W x splits
 constexpr int kBeamKeys = 4096;   // keys held in LDS
+
+// The larger of two scores, of equal ones the lower list.
+struct Head {
+  double s;
+  int l;
+};
+__device__ __forceinline__ Head better(Head a, Head b) { return b.s > a.s || (b.s == a.s && b.l < a.l) ? b : a; }
+template <int CTRL>
+__device__ __forceinline__ Head head_dpp(Head h) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, h.s);
+  auto mov = [](uint32_t x) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xF, 0xF, false); };
+  return {__builtin_bit_cast(double, (uint64_t)mov((uint32_t)(u >> 32)) << 32 | mov((uint32_t)u)), (int)mov((uint32_t)h.l)};
+}
+__device__ __forceinline__ Head head_xor(Head h, int o) { return {__shfl_xor(h.s, o, 64), __shfl_xor(h.l, o, 64)}; }
 
 template <typename T>
 __global__ __launch_bounds__(kTB) void beam_join_kernel(LogitRows a, int W, int K, int splits, Beams beams,
@@ -468,26 +483,34 @@ __global__ __launch_bounds__(kTB) void beam_join_kernel(LogitRows a, int W, int 
   __shared__ double head[kBeamLists];   // a list's best score that is left
   __shared__ uint16_t at[kBeamLists];   // and its place
   __shared__ double base[64], top[64];  // score - log of the sum; the maximum
+  __shared__ int alone[64];             // -1: an open beam; else it has ended with this token (-2: dead)
   const int g = blockIdx.x, tid = threadIdx.x, lane = tid & 63, lists = W * splits;
   const float zc = a.inv_temp * kLog2e;
   const double it = a.inv_temp;
+  constexpr double kNone = -(double)INFINITY;
   const char* w = ws + (int64_t)g * lists * split_stride(K);
   const bool held = lists * K <= kBeamKeys;
   for (int b = tid >> 6; b < W; b += kTB / 64) {
     const int r = g * W + b;
-    if (!beams.open(r)) continue;  // (uniform over the wavefront)
+    const float score = beams.score[r];
+    const int ended = beams.ended ? beams.ended[r] : -1;
+    const int kind = !(score > -INFINITY) ? -2 : ended >= 0 ? ended : -1;
     Stats st = {-INFINITY, 0.f, 0.f};
-    for (int k = lane; k < splits; k += 64)
-      st = merge(st, *reinterpret_cast<const Stats*>(w + (int64_t)(b * splits + k) * split_stride(K) + (int64_t)K * 8), zc);
-    st = wave_merge(st, zc);
+    if (kind == -1) {  // (uniform over the wavefront)
+      for (int k = lane; k < splits; k += 64)
+        st = merge(st, *reinterpret_cast<const Stats*>(w + (int64_t)(b * splits + k) * split_stride(K) + (int64_t)K * 8), zc);
+      if (splits > 1) st = wave_merge(st, zc);
+    }
     if (lane == 0) {
-      base[b] = (double)beams.score[r] - log((double)st.s);
+      alone[b] = kind;
+      base[b] = kind == -1 ? (double)score - log((double)st.s) : (double)score;
       top[b] = st.m;
     }
   }
+  __syncthreads();
   if (held)
     for (int q = tid; q < lists * K; q += kTB)
-      if (beams.open(g * W + q / (K * splits)))
+      if (alone[q / (K * splits)] == -1)
         keys[q] = reinterpret_cast<const u64*>(w + (int64_t)(q / K) * split_stride(K))[q % K];
   __syncthreads();
   auto key_of = [&](int l, int i) {
@@ -495,15 +518,12 @@ __global__ __launch_bounds__(kTB) void beam_join_kernel(LogitRows a, int W, int 
   };
   // (NaN, of a row with a logit of +inf, is no score)
   auto score_of = [&](int l, int i) {
-    const int b = l / splits, r = g * W + b;
-    if (!beams.open(r)) {  // an ended beam is its own one candidate
-      const bool one = i == 0 && l % splits == 0 && beams.score[r] > -INFINITY;
-      return one ? (double)beams.score[r] : -(double)INFINITY;
-    }
+    const int b = l / splits;
+    if (alone[b] != -1) return i == 0 && l % splits == 0 && alone[b] >= 0 ? base[b] : kNone;  // itself, once
     const u64 k = i < K ? key_of(l, i) : 0;
-    if (!k) return -(double)INFINITY;
+    if (!k) return kNone;
     const double s = base[b] + ((double)ord_value<T>((uint32_t)(k >> 32)) - top[b]) * it;
-    return s > -(double)INFINITY ? s : -(double)INFINITY;
+    return s > kNone ? s : kNone;
   };
   for (int l = tid; l < lists; l += kTB) {
     head[l] = score_of(l, 0);
@@ -512,37 +532,36 @@ __global__ __launch_bounds__(kTB) void beam_join_kernel(LogitRows a, int W, int 
   __syncthreads();
   if (tid >= 64) return;
   const int bits = index_bits(a.V);
-  for (int i = 0; i < K; ++i) {
-    double best = -(double)INFINITY;
-    int from = lists;
+  auto own = [&]() {  // the best of the lane's lists
+    Head h = {kNone, lists};
     for (int l = lane; l < lists; l += 64)
-      if (head[l] > best) {
-        best = head[l];
-        from = l;
-      }
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
-      const double s = __shfl_xor(best, o, 64);
-      const int f = __shfl_xor(from, o, 64);
-      if (s > best || (s == best && f < from)) {
-        best = s;
-        from = f;
-      }
-    }
-    const bool some = from < lists;  // the same in every lane
-    if (lane == (some ? from & 63 : 0)) {
+      if (head[l] > h.s) h = {head[l], l};
+    return h;
+  };
+  Head mine = own();
+  for (int i = 0; i < K; ++i) {
+    Head h = mine;
+    h = better(h, head_dpp<0xB1>(h));   // xor 1
+    h = better(h, head_dpp<0x4E>(h));   // xor 2
+    h = better(h, head_dpp<0x141>(h));  // the other four of eight
+    h = better(h, head_dpp<0x140>(h));  // the other eight of sixteen
+    h = better(h, head_xor(h, 16));
+    h = better(h, head_xor(h, 32));
+    const bool some = h.l < lists;  // the same in every lane
+    if (lane == (some ? h.l & 63 : 0)) {
       const int64_t j = (int64_t)g * K + i;
       int r = -1, v = -1;
       if (some) {
-        r = g * W + from / splits;
-        const int p = at[from];
-        v = beams.open(r) ? (int)((1u << bits) - (uint32_t)key_of(from, p)) : beams.ended[r];
-        head[from] = score_of(from, p + 1);
-        at[from] = (uint16_t)(p + 1);
+        const int b = h.l / splits, p = at[h.l];
+        r = g * W + b;
+        v = alone[b] == -1 ? (int)((1u << bits) - (uint32_t)key_of(h.l, p)) : alone[b];
+        head[h.l] = score_of(h.l, p + 1);
+        at[h.l] = (uint16_t)(p + 1);
+        mine = own();
       }
       parent[j] = r;
       token[j] = v;
-      out_score[j] = (float)best;
+      out_score[j] = (float)h.s;
     }
   }
 }

@@ -28,6 +28,21 @@ struct Cols {
 
   __device__ __forceinline__ int col(int j) const { return (j * stride + t) * VE; }
   __device__ __forceinline__ int have(int j) const { return min(max(C - col(j), 0), VE); }
+  // f(j, i) for the entries that the row has: whole vectors without a test of each
+  template <typename F>
+  __device__ __forceinline__ void each(F f) const {
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      if (col(j) + VE <= C) {
+#pragma unroll
+        for (int i = 0; i < VE; ++i) f(j, i);
+      } else if (col(j) < C) {
+#pragma unroll
+        for (int i = 0; i < VE - 1; ++i)
+          if (col(j) + i < C) f(j, i);
+      }
+    }
+  }
   // the raw vectors, zeros past the row's end
   __device__ __forceinline__ void load(const T* row, u32x4* x) const {
 #pragma unroll
@@ -84,124 +99,137 @@ struct Cols {
   }
 };
 
-// Mean and sum of squared deviations of n values, and of two such sets together: no sum of
-// squares is formed whose difference to the mean's square would lose digits.
-struct Moments {
-  float n, m, q;
+// A barrier behind which LDS is seen; loads from memory stay under way.
+__device__ __forceinline__ void sync_lds() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
+template <int CTRL>
+__device__ __forceinline__ float dpp(float v) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xF, 0xF, false));
+}
+
+__device__ __forceinline__ float sum16(float x) {
+  x += dpp<0xB1>(x);          // xor 1
+  x += dpp<0x4E>(x);          // xor 2
+  x += dpp<0x141>(x);         // the other four of eight
+  return x + dpp<0x140>(x);   // the other eight of sixteen
+}
+
+// N sums over a row: its LPR lanes, or (LPR == 0) the whole workgroup, whose wavefronts leave theirs in
+// `red` (zeros where there is no wavefront). Every lane receives them.
+constexpr int kWaves = 16;
+template <int N>
+struct Sums {
+  float v[N];
 };
-__device__ __forceinline__ Moments join(Moments a, Moments b) {
-  const float n = a.n + b.n, f = n > 0.f ? b.n / n : 0.f, d = b.m - a.m;
-  return {n, fmaf(d, f, a.m), a.q + b.q + d * d * a.n * f};
-}
-__device__ __forceinline__ Moments shifted(Moments a, int o) {
-  return {__shfl_xor(a.n, o, 64), __shfl_xor(a.m, o, 64), __shfl_xor(a.q, o, 64)};
-}
-
-// A row's reductions over LPR lanes of a wavefront, or (LPR == 0) the whole workgroup. `red` has
-// room for the wavefronts' values twice over: rows alternate, so a row's readers and the
-// next row's writers are one barrier apart.
-template <int LPR>
-__device__ __forceinline__ Moments reduce(Moments a, Moments* red) {
-  constexpr int W = LPR ? LPR : 64;
-  if constexpr (LPR == 0) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) a = join(a, shifted(a, o));
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = a;
-    __syncthreads();
-    a = red[0];
-    for (int k = 1; k < (int)blockDim.x / 64; ++k) a = join(a, red[k]);
-  } else {
-#pragma unroll
-    for (int o = W / 2; o > 0; o >>= 1) a = join(a, shifted(a, o));
-  }
-  return a;
-}
-template <int LPR>
-__device__ __forceinline__ float2 reduce(float2 a, float2* red) {
+template <int LPR, int N>
+__device__ __forceinline__ Sums<N> reduce(Sums<N> a, Sums<N>* red) {
   constexpr int W = LPR ? LPR : 64;
 #pragma unroll
-  for (int o = W / 2; o > 0; o >>= 1) {
-    a.x += __shfl_xor(a.x, o, 64);
-    a.y += __shfl_xor(a.y, o, 64);
+  for (int i = 0; i < N; ++i) {
+    float& x = a.v[i];
+    x = sum16(x);
+    if (W > 16) x += __shfl_xor(x, 16, 64);
+    if (W > 32) x += __shfl_xor(x, 32, 64);
   }
   if constexpr (LPR == 0) {
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = a;
-    __syncthreads();
-    a = red[0];
-    for (int k = 1; k < (int)blockDim.x / 64; ++k) a = {a.x + red[k].x, a.y + red[k].y};
+    sync_lds();
+    a = red[threadIdx.x & (kWaves - 1)];
+#pragma unroll
+    for (int i = 0; i < N; ++i) a.v[i] = sum16(a.v[i]);
   }
   return a;
 }
+// The places of wavefronts that a workgroup does not have.
+template <int N>
+__device__ __forceinline__ void clear_rest(Sums<N>* red) {
+  const int k = (int)blockDim.x / 64 + threadIdx.x;
+  if (k < kWaves)
+#pragma unroll
+    for (int i = 0; i < N; ++i) red[k].v[i] = 0.f;
+}
 
+// Threads of a workgroup that takes a row: up to 512, whose registers hold four vectors of a row, the next
+// one's, parameters and sums; 1,024 for the widest fp32 rows.
 template <typename T, int NV>
-__device__ __forceinline__ Moments moments_of(const Cols<T, NV>& c, const u32x4* x) {
-  constexpr int VE = Cols<T, NV>::VE;
-  float n = 0.f, s = 0.f, q = 0.f;
-#pragma unroll
-  for (int j = 0; j < NV; ++j) {
-    n += (float)c.have(j);
-#pragma unroll
-    for (int i = 0; i < VE; ++i) s += Cols<T, NV>::get(x[j], i);  // (zeros past the end)
-  }
-  const float m = n > 0.f ? s / n : 0.f;
-#pragma unroll
-  for (int j = 0; j < NV; ++j)
-#pragma unroll
-    for (int i = 0; i < VE; ++i) {
-      const float d = i < c.have(j) ? Cols<T, NV>::get(x[j], i) - m : 0.f;
-      q = fmaf(d, d, q);
-    }
-  return {n, m, q};
-}
-
-__device__ __forceinline__ float rstd_of(Moments a, float eps) { return 1.0f / sqrtf(a.q / a.n + eps); }
+constexpr int kThreads = sizeof(T) == 4 && NV == 4 ? 1024 : 512;
 
 // LPR lanes per row, 256 / LPR rows at a time (LPR == 0: the workgroup's threads, one row); workgroups
-// stride over the rows with their parameters in registers.
+// stride over the rows with their parameters in registers, the next row on its way meanwhile. The
+// variance is a second sum, of deviations: a sum of squares would lose the digits that a large mean takes. The
+// deviations' own sum, which only the mean's rounding leaves, corrects both.
 template <typename T, int NV, int LPR>
-__global__ __launch_bounds__(LPR ? 256 : 1024) void norm_kernel(const T* __restrict__ x, int64_t ldx, int rows, int C,
+__global__ __launch_bounds__((LPR ? 256 : kThreads<T, NV>)) void norm_kernel(const T* __restrict__ x, int64_t ldx, int rows, int C,
                                                                 const float* __restrict__ w,
                                                                 const float* __restrict__ b, float eps,
                                                                 T* __restrict__ y, int64_t ldy) {
   typedef Cols<T, NV> CL;
-  constexpr int VE = CL::VE, RB = LPR ? 256 / LPR : 1;
-  __shared__ Moments red[2][16];
+  constexpr int VE = CL::VE, RB = 256 / (LPR ? LPR : 256);
+  __shared__ __attribute__((aligned(16))) Sums<1> red[2][kWaves];
+  __shared__ __attribute__((aligned(16))) Sums<2> red2[2][kWaves];
   const int tid = threadIdx.x;
   const CL c = {C, LPR ? tid % (LPR ? LPR : 1) : tid, LPR ? LPR : (int)blockDim.x};
   float wv[NV][VE], bv[NV][VE];
   c.params(w, 1.f, wv);
   c.params(b, 0.f, bv);
+  const float inv_C = 1.0f / (float)C;
+  const int64_t own = LPR ? tid / (LPR ? LPR : 1) : 0, step = (int64_t)gridDim.x * RB;
+  u32x4 next[NV];
+  c.load(x + min((int64_t)blockIdx.x * RB + own, (int64_t)rows - 1) * ldx, next);
+  if constexpr (LPR == 0)
+    for (int k = 0; k < 2; ++k) {
+      clear_rest(red[k]);
+      clear_rest(red2[k]);
+    }
   int phase = 0;
-  for (int64_t r0 = (int64_t)blockIdx.x * RB; r0 < rows; r0 += (int64_t)gridDim.x * RB, phase ^= 1) {
-    const int64_t row = r0 + (LPR ? tid / (LPR ? LPR : 1) : 0);
-    const bool live = row < rows;
+  for (int64_t r0 = (int64_t)blockIdx.x * RB; r0 < rows; r0 += step, phase ^= 1) {
+    const int64_t row = r0 + own;
     u32x4 xv[NV];
-    c.load(x + (live ? row : r0) * ldx, xv);
-    const Moments st = reduce<LPR>(moments_of(c, xv), red[phase]);
-    const float r = rstd_of(st, eps);
-    if (!live) continue;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) xv[j] = next[j];
+    if (r0 + step < rows) c.load(x + min(row + step, (int64_t)rows - 1) * ldx, next);
+    Sums<1> s = {0.f};
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+      for (int i = 0; i < VE; ++i) s.v[0] += CL::get(xv[j], i);  // (zeros past the end)
+    const float m = reduce<LPR>(s, red[phase]).v[0] / (float)C;
+    Sums<2> q = {0.f, 0.f};
+    c.each([&](int j, int i) {
+      const float d = CL::get(xv[j], i) - m;
+      q.v[0] = fmaf(d, d, q.v[0]);
+      q.v[1] += d;
+    });
+    q = reduce<LPR>(q, red2[phase]);
+    const float more = q.v[1] * inv_C, r = 1.0f / sqrtf(fmaf(fmaf(-more, q.v[1], q.v[0]), inv_C, eps));
+    if (row >= rows) continue;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       float o[VE];
 #pragma unroll
-      for (int i = 0; i < VE; ++i) o[i] = fmaf((CL::get(xv[j], i) - st.m) * r, wv[j][i], bv[j][i]);
+      for (int i = 0; i < VE; ++i) o[i] = fmaf(((CL::get(xv[j], i) - m) - more) * r, wv[j][i], bv[j][i]);
       c.store(y + row * ldy, j, o);
     }
   }
 }
 
-// The same rows backwards. Every thread keeps its columns' sums for dw and db over the rows
-// that its workgroup takes; they leave as one partial vector per workgroup (part[block][2][C]).
+// The same rows backwards; sum g (x - m) comes with the variance, so there are two reductions here as well. Every
+// thread keeps its columns' sums for dw and db over the rows that its workgroup takes; they leave as one partial
+// vector per workgroup (part[block][2][C]).
 template <typename T, int NV, int LPR>
-__global__ __launch_bounds__(LPR ? 256 : 1024) void norm_bwd_kernel(const T* __restrict__ x, int64_t ldx, int rows,
+__global__ __launch_bounds__((LPR ? 256 : kThreads<T, NV>)) void norm_bwd_kernel(const T* __restrict__ x, int64_t ldx, int rows,
                                                                     int C, const float* __restrict__ w, float eps,
                                                                     const T* __restrict__ dy, int64_t lddy,
                                                                     T* __restrict__ dx, int64_t lddx,
                                                                     float* __restrict__ part) {
   typedef Cols<T, NV> CL;
-  constexpr int VE = CL::VE, RB = LPR ? 256 / LPR : 1;
-  __shared__ Moments red[2][16];
-  __shared__ float2 red2[2][16];
+  constexpr int VE = CL::VE, RB = 256 / (LPR ? LPR : 256);
+  __shared__ __attribute__((aligned(16))) Sums<2> red[2][kWaves];
+  __shared__ __attribute__((aligned(16))) Sums<3> red2[2][kWaves];
   const int tid = threadIdx.x;
   const CL c = {C, LPR ? tid % (LPR ? LPR : 1) : tid, LPR ? LPR : (int)blockDim.x};
   float wv[NV][VE], dw[NV][VE], db[NV][VE];
@@ -211,34 +239,58 @@ __global__ __launch_bounds__(LPR ? 256 : 1024) void norm_bwd_kernel(const T* __r
 #pragma unroll
     for (int i = 0; i < VE; ++i) dw[j][i] = db[j][i] = 0.f;
   const float inv_C = 1.0f / (float)C;
+  const int64_t own = LPR ? tid / (LPR ? LPR : 1) : 0, step = (int64_t)gridDim.x * RB;
+  const int64_t first = min((int64_t)blockIdx.x * RB + own, (int64_t)rows - 1);
+  u32x4 xn[NV], gn[NV];
+  c.load(x + first * ldx, xn);
+  c.load(dy + first * lddy, gn);
+  if constexpr (LPR == 0)
+    for (int k = 0; k < 2; ++k) {
+      clear_rest(red[k]);
+      clear_rest(red2[k]);
+    }
   int phase = 0;
-  for (int64_t r0 = (int64_t)blockIdx.x * RB; r0 < rows; r0 += (int64_t)gridDim.x * RB, phase ^= 1) {
-    const int64_t row = r0 + (LPR ? tid / (LPR ? LPR : 1) : 0);
-    const bool live = row < rows;
+  for (int64_t r0 = (int64_t)blockIdx.x * RB; r0 < rows; r0 += step, phase ^= 1) {
+    const int64_t row = r0 + own;
     u32x4 xv[NV], gv[NV];
-    c.load(x + (live ? row : r0) * ldx, xv);
-    c.load(dy + (live ? row : r0) * lddy, gv);
-    const Moments st = reduce<LPR>(moments_of(c, xv), red[phase]);
-    const float r = rstd_of(st, eps);
-    float2 s = {0.f, 0.f};  // sums of g and g h (dy is zero past the row's end)
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      xv[j] = xn[j];
+      gv[j] = gn[j];
+    }
+    if (r0 + step < rows) {
+      const int64_t after = min(row + step, (int64_t)rows - 1);
+      c.load(x + after * ldx, xn);
+      c.load(dy + after * lddy, gn);
+    }
+    Sums<2> s = {0.f, 0.f};
 #pragma unroll
     for (int j = 0; j < NV; ++j)
 #pragma unroll
       for (int i = 0; i < VE; ++i) {
-        const float g = CL::get(gv[j], i) * wv[j][i];
-        s.x += g;
-        s.y = fmaf(g, (CL::get(xv[j], i) - st.m) * r, s.y);
+        s.v[0] += CL::get(xv[j], i);  // (both are zero past the row's end)
+        s.v[1] = fmaf(CL::get(gv[j], i), wv[j][i], s.v[1]);
       }
-    s = reduce<LPR>(s, red2[phase]);
-    if (!live) continue;
-    const float mg = s.x * inv_C, mgh = s.y * inv_C;
+    s = reduce<LPR>(s, red[phase]);
+    const float m = s.v[0] / (float)C, mg = s.v[1] * inv_C;
+    Sums<3> q = {0.f, 0.f, 0.f};
+    c.each([&](int j, int i) {
+      const float d = CL::get(xv[j], i) - m;
+      q.v[0] = fmaf(d, d, q.v[0]);
+      q.v[1] += d;
+      q.v[2] = fmaf(CL::get(gv[j], i) * wv[j][i], d, q.v[2]);
+    });
+    q = reduce<LPR>(q, red2[phase]);
+    const float more = q.v[1] * inv_C, r = 1.0f / sqrtf(fmaf(fmaf(-more, q.v[1], q.v[0]), inv_C, eps));
+    const float mgh = fmaf(-more, s.v[1], q.v[2]) * inv_C * r * r;  // (times r)
+    if (row >= rows) continue;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       float o[VE];
 #pragma unroll
       for (int i = 0; i < VE; ++i) {
-        const float d = CL::get(gv[j], i), h = (CL::get(xv[j], i) - st.m) * r;
-        o[i] = r * (fmaf(d, wv[j][i], -mg) - h * mgh);
+        const float d = CL::get(gv[j], i), h = ((CL::get(xv[j], i) - m) - more) * r;
+        o[i] = fmaf(r, fmaf(d, wv[j][i], -mg), -h * mgh);
         dw[j][i] = fmaf(d, h, dw[j][i]);
         db[j][i] += d;
       }
@@ -290,7 +342,8 @@ __global__ __launch_bounds__(LPR ? 256 : 1024) void norm_bwd_kernel(const T* __r
 }
 
 // A row's vectors over the fewest lanes that hold it in one vector each, from 16 of them to a
-// wavefront; wider rows take a workgroup.
+// wavefront (two vectors up to 128); wider rows take a workgroup, with two vectors a thread from 256 on, which halve what the
+// reductions cost.
 struct Shape {
   int nv, lpr;   // vectors per thread; lanes per row, 0: the workgroup
   int threads;
@@ -302,19 +355,20 @@ Shape shape_of(bool bf16, int C) {
   if (v <= 32) return {1, 32, 256, 8};
   if (v <= 64) return {1, 64, 256, 4};
   if (v <= 128) return {2, 64, 256, 4};
-  const int nv = v <= 1024 ? 1 : v <= 2048 ? 2 : 4;
+  const int nv = v <= 256 ? 1 : v <= 1024 ? 2 : 4;
   return {nv, 0, ((v + nv - 1) / nv + 63) / 64 * 64, 1};
 }
 
-// Workgroups of the gradients: each leaves a partial vector, so no more than fill the GPU twice over.
+// Workgroups of the gradients: each leaves a partial vector, so as many as the registers let run at once (some 1,024
+// threads a CU) and no more: with twice as many the sums take 14 us instead of 8 at 5,120 columns.
 int bwd_parts(const Shape& s, int rows) {
-  const int fill = 256 * std::max(1, 2048 / s.threads);
+  const int fill = 256 * std::max(1, 1024 / s.threads);
   return std::min((rows + s.rows - 1) / s.rows, fill);
 }
 
 template <typename T, int NV, int LPR>
 hipError_t fwd(const NormOp& a, const Shape& sh, void* y, int64_t ldy, hipStream_t s) {
-  const int grid = std::min((a.rows + sh.rows - 1) / sh.rows, 256 * 8);
+  const int grid = std::min((a.rows + sh.rows - 1) / sh.rows, 256 * std::max(1, 2048 / sh.threads));
   norm_kernel<T, NV, LPR><<<grid, sh.threads, 0, s>>>(static_cast<const T*>(a.x), a.ldx, a.rows, a.C, a.w, a.b, a.eps,
                                                       static_cast<T*>(y), ldy);
   return hipGetLastError();
