@@ -7,6 +7,7 @@
 // aligned address and the row's start, and only the first and the last vector of a
 // row are read entry by entry.
 #include <algorithm>
+#include <type_traits>
 
 #include "common.h"
 #include "ops.h"
@@ -456,113 +457,136 @@ __global__ __launch_bounds__(kTB) void logprobs_join_kernel(LogitRows a, int K, 
 // sorted, so every round takes the best of the lists' heads. Scores are compared in 64 bits: fp32 would make
 // neighbours equal that a long search's sum of log probabilities (-100: steps of 8e-6) cannot tell
 // apart. Equal scores: the lower row, then the lower token, which is the lower list, as splits are in their
-// rows' order. A wavefront runs the rounds, out of LDS where the lists fit; a lane has its lists' best head
-// in registers, so that a round is the reduction over lanes and one lane's step on.
+// rows' order. All scores are formed at once, as numbers that rise with them (0: none); then a wavefront runs the
+// rounds, each the largest of its lanes' heads (the high halves as a rule tell) and one lane's step on, out of LDS
+// where the lists fit: some 0.3 us.
 constexpr int kBeamLists = 1024;  // W x splits
-constexpr int kBeamKeys = 4096;   // keys held in LDS
+constexpr int kBeamKeys = 4096;   // candidates held in LDS
 
-// The larger of two scores, of equal ones the lower list.
-struct Head {
-  double s;
-  int l;
-};
-__device__ __forceinline__ Head better(Head a, Head b) { return b.s > a.s || (b.s == a.s && b.l < a.l) ? b : a; }
-template <int CTRL>
-__device__ __forceinline__ Head head_dpp(Head h) {
-  const uint64_t u = __builtin_bit_cast(uint64_t, h.s);
-  auto mov = [](uint32_t x) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xF, 0xF, false); };
-  return {__builtin_bit_cast(double, (uint64_t)mov((uint32_t)(u >> 32)) << 32 | mov((uint32_t)u)), (int)mov((uint32_t)h.l)};
+__device__ __forceinline__ u64 order_of(double s) {  // 0 for -inf and NaN
+  if (!(s > -(double)INFINITY)) return 0;
+  const u64 u = __builtin_bit_cast(u64, s + 0.0);  // (-0 as 0)
+  return u >> 63 ? ~u : u | 1ull << 63;
 }
-__device__ __forceinline__ Head head_xor(Head h, int o) { return {__shfl_xor(h.s, o, 64), __shfl_xor(h.l, o, 64)}; }
+__device__ __forceinline__ double score_of(u64 k) {
+  return k == 0 ? -(double)INFINITY : __builtin_bit_cast(double, k >> 63 ? k & ~(1ull << 63) : ~k);
+}
+// The largest over a wavefront.
+__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
+  auto turn = [](uint32_t x, auto ctrl) {
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, decltype(ctrl)::value, 0xF, 0xF, false);
+  };
+  v = max(v, turn(v, std::integral_constant<int, 0x128>()));  // rows of 16 lanes, turned by 8, 4, 2, 1
+  v = max(v, turn(v, std::integral_constant<int, 0x124>()));
+  v = max(v, turn(v, std::integral_constant<int, 0x122>()));
+  v = max(v, turn(v, std::integral_constant<int, 0x121>()));
+  auto of = [&](int l) { return (uint32_t)__builtin_amdgcn_readlane((int)v, l); };
+  return max(max(of(0), of(16)), max(of(32), of(48)));
+}
 
 template <typename T>
 __global__ __launch_bounds__(kTB) void beam_join_kernel(LogitRows a, int W, int K, int splits, Beams beams,
                                                         int* __restrict__ parent, int* __restrict__ token,
                                                         float* __restrict__ out_score, const char* __restrict__ ws) {
-  __shared__ u64 keys[kBeamKeys];
-  __shared__ double head[kBeamLists];   // a list's best score that is left
+  __shared__ u64 keys[kBeamKeys], order[kBeamKeys];
+  __shared__ u64 head[kBeamLists];      // a list's best score that is left
   __shared__ uint16_t at[kBeamLists];   // and its place
+  __shared__ Stats part[kBeamLists];
   __shared__ double base[64], top[64];  // score - log of the sum; the maximum
+  __shared__ float own_score[64];
   __shared__ int alone[64];             // -1: an open beam; else it has ended with this token (-2: dead)
-  const int g = blockIdx.x, tid = threadIdx.x, lane = tid & 63, lists = W * splits;
+  __shared__ int from[kMaxTop];         // the candidates taken: list * K + place
+  __shared__ u64 taken[kMaxTop];
+  const int g = blockIdx.x, tid = threadIdx.x, lane = tid & 63, lists = W * splits, N = lists * K;
   const float zc = a.inv_temp * kLog2e;
   const double it = a.inv_temp;
-  constexpr double kNone = -(double)INFINITY;
   const char* w = ws + (int64_t)g * lists * split_stride(K);
-  const bool held = lists * K <= kBeamKeys;
+  const bool held = N <= kBeamKeys;
+  auto key_of = [&](int l, int i) {
+    return held ? keys[l * K + i] : reinterpret_cast<const u64*>(w + (int64_t)l * split_stride(K))[i];
+  };
+  // all that is read from memory at once (of rows that were not read whatever is there, for nothing)
+  if (held)
+    for (int q = tid; q < N; q += kTB) keys[q] = reinterpret_cast<const u64*>(w + (int64_t)(q / K) * split_stride(K))[q % K];
+  for (int l = tid; l < lists; l += kTB) part[l] = *reinterpret_cast<const Stats*>(w + (int64_t)l * split_stride(K) + (int64_t)K * 8);
+  if (tid < W) {
+    const float score = beams.score[g * W + tid];
+    const int ended = beams.ended ? beams.ended[g * W + tid] : -1;
+    own_score[tid] = score;
+    alone[tid] = !(score > -INFINITY) ? -2 : ended >= 0 ? ended : -1;
+  }
+  __syncthreads();
   for (int b = tid >> 6; b < W; b += kTB / 64) {
-    const int r = g * W + b;
-    const float score = beams.score[r];
-    const int ended = beams.ended ? beams.ended[r] : -1;
-    const int kind = !(score > -INFINITY) ? -2 : ended >= 0 ? ended : -1;
     Stats st = {-INFINITY, 0.f, 0.f};
-    if (kind == -1) {  // (uniform over the wavefront)
-      for (int k = lane; k < splits; k += 64)
-        st = merge(st, *reinterpret_cast<const Stats*>(w + (int64_t)(b * splits + k) * split_stride(K) + (int64_t)K * 8), zc);
-      if (splits > 1) st = wave_merge(st, zc);
-    }
+    for (int k = lane; k < splits; k += 64) st = merge(st, part[b * splits + k], zc);
+    if (splits > 1) st = wave_merge(st, zc);
     if (lane == 0) {
-      alone[b] = kind;
-      base[b] = kind == -1 ? (double)score - log((double)st.s) : (double)score;
+      base[b] = alone[b] == -1 ? (double)own_score[b] - log((double)st.s) : (double)own_score[b];
       top[b] = st.m;
     }
   }
   __syncthreads();
-  if (held)
-    for (int q = tid; q < lists * K; q += kTB)
-      if (alone[q / (K * splits)] == -1)
-        keys[q] = reinterpret_cast<const u64*>(w + (int64_t)(q / K) * split_stride(K))[q % K];
-  __syncthreads();
-  auto key_of = [&](int l, int i) {
-    return held ? keys[l * K + i] : reinterpret_cast<const u64*>(w + (int64_t)l * split_stride(K))[i];
-  };
-  // (NaN, of a row with a logit of +inf, is no score)
-  auto score_of = [&](int l, int i) {
+  auto make = [&](int l, int i) {
     const int b = l / splits;
-    if (alone[b] != -1) return i == 0 && l % splits == 0 && alone[b] >= 0 ? base[b] : kNone;  // itself, once
-    const u64 k = i < K ? key_of(l, i) : 0;
-    if (!k) return kNone;
-    const double s = base[b] + ((double)ord_value<T>((uint32_t)(k >> 32)) - top[b]) * it;
-    return s > kNone ? s : kNone;
+    if (alone[b] != -1) return i == 0 && l % splits == 0 && alone[b] >= 0 ? order_of(base[b]) : 0;  // itself, once
+    const u64 k = key_of(l, i);
+    return k ? order_of(base[b] + ((double)ord_value<T>((uint32_t)(k >> 32)) - top[b]) * it) : 0;
   };
+  if (held)
+    for (int q = tid; q < N; q += kTB) order[q] = make(q / K, q % K);
+  __syncthreads();
+  auto next_of = [&](int l, int i) { return i >= K ? 0 : held ? order[l * K + i] : make(l, i); };
   for (int l = tid; l < lists; l += kTB) {
-    head[l] = score_of(l, 0);
+    head[l] = next_of(l, 0);
     at[l] = 0;
+  }
+  if (tid < kMaxTop) {
+    from[tid] = -1;
+    taken[tid] = 0;
   }
   __syncthreads();
   if (tid >= 64) return;
-  const int bits = index_bits(a.V);
-  auto own = [&]() {  // the best of the lane's lists
-    Head h = {kNone, lists};
+  // the best of the lane's lists (of equal ones the lowest), as a rule the one that it has
+  u64 key = 0;
+  int mine = lane;
+  auto own = [&]() {
+    key = 0;
     for (int l = lane; l < lists; l += 64)
-      if (head[l] > h.s) h = {head[l], l};
-    return h;
-  };
-  Head mine = own();
-  for (int i = 0; i < K; ++i) {
-    Head h = mine;
-    h = better(h, head_dpp<0xB1>(h));   // xor 1
-    h = better(h, head_dpp<0x4E>(h));   // xor 2
-    h = better(h, head_dpp<0x141>(h));  // the other four of eight
-    h = better(h, head_dpp<0x140>(h));  // the other eight of sixteen
-    h = better(h, head_xor(h, 16));
-    h = better(h, head_xor(h, 32));
-    const bool some = h.l < lists;  // the same in every lane
-    if (lane == (some ? h.l & 63 : 0)) {
-      const int64_t j = (int64_t)g * K + i;
-      int r = -1, v = -1;
-      if (some) {
-        const int b = h.l / splits, p = at[h.l];
-        r = g * W + b;
-        v = alone[b] == -1 ? (int)((1u << bits) - (uint32_t)key_of(h.l, p)) : alone[b];
-        head[h.l] = score_of(h.l, p + 1);
-        at[h.l] = (uint16_t)(p + 1);
-        mine = own();
+      if (head[l] > key) {
+        key = head[l];
+        mine = l;
       }
-      parent[j] = r;
-      token[j] = v;
-      out_score[j] = (float)h.s;
+  };
+  own();
+  for (int i = 0; i < K; ++i) {
+    const uint32_t hi = (uint32_t)(key >> 32), lo = (uint32_t)key;
+    u64 best = __ballot(hi == wave_max(hi));
+    if (best & (best - 1)) {  // more than one: by the low halves, then by the list
+      const bool in = best >> lane & 1;
+      best &= __ballot(lo == wave_max(in ? lo : 0u));
+      if (best & (best - 1)) best &= __ballot(~mine == (int)wave_max(best >> lane & 1 ? (uint32_t)~mine : 0u));
     }
+    if (lane == __ffsll(best) - 1 && key) {
+      const int p = at[mine];
+      from[i] = mine * K + p;
+      taken[i] = key;
+      at[mine] = (uint16_t)(p + 1);
+      const u64 k = next_of(mine, p + 1);
+      head[mine] = k;
+      key = k;
+      if (lists > 64) own();
+    }
+  }
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+  const int bits = index_bits(a.V);
+  if (lane < K) {  // (K <= kMaxTop, a wavefront's lanes)
+    const int64_t j = (int64_t)g * K + lane;
+    const int q = from[lane], l = q / K, b = l / splits;
+    parent[j] = q < 0 ? -1 : g * W + b;
+    token[j] = q < 0 ? -1 : alone[b] == -1 ? (int)((1u << bits) - (uint32_t)key_of(l, q % K)) : alone[b];
+    out_score[j] = (float)score_of(taken[lane]);
   }
 }
 
