@@ -31,9 +31,9 @@ constexpr int kTParts = kMat / 2 * 3;  // floats that T's three bf16 parts take
 // Parts behind an answer: bf16 does not show what two leave out (2^-16).
 template <typename T>
 constexpr int kOutParts = sizeof(T) == 2 ? 2 : 3;
-// Floats of a chunk's matrices: T and P in parts, or for the gradients T in parts, T^T and P^T.
+// Floats of a chunk's matrices in parts: T and P, or for the gradients T, T^T and P^T.
 template <typename T, bool GRADS>
-constexpr int kMats = GRADS ? kTParts + 2 * kMat : kTParts + kMat / 2 * kOutParts<T>;
+constexpr int kMats = GRADS ? 3 * kTParts : kTParts + kMat / 2 * kOutParts<T>;
 
 __device__ __forceinline__ float to_f32(float v) { return v; }
 __device__ __forceinline__ float to_f32(uint16_t v) { return bf16_to_f32(v); }
@@ -61,6 +61,24 @@ __device__ __forceinline__ float exp_of(double x) {
   return ldexpf(__builtin_amdgcn_exp2f((float)(t - n)), n < -1000.0 ? -1000 : n > 1000.0 ? 1000 : (int)n);
 }
 __device__ __forceinline__ double log_decay(float g) { return g < -1e4f ? -1e4 : (double)g; }
+
+// What lane `lane` of a wavefront has of an array at a wave-uniform address: a scalar base and a 32-bit offset (left
+// to itself the compiler adds them up in vector registers); entries may start anywhere that their parts allow.
+typedef __attribute__((address_space(1))) char gchar;
+template <typename P>
+__device__ __forceinline__ gchar* uniform(const P* p) {
+  const uint64_t x = reinterpret_cast<uint64_t>(p);
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)x), hi = __builtin_amdgcn_readfirstlane((uint32_t)(x >> 32));
+  return (gchar*)((uint64_t)hi << 32 | lo);
+}
+template <typename V, typename P>
+__device__ __forceinline__ V at_lane(const P* p, int lane) {
+  return *(const __attribute__((address_space(1))) V*)(uniform(p) + (uint32_t)(lane * (int)sizeof(V)));
+}
+template <typename V, typename P>
+__device__ __forceinline__ V at_bytes(const P* p, uint32_t bytes) {
+  return {*(const __attribute__((address_space(1))) typename V::loose*)(uniform(p) + bytes)};
+}
 
 struct DeltaIn {
   const int* offs;
@@ -209,11 +227,6 @@ __device__ __forceinline__ floatx4 frag_t(const float* p, int ld, int s) {
   const float* q = p + (16 * s + 4 * (l >> 4)) * ld + (l & 15);
   return floatx4{q[0], q[ld], q[2 * ld], q[3 * ld]};
 }
-// A matrix [kC, kC] as fragments: of the 16 rows 16 w .. fragment s.
-__device__ __forceinline__ floatx4 mat_frag(const float* m, int w, int s) {
-  return *reinterpret_cast<const floatx4*>(m + ((w * 4 + s) * 64 + (threadIdx.x & 63)) * 4);
-}
-
 // fp32-level products on the bf16 matrix cores: a value is a sum of three bf16 parts, each 2^-8 of the one in
 // front (split3_pair), and of two values' nine products of parts the six down to 2^-16 count. What is bf16 in memory
 // is one part. v_mfma_f32_16x16x32_bf16: lane l holds A[l % 16] and B[..][l % 16] at eight k's (which eight of the
@@ -283,12 +296,18 @@ template <> struct Raw8<uint16_t> {
   u32x4 v;
   typedef u32x4 any __attribute__((aligned(2)));
   __device__ __forceinline__ void load(const uint16_t* p) { v = *reinterpret_cast<const any*>(p); }
+  // what lane `lane` has of an operand, eight entries each
+  __device__ __forceinline__ void load_lane(const uint16_t* p, int lane) { v = at_lane<u32x4>(p, lane); }
   __device__ __forceinline__ void clear() { v = u32x4{0, 0, 0, 0}; }
   __device__ __forceinline__ Parts<1> parts() const { return {{pack8(v)}}; }
 };
 template <> struct Raw8<float> {
   floatx4 a, b;
   __device__ __forceinline__ void load(const float* p) { a = ld4(p); b = ld4(p + 4); }
+  __device__ __forceinline__ void load_lane(const float* p, int lane) {
+    a = at_lane<floatx4>(p, 2 * lane);
+    b = at_lane<floatx4>(p, 2 * lane + 1);
+  }
   __device__ __forceinline__ void clear() { a = b = floatx4{0.f, 0.f, 0.f, 0.f}; }
   __device__ __forceinline__ Parts<3> parts() const { return split8<3>(a, b); }
 };
@@ -296,14 +315,21 @@ template <> struct Raw8<float> {
 template <typename T> struct Raw4;
 template <> struct Raw4<uint16_t> {
   u32x2 v;
+  typedef u32x2_any loose;
   __device__ __forceinline__ void load(const uint16_t* p) { v = *reinterpret_cast<const u32x2_any*>(p); }
   __device__ __forceinline__ void store(uint16_t* p) const { *reinterpret_cast<u32x2_any*>(p) = v; }
 };
 template <> struct Raw4<float> {
   floatx4 v;
+  typedef floatx4_any loose;
   __device__ __forceinline__ void load(const float* p) { v = ld4(p); }
   __device__ __forceinline__ void store(float* p) const { st4(p, v); }
 };
+__device__ __forceinline__ floatx4 widen(Raw4<float> x) { return x.v; }
+__device__ __forceinline__ floatx4 widen(Raw4<uint16_t> x) {
+  return floatx4{__uint_as_float(x.v[0] << 16), __uint_as_float(x.v[0] & 0xFFFF0000u), __uint_as_float(x.v[1] << 16),
+                 __uint_as_float(x.v[1] & 0xFFFF0000u)};
+}
 // In products over tokens, the eight of lane group kq of the 32 from 32 s on: 32 s + 16 a + 4 kq + m at
 // place 4 a + m. So the four tokens of a lane's results are neighbours in LDS, and two fragments (frag) of a
 // matrix are one operand. Where token t = 16 w + 4 lk stands:
@@ -404,29 +430,32 @@ __global__ __launch_bounds__(256) void delta_prep_kernel(DeltaIn a, const T* __r
       qk[t] = y.sum();
     }
   }
-  // K, Q and K^T as operands: a chunk's rows are a model's width apart, and every slice of every head that
+  // K, Q (for the gradients Q^T) and K^T as operands: a chunk's rows are a model's width apart, and every slice of every head that
   // reads them so would ask one channel of the cache for all of them
   {
     T* out = ops + ((int64_t)tile * a.Hk + hk) * 3 * DKP * kC;
 #pragma unroll
     for (int s = 0; s < NS; ++s) {
       *reinterpret_cast<Raw8<T>*>(out + ((w * NS + s) * 64 + lane) * 8) = kf[s];
-      *reinterpret_cast<Raw8<T>*>(out + DKP * kC + ((w * NS + s) * 64 + lane) * 8) = qf[s];
+      if constexpr (!GRADS) *reinterpret_cast<Raw8<T>*>(out + DKP * kC + ((w * NS + s) * 64 + lane) * 8) = qf[s];
     }
-    out += 2 * DKP * kC;
+    auto across = [&](const T* m, int64_t ld, T* to) {  // a chunk's rows as operands over tokens
 #pragma unroll
-    for (int f = w; f < DKP / 16 * 2; f += 4) {
-      const int col = 16 * (f >> 1) + li;
-      alignas(16) T v[8];
+      for (int f = w; f < DKP / 16 * 2; f += 4) {
+        const int col = 16 * (f >> 1) + li;
+        alignas(16) T v[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int t = 32 * (f & 1) + 16 * (i >> 2) + 4 * lk + (i & 3);
-        v[i] = t < c.n && col < a.Dk ? kp[(c.row + t) * a.ldk + col] : T(0);
+        for (int i = 0; i < 8; ++i) {
+          const int t = 32 * (f & 1) + 16 * (i >> 2) + 4 * lk + (i & 3);
+          v[i] = t < c.n && col < a.Dk ? m[(c.row + t) * ld + col] : T(0);
+        }
+        Raw8<T> x;
+        x.load(v);
+        *reinterpret_cast<Raw8<T>*>(to + (f * 64 + lane) * 8) = x;
       }
-      Raw8<T> x;
-      x.load(v);
-      *reinterpret_cast<Raw8<T>*>(out + (f * 64 + lane) * 8) = x;
-    }
+    };
+    across(kp, a.ldk, out + 2 * DKP * kC);
+    if constexpr (GRADS) across(q + (int64_t)hk * a.Dk, a.ldq, out + DKP * kC);
   }
   const int share = a.H / a.Hk;
   for (int hv = 0; hv < share; ++hv) {
@@ -520,10 +549,10 @@ __global__ __launch_bounds__(256) void delta_prep_kernel(DeltaIn a, const T* __r
     uint16_t* tp = reinterpret_cast<uint16_t*>(out);
     if constexpr (GRADS) {
 #pragma unroll
-      for (int s = 0; s < 4; ++s) {
-        float* p = out + kTParts + ((w * 4 + s) * 64 + lane) * 4;
-        *reinterpret_cast<floatx4*>(p) = frag_t(sT + 16 * w, kLdM, s);
-        *reinterpret_cast<floatx4*>(p + kMat) = frag_t(sA + 16 * w, kLdM, s);
+      for (int s = 0; s < 2; ++s) {
+        if (s < w >> 1) continue;  // (zeros)
+        put_mat<3>(tp + 2 * kTParts, w, s, frag_t(sT + 16 * w, kLdM, 2 * s), frag_t(sT + 16 * w, kLdM, 2 * s + 1));
+        put_mat<3>(tp + 4 * kTParts, w, s, frag_t(sA + 16 * w, kLdM, 2 * s), frag_t(sA + 16 * w, kLdM, 2 * s + 1));
       }
     }
 #pragma unroll
@@ -780,138 +809,207 @@ __global__ __launch_bounds__(SAVE ? 256 : 512) void delta_chunk_kernel(
 //          + sum_(j < t) (w k.(U dS1^T))_j + e^G_C <S0, dS1>
 // all chunks at once. (dg_t is what passes over token t; as sums of such terms alone, without differences of
 // the chunk's totals, it keeps its digits where a token forgets nearly all.)
-template <typename T, int DKP, int DVS>
-__global__ __launch_bounds__(256) void delta_back_kernel(DeltaIn a, const T* __restrict__ q, const T* __restrict__ k,
-                                                         const T* __restrict__ d_o, int64_t lddo,
-                                                         const float* __restrict__ mats,
-                                                         const float* __restrict__ coef,
+// Two kinds of wavefronts as in the forward walk: four of 16 tokens each form dU and dR, and put what dO gives into
+// LDS for the next chunk; four more the state's adjoint, Q^T (e dO) while dU and dR come about.
+template <typename T, int DKP>
+__global__ __launch_bounds__(512) void delta_back_kernel(DeltaIn a, const T* __restrict__ d_o, int64_t lddo,
+                                                         const float* __restrict__ mats, const float* __restrict__ coef,
+                                                         const T* __restrict__ ops,
                                                          const float* __restrict__ dstate_out, float* __restrict__ dstate,
                                                          T* __restrict__ dv, int64_t lddv, float* __restrict__ ds1,
                                                          float* __restrict__ drs) {
-  constexpr int NF = DKP / 16, NT = DKP / 64, MB = DVS / 16, LDS = DKP + 4;
-  __shared__ __attribute__((aligned(16))) float sS[DVS * LDS], sK[kC * LDS], sQ[kC * LDS], sO[DVS * kLdM],
-      sU[DVS * kLdM];
-  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, li = lane & 15, lk = lane >> 4;
-  const int parts = (a.Dv + DVS - 1) / DVS;
-  const int c0 = (int)(blockIdx.x % parts) * DVS, h = (int)(blockIdx.x / parts % a.H),
-            seq = (int)(blockIdx.x / parts / a.H), hk = h / (a.H / a.Hk);
+  constexpr int NS = DKP / 32, NT = DKP / 64, LS = DKP + 8, LR = kC + 8, KP = sizeof(T) == 2 ? 1 : 3, LV = 20;
+  __shared__ __attribute__((aligned(16))) uint16_t sS[3 * 16 * LS], sO[KP * 16 * LR], sE[3 * 16 * LR], sU[3 * 16 * LR],
+      sW[3 * 16 * LR];
+  __shared__ __attribute__((aligned(16))) float sV[4][16 * LV];
+  const int tid = threadIdx.x, lane = tid & 63, li = lane & 15, lk = lane >> 4;
+  const int wv = __builtin_amdgcn_readfirstlane(tid >> 6), w = wv & 3;
+  const int parts = (a.Dv + 15) / 16;
+  int head, part;
+  head_and_part(blockIdx.x, a.n_seq * a.H, parts, head, part);
+  const int c0 = part * 16, h = head % a.H, seq = head / a.H, hk = h / (a.H / a.Hk);
   const int base = min(max(a.offs ? a.offs[seq] : seq, 0), a.rows),
             len = a.offs ? min(max(a.offs[seq + 1], base), a.rows) - base : 1;
   const int key = !a.offs || kC > a.rows ? seq : base / kC + seq;
-  const T* kp = k + (int64_t)hk * a.Dk;
-  const T* qp = q + (int64_t)hk * a.Dk;
-  const int t = 16 * w + li;
-  floatx4 st[MB][NT];
-  auto at = [&](int m, int n) { return (int64_t)(16 * (NT * w + n) + li) * a.Dv + c0 + 16 * m + 4 * lk; };
-  auto in = [&](int m, int n) { return 16 * (NT * w + n) + li < a.Dk && c0 + 16 * m + 4 * lk < a.Dv; };
-  const int64_t head = (int64_t)a.Dk * a.Dv;
+  const bool col = c0 + li < a.Dv;
+  const int64_t size = (int64_t)a.Dk * a.Dv;
+  const int place = token_place(w, lk);
+  floatx4 st[NT];  // entries [16 (NT w + n) + 4 lk + r][c0 + li], of the last four wavefronts
+  auto at = [&](int n) { return (int64_t)(16 * (NT * w + n) + 4 * lk) * a.Dv + c0 + li; };
+  auto in = [&](int n) { return 16 * (NT * w + n) + 4 * lk < a.Dk && col; };
+  auto keep = [&](float* p, int n) {
+    if (in(n))
 #pragma unroll
-  for (int m = 0; m < MB; ++m)
+      for (int r = 0; r < 4; ++r) p[at(n) + (int64_t)r * a.Dv] = st[n][r];
+  };
+  auto share = [&]() {
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      st[m][n] = floatx4{0.f, 0.f, 0.f, 0.f};
-      if (dstate_out && in(m, n))
-        st[m][n] = *reinterpret_cast<const floatx4*>(dstate_out + ((int64_t)seq * a.H + h) * head + at(m, n));
+    for (int n = 0; n < NT; ++n) put_parts<3>(sS + li * LS + 16 * (NT * w + n) + 4 * lk, 16 * LS, st[n]);
+  };
+  const int chunks = (len + kC - 1) / kC;
+  auto chunk = [&](int ch) { return Chunk{base + ch * kC, min(kC, len - ch * kC)}; };
+  auto mat = [&](int ch, int i) {
+    return reinterpret_cast<const uint16_t*>(mats + ((int64_t)(key + ch) * a.H + h) * kMats<T, true> + i * kTParts);
+  };
+  auto op = [&](int ch, int i) { return ops + (((int64_t)(key + ch) * a.Hk + hk) * 3 + i) * DKP * kC; };
+  auto factor = [&](int ch, int i) {
+    return at_lane<floatx4>(coef + ((int64_t)(key + ch) * a.H + h) * 3 * kC + i * kC + 16 * w, lk);
+  };
+  auto load_tiles = [&](Raw8<T> (*f)[2], const T* p) {
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int s = 0; s < 2; ++s) f[n][s].load_lane(p + (2 * (NT * w + n) + s) * 512, lane);
+  };
+  if (wv < 4) {
+    const int cv = c0 + 4 * (lane & 3), tv = 16 * w + lane / 4, s0 = w >> 1;  // the first 32 tokens that T^T's rows reach
+    float* mine = sV[wv];
+    floatx4* rows = reinterpret_cast<floatx4*>(mine + lane / 4 * LV + 4 * (lane & 3));
+    Raw8<T> rf[NS];
+    Raw4<T> ov;
+    Parts<3> pf[2], tf[2];
+    floatx4 beta, e, wj;
+    auto load_rows = [&](int ch) {
+#pragma unroll
+      for (int s = 0; s < NS; ++s) rf[s].load_lane(op(ch, 0) + (w * NS + s) * 512, lane);
+    };
+    auto load_mat = [&](Parts<3>* f, const uint16_t* m) {
+      f[0] = mat_parts<3>(m, w, s0);
+      f[1] = mat_parts<3>(m, w, 1);
+    };
+    auto load_o = [&](int ch) {
+      const Chunk c = chunk(ch);
+      ov = at_bytes<Raw4<T>>(d_o + c.row * lddo + (int64_t)h * a.Dv,
+                             (uint32_t)(min(tv, c.n - 1) * (int)lddo + min(cv, a.Dv - 4)) * (uint32_t)sizeof(T));
+    };
+    // dO and scale e^G dO, zeros past the chunk's end, as columns into LDS
+    auto put_o = [&](int ch) {
+      const Chunk c = chunk(ch);
+      *rows = widen(ov);
+      sync_wave();
+      floatx4 x;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) x[r] = 16 * w + 4 * lk + r < c.n ? mine[(4 * lk + r) * LV + li] : 0.f;
+      put_parts<KP>(sO + li * LR + place, 16 * LR, x);
+      put_parts<3>(sE + li * LR + place, 16 * LR, x * e * a.scale);
+      sync_wave();
+    };
+    if (chunks > 0) {
+      const int ch = chunks - 1;
+      load_o(ch);
+      e = factor(ch, 1);
+      load_rows(ch);
+      wj = factor(ch, 2);
+      load_mat(pf, mat(ch, 2));
+      load_mat(tf, mat(ch, 1));
+      beta = factor(ch, 0);
+      put_o(ch);
     }
-  for (int ch = (len + kC - 1) / kC - 1; ch >= 0; --ch) {
-    const Chunk c = {base + ch * kC, min(kC, len - ch * kC)};
-    const int64_t th = (int64_t)(key + ch) * a.H + h;
-    const float* mat = mats + th * kMats<T, true> + kTParts;  // T^T, P^T
-    const float* co = coef + th * 3 * kC;
+    sync_lds();
+    for (int ch = chunks - 1; ch >= 0; --ch) {
+      const Chunk c = chunk(ch);
+      const int next = max(ch - 1, 0);
+      // ---- dU
+      Acc acc;
+      acc.clear();
 #pragma unroll
-    for (int m = 0; m < MB; ++m)
+      for (int s = 0; s < NS; ++s)
+        mma32<2>(rf[s].parts(), get_parts<3>(sS + li * LS + 32 * s + 8 * lk, 16 * LS), acc);
+      load_o(next);
+      load_rows(next);
+      const floatx4 y = acc.sum();
+      acc.clear();
+#pragma unroll
+      for (int s = 0; s < 2; ++s)
+        if (s >= s0) mma32<2>(pf[s], get_parts<KP>(sO + li * LR + 32 * s + 8 * lk, 16 * LR), acc);
+      load_mat(pf, mat(next, 2));
+      floatx4 x = acc.sum() + y * wj;
+      put_parts<3>(sU + li * LR + place, 16 * LR, x);
+      wj = factor(next, 2);
+      sync_lds();
+      // ---- dR
+      acc.clear();
+#pragma unroll
+      for (int s = 0; s < 2; ++s)
+        if (s >= s0) mma32<2>(tf[s], get_parts<3>(sU + li * LR + 32 * s + 8 * lk, 16 * LR), acc);
+      load_mat(tf, mat(next, 1));
+      const floatx4 dr = acc.sum();
+      put_parts<3>(sW + li * LR + place, 16 * LR, -(dr * beta * e));
+      sync_lds();
+      // ---- what leaves, and the next chunk's dO
+#pragma unroll
+      for (int r = 0; r < 4; ++r) mine[(4 * lk + r) * LV + li] = dr[r];
+      sync_wave();
+      const floatx4 row = *rows;
+      sync_wave();
+#pragma unroll
+      for (int r = 0; r < 4; ++r) mine[(4 * lk + r) * LV + li] = dr[r] * beta[r];
+      sync_wave();
+      const floatx4 rowb = *rows;
+      sync_wave();
+      beta = factor(next, 0);
+      e = factor(next, 1);
+      if (ch > 0) put_o(next);
+      if (tv < c.n && cv < a.Dv) {
+        *reinterpret_cast<floatx4*>(drs + ((int64_t)(c.row + tv) * a.H + h) * a.Dv + cv) = row;
+        st4(dv + (c.row + tv) * lddv + (int64_t)h * a.Dv + cv, rowb);
+      }
+      sync_lds();
+    }
+    return;
+  }
+  Raw8<T> qt[NT][2], kt[NT][2];
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    st[n] = floatx4{0.f, 0.f, 0.f, 0.f};
+    if (dstate_out && in(n))
+#pragma unroll
+      for (int r = 0; r < 4; ++r) st[n][r] = dstate_out[((int64_t)seq * a.H + h) * size + at(n) + (int64_t)r * a.Dv];
+  }
+  share();
+  float eC = 0.f;
+  if (chunks > 0) {
+    load_tiles(qt, op(chunks - 1, 1));
+    load_tiles(kt, op(chunks - 1, 2));
+    eC = at_lane<float>(coef + ((int64_t)(key + chunks - 1) * a.H + h) * 3 * kC + 2 * kC - 1, 0);
+  }
+  sync_lds();
+  for (int ch = chunks - 1; ch >= 0; --ch) {
+    const int next = max(ch - 1, 0);
+#pragma unroll
+    for (int n = 0; n < NT; ++n) keep(ds1 + ((int64_t)(key + ch) * a.H + h) * size, n);
+    Acc acc[NT];
+    {
+      Parts<3> ef[2];
+#pragma unroll
+      for (int s = 0; s < 2; ++s) ef[s] = get_parts<3>(sE + li * LR + 32 * s + 8 * lk, 16 * LR);
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
+        acc[n].clear();
 #pragma unroll
-        for (int r = 0; r < 4; ++r) sS[(16 * m + 4 * lk + r) * LDS + 16 * (NT * w + n) + li] = st[m][n][r];
-        if (in(m, n)) *reinterpret_cast<floatx4*>(ds1 + th * head + at(m, n)) = st[m][n];
+        for (int s = 0; s < 2; ++s) mma32<2>(qt[n][s].parts(), ef[s], acc[n]);
       }
-    floatx4 kf[NF], qf[NF], dov[MB];
-    row_frags<T, NF>(kp, a.ldk, c, w, a.Dk, kf);
-    row_frags<T, NF>(qp, a.ldq, c, w, a.Dk, qf);
-    const bool live = t < c.n;
-#pragma unroll
-    for (int m = 0; m < MB; ++m) {
-      dov[m] = floatx4{0.f, 0.f, 0.f, 0.f};
-      if (live && c0 + 16 * m + 4 * lk < a.Dv)
-        dov[m] = ld4(d_o + (c.row + t) * lddo + (int64_t)h * a.Dv + c0 + 16 * m + 4 * lk);
-#pragma unroll
-      for (int r = 0; r < 4; ++r) sO[(16 * m + 4 * lk + r) * kLdM + t] = dov[m][r];
     }
-    const float beta = co[t], e = co[kC + t], wj = co[2 * kC + t], eC = co[2 * kC - 1];
+    load_tiles(qt, op(next, 1));
+    sync_lds();
+    sync_lds();
+    Parts<3> wf[2];
 #pragma unroll
-    for (int s = 0; s < NF; ++s) {
-      *reinterpret_cast<floatx4*>(sK + t * LDS + 16 * s + 4 * lk) = kf[s];
-      *reinterpret_cast<floatx4*>(sQ + t * LDS + 16 * s + 4 * lk) = qf[s];
-    }
-    __syncthreads();
-    floatx4 du[MB];
-#pragma unroll
-    for (int m = 0; m < MB; ++m) {
-      du[m] = floatx4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int s = 0; s < NF; ++s) du[m] = mma16(frag(sS + 16 * m * LDS, LDS, s), kf[s], du[m]);
-#pragma unroll
-      for (int r = 0; r < 4; ++r) du[m][r] *= wj;
-    }
-#pragma unroll
-    for (int s = 0; s < 4; ++s) {
-      const floatx4 pf = mat_frag(mat + kMat, w, s);
-#pragma unroll
-      for (int m = 0; m < MB; ++m) du[m] = mma16(frag(sO + 16 * m * kLdM, kLdM, s), pf, du[m]);
-    }
-#pragma unroll
-    for (int m = 0; m < MB; ++m)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) sU[(16 * m + 4 * lk + r) * kLdM + t] = du[m][r];
-    __syncthreads();
-    floatx4 dr[MB];
-#pragma unroll
-    for (int m = 0; m < MB; ++m) dr[m] = floatx4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int s = 0; s < 4; ++s) {
-      const floatx4 tf = mat_frag(mat, w, s);
-#pragma unroll
-      for (int m = 0; m < MB; ++m) dr[m] = mma16(frag(sU + 16 * m * kLdM, kLdM, s), tf, dr[m]);
-    }
-    if (live)
-#pragma unroll
-      for (int m = 0; m < MB; ++m)
-        if (c0 + 16 * m + 4 * lk < a.Dv) {
-          *reinterpret_cast<floatx4*>(drs + ((int64_t)(c.row + t) * a.H + h) * a.Dv + c0 + 16 * m + 4 * lk) = dr[m];
-          st4(dv + (c.row + t) * lddv + (int64_t)h * a.Dv + c0 + 16 * m + 4 * lk, dr[m] * beta);
-        }
-    __syncthreads();  // sO and sU are read
-#pragma unroll
-    for (int m = 0; m < MB; ++m)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        sO[(16 * m + 4 * lk + r) * kLdM + t] = a.scale * e * dov[m][r];
-        sU[(16 * m + 4 * lk + r) * kLdM + t] = -beta * e * dr[m][r];
-      }
-    __syncthreads();
+    for (int s = 0; s < 2; ++s) wf[s] = get_parts<3>(sW + li * LR + 32 * s + 8 * lk, 16 * LR);
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
 #pragma unroll
-      for (int m = 0; m < MB; ++m) st[m][n] *= eC;
-#pragma unroll
-      for (int s = 0; s < 4; ++s) {
-        const floatx4 kt = frag_t(sK + 16 * (NT * w + n), LDS, s), qt = frag_t(sQ + 16 * (NT * w + n), LDS, s);
-#pragma unroll
-        for (int m = 0; m < MB; ++m) {
-          st[m][n] = mma16(frag(sO + 16 * m * kLdM, kLdM, s), qt, st[m][n]);
-          st[m][n] = mma16(frag(sU + 16 * m * kLdM, kLdM, s), kt, st[m][n]);
-        }
-      }
+      for (int s = 0; s < 2; ++s) mma32<2>(kt[n][s].parts(), wf[s], acc[n]);
+      st[n] = st[n] * eC + acc[n].sum();
     }
-    __syncthreads();
+    share();
+    load_tiles(kt, op(next, 2));
+    eC = at_lane<float>(coef + ((int64_t)(key + next) * a.H + h) * 3 * kC + 2 * kC - 1, 0);
+    sync_lds();
   }
   if (dstate)
 #pragma unroll
-    for (int m = 0; m < MB; ++m)
-#pragma unroll
-      for (int n = 0; n < NT; ++n)
-        if (in(m, n)) *reinterpret_cast<floatx4*>(dstate + ((int64_t)seq * a.H + h) * head + at(m, n)) = st[m][n];
+    for (int n = 0; n < NT; ++n) keep(dstate + ((int64_t)seq * a.H + h) * size, n);
 }
 
 // Sum over the 16 lanes that share l / 16; every lane receives it.
@@ -1226,8 +1324,8 @@ hipError_t grads(const DeltaOp& a, const void* d_o_, int64_t lddo, const float* 
   delta_prep_kernel<T, DKP, true><<<flat, 256, 0, s>>>(in, q, k, ws + b.mats, ws + b.coef, ops);
   delta_chunk_kernel<T, DKP, true><<<slices, 256, 0, s>>>(in, v, ws + b.mats, ws + b.coef, ops, nullptr, nullptr, 0,
                                                           ws + b.s0, ws + b.us);
-  delta_back_kernel<T, DKP, 16><<<slices, 256, 0, s>>>(in, q, k, d_o, lddo, ws + b.mats, ws + b.coef, dstate_out,
-                                                       g.dstate, static_cast<T*>(g.dv), g.lddv, ws + b.ds1, ws + b.drs);
+  delta_back_kernel<T, DKP><<<slices, 512, 0, s>>>(in, d_o, lddo, ws + b.mats, ws + b.coef, ops, dstate_out, g.dstate,
+                                                   static_cast<T*>(g.dv), g.lddv, ws + b.ds1, ws + b.drs);
   delta_grads_kernel<T, DKP><<<flat, 256, 0, s>>>(in, q, k, v, d_o, lddo, ws + b.coef, ws + b.s0, ws + b.ds1, ws + b.us,
                                                   ws + b.drs, static_cast<T*>(g.dq), g.lddq, static_cast<T*>(g.dk),
                                                   g.lddk, g.dg, g.lddg, g.dbeta, g.lddb);
