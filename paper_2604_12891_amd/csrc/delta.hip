@@ -290,6 +290,34 @@ __device__ __forceinline__ void mma32(const Parts<NA>& a, const Parts<NB>& b, Ac
     for (int j = 0; j < NB; ++j)
       if (i + j <= O) c.v[i + j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.p[i], b.p[j], c.v[i + j], 0, 0, 0);
 }
+// The same into one accumulator, where registers are short.
+template <int O, int NA, int NB>
+__device__ __forceinline__ void mma32(const Parts<NA>& a, const Parts<NB>& b, floatx4& c) {
+#pragma unroll
+  for (int o = O; o >= 0; --o)
+#pragma unroll
+    for (int i = 0; i < NA; ++i)
+      if (o - i >= 0 && o - i < NB) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.p[i], b.p[o - i], c, 0, 0, 0);
+}
+// Four values' parts, each for itself.
+template <int N>
+struct Parts4 {
+  u32x2 w[N];
+  __device__ __forceinline__ uint16_t get(int part, int i) const { return (uint16_t)(w[part][i >> 1] >> (16 * (i & 1))); }
+};
+template <int N>
+__device__ __forceinline__ Parts4<N> split4(floatx4 v) {
+  Parts4<N> r;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    uint32_t x, y, z;
+    split3_pair(v[2 * i], v[2 * i + 1], x, y, z);
+    r.w[0][i] = x;
+    if constexpr (N > 1) r.w[1][i] = y;
+    if constexpr (N > 2) r.w[2][i] = z;
+  }
+  return r;
+}
 // Eight neighbours of a row as they are in memory.
 template <typename T> struct Raw8;
 template <> struct Raw8<uint16_t> {
@@ -298,6 +326,9 @@ template <> struct Raw8<uint16_t> {
   __device__ __forceinline__ void load(const uint16_t* p) { v = *reinterpret_cast<const any*>(p); }
   // what lane `lane` has of an operand, eight entries each
   __device__ __forceinline__ void load_lane(const uint16_t* p, int lane) { v = at_lane<u32x4>(p, lane); }
+  __device__ __forceinline__ void load_bytes(const uint16_t* p, uint32_t bytes) {
+    v = *(const __attribute__((address_space(1))) any*)(uniform(p) + bytes);
+  }
   __device__ __forceinline__ void clear() { v = u32x4{0, 0, 0, 0}; }
   __device__ __forceinline__ Parts<1> parts() const { return {{pack8(v)}}; }
 };
@@ -308,9 +339,32 @@ template <> struct Raw8<float> {
     a = at_lane<floatx4>(p, 2 * lane);
     b = at_lane<floatx4>(p, 2 * lane + 1);
   }
+  __device__ __forceinline__ void load_bytes(const float* p, uint32_t bytes) {
+    a = *(const __attribute__((address_space(1))) floatx4_any*)(uniform(p) + bytes);
+    b = *(const __attribute__((address_space(1))) floatx4_any*)(uniform(p) + bytes + 16);
+  }
   __device__ __forceinline__ void clear() { a = b = floatx4{0.f, 0.f, 0.f, 0.f}; }
   __device__ __forceinline__ Parts<3> parts() const { return split8<3>(a, b); }
 };
+struct floatx8 {
+  floatx4 a, b;
+};
+__device__ __forceinline__ floatx8 widen(Raw8<float> x) { return {x.a, x.b}; }
+__device__ __forceinline__ floatx8 widen(Raw8<uint16_t> x) {
+  floatx8 r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float lo = __uint_as_float(x.v[i] << 16), hi = __uint_as_float(x.v[i] & 0xFFFF0000u);
+    if (i < 2) {
+      r.a[2 * i] = lo;
+      r.a[2 * i + 1] = hi;
+    } else {
+      r.b[2 * i - 4] = lo;
+      r.b[2 * i - 3] = hi;
+    }
+  }
+  return r;
+}
 // Four neighbours of a row as they are in memory.
 template <typename T> struct Raw4;
 template <> struct Raw4<uint16_t> {
@@ -757,7 +811,7 @@ __global__ __launch_bounds__(SAVE ? 256 : 512) void delta_chunk_kernel(
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
             const int t = 16 * w + 4 * lk + r;
-            if (t < c.n) us[((int64_t)(c.row + t) * a.H + h) * a.Dv + c0 + li] = u[r];
+            if (t < c.n) us[(((int64_t)(key + ch) * a.H + h) * kC + t) * a.Dv + c0 + li] = u[r];
           }
       } else {
         acc.clear();
@@ -951,7 +1005,7 @@ __global__ __launch_bounds__(512) void delta_back_kernel(DeltaIn a, const T* __r
       e = factor(next, 1);
       if (ch > 0) put_o(next);
       if (tv < c.n && cv < a.Dv) {
-        *reinterpret_cast<floatx4*>(drs + ((int64_t)(c.row + tv) * a.H + h) * a.Dv + cv) = row;
+        *reinterpret_cast<floatx4*>(drs + (((int64_t)(key + ch) * a.H + h) * kC + tv) * a.Dv + cv) = row;
         st4(dv + (c.row + tv) * lddv + (int64_t)h * a.Dv + cv, rowb);
       }
       sync_lds();
@@ -1012,75 +1066,72 @@ __global__ __launch_bounds__(512) void delta_back_kernel(DeltaIn a, const T* __r
     for (int n = 0; n < NT; ++n) keep(dstate + ((int64_t)seq * a.H + h) * size, n);
 }
 
-// Sum over the 16 lanes that share l / 16; every lane receives it.
+// Over the 16 lanes that share l / 16.
 __device__ __forceinline__ float sum16(float v) {
-  v += dpp<0xB1>(v);
-  v += dpp<0x4E>(v);
-  v += dpp<0x141>(v);  // half mirror: the other four of eight
-  return v + dpp<0x140>(v);  // mirror: the other eight
+  v = sum8(v);
+  return v + dpp<0x140>(v);
+}
+// The compiler asks for all operands of unrolled products at once, and spills others for them: not across this.
+__device__ __forceinline__ void keep_order() { __builtin_amdgcn_sched_barrier(0); }
+// Sum over the four lane groups l / 16; every lane receives it.
+__device__ __forceinline__ float sum4(float x) {
+  x += __shfl_xor(x, 16, 64);
+  return x + __shfl_xor(x, 32, 64);
 }
 
 // What the chunks give once their states and adjoints are known, a workgroup per chunk and key head, which
-// sums dQ and dK over the value heads that share it. Each wavefront has 16 tokens; U and slices of the states
-// go through LDS, 32 columns at a time.
-constexpr int kSl = 32, kLdSl = kSl + 4;
+// sums dQ and dK over the value heads that share it. Two sets of four wavefronts have 16 tokens each and
+// half of the rows of dQ^T and dK^T each; the first also forms dP and M1, the second dA and M2. The states, their
+// adjoints and U go through LDS in parts, 32 columns at a time; then M1 and M2 do, both ways round.
+constexpr int kSl = 32, kLdSl = kSl + 8, kLdZ = kC + 8, kLdF = kC + 1;
 
 template <typename T, int DKP>
-__global__ __launch_bounds__(256) void delta_grads_kernel(DeltaIn a, const T* __restrict__ q, const T* __restrict__ k,
+__global__ __launch_bounds__(512) void delta_grads_kernel(DeltaIn a, const T* __restrict__ q, const T* __restrict__ k,
                                                           const T* __restrict__ v, const T* __restrict__ d_o,
                                                           int64_t lddo, const float* __restrict__ coef,
-                                                          const float* __restrict__ s0, const float* __restrict__ ds1,
-                                                          const float* __restrict__ us, const float* __restrict__ drs,
-                                                          T* __restrict__ dq, int64_t lddq, T* __restrict__ dk,
-                                                          int64_t lddk, float* __restrict__ dg, int64_t lddg,
+                                                          const T* __restrict__ ops, const float* __restrict__ s0,
+                                                          const float* __restrict__ ds1, const float* __restrict__ us,
+                                                          const float* __restrict__ drs, T* __restrict__ dq,
+                                                          int64_t lddq, T* __restrict__ dk, int64_t lddk,
+                                                          float* __restrict__ dg, int64_t lddg,
                                                           float* __restrict__ dbeta, int64_t lddb) {
-  constexpr int NF = DKP / 16, LDS = DKP + 4;
-  constexpr int kSlices = 2 * DKP * kLdSl + kC * kLdSl;  // S0, dS1, U
-  constexpr int kPool = kSlices > 2 * kC * kLdM ? kSlices : 2 * kC * kLdM;  // then M1, M2 + M2^T
-  __shared__ __attribute__((aligned(16))) float sK[kC * LDS], sQ[kC * LDS], pool[kPool];
+  constexpr int NS = DKP / 32, NT = DKP / 32, OP = kOutParts<T>;  // NT: tiles of 16 rows to a wavefront
+  constexpr int kState = DKP * kLdSl, kU = kC * kLdSl, kZ = kC * kLdZ;  // bf16 entries of one part
+  constexpr int KP = sizeof(T) == 2 ? 1 : 3;  // parts of an activation
+  constexpr int kSlices = 6 * kState + (6 + KP) * kU, kProducts = 4 * OP * kZ + 2 * 2 * kC * kLdF;
+  __shared__ __attribute__((aligned(16))) uint16_t pool[kSlices > kProducts ? kSlices : kProducts];
   __shared__ double sG[kC];
-  __shared__ float sB[kC], sRow[kC], sCol[kC], sSeg[4][kC], sDot[4];
-  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, li = lane & 15, lk = lane >> 4;
+  __shared__ float sB[kC], sQ1[2][kC], sK2[2][kC], sK3[2][kC], sRow[kC], sCol[kC], sSum[2][kC], sSeg[8][kC], sDot[8];
+  uint16_t* sS0 = pool;
+  uint16_t* sD1 = pool + 3 * kState;
+  uint16_t* sUs = pool + 6 * kState;
+  uint16_t* sDr = sUs + 3 * kU;
+  uint16_t* sDo = sDr + 3 * kU;
+  const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), w = wv & 3, set = wv >> 2;
   const int tile = blockIdx.x / a.Hk, hk = blockIdx.x % a.Hk;
   const Tile tl = find_tile(a.offs, a.n_seq, a.rows, kC, tile);
   if (tl.seq < 0 || tl.len == 0) return;
   const Chunk c = {tl.base + tl.j * kC, min(kC, tl.len - tl.j * kC)};
-  const int t = 16 * w + li;
-  const bool live = t < c.n;
   const floatx4 zero = {0.f, 0.f, 0.f, 0.f};
-  floatx4 kk[4], qk[4];  // [16 w + 4 lk + r][16 j + li]
-  {
-    floatx4 kf[NF], qf[NF];
-    row_frags<T, NF>(k + (int64_t)hk * a.Dk, a.ldk, c, w, a.Dk, kf);
-    row_frags<T, NF>(q + (int64_t)hk * a.Dk, a.ldq, c, w, a.Dk, qf);
+  const T* kp = k + (int64_t)hk * a.Dk;
+  const T* qp = q + (int64_t)hk * a.Dk;
+  const T* op = ops + ((int64_t)tile * a.Hk + hk) * 3 * DKP * kC;  // K, Q^T, K^T
+  floatx4 dqa[NT], dka[NT];
 #pragma unroll
-    for (int s = 0; s < NF; ++s) {
-      *reinterpret_cast<floatx4*>(sK + t * LDS + 16 * s + 4 * lk) = kf[s];
-      *reinterpret_cast<floatx4*>(sQ + t * LDS + 16 * s + 4 * lk) = qf[s];
-    }
-    __syncthreads();
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      kk[j] = qk[j] = zero;
-      if (j > w) continue;
-#pragma unroll
-      for (int s = 0; s < NF; ++s) {
-        const floatx4 bf = frag(sK + 16 * j * LDS, LDS, s);
-        kk[j] = mma16(kf[s], bf, kk[j]);
-        qk[j] = mma16(qf[s], bf, qk[j]);
-      }
-    }
-  }
-  floatx4 dqa[NF], dka[NF];  // [16 n + 4 lk + r][16 w + li]
-#pragma unroll
-  for (int n = 0; n < NF; ++n) dqa[n] = dka[n] = zero;
+  for (int n = 0; n < NT; ++n) dqa[n] = dka[n] = zero;
   const int share = a.H / a.Hk;
   const int64_t head = (int64_t)a.Dk * a.Dv;
   for (int hv = 0; hv < share; ++hv) {
     const int h = hk * share + hv;
     const int64_t th = (int64_t)tile * a.H + h;
     const float* co = coef + th * 3 * kC;
-    __syncthreads();
+    // (as if it were another thread for every head: addresses formed once for all heads would not fit the registers)
+    int tid = threadIdx.x;
+    asm volatile("" : "+v"(tid));
+    const int lane = tid & 63, li = lane & 15, lk = lane >> 4;
+    const int t = 16 * w + li, t_in = min(t, c.n - 1);
+    const int d0 = set * NT * 16 + 4 * lk;  // the lane's rows of tile n: d0 + 16 n + r
+    sync_lds();
     if (tid < kC) {
       double G = tid < c.n ? log_decay(a.g[(c.row + tid) * a.ldg + h]) : 0.0;
 #pragma unroll
@@ -1091,71 +1142,91 @@ __global__ __launch_bounds__(256) void delta_grads_kernel(DeltaIn a, const T* __
       sG[tid] = G;
       sB[tid] = co[tid];
     }
-    floatx4 dp[4], da[4], x1[NF], x2[NF], x3[NF];
+    // a slice's share of this thread
+    constexpr int NL = DKP * (kSl / 4) / 512;
+    const int ut = tid / (kSl / 4), uc = 4 * (tid % (kSl / 4));
+    floatx4 sv[NL], dvv[NL], uv, rr;
+    Raw4<T> ov, vv;
+    auto load = [&](int c0) {
+      const float* sp = s0 + th * head + c0;
+      const float* dp = ds1 + th * head + c0;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) dp[j] = da[j] = zero;
+      for (int m = 0; m < NL; ++m) {
+        const int r = ut + 64 * m;
+        sv[m] = dvv[m] = zero;
+        if (r < a.Dk && c0 + uc < a.Dv) {
+          sv[m] = at_bytes<Raw4<float>>(sp, (uint32_t)(r * a.Dv + uc) * 4).v;
+          dvv[m] = at_bytes<Raw4<float>>(dp, (uint32_t)(r * a.Dv + uc) * 4).v;
+        }
+      }
+      uv = rr = zero;
+      ov.v = vv.v = {};
+      if (ut < c.n && c0 + uc < a.Dv) {
+        const uint32_t at = (uint32_t)(ut * a.Dv + uc) * 4;
+        uv = at_bytes<Raw4<float>>(us + th * kC * a.Dv + c0, at).v;
+        rr = at_bytes<Raw4<float>>(drs + th * kC * a.Dv + c0, at).v;
+        ov = at_bytes<Raw4<T>>(d_o + c.row * lddo + (int64_t)h * a.Dv + c0, (uint32_t)(ut * (int)lddo + uc) * (uint32_t)sizeof(T));
+        vv = at_bytes<Raw4<T>>(v + c.row * a.ldv + (int64_t)h * a.Dv + c0, (uint32_t)(ut * (int)a.ldv + uc) * (uint32_t)sizeof(T));
+      }
+    };
+    load(0);
+    floatx4 dz[4], x1[NT], x2[NT], x3[NT];  // dP or dA (but for its sign), transposed; S0 dO^T, S0 dR^T, dS1 U^T
 #pragma unroll
-    for (int n = 0; n < NF; ++n) x1[n] = x2[n] = x3[n] = zero;
+    for (int b = 0; b < 4; ++b) dz[b] = zero;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) x1[n] = x2[n] = x3[n] = zero;
     float rv = 0.f, dot = 0.f;
     for (int c0 = 0; c0 < a.Dv; c0 += kSl) {
-      float* sS0 = pool;
-      float* sD1 = pool + DKP * kLdSl;
-      float* sUs = pool + 2 * DKP * kLdSl;
-      __syncthreads();
-      for (int i = tid; i < DKP * (kSl / 4); i += 256) {
-        const int r = i / (kSl / 4), cc = 4 * (i % (kSl / 4));
-        floatx4 x = zero, y = zero;
-        if (r < a.Dk && c0 + cc < a.Dv) {
-          x = *reinterpret_cast<const floatx4*>(s0 + th * head + (int64_t)r * a.Dv + c0 + cc);
-          y = *reinterpret_cast<const floatx4*>(ds1 + th * head + (int64_t)r * a.Dv + c0 + cc);
-        }
-        *reinterpret_cast<floatx4*>(sS0 + r * kLdSl + cc) = x;
-        *reinterpret_cast<floatx4*>(sD1 + r * kLdSl + cc) = y;
+      sync_lds();  // (the slice before is read)
 #pragma unroll
-        for (int m = 0; m < 4; ++m) dot = fmaf(x[m], y[m], dot);
+      for (int m = 0; m < NL; ++m) {
+        put_parts<3>(sS0 + (ut + 64 * m) * kLdSl + uc, kState, sv[m]);
+        put_parts<3>(sD1 + (ut + 64 * m) * kLdSl + uc, kState, dvv[m]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) dot = fmaf(sv[m][e], dvv[m][e], dot);
       }
-      floatx4 of[2], uf[2], rf[2];
+      put_parts<3>(sUs + ut * kLdSl + uc, kU, uv);
+      put_parts<3>(sDr + ut * kLdSl + uc, kU, rr);
+      put_parts<KP>(sDo + ut * kLdSl + uc, kU, widen(ov));
+      const floatx4 vw = widen(vv);
 #pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        const int cc = c0 + 16 * s + 4 * lk;
-        of[s] = uf[s] = rf[s] = zero;
-        if (live && cc < a.Dv) {
-          const int64_t row = c.row + t;
-          of[s] = ld4(d_o + row * lddo + (int64_t)h * a.Dv + cc);
-          uf[s] = *reinterpret_cast<const floatx4*>(us + (row * a.H + h) * a.Dv + cc);
-          rf[s] = *reinterpret_cast<const floatx4*>(drs + (row * a.H + h) * a.Dv + cc);
-          const floatx4 vv = ld4(v + row * a.ldv + (int64_t)h * a.Dv + cc);
+      for (int e = 0; e < 4; ++e) rv = fmaf(rr[e], vw[e], rv);
+      if (c0 + kSl < a.Dv) load(c0 + kSl);
+      sync_lds();
+      const int own = t * kLdSl + 8 * lk;
+      const Parts<3> rb = get_parts<3>(sDr + own, kU);
+      const Parts<KP> ob = get_parts<KP>(sDo + own, kU);
 #pragma unroll
-          for (int m = 0; m < 4; ++m) rv = fmaf(rf[s][m], vv[m], rv);
-        }
-        *reinterpret_cast<floatx4*>(sUs + t * kLdSl + 16 * s + 4 * lk) = uf[s];
+      for (int b = 0; b < 4; ++b) {
+        if (b > w) continue;
+        const Parts<3> ub = get_parts<3>(sUs + (16 * b + li) * kLdSl + 8 * lk, kU);
+        if (set) mma32<2>(ub, rb, dz[b]);
+        else mma32<2>(ub, ob, dz[b]);
+        keep_order();
       }
-      __syncthreads();
+      const Parts<3> ub = get_parts<3>(sUs + own, kU);
 #pragma unroll
-      for (int s = 0; s < 2; ++s) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          if (j > w) continue;
-          const floatx4 uj = frag(sUs + 16 * j * kLdSl, kLdSl, s);
-          dp[j] = mma16(of[s], uj, dp[j]);
-          da[j] = mma16(rf[s], uj, da[j]);
-        }
-#pragma unroll
-        for (int n = 0; n < NF; ++n) {
-          const floatx4 x = frag(sS0 + 16 * n * kLdSl, kLdSl, s), y = frag(sD1 + 16 * n * kLdSl, kLdSl, s);
-          x1[n] = mma16(x, of[s], x1[n]);
-          x2[n] = mma16(x, rf[s], x2[n]);
-          x3[n] = mma16(y, uf[s], x3[n]);
-        }
+      for (int n = 0; n < NT; ++n) {
+        const int r = ((set * NT + n) * 16 + li) * kLdSl + 8 * lk;
+        const Parts<3> x = get_parts<3>(sS0 + r, kState), y = get_parts<3>(sD1 + r, kState);
+        mma32<2>(x, ob, x1[n]);
+        mma32<2>(x, rb, x2[n]);
+        mma32<2>(y, ub, x3[n]);
+        keep_order();
       }
     }
+    rv = sum8(rv);
+    if ((tid & 7) == 0) sSum[1][ut] = rv;
     const float beta = co[t], e = co[kC + t], wj = co[2 * kC + t], eC = co[2 * kC - 1];
-    // q.(dO S0^T), k.(dR S0^T), k.(U dS1^T) of the lane's token, and dQ, dK's terms
+    // q.(dO S0^T), k.(dR S0^T), k.(U dS1^T) of the lane's token (the set's half of the rows), and dQ, dK's terms
     float q1 = 0.f, k2 = 0.f, k3 = 0.f;
 #pragma unroll
-    for (int n = 0; n < NF; ++n) {
-      const floatx4 qv = *reinterpret_cast<const floatx4*>(sQ + t * LDS + 16 * n + 4 * lk),
-                    kv = *reinterpret_cast<const floatx4*>(sK + t * LDS + 16 * n + 4 * lk);
+    for (int n = 0; n < NT; ++n) {
+      floatx4 qv = zero, kv = zero;
+      if (d0 + 16 * n < a.Dk) {
+        qv = widen(at_bytes<Raw4<T>>(qp + c.row * a.ldq + 16 * n, (uint32_t)(t_in * (int)a.ldq + d0) * (uint32_t)sizeof(T)));
+        kv = widen(at_bytes<Raw4<T>>(kp + c.row * a.ldk + 16 * n, (uint32_t)(t_in * (int)a.ldk + d0) * (uint32_t)sizeof(T)));
+      }
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         q1 = fmaf(qv[r], x1[n][r], q1);
@@ -1165,95 +1236,158 @@ __global__ __launch_bounds__(256) void delta_grads_kernel(DeltaIn a, const T* __
         dka[n][r] = fmaf(wj, x3[n][r], fmaf(-beta * e, x2[n][r], dka[n][r]));
       }
     }
-    auto sum4 = [](float x) {
-      x += __shfl_xor(x, 16, 64);
-      return x + __shfl_xor(x, 32, 64);
-    };
-    q1 = sum4(q1); k2 = sum4(k2); k3 = sum4(k3); rv = sum4(rv);
-    dot = wave_sum(dot);
+    q1 = sum4(q1); k2 = sum4(k2); k3 = sum4(k3);
+    dot = sum4(sum16(dot));
     if (lk == 0) {
-      sRow[t] = a.scale * e * q1 - beta * e * k2;
-      sCol[t] = wj * k3;
+      sQ1[set][t] = q1;
+      sK2[set][t] = k2;
+      sK3[set][t] = k3;
     }
-    if (lane == 0) sDot[w] = dot;
-    float db = rv - e * k2;  // of the lane's token; the products with kk follow by rows
-    __syncthreads();         // the slices are read, sG is written
-    float* m1 = pool;
-    float* m2 = pool + kC * kLdM;
-    floatx4 mm[4];   // dP P + dA A
-    floatx4 rowsum = zero;
+    if (lane == 0) sDot[wv] = dot;
+    sync_lds();  // the slices are read
+    // products of keys j with the set's rows (queries or keys) i: [16 b + 4 lk + r][t]; formed here for every head,
+    // as through the slices there are no registers for them
+    floatx4 zz[4];
+    {
+      Raw8<T> rf[NS];
+      row_raw<T, NS>(set ? kp : qp, set ? a.ldk : a.ldq, c, w, a.Dk, rf);
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+      for (int b = 0; b < 4; ++b) {
+        zz[b] = zero;
+        if (b > w) continue;
+        Raw8<T> kf[NS];
+#pragma unroll
+        for (int s = 0; s < NS; ++s) kf[s].load_lane(op + (b * NS + s) * 512, lane);
+#pragma unroll
+        for (int s = 0; s < NS; ++s) mma32<2>(kf[s].parts(), rf[s].parts(), zz[b]);
+        keep_order();
+      }
+    }
+    // the set's matrix, M1 or M2 (below the diagonal), as rows and as columns over tokens in place
+    uint16_t* sZ = pool + set * 2 * OP * kZ;
+    uint16_t* sZT = sZ + OP * kZ;
+    float* sF = reinterpret_cast<float*>(pool + 4 * OP * kZ) + set * kC * kLdF;  // dP P or dA A
+    float rowsum = 0.f;  // of dA D kk, of the lane's token
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+      if (b > (w | 1)) continue;  // (the block behind the diagonal's too where they share 32 tokens: zeros)
+      floatx4 z = zero, f = zero;
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        const int row = 16 * w + 4 * lk + r, col = 16 * j + li;
-        const float d = col <= row ? exp_of(sG[row] - sG[col]) : 0.f;
-        const float ga = col < row ? -da[j][r] * d : 0.f, gp = a.scale * d * dp[j][r];
-        m1[row * kLdM + col] = col <= row ? gp : 0.f;
-        const float y = sB[row] * ga;
-        if (col < row) {
-          m2[row * kLdM + col] = y;
-          m2[col * kLdM + row] = y;
-        } else if (col == row) {
-          m2[row * kLdM + col] = 0.f;
+        const int j = 16 * b + 4 * lk + r;
+        if (j <= t) {
+          const float d = exp_of(sG[t] - sG[j]);
+          if (set) {
+            const float ga = j < t ? -dz[b][r] * d : 0.f;
+            z[r] = beta * ga;
+            rowsum = fmaf(ga, zz[b][r], rowsum);
+          } else {
+            z[r] = a.scale * d * dz[b][r];
+          }
+          f[r] = j < t ? z[r] * zz[b][r] : 0.f;
         }
-        mm[j][r] = col < row ? fmaf(gp, qk[j][r], y * kk[j][r]) : 0.f;
-        rowsum[r] = fmaf(ga, kk[j][r], rowsum[r]);
       }
-    __syncthreads();
+      put_parts<OP>(sZ + t * kLdZ + token_place(b, lk), kZ, z);
+      const Parts4<OP> p = split4<OP>(z);
 #pragma unroll
-    for (int s = 0; s < 4; ++s) {
-      const floatx4 b1 = frag(m1 + 16 * w * kLdM, kLdM, s), b2 = frag_t(m1 + 16 * w, kLdM, s),
-                    b3 = frag(m2 + 16 * w * kLdM, kLdM, s);
+      for (int r = 0; r < 4; ++r) {
+        const int j = 16 * b + 4 * lk + r, at = token_place(w, li >> 2) + (li & 3);
 #pragma unroll
-      for (int n = 0; n < NF; ++n) {
-        const floatx4 kt = frag_t(sK + 16 * n, LDS, s), qt = frag_t(sQ + 16 * n, LDS, s);
-        if (s <= w) dqa[n] = mma16(kt, b1, dqa[n]);
-        if (s >= w) dka[n] = mma16(qt, b2, dka[n]);
-        dka[n] = mma16(kt, b3, dka[n]);
+        for (int i = 0; i < OP; ++i) sZT[i * kZ + j * kLdZ + at] = p.get(i, r);
+        if (j <= t) sF[t * kLdF + j] = f[r];
+      }
+      keep_order();
+    }
+    rowsum = sum4(rowsum);
+    if (set && lk == 0) sSum[0][t] = rowsum;
+    sync_lds();
+    {
+      const uint16_t* m1 = pool;
+      const uint16_t* m1t = pool + OP * kZ;
+      const uint16_t* m2 = pool + 2 * OP * kZ;
+      const uint16_t* m2t = pool + 3 * OP * kZ;
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        const int at = t * kLdZ + 32 * s + 8 * lk;
+        const bool lo = s <= w >> 1, hi = s >= w >> 1;
+        Parts<OP> b1, b1t, b2, b2t;
+        if (lo) {
+          b1 = get_parts<OP>(m1 + at, kZ);
+          b2 = get_parts<OP>(m2 + at, kZ);
+        }
+        if (hi) {
+          b1t = get_parts<OP>(m1t + at, kZ);
+          b2t = get_parts<OP>(m2t + at, kZ);
+        }
+        Raw8<T> kt[NT], qt[NT];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          kt[n].load_lane(op + 2 * DKP * kC + (2 * (set * NT + n) + s) * 512, lane);
+          if (hi) qt[n].load_lane(op + DKP * kC + (2 * (set * NT + n) + s) * 512, lane);
+        }
+        keep_order();
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          const auto ka = kt[n].parts();
+          if (lo) {
+            mma32<OP - 1>(ka, b1, dqa[n]);
+            mma32<OP - 1>(ka, b2, dka[n]);
+          }
+          if (hi) {
+            mma32<OP - 1>(qt[n].parts(), b1t, dka[n]);
+            mma32<OP - 1>(ka, b2t, dka[n]);
+          }
+          keep_order();
+        }
       }
     }
-    // sums of rows of dA D kk to their tokens' lanes
-#pragma unroll
-    for (int r = 0; r < 4; ++r) rowsum[r] = sum16(rowsum[r]);
-    __syncthreads();  // m1, m2 are read
-    if (li == 0)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) sSeg[0][16 * w + 4 * lk + r] = rowsum[r];
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) m1[(16 * w + 4 * lk + r) * kLdM + 16 * j + li] = mm[j][r];
-    __syncthreads();
-    if (lk == 0 && live) dbeta[(c.row + t) * lddb + h] = db + sSeg[0][t];
-    __syncthreads();
-    // column `lane`, rows 16 w .. + 15: sums from each row to the last
+    if (tid < kC && tid < c.n) {
+      const float b = co[tid], ee = co[kC + tid];
+      const float kr = sK2[0][tid] + sK2[1][tid];
+      dbeta[(c.row + tid) * lddb + h] = sSum[1][tid] - ee * kr + sSum[0][tid];
+      sRow[tid] = a.scale * ee * (sQ1[0][tid] + sQ1[1][tid]) - b * ee * kr;
+      sCol[tid] = co[2 * kC + tid] * (sK3[0][tid] + sK3[1][tid]);
+    } else if (tid < kC) {
+      sRow[tid] = sCol[tid] = 0.f;
+    }
+    // column `lane` of the set's matrix, rows 16 w .. + 15: sums from each row to the last
     float z[16], z_all = 0.f;
 #pragma unroll
     for (int i = 15; i >= 0; --i) {
-      z_all += m1[(16 * w + i) * kLdM + lane];
+      if (lane <= 16 * w + i) z_all += sF[(16 * w + i) * kLdF + lane];
       z[i] = z_all;
     }
-    sSeg[w][lane] = z_all;
-    __syncthreads();
+    sSeg[wv][lane] = z_all;
+    sync_lds();
     float below = 0.f;
-    for (int x = w + 1; x < 4; ++x) below += sSeg[x][lane];
-    const float rt = sRow[lane], ct = sCol[lane], all = eC * (sDot[0] + sDot[1] + sDot[2] + sDot[3]);
+    for (int x = w + 1; x < 4; ++x) below += sSeg[4 * set + x][lane];
+    // entry [row, j]: what the pairs (i >= row, j) add to token row's sum
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const int row = 16 * w + i;
-      // lane j: what it adds to token `row`'s sum
-      const float x = (lane >= row ? rt : ct + z[i] + below);
-      const float sum = wave_sum(x);
-      if (lane == 0 && row < c.n) dg[(c.row + row) * lddg + h] = sum + all;
+    for (int i = 0; i < 16; ++i) sF[(16 * w + i) * kLdF + lane] = z[i] + below;
+    sync_lds();
+    {
+      const int row = tid >> 3, p = tid & 7;  // eight lanes to a token
+      const float* f0 = reinterpret_cast<const float*>(pool + 4 * OP * kZ);
+      float sum = 0.f;
+#pragma unroll
+      for (int x = 0; x < 8; ++x) {
+        const int j = 8 * x + p;
+        sum += j >= row ? sRow[j] : sCol[j] + f0[row * kLdF + j] + f0[(kC + row) * kLdF + j];
+      }
+      sum = sum8(sum);
+      float all = 0.f;
+#pragma unroll
+      for (int x = 0; x < 8; ++x) all += sDot[x];
+      if (p == 0 && row < c.n) dg[(c.row + row) * lddg + h] = fmaf(eC, all, sum);
     }
   }
-  if (live)
+  const int t = 16 * w + (threadIdx.x & 15), d0 = set * NT * 16 + 4 * (threadIdx.x >> 4 & 3);
+  if (t < c.n)
 #pragma unroll
-    for (int n = 0; n < NF; ++n)
-      if (16 * n + 4 * lk < a.Dk) {
-        st4(dq + (c.row + t) * lddq + (int64_t)hk * a.Dk + 16 * n + 4 * lk, dqa[n]);
-        st4(dk + (c.row + t) * lddk + (int64_t)hk * a.Dk + 16 * n + 4 * lk, dka[n]);
+    for (int n = 0; n < NT; ++n)
+      if (d0 + 16 * n < a.Dk) {
+        st4(dq + (c.row + t) * lddq + (int64_t)hk * a.Dk + d0 + 16 * n, dqa[n]);
+        st4(dk + (c.row + t) * lddk + (int64_t)hk * a.Dk + d0 + 16 * n, dka[n]);
       }
 }
 
@@ -1299,7 +1433,7 @@ int64_t op_floats(bool bf16, int n_seq, int rows, int Hk, int Dk) {
 struct BackSpace {
   int64_t coef, mats, s0, ds1, us, drs, ops, end;
   BackSpace(bool bf16, int n_seq, int rows, int Hk, int H, int Dk, int Dv) {
-    const int64_t th = tiles_of(n_seq, rows) * H, head = (int64_t)Dk * Dv, act = (int64_t)rows * H * Dv;
+    const int64_t th = tiles_of(n_seq, rows) * H, head = (int64_t)Dk * Dv, act = th * kC * Dv;
     coef = 0;
     mats = coef + th * 3 * kC;
     s0 = mats + th * kMats<float, true>;
@@ -1326,8 +1460,8 @@ hipError_t grads(const DeltaOp& a, const void* d_o_, int64_t lddo, const float* 
                                                           ws + b.s0, ws + b.us);
   delta_back_kernel<T, DKP><<<slices, 512, 0, s>>>(in, d_o, lddo, ws + b.mats, ws + b.coef, ops, dstate_out, g.dstate,
                                                    static_cast<T*>(g.dv), g.lddv, ws + b.ds1, ws + b.drs);
-  delta_grads_kernel<T, DKP><<<flat, 256, 0, s>>>(in, q, k, v, d_o, lddo, ws + b.coef, ws + b.s0, ws + b.ds1, ws + b.us,
-                                                  ws + b.drs, static_cast<T*>(g.dq), g.lddq, static_cast<T*>(g.dk),
+  delta_grads_kernel<T, DKP><<<flat, 512, 0, s>>>(in, q, k, v, d_o, lddo, ws + b.coef, ops, ws + b.s0, ws + b.ds1,
+                                                  ws + b.us, ws + b.drs, static_cast<T*>(g.dq), g.lddq, static_cast<T*>(g.dk),
                                                   g.lddk, g.dg, g.lddg, g.dbeta, g.lddb);
   return hipGetLastError();
 }
