@@ -446,13 +446,13 @@ __device__ __forceinline__ void row_raw(const T* p, int64_t ld, Chunk c, int w, 
 constexpr int kLdM = kC + 4;
 
 template <typename T, int DKP, bool GRADS>
-__global__ __launch_bounds__(256) void delta_prep_kernel(DeltaIn a, const T* __restrict__ q, const T* __restrict__ k,
+__global__ __launch_bounds__(256, (sizeof(T) == 4 && DKP == 128 ? 2 : 4)) void delta_prep_kernel(DeltaIn a, const T* __restrict__ q, const T* __restrict__ k,
                                                          float* __restrict__ mats, float* __restrict__ coef,
                                                          T* __restrict__ ops) {
   __shared__ __attribute__((aligned(16))) float sA[kC * kLdM], sT[kC * kLdM], sX[32 * 36];
   __shared__ double sG[kC];
   __shared__ float sB[kC];
-  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, li = lane & 15, lk = lane >> 4;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int tile = blockIdx.x / a.Hk, hk = blockIdx.x % a.Hk;
   const Tile tl = find_tile(a.offs, a.n_seq, a.rows, kC, tile);
   if (tl.seq < 0 || tl.len == 0) return;
@@ -484,6 +484,7 @@ __global__ __launch_bounds__(256) void delta_prep_kernel(DeltaIn a, const T* __r
       qk[t] = y.sum();
     }
   }
+  const int lane = threadIdx.x & 63, li = lane & 15, lk = lane >> 4;
   // K, Q (for the gradients Q^T) and K^T as operands: a chunk's rows are a model's width apart, and every slice of every head that
   // reads them so would ask one channel of the cache for all of them
   {
@@ -516,6 +517,10 @@ __global__ __launch_bounds__(256) void delta_prep_kernel(DeltaIn a, const T* __r
     const int h = hk * share + hv;
     float* out = mats + ((int64_t)tile * a.H + h) * kMats<T, GRADS>;
     float* co = coef + ((int64_t)tile * a.H + h) * 3 * kC;
+    // (as if it were another thread for every head: addresses formed once for all heads would not fit the registers)
+    int tid = threadIdx.x;
+    asm volatile("" : "+v"(tid));
+    const int lane = tid & 63, li = lane & 15, lk = lane >> 4;
     __syncthreads();
     if (tid < kC) {
       // past the chunk's end nothing decays and nothing is written

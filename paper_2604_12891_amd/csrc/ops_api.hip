@@ -303,8 +303,9 @@ TCL_API tcl_status tcl_layer_norm_backward(int32_t dtype, int32_t rows, int32_t 
 
 namespace {
 
-// Fewer than 2^32 threads a launch: a sequence's head takes 16 workgroups of 256 at most, a chunk's (64 rows, or the rest
-// of a sequence) one.
+// Fewer than 2^32 threads a launch: of packed sequences a head takes 16 workgroups of 512 at most (kMaxSeqHeads),
+// of single tokens 8 of 64 (kMaxTokenHeads); a chunk's key head, of 64 rows or the rest of a sequence, one of 512.
+constexpr int64_t kMaxSeqHeads = ((int64_t)1 << 19) - 1, kMaxTokenHeads = ((int64_t)1 << 22) - 1;
 constexpr int kMaxHeads = 1024, kMaxDk = 128, kMaxDv = 256;
 // (a chunk's rows are addressed in 31 bits)
 constexpr int64_t kMaxLd = (int64_t)1 << 22;
@@ -312,7 +313,7 @@ constexpr int64_t kMaxLd = (int64_t)1 << 22;
 bool delta_sizes(int32_t n_seq, int32_t rows, int32_t Hk, int32_t H, int32_t Dk, int32_t Dv) {
   return n_seq >= 0 && rows >= 0 && n_seq <= kMaxRows && rows <= kMaxRows && Hk >= 1 && H >= Hk && H <= kMaxHeads &&
          H % Hk == 0 && Dk >= 8 && Dk <= kMaxDk && Dk % 8 == 0 && Dv >= 8 && Dv <= kMaxDv && Dv % 8 == 0 &&
-         (int64_t)rows * H <= ((int64_t)1 << 28) && (int64_t)n_seq * H < ((int64_t)1 << 20);
+         (int64_t)rows * H <= ((int64_t)1 << 28) && (int64_t)n_seq * H <= kMaxTokenHeads;
 }
 
 tcl_status delta_op(const tcl_delta_rule_args* a, DeltaOp* op) {
@@ -327,7 +328,8 @@ tcl_status delta_op(const tcl_delta_rule_args* a, DeltaOp* op) {
   if (a->Dk < 8 || a->Dk > kMaxDk || a->Dk % 8 || a->Dv < 8 || a->Dv > kMaxDv || a->Dv % 8)
     return fail(TCL_ERR_UNSUPPORTED, "Dk and Dv must be multiples of 8, at most %d and %d (got %d, %d)", kMaxDk, kMaxDv,
                 a->Dk, a->Dv);
-  if (!delta_sizes(a->n_seq, a->rows, a->Hk, a->H, a->Dk, a->Dv))
+  if (!delta_sizes(a->n_seq, a->rows, a->Hk, a->H, a->Dk, a->Dv) ||
+      (a->d_offs && (int64_t)a->n_seq * a->H > kMaxSeqHeads))
     return fail(TCL_ERR_UNSUPPORTED, "too many rows or sequences x heads (n_seq=%d rows=%d H=%d)", a->n_seq, a->rows,
                 a->H);
   const int64_t qk = (int64_t)a->Hk * a->Dk, v = (int64_t)a->H * a->Dv;
@@ -404,6 +406,8 @@ TCL_API tcl_status tcl_delta_rule_backward(const tcl_delta_rule_args* args, cons
     return fail(TCL_ERR_INVALID_ARG, "activations are not aligned to their type");
   if (misaligned(d_dstate_out, 16) || misaligned(g->d_dstate, 16))
     return fail(TCL_ERR_INVALID_ARG, "the states' gradients must be 16-byte aligned");
+  if ((int64_t)op.n_seq * op.H > kMaxSeqHeads)
+    return fail(TCL_ERR_UNSUPPORTED, "too many sequences x heads (n_seq=%d H=%d)", op.n_seq, op.H);
   if (op.n_seq == 0) return fail(TCL_ERR_INVALID_ARG, "no sequences to take gradients of");
   op.n_slots = op.n_seq;
   const size_t need = delta_rule_bwd_workspace_bytes(op.bf16, op.n_seq, op.rows, op.Hk, op.H, op.Dk, op.Dv);
