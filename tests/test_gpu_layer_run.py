@@ -1,0 +1,171 @@
+"""Layer norm, the convolution, the gated delta rule, log probabilities and beam search together, as a model
+of one layer uses them: trained a step against float64 differentiation, and searched with, its states
+reordered in their pools, against a search that reads every prefix anew."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import layer as ol
+from oracle import sequence as osq
+
+pytestmark = pytest.mark.gpu
+C, HK, H, DK, DV, V, KC = 48, 2, 4, 16, 24, 61, 4
+QK, E = HK * DK, 2 * HK * DK + H * DV
+
+
+def _tb():
+    from paper_2604_12891_amd import binding as tb
+    return tb
+
+
+def _weights(seed):
+    rng = np.random.default_rng(seed)
+    n = lambda *s: rng.standard_normal(s).astype(np.float32)
+    return dict(emb=n(V, C), w1=1 + 0.2 * n(C), b1=0.1 * n(C), w_in=n(C, E) / C ** 0.5, conv=n(E, KC) / 2, conv_b=0.1 * n(E),
+                w_g=n(C, H) / C ** 0.5, w_beta=n(C, H) / C ** 0.5, w_out=n(H * DV, C) / (H * DV) ** 0.5, w2=1 + 0.2 * n(C),
+                b2=0.1 * n(C), head=n(C, V) / C ** 0.5 * 2)
+
+
+def _unit(a):
+    return a / a.pow(2).sum(-1, keepdim=True).add(1e-6).sqrt()
+
+
+def _mixed(u):
+    """q, k (unit length) and v of the convolution's channels."""
+    q, k, v = u[:, :QK], u[:, QK:2 * QK], u[:, 2 * QK:]
+    return _unit(q.unflatten(1, (HK, DK))), _unit(k.unflatten(1, (HK, DK))), v.unflatten(1, (H, DV))
+
+
+def _gates(n, w):
+    return -torch.nn.functional.softplus(n @ w["w_g"]), torch.sigmoid(n @ w["w_beta"])
+
+
+def _forward(tb, w, tokens, offs=None, conv=None, state=None, slots=None):
+    """Logits of the tokens' successors; states (in pools, changed in place) where given."""
+    x = w["emb"][tokens.long()]
+    n = tb.layer_norm(x, w["w1"], w["b1"])
+    u = tb.ssm_conv(n @ w["w_in"], w["conv"], w["conv_b"], offs=offs, state=conv, state_out=conv, slots=slots)
+    q, k, v = _mixed(u)
+    o = tb.delta_rule(q, k, v, *_gates(n, w), offs=offs, state=state, state_out=state, slots=slots)
+    y = x + o.flatten(1) @ w["w_out"]
+    return tb.layer_norm(y, w["w2"], w["b2"]) @ w["head"]
+
+
+def _logits64(w, tokens):
+    """The same for one sequence, token by token in 64 bits."""
+    w = {k: v.astype(np.float64) for k, v in w.items()}
+    x = w["emb"][tokens]
+    n = ol.layer_norm(x, w["w1"], w["b1"])["y"]
+    offs = np.array([0, len(tokens)])
+    u = osq.conv(n @ w["w_in"], w["conv"], w["conv_b"], offs)["u"]
+    q, k, v = (a.numpy() for a in _mixed(torch.from_numpy(u)))
+    g, beta = (a.numpy() for a in _gates(torch.from_numpy(n), {k: torch.from_numpy(v) for k, v in w.items()}))
+    o = ol.delta_rule(q, k, v, g, beta, offs)["o"]
+    y = x + o.reshape(len(tokens), -1) @ w["w_out"]
+    return ol.layer_norm(y, w["w2"], w["b2"])["y"] @ w["head"]
+
+
+def test_a_search_with_states():
+    """Two prompts of different lengths, four beams each, eight tokens: the same beams and scores as a search
+    that reads its prefixes anew in 64 bits."""
+    tb, w = _tb(), _weights(1)
+    g = {k: torch.from_numpy(v).cuda() for k, v in w.items()}
+    prompts, W, steps = [[3, 17, 5, 40, 2], [9, 9, 30]], 4, 8
+    G = len(prompts)
+    pool = G * W + 3
+    conv = torch.zeros(pool, KC - 1, E, device="cuda")
+    state = torch.zeros(pool, H, DK, DV, device="cuda")
+    order = torch.randperm(pool, generator=torch.Generator().manual_seed(0))[:G * W].int().cuda().view(G, W)
+    slots = order
+    # the prompts into each group's first beam, the only one that lives at first
+    toks = torch.tensor(sum(prompts, []), dtype=torch.int32, device="cuda")
+    offs = torch.tensor([0, 5, 8], dtype=torch.int32, device="cuda")
+    out = _forward(tb, g, toks, offs, conv, state, slots[:, 0].contiguous())
+    logits = torch.zeros(G * W, V, device="cuda")
+    logits[::W] = out[offs[1:].long() - 1]
+    score = torch.full((G, W), -float("inf"), device="cuda")
+    score[:, 0] = 0.0
+    history = [[list(p)] for p in prompts]
+    ref = [[(list(p), 0.0)] for p in prompts]
+    got = [[list(p)] * W for p in prompts]
+    for _ in range(steps):
+        r = tb.beam_select(logits, score)
+        slots = tb.beam_reorder(r["parent"], slots, [conv, state])
+        score = r["score"]
+        par, tok = r["parent"].cpu(), r["token"].cpu()
+        got = [[got[i][par[i, b] - i * W] + [int(tok[i, b])] for b in range(W)] for i in range(G)]
+        logits = _forward(tb, g, r["token"].view(-1), None, conv, state, slots.view(-1))
+        for i in range(G):
+            cand = []
+            for seq, s in ref[i]:
+                z = _logits64(w, np.array(seq))[-1]
+                lp = z - z.max() - np.log(np.exp(z - z.max()).sum())
+                cand += [(s + lp[t], seq + [t]) for t in range(V)]
+            cand.sort(key=lambda c: -c[0])
+            # (the search is one that fp32 can tell apart)
+            assert all(cand[j][0] - cand[j + 1][0] > 1e-4 for j in range(W))
+            ref[i] = [(seq, s) for s, seq in cand[:W]]
+            assert [seq for seq, _ in ref[i]] == got[i]
+            # logits of order 5 are sums of some 100 fp32 products, ten tokens' states behind them: 2^-24 x 5 x 100 each
+            assert np.abs(score[i].cpu().numpy() - [s for _, s in ref[i]]).max() < 2.0 ** -24 * 500 * 12
+    assert sorted(slots.flatten().tolist()) == sorted(order.flatten().tolist())
+    rest = [i for i in range(pool) if i not in order.flatten().tolist()]
+    assert not state[rest].any() and not conv[rest].any()
+
+
+def test_a_training_step():
+    """Gradients of all weights of the layer, sequence operators' own backward calls chained by hand,
+    against float64 differentiation of the same formulas. 2-norms: sums of up to 200 rows of some 100 products each through
+    five operators, 2^-24 sqrt(100) x 5 < 3.1e-6 of the result; 1e-5 with what their cancellations take."""
+    tb, wn = _tb(), _weights(2)
+    w = {k: torch.from_numpy(v).cuda() for k, v in wn.items()}
+    lens = [70, 1, 0, 55, 74]
+    offs = torch.tensor(np.concatenate([[0], np.cumsum(lens)]), dtype=torch.int32, device="cuda")
+    T = sum(lens)
+    torch.manual_seed(3)
+    x, dy = torch.randn(T, C, device="cuda"), torch.randn(T, C, device="cuda")
+    # forward
+    n = tb.layer_norm(x, w["w1"], w["b1"])
+    xin = n @ w["w_in"]
+    u = tb.ssm_conv(xin, w["conv"], w["conv_b"], offs=offs)
+    ul, nl = u.detach().requires_grad_(True), n.detach().requires_grad_(True)
+    wl = {k: w[k].detach().requires_grad_(True) for k in ("w_g", "w_beta")}
+    q, k, v = _mixed(ul)
+    g, beta = _gates(nl, wl)
+    o = tb.delta_rule(q.detach(), k.detach(), v.detach(), g.detach(), beta.detach(), offs=offs)
+    # backward
+    got = dict(w_out=o.flatten(1).T @ dy)
+    do = (dy @ w["w_out"].T).view(T, H, DV)
+    d = tb.delta_rule_backward(q.detach(), k.detach(), v.detach(), g.detach(), beta.detach(), do, offs=offs)
+    du, dn, got["w_g"], got["w_beta"] = torch.autograd.grad(
+        [q, k, v, g, beta], [ul, nl, wl["w_g"], wl["w_beta"]], [d["dq"], d["dk"], d["dv"], d["dg"], d["dbeta"]])
+    c = tb.ssm_conv_backward(xin, w["conv"], w["conv_b"], du.contiguous(), offs=offs)
+    got.update(conv=c["dw"], conv_b=c["db"], w_in=n.T @ c["dx"])
+    ln = tb.layer_norm_backward(x, w["w1"], dn + c["dx"] @ w["w_in"].T)
+    got.update(w1=ln["dw"], b1=ln["db"], x=ln["dx"] + dy)
+    # the same in float64 on the host
+    p = {k: torch.from_numpy(a).double().requires_grad_(True) for k, a in wn.items()}
+    X = x.cpu().double().requires_grad_(True)
+    N = torch.nn.functional.layer_norm(X, (C,), p["w1"], p["b1"])
+    outs, at = [], 0
+    for L in lens:
+        m = N[at:at + L]
+        xi = m @ p["w_in"]
+        win = torch.cat([torch.zeros(KC - 1, E, dtype=torch.float64), xi])
+        pre = p["conv_b"] + sum(p["conv"][:, j] * win[j:j + L] for j in range(KC))
+        qq, kk, vv = _mixed(pre * torch.sigmoid(pre))
+        gg, bb = _gates(m, p)
+        S = torch.zeros(H, DK, DV, dtype=torch.float64)
+        qq, kk = qq.repeat_interleave(H // HK, 1), kk.repeat_interleave(H // HK, 1)
+        for t in range(L):
+            S = S * gg[t].exp()[:, None, None]
+            uu = bb[t][:, None] * (vv[t] - (S * kk[t][:, :, None]).sum(1))
+            S = S + kk[t][:, :, None] * uu[:, None, :]
+            outs.append((S * qq[t][:, :, None]).sum(1) * DK ** -0.5)
+        at += L
+    Y = X + torch.stack(outs).flatten(1) @ p["w_out"]
+    names = ["w1", "b1", "w_in", "conv", "conv_b", "w_g", "w_beta", "w_out"]
+    want = dict(zip(names + ["x"], torch.autograd.grad((Y * dy.cpu().double()).sum(), [p[k] for k in names] + [X])))
+    for name, ref in want.items():
+        e = ((got[name].cpu().double() - ref).norm() / ref.norm()).item()
+        assert e < 1e-5, (name, e)
