@@ -597,14 +597,13 @@ def _under(stream, call, *args, **kw):
 
 def _results(new, out, like):
     """new's tensors (name: shape, type, rows of a leading dimension or not), out's where it has them."""
-    import torch
     r = {}
     for name, spec in new.items():
         t = None if out is None else out.get(name)
         if spec is None:
             r[name] = None
         elif t is None:
-            r[name] = torch.empty(spec[0], dtype=spec[1], device=like.device)
+            r[name] = like.new_empty(spec[0], dtype=spec[1])
         else:
             _expect(name, t, spec[1], spec[0], like, rows=spec[2])
             r[name] = t
@@ -625,7 +624,7 @@ def _workspace(workspace, like, size, *args):
             raise ValueError(f"workspace: contiguous memory on {like.device} expected")
         return workspace
     need = size(*args)
-    return torch.empty(need, dtype=torch.uint8, device=like.device) if need else None
+    return like.new_empty(need, dtype=torch.uint8) if need else None
 
 
 def _ws_args(ws):
@@ -809,13 +808,13 @@ def ssm_scan_backward(u, dt, A_log, B, C, dy, D=None, z=None, b_dt=None, offs=No
 
 def _heads_ld(name, t, dtype, shape, like) -> int:
     """Checks a tensor [rows, heads, width] whose rows are contiguous; its leading dimension."""
+    width = shape[1] * shape[2]
+    if t.dtype is dtype and t.shape == shape and t.is_contiguous() and t.get_device() == like.get_device():
+        return width
     if t.dtype is not dtype or t.shape != shape:
         raise ValueError(f"{name}: {dtype} {tuple(shape)} expected, not {t.dtype} {tuple(t.shape)}")
     if t.get_device() != like.get_device():
         raise ValueError(f"{name} is on {t.device}, not on {like.device}")
-    width = shape[1] * shape[2]
-    if t.is_contiguous():
-        return width
     if (shape[2] != 1 and t.stride(2) != 1) or (shape[1] != 1 and t.stride(1) != shape[2]) or (
             shape[0] != 1 and t.stride(0) < width):
         raise ValueError(f"{name}: rows not contiguous (strides {t.stride()})")
@@ -823,23 +822,23 @@ def _heads_ld(name, t, dtype, shape, like) -> int:
 
 
 def _delta_args(q, k, v, g, beta, scale, offs, state):
-    """(number of sequences, the packed tcl_delta_rule_args)"""
+    """(number of sequences, a state's shape, the packed tcl_delta_rule_args)"""
     import torch
-    for name, t in (("q", q), ("v", v)):
-        if t.dim() != 3:
-            raise ValueError(f"{name}: [rows, heads, width] expected, not {tuple(t.shape)}")
+    sq, sv, dt, f32 = q.shape, v.shape, q.dtype, torch.float32
+    if len(sq) != 3 or len(sv) != 3:
+        raise ValueError(f"q, v: [rows, heads, width] expected, not {tuple(sq)}, {tuple(sv)}")
     _on_device(q)
-    n_seq = q.shape[0]
+    (rows, Hk, Dk), (_, H, Dv) = sq, sv
+    n_seq = rows
     if offs is not None:
         if offs.dim() != 1 or offs.numel() < 1:
             raise ValueError("offs: [n_seq + 1] expected")
         _expect("offs", offs, torch.int32, offs.shape, q)
         n_seq = offs.numel() - 1
-    (rows, Hk, Dk), (_, H, Dv) = q.shape, v.shape
-    ldq, ldk = _heads_ld("q", q, q.dtype, q.shape, q), _heads_ld("k", k, q.dtype, q.shape, q)
-    ldv = _heads_ld("v", v, q.dtype, (rows, H, Dv), q)
-    ldg, ldb = _row_ld("g", g, torch.float32, (rows, H), q), _row_ld("beta", beta, torch.float32, (rows, H), q)
-    return n_seq, _PACK_DELTA.pack(_dtype(q), n_seq, rows, Hk, H, Dk, Dv, Dk ** -0.5 if scale is None else scale,
+    ldq, ldk = _heads_ld("q", q, dt, sq, q), _heads_ld("k", k, dt, sq, q)
+    ldv = _heads_ld("v", v, dt, (rows, H, Dv), q)
+    ldg, ldb = _row_ld("g", g, f32, (rows, H), q), _row_ld("beta", beta, f32, (rows, H), q)
+    return n_seq, (H, Dk, Dv), _PACK_DELTA.pack(_dtype(q), n_seq, rows, Hk, H, Dk, Dv, Dk ** -0.5 if scale is None else scale,
                                    _adr(offs), q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(), ldv, g.data_ptr(),
                                    ldg, beta.data_ptr(), ldb, _adr(state))
 
@@ -863,12 +862,10 @@ def delta_rule(q, k, v, g, beta, scale=None, offs=None, state=None, state_out=No
     if stream is not None:
         return _under(stream, delta_rule, q, k, v, g, beta, scale, offs, state, state_out, slots, out, workspace)
     import torch
-    n_seq, a = _delta_args(q, k, v, g, beta, scale, offs, state)
-    shape = (v.shape[1], q.shape[2], v.shape[2])
+    n_seq, shape, a = _delta_args(q, k, v, g, beta, scale, offs, state)
     n_slots = _pools(state, state_out, slots, n_seq, shape, torch.float32, q)
     if out is None:
-        out = torch.empty(v.shape, dtype=v.dtype, device=v.device)
-        ldo = v.shape[1] * v.shape[2]
+        out, ldo = v.new_empty(v.shape), shape[0] * shape[2]
     else:
         ldo = _heads_ld("out", out, q.dtype, v.shape, q)
     ws = None if offs is None else _workspace(workspace, q, lib().tcl_delta_rule_workspace_bytes, _dtype(q), n_seq,
@@ -887,9 +884,9 @@ def delta_rule_backward(q, k, v, g, beta, do, scale=None, offs=None, state=None,
     if stream is not None:
         return _under(stream, delta_rule_backward, q, k, v, g, beta, do, scale, offs, state, state_grad, workspace, out)
     import torch
-    n_seq, a = _delta_args(q, k, v, g, beta, scale, offs, state)
+    n_seq, shape, a = _delta_args(q, k, v, g, beta, scale, offs, state)
     lddo = _heads_ld("do", do, q.dtype, v.shape, q)
-    f32, full = torch.float32, (n_seq, v.shape[1], q.shape[2], v.shape[2])
+    f32, full = torch.float32, (n_seq, *shape)
     for name, t in (("state", state), ("state_grad", state_grad)):
         _expect(name, t, f32, full, q)
     r = _results(dict(dq=(q.shape, q.dtype, False), dk=(q.shape, q.dtype, False), dv=(v.shape, q.dtype, False),
@@ -917,14 +914,15 @@ def layer_norm(x, w=None, b=None, eps=1e-5, out=None, stream=None):
     if stream is not None:
         return _under(stream, layer_norm, x, w, b, eps, out)
     import torch
-    rows, C = _row_matrix(x)
-    ldx = _row_ld("x", x, x.dtype, x.shape, x)
+    shape = _row_matrix(x)
+    rows, C = shape
+    ldx = _row_ld("x", x, x.dtype, shape, x)
     _expect("w", w, torch.float32, (C,), x)
     _expect("b", b, torch.float32, (C,), x)
     if out is None:
-        out, ldy = torch.empty(x.shape, dtype=x.dtype, device=x.device), C
+        out, ldy = x.new_empty(shape), C
     else:
-        ldy = _row_ld("out", out, x.dtype, x.shape, x)
+        ldy = _row_ld("out", out, x.dtype, shape, x)
     check(lib().tcl_layer_norm(_dtype(x), rows, C, x.data_ptr(), ldx, _ptr(w), _ptr(b), eps, out.data_ptr(), ldy,
                                _stream_of(x)))
     return out
@@ -1054,9 +1052,9 @@ def beam_select(logits, score, K=None, ended=None, temperature=1.0, workspace=No
     _expect("score", score, torch.float32, (G, W), logits)
     _expect("ended", ended, torch.int32, (G, W), logits)
     K = W if K is None else K
-    r = dict(parent=torch.empty(G, max(K, 0), dtype=torch.int32, device=logits.device),
-             token=torch.empty(G, max(K, 0), dtype=torch.int32, device=logits.device),
-             score=torch.empty(G, max(K, 0), dtype=torch.float32, device=logits.device))
+    places = (G, max(K, 0))
+    r = dict(parent=logits.new_empty(places, dtype=torch.int32), token=logits.new_empty(places, dtype=torch.int32),
+             score=score.new_empty(places))
     ws = _workspace(workspace, logits, lib().tcl_beam_select_workspace_bytes, G, W, V, K)
     check(lib().tcl_beam_select(_dtype(logits), G, W, V, logits.data_ptr(), ld, temperature, score.data_ptr(),
                                 _ptr(ended), K, r["parent"].data_ptr(), r["token"].data_ptr(), r["score"].data_ptr(),
@@ -1088,7 +1086,7 @@ def beam_reorder(parent, slots, pools, out=None, stream=None):
         array[i].d_states = t.data_ptr()
         array[i].bytes = t.numel() // max(n_slots, 1) * t.element_size() if n_slots else 1
     if out is None:
-        out = torch.empty(G, W, dtype=torch.int32, device=parent.device)
+        out = parent.new_empty((G, W))
     check(lib().tcl_beam_reorder(G, W, parent.data_ptr(), slots.data_ptr(), n_slots, out.data_ptr(), len(pools), array,
                                  _stream_of(parent)))
     return out
