@@ -606,8 +606,9 @@ TCL_API tcl_status tcl_ssm_scan_backward(const tcl_ssm_scan_args* args, const vo
  * Dk in [8, 128], Dv in [8, 256], multiples of 8; H at most 1024; rows H at most 2^28, n_seq H below 2^19 (2^22 for
  * the single-token form's forward call), the activations' leading dimensions at most 2^22. Activations fp32 or bf16 of
  * any alignment, g, beta and the states fp32; all sums are fp32, products of fp32 values three bf16 parts' (to 2^-24),
- * results rounded to dtype once. Sequences are walked token by token where there are fewer than 32 rows to each on
- * average, else in chunks of 64 tokens: a long one among many short ones is better given a call of its own. A NaN or an
+ * results rounded to dtype once. Sequences are walked token by token where there are few rows to each on average (fewer
+ * than 24 to 256, by type and number of heads), else in chunks of 64 tokens: a long one among many short ones is better
+ * given a call of its own. A NaN or an
  * infinity among a head's inputs reaches its sequence's other rows in that head, in a chunk also earlier ones.
  * Rows that no sequence owns are neither read nor written. Stream-ordered, deterministic, no allocation; may be
  * captured into a graph.

@@ -11,7 +11,9 @@ namespace {
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef u32x4 u32x4_any __attribute__((aligned(1)));  // states of any size start anywhere
 
-constexpr int kSegment = 16 * 1024;  // bytes that one workgroup copies of each state
+// Bytes that one workgroup copies of each state: 64 groups of 8 beams with 130 segments of 16 KB take 83.9 us, of 8 KB 80.9,
+// of 4 KB 82.9.
+constexpr int kSegment = 8 * 1024;
 constexpr int kThreads = 256;
 
 struct Pools {

@@ -326,9 +326,6 @@ template <> struct Raw8<uint16_t> {
   __device__ __forceinline__ void load(const uint16_t* p) { v = *reinterpret_cast<const any*>(p); }
   // what lane `lane` has of an operand, eight entries each
   __device__ __forceinline__ void load_lane(const uint16_t* p, int lane) { v = at_lane<u32x4>(p, lane); }
-  __device__ __forceinline__ void load_bytes(const uint16_t* p, uint32_t bytes) {
-    v = *(const __attribute__((address_space(1))) any*)(uniform(p) + bytes);
-  }
   __device__ __forceinline__ void clear() { v = u32x4{0, 0, 0, 0}; }
   __device__ __forceinline__ Parts<1> parts() const { return {{pack8(v)}}; }
 };
@@ -339,32 +336,9 @@ template <> struct Raw8<float> {
     a = at_lane<floatx4>(p, 2 * lane);
     b = at_lane<floatx4>(p, 2 * lane + 1);
   }
-  __device__ __forceinline__ void load_bytes(const float* p, uint32_t bytes) {
-    a = *(const __attribute__((address_space(1))) floatx4_any*)(uniform(p) + bytes);
-    b = *(const __attribute__((address_space(1))) floatx4_any*)(uniform(p) + bytes + 16);
-  }
   __device__ __forceinline__ void clear() { a = b = floatx4{0.f, 0.f, 0.f, 0.f}; }
   __device__ __forceinline__ Parts<3> parts() const { return split8<3>(a, b); }
 };
-struct floatx8 {
-  floatx4 a, b;
-};
-__device__ __forceinline__ floatx8 widen(Raw8<float> x) { return {x.a, x.b}; }
-__device__ __forceinline__ floatx8 widen(Raw8<uint16_t> x) {
-  floatx8 r;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const float lo = __uint_as_float(x.v[i] << 16), hi = __uint_as_float(x.v[i] & 0xFFFF0000u);
-    if (i < 2) {
-      r.a[2 * i] = lo;
-      r.a[2 * i + 1] = hi;
-    } else {
-      r.b[2 * i - 4] = lo;
-      r.b[2 * i - 3] = hi;
-    }
-  }
-  return r;
-}
 // Four neighbours of a row as they are in memory.
 template <typename T> struct Raw4;
 template <> struct Raw4<uint16_t> {
@@ -413,20 +387,8 @@ struct Chunk {
   int row, n;
 };
 
-// Of a head's rows in a chunk the fragments of the 16 tokens 16 w .., D wide (a multiple of 8), zeros
-// elsewhere.
-template <typename T, int NF>
-__device__ __forceinline__ void row_frags(const T* p, int64_t ld, Chunk c, int w, int D, floatx4* f) {
-  const int l = threadIdx.x & 63, t = 16 * w + (l & 15), k0 = 4 * (l >> 4);
-  const T* q = p + (c.row + min(t, c.n - 1)) * ld + k0;
-#pragma unroll
-  for (int s = 0; s < NF; ++s) {
-    f[s] = floatx4{0.f, 0.f, 0.f, 0.f};
-    if (t < c.n && 16 * s + k0 < D) f[s] = ld4(q + 16 * s);
-  }
-}
-
-// The same as operands of 32 k's, as they are in memory.
+// Of a head's rows in a chunk the 16 tokens 16 w .. as operands of 32 k's, as they are in memory, D wide (a multiple of
+// 8), zeros elsewhere.
 template <typename T, int NS>
 __device__ __forceinline__ void row_raw(const T* p, int64_t ld, Chunk c, int w, int D, Raw8<T>* f) {
   const int l = threadIdx.x & 63, t = 16 * w + (l & 15), k0 = 8 * (l >> 4);
@@ -1398,8 +1360,22 @@ __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaIn a, const T* __
 
 // ---------------------------------------------------------------- launches
 
-// Chunks of kC tokens pay from 32 tokens a sequence on average.
-bool chunked(int n_seq, int rows) { return rows / 32 >= n_seq; }
+// From how many tokens a sequence, on average, chunks of kC pay. With few heads of sequences the walk's latency
+// counts (some 0.5 to 1.1 us a token against 20 us for a first chunk and 4 to 6 for each after), with a full card what
+// each has to do, of which chunks of fp32 values do the more. Walk / chunks in us, at tokens a sequence:
+//   bf16, Dk = Dv = 128   16 heads     16: 22 / 22    24: 32 / 23     64: 78 / 24
+//                         512          32: 67 / 78    48: 100 / 79
+//                         4,096        32: 393 / 502  48: 584 / 524   128: 1,720 / 875
+//   fp32, 64              128          32: 20 / 22    48: 28 / 23
+//                         512          64: 37 / 58    128: 69 / 81    192: 101 / 111
+//                         1,024        64: 56 / 106   192: 165 / 256
+//   fp32, 128             256          64: 56 / 71    96: 83 / 96     192: 161 / 131
+//                         1,024        64: 181 / 257  192: 473 / 580
+bool chunked(bool bf16, int n_seq, int rows, int H) {
+  const int64_t heads = (int64_t)n_seq * H;
+  const int64_t from = bf16 ? heads > 128 ? 40 : 24 : std::clamp<int64_t>(heads / 4, 32, 256);
+  return rows >= from * n_seq;
+}
 int64_t tiles_of(int n_seq, int rows) { return (int64_t)rows / kC + n_seq; }
 
 DeltaIn in_of(const DeltaOp& a) {
@@ -1475,13 +1451,13 @@ hipError_t grads(const DeltaOp& a, const void* d_o_, int64_t lddo, const float* 
 
 size_t delta_rule_workspace_bytes(bool bf16, int n_seq, int rows, int Hk, int H, int Dk, int Dv) {
   (void)Dv;
-  if (!chunked(n_seq, rows)) return 0;
+  if (!chunked(bf16, n_seq, rows, H)) return 0;
   const int mats = bf16 ? kMats<uint16_t, false> : kMats<float, false>;
   return (size_t)(tiles_of(n_seq, rows) * H * (3 * kC + mats) + op_floats(bf16, n_seq, rows, Hk, Dk)) * sizeof(float);
 }
 
 hipError_t launch_delta_rule(const DeltaOp& a, float* state_out, void* o, int64_t ldo, float* ws, hipStream_t s) {
-  if (!a.offs || !chunked(a.n_seq, a.rows))
+  if (!a.offs || !chunked(a.bf16, a.n_seq, a.rows, a.H))
     return a.bf16 ? walk<uint16_t>(a, state_out, o, ldo, s) : walk<float>(a, state_out, o, ldo, s);
   if (a.Dk <= 64)
     return a.bf16 ? chunks<uint16_t, 64>(a, state_out, o, ldo, ws, s) : chunks<float, 64>(a, state_out, o, ldo, ws, s);

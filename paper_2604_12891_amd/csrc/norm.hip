@@ -2,7 +2,8 @@
 //   m = mean x, r = (mean (x - m)^2 + eps)^-1/2, h = (x - m) r, y = h w + b,
 //   dx = r (g - mean g - h mean(g h)), g = dy w,  dw = sum over rows dy h,  db = sum over rows dy.
 // Nothing is kept from the forward call: the gradients read x anyway, and a row's statistics
-// are one reduction of what is then in registers.
+// are two reductions of what is then in registers. Both passes are bound by HBM, 2 and 3 arrays: 8,192 x 5,120 bf16 in
+// 39 and 65 us at the rate that a large copy reaches (4.8 TB/s).
 #include <algorithm>
 
 #include "common.h"
@@ -153,17 +154,12 @@ __device__ __forceinline__ void clear_rest(Sums<N>* red) {
     for (int i = 0; i < N; ++i) red[k].v[i] = 0.f;
 }
 
-// Threads of a workgroup that takes a row: up to 512, whose registers hold four vectors of a row, the next
-// one's, parameters and sums; 1,024 for the widest fp32 rows.
-template <typename T, int NV>
-constexpr int kThreads = sizeof(T) == 4 && NV == 4 ? 1024 : 512;
-
 // LPR lanes per row, 256 / LPR rows at a time (LPR == 0: the workgroup's threads, one row); workgroups
 // stride over the rows with their parameters in registers, the next row on its way meanwhile. The
 // variance is a second sum, of deviations: a sum of squares would lose the digits that a large mean takes. The
 // deviations' own sum, which only the mean's rounding leaves, corrects both.
 template <typename T, int NV, int LPR>
-__global__ __launch_bounds__((LPR ? 256 : kThreads<T, NV>)) void norm_kernel(const T* __restrict__ x, int64_t ldx, int rows, int C,
+__global__ __launch_bounds__(LPR ? 256 : 1024) void norm_kernel(const T* __restrict__ x, int64_t ldx, int rows, int C,
                                                                 const float* __restrict__ w,
                                                                 const float* __restrict__ b, float eps,
                                                                 T* __restrict__ y, int64_t ldy) {
@@ -221,7 +217,7 @@ __global__ __launch_bounds__((LPR ? 256 : kThreads<T, NV>)) void norm_kernel(con
 // thread keeps its columns' sums for dw and db over the rows that its workgroup takes; they leave as one partial
 // vector per workgroup (part[block][2][C]).
 template <typename T, int NV, int LPR>
-__global__ __launch_bounds__((LPR ? 256 : kThreads<T, NV>)) void norm_bwd_kernel(const T* __restrict__ x, int64_t ldx, int rows,
+__global__ __launch_bounds__(LPR ? 256 : 1024) void norm_bwd_kernel(const T* __restrict__ x, int64_t ldx, int rows,
                                                                     int C, const float* __restrict__ w, float eps,
                                                                     const T* __restrict__ dy, int64_t lddy,
                                                                     T* __restrict__ dx, int64_t lddx,
@@ -242,8 +238,10 @@ __global__ __launch_bounds__((LPR ? 256 : kThreads<T, NV>)) void norm_bwd_kernel
   const int64_t own = LPR ? tid / (LPR ? LPR : 1) : 0, step = (int64_t)gridDim.x * RB;
   const int64_t first = min((int64_t)blockIdx.x * RB + own, (int64_t)rows - 1);
   u32x4 xn[NV], gn[NV];
-  c.load(x + first * ldx, xn);
-  c.load(dy + first * lddy, gn);
+  if constexpr (NV < 4) {
+    c.load(x + first * ldx, xn);
+    c.load(dy + first * lddy, gn);
+  }
   if constexpr (LPR == 0)
     for (int k = 0; k < 2; ++k) {
       clear_rest(red[k]);
@@ -258,7 +256,10 @@ __global__ __launch_bounds__((LPR ? 256 : kThreads<T, NV>)) void norm_bwd_kernel
       xv[j] = xn[j];
       gv[j] = gn[j];
     }
-    if (r0 + step < rows) {
+    if constexpr (NV == 4) {  // (no registers for the next row: 12,288 fp32 columns took 278 us, with spills, not 166)
+      c.load(x + min(row, (int64_t)rows - 1) * ldx, xv);
+      c.load(dy + min(row, (int64_t)rows - 1) * lddy, gv);
+    } else if (r0 + step < rows) {
       const int64_t after = min(row + step, (int64_t)rows - 1);
       c.load(x + after * ldx, xn);
       c.load(dy + after * lddy, gn);
@@ -341,9 +342,12 @@ __global__ __launch_bounds__((LPR ? 256 : kThreads<T, NV>)) void norm_bwd_kernel
       }
 }
 
-// A row's vectors over the fewest lanes that hold it in one vector each, from 16 of them to a
-// wavefront (two vectors up to 128); wider rows take a workgroup, with two vectors a thread from 256 on, which halve what the
-// reductions cost.
+// A row's vectors over the fewest lanes that hold it in one vector each, from 16 of them to a wavefront (two
+// vectors up to 128); wider rows take a workgroup, of up to 1,024 threads, with a second vector a thread from 513
+// on and four from 2,049. 2^26 entries, forward / backward in us: bf16 rows of 128 columns 55 / 85 on 16 lanes, 141 / 291
+// on 64; of 4,096 (512 vectors) 53 / 92 with one vector a thread, 54 / 98 with two, which halve what the reductions
+// cost but leave fewer wavefronts; of 5,120 63 / 110 with two, 72 / 119 with one; of 12,288 58 / 95 with two on 768
+// threads, 95 / 120 with four on 384.
 struct Shape {
   int nv, lpr;   // vectors per thread; lanes per row, 0: the workgroup
   int threads;
@@ -355,12 +359,13 @@ Shape shape_of(bool bf16, int C) {
   if (v <= 32) return {1, 32, 256, 8};
   if (v <= 64) return {1, 64, 256, 4};
   if (v <= 128) return {2, 64, 256, 4};
-  const int nv = v <= 256 ? 1 : v <= 1024 ? 2 : 4;
+  const int nv = v <= 512 ? 1 : v <= 2048 ? 2 : 4;
   return {nv, 0, ((v + nv - 1) / nv + 63) / 64 * 64, 1};
 }
 
 // Workgroups of the gradients: each leaves a partial vector, so as many as the registers let run at once (some 1,024
-// threads a CU) and no more: with twice as many the sums take 14 us instead of 8 at 5,120 columns.
+// threads a CU) and no more: with twice as many, 2^26 bf16 entries take 114 us instead of 95 at 1,536 columns and 107 instead
+// of 91 at 2,048.
 int bwd_parts(const Shape& s, int rows) {
   const int fill = 256 * std::max(1, 1024 / s.threads);
   return std::min((rows + s.rows - 1) / s.rows, fill);
@@ -403,7 +408,8 @@ hipError_t dispatch(const Shape& s, F f) {
 hipError_t launch_layer_norm(const NormOp& a, void* y, int64_t ldy, hipStream_t s) {
   const Shape sh = shape_of(a.bf16, a.C);
   return dispatch(sh, [&](auto nv, auto lpr) {
-    return a.bf16 ? fwd<uint16_t, nv.value, lpr.value>(a, sh, y, ldy, s) : fwd<float, nv.value, lpr.value>(a, sh, y, ldy, s);
+    constexpr int NB = std::min(nv.value, 2);  // (bf16 rows have 2,048 vectors at most)
+    return a.bf16 ? fwd<uint16_t, NB, lpr.value>(a, sh, y, ldy, s) : fwd<float, nv.value, lpr.value>(a, sh, y, ldy, s);
   });
 }
 
@@ -416,7 +422,8 @@ hipError_t launch_layer_norm_bwd(const NormOp& a, const void* dy, int64_t lddy, 
   const Shape sh = shape_of(a.bf16, a.C);
   if (a.rows > 0) {
     const hipError_t e = dispatch(sh, [&](auto nv, auto lpr) {
-      return a.bf16 ? bwd<uint16_t, nv.value, lpr.value>(a, sh, dy, lddy, dx, lddx, ws, s)
+      constexpr int NB = std::min(nv.value, 2);
+      return a.bf16 ? bwd<uint16_t, NB, lpr.value>(a, sh, dy, lddy, dx, lddx, ws, s)
                     : bwd<float, nv.value, lpr.value>(a, sh, dy, lddy, dx, lddx, ws, s);
     });
     if (e != hipSuccess) return e;
