@@ -113,6 +113,34 @@ def test_delta_call_refusals(lib):
         assert _call(lib.tcl_delta_rule_backward, ok, g=ctypes.byref(_grads(**kw))) == -1, kw
 
 
+def test_delta_limits(lib):
+    """Leading dimensions whose chunk would not be addressed in 31 bits, and launches of 2^32 threads, are refused; the
+    largest that are not come to the next check."""
+    top = 1 << 22
+    ok = dict(a=None, slots=None, n_slots=1 << 20, so=None, o=None, ldo=128, ws=FAKE, n=BIG, stream=None)
+    call = lambda ldo=128, **kw: _call(lib.tcl_delta_rule, ok, a=ctypes.byref(_delta(**kw)), ldo=ldo)
+    for name in ("ldq", "ldk", "ldv"):
+        assert call(**{name: top}) == -1  # (no o)
+        assert call(**{name: top + 1}) == -2
+    assert call(ldo=top) == -1 and call(ldo=top + 1) == -2
+    # a token of each sequence: 2^22 heads of sequences; packed: 2^19; gradients: 2^19 for both
+    token = dict(rows=1 << 18, n_seq=1 << 18, d_offs=None, Hk=1, ldg=16, ldbeta=16, ldv=512)
+    assert call(ldo=512, H=15, **token) == -1
+    assert call(ldo=512, H=16, **token) == -2
+    packed = dict(n_seq=1 << 17, Hk=1)
+    assert call(H=3, **packed) == -1 and call(H=4, **packed) == -2
+    grads = dict(a=None, do=None, lddo=512, dso=None, g=ctypes.byref(_grads()), ws=FAKE, n=BIG, stream=None)
+    back = lambda g=None, lddo=512, **kw: _call(lib.tcl_delta_rule_backward, grads, a=ctypes.byref(_delta(**kw)), lddo=lddo,
+                                                g=ctypes.byref(_grads(**(g or {}))))
+    token.update(rows=1 << 17, n_seq=1 << 17)
+    assert back(H=3, **token) == -1  # (no dO)
+    assert back(lddo=top) == -1 and back(lddo=top + 1) == -2
+    for name in ("lddq", "lddk", "lddv"):
+        assert back({name: top}) == -1 and back({name: top + 1}) == -2
+    grads["do"] = FAKE
+    assert back(H=4, **token) == -2
+
+
 def test_delta_layouts():
     """The structures' bytes as the binding packs them are the structures."""
     v = list(range(1, 20))

@@ -128,6 +128,22 @@ def test_rule_and_gradients(lens, Hk, H, Dk, Dv, steep, dtype):
             assert (g[name][T:] == 7.0).all(), name
 
 
+@pytest.mark.parametrize("dtype,lens,H", [
+    ("bf16", [24] * 3, 4), ("bf16", [23] * 3, 4), ("bf16", [39, 40] * 20, 8), ("bf16", [40, 41] * 20, 8),
+    ("f32", [31, 32], 4), ("f32", [32, 33], 4), ("f32", [150, 172] * 10, 32), ("f32", [150, 168] * 10, 32),
+    ("f32", [300, 210, 258] * 5, 80), ("f32", [300, 205, 258] * 5, 80)])
+def test_token_by_token_or_in_chunks(dtype, lens, H):
+    """Averages on both sides of where chunks begin, with few and many heads: no answer depends on it."""
+    print(f"delta rule's two forms: {len(lens)} sequences of {lens[:3]} H={H} {dtype}", flush=True)
+    a = _case(lens, H // 2, H, 8, 8, dtype, len(lens) + H)
+    x, offs = _gpu(a, dtype, loose=False, spare=0), torch.from_numpy(a["offs"]).cuda()
+    S = torch.from_numpy(a["state"]).float().cuda()
+    o = _tb().delta_rule(**x, offs=offs, state=S, state_out=S)
+    r, tol = ol.delta_rule(**a), tolerance(8, lens)
+    _near("o", o, r["o"], tol + (2.0 ** -8 if dtype == "bf16" else 0.0))
+    _near("end", S, r["end"], tol)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("n,Hk,H,Dk,Dv", [(1, 1, 1, 64, 64), (7, 2, 4, 24, 40), (40, 1, 2, 128, 256), (3, 1, 1, 8, 8)])
 def test_tokens_with_slots(n, Hk, H, Dk, Dv, dtype):

@@ -169,3 +169,29 @@ def test_a_training_step():
     for name, ref in want.items():
         e = ((got[name].cpu().double() - ref).norm() / ref.norm()).item()
         assert e < 1e-5, (name, e)
+
+
+def test_the_readme_example():
+    """What the readme shows of them, on small tensors."""
+    from paper_2604_12891_amd import binding as tcl
+    T, C, H, Hk, D, G, W, V = 12, 24, 4, 2, 16, 2, 3, 40
+    r = lambda *s: torch.randn(*s, device="cuda")
+    x, w, b, dh, do = r(T, C), r(C), r(C), r(T, C), r(T, H, D)
+    q, k, v, g, beta = r(T, Hk, D) / 4, r(T, Hk, D) / 4, r(T, H, D), -torch.rand(T, H, device="cuda"), torch.rand(T, H, device="cuda")
+    offs, state = torch.tensor([0, 5, 5, 12], dtype=torch.int32, device="cuda"), torch.empty(3, H, D, D, device="cuda")
+    n1 = G * W
+    q1, k1, v1, g1, beta1 = q[:n1], k[:n1], v[:n1], g[:n1], beta[:n1]
+    pool, slots = torch.zeros(n1 + 2, H, D, D, device="cuda"), torch.arange(n1, dtype=torch.int32, device="cuda").view(G, W)
+    logits, score = r(n1, V), r(G, W)
+    ended = torch.tensor([[-1, -1, 7], [-1, -1, -1]], dtype=torch.int32, device="cuda")
+    h = tcl.layer_norm(x, w, b)
+    o = tcl.delta_rule(q, k, v, g, beta, offs=offs, state_out=state)
+    n = tcl.layer_norm_backward(x, w, dh)
+    d = tcl.delta_rule_backward(q, k, v, g, beta, do, offs=offs)
+    o1 = tcl.delta_rule(q1, k1, v1, g1, beta1, state=pool, state_out=pool, slots=slots.view(-1))
+    s = tcl.beam_select(logits, score, ended=ended)
+    slots = tcl.beam_reorder(s["parent"], slots, [pool])
+    for t in (h, o, state, *n.values(), *(d[i] for i in ("dq", "dk", "dv", "dg", "dbeta")), o1, s["score"], pool):
+        assert torch.isfinite(t).all()
+    assert sorted(slots.flatten().tolist()) == list(range(n1)) and s["parent"].shape == (G, W)
+    assert not state[1].any()  # the empty sequence's

@@ -67,7 +67,7 @@ def test_norm_and_gradients(rows, C, pad, first, dtype):
         assert (buf == 7.0).sum() >= buf.numel() - rows * C
 
 
-@pytest.mark.parametrize("rows,C", [(5000, 40), (3000, 256), (2100, 2056)])
+@pytest.mark.parametrize("rows,C", [(5000, 40), (3000, 256), (2100, 2056), (1100, 5120), (600, 9001)])
 def test_many_rows(rows, C):
     """More rows than workgroups; the same bits every time."""
     print(f"norm rows={rows} C={C}", flush=True)
