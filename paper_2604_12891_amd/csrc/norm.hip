@@ -346,7 +346,7 @@ __global__ __launch_bounds__(LPR ? 256 : 1024) void norm_bwd_kernel(const T* __r
 // vectors up to 128); wider rows take a workgroup, of up to 1,024 threads, with a second vector a thread from 513
 // on and four from 2,049. 2^26 entries, forward / backward in us: bf16 rows of 128 columns 55 / 85 on 16 lanes, 141 / 291
 // on 64; of 4,096 (512 vectors) 53 / 92 with one vector a thread, 54 / 98 with two, which halve what the reductions
-// cost but leave fewer wavefronts; of 5,120 63 / 110 with two, 72 / 119 with one; of 12,288 58 / 95 with two on 768
+// cost but leave fewer wavefronts; of 5,120 55 / 93 with two, 72 / 119 with one; of 12,288 58 / 95 with two on 768
 // threads, 95 / 120 with four on 384.
 struct Shape {
   int nv, lpr;   // vectors per thread; lanes per row, 0: the workgroup
@@ -363,18 +363,19 @@ Shape shape_of(bool bf16, int C) {
   return {nv, 0, ((v + nv - 1) / nv + 63) / 64 * 64, 1};
 }
 
-// Workgroups of the gradients: each leaves a partial vector, so as many as the registers let run at once (some 1,024
-// threads a CU) and no more: with twice as many, 2^26 bf16 entries take 114 us instead of 95 at 1,536 columns and 107 instead
-// of 91 at 2,048.
+// Workgroups: as many as are on a CU at once and no more (of 2^26 bf16 entries, 5,120 columns: forward 69 us with 4 a CU,
+// 80 with 6). For the gradients, whose every workgroup leaves a partial vector, still fewer: 113 us with 2 a CU, 131 with 3,
+// and half the sums; with one vector a thread, whose rows need the most wavefronts, 3 (2,560 columns 96, 109 with 2).
+int fwd_parts(const Shape& s, int rows) {
+  return std::min((rows + s.rows - 1) / s.rows, 256 * std::max(1, (s.nv == 1 ? 2048 : 1280) / s.threads));
+}
 int bwd_parts(const Shape& s, int rows) {
-  const int fill = 256 * std::max(1, 1024 / s.threads);
-  return std::min((rows + s.rows - 1) / s.rows, fill);
+  return std::min((rows + s.rows - 1) / s.rows, 256 * std::max(1, (s.lpr || s.nv > 1 ? 768 : 1024) / s.threads));
 }
 
 template <typename T, int NV, int LPR>
 hipError_t fwd(const NormOp& a, const Shape& sh, void* y, int64_t ldy, hipStream_t s) {
-  const int grid = std::min((a.rows + sh.rows - 1) / sh.rows, 256 * std::max(1, 2048 / sh.threads));
-  norm_kernel<T, NV, LPR><<<grid, sh.threads, 0, s>>>(static_cast<const T*>(a.x), a.ldx, a.rows, a.C, a.w, a.b, a.eps,
+  norm_kernel<T, NV, LPR><<<fwd_parts(sh, a.rows), sh.threads, 0, s>>>(static_cast<const T*>(a.x), a.ldx, a.rows, a.C, a.w, a.b, a.eps,
                                                       static_cast<T*>(y), ldy);
   return hipGetLastError();
 }
