@@ -96,8 +96,9 @@ struct DeltaIn {
 // that sums over the rows are lanes' neighbours (DPP) and a state's lines are read whole. With
 // p = S^T k and r = S^T q of the state before the token,
 //   u = beta (v - a p),  o = scale (a r + (k.q) u),  S <- a S + k u^T:
-// one reduction per token. Single tokens are bound by the states' bytes; sequences by the chain of a token's
-// products, reduction and update.
+// one reduction per token. Single tokens are bound by the states' bytes (192 x 32 heads of 128 x 128: 172 us for 805 MB,
+// the rate of a large copy); sequences by the chain of a token's products, reduction and update (1.1 us a token, 0.5 for
+// 64 x 64).
 template <int CTRL>
 __device__ __forceinline__ float dpp(float v) {
   return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xF, 0xF, false));
@@ -404,7 +405,9 @@ __device__ __forceinline__ void row_raw(const T* p, int64_t ld, Chunk c, int w, 
 // T and P (or, for the gradients, T, T^T and P^T) as fragments and beta, e^G and w of every chunk, a
 // workgroup per chunk and key head, which goes through the value heads that share it. Each of four
 // wavefronts has 16 rows. T: the diagonal blocks of 16 by substitution, a column per lane, then blocks of
-// 32 and 64 by products, T21 = -T22 A21 T11.
+// 32 and 64 by products, T21 = -T22 A21 T11. Bound by what it writes, the matrices in parts above all: 126 chunks of 32
+// heads (16 key heads) in bf16, 227 MiB, 84 us; a chain of ten barriers a head hides only under the other workgroups of
+// a CU (with room for fewer, 105).
 constexpr int kLdM = kC + 4;
 
 template <typename T, int DKP, bool GRADS>
@@ -601,21 +604,30 @@ __device__ __forceinline__ void head_and_part(int b, int heads, int parts, int& 
   }
 }
 
+// Where entry k of row r (of 16) is in an array of D to a row: the eights of a row change places with the row, so that a
+// column of eights is in different banks (rows 8 entries longer instead: conflicts in 18% of the walk's cycles, not 6%).
+template <int D>
+__device__ __forceinline__ int swap8(int r, int k) {
+  return r * D + ((((k >> 3) ^ (D == 128 ? r : r >> 1)) & (D / 8 - 1)) << 3) + (k & 7);
+}
+
 // A workgroup per sequence, value head and slice of 16 columns. The parts of the state in LDS, [column][row],
 // feed the products; the state itself stays in registers, tiles of 16 rows to a wavefront. Three barriers a chunk
 // make three phases. Four wavefronts of 16 tokens each form R (K S0), then U (T R); four more the answers of
 // the chunk before (P U), then Q S0, then the new state. So each SIMD has two to issue from, and LDS, whose 128
 // bytes a cycle every product's operands share, is asked evenly. What
 // the next chunk reads from memory is asked for as soon as its registers are free. SAVE (for the gradients): the states in
-// front of the chunks and U are kept, no answers are formed, by the first four alone.
+// front of the chunks and U are kept, no answers are formed, by the first four alone. Bound by the chain of a chunk's three
+// phases: 126 chunks of 32 heads of 128 x 128 (one workgroup a CU) in 237 us, 1.9 a chunk, the matrix cores 17% busy, LDS
+// 26%, the vector units 23%; out of registers alone, without a load, 172; with all the work on four wavefronts 336.
 template <typename T, int DKP, bool SAVE>
 __global__ __launch_bounds__(SAVE ? 256 : 512) void delta_chunk_kernel(
     DeltaIn a, const T* __restrict__ v, const float* __restrict__ mats, const float* __restrict__ coef,
     const T* __restrict__ ops, float* state_out, T* __restrict__ o, int64_t ldo,
     float* __restrict__ s0, float* __restrict__ us) {
   constexpr int NW = SAVE ? 4 : 8, NT = DKP / 64;
-  constexpr int NS = DKP / 32, LS = DKP + 8, LR = kC + 8, OP = kOutParts<T>;
-  __shared__ __attribute__((aligned(16))) uint16_t sS[3 * 16 * LS], sR[3 * 16 * LR], sW[3 * 16 * LR], sU[3 * 16 * LR];
+  constexpr int NS = DKP / 32, OP = kOutParts<T>;
+  __shared__ __attribute__((aligned(16))) uint16_t sS[3 * 16 * DKP], sR[3 * 16 * kC], sW[3 * 16 * kC], sU[3 * 16 * kC];
   // a wavefront's tokens' values and answers, on their way between rows in memory and columns in registers
   constexpr int LV = 20;
   __shared__ __attribute__((aligned(16))) T sV[NW][16 * LV];
@@ -644,7 +656,7 @@ __global__ __launch_bounds__(SAVE ? 256 : 512) void delta_chunk_kernel(
   };
   auto share = [&]() {
 #pragma unroll
-    for (int n = 0; n < NT; ++n) put_parts<3>(sS + li * LS + 16 * (NT * w + n) + 4 * lk, 16 * LS, st[n]);
+    for (int n = 0; n < NT; ++n) put_parts<3>(sS + swap8<DKP>(li, 16 * (NT * w + n) + 4 * lk), 16 * DKP, st[n]);
   };
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
@@ -727,7 +739,7 @@ __global__ __launch_bounds__(SAVE ? 256 : 512) void delta_chunk_kernel(
       acc.clear();
 #pragma unroll
       for (int s = 0; s < 2; ++s)
-        if (s <= s1) mma32<OP - 1>(pf[s], get_parts<OP>(sU + li * LR + 32 * s + 8 * lk, 16 * LR), acc);
+        if (s <= s1) mma32<OP - 1>(pf[s], get_parts<OP>(sU + swap8<kC>(li, 32 * s + 8 * lk), 16 * kC), acc);
       load_p(next);
       const floatx4 x = acc.sum();
 #pragma unroll
@@ -747,12 +759,12 @@ __global__ __launch_bounds__(SAVE ? 256 : 512) void delta_chunk_kernel(
         acc.clear();
 #pragma unroll
         for (int s = 0; s < NS; ++s)
-          mma32<2>(rf[s].parts(), get_parts<3>(sS + li * LS + 32 * s + 8 * lk, 16 * LS), acc);
+          mma32<2>(rf[s].parts(), get_parts<3>(sS + swap8<DKP>(li, 32 * s + 8 * lk), 16 * DKP), acc);
         load_rows(next);
         out = acc.sum();
 #pragma unroll
         for (int r = 0; r < 4; ++r) out[r] = beta[r] * fmaf(-e[r], out[r], to_f32(mine[(4 * lk + r) * LV + li]));
-        put_parts<3>(sR + li * LR + place, 16 * LR, out);
+        put_parts<3>(sR + swap8<kC>(li, place), 16 * kC, out);
         sync_wave();  // (the values are read)
         load_v(next);
         beta = factor(next, 0);
@@ -768,12 +780,12 @@ __global__ __launch_bounds__(SAVE ? 256 : 512) void delta_chunk_kernel(
         acc.clear();
 #pragma unroll
         for (int s = 0; s < 2; ++s)
-          if (s <= s1) mma32<2>(tf[s], get_parts<3>(sR + li * LR + 32 * s + 8 * lk, 16 * LR), acc);
+          if (s <= s1) mma32<2>(tf[s], get_parts<3>(sR + swap8<kC>(li, 32 * s + 8 * lk), 16 * kC), acc);
         load_t(next);
         const floatx4 u = acc.sum();
-        put_parts<3>(sW + li * LR + place, 16 * LR, u * wj);
+        put_parts<3>(sW + swap8<kC>(li, place), 16 * kC, u * wj);
         wj = factor(next, 2);
-        if constexpr (!SAVE) put_parts<OP>(sU + li * LR + place, 16 * LR, u);
+        if constexpr (!SAVE) put_parts<OP>(sU + swap8<kC>(li, place), 16 * kC, u);
         if (SAVE && col)
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
@@ -784,7 +796,7 @@ __global__ __launch_bounds__(SAVE ? 256 : 512) void delta_chunk_kernel(
         acc.clear();
 #pragma unroll
         for (int s = 0; s < NS; ++s)
-          mma32<OP - 1>(rf[s].parts(), get_parts<OP>(sS + li * LS + 32 * s + 8 * lk, 16 * LS), acc);
+          mma32<OP - 1>(rf[s].parts(), get_parts<OP>(sS + swap8<DKP>(li, 32 * s + 8 * lk), 16 * DKP), acc);
         load_rows(next);
         out = acc.sum();
       }
@@ -793,7 +805,7 @@ __global__ __launch_bounds__(SAVE ? 256 : 512) void delta_chunk_kernel(
         const float eC = coef[((int64_t)(key + ch) * a.H + h) * 3 * kC + 2 * kC - 1];
         Parts<3> wf[2];
 #pragma unroll
-        for (int s = 0; s < 2; ++s) wf[s] = get_parts<3>(sW + li * LR + 32 * s + 8 * lk, 16 * LR);
+        for (int s = 0; s < 2; ++s) wf[s] = get_parts<3>(sW + swap8<kC>(li, 32 * s + 8 * lk), 16 * kC);
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
           acc.clear();
@@ -831,7 +843,8 @@ __global__ __launch_bounds__(SAVE ? 256 : 512) void delta_chunk_kernel(
 // all chunks at once. (dg_t is what passes over token t; as sums of such terms alone, without differences of
 // the chunk's totals, it keeps its digits where a token forgets nearly all.)
 // Two kinds of wavefronts as in the forward walk: four of 16 tokens each form dU and dR, and put what dO gives into
-// LDS for the next chunk; four more the state's adjoint, Q^T (e dO) while dU and dR come about.
+// LDS for the next chunk; four more the state's adjoint, Q^T (e dO) while dU and dR come about. Bound as that walk is:
+// four sequences of up to 2,048 tokens, 16 heads of 128 x 128 in bf16, 125 us (the states' walk forwards 80).
 template <typename T, int DKP>
 __global__ __launch_bounds__(512) void delta_back_kernel(DeltaIn a, const T* __restrict__ d_o, int64_t lddo,
                                                          const float* __restrict__ mats, const float* __restrict__ coef,
@@ -839,9 +852,9 @@ __global__ __launch_bounds__(512) void delta_back_kernel(DeltaIn a, const T* __r
                                                          const float* __restrict__ dstate_out, float* __restrict__ dstate,
                                                          T* __restrict__ dv, int64_t lddv, float* __restrict__ ds1,
                                                          float* __restrict__ drs) {
-  constexpr int NS = DKP / 32, NT = DKP / 64, LS = DKP + 8, LR = kC + 8, KP = sizeof(T) == 2 ? 1 : 3, LV = 20;
-  __shared__ __attribute__((aligned(16))) uint16_t sS[3 * 16 * LS], sO[KP * 16 * LR], sE[3 * 16 * LR], sU[3 * 16 * LR],
-      sW[3 * 16 * LR];
+  constexpr int NS = DKP / 32, NT = DKP / 64, KP = sizeof(T) == 2 ? 1 : 3, LV = 20;
+  __shared__ __attribute__((aligned(16))) uint16_t sS[3 * 16 * DKP], sO[KP * 16 * kC], sE[3 * 16 * kC], sU[3 * 16 * kC],
+      sW[3 * 16 * kC];
   __shared__ __attribute__((aligned(16))) float sV[4][16 * LV];
   const int tid = threadIdx.x, lane = tid & 63, li = lane & 15, lk = lane >> 4;
   const int wv = __builtin_amdgcn_readfirstlane(tid >> 6), w = wv & 3;
@@ -865,7 +878,7 @@ __global__ __launch_bounds__(512) void delta_back_kernel(DeltaIn a, const T* __r
   };
   auto share = [&]() {
 #pragma unroll
-    for (int n = 0; n < NT; ++n) put_parts<3>(sS + li * LS + 16 * (NT * w + n) + 4 * lk, 16 * LS, st[n]);
+    for (int n = 0; n < NT; ++n) put_parts<3>(sS + swap8<DKP>(li, 16 * (NT * w + n) + 4 * lk), 16 * DKP, st[n]);
   };
   const int chunks = (len + kC - 1) / kC;
   auto chunk = [&](int ch) { return Chunk{base + ch * kC, min(kC, len - ch * kC)}; };
@@ -911,8 +924,8 @@ __global__ __launch_bounds__(512) void delta_back_kernel(DeltaIn a, const T* __r
       floatx4 x;
 #pragma unroll
       for (int r = 0; r < 4; ++r) x[r] = 16 * w + 4 * lk + r < c.n ? mine[(4 * lk + r) * LV + li] : 0.f;
-      put_parts<KP>(sO + li * LR + place, 16 * LR, x);
-      put_parts<3>(sE + li * LR + place, 16 * LR, x * e * a.scale);
+      put_parts<KP>(sO + swap8<kC>(li, place), 16 * kC, x);
+      put_parts<3>(sE + swap8<kC>(li, place), 16 * kC, x * e * a.scale);
       sync_wave();
     };
     if (chunks > 0) {
@@ -935,27 +948,27 @@ __global__ __launch_bounds__(512) void delta_back_kernel(DeltaIn a, const T* __r
       acc.clear();
 #pragma unroll
       for (int s = 0; s < NS; ++s)
-        mma32<2>(rf[s].parts(), get_parts<3>(sS + li * LS + 32 * s + 8 * lk, 16 * LS), acc);
+        mma32<2>(rf[s].parts(), get_parts<3>(sS + swap8<DKP>(li, 32 * s + 8 * lk), 16 * DKP), acc);
       load_o(next);
       load_rows(next);
       const floatx4 y = acc.sum();
       acc.clear();
 #pragma unroll
       for (int s = 0; s < 2; ++s)
-        if (s >= s0) mma32<2>(pf[s], get_parts<KP>(sO + li * LR + 32 * s + 8 * lk, 16 * LR), acc);
+        if (s >= s0) mma32<2>(pf[s], get_parts<KP>(sO + swap8<kC>(li, 32 * s + 8 * lk), 16 * kC), acc);
       load_mat(pf, mat(next, 2));
       floatx4 x = acc.sum() + y * wj;
-      put_parts<3>(sU + li * LR + place, 16 * LR, x);
+      put_parts<3>(sU + swap8<kC>(li, place), 16 * kC, x);
       wj = factor(next, 2);
       sync_lds();
       // ---- dR
       acc.clear();
 #pragma unroll
       for (int s = 0; s < 2; ++s)
-        if (s >= s0) mma32<2>(tf[s], get_parts<3>(sU + li * LR + 32 * s + 8 * lk, 16 * LR), acc);
+        if (s >= s0) mma32<2>(tf[s], get_parts<3>(sU + swap8<kC>(li, 32 * s + 8 * lk), 16 * kC), acc);
       load_mat(tf, mat(next, 1));
       const floatx4 dr = acc.sum();
-      put_parts<3>(sW + li * LR + place, 16 * LR, -(dr * beta * e));
+      put_parts<3>(sW + swap8<kC>(li, place), 16 * kC, -(dr * beta * e));
       sync_lds();
       // ---- what leaves, and the next chunk's dO
 #pragma unroll
@@ -1003,7 +1016,7 @@ __global__ __launch_bounds__(512) void delta_back_kernel(DeltaIn a, const T* __r
     {
       Parts<3> ef[2];
 #pragma unroll
-      for (int s = 0; s < 2; ++s) ef[s] = get_parts<3>(sE + li * LR + 32 * s + 8 * lk, 16 * LR);
+      for (int s = 0; s < 2; ++s) ef[s] = get_parts<3>(sE + swap8<kC>(li, 32 * s + 8 * lk), 16 * kC);
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
         acc[n].clear();
@@ -1016,7 +1029,7 @@ __global__ __launch_bounds__(512) void delta_back_kernel(DeltaIn a, const T* __r
     sync_lds();
     Parts<3> wf[2];
 #pragma unroll
-    for (int s = 0; s < 2; ++s) wf[s] = get_parts<3>(sW + li * LR + 32 * s + 8 * lk, 16 * LR);
+    for (int s = 0; s < 2; ++s) wf[s] = get_parts<3>(sW + swap8<kC>(li, 32 * s + 8 * lk), 16 * kC);
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
 #pragma unroll
@@ -1049,7 +1062,10 @@ __device__ __forceinline__ float sum4(float x) {
 // What the chunks give once their states and adjoints are known, a workgroup per chunk and key head, which
 // sums dQ and dK over the value heads that share it. Two sets of four wavefronts have 16 tokens each and
 // half of the rows of dQ^T and dK^T each; the first also forms dP and M1, the second dA and M2. The states, their
-// adjoints and U go through LDS in parts, 32 columns at a time; then M1 and M2 do, both ways round.
+// adjoints and U go through LDS in parts, 32 columns at a time; then M1 and M2 do, both ways round. 110 KB of LDS (146 in
+// fp32) and 256 registers leave one workgroup to a CU, whose phases (a slice into LDS, its products, the matrices,
+// their sums) follow each other: 87 chunks of 16 heads of 128 x 128 in bf16 186 us, matrix cores 13% busy, in 2.7
+// rounds of the CUs.
 constexpr int kSl = 32, kLdSl = kSl + 8, kLdZ = kC + 8, kLdF = kC + 1;
 
 template <typename T, int DKP>

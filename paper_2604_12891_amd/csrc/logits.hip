@@ -459,7 +459,9 @@ __global__ __launch_bounds__(kTB) void logprobs_join_kernel(LogitRows a, int K, 
 // apart. Equal scores: the lower row, then the lower token, which is the lower list, as splits are in their
 // rows' order. All scores are formed at once, as numbers that rise with them (0: none); then a wavefront runs the
 // rounds, each the largest of its lanes' heads (the high halves as a rule tell) and one lane's step on, out of LDS
-// where the lists fit: some 0.3 us.
+// where the lists fit: some 0.3 us. A chain of latencies: 5.8 us for 4 beams and K = 4, 9.8 for 64 groups of 8 and K = 16
+// (the rows' lists, 512 rows of 131,072 bf16 entries, 37 at the rate of 3.6 TB/s); counting how many candidates beat each
+// instead of rounds took 12 to 26.
 constexpr int kBeamLists = 1024;  // W x splits
 constexpr int kBeamKeys = 4096;   // candidates held in LDS
 
