@@ -413,7 +413,7 @@ constexpr int kLdM = kC + 4;
 template <typename T, int DKP, bool GRADS>
 __global__ __launch_bounds__(256, (sizeof(T) == 4 && DKP == 128 ? 2 : 4)) void delta_prep_kernel(DeltaIn a, const T* __restrict__ q, const T* __restrict__ k,
                                                          float* __restrict__ mats, float* __restrict__ coef,
-                                                         T* __restrict__ ops) {
+                                                         T* __restrict__ ops, float* __restrict__ prods) {
   __shared__ __attribute__((aligned(16))) float sA[kC * kLdM], sT[kC * kLdM], sX[32 * 36];
   __shared__ double sG[kC];
   __shared__ float sB[kC];
@@ -424,7 +424,7 @@ __global__ __launch_bounds__(256, (sizeof(T) == 4 && DKP == 128 ? 2 : 4)) void d
   const Chunk c = {tl.base + tl.j * kC, min(kC, tl.len - tl.j * kC)};
   constexpr int NS = DKP / 32;
   const T* kp = k + (int64_t)hk * a.Dk;
-  // products of rows: lane's entries [16 w + 4 lk + r][16 t + li]
+  // products of rows: lane's entries, of row 16 w + li with key 16 t + 4 lk + r
   floatx4 kk[4], qk[4];
   Raw8<T> kf[NS], qf[NS];
   row_raw<T, NS>(kp, a.ldk, c, w, a.Dk, kf);
@@ -442,14 +442,23 @@ __global__ __launch_bounds__(256, (sizeof(T) == 4 && DKP == 128 ? 2 : 4)) void d
 #pragma unroll
       for (int s = 0; s < NS; ++s) {
         const auto b = bf[s].parts();
-        mma32<2>(kf[s].parts(), b, x);
-        mma32<2>(qf[s].parts(), b, y);
+        mma32<2>(b, kf[s].parts(), x);
+        mma32<2>(b, qf[s].parts(), y);
       }
       kk[t] = x.sum();
       qk[t] = y.sum();
     }
   }
   const int lane = threadIdx.x & 63, li = lane & 15, lk = lane >> 4;
+  if constexpr (GRADS) {  // they are wanted again: forming them anew takes 22 us, writing them 2
+    floatx4* out = reinterpret_cast<floatx4*>(prods) + ((int64_t)tile * a.Hk + hk) * (2 * kMat / 4);
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+      if (t <= w) {
+        out[(w * 4 + t) * 64 + lane] = qk[t];
+        out[kMat / 4 + (w * 4 + t) * 64 + lane] = kk[t];
+      }
+  }
   // K, Q (for the gradients Q^T) and K^T as operands: a chunk's rows are a model's width apart, and every slice of every head that
   // reads them so would ask one channel of the cache for all of them
   {
@@ -506,15 +515,23 @@ __global__ __launch_bounds__(256, (sizeof(T) == 4 && DKP == 128 ? 2 : 4)) void d
     for (int i = tid; i < kC * kLdM; i += 256) sT[i] = 0.f;
     __syncthreads();
     floatx4 pm[4];
+    {
+      const int i = 16 * w + li;
+      const double Gi = sG[i];
+      const float bi = sB[i];
 #pragma unroll
-    for (int t = 0; t < 4; ++t)
+      for (int t = 0; t < 4; ++t) {
+        floatx4 am;
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int i = 16 * w + 4 * lk + r, j = 16 * t + li;
-        const float d = j <= i ? exp_of(sG[i] - sG[j]) : 0.f;
-        sA[i * kLdM + j] = j < i ? sB[i] * d * kk[t][r] : 0.f;
-        pm[t][r] = j <= i ? a.scale * d * qk[t][r] : 0.f;
+        for (int r = 0; r < 4; ++r) {
+          const int j = 16 * t + 4 * lk + r;
+          const float d = j <= i ? exp_of(Gi - sG[j]) : 0.f;
+          am[r] = j < i ? bi * d * kk[t][r] : 0.f;
+          pm[t][r] = j <= i ? a.scale * d * qk[t][r] : 0.f;
+        }
+        *reinterpret_cast<floatx4*>(sA + i * kLdM + 16 * t + 4 * lk) = am;
       }
+    }
     __syncthreads();
     {  // diagonal block w, column li (four lanes do the same)
       const float* A = sA + 16 * w * kLdM + 16 * w;
@@ -566,9 +583,7 @@ __global__ __launch_bounds__(256, (sizeof(T) == 4 && DKP == 128 ? 2 : 4)) void d
     }
     __syncthreads();  // P to where A was
 #pragma unroll
-    for (int t = 0; t < 4; ++t)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) sA[(16 * w + 4 * lk + r) * kLdM + 16 * t + li] = pm[t][r];
+    for (int t = 0; t < 4; ++t) *reinterpret_cast<floatx4*>(sA + (16 * w + li) * kLdM + 16 * t + 4 * lk) = pm[t];
     __syncthreads();
     uint16_t* tp = reinterpret_cast<uint16_t*>(out);
     if constexpr (GRADS) {
@@ -1064,21 +1079,22 @@ __device__ __forceinline__ float sum4(float x) {
 // half of the rows of dQ^T and dK^T each; the first also forms dP and M1, the second dA and M2. The states, their
 // adjoints and U go through LDS in parts, 32 columns at a time; then M1 and M2 do, both ways round. 110 KB of LDS (146 in
 // fp32) and 256 registers leave one workgroup to a CU, whose phases (a slice into LDS, its products, the matrices,
-// their sums) follow each other: 87 chunks of 16 heads of 128 x 128 in bf16 186 us, matrix cores 13% busy, in 2.7
-// rounds of the CUs.
+// their sums) follow each other: 87 chunks of 16 heads of 128 x 128 in bf16 168 us in 2.7 rounds of the CUs (190 with
+// the products of keys formed here again).
 constexpr int kSl = 32, kLdSl = kSl + 8, kLdZ = kC + 8, kLdF = kC + 1;
 
 template <typename T, int DKP>
 __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaIn a, const T* __restrict__ q, const T* __restrict__ k,
                                                           const T* __restrict__ v, const T* __restrict__ d_o,
                                                           int64_t lddo, const float* __restrict__ coef,
-                                                          const T* __restrict__ ops, const float* __restrict__ s0,
+                                                          const T* __restrict__ ops, const float* __restrict__ prods,
+                                                          const float* __restrict__ s0,
                                                           const float* __restrict__ ds1, const float* __restrict__ us,
                                                           const float* __restrict__ drs, T* __restrict__ dq,
                                                           int64_t lddq, T* __restrict__ dk, int64_t lddk,
                                                           float* __restrict__ dg, int64_t lddg,
                                                           float* __restrict__ dbeta, int64_t lddb) {
-  constexpr int NS = DKP / 32, NT = DKP / 32, OP = kOutParts<T>;  // NT: tiles of 16 rows to a wavefront
+  constexpr int NT = DKP / 32, OP = kOutParts<T>;  // NT: tiles of 16 rows to a wavefront
   constexpr int kState = DKP * kLdSl, kU = kC * kLdSl, kZ = kC * kLdZ;  // bf16 entries of one part
   constexpr int KP = sizeof(T) == 2 ? 1 : 3;  // parts of an activation
   constexpr int kSlices = 6 * kState + (6 + KP) * kU, kProducts = 4 * OP * kZ + 2 * 2 * kC * kLdF;
@@ -1198,6 +1214,13 @@ __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaIn a, const T* __
         keep_order();
       }
     }
+    // products of keys j with the set's rows (queries or keys) i: [16 b + 4 lk + r][t], as the preparation left them
+    floatx4 zz[4];
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+      zz[b] = zero;
+      if (b <= w) zz[b] = at_lane<floatx4>(prods + (((int64_t)tile * a.Hk + hk) * 2 + set) * kMat + (w * 4 + b) * 256, lane);
+    }
     rv = sum8(rv);
     if ((tid & 7) == 0) sSum[1][ut] = rv;
     const float beta = co[t], e = co[kC + t], wj = co[2 * kC + t], eC = co[2 * kC - 1];
@@ -1228,24 +1251,6 @@ __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaIn a, const T* __
     }
     if (lane == 0) sDot[wv] = dot;
     sync_lds();  // the slices are read
-    // products of keys j with the set's rows (queries or keys) i: [16 b + 4 lk + r][t]; formed here for every head,
-    // as through the slices there are no registers for them
-    floatx4 zz[4];
-    {
-      Raw8<T> rf[NS];
-      row_raw<T, NS>(set ? kp : qp, set ? a.ldk : a.ldq, c, w, a.Dk, rf);
-#pragma unroll
-      for (int b = 0; b < 4; ++b) {
-        zz[b] = zero;
-        if (b > w) continue;
-        Raw8<T> kf[NS];
-#pragma unroll
-        for (int s = 0; s < NS; ++s) kf[s].load_lane(op + (b * NS + s) * 512, lane);
-#pragma unroll
-        for (int s = 0; s < NS; ++s) mma32<2>(kf[s].parts(), rf[s].parts(), zz[b]);
-        keep_order();
-      }
-    }
     // the set's matrix, M1 or M2 (below the diagonal), as rows and as columns over tokens in place
     uint16_t* sZ = pool + set * 2 * OP * kZ;
     uint16_t* sZT = sZ + OP * kZ;
@@ -1306,7 +1311,7 @@ __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaIn a, const T* __
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
           kt[n].load_lane(op + 2 * DKP * kC + (2 * (set * NT + n) + s) * 512, lane);
-          if (hi) qt[n].load_lane(op + DKP * kC + (2 * (set * NT + n) + s) * 512, lane);
+          qt[n].load_lane(op + DKP * kC + (2 * (set * NT + n) + s) * 512, lane);  // (always: a branch spilled 58 registers)
         }
         keep_order();
 #pragma unroll
@@ -1415,7 +1420,8 @@ hipError_t chunks(const DeltaOp& a, float* state_out, void* o, int64_t ldo, floa
   float* mats = ws + tiles * a.H * 3 * kC;
   const T *q = static_cast<const T*>(a.q), *k = static_cast<const T*>(a.k), *v = static_cast<const T*>(a.v);
   T* ops = reinterpret_cast<T*>(mats + tiles * a.H * kMats<T, false>);
-  delta_prep_kernel<T, DKP, false><<<dim3((unsigned)(tiles * a.Hk)), 256, 0, s>>>(in_of(a), q, k, mats, coef, ops);
+  delta_prep_kernel<T, DKP, false><<<dim3((unsigned)(tiles * a.Hk)), 256, 0, s>>>(in_of(a), q, k, mats, coef, ops,
+                                                                                     nullptr);
   delta_chunk_kernel<T, DKP, false><<<dim3((unsigned)((int64_t)a.n_seq * a.H * ((a.Dv + 15) / 16))), 512, 0, s>>>(
       in_of(a), v, mats, coef, ops, state_out, static_cast<T*>(o), ldo, nullptr, nullptr);
   return hipGetLastError();
@@ -1428,12 +1434,13 @@ int64_t op_floats(bool bf16, int n_seq, int rows, int Hk, int Dk) {
 
 // The parts of the gradients' workspace, in floats.
 struct BackSpace {
-  int64_t coef, mats, s0, ds1, us, drs, ops, end;
+  int64_t coef, mats, prods, s0, ds1, us, drs, ops, end;
   BackSpace(bool bf16, int n_seq, int rows, int Hk, int H, int Dk, int Dv) {
     const int64_t th = tiles_of(n_seq, rows) * H, head = (int64_t)Dk * Dv, act = th * kC * Dv;
     coef = 0;
     mats = coef + th * 3 * kC;
-    s0 = mats + th * kMats<float, true>;
+    prods = mats + th * kMats<float, true>;
+    s0 = prods + tiles_of(n_seq, rows) * Hk * 2 * kMat;
     ds1 = s0 + th * head;
     us = ds1 + th * head;
     drs = us + act;
@@ -1452,12 +1459,12 @@ hipError_t grads(const DeltaOp& a, const void* d_o_, int64_t lddo, const float* 
   const T* d_o = static_cast<const T*>(d_o_);
   const DeltaIn in = in_of(a);
   const dim3 flat((unsigned)(tiles * a.Hk)), slices((unsigned)((int64_t)a.n_seq * a.H * ((a.Dv + 15) / 16)));
-  delta_prep_kernel<T, DKP, true><<<flat, 256, 0, s>>>(in, q, k, ws + b.mats, ws + b.coef, ops);
+  delta_prep_kernel<T, DKP, true><<<flat, 256, 0, s>>>(in, q, k, ws + b.mats, ws + b.coef, ops, ws + b.prods);
   delta_chunk_kernel<T, DKP, true><<<slices, 256, 0, s>>>(in, v, ws + b.mats, ws + b.coef, ops, nullptr, nullptr, 0,
                                                           ws + b.s0, ws + b.us);
   delta_back_kernel<T, DKP><<<slices, 512, 0, s>>>(in, d_o, lddo, ws + b.mats, ws + b.coef, ops, dstate_out, g.dstate,
                                                    static_cast<T*>(g.dv), g.lddv, ws + b.ds1, ws + b.drs);
-  delta_grads_kernel<T, DKP><<<flat, 512, 0, s>>>(in, q, k, v, d_o, lddo, ws + b.coef, ops, ws + b.s0, ws + b.ds1,
+  delta_grads_kernel<T, DKP><<<flat, 512, 0, s>>>(in, q, k, v, d_o, lddo, ws + b.coef, ops, ws + b.prods, ws + b.s0, ws + b.ds1,
                                                   ws + b.us, ws + b.drs, static_cast<T*>(g.dq), g.lddq, static_cast<T*>(g.dk),
                                                   g.lddk, g.dg, g.lddg, g.dbeta, g.lddb);
   return hipGetLastError();
