@@ -744,12 +744,12 @@ TCL_API tcl_status tcl_distill_topk(int32_t dtype, int32_t n_rows, int32_t V, co
  * The selection: candidate (b, v) is beam b followed by token v, with the score
  *   d_score[g, b] + log p_b(v),   p = softmax(logits / temperature),
  * d_score [n_groups, W] fp32 the beams' own. A group's K best go to d_parent (the row g W + b), d_token
- * (v) and d_out_score, all [n_groups, K]: highest first, equal scores by lower row, then by lower token
- * (compared in 64 bits, rounded to fp32 at the end). d_ended [n_groups, W] int32 or NULL: a beam with an entry
- * >= 0 has ended, and is one candidate itself, with that entry as its token and its own score. A beam
- * whose score is -inf or NaN is dead. Neither's logits are read. Masked (-inf) and NaN logits, and rows with a logit of
- * +inf, are no candidates; past the end of a group with fewer than K: -1, -1 and -inf. logits
- * as for tcl_logprobs (rows); W and K in [1, 64], n_groups W < 2^22. d_workspace: >=
+ * (v) and d_out_score, all [n_groups, K]: highest first (compared in 64 bits, rounded to fp32 at the end), equal
+ * scores by lower row; a row's own candidates in tcl_topk's order, by their logits, then by lower token. d_ended
+ * [n_groups, W] int32 or NULL: a beam with an entry >= 0 has ended, and is one candidate itself, with that entry
+ * as its token and its own score. A beam whose score is -inf or NaN is dead. Neither's logits are read. Masked
+ * (-inf) and NaN logits, and rows with a logit of +inf, are no candidates; past the end of a group with fewer than
+ * K: -1, -1 and -inf. logits as for tcl_logprobs (rows); W and K in [1, 64], n_groups W < 2^22. d_workspace: >=
  * tcl_beam_select_workspace_bytes bytes, 256-byte aligned. n_groups == 0 is TCL_OK. */
 TCL_API size_t tcl_beam_select_workspace_bytes(int32_t n_groups, int32_t W, int32_t V, int32_t K);
 TCL_API tcl_status tcl_beam_select(int32_t dtype, int32_t n_groups, int32_t W, int32_t V, const void* d_logits,

@@ -6,7 +6,7 @@ import numpy as np
 
 def beam_select(logits, score, K, ended=None, temperature=1.0):
     """logits [G W, V], score [G, W]: the K best (beam, token) of each group by score + log p, highest
-    first, equal ones by lower beam and token. -> dict(parent, token, score) [G, K]"""
+    first, equal ones by lower beam, a beam's own by logit, then by lower token. -> dict(parent, token, score) [G, K]"""
     logits, score = np.asarray(logits, np.float64), np.asarray(score, np.float64)
     G, W = score.shape
     parent, token = np.full((G, K), -1, np.int64), np.full((G, K), -1, np.int64)
@@ -18,7 +18,7 @@ def beam_select(logits, score, K, ended=None, temperature=1.0):
             if not s > -np.inf:
                 continue
             if ended is not None and ended[g, w] >= 0:
-                cand.append((-s, w, int(ended[g, w])))
+                cand.append((-s, w, 0, int(ended[g, w])))
                 continue
             x = logits[g * W + w]
             x = np.where(np.isnan(x), -np.inf, x)
@@ -27,9 +27,9 @@ def beam_select(logits, score, K, ended=None, temperature=1.0):
                 continue
             z = (x - m) / temperature
             lp = z - np.log(np.exp(z).sum())
-            best = np.lexsort((np.arange(lp.size), -lp))[:K]
-            cand += [(-(s + lp[v]), w, int(v)) for v in best if lp[v] > -np.inf]
-        for i, (s, w, v) in enumerate(sorted(cand)[:K]):
+            best = np.lexsort((np.arange(lp.size), -x))[:K]
+            cand += [(-(s + lp[v]), w, i, int(v)) for i, v in enumerate(best) if lp[v] > -np.inf]
+        for i, (s, w, _, v) in enumerate(sorted(cand)[:K]):
             parent[g, i], token[g, i], out[g, i] = g * W + w, v, -s
     return dict(parent=parent, token=token, score=out)
 

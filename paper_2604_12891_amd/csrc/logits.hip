@@ -456,8 +456,8 @@ __global__ __launch_bounds__(kTB) void logprobs_join_kernel(LogitRows a, int K, 
 // A group's K best candidates (b, v) by score_b + log p_b(v), out of its rows' lists of K: each list is
 // sorted, so every round takes the best of the lists' heads. Scores are compared in 64 bits: fp32 would make
 // neighbours equal that a long search's sum of log probabilities (-100: steps of 8e-6) cannot tell
-// apart. Equal scores: the lower row, then the lower token, which is the lower list, as splits are in their
-// rows' order. All scores are formed at once, as numbers that rise with them (0: none); then a wavefront runs the
+// apart. Equal scores (a temperature or a score beyond which the logits' differences count nothing): the lower row, and
+// in a row the order that its list has, by the logits. All scores are formed at once, as numbers that rise with them (0: none); then a wavefront runs the
 // rounds, each the largest of its lanes' heads (the high halves as a rule tell) and one lane's step on, out of LDS
 // where the lists fit: some 0.3 us. A chain of latencies: 5.8 us for 4 beams and K = 4, 9.8 for 64 groups of 8 and K = 16
 // (the rows' lists, 512 rows of 131,072 bf16 entries, 37 at the rate of 3.6 TB/s); counting how many candidates beat each
@@ -566,7 +566,16 @@ __global__ __launch_bounds__(kTB) void beam_join_kernel(LogitRows a, int W, int 
     if (best & (best - 1)) {  // more than one: by the low halves, then by the list
       const bool in = best >> lane & 1;
       best &= __ballot(lo == wave_max(in ? lo : 0u));
-      if (best & (best - 1)) best &= __ballot(~mine == (int)wave_max(best >> lane & 1 ? (uint32_t)~mine : 0u));
+      if (best & (best - 1)) {  // equal scores: the lowest row, then of its parts the highest logit and lowest token
+        const uint32_t row = (uint32_t)~(mine / splits);
+        best &= __ballot(row == wave_max(best >> lane & 1 ? row : 0u));
+        if (best & (best - 1)) {
+          const u64 k = best >> lane & 1 && key ? key_of(mine, at[mine]) : 0;
+          const uint32_t khi = (uint32_t)(k >> 32), klo = (uint32_t)k;
+          best &= __ballot(khi == wave_max(khi));
+          best &= __ballot(klo == wave_max(best >> lane & 1 ? klo : 0u));
+        }
+      }
     }
     if (lane == __ffsll(best) - 1 && key) {
       const int p = at[mine];

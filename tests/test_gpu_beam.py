@@ -30,7 +30,8 @@ def _same(r, ref):
 
 # rows whole, in wavefronts and in parts; lists in LDS and not; fewer candidates than places
 SIZES = [(1, 1, 1, 1), (1, 4, 50001, 4), (3, 5, 7, 64), (2, 64, 40, 64), (70, 4, 1000, 8), (1, 64, 70001, 64),
-         (9, 8, 20000, 16), (300, 3, 90, 3), (2, 1, 131072, 2), (33, 16, 5000, 33), (1, 16, 40000, 64)]
+         (9, 8, 20000, 16), (300, 3, 90, 3), (2, 1, 131072, 2), (33, 16, 5000, 33), (1, 16, 40000, 64),
+         (700, 3, 90, 3), (520, 4, 2500, 32)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
@@ -71,6 +72,23 @@ def test_ties():
         x[0, 3], x[1, 2] = 1e-4, 2e-4
         r = _tb().beam_select(x, torch.full((1, 2), -20000.0, device="cuda"), 2)
         assert r["parent"].tolist() == [[1, 0]] and r["token"].tolist() == [[2, 3]]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V,score,T,scale", [(60000, -1.0, 1e30, 1.0), (60000, -1e30, 1.0, 1.0), (60000, -1.0, 1.0, 1e-30),
+                                             (90, -1.0, 1e30, 1.0), (90, 1e30, 1.0, 1.0)])
+def test_scores_that_no_logit_moves(V, score, T, scale, dtype):
+    """All candidates' scores are equal in 64 bits: the first row's, in the order of its logits, however the
+    row is read."""
+    rng = np.random.default_rng(V)
+    x = torch.from_numpy(scale * rng.standard_normal((8, V))).to(DT[dtype])
+    x[0, 5:] = torch.where(torch.from_numpy(rng.random(V - 5) < (0.9 if V < 100 else 0.0)), torch.tensor(-INF), x[0, 5:].float()).to(DT[dtype])
+    s = np.full((2, 4), score, np.float32)
+    s[1, 0] = -INF
+    ended = np.full((2, 4), -1, np.int32)
+    ended[1, 1] = 7
+    r = _tb().beam_select(x.cuda(), torch.from_numpy(s).cuda(), 20, torch.from_numpy(ended).cuda(), temperature=T)
+    _same(r, osr.beam_select(x.double().numpy(), s, 20, ended, T))
 
 
 def test_masks_and_infinities():
