@@ -403,7 +403,8 @@ __device__ __forceinline__ void row_raw(const T* p, int64_t ld, Chunk c, int w, 
 
 // ---------------------------------------------------------------- what needs no state
 // T and P (or, for the gradients, T, T^T and P^T) as fragments and beta, e^G and w of every chunk, a
-// workgroup per chunk and key head, which goes through the value heads that share it. Each of four
+// workgroup per chunk and key head, which goes through the value heads that share it (or, where chunks are few, `parts`
+// workgroups that share them out). Each of four
 // wavefronts has 16 rows. T: the diagonal blocks of 16 by substitution, a column per lane, then blocks of
 // 32 and 64 by products, T21 = -T22 A21 T11. Bound by what it writes, the matrices in parts above all: 126 chunks of 32
 // heads (16 key heads) in bf16, 227 MiB, 84 us; a chain of ten barriers a head hides only under the other workgroups of
@@ -413,12 +414,12 @@ constexpr int kLdM = kC + 4;
 template <typename T, int DKP, bool GRADS>
 __global__ __launch_bounds__(256, (sizeof(T) == 4 && DKP == 128 ? 2 : 4)) void delta_prep_kernel(DeltaIn a, const T* __restrict__ q, const T* __restrict__ k,
                                                          float* __restrict__ mats, float* __restrict__ coef,
-                                                         T* __restrict__ ops, float* __restrict__ prods) {
+                                                         T* __restrict__ ops, float* __restrict__ prods, int parts) {
   __shared__ __attribute__((aligned(16))) float sA[kC * kLdM], sT[kC * kLdM], sX[32 * 36];
   __shared__ double sG[kC];
   __shared__ float sB[kC];
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int tile = blockIdx.x / a.Hk, hk = blockIdx.x % a.Hk;
+  const int part = blockIdx.x % parts, tile = blockIdx.x / parts / a.Hk, hk = blockIdx.x / parts % a.Hk;
   const Tile tl = find_tile(a.offs, a.n_seq, a.rows, kC, tile);
   if (tl.seq < 0 || tl.len == 0) return;
   const Chunk c = {tl.base + tl.j * kC, min(kC, tl.len - tl.j * kC)};
@@ -450,7 +451,7 @@ __global__ __launch_bounds__(256, (sizeof(T) == 4 && DKP == 128 ? 2 : 4)) void d
     }
   }
   const int lane = threadIdx.x & 63, li = lane & 15, lk = lane >> 4;
-  if constexpr (GRADS) {  // they are wanted again: forming them anew takes 22 us, writing them 2
+  if (GRADS && part == 0) {  // they are wanted again: forming them anew takes 22 us, writing them 2
     floatx4* out = reinterpret_cast<floatx4*>(prods) + ((int64_t)tile * a.Hk + hk) * (2 * kMat / 4);
 #pragma unroll
     for (int t = 0; t < 4; ++t)
@@ -461,7 +462,7 @@ __global__ __launch_bounds__(256, (sizeof(T) == 4 && DKP == 128 ? 2 : 4)) void d
   }
   // K, Q (for the gradients Q^T) and K^T as operands: a chunk's rows are a model's width apart, and every slice of every head that
   // reads them so would ask one channel of the cache for all of them
-  {
+  if (part == 0) {
     T* out = ops + ((int64_t)tile * a.Hk + hk) * 3 * DKP * kC;
 #pragma unroll
     for (int s = 0; s < NS; ++s) {
@@ -487,7 +488,7 @@ __global__ __launch_bounds__(256, (sizeof(T) == 4 && DKP == 128 ? 2 : 4)) void d
     if constexpr (GRADS) across(q + (int64_t)hk * a.Dk, a.ldq, out + DKP * kC);
   }
   const int share = a.H / a.Hk;
-  for (int hv = 0; hv < share; ++hv) {
+  for (int hv = part; hv < share; hv += parts) {
     const int h = hk * share + hv;
     float* out = mats + ((int64_t)tile * a.H + h) * kMats<T, GRADS>;
     float* co = coef + ((int64_t)tile * a.H + h) * 3 * kC;
@@ -1397,6 +1398,7 @@ bool chunked(bool bf16, int n_seq, int rows, int H) {
   const int64_t from = bf16 ? heads > 128 ? 40 : 24 : std::clamp<int64_t>(heads / 4, 32, 256);
   return rows >= from * n_seq;
 }
+constexpr int kPrepFill = 256;  // CUs
 int64_t tiles_of(int n_seq, int rows) { return (int64_t)rows / kC + n_seq; }
 
 DeltaIn in_of(const DeltaOp& a) {
@@ -1413,6 +1415,12 @@ hipError_t walk(const DeltaOp& a, float* state_out, void* o, int64_t ldo, hipStr
   return hipGetLastError();
 }
 
+// Workgroups of the preparation for a chunk and key head: one for each value head where one for all leaves CUs idle (a
+// prompt of 1,000 bf16 tokens, one key head, 2 value heads 46 -> 40 us a call, 16 of them 124 -> 42); they form the keys'
+// products each for itself, so from more chunks on one (1,500 tokens of 4 sequences, 4 key heads, 12 value heads, fp32 169,
+// else 180).
+int prep_parts(const DeltaOp& a, int64_t tiles) { return tiles * a.Hk < kPrepFill ? a.H / a.Hk : 1; }
+
 template <typename T, int DKP>
 hipError_t chunks(const DeltaOp& a, float* state_out, void* o, int64_t ldo, float* ws, hipStream_t s) {
   const int64_t tiles = tiles_of(a.n_seq, a.rows);
@@ -1420,8 +1428,9 @@ hipError_t chunks(const DeltaOp& a, float* state_out, void* o, int64_t ldo, floa
   float* mats = ws + tiles * a.H * 3 * kC;
   const T *q = static_cast<const T*>(a.q), *k = static_cast<const T*>(a.k), *v = static_cast<const T*>(a.v);
   T* ops = reinterpret_cast<T*>(mats + tiles * a.H * kMats<T, false>);
-  delta_prep_kernel<T, DKP, false><<<dim3((unsigned)(tiles * a.Hk)), 256, 0, s>>>(in_of(a), q, k, mats, coef, ops,
-                                                                                     nullptr);
+  const int parts = prep_parts(a, tiles);
+  delta_prep_kernel<T, DKP, false><<<dim3((unsigned)(tiles * a.Hk * parts)), 256, 0, s>>>(in_of(a), q, k, mats, coef, ops,
+                                                                                          nullptr, parts);
   delta_chunk_kernel<T, DKP, false><<<dim3((unsigned)((int64_t)a.n_seq * a.H * ((a.Dv + 15) / 16))), 512, 0, s>>>(
       in_of(a), v, mats, coef, ops, state_out, static_cast<T*>(o), ldo, nullptr, nullptr);
   return hipGetLastError();
@@ -1459,7 +1468,9 @@ hipError_t grads(const DeltaOp& a, const void* d_o_, int64_t lddo, const float* 
   const T* d_o = static_cast<const T*>(d_o_);
   const DeltaIn in = in_of(a);
   const dim3 flat((unsigned)(tiles * a.Hk)), slices((unsigned)((int64_t)a.n_seq * a.H * ((a.Dv + 15) / 16)));
-  delta_prep_kernel<T, DKP, true><<<flat, 256, 0, s>>>(in, q, k, ws + b.mats, ws + b.coef, ops, ws + b.prods);
+  const int parts = prep_parts(a, tiles);
+  delta_prep_kernel<T, DKP, true><<<dim3(flat.x * parts), 256, 0, s>>>(in, q, k, ws + b.mats, ws + b.coef, ops,
+                                                                       ws + b.prods, parts);
   delta_chunk_kernel<T, DKP, true><<<slices, 256, 0, s>>>(in, v, ws + b.mats, ws + b.coef, ops, nullptr, nullptr, 0,
                                                           ws + b.s0, ws + b.us);
   delta_back_kernel<T, DKP><<<slices, 512, 0, s>>>(in, d_o, lddo, ws + b.mats, ws + b.coef, ops, dstate_out, g.dstate,

@@ -81,7 +81,7 @@ def _gpu(a, dtype, loose, spare=2, drop=("offs", "state")):
 # lengths: empty sequences, one token, chunks that end before, at and after their last token
 CASES = [([1, 0, 25, 7, 2], 1, 2, 64, 64), ([64], 1, 1, 64, 64), ([65, 63, 0, 128], 2, 4, 128, 128),
          ([200, 129, 1], 2, 2, 72, 40), ([33, 90], 1, 3, 8, 8), ([150], 1, 1, 128, 256), ([70, 40], 3, 3, 24, 136),
-         ([1] * 40, 2, 2, 16, 32), ([0, 0], 1, 1, 8, 16), ([2, 400], 1, 1, 120, 72)]
+         ([1] * 40, 2, 2, 16, 32), ([60] * 70, 2, 4, 16, 24), ([0, 0], 1, 1, 8, 16), ([2, 400], 1, 1, 120, 72)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
