@@ -2,8 +2,8 @@
 //   m = mean x, r = (mean (x - m)^2 + eps)^-1/2, h = (x - m) r, y = h w + b,
 //   dx = r (g - mean g - h mean(g h)), g = dy w,  dw = sum over rows dy h,  db = sum over rows dy.
 // Nothing is kept from the forward call: the gradients read x anyway, and a row's statistics
-// are two reductions of what is then in registers. Both passes are bound by HBM, 2 and 3 arrays: 8,192 x 5,120 bf16 in
-// 39 and 65 us at the rate that a large copy reaches (4.8 TB/s).
+// are two reductions of what is then in registers. Both passes are bound by HBM, 2 and 3 arrays: 16,384 x 5,120 bf16 in
+// 69 and 113 us, where a large copy's rate (4.8 TB/s) would take 70 and 106.
 #include <algorithm>
 
 #include "common.h"
@@ -363,9 +363,9 @@ Shape shape_of(bool bf16, int C) {
   return {nv, 0, ((v + nv - 1) / nv + 63) / 64 * 64, 1};
 }
 
-// Workgroups: as many as are on a CU at once and no more (of 2^26 bf16 entries, 5,120 columns: forward 69 us with 4 a CU,
-// 80 with 6). For the gradients, whose every workgroup leaves a partial vector, still fewer: 113 us with 2 a CU, 131 with 3,
-// and half the sums; with one vector a thread, whose rows need the most wavefronts, 3 (2,560 columns 96, 109 with 2).
+// Workgroups: as many as are on a CU at once and no more (16,384 x 5,120 bf16: forward 69 us with 4 a CU, 80 with 6). For
+// the gradients, whose every workgroup leaves a partial vector, still fewer: 113 us with 2 a CU, 131 with 3, and half the
+// sums; with one vector a thread, whose rows need the most wavefronts, 3 (26,214 x 2,560 96, with 2 109).
 int fwd_parts(const Shape& s, int rows) {
   return std::min((rows + s.rows - 1) / s.rows, 256 * std::max(1, (s.nv == 1 ? 2048 : 1280) / s.threads));
 }
