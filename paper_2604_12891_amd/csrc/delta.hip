@@ -27,13 +27,10 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kC = 64;        // tokens of a chunk
 constexpr int kMat = kC * kC;        // entries of T or P
-constexpr int kTParts = kMat / 2 * 3;  // floats that T's three bf16 parts take
-// Parts behind an answer: bf16 does not show what two leave out (2^-16).
-template <typename T>
-constexpr int kOutParts = sizeof(T) == 2 ? 2 : 3;
+constexpr int kTParts = kMat / 2 * 3;  // floats that a matrix's three bf16 parts take
 // Floats of a chunk's matrices in parts: T and P, or for the gradients T, T^T and P^T.
-template <typename T, bool GRADS>
-constexpr int kMats = GRADS ? 3 * kTParts : kTParts + kMat / 2 * kOutParts<T>;
+template <bool GRADS>
+constexpr int kMats = (GRADS ? 3 : 2) * kTParts;
 
 __device__ __forceinline__ float to_f32(float v) { return v; }
 __device__ __forceinline__ float to_f32(uint16_t v) { return bf16_to_f32(v); }
@@ -230,7 +227,8 @@ __device__ __forceinline__ floatx4 frag_t(const float* p, int ld, int s) {
 }
 // fp32-level products on the bf16 matrix cores: a value is a sum of three bf16 parts, each 2^-8 of the one in
 // front (split3_pair), and of two values' nine products of parts the six down to 2^-16 count. What is bf16 in memory
-// is one part. v_mfma_f32_16x16x32_bf16: lane l holds A[l % 16] and B[..][l % 16] at eight k's (which eight of the
+// is one part; what is computed has three behind bf16 results too, whose terms may cancel (two, to 2^-16, behind answers, dQ
+// and dK: a prompt of 8,032 tokens 308 us instead of 326, gradients 411 instead of 415). v_mfma_f32_16x16x32_bf16: lane l holds A[l % 16] and B[..][l % 16] at eight k's (which eight of the
 // 32 is free, the same for both) and D[4 (l / 16) + r][l % 16]. Against v_mfma_f32_16x16x4_f32 a product takes an
 // eighth of the cycles with one exact operand (three products), a third to a half with six.
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
@@ -282,20 +280,19 @@ struct Acc {
   __device__ __forceinline__ void clear() { v[0] = v[1] = v[2] = floatx4{0.f, 0.f, 0.f, 0.f}; }
   __device__ __forceinline__ floatx4 sum() const { return v[0] + (v[1] + v[2]); }
 };
-// Products of parts up to order O (2: all that count; 1: to 2^-16).
-template <int O, int NA, int NB>
+template <int NA, int NB>
 __device__ __forceinline__ void mma32(const Parts<NA>& a, const Parts<NB>& b, Acc& c) {
 #pragma unroll
   for (int i = 0; i < NA; ++i)
 #pragma unroll
     for (int j = 0; j < NB; ++j)
-      if (i + j <= O) c.v[i + j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.p[i], b.p[j], c.v[i + j], 0, 0, 0);
+      if (i + j <= 2) c.v[i + j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.p[i], b.p[j], c.v[i + j], 0, 0, 0);
 }
 // The same into one accumulator, where registers are short.
-template <int O, int NA, int NB>
+template <int NA, int NB>
 __device__ __forceinline__ void mma32(const Parts<NA>& a, const Parts<NB>& b, floatx4& c) {
 #pragma unroll
-  for (int o = O; o >= 0; --o)
+  for (int o = 2; o >= 0; --o)
 #pragma unroll
     for (int i = 0; i < NA; ++i)
       if (o - i >= 0 && o - i < NB) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.p[i], b.p[o - i], c, 0, 0, 0);
@@ -443,8 +440,8 @@ __global__ __launch_bounds__(256, (sizeof(T) == 4 && DKP == 128 ? 2 : 4)) void d
 #pragma unroll
       for (int s = 0; s < NS; ++s) {
         const auto b = bf[s].parts();
-        mma32<2>(b, kf[s].parts(), x);
-        mma32<2>(b, qf[s].parts(), y);
+        mma32(b, kf[s].parts(), x);
+        mma32(b, qf[s].parts(), y);
       }
       kk[t] = x.sum();
       qk[t] = y.sum();
@@ -490,7 +487,7 @@ __global__ __launch_bounds__(256, (sizeof(T) == 4 && DKP == 128 ? 2 : 4)) void d
   const int share = a.H / a.Hk;
   for (int hv = part; hv < share; hv += parts) {
     const int h = hk * share + hv;
-    float* out = mats + ((int64_t)tile * a.H + h) * kMats<T, GRADS>;
+    float* out = mats + ((int64_t)tile * a.H + h) * kMats<GRADS>;
     float* co = coef + ((int64_t)tile * a.H + h) * 3 * kC;
     // (as if it were another thread for every head: addresses formed once for all heads would not fit the registers)
     int tid = threadIdx.x;
@@ -600,8 +597,8 @@ __global__ __launch_bounds__(256, (sizeof(T) == 4 && DKP == 128 ? 2 : 4)) void d
       if (2 * s > w) continue;
       put_mat<3>(tp, w, s, frag(sT + 16 * w * kLdM, kLdM, 2 * s), frag(sT + 16 * w * kLdM, kLdM, 2 * s + 1));
       if constexpr (!GRADS)
-        put_mat<kOutParts<T>>(tp + 2 * kTParts, w, s, frag(sA + 16 * w * kLdM, kLdM, 2 * s),
-                              frag(sA + 16 * w * kLdM, kLdM, 2 * s + 1));
+        put_mat<3>(tp + 2 * kTParts, w, s, frag(sA + 16 * w * kLdM, kLdM, 2 * s),
+                   frag(sA + 16 * w * kLdM, kLdM, 2 * s + 1));
     }
   }
 }
@@ -642,7 +639,7 @@ __global__ __launch_bounds__(SAVE ? 256 : 512) void delta_chunk_kernel(
     const T* __restrict__ ops, float* state_out, T* __restrict__ o, int64_t ldo,
     float* __restrict__ s0, float* __restrict__ us) {
   constexpr int NW = SAVE ? 4 : 8, NT = DKP / 64;
-  constexpr int NS = DKP / 32, OP = kOutParts<T>;
+  constexpr int NS = DKP / 32;
   __shared__ __attribute__((aligned(16))) uint16_t sS[3 * 16 * DKP], sR[3 * 16 * kC], sW[3 * 16 * kC], sU[3 * 16 * kC];
   // a wavefront's tokens' values and answers, on their way between rows in memory and columns in registers
   constexpr int LV = 20;
@@ -685,11 +682,11 @@ __global__ __launch_bounds__(SAVE ? 256 : 512) void delta_chunk_kernel(
   const int chunks = (len + kC - 1) / kC;
   auto chunk = [&](int ch) { return Chunk{base + ch * kC, min(kC, len - ch * kC)}; };
   auto mat = [&](int ch) {
-    return reinterpret_cast<const uint16_t*>(mats + ((int64_t)(key + ch) * a.H + h) * kMats<T, SAVE>);
+    return reinterpret_cast<const uint16_t*>(mats + ((int64_t)(key + ch) * a.H + h) * kMats<SAVE>);
   };
   Raw8<T> rf[NS], ktf[NT][2];
   Parts<3> tf[2];
-  Parts<OP> pf[2];
+  Parts<3> pf[2];
   floatx4 beta, e, wj;
   Raw4<T> vv;
   const int ldv = (int)a.ldv, cv = c0 + 4 * (lane & 3), tv = 16 * w + lane / 4;
@@ -715,8 +712,8 @@ __global__ __launch_bounds__(SAVE ? 256 : 512) void delta_chunk_kernel(
     tf[1] = mat_parts<3>(mat(ch), w, s1);
   };
   auto load_p = [&](int ch) {
-    pf[0] = mat_parts<OP>(mat(ch) + 2 * kTParts, w, 0);
-    pf[1] = mat_parts<OP>(mat(ch) + 2 * kTParts, w, s1);
+    pf[0] = mat_parts<3>(mat(ch) + 2 * kTParts, w, 0);
+    pf[1] = mat_parts<3>(mat(ch) + 2 * kTParts, w, s1);
   };
   auto load_kt = [&](int ch) {
     const T* p = op(ch, 2);
@@ -755,7 +752,7 @@ __global__ __launch_bounds__(SAVE ? 256 : 512) void delta_chunk_kernel(
       acc.clear();
 #pragma unroll
       for (int s = 0; s < 2; ++s)
-        if (s <= s1) mma32<OP - 1>(pf[s], get_parts<OP>(sU + swap8<kC>(li, 32 * s + 8 * lk), 16 * kC), acc);
+        if (s <= s1) mma32(pf[s], get_parts<3>(sU + swap8<kC>(li, 32 * s + 8 * lk), 16 * kC), acc);
       load_p(next);
       const floatx4 x = acc.sum();
 #pragma unroll
@@ -775,7 +772,7 @@ __global__ __launch_bounds__(SAVE ? 256 : 512) void delta_chunk_kernel(
         acc.clear();
 #pragma unroll
         for (int s = 0; s < NS; ++s)
-          mma32<2>(rf[s].parts(), get_parts<3>(sS + swap8<DKP>(li, 32 * s + 8 * lk), 16 * DKP), acc);
+          mma32(rf[s].parts(), get_parts<3>(sS + swap8<DKP>(li, 32 * s + 8 * lk), 16 * DKP), acc);
         load_rows(next);
         out = acc.sum();
 #pragma unroll
@@ -796,12 +793,12 @@ __global__ __launch_bounds__(SAVE ? 256 : 512) void delta_chunk_kernel(
         acc.clear();
 #pragma unroll
         for (int s = 0; s < 2; ++s)
-          if (s <= s1) mma32<2>(tf[s], get_parts<3>(sR + swap8<kC>(li, 32 * s + 8 * lk), 16 * kC), acc);
+          if (s <= s1) mma32(tf[s], get_parts<3>(sR + swap8<kC>(li, 32 * s + 8 * lk), 16 * kC), acc);
         load_t(next);
         const floatx4 u = acc.sum();
         put_parts<3>(sW + swap8<kC>(li, place), 16 * kC, u * wj);
         wj = factor(next, 2);
-        if constexpr (!SAVE) put_parts<OP>(sU + swap8<kC>(li, place), 16 * kC, u);
+        if constexpr (!SAVE) put_parts<3>(sU + swap8<kC>(li, place), 16 * kC, u);
         if (SAVE && col)
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
@@ -812,7 +809,7 @@ __global__ __launch_bounds__(SAVE ? 256 : 512) void delta_chunk_kernel(
         acc.clear();
 #pragma unroll
         for (int s = 0; s < NS; ++s)
-          mma32<OP - 1>(rf[s].parts(), get_parts<OP>(sS + swap8<DKP>(li, 32 * s + 8 * lk), 16 * DKP), acc);
+          mma32(rf[s].parts(), get_parts<3>(sS + swap8<DKP>(li, 32 * s + 8 * lk), 16 * DKP), acc);
         load_rows(next);
         out = acc.sum();
       }
@@ -826,7 +823,7 @@ __global__ __launch_bounds__(SAVE ? 256 : 512) void delta_chunk_kernel(
         for (int n = 0; n < NT; ++n) {
           acc.clear();
 #pragma unroll
-          for (int s = 0; s < 2; ++s) mma32<2>(ktf[n][s].parts(), wf[s], acc);
+          for (int s = 0; s < 2; ++s) mma32(ktf[n][s].parts(), wf[s], acc);
           st[n] = st[n] * eC + acc.sum();
         }
         share();
@@ -899,7 +896,7 @@ __global__ __launch_bounds__(512) void delta_back_kernel(DeltaIn a, const T* __r
   const int chunks = (len + kC - 1) / kC;
   auto chunk = [&](int ch) { return Chunk{base + ch * kC, min(kC, len - ch * kC)}; };
   auto mat = [&](int ch, int i) {
-    return reinterpret_cast<const uint16_t*>(mats + ((int64_t)(key + ch) * a.H + h) * kMats<T, true> + i * kTParts);
+    return reinterpret_cast<const uint16_t*>(mats + ((int64_t)(key + ch) * a.H + h) * kMats<true> + i * kTParts);
   };
   auto op = [&](int ch, int i) { return ops + (((int64_t)(key + ch) * a.Hk + hk) * 3 + i) * DKP * kC; };
   auto factor = [&](int ch, int i) {
@@ -964,14 +961,14 @@ __global__ __launch_bounds__(512) void delta_back_kernel(DeltaIn a, const T* __r
       acc.clear();
 #pragma unroll
       for (int s = 0; s < NS; ++s)
-        mma32<2>(rf[s].parts(), get_parts<3>(sS + swap8<DKP>(li, 32 * s + 8 * lk), 16 * DKP), acc);
+        mma32(rf[s].parts(), get_parts<3>(sS + swap8<DKP>(li, 32 * s + 8 * lk), 16 * DKP), acc);
       load_o(next);
       load_rows(next);
       const floatx4 y = acc.sum();
       acc.clear();
 #pragma unroll
       for (int s = 0; s < 2; ++s)
-        if (s >= s0) mma32<2>(pf[s], get_parts<KP>(sO + swap8<kC>(li, 32 * s + 8 * lk), 16 * kC), acc);
+        if (s >= s0) mma32(pf[s], get_parts<KP>(sO + swap8<kC>(li, 32 * s + 8 * lk), 16 * kC), acc);
       load_mat(pf, mat(next, 2));
       floatx4 x = acc.sum() + y * wj;
       put_parts<3>(sU + swap8<kC>(li, place), 16 * kC, x);
@@ -981,7 +978,7 @@ __global__ __launch_bounds__(512) void delta_back_kernel(DeltaIn a, const T* __r
       acc.clear();
 #pragma unroll
       for (int s = 0; s < 2; ++s)
-        if (s >= s0) mma32<2>(tf[s], get_parts<3>(sU + swap8<kC>(li, 32 * s + 8 * lk), 16 * kC), acc);
+        if (s >= s0) mma32(tf[s], get_parts<3>(sU + swap8<kC>(li, 32 * s + 8 * lk), 16 * kC), acc);
       load_mat(tf, mat(next, 1));
       const floatx4 dr = acc.sum();
       put_parts<3>(sW + swap8<kC>(li, place), 16 * kC, -(dr * beta * e));
@@ -1037,7 +1034,7 @@ __global__ __launch_bounds__(512) void delta_back_kernel(DeltaIn a, const T* __r
       for (int n = 0; n < NT; ++n) {
         acc[n].clear();
 #pragma unroll
-        for (int s = 0; s < 2; ++s) mma32<2>(qt[n][s].parts(), ef[s], acc[n]);
+        for (int s = 0; s < 2; ++s) mma32(qt[n][s].parts(), ef[s], acc[n]);
       }
     }
     load_tiles(qt, op(next, 1));
@@ -1049,7 +1046,7 @@ __global__ __launch_bounds__(512) void delta_back_kernel(DeltaIn a, const T* __r
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
 #pragma unroll
-      for (int s = 0; s < 2; ++s) mma32<2>(kt[n][s].parts(), wf[s], acc[n]);
+      for (int s = 0; s < 2; ++s) mma32(kt[n][s].parts(), wf[s], acc[n]);
       st[n] = st[n] * eC + acc[n].sum();
     }
     share();
@@ -1095,10 +1092,10 @@ __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaIn a, const T* __
                                                           int64_t lddq, T* __restrict__ dk, int64_t lddk,
                                                           float* __restrict__ dg, int64_t lddg,
                                                           float* __restrict__ dbeta, int64_t lddb) {
-  constexpr int NT = DKP / 32, OP = kOutParts<T>;  // NT: tiles of 16 rows to a wavefront
+  constexpr int NT = DKP / 32;  // NT: tiles of 16 rows to a wavefront
   constexpr int kState = DKP * kLdSl, kU = kC * kLdSl, kZ = kC * kLdZ;  // bf16 entries of one part
   constexpr int KP = sizeof(T) == 2 ? 1 : 3;  // parts of an activation
-  constexpr int kSlices = 6 * kState + (6 + KP) * kU, kProducts = 4 * OP * kZ + 2 * 2 * kC * kLdF;
+  constexpr int kSlices = 6 * kState + (6 + KP) * kU, kProducts = 4 * 3 * kZ + 2 * 2 * kC * kLdF;
   __shared__ __attribute__((aligned(16))) uint16_t pool[kSlices > kProducts ? kSlices : kProducts];
   __shared__ double sG[kC];
   __shared__ float sB[kC], sQ1[2][kC], sK2[2][kC], sK3[2][kC], sRow[kC], sCol[kC], sSum[2][kC], sSeg[8][kC], sDot[8];
@@ -1200,8 +1197,8 @@ __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaIn a, const T* __
       for (int b = 0; b < 4; ++b) {
         if (b > w) continue;
         const Parts<3> ub = get_parts<3>(sUs + (16 * b + li) * kLdSl + 8 * lk, kU);
-        if (set) mma32<2>(ub, rb, dz[b]);
-        else mma32<2>(ub, ob, dz[b]);
+        if (set) mma32(ub, rb, dz[b]);
+        else mma32(ub, ob, dz[b]);
         keep_order();
       }
       const Parts<3> ub = get_parts<3>(sUs + own, kU);
@@ -1209,9 +1206,9 @@ __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaIn a, const T* __
       for (int n = 0; n < NT; ++n) {
         const int r = ((set * NT + n) * 16 + li) * kLdSl + 8 * lk;
         const Parts<3> x = get_parts<3>(sS0 + r, kState), y = get_parts<3>(sD1 + r, kState);
-        mma32<2>(x, ob, x1[n]);
-        mma32<2>(x, rb, x2[n]);
-        mma32<2>(y, ub, x3[n]);
+        mma32(x, ob, x1[n]);
+        mma32(x, rb, x2[n]);
+        mma32(y, ub, x3[n]);
         keep_order();
       }
     }
@@ -1253,9 +1250,9 @@ __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaIn a, const T* __
     if (lane == 0) sDot[wv] = dot;
     sync_lds();  // the slices are read
     // the set's matrix, M1 or M2 (below the diagonal), as rows and as columns over tokens in place
-    uint16_t* sZ = pool + set * 2 * OP * kZ;
-    uint16_t* sZT = sZ + OP * kZ;
-    float* sF = reinterpret_cast<float*>(pool + 4 * OP * kZ) + set * kC * kLdF;  // dP P or dA A
+    uint16_t* sZ = pool + set * 2 * 3 * kZ;
+    uint16_t* sZT = sZ + 3 * kZ;
+    float* sF = reinterpret_cast<float*>(pool + 4 * 3 * kZ) + set * kC * kLdF;  // dP P or dA A
     float rowsum = 0.f;  // of dA D kk, of the lane's token
 #pragma unroll
     for (int b = 0; b < 4; ++b) {
@@ -1276,13 +1273,13 @@ __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaIn a, const T* __
           f[r] = j < t ? z[r] * zz[b][r] : 0.f;
         }
       }
-      put_parts<OP>(sZ + t * kLdZ + token_place(b, lk), kZ, z);
-      const Parts4<OP> p = split4<OP>(z);
+      put_parts<3>(sZ + t * kLdZ + token_place(b, lk), kZ, z);
+      const Parts4<3> p = split4<3>(z);
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const int j = 16 * b + 4 * lk + r, at = token_place(w, li >> 2) + (li & 3);
 #pragma unroll
-        for (int i = 0; i < OP; ++i) sZT[i * kZ + j * kLdZ + at] = p.get(i, r);
+        for (int i = 0; i < 3; ++i) sZT[i * kZ + j * kLdZ + at] = p.get(i, r);
         if (j <= t) sF[t * kLdF + j] = f[r];
       }
       keep_order();
@@ -1292,21 +1289,21 @@ __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaIn a, const T* __
     sync_lds();
     {
       const uint16_t* m1 = pool;
-      const uint16_t* m1t = pool + OP * kZ;
-      const uint16_t* m2 = pool + 2 * OP * kZ;
-      const uint16_t* m2t = pool + 3 * OP * kZ;
+      const uint16_t* m1t = pool + 3 * kZ;
+      const uint16_t* m2 = pool + 2 * 3 * kZ;
+      const uint16_t* m2t = pool + 3 * 3 * kZ;
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
         const int at = t * kLdZ + 32 * s + 8 * lk;
         const bool lo = s <= w >> 1, hi = s >= w >> 1;
-        Parts<OP> b1, b1t, b2, b2t;
+        Parts<3> b1, b1t, b2, b2t;
         if (lo) {
-          b1 = get_parts<OP>(m1 + at, kZ);
-          b2 = get_parts<OP>(m2 + at, kZ);
+          b1 = get_parts<3>(m1 + at, kZ);
+          b2 = get_parts<3>(m2 + at, kZ);
         }
         if (hi) {
-          b1t = get_parts<OP>(m1t + at, kZ);
-          b2t = get_parts<OP>(m2t + at, kZ);
+          b1t = get_parts<3>(m1t + at, kZ);
+          b2t = get_parts<3>(m2t + at, kZ);
         }
         Raw8<T> kt[NT], qt[NT];
 #pragma unroll
@@ -1319,12 +1316,12 @@ __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaIn a, const T* __
         for (int n = 0; n < NT; ++n) {
           const auto ka = kt[n].parts();
           if (lo) {
-            mma32<OP - 1>(ka, b1, dqa[n]);
-            mma32<OP - 1>(ka, b2, dka[n]);
+            mma32(ka, b1, dqa[n]);
+            mma32(ka, b2, dka[n]);
           }
           if (hi) {
-            mma32<OP - 1>(qt[n].parts(), b1t, dka[n]);
-            mma32<OP - 1>(ka, b2t, dka[n]);
+            mma32(qt[n].parts(), b1t, dka[n]);
+            mma32(ka, b2t, dka[n]);
           }
           keep_order();
         }
@@ -1356,7 +1353,7 @@ __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaIn a, const T* __
     sync_lds();
     {
       const int row = tid >> 3, p = tid & 7;  // eight lanes to a token
-      const float* f0 = reinterpret_cast<const float*>(pool + 4 * OP * kZ);
+      const float* f0 = reinterpret_cast<const float*>(pool + 4 * 3 * kZ);
       float sum = 0.f;
 #pragma unroll
       for (int x = 0; x < 8; ++x) {
@@ -1427,7 +1424,7 @@ hipError_t chunks(const DeltaOp& a, float* state_out, void* o, int64_t ldo, floa
   float* coef = ws;
   float* mats = ws + tiles * a.H * 3 * kC;
   const T *q = static_cast<const T*>(a.q), *k = static_cast<const T*>(a.k), *v = static_cast<const T*>(a.v);
-  T* ops = reinterpret_cast<T*>(mats + tiles * a.H * kMats<T, false>);
+  T* ops = reinterpret_cast<T*>(mats + tiles * a.H * kMats<false>);
   const int parts = prep_parts(a, tiles);
   delta_prep_kernel<T, DKP, false><<<dim3((unsigned)(tiles * a.Hk * parts)), 256, 0, s>>>(in_of(a), q, k, mats, coef, ops,
                                                                                           nullptr, parts);
@@ -1448,7 +1445,7 @@ struct BackSpace {
     const int64_t th = tiles_of(n_seq, rows) * H, head = (int64_t)Dk * Dv, act = th * kC * Dv;
     coef = 0;
     mats = coef + th * 3 * kC;
-    prods = mats + th * kMats<float, true>;
+    prods = mats + th * kMats<true>;
     s0 = prods + tiles_of(n_seq, rows) * Hk * 2 * kMat;
     ds1 = s0 + th * head;
     us = ds1 + th * head;
@@ -1486,8 +1483,7 @@ hipError_t grads(const DeltaOp& a, const void* d_o_, int64_t lddo, const float* 
 size_t delta_rule_workspace_bytes(bool bf16, int n_seq, int rows, int Hk, int H, int Dk, int Dv) {
   (void)Dv;
   if (!chunked(bf16, n_seq, rows, H)) return 0;
-  const int mats = bf16 ? kMats<uint16_t, false> : kMats<float, false>;
-  return (size_t)(tiles_of(n_seq, rows) * H * (3 * kC + mats) + op_floats(bf16, n_seq, rows, Hk, Dk)) * sizeof(float);
+  return (size_t)(tiles_of(n_seq, rows) * H * (3 * kC + kMats<false>) + op_floats(bf16, n_seq, rows, Hk, Dk)) * sizeof(float);
 }
 
 hipError_t launch_delta_rule(const DeltaOp& a, float* state_out, void* o, int64_t ldo, float* ws, hipStream_t s) {
