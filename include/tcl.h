@@ -745,7 +745,9 @@ TCL_API tcl_status tcl_distill_topk(int32_t dtype, int32_t n_rows, int32_t V, co
  *   d_score[g, b] + log p_b(v),   p = softmax(logits / temperature),
  * d_score [n_groups, W] fp32 the beams' own. A group's K best go to d_parent (the row g W + b), d_token
  * (v) and d_out_score, all [n_groups, K]: highest first (compared in 64 bits, rounded to fp32 at the end), equal
- * scores by lower row; a row's own candidates in tcl_topk's order, by their logits, then by lower token. d_ended
+ * scores by lower row; a row's own candidates in tcl_topk's order, by their logits, then by lower token. A row's sum of
+ * exponentials is fp32, log p_b good to some 4e-7 (1e-6 for a million tokens): candidates of different rows that are closer
+ * may change places. Rows of the same logits have the same sums, wherever they start. d_ended
  * [n_groups, W] int32 or NULL: a beam with an entry >= 0 has ended, and is one candidate itself, with that entry
  * as its token and its own score. A beam whose score is -inf or NaN is dead. Neither's logits are read. Masked
  * (-inf) and NaN logits, and rows with a logit of +inf, are no candidates; past the end of a group with fewer than
