@@ -751,8 +751,9 @@ TCL_API tcl_status tcl_distill_topk(int32_t dtype, int32_t n_rows, int32_t V, co
  * [n_groups, W] int32 or NULL: a beam with an entry >= 0 has ended, and is one candidate itself, with that entry
  * as its token and its own score. A beam whose score is -inf or NaN is dead. Neither's logits are read. Masked
  * (-inf) and NaN logits, and rows with a logit of +inf, are no candidates; past the end of a group with fewer than
- * K: -1, -1 and -inf. logits as for tcl_logprobs (rows); W and K in [1, 64], n_groups W < 2^22. d_workspace: >=
- * tcl_beam_select_workspace_bytes bytes, 256-byte aligned. n_groups == 0 is TCL_OK. */
+ * K: -1, -1 and -inf. The outputs must not overlap each other, d_score, d_ended or the workspace. logits as for
+ * tcl_logprobs (rows); W and K in [1, 64], n_groups W < 2^22. d_workspace: >= tcl_beam_select_workspace_bytes bytes,
+ * 256-byte aligned. n_groups == 0 is TCL_OK. */
 TCL_API size_t tcl_beam_select_workspace_bytes(int32_t n_groups, int32_t W, int32_t V, int32_t K);
 TCL_API tcl_status tcl_beam_select(int32_t dtype, int32_t n_groups, int32_t W, int32_t V, const void* d_logits,
                                    int64_t ld, float temperature, const float* d_score, const int32_t* d_ended,

@@ -11,6 +11,16 @@ namespace {
 
 bool misaligned(const void* p, uintptr_t n) { return reinterpret_cast<uintptr_t>(p) % n != 0; }
 
+// Arrays of n bytes that share one (NULL: no array).
+struct Bytes {
+  const void* p;
+  size_t n;
+};
+bool overlap(Bytes a, Bytes b) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
+  return x && y && a.n && b.n && x < y + b.n && y < x + a.n;
+}
+
 // A launch has fewer than 2^32 threads. A scan's tiles hold 30 rows or more, besides one per sequence, and
 // their channels are rounded up to 64, in the gradients (wavefronts in fours) to less than twice that: with these
 // bounds 2 (2^34 / 30 + 2^30) threads at most, and row and tile indices far inside 31 bits. The convolution's
@@ -452,8 +462,17 @@ TCL_API tcl_status tcl_beam_select(int32_t dtype, int32_t n_groups, int32_t W, i
   if (tcl_status st = logit_rows(dtype, n_groups * W, V, d_logits, ld, nullptr, temperature, &a)) return st;
   if (n_groups == 0) return TCL_OK;
   if (!d_score || !d_parent || !d_token || !d_out_score) return fail(TCL_ERR_INVALID_ARG, "NULL device pointer");
-  if (d_out_score == d_score) return fail(TCL_ERR_INVALID_ARG, "the candidates' scores in place of the beams'");
-  if (tcl_status st = check_workspace(d_workspace, ws_bytes, beam_select_workspace_bytes(n_groups, W, V, K))) return st;
+  const size_t need = beam_select_workspace_bytes(n_groups, W, V, K);
+  if (tcl_status st = check_workspace(d_workspace, ws_bytes, need)) return st;
+  const size_t out = (size_t)n_groups * K * 4, in = (size_t)n_groups * W * 4;
+  const Bytes outs[] = {{d_parent, out}, {d_token, out}, {d_out_score, out}};
+  const Bytes ins[] = {{d_score, in}, {d_ended, in}, {d_workspace, need}};  // (what a group reads while others write)
+  for (int i = 0; i < 3; ++i) {
+    for (const Bytes& b : ins)
+      if (overlap(outs[i], b)) return fail(TCL_ERR_INVALID_ARG, "an output overlaps the scores, d_ended or the workspace");
+    for (int j = 0; j < i; ++j)
+      if (overlap(outs[i], outs[j])) return fail(TCL_ERR_INVALID_ARG, "outputs overlap each other");
+  }
   TCL_HIP(launch_beam_select(a, W, K, d_score, d_ended, d_parent, d_token, d_out_score, d_workspace,
                              static_cast<hipStream_t>(stream)));
   return TCL_OK;
@@ -476,9 +495,8 @@ TCL_API tcl_status tcl_beam_reorder(int32_t n_groups, int32_t W, const int32_t* 
   }
   if (n_groups == 0) return TCL_OK;
   if (!d_parent || !d_slots || !d_slots_out) return fail(TCL_ERR_INVALID_ARG, "NULL device pointer");
-  const uintptr_t in = reinterpret_cast<uintptr_t>(d_slots), par = reinterpret_cast<uintptr_t>(d_parent),
-                  out = reinterpret_cast<uintptr_t>(d_slots_out), len = (uintptr_t)n_groups * W * sizeof(int32_t);
-  if ((out < in + len && in < out + len) || (out < par + len && par < out + len))
+  const size_t len = (size_t)n_groups * W * sizeof(int32_t);
+  if (overlap({d_slots_out, len}, {d_slots, len}) || overlap({d_slots_out, len}, {d_parent, len}))
     return fail(TCL_ERR_INVALID_ARG, "d_slots_out overlaps an input");
   static_assert(sizeof(tcl_beam_pool) == sizeof(BeamPool), "one layout");
   TCL_HIP(launch_beam_reorder(n_groups, W, d_parent, d_slots, n_slots, d_slots_out, n_pools,
