@@ -671,7 +671,7 @@ TCL_API tcl_status tcl_delta_rule_backward(const tcl_delta_rule_args* args, cons
  *   h = (x - mean x) / sqrt(mean (x - mean x)^2 + eps),   y = h w + b.
  * x and y are fp32 or bf16 (dtype) of any alignment, rows with a leading dimension >= C; w and b [C] fp32, NULL: ones,
  * zeros. Statistics are fp32, the variance from deviations; y is rounded to dtype once and must not
- * overlap x. eps finite, not negative (0: a row of equal values gives NaN); C in [1, 16384], rows <= 2^30; rows == 0
+ * overlap x, w or b (refused; columns beside x's in one buffer do not). eps finite, not negative (0: a row of equal values gives NaN); C in [1, 16384], rows <= 2^30; rows == 0
  * is TCL_OK. Stream-ordered, deterministic, no allocation.
  * ------------------------------------------------------------------- */
 TCL_API tcl_status tcl_layer_norm(int32_t dtype, int32_t rows, int32_t C, const void* d_x, int64_t ldx,
@@ -679,8 +679,8 @@ TCL_API tcl_status tcl_layer_norm(int32_t dtype, int32_t rows, int32_t C, const 
                                   void* stream);
 
 /* Gradients from x, w and d_dy [rows, C] (lddy); nothing is kept from the forward call. d_dx [rows, C] (lddx)
- * has x's type and must not overlap the inputs; d_dw and d_db (NULL: not wanted) [C] are fp32, summed over all rows
- * and overwritten (zeros for no rows). d_workspace: >= tcl_layer_norm_workspace_bytes bytes, 256-byte aligned. */
+ * has x's type and must not overlap the inputs; d_dw [C] and d_db [C] (NULL: not wanted) are fp32, summed over all rows
+ * and overwritten (zeros for no rows). No output may overlap another or the workspace. d_workspace: >= tcl_layer_norm_workspace_bytes bytes, 256-byte aligned. */
 TCL_API size_t tcl_layer_norm_workspace_bytes(int32_t dtype, int32_t rows, int32_t C);
 TCL_API tcl_status tcl_layer_norm_backward(int32_t dtype, int32_t rows, int32_t C, const void* d_x, int64_t ldx,
                                            const float* d_w, float eps, const void* d_dy, int64_t lddy, void* d_dx,

@@ -1,6 +1,8 @@
 // C entry points of the sequence and logit operators (include/tcl.h): argument
 // checks, then the launchers of ssm.hip, delta.hip, norm.hip, logits.hip and beam.hip.
+#include <algorithm>
 #include <cmath>
+#include <numeric>
 
 #include "model.h"
 #include "ops.h"
@@ -11,14 +13,26 @@ namespace {
 
 bool misaligned(const void* p, uintptr_t n) { return reinterpret_cast<uintptr_t>(p) % n != 0; }
 
-// Arrays of n bytes that share one (NULL: no array).
-struct Bytes {
+// Matrices of n rows of w bytes, ld apart, that share a byte; columns beside each other in one buffer, or rows between each
+// other's, do not.
+struct Rows {
   const void* p;
-  size_t n;
+  int64_t n, w, ld;
 };
-bool overlap(Bytes a, Bytes b) {
-  const uintptr_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
-  return x && y && a.n && b.n && x < y + b.n && y < x + a.n;
+Rows flat(const void* p, size_t bytes) { return {p, bytes > 0, (int64_t)bytes, (int64_t)bytes}; }
+bool overlap(Rows a, Rows b) {
+  if (!a.p || !b.p || a.n < 1 || b.n < 1) return false;
+  const int64_t x = reinterpret_cast<int64_t>(a.p), y = reinterpret_cast<int64_t>(b.p);
+  const int64_t x_end = x + (a.n - 1) * a.ld + a.w, y_end = y + (b.n - 1) * b.ld + b.w;
+  if (x >= y_end || y >= x_end) return false;
+  // where rows of b begin behind rows of a: always the same, modulo what both strides are multiples of
+  const int64_t g = std::gcd(a.ld, b.ld), d = ((y - x) % g + g) % g;
+  if (d >= a.w && g - d >= b.w) return false;
+  for (int64_t i = std::max<int64_t>(0, (y - a.w - x) / a.ld); i < a.n && x + i * a.ld < y_end; ++i) {
+    const int64_t at = x + i * a.ld, last = at + a.w - 1 - y;  // b's last row that begins in front of the row's end
+    if (last >= 0 && y + std::min(b.n - 1, last / b.ld) * b.ld + b.w > at) return true;
+  }
+  return false;
 }
 
 // A launch has fewer than 2^32 threads. A scan's tiles hold 30 rows or more, besides one per sequence, and
@@ -282,7 +296,11 @@ TCL_API tcl_status tcl_layer_norm(int32_t dtype, int32_t rows, int32_t C, const 
   if (ldy < C) return fail(TCL_ERR_INVALID_ARG, "leading dimension smaller than C");
   if (rows == 0) return TCL_OK;
   if (!d_y) return fail(TCL_ERR_INVALID_ARG, "NULL device pointer");
-  if (misaligned(d_y, op.bf16 ? 2 : 4)) return fail(TCL_ERR_INVALID_ARG, "y is not aligned to its type");
+  const int64_t el = op.bf16 ? 2 : 4;
+  if (misaligned(d_y, el)) return fail(TCL_ERR_INVALID_ARG, "y is not aligned to its type");
+  const Rows y = {d_y, rows, C * el, ldy * el};
+  if (overlap(y, {d_x, rows, C * el, ldx * el}) || overlap(y, flat(d_w, C * 4)) || overlap(y, flat(d_b, C * 4)))
+    return fail(TCL_ERR_INVALID_ARG, "y overlaps an input");
   TCL_HIP(launch_layer_norm(op, d_y, ldy, static_cast<hipStream_t>(stream)));
   return TCL_OK;
 }
@@ -300,10 +318,17 @@ TCL_API tcl_status tcl_layer_norm_backward(int32_t dtype, int32_t rows, int32_t 
   if (tcl_status st = norm_op(dtype, rows, C, d_x, ldx, d_w, nullptr, eps, &op)) return st;
   if (lddy < C || lddx < C) return fail(TCL_ERR_INVALID_ARG, "leading dimension smaller than C");
   if (!d_dw || (rows > 0 && (!d_dy || !d_dx))) return fail(TCL_ERR_INVALID_ARG, "NULL device pointer");
-  if (misaligned(d_dy, op.bf16 ? 2 : 4) || misaligned(d_dx, op.bf16 ? 2 : 4))
+  const int64_t el = op.bf16 ? 2 : 4;
+  if (misaligned(d_dy, el) || misaligned(d_dx, el))
     return fail(TCL_ERR_INVALID_ARG, "dy and dx have to be aligned to their type");
   const size_t need = rows > 0 ? layer_norm_workspace_bytes(op.bf16, rows, C) : 0;
   if (tcl_status st = check_workspace(d_workspace, ws_bytes, need)) return st;
+  const Rows dx = {d_dx, rows, C * el, lddx * el}, dw = flat(d_dw, C * 4), db = flat(d_db, C * 4), ws = flat(d_workspace, need);
+  if (overlap(dx, {d_x, rows, C * el, ldx * el}) || overlap(dx, {d_dy, rows, C * el, lddy * el}) ||
+      overlap(dx, flat(d_w, C * 4)) || overlap(dx, ws) || overlap(dw, ws) || overlap(db, ws))
+    return fail(TCL_ERR_INVALID_ARG, "an output overlaps an input or the workspace");
+  if (overlap(dw, db) || overlap(dw, dx) || overlap(db, dx))
+    return fail(TCL_ERR_INVALID_ARG, "outputs overlap each other");
   TCL_HIP(launch_layer_norm_bwd(op, d_dy, lddy, d_dx, lddx, d_dw, d_db, static_cast<float*>(d_workspace),
                                 static_cast<hipStream_t>(stream)));
   return TCL_OK;
@@ -465,10 +490,10 @@ TCL_API tcl_status tcl_beam_select(int32_t dtype, int32_t n_groups, int32_t W, i
   const size_t need = beam_select_workspace_bytes(n_groups, W, V, K);
   if (tcl_status st = check_workspace(d_workspace, ws_bytes, need)) return st;
   const size_t out = (size_t)n_groups * K * 4, in = (size_t)n_groups * W * 4;
-  const Bytes outs[] = {{d_parent, out}, {d_token, out}, {d_out_score, out}};
-  const Bytes ins[] = {{d_score, in}, {d_ended, in}, {d_workspace, need}};  // (what a group reads while others write)
+  const Rows outs[] = {flat(d_parent, out), flat(d_token, out), flat(d_out_score, out)};
+  const Rows ins[] = {flat(d_score, in), flat(d_ended, in), flat(d_workspace, need)};  // (what a group reads while others write)
   for (int i = 0; i < 3; ++i) {
-    for (const Bytes& b : ins)
+    for (const Rows& b : ins)
       if (overlap(outs[i], b)) return fail(TCL_ERR_INVALID_ARG, "an output overlaps the scores, d_ended or the workspace");
     for (int j = 0; j < i; ++j)
       if (overlap(outs[i], outs[j])) return fail(TCL_ERR_INVALID_ARG, "outputs overlap each other");
@@ -496,7 +521,7 @@ TCL_API tcl_status tcl_beam_reorder(int32_t n_groups, int32_t W, const int32_t* 
   if (n_groups == 0) return TCL_OK;
   if (!d_parent || !d_slots || !d_slots_out) return fail(TCL_ERR_INVALID_ARG, "NULL device pointer");
   const size_t len = (size_t)n_groups * W * sizeof(int32_t);
-  if (overlap({d_slots_out, len}, {d_slots, len}) || overlap({d_slots_out, len}, {d_parent, len}))
+  if (overlap(flat(d_slots_out, len), flat(d_slots, len)) || overlap(flat(d_slots_out, len), flat(d_parent, len)))
     return fail(TCL_ERR_INVALID_ARG, "d_slots_out overlaps an input");
   static_assert(sizeof(tcl_beam_pool) == sizeof(BeamPool), "one layout");
   TCL_HIP(launch_beam_reorder(n_groups, W, d_parent, d_slots, n_slots, d_slots_out, n_pools,
