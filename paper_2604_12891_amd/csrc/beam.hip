@@ -101,20 +101,24 @@ __global__ __launch_bounds__(kThreads) void beam_reorder_kernel(int W, const int
 
 hipError_t launch_beam_reorder(int groups, int W, const int* parent, const int* slots, int n_slots, int* slots_out,
                                int n_pools, const BeamPool* pools, hipStream_t s) {
-  for (int k = 0; k == 0 || k < n_pools; k += kPoolsPerLaunch) {
+  // fewer than 2^32 threads in a launch: what 63 of the largest pools take, and many groups of large states share workgroups
+  constexpr int kMaxGroups = (1 << 24) - 1;
+  int k = 0;
+  do {
     Pools p = {};
-    p.n = std::min(n_pools - k, kPoolsPerLaunch);
-    for (int i = 0; i < p.n; ++i) {
-      p.p[i] = pools[k + i];
-      p.first[i + 1] = p.first[i] + (int)((pools[k + i].bytes + kSegment - 1) / kSegment);
+    for (; k + p.n < n_pools && p.n < kPoolsPerLaunch; ++p.n) {
+      const int segs = (int)((pools[k + p.n].bytes + kSegment - 1) / kSegment);
+      if (segs > kMaxGroups - p.first[p.n]) break;
+      p.p[p.n] = pools[k + p.n];
+      p.first[p.n + 1] = p.first[p.n] + segs;
     }
-    // fewer than 2^32 threads in a launch: many groups of large states share workgroups
     const int segs = std::max(p.first[p.n], 1);
-    const dim3 grid(segs, std::min({groups, 65535, std::max(1, ((1 << 24) - 1) / segs)}));
+    const dim3 grid(segs, std::min({groups, 65535, kMaxGroups / segs}));
     beam_reorder_kernel<<<grid, kThreads, 0, s>>>(W, parent, slots, n_slots, k == 0 ? slots_out : nullptr, groups, p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-  }
+    k += p.n;
+  } while (k < n_pools);
   return hipSuccess;
 }
 
