@@ -1098,7 +1098,7 @@ __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaIn a, const T* __
   constexpr int kSlices = 6 * kState + (6 + KP) * kU, kProducts = 4 * 3 * kZ + 2 * 2 * kC * kLdF;
   __shared__ __attribute__((aligned(16))) uint16_t pool[kSlices > kProducts ? kSlices : kProducts];
   __shared__ double sG[kC];
-  __shared__ float sB[kC], sQ1[2][kC], sK2[2][kC], sK3[2][kC], sRow[kC], sCol[kC], sSum[2][kC], sSeg[8][kC], sDot[8];
+  __shared__ float sQ1[2][kC], sK2[2][kC], sK3[2][kC], sRow[kC], sCol[kC], sSum[2][kC], sSeg[8][kC], sDot[8];
   uint16_t* sS0 = pool;
   uint16_t* sD1 = pool + 3 * kState;
   uint16_t* sUs = pool + 6 * kState;
@@ -1137,7 +1137,6 @@ __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaIn a, const T* __
         if (tid >= o) G += up;
       }
       sG[tid] = G;
-      sB[tid] = co[tid];
     }
     // a slice's share of this thread
     constexpr int NL = DKP * (kSl / 4) / 512;
