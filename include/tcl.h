@@ -606,9 +606,10 @@ TCL_API tcl_status tcl_ssm_scan_backward(const tcl_ssm_scan_args* args, const vo
  * Dk in [8, 128], Dv in [8, 256], multiples of 8; H at most 1024; rows H at most 2^28, n_seq H below 2^19 (2^22 for
  * the single-token form's forward call), the activations' leading dimensions at most 2^22. Activations fp32 or bf16 of
  * any alignment, g, beta and the states fp32; all sums are fp32, products of fp32 values three bf16 parts' (to 2^-24),
- * results rounded to dtype once. Sequences are walked token by token where there are few rows to each on average (fewer
- * than 24 to 256, by type and number of heads), else in chunks of 64 tokens: a long one among many short ones is better
- * given a call of its own. A NaN or an
+ * results rounded to dtype once. The forward call walks sequences token by token where there are few rows to each on
+ * average (fewer than 24 to 256, by type and number of heads), else in chunks of 64 tokens: a long one among many short
+ * ones is better given a call of its own. The gradients always take chunks, each sequence (an empty one too) one at least,
+ * at their cost in time and in workspace (see there). A NaN or an
  * infinity among a head's inputs reaches its sequence's other rows in that head, in a chunk also earlier ones.
  * Rows that no sequence owns are neither read nor written. Stream-ordered, deterministic, no allocation; may be
  * captured into a graph.
@@ -659,7 +660,9 @@ typedef struct tcl_delta_rule_grads {
 
 /* Gradients from the inputs and d_do [rows, H, Dv] (lddo); nothing is kept from the forward
  * call. d_dstate_out [n_seq, H, Dk, Dv]: the gradient of the end states (NULL: zeros). State i belongs to
- * sequence i (no slots). No sequences at all are refused (TCL_ERR_INVALID_ARG). */
+ * sequence i (no slots). The workspace holds rows / 64 + n_seq chunks of 73 KiB + 8 Dk Dv + 512 Dv bytes a value head (64 x 64:
+ * 137 KiB, 128 x 128: 265) and 56 to 128 KiB a key head: 4,096 sequences of 15 tokens with 8 key heads and 16 value heads of
+ * 128 x 128 need 25 GB in bf16, so many short sequences are better given several calls. No sequences at all are refused (TCL_ERR_INVALID_ARG). */
 TCL_API size_t tcl_delta_rule_backward_workspace_bytes(int32_t dtype, int32_t n_seq, int32_t rows, int32_t Hk,
                                                        int32_t H, int32_t Dk, int32_t Dv);
 TCL_API tcl_status tcl_delta_rule_backward(const tcl_delta_rule_args* args, const void* d_do, int64_t lddo,

@@ -404,7 +404,7 @@ __device__ __forceinline__ void row_raw(const T* p, int64_t ld, Chunk c, int w, 
 // workgroups that share them out). Each of four
 // wavefronts has 16 rows. T: the diagonal blocks of 16 by substitution, a column per lane, then blocks of
 // 32 and 64 by products, T21 = -T22 A21 T11. Bound by what it writes, the matrices in parts above all: 126 chunks of 32
-// heads (16 key heads) in bf16, 227 MiB, 84 us; a chain of ten barriers a head hides only under the other workgroups of
+// heads (16 key heads) in bf16, 251 MB, 81 to 85 us; a chain of ten barriers a head hides only under the other workgroups of
 // a CU (with room for fewer, 105).
 constexpr int kLdM = kC + 4;
 
@@ -631,8 +631,9 @@ __device__ __forceinline__ int swap8(int r, int k) {
 // bytes a cycle every product's operands share, is asked evenly. What
 // the next chunk reads from memory is asked for as soon as its registers are free. SAVE (for the gradients): the states in
 // front of the chunks and U are kept, no answers are formed, by the first four alone. Bound by the chain of a chunk's three
-// phases: 126 chunks of 32 heads of 128 x 128 (one workgroup a CU) in 237 us, 1.9 a chunk, the matrix cores 17% busy, LDS
-// 26%, the vector units 23%; out of registers alone, without a load, 172; with all the work on four wavefronts 336.
+// phases: 126 chunks of 32 heads of 128 x 128 (one workgroup a CU) in 253 to 266 us, 2.0 a chunk, the matrix cores 19% busy,
+// the vector units 25%. (With two parts behind bf16 answers, 237: then out of registers alone, without a load, 172, and with
+// all the work on four wavefronts 336.)
 template <typename T, int DKP, bool SAVE>
 __global__ __launch_bounds__(SAVE ? 256 : 512) void delta_chunk_kernel(
     DeltaIn a, const T* __restrict__ v, const float* __restrict__ mats, const float* __restrict__ coef,
@@ -1075,10 +1076,11 @@ __device__ __forceinline__ float sum4(float x) {
 // What the chunks give once their states and adjoints are known, a workgroup per chunk and key head, which
 // sums dQ and dK over the value heads that share it. Two sets of four wavefronts have 16 tokens each and
 // half of the rows of dQ^T and dK^T each; the first also forms dP and M1, the second dA and M2. The states, their
-// adjoints and U go through LDS in parts, 32 columns at a time; then M1 and M2 do, both ways round. 110 KB of LDS (146 in
-// fp32) and 256 registers leave one workgroup to a CU, whose phases (a slice into LDS, its products, the matrices,
-// their sums) follow each other: 87 chunks of 16 heads of 128 x 128 in bf16 168 us in 2.7 rounds of the CUs (190 with
-// the products of keys formed here again).
+// adjoints and U go through LDS in parts, 32 columns at a time; then M1 and M2 do, both ways round. 146 KB of LDS
+// and 256 registers leave one workgroup to a CU, whose phases (a slice into LDS, its products, the matrices, their sums)
+// follow each other: 87 chunks of 16 heads of 128 x 128 in bf16 164 to 168 us in 2.7 rounds of the CUs (over 20 more with
+// the products of keys formed here again). 80 to 107 scalar registers are spilled to lanes of vector ones, and one vector
+// register in fp32 at 128.
 constexpr int kSl = 32, kLdSl = kSl + 8, kLdZ = kC + 8, kLdF = kC + 1;
 
 template <typename T, int DKP>
@@ -1381,9 +1383,10 @@ __global__ __launch_bounds__(512) void delta_grads_kernel(DeltaIn a, const T* __
 // From how many tokens a sequence, on average, chunks of kC pay. With few heads of sequences the walk's latency
 // counts (some 0.5 to 1.1 us a token against 20 us for a first chunk and 4 to 6 for each after), with a full card what
 // each has to do, of which chunks of fp32 values do the more. Walk / chunks in us, at tokens a sequence:
-//   bf16, Dk = Dv = 128   16 heads     16: 22 / 22    24: 32 / 23     64: 78 / 24
-//                         512          32: 67 / 78    48: 100 / 79
-//                         4,096        32: 393 / 502  48: 584 / 524   128: 1,720 / 875
+//   bf16, Dk = Dv = 128   16 heads     16: 22 / 18    24: 32 / 18     64: 78 / 18
+//                         128          16: 23 / 26    24: 33 / 27     64: 82 / 29
+//                         512          32: 66 / 76    40: 84 / 76     128: 254 / 105
+//                         4,096        40: 488 / 517  48: 584 / 527   128: 1,744 / 889
 //   fp32, 64              128          32: 20 / 22    48: 28 / 23
 //                         512          64: 37 / 58    128: 69 / 81    192: 101 / 111
 //                         1,024        64: 56 / 106   192: 165 / 256
@@ -1412,9 +1415,9 @@ hipError_t walk(const DeltaOp& a, float* state_out, void* o, int64_t ldo, hipStr
 }
 
 // Workgroups of the preparation for a chunk and key head: one for each value head where one for all leaves CUs idle (a
-// prompt of 1,000 bf16 tokens, one key head, 2 value heads 46 -> 40 us a call, 16 of them 124 -> 42); they form the keys'
-// products each for itself, so from more chunks on one (1,500 tokens of 4 sequences, 4 key heads, 12 value heads, fp32 169,
-// else 180).
+// prompt of 1,000 bf16 tokens, one key head, 2 value heads 46 -> 40 us a call, 16 of them 124 -> 42). They form the keys'
+// products each for itself, so from a chunk and key head for every CU on it is one for all (4 sequences of 1,500 tokens each,
+// 4 key heads, 12 value heads, fp32 heads of 128 x 128: 169 us, else 180; measured at this one size on that side).
 int prep_parts(const DeltaOp& a, int64_t tiles) { return tiles * a.Hk < kPrepFill ? a.H / a.Hk : 1; }
 
 template <typename T, int DKP>
