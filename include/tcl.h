@@ -662,7 +662,8 @@ typedef struct tcl_delta_rule_grads {
  * call. d_dstate_out [n_seq, H, Dk, Dv]: the gradient of the end states (NULL: zeros). State i belongs to
  * sequence i (no slots). The workspace holds rows / 64 + n_seq chunks of 73 KiB + 8 Dk Dv + 512 Dv bytes a value head (64 x 64:
  * 137 KiB, 128 x 128: 265) and 56 to 128 KiB a key head: 4,096 sequences of 15 tokens with 8 key heads and 16 value heads of
- * 128 x 128 need 25 GB in bf16, so many short sequences are better given several calls. No sequences at all are refused (TCL_ERR_INVALID_ARG). */
+ * 128 x 128 need 25 GB in bf16, so many short sequences are better given several calls. No sequences at all are refused
+ * (TCL_ERR_INVALID_ARG). */
 TCL_API size_t tcl_delta_rule_backward_workspace_bytes(int32_t dtype, int32_t n_seq, int32_t rows, int32_t Hk,
                                                        int32_t H, int32_t Dk, int32_t Dv);
 TCL_API tcl_status tcl_delta_rule_backward(const tcl_delta_rule_args* args, const void* d_do, int64_t lddo,
@@ -673,9 +674,11 @@ TCL_API tcl_status tcl_delta_rule_backward(const tcl_delta_rule_args* args, cons
  * Layer norm over the C columns of each row, in front of a block:
  *   h = (x - mean x) / sqrt(mean (x - mean x)^2 + eps),   y = h w + b.
  * x and y are fp32 or bf16 (dtype) of any alignment, rows with a leading dimension >= C; w and b [C] fp32, NULL: ones,
- * zeros. Statistics are fp32, the variance from deviations; y is rounded to dtype once and must not
- * overlap x, w or b (refused; columns beside x's in one buffer do not). eps finite, not negative (0: a row of equal values gives NaN); C in [1, 16384], rows <= 2^30; rows == 0
- * is TCL_OK. Stream-ordered, deterministic, no allocation.
+ * zeros. Statistics are fp32, the variance from deviations (of less than 1e17, as their squares are summed); a NaN or an
+ * infinity in a row makes all of it NaN, and no other; y is rounded to dtype once and must not
+ * overlap x, w or b (refused; columns beside x's in one buffer do not). eps finite, not negative (0: a row of equal
+ * values has no result, as a rule NaN); C in [1, 16384], rows <= 2^30; rows == 0 is TCL_OK. Stream-ordered, deterministic,
+ * no allocation.
  * ------------------------------------------------------------------- */
 TCL_API tcl_status tcl_layer_norm(int32_t dtype, int32_t rows, int32_t C, const void* d_x, int64_t ldx,
                                   const float* d_w, const float* d_b, float eps, void* d_y, int64_t ldy,
@@ -683,7 +686,8 @@ TCL_API tcl_status tcl_layer_norm(int32_t dtype, int32_t rows, int32_t C, const 
 
 /* Gradients from x, w and d_dy [rows, C] (lddy); nothing is kept from the forward call. d_dx [rows, C] (lddx)
  * has x's type and must not overlap the inputs; d_dw [C] and d_db [C] (NULL: not wanted) are fp32, summed over all rows
- * and overwritten (zeros for no rows). No output may overlap another or the workspace. d_workspace: >= tcl_layer_norm_workspace_bytes bytes, 256-byte aligned. */
+ * and overwritten (zeros for no rows). No output may overlap another or the workspace. d_workspace: >=
+ * tcl_layer_norm_workspace_bytes bytes, 256-byte aligned. */
 TCL_API size_t tcl_layer_norm_workspace_bytes(int32_t dtype, int32_t rows, int32_t C);
 TCL_API tcl_status tcl_layer_norm_backward(int32_t dtype, int32_t rows, int32_t C, const void* d_x, int64_t ldx,
                                            const float* d_w, float eps, const void* d_dy, int64_t lddy, void* d_dx,
@@ -749,14 +753,14 @@ TCL_API tcl_status tcl_distill_topk(int32_t dtype, int32_t n_rows, int32_t V, co
  * d_score [n_groups, W] fp32 the beams' own. A group's K best go to d_parent (the row g W + b), d_token
  * (v) and d_out_score, all [n_groups, K]: highest first (compared in 64 bits, rounded to fp32 at the end), equal
  * scores by lower row; a row's own candidates in tcl_topk's order, by their logits, then by lower token. A row's sum of
- * exponentials is fp32, log p_b good to some 4e-7 (1e-6 for a million tokens): candidates of different rows that are closer
- * may change places. Rows of the same logits have the same sums, wherever they start. d_ended
- * [n_groups, W] int32 or NULL: a beam with an entry >= 0 has ended, and is one candidate itself, with that entry
- * as its token and its own score. A beam whose score is -inf or NaN is dead. Neither's logits are read. Masked
- * (-inf) and NaN logits, and rows with a logit of +inf, are no candidates; past the end of a group with fewer than
- * K: -1, -1 and -inf. The outputs must not overlap each other, d_score, d_ended or the workspace. logits as for
- * tcl_logprobs (rows); W and K in [1, 64], n_groups W < 2^22. d_workspace: >= tcl_beam_select_workspace_bytes bytes,
- * 256-byte aligned. n_groups == 0 is TCL_OK. */
+ * exponentials and 1 / temperature are fp32, log p_b good to some 4e-7 (1e-6 for a million tokens), and 2^-24 of the
+ * distance from the row's highest logit over the temperature: candidates of different rows that are closer may change places.
+ * Rows of the same logits have the same sums, wherever they start. d_ended [n_groups, W] int32 or NULL: a beam with an
+ * entry >= 0 has ended, and is one candidate itself, with that entry as its token and its own score. A beam whose score
+ * is -inf or NaN is dead. Neither's logits are read. Masked (-inf) and NaN logits, and rows with a logit of +inf, are
+ * no candidates; past the end of a group with fewer than K: -1, -1 and -inf. The outputs must not overlap each other,
+ * d_score, d_ended or the workspace. logits as for tcl_logprobs (rows); W and K in [1, 64], n_groups W < 2^22.
+ * d_workspace: >= tcl_beam_select_workspace_bytes bytes, 256-byte aligned. n_groups == 0 is TCL_OK. */
 TCL_API size_t tcl_beam_select_workspace_bytes(int32_t n_groups, int32_t W, int32_t V, int32_t K);
 TCL_API tcl_status tcl_beam_select(int32_t dtype, int32_t n_groups, int32_t W, int32_t V, const void* d_logits,
                                    int64_t ld, float temperature, const float* d_score, const int32_t* d_ended,

@@ -910,7 +910,7 @@ def _row_matrix(x):
 
 def layer_norm(x, w=None, b=None, eps=1e-5, out=None, stream=None):
     """Layer norm over the columns of x [rows, C] fp32 or bf16 (tcl_layer_norm); w, b [C] fp32
-    (None: ones, zeros). Returns y [rows, C]."""
+    (None: ones, zeros). Returns y [rows, C]; out: a matrix to write it to, which must not overlap x."""
     if stream is not None:
         return _under(stream, layer_norm, x, w, b, eps, out)
     import torch

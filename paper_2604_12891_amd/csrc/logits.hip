@@ -467,14 +467,15 @@ __global__ __launch_bounds__(kTB) void logprobs_join_kernel(LogitRows a, int K, 
 // A group's K best candidates (b, v) by score_b + log p_b(v), out of its rows' lists of K: each list is
 // sorted, so every round takes the best of the lists' heads. Scores are compared in 64 bits: fp32 would make
 // neighbours equal that a long search's sum of log probabilities (-100: steps of 8e-6) cannot tell
-// apart. (The sums of exponentials in them are fp32: against 64 bits their logarithms were off by up to 4e-7 for 77 to 131,073
-// entries, 8e-7 for 1,000,003. Rows of the same entries have the same: lists come from rows read from their start, 512 of
-// 131,073 bf16 entries in 52.5 us a call, 4 of 50,001 in fp32 in 16.4; by aligned vectors 48.8 and 15.7.) Equal scores (a temperature or a score beyond which the logits' differences count nothing): the lower row, and
-// in a row the order that its list has, by the logits. All scores are formed at once, as numbers that rise with them (0: none); then a wavefront runs the
-// rounds, each the largest of its lanes' heads (the high halves as a rule tell) and one lane's step on, out of LDS
-// where the lists fit: some 0.3 us. A chain of latencies: 5.8 us for 4 beams and K = 4, 9.8 for 64 groups of 8 and K = 16
-// (the rows' lists, 512 rows of 131,072 bf16 entries, 37 at the rate of 3.6 TB/s); counting how many candidates beat each
-// instead of rounds took 12 to 26.
+// apart. (The sums of exponentials in them are fp32: against 64 bits their logarithms were off by up to 4e-7 for 77
+// to 131,073 entries, 8e-7 for 1,000,003. Rows of the same entries have the same: lists come from rows read from
+// their start, 512 of 131,073 bf16 entries in 52.5 us a call, 4 of 50,001 in fp32 in 16.4; by aligned vectors 48.8
+// and 15.7.) Equal scores (a temperature or a score beyond which the logits' differences count nothing): the lower
+// row, and in a row the order that its list has, by the logits. All scores are formed at once, as numbers that rise
+// with them (0: none); then a wavefront runs the rounds, each the largest of its lanes' heads (the high halves as a
+// rule tell) and one lane's step on, out of LDS where the lists fit: some 0.3 us. A chain of latencies: 5.7 us for 4
+// beams and K = 4, 9.8 to 10.8 for 64 groups of 8 and K = 16 (the rows' lists, 512 rows of 131,072 bf16 entries, 37
+// at the rate of 3.6 TB/s); counting how many candidates beat each instead of rounds took 12 to 26.
 constexpr int kBeamLists = 1024;  // W x splits
 constexpr int kBeamKeys = 4096;   // candidates held in LDS
 
